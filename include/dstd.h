@@ -409,6 +409,104 @@ const char *dstd_error_string(int code);
 /* Library version, major*10000 + minor*100 + patch. */
 int dstd_version(void);
 
+/* ---------------------------------------------------------------------------
+ * Training and serving in 8 bits
+ *
+ * A layer's contraction w^ = W s as a product of 8-bit rows: each weight row
+ * (channel) and each row of grid weights (token: one grid point of one sample)
+ * is held as whole numbers of [-127, 127] and one fp32 scale. Training rounds
+ * the weights and the grid weights in the forward and passes the gradient
+ * straight through the rounding; the update is clipped by the norm of all
+ * gradients. (The paper trains in floating point; this is for networks that
+ * are to run with 8-bit weights.)
+ * Row strides (ld_*) are in elements. Pointers of this section need only the
+ * alignment of their element type (workspaces: 16 bytes). An empty list,
+ * no rows, no columns or no tokens are valid where stated and launch what
+ * they need, if anything.
+ * ------------------------------------------------------------------------- */
+typedef enum { DSTD_TYPE_F32 = 0, DSTD_TYPE_BF16 = 1, DSTD_TYPE_F16 = 2 } dstd_type;
+
+/* Rows to 8 bits. With a = max_k |x_rk|: scale_r = a / 127, q_rk = x_rk (127 / a)
+ * rounded to the nearest (ties to even), values_rk = q_rk scale_r, in fp32.
+ * A row of zeros has scale 0 and codes 0. A row that holds an infinity or a NaN
+ * has scale NaN and codes 0, so that every result computed from it is NaN.
+ *  x       [rows, cols] of `type`, row stride ld_x >= cols; rows, cols >= 0.
+ *  q       [rows, cols] out, row stride ld_q >= cols.
+ *  scale   [rows] out.
+ *  values  [rows, cols] fp32 out, row stride ld_values >= cols (may be NULL).
+ * The outputs must not overlap x. */
+int dstd_quantize_rows(const void *x, dstd_type type, int rows, int cols, int64_t ld_x, int8_t *q, int64_t ld_q,
+                       float *scale, float *values, int64_t ld_values, dstd_stream_t stream);
+
+/* Workspace bytes of dstd_int8_matmul for T tokens, N channels and K inputs;
+ * 0 on invalid sizes. */
+size_t dstd_int8_matmul_workspace_bytes(int T, int N, int K);
+
+/* Product of 8-bit rows with a scale for each token and channel:
+ *     out_tn = x_scale_t w_scale_n sum_k x_tk w_nk.
+ * The sum is exact (any codes, -128 among them); it is rounded to fp32, times
+ * x_scale_t, times w_scale_n, and rounded once more to a 16-bit out_type.
+ *  x [T, K], w [N, K], row strides ld_x, ld_w >= K; T, N >= 0, 0 <= K <= 131071
+ *  (K = 0 gives zeros); x_scale [T], w_scale [N].
+ *  out [T, N] of out_type, row stride ld_out >= N; overlaps no input.
+ *  workspace  dstd_int8_matmul_workspace_bytes(T, N, K) bytes, any contents;
+ *             calls that can overlap on the GPU need one each. */
+int dstd_int8_matmul(const int8_t *x, int64_t ld_x, const float *x_scale, const int8_t *w, int64_t ld_w,
+                     const float *w_scale, int T, int N, int K, void *out, dstd_type out_type, int64_t ld_out,
+                     void *workspace, size_t ws_bytes, dstd_stream_t stream);
+
+/* Workspace bytes of dstd_dense_fwd_q8; 0 on invalid arguments. */
+size_t dstd_dense_q8_workspace_bytes(int B, int N_in, int N_out, const dstd_params *p);
+
+/* dstd_dense_fwd with the contraction in 8 bits: binning, the grid weights
+ * quantised for each (sample, grid point), the 8-bit product with the weights'
+ * codes, scan/solve/select in fp32.
+ *  w_q [N_out, N_in] codes (contiguous), w_scale [N_out], as from
+ *  dstd_quantize_rows; the other arguments as in dstd_dense_fwd. M <= 128.
+ * The backward is dstd_dense_bwd with the weights' values (w_scale q). */
+int dstd_dense_fwd_q8(const float *t_in, const int8_t *w_q, const float *w_scale, int B, int N_in, int N_out,
+                      const dstd_params *p, float *t_out, void *saved, float *penalty, void *workspace,
+                      size_t ws_bytes, dstd_stream_t stream);
+
+/* Norm of many gradients, clipping by it, and the clipped update.
+ *
+ * The three calls below share a workspace of
+ * dstd_grad_norm_workspace_bytes(count, n) bytes, whose first 256 bytes are
+ * zero before its first use and are left so; calls that can overlap on the GPU
+ * need one each. count >= 1 tensors of n[i] >= 0 elements (the arrays of
+ * pointers and sizes are host memory, read during the call); type[i] is the
+ * dstd_type of gradient i. Sums are formed in a fixed order: the same call on
+ * the same tensors gives the same bits. */
+size_t dstd_grad_norm_workspace_bytes(int count, const int64_t *n);
+
+/* norm[0] = sqrt(sum over all tensors of g^2), fp32 (+inf where it passes fp32;
+ * infinite or NaN when a gradient is).
+ *  tensor_norms [count] out: each tensor's own (may be NULL). */
+int dstd_grad_norm(int count, const void *const *g, const int64_t *n, const int32_t *type, float *norm,
+                   float *tensor_norms, void *workspace, size_t ws_bytes, dstd_stream_t stream);
+
+/* out_i = c g_i with c = min(1, max_norm / norm), norm as above (norm[0] out).
+ * When the norm is not finite the gradients pass unchanged (c = 1): the caller
+ * sees it in norm. out_i has g_i's type and is g_i itself or does not overlap
+ * any gradient. max_norm > 0 (+inf: no clipping). */
+int dstd_clip_grads(int count, const void *const *g, void *const *out, const int64_t *n, const int32_t *type,
+                    double max_norm, float *norm, void *workspace, size_t ws_bytes, dstd_stream_t stream);
+
+/* One AdamW step of every tensor with its gradient clipped as above; the
+ * gradients are only read. With t the count of updates after this one:
+ *     m = beta1 m + (1 - beta1) c g,  v = beta2 v + (1 - beta2) (c g)^2,
+ *     w = w (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps).
+ * When the norm is not finite (a gradient is infinite or NaN), w, m, v and the
+ * count stay as they were. w, m, v are fp32; g of type[i].
+ *  step    device int32[1]: updates done so far, advanced by the call.
+ *  lr_dev  device float replacing lr (may be NULL).
+ *  norm    device float[1] out.
+ * The hyperparameters are double: 1 - beta2 is taken before rounding to fp32. */
+int dstd_adamw_clip(int count, float *const *w, const void *const *g, float *const *m, float *const *v,
+                    const int64_t *n, const int32_t *type, double lr, double beta1, double beta2, double eps,
+                    double weight_decay, double max_norm, int32_t *step, const float *lr_dev, float *norm,
+                    void *workspace, size_t ws_bytes, dstd_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -90,12 +90,12 @@ inline int cu(cudaError_t e) { return e == cudaSuccess ? DSTD_OK : DSTD_E_CUDA; 
 enum Kind {
     KK_PREP = 0, KK_BIN, KK_BIN_T, KK_GEMM_FWD, KK_SCAN, KK_DWHAT, KK_GEMM_DS, KK_GT, KK_GEMM_DW, KK_REDUCE,
     KK_LOSS, KK_ADAMW, KK_BIN_PUB, KK_WHAT_PUB, KK_SELFTEST, KK_NARROW_FWD, KK_NARROW_BWD, KK_EXACT_FWD, KK_SKIP,
-    KK_EXACT_BWD, KK_COUNT
+    KK_EXACT_BWD, KK_QUANTIZE, KK_INT8, KK_CLIP, KK_COUNT
 };
 const char *const kKindNames[KK_COUNT] = {
     "prep_weights", "binning", "binning_T", "gemm_fwd_scan", "scan_solve", "dwhat", "gemm_dS_gradt",
     "gradt_gather", "gemm_dW", "dw_reduce", "loss", "adamw", "binning_public", "what_public", "selftest", "narrow_fwd",
-    "narrow_bwd", "exact_fwd", "skip_channels", "exact_bwd"};
+    "narrow_bwd", "exact_fwd", "skip_channels", "exact_bwd", "quantize_rows", "int8_matmul", "clip"};
 
 struct Timing {
     std::mutex mu;
@@ -1652,6 +1652,204 @@ int dstd_conv_set_operand_policy(int policy) {
     const int prev = g_conv_operand_policy;
     g_conv_operand_policy = policy;
     return prev;
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// Training and serving in 8 bits: rows, products, the clipped update.
+// ---------------------------------------------------------------------------
+namespace {
+
+size_t type_bytes(dstd_type t) { return t == DSTD_TYPE_F32 ? 4 : 2; }
+bool type_ok(int t) { return t == DSTD_TYPE_F32 || t == DSTD_TYPE_BF16 || t == DSTD_TYPE_F16; }
+bool aligned_to(const void *p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
+constexpr int64_t kMaxElements = int64_t(1) << 46;  // of a tensor list
+
+// what the three calls on tensor lists check alike
+int check_tensors(int count, const void *const *g, const int64_t *n, const int32_t *type, float *norm, void *workspace,
+                  size_t ws_bytes) {
+    if (count < 1 || !g || !n || !type || !norm || !workspace) return DSTD_E_INVALID;
+    if (!aligned_to(norm, 4) || !aligned16(workspace)) return DSTD_E_INVALID;
+    int64_t total = 0;
+    for (int i = 0; i < count; ++i) {
+        if (n[i] < 0 || !type_ok(type[i])) return DSTD_E_INVALID;
+        if (n[i] > 0 && (!g[i] || !aligned_to(g[i], type_bytes((dstd_type)type[i])))) return DSTD_E_INVALID;
+        if (n[i] > kMaxElements || (total += n[i]) > kMaxElements) return DSTD_E_UNSUPPORTED;
+    }
+    if (ws_bytes < clip_workspace_bytes(count, n)) return DSTD_E_WORKSPACE;
+    return DSTD_OK;
+}
+
+// layout of the 8-bit layer forward: grid weights, their codes and scales, w^
+// (D[i][(b, m)], as the scan reads it), the weights' row sums, the product's scratch
+struct Q8Ws {
+    float *s32 = nullptr, *scale = nullptr, *D = nullptr, *rowsum = nullptr;
+    int8_t *q = nullptr;
+    char *product = nullptr;
+    size_t bytes = 0;
+    int ld = 0;
+    long long ld_q = 0;
+};
+Q8Ws q8_layout(void *base, int B, int N_in, int N_out, int Mp) {
+    Q8Ws w;
+    Bump b(base);
+    const long long T = (long long)B * Mp;
+    w.ld = pad8(N_in);
+    w.ld_q = ((long long)N_in + 15) / 16 * 16;
+    w.rowsum = b.take<float>(N_out);
+    w.scale = b.take<float>((size_t)T);
+    w.s32 = b.take<float>((size_t)T * w.ld);
+    w.q = b.take<int8_t>((size_t)T * w.ld_q);
+    w.D = b.take<float>((size_t)T * N_out);
+    w.product = b.take<char>(q8_workspace_bytes((int)T, N_out, N_in));
+    w.bytes = b.off;
+    return w;
+}
+int check_q8_sizes(int B, int N_in, int N_out, const dstd_params *p) {
+    TRY(check_sizes(B, N_in, N_out));
+    TRY(check_params(p));
+    if (padded_M(p->M) > 128 || N_in > kQ8MaxK) return DSTD_E_UNSUPPORTED;
+    return DSTD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int dstd_quantize_rows(const void *x, dstd_type type, int rows, int cols, int64_t ld_x, int8_t *q, int64_t ld_q,
+                       float *scale, float *values, int64_t ld_values, dstd_stream_t stream) {
+    if (rows < 0 || cols < 0 || !type_ok(type)) return DSTD_E_INVALID;
+    if (rows > 0 && (!scale || !aligned_to(scale, 4))) return DSTD_E_INVALID;
+    if (rows > 0 && cols > 0) {
+        if (!x || !q || !aligned_to(x, type_bytes(type)) || ld_x < cols || ld_q < cols) return DSTD_E_INVALID;
+        if (values && (!aligned_to(values, 4) || ld_values < cols)) return DSTD_E_INVALID;
+    }
+    TRY(device_ok());
+    Timed tm(KK_QUANTIZE, (cudaStream_t)stream);
+    return cu(launch_quantize_rows(x, type, rows, cols, ld_x, q, ld_q, scale, values, ld_values,
+                                   (cudaStream_t)stream));
+}
+
+size_t dstd_int8_matmul_workspace_bytes(int T, int N, int K) {
+    if (T < 0 || N < 0 || K < 0 || K > kQ8MaxK) return 0;
+    return q8_workspace_bytes(T, N, K);
+}
+
+int dstd_int8_matmul(const int8_t *x, int64_t ld_x, const float *x_scale, const int8_t *w, int64_t ld_w,
+                     const float *w_scale, int T, int N, int K, void *out, dstd_type out_type, int64_t ld_out,
+                     void *workspace, size_t ws_bytes, dstd_stream_t stream) {
+    if (T < 0 || N < 0 || K < 0 || !type_ok(out_type)) return DSTD_E_INVALID;
+    if (K > kQ8MaxK) return DSTD_E_UNSUPPORTED;
+    if (T > 0 && N > 0) {
+        if (!x_scale || !w_scale || !out || !aligned_to(x_scale, 4) || !aligned_to(w_scale, 4) ||
+            !aligned_to(out, type_bytes(out_type)) || ld_out < N)
+            return DSTD_E_INVALID;
+        if (K > 0 && (!x || !w || ld_x < K || ld_w < K)) return DSTD_E_INVALID;
+        if (!workspace || !aligned16(workspace)) return DSTD_E_INVALID;
+        if (ws_bytes < q8_workspace_bytes(T, N, K)) return DSTD_E_WORKSPACE;
+    }
+    TRY(device_ok());
+    Timed tm(KK_INT8, (cudaStream_t)stream);
+    const Q8Args a{x, w, ld_x, ld_w, x_scale, w_scale, T, N, K, Q8Out{out, out_type, ld_out, 1}};
+    return cu(launch_q8_product(a, workspace, (cudaStream_t)stream));
+}
+
+size_t dstd_dense_q8_workspace_bytes(int B, int N_in, int N_out, const dstd_params *p) {
+    if (check_q8_sizes(B, N_in, N_out, p) != DSTD_OK) return 0;
+    return q8_layout(nullptr, B, N_in, N_out, padded_M(p->M)).bytes;
+}
+
+int dstd_dense_fwd_q8(const float *t_in, const int8_t *w_q, const float *w_scale, int B, int N_in, int N_out,
+                      const dstd_params *p, float *t_out, void *saved, float *penalty, void *workspace,
+                      size_t ws_bytes, dstd_stream_t stream) {
+    if (!t_in || !w_q || !w_scale || !t_out || !saved || !workspace) return DSTD_E_INVALID;
+    TRY(check_q8_sizes(B, N_in, N_out, p));
+    if (!aligned16(t_in) || !aligned16(w_q) || !aligned_to(w_scale, 4) || !aligned16(workspace) || !aligned16(saved))
+        return DSTD_E_INVALID;
+    const int Mp = padded_M(p->M), T = B * Mp;
+    Q8Ws ws = q8_layout(workspace, B, N_in, N_out, Mp);
+    if (ws_bytes < ws.bytes) return DSTD_E_WORKSPACE;
+    TRY(device_ok());
+    LifConst c = make_const(*p, Mp);
+    cudaStream_t st = (cudaStream_t)stream;
+    Saved sv = saved_view(saved, B, N_out);
+    if (penalty) TRY(cu(cudaMemsetAsync(penalty, 0, 4 * sizeof(float), st)));
+    {
+        Timed tm(KK_BIN, st);
+        TRY(cu(launch_binning(t_in, B, N_in, c, OpKind::F32, false, ws.s32, nullptr, ws.ld, st)));
+    }
+    {
+        Timed tm(KK_QUANTIZE, st);
+        TRY(cu(launch_quantize_rows(ws.s32, DSTD_TYPE_F32, T, N_in, ws.ld, ws.q, ws.ld_q, ws.scale, nullptr, 0, st)));
+        TRY(cu(launch_q8_rowsum(w_q, N_in, N_out, N_in, w_scale, ws.rowsum, st)));
+    }
+    {
+        Timed tm(KK_INT8, st);
+        const Q8Args a{ws.q, w_q, ws.ld_q, N_in, ws.scale, w_scale, T, N_out, N_in, Q8Out{ws.D, DSTD_TYPE_F32, 1, T}};
+        TRY(cu(launch_q8_product(a, ws.product, st)));
+    }
+    Timed tm(KK_SCAN, st);
+    return cu(launch_scan_solve(ws.D, Mp, T, 1, B, N_out, c, nullptr, ws.rowsum, t_out, sv.q, sv.s, sv.vdot, penalty,
+                                st));
+}
+
+size_t dstd_grad_norm_workspace_bytes(int count, const int64_t *n) {
+    if (count < 1 || !n) return 0;
+    int64_t total = 0;
+    for (int i = 0; i < count; ++i)
+        if (n[i] < 0 || n[i] > kMaxElements || (total += n[i]) > kMaxElements) return 0;
+    return clip_workspace_bytes(count, n);
+}
+
+int dstd_grad_norm(int count, const void *const *g, const int64_t *n, const int32_t *type, float *norm,
+                   float *tensor_norms, void *workspace, size_t ws_bytes, dstd_stream_t stream) {
+    TRY(check_tensors(count, g, n, type, norm, workspace, ws_bytes));
+    if (tensor_norms && !aligned_to(tensor_norms, 4)) return DSTD_E_INVALID;
+    TRY(device_ok());
+    Timed tm(KK_CLIP, (cudaStream_t)stream);
+    const ClipTensors t{count, g, nullptr, nullptr, nullptr, n, type};
+    ClipHyper h{};
+    h.max_norm = INFINITY;
+    return cu(launch_clip(t, ClipOp::Norm, h, norm, tensor_norms, workspace, (cudaStream_t)stream));
+}
+
+int dstd_clip_grads(int count, const void *const *g, void *const *out, const int64_t *n, const int32_t *type,
+                    double max_norm, float *norm, void *workspace, size_t ws_bytes, dstd_stream_t stream) {
+    TRY(check_tensors(count, g, n, type, norm, workspace, ws_bytes));
+    if (!out || !(max_norm > 0.0)) return DSTD_E_INVALID;
+    for (int i = 0; i < count; ++i)
+        if (n[i] > 0 && (!out[i] || !aligned_to(out[i], type_bytes((dstd_type)type[i])))) return DSTD_E_INVALID;
+    TRY(device_ok());
+    Timed tm(KK_CLIP, (cudaStream_t)stream);
+    const ClipTensors t{count, g, out, nullptr, nullptr, n, type};
+    ClipHyper h{};
+    h.max_norm = max_norm;
+    TRY(cu(launch_clip(t, ClipOp::Norm, h, norm, nullptr, workspace, (cudaStream_t)stream)));
+    return cu(launch_clip(t, ClipOp::Scale, h, norm, nullptr, workspace, (cudaStream_t)stream));
+}
+
+int dstd_adamw_clip(int count, float *const *w, const void *const *g, float *const *m, float *const *v,
+                    const int64_t *n, const int32_t *type, double lr, double beta1, double beta2, double eps,
+                    double weight_decay, double max_norm, int32_t *step, const float *lr_dev, float *norm,
+                    void *workspace, size_t ws_bytes, dstd_stream_t stream) {
+    TRY(check_tensors(count, g, n, type, norm, workspace, ws_bytes));
+    if (!w || !m || !v || !step || !aligned_to(step, 4) || (lr_dev && !aligned_to(lr_dev, 4))) return DSTD_E_INVALID;
+    if (!(lr >= 0.0) || !isfinite((float)lr) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) ||
+        !((float)eps > 0.0f) || !isfinite((float)eps) || !isfinite((float)weight_decay) ||
+        !(max_norm > 0.0))
+        return DSTD_E_INVALID;
+    for (int i = 0; i < count; ++i)
+        if (n[i] > 0 && (!w[i] || !m[i] || !v[i] || !aligned_to(w[i], 4) || !aligned_to(m[i], 4) ||
+                         !aligned_to(v[i], 4)))
+            return DSTD_E_INVALID;
+    TRY(device_ok());
+    Timed tm(KK_CLIP, (cudaStream_t)stream);
+    const ClipTensors t{count, g, reinterpret_cast<void *const *>(w), m, v, n, type};
+    const ClipHyper h{max_norm, lr, beta1, beta2, eps, weight_decay, step, lr_dev};
+    TRY(cu(launch_clip(t, ClipOp::Norm, h, norm, nullptr, workspace, (cudaStream_t)stream)));
+    return cu(launch_clip(t, ClipOp::Adamw, h, norm, nullptr, workspace, (cudaStream_t)stream));
 }
 
 }  // extern "C"

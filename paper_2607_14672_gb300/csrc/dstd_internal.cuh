@@ -668,4 +668,77 @@ struct AdamMultiArgs {
 };
 cudaError_t launch_adamw_multi(const AdamMultiArgs &args, cudaStream_t st);
 
+// Norm of many gradients, clipping and the clipped AdamW update (dstd_clip.cu).
+struct ClipTensors {
+    int count;
+    const void *const *g;
+    void *const *out;  // clipped copies, or the weights of the update
+    float *const *m;
+    float *const *v;
+    const int64_t *n;
+    const int32_t *type;  // dstd_type of each g (and clipped copy)
+};
+struct ClipHyper {
+    double max_norm, lr, b1, b2, eps, wd;
+    int32_t *step;        // device: updates done so far, or null
+    const float *lr_dev;  // device learning rate, or null for lr
+};
+struct ClipSeg {
+    const void *g;
+    void *out;
+    float *m, *v;
+    long long n;
+    unsigned first;  // number of the tensor's first chunk
+    int type;
+};
+struct ClipResult {
+    double sum;
+    float coef;  // min(1, max_norm / norm); 1 when the norm is not finite
+    int skip;    // 1 when the norm is not finite
+};
+// tensors of one launch (a kernel's arguments hold them); longer lists take several
+constexpr int kClipFewTensors = 32, kClipMaxTensors = 512;
+template <int CAP>
+struct ClipArgs {
+    ClipSeg seg[CAP];
+    int count;
+    unsigned chunks;
+    long long chunk;  // elements of a chunk
+    int launch, last_launch;
+    unsigned *ticket;  // 0 between calls
+    ClipResult *result;
+    double *partial;  // one sum of squares per chunk of the launch
+    float *norm, *norm_each;
+    double max_norm;
+    float lr, b1, b2, one_b1, one_b2, ln_b1, ln_b2, eps, wd;
+    int32_t *step;
+    const float *lr_dev;
+};
+enum class ClipOp { Norm, Scale, Adamw };
+size_t clip_workspace_bytes(int count, const int64_t *n);
+cudaError_t launch_clip(const ClipTensors &t, ClipOp op, const ClipHyper &h, float *norm, float *norm_each,
+                        void *workspace, cudaStream_t st);
+
+// 8-bit rows and their products (dstd_q8.cu).
+cudaError_t launch_quantize_rows(const void *x, dstd_type type, int rows, int cols, long long ld_x, int8_t *q,
+                                 long long ld_q, float *scale, float *values, long long ld_v, cudaStream_t st);
+cudaError_t launch_q8_rowsum(const int8_t *w, long long ld, int N, int K, const float *scale, float *rowsum,
+                             cudaStream_t st);
+// y at p[t * ld_t + n * ld_n]
+struct Q8Out {
+    void *p;
+    dstd_type type;
+    long long ld_t, ld_n;
+};
+struct Q8Args {
+    const int8_t *x, *w;  // [T, K] and [N, K] rows
+    long long ld_x, ld_w;
+    const float *x_scale, *w_scale;
+    int T, N, K;
+    Q8Out out;
+};
+constexpr int kQ8MaxK = 131071;  // (2^31 - 1) / 128^2: no 32-bit sum of products overflows
+size_t q8_workspace_bytes(int T, int N, int K);
+cudaError_t launch_q8_product(const Q8Args &a, void *workspace, cudaStream_t st);
+
 }  // namespace dstd

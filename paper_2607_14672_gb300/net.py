@@ -24,12 +24,44 @@ def narrow_layer(n_in, n_out, M, math_mode):
     return smem <= 200 * 1024
 
 
-class DenseNet:
-    """A stack of dense DSTD layers (configs.py layer dicts) on one GPU."""
+class Clipped:
+    """The optimiser's buffers of a network and its clipped AdamW step: one
+    norm over the gradients of all layers, then every layer's update."""
 
-    def __init__(self, cfg, math_mode="x3", batch=None, device="cuda", with_adamw=False):
+    def clip_setup(self):
+        self.clip_workspace = torch.zeros(dstd.grad_norm_workspace_bytes(self.gW), dtype=torch.uint8,
+                                          device=self.device)
+        # of the last clipped step, before clipping
+        self.grad_norm = torch.zeros(1, dtype=torch.float32, device=self.device)
+
+    def optimizer(self, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, stream=None, max_norm=None):
+        """AdamW; with max_norm on gradients clipped to that global norm
+        (a step whose norm is not finite changes no weight)."""
+        if max_norm is None:
+            dstd.adamw_multi(self.W, self.gW, self.m, self.v, lr, betas[0], betas[1], eps, weight_decay,
+                             self.adam_state, None, stream)
+        else:
+            dstd.adamw_clip(self.W, self.gW, self.m, self.v, lr, betas[0], betas[1], eps, weight_decay,
+                            self.adam_state, max_norm, self.grad_norm, self.clip_workspace, stream=stream)
+
+
+class DenseNet(Clipped):
+    """A stack of dense DSTD layers (configs.py layer dicts) on one GPU.
+
+    math_mode "q8" trains for 8-bit weights: every forward quantises the
+    weights by rows and runs the layers' contractions on 8-bit codes; the
+    backward (three-product mode) runs at the values the codes stand for, and
+    the gradient passes straight through the rounding to the fp32 weights.
+    ``serve`` is the forward alone on the codes of the last ``quantize``.
+    max_norm: clip the AdamW step's gradients to this global norm.
+    """
+
+    def __init__(self, cfg, math_mode="x3", batch=None, device="cuda", with_adamw=False, max_norm=None):
         self.cfg = cfg
-        self.math = math_mode
+        self.q8 = math_mode == "q8"
+        self.math = "x3" if self.q8 else math_mode
+        self.max_norm = max_norm
+        math_mode = self.math
         self.B = int(batch or cfg["batch"])
         self.layers = [dict(L) for L in cfg["layers"]]
         self.loss_kind = cfg.get("loss", "sum_t")
@@ -48,6 +80,13 @@ class DenseNet:
         self.gW = [torch.empty_like(w) for w in self.W]
         ws = max(dstd.dense_workspace_bytes(B, self.sizes[l], self.sizes[l + 1], self.p[l], math_mode)
                  for l in range(len(self.W)))
+        if self.q8:
+            need = [dstd.dense_q8_workspace_bytes(B, self.sizes[l], self.sizes[l + 1], self.p[l])
+                    for l in range(len(self.W))]
+            ws = 0 if ws == 0 or 0 in need else max(ws, *need)
+            self.Wq = [torch.empty_like(w, dtype=torch.int8) for w in self.W]
+            self.w_scale = [torch.empty(w.shape[0], dtype=torch.float32, device=dev) for w in self.W]
+            self.Wv = [torch.empty_like(w) for w in self.W]
         if ws == 0:
             raise ValueError("unsupported layer sizes or constants for the library")
         self.workspace = torch.empty(ws, dtype=torch.uint8, device=dev)
@@ -60,6 +99,7 @@ class DenseNet:
             self.v = [torch.zeros_like(w) for w in self.W]
             # (updates done, kernel scratch): advanced on the device by each AdamW launch
             self.adam_state = torch.zeros(2, dtype=torch.int32, device=dev)
+            self.clip_setup()
 
     # -- inputs -----------------------------------------------------------
     def set_offsets(self, offsets):
@@ -76,7 +116,22 @@ class DenseNet:
     def layer_input(self, l):
         return self.t_in if l == 0 else self.t[l - 1]
 
+    def quantize(self, stream=None):
+        """8-bit codes, row scales and values of the present weights."""
+        for w, q, scale, v in zip(self.W, self.Wq, self.w_scale, self.Wv):
+            dstd.quantize_rows(w, q, scale, v, stream)
+
+    def serve(self, stream=None):
+        """The forward on the 8-bit codes as they are (no weight is read in fp32)."""
+        for l in range(len(self.W)):
+            dstd.dense_fwd_q8(self.layer_input(l), self.Wq[l], self.w_scale[l], self.p[l], self.t[l], self.saved[l],
+                              self.penalty[l], self.workspace, stream)
+
     def forward(self, stream=None):
+        if self.q8:
+            self.quantize(stream)
+            self.serve(stream)
+            return
         for l in range(len(self.W)):
             dstd.dense_fwd(self.layer_input(l), self.W[l], self.p[l], self.math, self.t[l], self.saved[l],
                            self.penalty[l], self.workspace, stream)
@@ -91,7 +146,7 @@ class DenseNet:
     def forward_loss(self, stream=None):
         """forward, then the loss; with the CE loss the output layer and the
         loss are one library call (one kernel when the layer has few outputs)."""
-        if self.loss_kind != "ce":
+        if self.loss_kind != "ce" or self.q8:
             self.forward(stream)
             self.loss_grad(stream)
             return
@@ -106,19 +161,15 @@ class DenseNet:
     def backward(self, stream=None):
         for l in range(len(self.W) - 1, -1, -1):
             g_in = self.g[l - 1] if l > 0 else None
-            dstd.dense_bwd(self.layer_input(l), self.W[l], self.t[l], self.saved[l], self.g[l], self.p[l],
+            dstd.dense_bwd(self.layer_input(l), self.Wv[l] if self.q8 else self.W[l], self.t[l], self.saved[l], self.g[l], self.p[l],
                            self.math, g_in, self.gW[l], self.workspace, stream)
-
-    def optimizer(self, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, stream=None):
-        dstd.adamw_multi(self.W, self.gW, self.m, self.v, lr, betas[0], betas[1], eps, weight_decay,
-                         self.adam_state, None, stream)
 
     def step(self, stream=None):
         """One training step: forward, loss, backward (and AdamW if enabled)."""
         self.forward_loss(stream)
         self.backward(stream)
         if self.with_adamw:
-            self.optimizer(stream=stream)
+            self.optimizer(stream=stream, max_norm=self.max_norm)
 
     def objective(self):
         """Eq. cost_function on the last batch: loss + T + gamma_Q Q (device scalar)."""
@@ -128,6 +179,8 @@ class DenseNet:
         """Kernels the library launches per ``step`` (memsets not counted)."""
         tc = self.math != "f32"
         L = len(self.W)
+        if self.q8:
+            raise NotImplementedError("launches_per_step counts the f32, x3 and bf16 modes")
         fused_loss = self.loss_kind == "ce" and narrow_layer(self.sizes[-2], self.sizes[-1], self.layers[-1]["M"],
                                                              self.math)
         n = 0 if fused_loss else 1                # loss (inside the output layer's kernel when fused)
@@ -145,18 +198,20 @@ class DenseNet:
         return n
 
 
-class ConvNet:
+class ConvNet(Clipped):
     """A stack of conv DSTD layers and a dense readout (configs 4 and 5) on one GPU.
 
     Spike tensors are NHWC ([B, H, W, C]); filters are kept as [C_out, k, k,
     C_in]. The layer dicts hold oracle-layout weights ([C_out, C_in, k, k]
     filters; the readout's columns in (C, H, W) order), which the constructor
     permutes once, so both sides compute the same network. T and Q of a conv
-    layer are normalised by B Ho Wo (App. C.1).
+    layer are normalised by B Ho Wo (App. C.1). max_norm: clip the AdamW step's
+    gradients to this global norm.
     """
 
-    def __init__(self, cfg, math_mode=None, batch=None, device="cuda", with_adamw=True):
+    def __init__(self, cfg, math_mode=None, batch=None, device="cuda", with_adamw=True, max_norm=None):
         self.cfg = cfg
+        self.max_norm = max_norm
         self.math = math_mode or cfg.get("math", "bf16")
         self.B = B = int(batch or cfg["batch"])
         self.layers = [dict(L) for L in cfg["layers"]]
@@ -223,6 +278,7 @@ class ConvNet:
             self.v = [torch.zeros_like(w) for w in self.W]
             # (updates done, kernel scratch): advanced on the device by each AdamW launch
             self.adam_state = torch.zeros(2, dtype=torch.int32, device=dev)
+            self.clip_setup()
 
     def set_offsets(self, offsets):
         for p, L, o in zip(self.p, self.layers, offsets):
@@ -290,17 +346,13 @@ class ConvNet:
                 if sm is not None and sm[0] == l - 1 and l > 0:
                     dstd.split_channels(sm[3], sm[4], g_a=self.g[l - 1], accumulate_a=True, stream=stream)
 
-    def optimizer(self, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, stream=None):
-        dstd.adamw_multi(self.W, self.gW, self.m, self.v, lr, betas[0], betas[1], eps, weight_decay,
-                         self.adam_state, None, stream)
-
     def step(self, stream=None):
         """One training step: forward, loss, backward, AdamW."""
         self.forward(stream)
         self.loss_grad(stream)
         self.backward(stream)
         if self.with_adamw:
-            self.optimizer(stream=stream)
+            self.optimizer(stream=stream, max_norm=self.max_norm)
 
     def objective(self):
         return self.loss[0] + self.penalty[:, 0].sum() + self.penalty[:, 1].sum()
