@@ -1634,10 +1634,11 @@ int dstd_dense_fwd_noalloc(const float *t_in, const float *W, int B, int N_in, i
 
 int dstd_device_status(int clear) {
     if (cudaDeviceSynchronize() != cudaSuccess) return DSTD_E_CUDA;
-    unsigned int s = 0, s2 = 0;
+    unsigned int s = 0, s2 = 0, s3 = 0;
     if (status_read(&s, clear) != cudaSuccess) return DSTD_E_CUDA;
     if (conv_status_read(&s2, clear) != cudaSuccess) return DSTD_E_CUDA;
-    return ((s | s2) & STATUS_TIMEOUT) ? DSTD_E_TIMEOUT : DSTD_OK;
+    if (q8_status_read(&s3, clear) != cudaSuccess) return DSTD_E_CUDA;
+    return ((s | s2 | s3) & STATUS_TIMEOUT) ? DSTD_E_TIMEOUT : DSTD_OK;
 }
 
 int dstd_conv_set_chunk_images(int max_images) {

@@ -412,6 +412,7 @@ __device__ __forceinline__ void finish_neuron(const LifConst &c, const ScanState
 // ---------------------------------------------------------------------------
 constexpr unsigned int STATUS_TIMEOUT = 1u;
 cudaError_t status_read(unsigned int *out, int clear);
+void *tensor_map_encoder();  // the driver's cuTensorMapEncodeTiled, or null
 cudaError_t launch_wait_selftest(unsigned long long limit_ns, cudaStream_t st);
 
 // ---------------------------------------------------------------------------
@@ -739,6 +740,7 @@ struct Q8Args {
 };
 constexpr int kQ8MaxK = 131071;  // (2^31 - 1) / 128^2: no 32-bit sum of products overflows
 size_t q8_workspace_bytes(int T, int N, int K);
+cudaError_t q8_status_read(unsigned int *out, int clear);
 cudaError_t launch_q8_product(const Q8Args &a, void *workspace, cudaStream_t st);
 
 }  // namespace dstd

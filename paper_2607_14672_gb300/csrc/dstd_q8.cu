@@ -1,8 +1,9 @@
 // 8-bit rows and their products: the row quantiser and
 // y_tn = sx_t sw_n sum_k x_tk w_nk with the sum exact in whole numbers.
 #include "dstd_internal.cuh"
+#include "dstd_tc_ptx.cuh"
 
-#include <limits.h>
+#include <algorithm>
 
 namespace dstd {
 
@@ -153,17 +154,528 @@ __global__ void __launch_bounds__(256) k_q8_dot(Q8Args a, bool aligned) {
         }
 }
 
+// ---------------------------------------------------------------------------
+// Product on tensor cores. sm_103a has no fast 8-bit integer rate, but a code
+// is exact in fp16 and so is a product of two in fp32, so the 16-bit tensor
+// cores give the whole-number sum as long as it stays within 2^24, which 1024
+// products of at most 2^14 do. Computed transposed, D[n, t]: the weights are
+// the M operand. They stay 8 bits wide until they are in the SM (TMA tiles of
+// 128 rows x 128 codes); four warps turn them into fp16 pairs in TMEM, from
+// where the tensor core reads them. The tokens, which every tile row shares,
+// are turned into fp16 once per call and read through TMA.
+// A pair of SMs works on 256 channels x NT tokens: each holds 128 channels and
+// half of the tokens' operand. Two accumulators of NT columns alternate every
+// 1024 codes of K; eight epilogue warps take the full one into 32-bit integers
+// in registers while the other fills.
+// With few tiles K is split among pairs: each writes its integer sums to the
+// workspace, and the last one to finish a part (a ticket counts them) adds the
+// others' and stores. Integer sums do not depend on the order.
+// ---------------------------------------------------------------------------
+__device__ unsigned int g_status_q8 = 0;
+
+cudaError_t q8_status_read(unsigned int *out, int clear) {
+    cudaError_t e = cudaMemcpyFromSymbol(out, g_status_q8, sizeof(unsigned int));
+    if (e != cudaSuccess || !clear) return e;
+    unsigned int z = 0;
+    return cudaMemcpyToSymbol(g_status_q8, &z, sizeof(z));
+}
+
+namespace {
+using namespace tc;
+
+constexpr int KB = 128;          // codes of K per stage
+constexpr int FOLD = 1024 / KB;  // stages per accumulator
+constexpr int W_BYTES = 128 * KB;
+constexpr int CONV_WARPS = 4, EPI_WARPS = 8, TC_THREADS = 32 * (CONV_WARPS + EPI_WARPS + 2);
+
+template <int NT>
+struct Q8Cfg {
+    static constexpr int X_BYTES = NT / 2 * 128;  // 64 fp16 of K for this SM's half of the tokens
+    static constexpr int STAGE = W_BYTES + 2 * X_BYTES;
+    static constexpr int STAGES = 200 * 1024 / STAGE > 8 ? 8 : 200 * 1024 / STAGE;
+    static constexpr int SMEM = STAGES * STAGE + 1024 + 512;
+    static constexpr int A_STAGES = (512 - 2 * NT) / 32 > 4 ? 4 : (512 - 2 * NT) / 32;  // of 64 codes, 32 columns each
+    static constexpr int A_COL = 2 * NT;
+    static constexpr int COLS = NT / 2;                   // columns of one epilogue warp
+    static constexpr int CH = COLS == 32 || COLS == 64 ? 32 : 16;  // columns per TMEM read
+};
+
+struct Q8Plan {
+    int nt, splits;
+    int tiles_n, tiles_t, blocks, per;  // K blocks of 128, and of one split
+};
+
+struct Q8Tc {
+    int T, N, K, tiles_n, tiles_t, splits, blocks, per;
+    const float *x_scale, *w_scale;
+    Q8Out out;
+    int *partial;      // [item][16 warps][COLS][32]
+    unsigned *ticket;  // [tile][16 warps], zeroed before the launch
+};
+
+// tiles are taken in groups of 8 token tiles, so that the pairs at work at one
+// time share both operands in L2
+__device__ __forceinline__ void tile_of(int i, int tiles_n, int tiles_t, int &tn, int &tt) {
+    const int per_group = 8 * tiles_n;
+    const int group = i / per_group, r = i - group * per_group;
+    const int left = tiles_t - group * 8, wide = left < 8 ? left : 8;
+    tn = r / wide;
+    tt = group * 8 + r - tn * wide;
+}
+
+// four codes (one word) to two fp16 pairs: 1024 + (code + 128) as fp16 bits
+// (0x6400 | byte), minus 1152
+__device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t &lo, uint32_t &hi) {
+    const uint32_t u = w ^ 0x80808080u;
+    const __half2 off = __half2half2(__ushort_as_half(0x6480));
+    uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
+    const __half2 x = __hsub2(*reinterpret_cast<__half2 *>(&a), off), y = __hsub2(*reinterpret_cast<__half2 *>(&b), off);
+    lo = *reinterpret_cast<const uint32_t *>(&x);
+    hi = *reinterpret_cast<const uint32_t *>(&y);
+}
+
+template <int CH>
+__device__ __forceinline__ void tmem_ld(uint32_t addr, float (&v)[CH]) {
+    if constexpr (CH == 32) tmem_ld32(addr, v);
+    else tmem_ld16(addr, v);
+}
+
+__device__ __forceinline__ void q8_timeout() { atomicOr(&g_status_q8, STATUS_TIMEOUT); }
+
+template <int NT>
+__global__ void __launch_bounds__(TC_THREADS, 1)
+    k_q8_tc(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const Q8Tc a) {
+    using C = Q8Cfg<NT>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint64_t *w_full = reinterpret_cast<uint64_t *>(smem + C::STAGES * C::STAGE);  // own weights have landed
+    uint64_t *x_full = w_full + C::STAGES;        // (leader) both halves of the tokens have
+    uint64_t *empty = x_full + C::STAGES;         // the pair's MMAs have read the stage
+    uint64_t *a_full = empty + C::STAGES;         // (leader) both SMs' fp16 weights are in TMEM
+    uint64_t *a_empty = a_full + C::A_STAGES;
+    uint64_t *acc_full = a_empty + C::A_STAGES;   // [2]
+    uint64_t *acc_empty = acc_full + 2;           // [2] (leader)
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(acc_empty + 2);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)cluster_ctarank(), cid = (int)cluster_id_x(), ncl = (int)cluster_count_x();
+    const int items = a.tiles_n * a.tiles_t * a.splits;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::STAGES; ++s) {
+            mbar_init(&w_full[s], 1);
+            mbar_init(&x_full[s], 1);
+            mbar_init(&empty[s], 1);
+        }
+        for (int s = 0; s < C::A_STAGES; ++s) {
+            mbar_init(&a_full[s], 2 * CONV_WARPS);
+            mbar_init(&a_empty[s], 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(&acc_full[s], 1);
+            mbar_init(&acc_empty[s], 2 * EPI_WARPS);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == CONV_WARPS + EPI_WARPS + 1) tmem_alloc_pair(tmem_slot, 512);
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();  // both SMs' barriers exist before any remote signal
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp == CONV_WARPS + EPI_WARPS) {
+        if (lane == 0) {
+            // TMA producer of this SM's weights and its half of the tokens
+            const uint32_t x_full0 = mapa_rank(smem_u32(&x_full[0]), 0);
+            uint32_t it = 0;
+            bool ok = true;
+            for (int i = cid; i < items && ok; i += ncl) {
+                const int tile = i / a.splits, sp = i - tile * a.splits;
+                int tn, tt;
+                tile_of(tile, a.tiles_n, a.tiles_t, tn, tt);
+                const int n0 = tn * 256 + rank * 128, t0 = tt * NT + rank * (NT / 2);
+                const int end = min(a.blocks, (sp + 1) * a.per);
+                for (int b = sp * a.per; b < end; ++b, ++it) {
+                    const int s = it % C::STAGES;
+                    if (!mbar_wait_cluster_spin(&empty[s], ((it / C::STAGES) & 1u) ^ 1u)) {
+                        q8_timeout();
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t st = smem_u32(smem + s * C::STAGE);
+                    const bool two = b * KB + 64 < a.K;  // a second half of the stage to read
+                    mbar_expect_tx(&w_full[s], (uint32_t)W_BYTES);
+                    tma_load_2d(st, &map_w, &w_full[s], b * KB, n0);
+                    if (rank == 0) mbar_expect_tx(&x_full[s], (uint32_t)((two ? 4 : 2) * C::X_BYTES));
+                    const uint32_t xb = x_full0 + (uint32_t)(s * sizeof(uint64_t));
+                    tma_load_2d_pair(st + W_BYTES, &map_x, xb, b * KB, t0);
+                    if (two) tma_load_2d_pair(st + W_BYTES + C::X_BYTES, &map_x, xb, b * KB + 64, t0);
+                }
+            }
+            if (ok) {
+                // every stage released: no copy is in flight and no commit targets this SM's stages afterwards
+                for (int i = 0; i < C::STAGES; ++i, ++it)
+                    if (!mbar_wait_cluster_spin(&empty[it % C::STAGES], ((it / C::STAGES) & 1u) ^ 1u)) {
+                        q8_timeout();
+                        break;
+                    }
+            }
+        }
+        __syncwarp();
+    } else if (warp == CONV_WARPS + EPI_WARPS + 1) {
+        if (lane == 0 && rank == 0) {
+            // MMA issuer of the pair
+            constexpr uint32_t idesc = idesc_16bit(256, NT, true);
+            uint32_t it = 0, ga = 0, j = 0;
+            bool ok = true;
+            for (int i = cid; i < items && ok; i += ncl) {
+                const int sp = i % a.splits;
+                const int end = min(a.blocks, (sp + 1) * a.per);
+                int in_chunk = 0;
+                for (int b = sp * a.per; b < end; ++b, ++it) {
+                    const int s = it % C::STAGES;
+                    if (in_chunk == 0 && !mbar_wait_cluster_spin(&acc_empty[j & 1u], ((j >> 1) & 1u) ^ 1u)) {
+                        ok = false;
+                        break;
+                    }
+                    if (!mbar_wait_cluster_spin(&x_full[s], (it / C::STAGES) & 1u)) {
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t acc = tmem + (j & 1u) * NT;
+                    const int halves = b * KB + 64 < a.K ? 2 : 1;
+                    for (int h = 0; h < halves; ++h, ++ga) {
+                        const int as = ga % C::A_STAGES;
+                        if (!mbar_wait_cluster_spin(&a_full[as], (ga / C::A_STAGES) & 1u)) {
+                            ok = false;
+                            break;
+                        }
+                        tc_fence_after();
+                        const uint32_t xs = smem_u32(smem + s * C::STAGE + W_BYTES + h * C::X_BYTES);
+                        const uint32_t at = tmem + C::A_COL + as * 32;
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk)
+                            mma_pair_ts(acc, at + kk * 8, sdesc_sw128(xs + kk * 32), idesc,
+                                        (in_chunk > 0 || h > 0 || kk > 0) ? 1u : 0u);
+                        mma_commit_pair(&a_empty[as]);
+                    }
+                    if (!ok) break;
+                    mma_commit_pair(&empty[s]);
+                    if (++in_chunk == FOLD || b + 1 == end) {
+                        mma_commit_pair(&acc_full[j & 1u]);
+                        in_chunk = 0;
+                        ++j;
+                    }
+                }
+            }
+            if (!ok) q8_timeout();
+        }
+        __syncwarp();
+    } else if (warp < CONV_WARPS) {
+        // weights to fp16: a thread takes one row, 64 codes at a time
+        const int row = warp * 32 + lane, swz = row & 7;
+        const uint32_t a_full0 = mapa_rank(smem_u32(&a_full[0]), 0);
+        const uint32_t tbase = tmem + ((uint32_t)(warp * 32) << 16) + C::A_COL;
+        uint32_t it = 0, ga = 0;
+        bool ok = true;
+        for (int i = cid; i < items && ok; i += ncl) {
+            const int sp = i % a.splits;
+            const int end = min(a.blocks, (sp + 1) * a.per);
+            for (int b = sp * a.per; b < end && ok; ++b, ++it) {
+                const int s = it % C::STAGES;
+                if (!mbar_wait_spin(&w_full[s], (it / C::STAGES) & 1u)) {
+                    ok = false;
+                    break;
+                }
+                const uint8_t *src = smem + s * C::STAGE + row * 128;
+                const int halves = b * KB + 64 < a.K ? 2 : 1;
+                for (int h = 0; h < halves; ++h, ++ga) {
+                    uint32_t r[32];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const uint4 v = *reinterpret_cast<const uint4 *>(src + (((h * 4 + c) ^ swz) << 4));
+                        codes_to_half(v.x, r[8 * c], r[8 * c + 1]);
+                        codes_to_half(v.y, r[8 * c + 2], r[8 * c + 3]);
+                        codes_to_half(v.z, r[8 * c + 4], r[8 * c + 5]);
+                        codes_to_half(v.w, r[8 * c + 6], r[8 * c + 7]);
+                    }
+                    const int as = ga % C::A_STAGES;
+                    if (!mbar_wait_cluster_spin(&a_empty[as], ((ga / C::A_STAGES) & 1u) ^ 1u)) {
+                        ok = false;
+                        break;
+                    }
+                    __syncwarp();
+                    tc_fence_after();
+                    tmem_st32(tbase + as * 32, r);
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(a_full0 + (uint32_t)(as * sizeof(uint64_t)));
+                }
+            }
+        }
+        if (ok) {
+            // the last commits on this SM's barriers have landed
+            for (int i = 0; i < C::A_STAGES && ok; ++i, ++ga)
+                ok = mbar_wait_cluster_spin(&a_empty[ga % C::A_STAGES], ((ga / C::A_STAGES) & 1u) ^ 1u);
+        }
+        if (!ok) q8_timeout();
+    } else {
+        // epilogue: rows of quarter (warp & 3), half of the columns
+        const int ew = warp - CONV_WARPS, quarter = warp & 3, group = ew >> 2;
+        const uint32_t tbase = tmem + ((uint32_t)(quarter * 32) << 16) + group * C::COLS;
+        const uint32_t acc_empty0 = mapa_rank(smem_u32(&acc_empty[0]), 0);
+        uint32_t j = 0;
+        for (int i = cid; i < items; i += ncl) {
+            const int tile = i / a.splits, sp = i - tile * a.splits;
+            int tn, tt;
+            tile_of(tile, a.tiles_n, a.tiles_t, tn, tt);
+            const int n = tn * 256 + rank * 128 + quarter * 32 + lane, t0 = tt * NT + group * C::COLS;
+            const int begin = sp * a.per, end = min(a.blocks, begin + a.per);
+            int sum[C::COLS];
+#pragma unroll
+            for (int c = 0; c < C::COLS; ++c) sum[c] = 0;
+            bool ok = true;
+            for (int b = begin; b < end; b += FOLD, ++j) {
+                if (!mbar_wait_cluster(&acc_full[j & 1u], (j >> 1) & 1u, false)) {
+                    q8_timeout();
+                    ok = false;
+                    break;
+                }
+                __syncwarp();
+                tc_fence_after();
+#pragma unroll
+                for (int c0 = 0; c0 < C::COLS; c0 += C::CH) {
+                    float v[C::CH];
+                    tmem_ld<C::CH>(tbase + (j & 1u) * NT + c0, v);
+#pragma unroll
+                    for (int c = 0; c < C::CH; ++c) sum[c0 + c] += __float2int_rn(v[c]);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(acc_empty0 + (uint32_t)((j & 1u) * sizeof(uint64_t)));
+            }
+            if (!ok) break;
+            if (a.splits > 1) {
+                const int part = rank * EPI_WARPS + ew;
+                const long long stride = (long long)16 * C::COLS * 32;  // of one item
+                int *mine = a.partial + (long long)i * stride + (long long)part * C::COLS * 32 + lane;
+#pragma unroll
+                for (int c = 0; c < C::COLS; ++c) __stcg(mine + c * 32, sum[c]);
+                __threadfence();
+                __syncwarp();
+                unsigned drawn = 0;
+                if (lane == 0) drawn = atomicAdd(&a.ticket[tile * 16 + part], 1u);
+                drawn = __shfl_sync(0xffffffffu, drawn, 0);
+                if (drawn != (unsigned)(a.splits - 1)) continue;
+                __threadfence();
+                const int *other = mine - (long long)sp * stride;
+                for (int q = 0; q < a.splits; ++q, other += stride) {
+                    if (q == sp) continue;
+#pragma unroll
+                    for (int c = 0; c < C::COLS; ++c) sum[c] += __ldcg(other + c * 32);
+                }
+            }
+            if (n < a.N) {
+                const float ws = a.w_scale[n];
+                if (a.out.ld_t == 1 && a.out.type == DSTD_TYPE_F32) {  // a row of tokens per channel
+                    float *dst = (float *)a.out.p + (long long)n * a.out.ld_n + t0;
+                    const bool vec = (reinterpret_cast<uintptr_t>(dst) & 15) == 0;
+#pragma unroll
+                    for (int c = 0; c < C::COLS; c += 4) {
+                        float y[4];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+                            y[u] = t0 + c + u < a.T ? ((float)sum[c + u] * a.x_scale[t0 + c + u]) * ws : 0.f;
+                        if (vec && t0 + c + 4 <= a.T) {
+                            *reinterpret_cast<float4 *>(dst + c) = make_float4(y[0], y[1], y[2], y[3]);
+                        } else {
+#pragma unroll
+                            for (int u = 0; u < 4; ++u)
+                                if (t0 + c + u < a.T) dst[c + u] = y[u];
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < C::COLS; ++c)
+                        if (t0 + c < a.T) store_out(a.out, t0 + c, n, ((float)sum[c] * a.x_scale[t0 + c]) * ws);
+                }
+            }
+            __syncwarp();
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();  // both SMs are done with TMEM, every remote arrive has landed
+    if (warp == CONV_WARPS + EPI_WARPS + 1) tmem_dealloc_pair(tmem, 512);
+}
+
+// tokens to fp16 rows [T, ld] (16 codes a thread), and the tickets to zero
+__global__ void __launch_bounds__(256) k_q8_half(const int8_t *__restrict__ x, long long ld_x, int T, int K, __half *y,
+                                                 int ld, bool aligned, unsigned *ticket, int tickets) {
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (i < tickets) ticket[i] = 0;
+    const int chunks = (ld + 15) / 16;
+    const long long t = i / chunks;
+    const int k = (int)(i - t * chunks) * 16;
+    if (t >= T) return;
+    const int4 v = load16(x + t * ld_x + k, K - k, aligned);
+    uint4 lo, hi;
+    codes_to_half((uint32_t)v.x, lo.x, lo.y);
+    codes_to_half((uint32_t)v.y, lo.z, lo.w);
+    codes_to_half((uint32_t)v.z, hi.x, hi.y);
+    codes_to_half((uint32_t)v.w, hi.z, hi.w);
+    *reinterpret_cast<uint4 *>(y + t * ld + k) = lo;
+    if (k + 8 < ld) *reinterpret_cast<uint4 *>(y + t * ld + k + 8) = hi;
+}
+
+constexpr int kPairs = 76;  // SM pairs of the GPU, for planning
+
+// fewer tokens than this go to the dot form
+constexpr int kTcMinTokens = 9;
+
+Q8Plan q8_plan(int T, int N, int K) {
+    Q8Plan best{};
+    double best_cost = 0;
+    for (int nt : {32, 64, 96, 128, 160, 192}) {
+        Q8Plan p{};
+        p.nt = nt;
+        p.tiles_n = (N + 255) / 256;
+        p.tiles_t = (T + nt - 1) / nt;
+        p.blocks = (K + KB - 1) / KB;
+        const long long tiles = (long long)p.tiles_n * p.tiles_t;
+        for (int want = 1; want <= 32; ++want) {
+            p.per = (p.blocks + want - 1) / want;
+            p.splits = (p.blocks + p.per - 1) / p.per;
+            if (p.splits != want) continue;
+            if (want > 1 && tiles * want > 2 * kPairs) break;
+            const double rounds = (double)((tiles * want + kPairs - 1) / kPairs);
+            const double block = 8 * (nt / 2) > 400 ? 8 * (nt / 2) : 400;
+            const double cost = rounds * (p.per * block + 1500 + 12 * nt + (want > 1 ? 1500 + 4.0 * want * nt : 0));
+            if (best.nt == 0 || cost < best_cost) {
+                best_cost = cost;
+                best = p;
+            }
+        }
+    }
+    return best;
+}
+
+struct Q8Scratch {
+    __half *x;
+    unsigned *ticket;
+    int *partial;
+    int ld;
+    size_t bytes;
+};
+Q8Scratch q8_scratch(void *base, int T, int K, const Q8Plan &p) {
+    Q8Scratch s{};
+    char *b = static_cast<char *>(base);
+    s.ld = (K + 7) / 8 * 8;
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        char *at = b ? b + off : nullptr;
+        off += (bytes + 255) / 256 * 256;
+        return at;
+    };
+    s.x = (__half *)take((size_t)T * s.ld * 2);
+    const size_t tiles = (size_t)p.tiles_n * p.tiles_t;
+    s.ticket = (unsigned *)take(p.splits > 1 ? tiles * 16 * 4 : 0);
+    s.partial = (int *)take(p.splits > 1 ? tiles * p.splits * 256 * p.nt * 4 : 0);
+    s.bytes = off;
+    return s;
+}
+
+typedef CUresult (*EncodeFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                             const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                             CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// rows of 128-byte boxes, swizzled; beyond the matrix zeros are read
+bool row_map(CUtensorMap *m, CUtensorMapDataType type, int bytes, const void *p, int rows, int cols, long long ld,
+             int box_rows) {
+    EncodeFn enc = reinterpret_cast<EncodeFn>(tensor_map_encoder());
+    if (!enc) return false;
+    const cuuint64_t dim[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t stride[1] = {(cuuint64_t)ld * bytes};
+    const cuuint32_t box[2] = {(cuuint32_t)(128 / bytes), (cuuint32_t)box_rows};
+    const cuuint32_t one[2] = {1, 1};
+    return enc(m, type, 2, const_cast<void *>(p), dim, stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int NT>
+cudaError_t launch_tc(const Q8Args &q, const Q8Plan &p, const Q8Scratch &s, cudaStream_t st) {
+    using C = Q8Cfg<NT>;
+    auto kern = k_q8_tc<NT>;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    if (e != cudaSuccess) return e;
+    CUtensorMap map_w, map_x;
+    if (!row_map(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, q.w, q.N, q.K, q.ld_w, 128) ||
+        !row_map(&map_x, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, s.x, q.T, q.K, s.ld, NT / 2))
+        return cudaErrorInvalidValue;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cfg.blockDim = dim3(TC_THREADS);
+    cfg.dynamicSmemBytes = C::SMEM;
+    cfg.stream = st;
+    static int resident = 0;  // pairs that can be at work at once
+    if (resident == 0) {
+        cfg.gridDim = dim3(2 * kPairs);
+        int n = 0;
+        e = cudaOccupancyMaxActiveClusters(&n, kern, &cfg);
+        if (e != cudaSuccess) return e;
+        if (n < 1) return cudaErrorInvalidConfiguration;
+        resident = n;
+    }
+    const long long items = (long long)p.tiles_n * p.tiles_t * p.splits;
+    cfg.gridDim = dim3(2 * (unsigned)(items < resident ? items : resident));
+    const Q8Tc a{q.T, q.N, q.K, p.tiles_n, p.tiles_t, p.splits, p.blocks, p.per, q.x_scale, q.w_scale, q.out, s.partial,
+                 s.ticket};
+    return cudaLaunchKernelEx(&cfg, kern, map_w, map_x, a);
+}
+
+bool use_tc(const Q8Args &a) {
+    return a.T >= kTcMinTokens && a.K >= 16 && (reinterpret_cast<uintptr_t>(a.w) & 15) == 0 && a.ld_w % 16 == 0;
+}
+
+}  // namespace
+
 size_t q8_workspace_bytes(int T, int N, int K) {
-    (void)T, (void)N, (void)K;
-    return 256;
+    if (T < kTcMinTokens || N < 1 || K < 1) return 256;
+    return 256 + q8_scratch(nullptr, T, K, q8_plan(T, N, K)).bytes;
 }
 
 cudaError_t launch_q8_product(const Q8Args &a, void *workspace, cudaStream_t st) {
-    (void)workspace;
     if (a.T == 0 || a.N == 0) return cudaSuccess;
+    const bool x_aligned = ((reinterpret_cast<uintptr_t>(a.x) | (uintptr_t)a.ld_x) & 15) == 0;
+    if (use_tc(a)) {
+        const Q8Plan p = q8_plan(a.T, a.N, a.K);
+        const Q8Scratch s = q8_scratch(workspace, a.T, a.K, p);
+        const int tickets = p.splits > 1 ? p.tiles_n * p.tiles_t * 16 : 0;
+        const long long threads = std::max((long long)a.T * ((s.ld + 15) / 16), (long long)tickets);
+        k_q8_half<<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(a.x, a.ld_x, a.T, a.K, s.x, s.ld, x_aligned,
+                                                                    s.ticket, tickets);
+        cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+        switch (p.nt) {
+            case 32: return launch_tc<32>(a, p, s, st);
+            case 64: return launch_tc<64>(a, p, s, st);
+            case 96: return launch_tc<96>(a, p, s, st);
+            case 128: return launch_tc<128>(a, p, s, st);
+            case 160: return launch_tc<160>(a, p, s, st);
+            default: return launch_tc<192>(a, p, s, st);
+        }
+    }
     constexpr int TT = 8, R = 2;
-    const bool aligned = ((reinterpret_cast<uintptr_t>(a.w) | reinterpret_cast<uintptr_t>(a.x) | (uintptr_t)a.ld_w |
-                           (uintptr_t)a.ld_x) & 15) == 0;
+    const bool aligned = x_aligned && ((reinterpret_cast<uintptr_t>(a.w) | (uintptr_t)a.ld_w) & 15) == 0;
     const int tt_max = 65535 * TT;  // tokens of one launch
     for (int t = 0; t < a.T; t += tt_max) {
         Q8Args b = a;
