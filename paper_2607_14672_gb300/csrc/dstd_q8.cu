@@ -167,9 +167,11 @@ __global__ void __launch_bounds__(256) k_q8_dot(Q8Args a, bool aligned) {
 // half of the tokens' operand. Two accumulators of NT columns alternate every
 // 1024 codes of K; eight epilogue warps take the full one into 32-bit integers
 // in registers while the other fills.
-// With few tiles K is split among pairs: each writes its integer sums to the
-// workspace, and the last one to finish a part (a ticket counts them) adds the
-// others' and stores. Integer sums do not depend on the order.
+// Whole rounds of tiles go one to a pair. The tiles left over (all of them, when
+// there are few) are cut along K into equal shares for all pairs, where that
+// is shorter than one more round: a pair adds its integer sums into the
+// workspace with atomics, and the last one of a part (a ticket counts them)
+// stores the result. Whole-number sums do not depend on the order.
 // ---------------------------------------------------------------------------
 __device__ unsigned int g_status_q8 = 0;
 
@@ -186,7 +188,11 @@ using namespace tc;
 constexpr int KB = 128;          // codes of K per stage
 constexpr int FOLD = 1024 / KB;  // stages per accumulator
 constexpr int W_BYTES = 128 * KB;
-constexpr int CONV_WARPS = 4, EPI_WARPS = 8, TC_THREADS = 32 * (CONV_WARPS + EPI_WARPS + 2);
+constexpr int CONV_WARPS = 8, EPI_WARPS = 8, TC_THREADS = 32 * (CONV_WARPS + EPI_WARPS + 4);
+// registers a thread of each role, where the kernel splits them (whole warpgroups)
+constexpr int REGS_CONV = 72, REGS_EPI = 136, REGS_REST = 48;
+constexpr int REGS_SUM = 32 * (CONV_WARPS * REGS_CONV + EPI_WARPS * REGS_EPI + 4 * REGS_REST);
+
 
 template <int NT>
 struct Q8Cfg {
@@ -194,23 +200,58 @@ struct Q8Cfg {
     static constexpr int STAGE = W_BYTES + 2 * X_BYTES;
     static constexpr int STAGES = 200 * 1024 / STAGE > 8 ? 8 : 200 * 1024 / STAGE;
     static constexpr int SMEM = STAGES * STAGE + 1024 + 512;
-    static constexpr int A_STAGES = (512 - 2 * NT) / 32 > 4 ? 4 : (512 - 2 * NT) / 32;  // of 64 codes, 32 columns each
+    static constexpr int A_STAGES = (512 - 2 * NT) / 64 > 4 ? 4 : (512 - 2 * NT) / 64;  // of 128 codes, 64 columns each
     static constexpr int A_COL = 2 * NT;
     static constexpr int COLS = NT / 2;                   // columns of one epilogue warp
-    static constexpr int CH = COLS == 32 || COLS == 64 ? 32 : 16;  // columns per TMEM read
+    // the epilogue's sums do not fit an even share of the registers: the other warps give some of theirs
+    // (REGS_SUM = 59392, of the 640 x 96 = 61440 that the block is launched with; checked before the launch)
+    static constexpr bool SPLIT_REGS = NT > 64;
+    static constexpr int CH = COLS == 32 ? 32 : 16;  // columns per TMEM read
 };
 
 struct Q8Plan {
-    int nt, splits;
-    int tiles_n, tiles_t, blocks, per;  // K blocks of 128, and of one split
+    int nt, tiles_n, tiles_t, blocks;  // blocks of 128 along K
+    int whole;                         // tiles computed in one piece
+    int share;                         // blocks of one pair's share of the others (0: none are left)
 };
 
 struct Q8Tc {
-    int T, N, K, tiles_n, tiles_t, splits, blocks, per;
+    int T, N, K;
+    Q8Plan p;
     const float *x_scale, *w_scale;
     Q8Out out;
-    int *partial;      // [item][16 warps][COLS][32]
-    unsigned *ticket;  // [tile][16 warps], zeroed before the launch
+    int *partial;      // [tile][16 warps][COLS][32] of the tiles that are cut, zeroed before the launch
+    unsigned *ticket;  // [tile][16 warps], too
+};
+
+// What a pair works on, in order: tile and blocks [b0, b1) of K, cut into `parts` shares among pairs.
+struct Work {
+    int tile, b0, b1, parts;
+    int i, step, g, end;
+    __device__ __forceinline__ Work(const Q8Plan &p, int cid, int ncl) : i(cid), step(ncl) {
+        const long long rest = (long long)(p.tiles_n * p.tiles_t - p.whole) * p.blocks;
+        const long long lo = (long long)cid * p.share, hi = lo + p.share;
+        g = (int)(lo < rest ? lo : rest);
+        end = (int)(hi < rest ? hi : rest);
+    }
+    __device__ __forceinline__ bool next(const Q8Plan &p) {
+        if (i < p.whole) {
+            tile = i;
+            b0 = 0;
+            b1 = p.blocks;
+            parts = 1;
+            i += step;
+            return true;
+        }
+        if (g >= end) return false;
+        const int r = g / p.blocks;
+        tile = p.whole + r;
+        b0 = g - r * p.blocks;
+        b1 = min(p.blocks, b0 + end - g);
+        parts = (r * p.blocks + p.blocks - 1) / p.share - r * p.blocks / p.share + 1;
+        g += b1 - b0;
+        return true;
+    }
 };
 
 // tiles are taken in groups of 8 token tiles, so that the pairs at work at one
@@ -249,27 +290,22 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint64_t *w_full = reinterpret_cast<uint64_t *>(smem + C::STAGES * C::STAGE);  // own weights have landed
-    uint64_t *x_full = w_full + C::STAGES;        // (leader) both halves of the tokens have
-    uint64_t *empty = x_full + C::STAGES;         // the pair's MMAs have read the stage
-    uint64_t *a_full = empty + C::STAGES;         // (leader) both SMs' fp16 weights are in TMEM
-    uint64_t *a_empty = a_full + C::A_STAGES;
-    uint64_t *acc_full = a_empty + C::A_STAGES;   // [2]
+    // (leader) both halves of the tokens have, and both SMs' fp16 weights are in TMEM
+    uint64_t *ready = w_full + C::STAGES;
+    uint64_t *empty = ready + C::STAGES;          // the pair's MMAs have read the stage
+    uint64_t *acc_full = empty + C::STAGES;       // [2]
     uint64_t *acc_empty = acc_full + 2;           // [2] (leader)
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(acc_empty + 2);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = (int)cluster_ctarank(), cid = (int)cluster_id_x(), ncl = (int)cluster_count_x();
-    const int items = a.tiles_n * a.tiles_t * a.splits;
+    const int rank = (int)cluster_ctarank();
+    Work wk(a.p, (int)cluster_id_x(), (int)cluster_count_x());
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::STAGES; ++s) {
             mbar_init(&w_full[s], 1);
-            mbar_init(&x_full[s], 1);
+            mbar_init(&ready[s], 1 + 2 * CONV_WARPS / 2);  // one group of each SM takes a block
             mbar_init(&empty[s], 1);
-        }
-        for (int s = 0; s < C::A_STAGES; ++s) {
-            mbar_init(&a_full[s], 2 * CONV_WARPS);
-            mbar_init(&a_empty[s], 1);
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(&acc_full[s], 1);
@@ -285,113 +321,103 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
 
+    if constexpr (C::SPLIT_REGS) {
+        if (warp >= CONV_WARPS + EPI_WARPS) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_REST));
+    }
     if (warp == CONV_WARPS + EPI_WARPS) {
-        if (lane == 0) {
-            // TMA producer of this SM's weights and its half of the tokens
-            const uint32_t x_full0 = mapa_rank(smem_u32(&x_full[0]), 0);
-            uint32_t it = 0;
-            bool ok = true;
-            for (int i = cid; i < items && ok; i += ncl) {
-                const int tile = i / a.splits, sp = i - tile * a.splits;
-                int tn, tt;
-                tile_of(tile, a.tiles_n, a.tiles_t, tn, tt);
-                const int n0 = tn * 256 + rank * 128, t0 = tt * NT + rank * (NT / 2);
-                const int end = min(a.blocks, (sp + 1) * a.per);
-                for (int b = sp * a.per; b < end; ++b, ++it) {
-                    const int s = it % C::STAGES;
-                    if (!mbar_wait_cluster_spin(&empty[s], ((it / C::STAGES) & 1u) ^ 1u)) {
-                        q8_timeout();
-                        ok = false;
-                        break;
-                    }
+        // TMA producer of this SM's weights and its half of the tokens
+        const uint32_t ready0 = mapa_rank(smem_u32(&ready[0]), 0);
+        uint32_t it = 0;
+        bool ok = true;
+        while (ok && wk.next(a.p)) {
+            int tn, tt;
+            tile_of(wk.tile, a.p.tiles_n, a.p.tiles_t, tn, tt);
+            const int n0 = tn * 256 + rank * 128, t0 = tt * NT + rank * (NT / 2);
+            for (int b = wk.b0; b < wk.b1; ++b, ++it) {
+                const int s = it % C::STAGES;
+                ok = mbar_wait_cycles(&empty[s], ((it / C::STAGES) & 1u) ^ 1u);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                if (elect_one()) {
                     const uint32_t st = smem_u32(smem + s * C::STAGE);
                     const bool two = b * KB + 64 < a.K;  // a second half of the stage to read
                     mbar_expect_tx(&w_full[s], (uint32_t)W_BYTES);
                     tma_load_2d(st, &map_w, &w_full[s], b * KB, n0);
-                    if (rank == 0) mbar_expect_tx(&x_full[s], (uint32_t)((two ? 4 : 2) * C::X_BYTES));
-                    const uint32_t xb = x_full0 + (uint32_t)(s * sizeof(uint64_t));
-                    tma_load_2d_pair(st + W_BYTES, &map_x, xb, b * KB, t0);
-                    if (two) tma_load_2d_pair(st + W_BYTES + C::X_BYTES, &map_x, xb, b * KB + 64, t0);
+                    if (rank == 0) mbar_expect_tx(&ready[s], (uint32_t)((two ? 4 : 2) * C::X_BYTES));
+                    const uint32_t rb = ready0 + (uint32_t)(s * sizeof(uint64_t));
+                    tma_load_2d_pair(st + W_BYTES, &map_x, rb, b * KB, t0);
+                    if (two) tma_load_2d_pair(st + W_BYTES + C::X_BYTES, &map_x, rb, b * KB + 64, t0);
                 }
-            }
-            if (ok) {
-                // every stage released: no copy is in flight and no commit targets this SM's stages afterwards
-                for (int i = 0; i < C::STAGES; ++i, ++it)
-                    if (!mbar_wait_cluster_spin(&empty[it % C::STAGES], ((it / C::STAGES) & 1u) ^ 1u)) {
-                        q8_timeout();
-                        break;
-                    }
+                __syncwarp();
             }
         }
+        // every stage released: no copy is in flight and no commit targets this SM's stages afterwards
+        for (int i = 0; i < C::STAGES && ok; ++i, ++it)
+            ok = mbar_wait_cycles(&empty[it % C::STAGES], ((it / C::STAGES) & 1u) ^ 1u);
+        if (!ok) q8_timeout();
         __syncwarp();
     } else if (warp == CONV_WARPS + EPI_WARPS + 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
             // MMA issuer of the pair
             constexpr uint32_t idesc = idesc_16bit(256, NT, true);
-            uint32_t it = 0, ga = 0, j = 0;
+            uint32_t it = 0, j = 0;
             bool ok = true;
-            for (int i = cid; i < items && ok; i += ncl) {
-                const int sp = i % a.splits;
-                const int end = min(a.blocks, (sp + 1) * a.per);
+            while (ok && wk.next(a.p)) {
                 int in_chunk = 0;
-                for (int b = sp * a.per; b < end; ++b, ++it) {
-                    const int s = it % C::STAGES;
-                    if (in_chunk == 0 && !mbar_wait_cluster_spin(&acc_empty[j & 1u], ((j >> 1) & 1u) ^ 1u)) {
-                        ok = false;
-                        break;
-                    }
-                    if (!mbar_wait_cluster_spin(&x_full[s], (it / C::STAGES) & 1u)) {
-                        ok = false;
-                        break;
-                    }
-                    const uint32_t acc = tmem + (j & 1u) * NT;
-                    const int halves = b * KB + 64 < a.K ? 2 : 1;
-                    for (int h = 0; h < halves; ++h, ++ga) {
-                        const int as = ga % C::A_STAGES;
-                        if (!mbar_wait_cluster_spin(&a_full[as], (ga / C::A_STAGES) & 1u)) {
-                            ok = false;
-                            break;
-                        }
-                        tc_fence_after();
-                        const uint32_t xs = smem_u32(smem + s * C::STAGE + W_BYTES + h * C::X_BYTES);
-                        const uint32_t at = tmem + C::A_COL + as * 32;
+                for (int b = wk.b0; b < wk.b1; ++b, ++it) {
+                    const int s = it % C::STAGES, as = it % C::A_STAGES;
+                    ok = (in_chunk > 0 || mbar_wait_cycles(&acc_empty[j & 1u], ((j >> 1) & 1u) ^ 1u)) &&
+                         mbar_wait_cycles(&ready[s], (it / C::STAGES) & 1u);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t acc = tmem + (j & 1u) * NT, at = tmem + C::A_COL + as * 64;
+                    const uint64_t xd = sdesc_sw128(smem_u32(smem + s * C::STAGE + W_BYTES));
+                    const bool two = b * KB + 64 < a.K, last = in_chunk + 1 == FOLD || b + 1 == wk.b1;
+                    if (elect_one()) {
 #pragma unroll
                         for (int kk = 0; kk < 4; ++kk)
-                            mma_pair_ts(acc, at + kk * 8, sdesc_sw128(xs + kk * 32), idesc,
-                                        (in_chunk > 0 || h > 0 || kk > 0) ? 1u : 0u);
-                        mma_commit_pair(&a_empty[as]);
+                            mma_pair_ts(acc, at + kk * 8, xd + kk * 2, idesc, (in_chunk > 0 || kk > 0) ? 1u : 0u);
+                        if (two) {
+#pragma unroll
+                            for (int kk = 0; kk < 4; ++kk)
+                                mma_pair_ts(acc, at + 32 + kk * 8, xd + C::X_BYTES / 16 + kk * 2, idesc, 1u);
+                        }
+                        mma_commit_pair(&empty[s]);
+                        if (last) mma_commit_pair(&acc_full[j & 1u]);
                     }
-                    if (!ok) break;
-                    mma_commit_pair(&empty[s]);
-                    if (++in_chunk == FOLD || b + 1 == end) {
-                        mma_commit_pair(&acc_full[j & 1u]);
-                        in_chunk = 0;
-                        ++j;
-                    }
+                    __syncwarp();
+                    in_chunk = last ? 0 : in_chunk + 1;
+                    j += last ? 1 : 0;
                 }
             }
             if (!ok) q8_timeout();
         }
         __syncwarp();
     } else if (warp < CONV_WARPS) {
-        // weights to fp16: a thread takes one row, 64 codes at a time
-        const int row = warp * 32 + lane, swz = row & 7;
-        const uint32_t a_full0 = mapa_rank(smem_u32(&a_full[0]), 0);
-        const uint32_t tbase = tmem + ((uint32_t)(warp * 32) << 16) + C::A_COL;
-        uint32_t it = 0, ga = 0;
+        // weights to fp16: a thread takes one row; two groups of four warps take the blocks in turn
+        if constexpr (C::SPLIT_REGS) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_CONV));
+        const int group = warp >> 2, row = (warp & 3) * 32 + lane, swz = row & 7;
+        const uint32_t ready0 = mapa_rank(smem_u32(&ready[0]), 0);
+        const uint32_t tbase = tmem + ((uint32_t)((warp & 3) * 32) << 16) + C::A_COL;
+        uint32_t it = 0;
         bool ok = true;
-        for (int i = cid; i < items && ok; i += ncl) {
-            const int sp = i % a.splits;
-            const int end = min(a.blocks, (sp + 1) * a.per);
-            for (int b = sp * a.per; b < end && ok; ++b, ++it) {
-                const int s = it % C::STAGES;
-                if (!mbar_wait_spin(&w_full[s], (it / C::STAGES) & 1u)) {
-                    ok = false;
-                    break;
+        while (ok && wk.next(a.p)) {
+            for (int b = wk.b0; b < wk.b1; ++b, ++it) {
+                if ((it & 1u) != (uint32_t)group) continue;
+                const int s = it % C::STAGES, as = it % C::A_STAGES;
+                ok = mbar_wait_cycles(&w_full[s], (it / C::STAGES) & 1u);
+                // the block that used these columns has been multiplied
+                if (ok && it >= C::A_STAGES) {
+                    const uint32_t old = it - C::A_STAGES;
+                    ok = mbar_wait_cycles(&empty[old % C::STAGES], (old / C::STAGES) & 1u);
                 }
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc_fence_after();
                 const uint8_t *src = smem + s * C::STAGE + row * 128;
                 const int halves = b * KB + 64 < a.K ? 2 : 1;
-                for (int h = 0; h < halves; ++h, ++ga) {
+                for (int h = 0; h < halves; ++h) {
                     uint32_t r[32];
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
@@ -401,44 +427,32 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                         codes_to_half(v.z, r[8 * c + 4], r[8 * c + 5]);
                         codes_to_half(v.w, r[8 * c + 6], r[8 * c + 7]);
                     }
-                    const int as = ga % C::A_STAGES;
-                    if (!mbar_wait_cluster_spin(&a_empty[as], ((ga / C::A_STAGES) & 1u) ^ 1u)) {
-                        ok = false;
-                        break;
-                    }
-                    __syncwarp();
-                    tc_fence_after();
-                    tmem_st32(tbase + as * 32, r);
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_cluster(a_full0 + (uint32_t)(as * sizeof(uint64_t)));
+                    tmem_st32(tbase + as * 64 + h * 32, r);
                 }
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_pair(ready0 + (uint32_t)(s * sizeof(uint64_t)));
             }
         }
-        if (ok) {
-            // the last commits on this SM's barriers have landed
-            for (int i = 0; i < C::A_STAGES && ok; ++i, ++ga)
-                ok = mbar_wait_cluster_spin(&a_empty[ga % C::A_STAGES], ((ga / C::A_STAGES) & 1u) ^ 1u);
-        }
         if (!ok) q8_timeout();
-    } else {
+    } else if (warp < CONV_WARPS + EPI_WARPS) {
         // epilogue: rows of quarter (warp & 3), half of the columns
+        if constexpr (C::SPLIT_REGS) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_EPI));
         const int ew = warp - CONV_WARPS, quarter = warp & 3, group = ew >> 2;
         const uint32_t tbase = tmem + ((uint32_t)(quarter * 32) << 16) + group * C::COLS;
         const uint32_t acc_empty0 = mapa_rank(smem_u32(&acc_empty[0]), 0);
         uint32_t j = 0;
-        for (int i = cid; i < items; i += ncl) {
-            const int tile = i / a.splits, sp = i - tile * a.splits;
+        while (wk.next(a.p)) {
             int tn, tt;
-            tile_of(tile, a.tiles_n, a.tiles_t, tn, tt);
+            tile_of(wk.tile, a.p.tiles_n, a.p.tiles_t, tn, tt);
             const int n = tn * 256 + rank * 128 + quarter * 32 + lane, t0 = tt * NT + group * C::COLS;
-            const int begin = sp * a.per, end = min(a.blocks, begin + a.per);
             int sum[C::COLS];
 #pragma unroll
             for (int c = 0; c < C::COLS; ++c) sum[c] = 0;
             bool ok = true;
-            for (int b = begin; b < end; b += FOLD, ++j) {
-                if (!mbar_wait_cluster(&acc_full[j & 1u], (j >> 1) & 1u, false)) {
+            for (int b = wk.b0; b < wk.b1; b += FOLD, ++j) {
+                if (!mbar_wait_cycles(&acc_full[j & 1u], (j >> 1) & 1u)) {
                     q8_timeout();
                     ok = false;
                     break;
@@ -454,28 +468,23 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(acc_empty0 + (uint32_t)((j & 1u) * sizeof(uint64_t)));
+                if (lane == 0) mbar_arrive_pair(acc_empty0 + (uint32_t)((j & 1u) * sizeof(uint64_t)));
             }
             if (!ok) break;
-            if (a.splits > 1) {
-                const int part = rank * EPI_WARPS + ew;
-                const long long stride = (long long)16 * C::COLS * 32;  // of one item
-                int *mine = a.partial + (long long)i * stride + (long long)part * C::COLS * 32 + lane;
+            if (wk.parts > 1) {
+                const int cut = (wk.tile - a.p.whole) * 16 + rank * EPI_WARPS + ew;
+                int *all = a.partial + (long long)cut * C::COLS * 32 + lane;
 #pragma unroll
-                for (int c = 0; c < C::COLS; ++c) __stcg(mine + c * 32, sum[c]);
+                for (int c = 0; c < C::COLS; ++c) atomicAdd(all + c * 32, sum[c]);
                 __threadfence();
                 __syncwarp();
                 unsigned drawn = 0;
-                if (lane == 0) drawn = atomicAdd(&a.ticket[tile * 16 + part], 1u);
+                if (lane == 0) drawn = atomicAdd(&a.ticket[cut], 1u);
                 drawn = __shfl_sync(0xffffffffu, drawn, 0);
-                if (drawn != (unsigned)(a.splits - 1)) continue;
+                if (drawn != (unsigned)(wk.parts - 1)) continue;
                 __threadfence();
-                const int *other = mine - (long long)sp * stride;
-                for (int q = 0; q < a.splits; ++q, other += stride) {
-                    if (q == sp) continue;
 #pragma unroll
-                    for (int c = 0; c < C::COLS; ++c) sum[c] += __ldcg(other + c * 32);
-                }
+                for (int c = 0; c < C::COLS; ++c) sum[c] = __ldcg(all + c * 32);
             }
             if (n < a.N) {
                 const float ws = a.w_scale[n];
@@ -511,11 +520,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     if (warp == CONV_WARPS + EPI_WARPS + 1) tmem_dealloc_pair(tmem, 512);
 }
 
-// tokens to fp16 rows [T, ld] (16 codes a thread), and the tickets to zero
+// tokens to fp16 rows [T, ld] (16 codes a thread); the tickets and sums of the tiles that are cut to zero
 __global__ void __launch_bounds__(256) k_q8_half(const int8_t *__restrict__ x, long long ld_x, int T, int K, __half *y,
-                                                 int ld, bool aligned, unsigned *ticket, int tickets) {
+                                                 int ld, bool aligned, uint4 *zero, long long zeros) {
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (i < tickets) ticket[i] = 0;
+    if (i < zeros) zero[i] = make_uint4(0, 0, 0, 0);
     const int chunks = (ld + 15) / 16;
     const long long t = i / chunks;
     const int k = (int)(i - t * chunks) * 16;
@@ -535,28 +544,45 @@ constexpr int kPairs = 76;  // SM pairs of the GPU, for planning
 // fewer tokens than this go to the dot form
 constexpr int kTcMinTokens = 9;
 
-Q8Plan q8_plan(int T, int N, int K) {
+// Time of one block of 128 codes in a pair's pipeline, in cycles, measured with
+// 4096 tokens, 16384 inputs and channels: the conversion and the issue of the
+// MMAs hold it at about 700 up to 128 tokens a tile, and with 192 only two
+// blocks fit beside the accumulators in TMEM.
+struct TileCost {
+    int nt, block;
+};
+constexpr TileCost kTiles[] = {{32, 680}, {64, 680}, {96, 770}, {128, 800}, {160, 830}, {192, 1010}};
+
+// `pairs`: SM pairs at work at a time. Whole rounds of tiles, then the rest
+// either as one more round or in shares along K; the tile width by the sum.
+Q8Plan q8_plan(int T, int N, int K, int pairs) {
     Q8Plan best{};
     double best_cost = 0;
-    for (int nt : {32, 64, 96, 128, 160, 192}) {
+    for (const TileCost &tc : kTiles) {
         Q8Plan p{};
-        p.nt = nt;
+        p.nt = tc.nt;
         p.tiles_n = (N + 255) / 256;
-        p.tiles_t = (T + nt - 1) / nt;
+        p.tiles_t = (T + tc.nt - 1) / tc.nt;
         p.blocks = (K + KB - 1) / KB;
-        const long long tiles = (long long)p.tiles_n * p.tiles_t;
-        for (int want = 1; want <= 32; ++want) {
-            p.per = (p.blocks + want - 1) / want;
-            p.splits = (p.blocks + p.per - 1) / p.per;
-            if (p.splits != want) continue;
-            if (want > 1 && tiles * want > 2 * kPairs) break;
-            const double rounds = (double)((tiles * want + kPairs - 1) / kPairs);
-            const double block = 8 * (nt / 2) > 400 ? 8 * (nt / 2) : 400;
-            const double cost = rounds * (p.per * block + 1500 + 12 * nt + (want > 1 ? 1500 + 4.0 * want * nt : 0));
-            if (best.nt == 0 || cost < best_cost) {
-                best_cost = cost;
-                best = p;
+        const int tiles = p.tiles_n * p.tiles_t, rest = tiles % pairs;
+        p.whole = tiles;
+        const double tile = (double)p.blocks * tc.block;
+        double cost = (tiles / pairs) * tile + 12.0 * tc.nt;
+        if (rest > 0) {
+            // a share of at least two blocks; adding up and the wait for the last part cost about as much as 2000 +
+            // 20 nt cycles
+            const long long blocks = (long long)rest * p.blocks;
+            const int share = (int)std::max((blocks + pairs - 1) / pairs, 2ll);
+            const double cut = (double)share * tc.block + 2000 + 20.0 * tc.nt;
+            if (cut < tile) {
+                p.whole = tiles - rest;
+                p.share = share;
             }
+            cost += std::min(cut, tile);
+        }
+        if (best.nt == 0 || cost < best_cost) {
+            best_cost = cost;
+            best = p;
         }
     }
     return best;
@@ -567,23 +593,19 @@ struct Q8Scratch {
     unsigned *ticket;
     int *partial;
     int ld;
-    size_t bytes;
+    long long zeros;  // 16-byte words from ticket on
 };
+// of a plan: the fp16 tokens, then tickets and sums of the tiles that are cut
 Q8Scratch q8_scratch(void *base, int T, int K, const Q8Plan &p) {
     Q8Scratch s{};
     char *b = static_cast<char *>(base);
     s.ld = (K + 7) / 8 * 8;
-    size_t off = 0;
-    auto take = [&](size_t bytes) {
-        char *at = b ? b + off : nullptr;
-        off += (bytes + 255) / 256 * 256;
-        return at;
-    };
-    s.x = (__half *)take((size_t)T * s.ld * 2);
-    const size_t tiles = (size_t)p.tiles_n * p.tiles_t;
-    s.ticket = (unsigned *)take(p.splits > 1 ? tiles * 16 * 4 : 0);
-    s.partial = (int *)take(p.splits > 1 ? tiles * p.splits * 256 * p.nt * 4 : 0);
-    s.bytes = off;
+    const size_t x = ((size_t)T * s.ld * 2 + 255) / 256 * 256;
+    const long long cut = (long long)p.tiles_n * p.tiles_t - p.whole;
+    s.x = (__half *)b;
+    s.ticket = (unsigned *)(b + x);
+    s.partial = (int *)(b + x + cut * 64);
+    s.zeros = (cut * 64 + cut * 1024 * p.nt) / 16;
     return s;
 }
 
@@ -606,17 +628,8 @@ bool row_map(CUtensorMap *m, CUtensorMapDataType type, int bytes, const void *p,
 }
 
 template <int NT>
-cudaError_t launch_tc(const Q8Args &q, const Q8Plan &p, const Q8Scratch &s, cudaStream_t st) {
-    using C = Q8Cfg<NT>;
-    auto kern = k_q8_tc<NT>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
-    if (e != cudaSuccess) return e;
-    CUtensorMap map_w, map_x;
-    if (!row_map(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, q.w, q.N, q.K, q.ld_w, 128) ||
-        !row_map(&map_x, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, s.x, q.T, q.K, s.ld, NT / 2))
-        return cudaErrorInvalidValue;
+cudaLaunchConfig_t tc_config(cudaLaunchAttribute *attr) {
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2;
     attr[0].val.clusterDim.y = 1;
@@ -624,22 +637,56 @@ cudaError_t launch_tc(const Q8Args &q, const Q8Plan &p, const Q8Scratch &s, cuda
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     cfg.blockDim = dim3(TC_THREADS);
-    cfg.dynamicSmemBytes = C::SMEM;
-    cfg.stream = st;
-    static int resident = 0;  // pairs that can be at work at once
-    if (resident == 0) {
+    cfg.dynamicSmemBytes = Q8Cfg<NT>::SMEM;
+    return cfg;
+}
+
+// kernel attributes, set once per tile width; 0 or an error
+template <int NT>
+cudaError_t tc_setup() {
+    using C = Q8Cfg<NT>;
+    static cudaError_t done = [] {
+        cudaError_t e = cudaFuncSetAttribute(k_q8_tc<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+        if (e != cudaSuccess || !C::SPLIT_REGS) return e;
+        // a split of more registers than the block has would wait forever
+        cudaFuncAttributes at;
+        e = cudaFuncGetAttributes(&at, k_q8_tc<NT>);
+        if (e != cudaSuccess) return e;
+        if (at.numRegs * TC_THREADS < REGS_SUM || at.numRegs < REGS_CONV || at.numRegs > REGS_EPI)
+            return cudaErrorInvalidConfiguration;
+        return cudaSuccess;
+    }();
+    return done;
+}
+
+// SM pairs that can be at work at once (0: an error); every tile width takes a whole SM
+int resident_pairs() {
+    static int resident = [] {
+        cudaLaunchAttribute attr[1];
+        cudaLaunchConfig_t cfg = tc_config<192>(attr);
         cfg.gridDim = dim3(2 * kPairs);
         int n = 0;
-        e = cudaOccupancyMaxActiveClusters(&n, kern, &cfg);
-        if (e != cudaSuccess) return e;
-        if (n < 1) return cudaErrorInvalidConfiguration;
-        resident = n;
-    }
-    const long long items = (long long)p.tiles_n * p.tiles_t * p.splits;
-    cfg.gridDim = dim3(2 * (unsigned)(items < resident ? items : resident));
-    const Q8Tc a{q.T, q.N, q.K, p.tiles_n, p.tiles_t, p.splits, p.blocks, p.per, q.x_scale, q.w_scale, q.out, s.partial,
-                 s.ticket};
-    return cudaLaunchKernelEx(&cfg, kern, map_w, map_x, a);
+        if (tc_setup<192>() != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, k_q8_tc<192>, &cfg) != cudaSuccess)
+            return 0;
+        return std::min(n, kPairs);
+    }();
+    return resident;
+}
+
+template <int NT>
+cudaError_t launch_tc(const Q8Args &q, const Q8Plan &p, const Q8Scratch &s, int pairs, cudaStream_t st) {
+    cudaError_t e = tc_setup<NT>();
+    if (e != cudaSuccess) return e;
+    CUtensorMap map_w, map_x;
+    if (!row_map(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, q.w, q.N, q.K, q.ld_w, 128) ||
+        !row_map(&map_x, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, s.x, q.T, q.K, s.ld, NT / 2))
+        return cudaErrorInvalidValue;
+    cudaLaunchAttribute attr[1];
+    cudaLaunchConfig_t cfg = tc_config<NT>(attr);
+    cfg.stream = st;
+    cfg.gridDim = dim3(2 * (unsigned)(p.share ? pairs : std::min(p.whole, pairs)));
+    const Q8Tc a{q.T, q.N, q.K, p, q.x_scale, q.w_scale, q.out, s.partial, s.ticket};
+    return cudaLaunchKernelEx(&cfg, k_q8_tc<NT>, map_w, map_x, a);
 }
 
 bool use_tc(const Q8Args &a) {
@@ -650,28 +697,31 @@ bool use_tc(const Q8Args &a) {
 
 size_t q8_workspace_bytes(int T, int N, int K) {
     if (T < kTcMinTokens || N < 1 || K < 1) return 256;
-    return 256 + q8_scratch(nullptr, T, K, q8_plan(T, N, K)).bytes;
+    // whatever the plan: the fp16 tokens, and fewer than kPairs cut tiles of at most 192 tokens
+    const long long cut = std::min<long long>((long long)((N + 255) / 256) * ((T + 31) / 32), kPairs);
+    return (size_t)T * ((K + 7) / 8 * 8) * 2 + 512 + (size_t)cut * (64 + 1024 * 192);
 }
 
 cudaError_t launch_q8_product(const Q8Args &a, void *workspace, cudaStream_t st) {
     if (a.T == 0 || a.N == 0) return cudaSuccess;
     const bool x_aligned = ((reinterpret_cast<uintptr_t>(a.x) | (uintptr_t)a.ld_x) & 15) == 0;
     if (use_tc(a)) {
-        const Q8Plan p = q8_plan(a.T, a.N, a.K);
+        const int pairs = resident_pairs();
+        if (pairs < 1) return cudaErrorInvalidConfiguration;
+        const Q8Plan p = q8_plan(a.T, a.N, a.K, pairs);
         const Q8Scratch s = q8_scratch(workspace, a.T, a.K, p);
-        const int tickets = p.splits > 1 ? p.tiles_n * p.tiles_t * 16 : 0;
-        const long long threads = std::max((long long)a.T * ((s.ld + 15) / 16), (long long)tickets);
+        const long long threads = std::max((long long)a.T * ((s.ld + 15) / 16), s.zeros);
         k_q8_half<<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(a.x, a.ld_x, a.T, a.K, s.x, s.ld, x_aligned,
-                                                                    s.ticket, tickets);
+                                                                    (uint4 *)s.ticket, s.zeros);
         cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
         switch (p.nt) {
-            case 32: return launch_tc<32>(a, p, s, st);
-            case 64: return launch_tc<64>(a, p, s, st);
-            case 96: return launch_tc<96>(a, p, s, st);
-            case 128: return launch_tc<128>(a, p, s, st);
-            case 160: return launch_tc<160>(a, p, s, st);
-            default: return launch_tc<192>(a, p, s, st);
+            case 32: return launch_tc<32>(a, p, s, pairs, st);
+            case 64: return launch_tc<64>(a, p, s, pairs, st);
+            case 96: return launch_tc<96>(a, p, s, pairs, st);
+            case 128: return launch_tc<128>(a, p, s, pairs, st);
+            case 160: return launch_tc<160>(a, p, s, pairs, st);
+            default: return launch_tc<192>(a, p, s, pairs, st);
         }
     }
     constexpr int TT = 8, R = 2;

@@ -83,6 +83,20 @@ static __device__ __forceinline__ bool mbar_wait_spin(uint64_t *bar, uint32_t pa
     }
 }
 
+// the same bound on the SM's cycle counter: reading %globaltimer takes longer
+// than most waits of a pipeline with short steps
+constexpr long long WAIT_CYCLES = 4000000000ll;  // about 2 s
+static __device__ __forceinline__ bool mbar_wait_cycles(uint64_t *bar, uint32_t parity) {
+    for (int i = 0; i < 16; ++i)
+        if (mbar_try_wait_now(bar, parity)) return true;
+    const long long t0 = clock64();
+    for (;;) {
+        for (int i = 0; i < 32; ++i)
+            if (mbar_try_wait_now(bar, parity)) return true;
+        if (clock64() - t0 > WAIT_CYCLES) return false;
+    }
+}
+
 // bounded wait: false if the phase did not complete within limit_ns
 static __device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity,
                                           unsigned long long limit_ns = WAIT_NS) {
@@ -113,6 +127,24 @@ static __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorM
             "r"(dst),
         "l"((uint64_t)map), "r"(x), "r"(y), "r"(smem_u32(bar))
         : "memory");
+}
+
+// one lane of a converged warp. Issuing tensor-core and copy instructions under
+// this predicate, inside a loop that the whole warp runs, keeps their operands
+// in uniform registers; from a branch on the lane number each instruction took
+// over 100 cycles to issue.
+static __device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "elect.sync _|p, 0xffffffff;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(p)
+        :
+        : "memory");
+    return p != 0;
 }
 
 static __device__ __forceinline__ uint32_t cluster_ctarank() {
@@ -246,27 +278,11 @@ static __device__ __forceinline__ bool mbar_wait_cluster(uint64_t *bar, uint32_t
     }
 }
 
-// the same for threads on a pipeline's critical path: no suspend-time hint, no sleep
-static __device__ __forceinline__ bool mbar_wait_cluster_spin(uint64_t *bar, uint32_t parity) {
-    uint64_t t0 = 0;
-    for (int i = 0;; ++i) {
-        uint32_t ok;
-        asm volatile(
-            "{\n"
-            ".reg .pred p;\n"
-            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
-            "selp.u32 %0, 1, 0, p;\n"
-            "}\n"
-            : "=r"(ok)
-            : "r"(smem_u32(bar)), "r"(parity)
-            : "memory");
-        if (ok) return true;
-        if ((i & 31) == 31) {
-            const uint64_t t = globaltimer();
-            if (t0 == 0) t0 = t;
-            else if (t - t0 > WAIT_NS) return false;
-        }
-    }
+// arrive on a barrier of either CTA of the pair, for a peer that goes on to
+// tensor memory only: tcgen05 fences order that, so no cluster-scope release
+// of ordinary memory is paid for (nor an acquire by the waiting side)
+static __device__ __forceinline__ void mbar_arrive_pair(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 // A in TMEM (each lane a row, two 16-bit elements of K per column), B in the
@@ -283,13 +299,15 @@ static __device__ __forceinline__ void mma_pair_ts(uint32_t d_tmem, uint32_t a_t
         : "memory");
 }
 
-// 32 lanes x 32 consecutive 32-bit columns from registers; complete on return
+static __device__ __forceinline__ void tmem_st_wait() {
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+// 32 lanes x 32 consecutive 32-bit columns from registers; tmem_st_wait() completes it
 static __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
         "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};\n"
-        "tcgen05.wait::st.sync.aligned;\n" ::"r"(r[0]),
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};\n" ::"r"(r[0]),
         "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
         "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
         "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
