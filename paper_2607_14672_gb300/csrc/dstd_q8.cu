@@ -45,15 +45,110 @@ __device__ __forceinline__ RowCode row_code(unsigned top_bits) {
 // an infinity times pre = 0 is NaN, whose conversion to an integer is 0
 __device__ __forceinline__ int code_of(float x, const RowCode &c) { return __float2int_rn((x * c.pre) * c.inv); }
 
+// Four consecutive elements, the first at a multiple of four elements from an
+// address that the launch has checked; one at a time at the row's end.
+__device__ __forceinline__ void load4(const float *p, float (&x)[4]) {
+    const float4 v = *reinterpret_cast<const float4 *>(p);
+    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+}
+__device__ __forceinline__ void load4(const __nv_bfloat16 *p, float (&x)[4]) {
+    const uint2 u = *reinterpret_cast<const uint2 *>(p);
+    x[0] = __uint_as_float(u.x << 16), x[1] = __uint_as_float(u.x & 0xffff0000u);
+    x[2] = __uint_as_float(u.y << 16), x[3] = __uint_as_float(u.y & 0xffff0000u);
+}
+__device__ __forceinline__ void load4(const __half *p, float (&x)[4]) {
+    const uint2 u = *reinterpret_cast<const uint2 *>(p);
+    const float2 lo = __half22float2(*reinterpret_cast<const __half2 *>(&u.x));
+    const float2 hi = __half22float2(*reinterpret_cast<const __half2 *>(&u.y));
+    x[0] = lo.x, x[1] = lo.y, x[2] = hi.x, x[3] = hi.y;
+}
+
+struct QuantArgs {
+    int rows, cols;
+    long long ld_x, ld_q, ld_v;
+    int8_t *q;
+    float *scale, *values;
+};
+
+// One pass: THREADS threads (a warp, or a whole block) hold their row in E
+// registers each, find the largest |x|, and write. VEC elements at a time:
+// four where every row's start allows it, else one (loads and stores of
+// neighbouring threads are still neighbours).
+template <class T, int VEC, int E, int THREADS, int BLOCK = THREADS == 32 ? 256 : THREADS>
+__global__ void __launch_bounds__(BLOCK) k_quantize_rows(const T *__restrict__ x, const QuantArgs a) {
+    __shared__ unsigned s_top[32];
+    const int t = threadIdx.x % THREADS;
+    const long long r = (long long)blockIdx.x * (BLOCK / THREADS) + threadIdx.x / THREADS;
+    if (r >= a.rows) return;  // a whole warp, or never
+    const T *row = x + r * a.ld_x;
+    float v[E / VEC][VEC];
+    unsigned top = 0;
+#pragma unroll
+    for (int j = 0; j < E / VEC; ++j) {
+        const int k = (j * THREADS + t) * VEC;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[j][i] = 0.f;
+        if constexpr (VEC == 4) {
+            if (k + 4 <= a.cols) {
+                load4(row + k, v[j]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (k + i < a.cols) v[j][i] = to_f32<T>(row[k + i]);
+            }
+        } else {
+            if (k < a.cols) v[j][0] = to_f32<T>(row[k]);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < E / VEC; ++j)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) top = max(top, __float_as_uint(v[j][i]) & 0x7fffffffu);
+    top = __reduce_max_sync(0xffffffffu, top);
+    if constexpr (THREADS > 32) {
+        if ((t & 31) == 0) s_top[t >> 5] = top;
+        __syncthreads();
+        top = s_top[(t & 31) % (THREADS / 32)];
+        top = __reduce_max_sync(0xffffffffu, top);
+    }
+    const RowCode c = row_code(top);
+    if (t == 0) a.scale[r] = c.scale;
+    int8_t *q = a.q + r * a.ld_q;
+    float *val = a.values ? a.values + r * a.ld_v : nullptr;
+#pragma unroll
+    for (int j = 0; j < E / VEC; ++j) {
+        const int k = (j * THREADS + t) * VEC;
+        if (k >= a.cols) break;
+        int n[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) n[i] = code_of(v[j][i], c);
+        if constexpr (VEC == 4) {
+            if (k + 4 <= a.cols) {
+                *reinterpret_cast<char4 *>(q + k) = make_char4((char)n[0], (char)n[1], (char)n[2], (char)n[3]);
+                if (val)
+                    *reinterpret_cast<float4 *>(val + k) =
+                        make_float4(n[0] * c.scale, n[1] * c.scale, n[2] * c.scale, n[3] * c.scale);
+                continue;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+            if (k + i < a.cols) {
+                q[k + i] = (int8_t)n[i];
+                if (val) val[k + i] = n[i] * c.scale;
+            }
+    }
+}
+
+// rows too long for the registers: read twice (the second time mostly from L2)
 template <class T>
-__global__ void __launch_bounds__(256) k_quantize_rows(const T *__restrict__ x, int cols, long long ld_x, int8_t *q,
-                                                       long long ld_q, float *scale, float *values,
-                                                       long long ld_v) {
+__global__ void __launch_bounds__(256) k_quantize_long(const T *__restrict__ x, const QuantArgs a) {
     __shared__ unsigned s_top[8];
     const long long r = blockIdx.x;
-    const T *row = x + r * ld_x;
+    const T *row = x + r * a.ld_x;
     unsigned top = 0;
-    for (int k = threadIdx.x; k < cols; k += 256)
+#pragma unroll 8
+    for (int k = threadIdx.x; k < a.cols; k += 256)
         top = max(top, __float_as_uint(to_f32<T>(row[k])) & 0x7fffffffu);
     top = __reduce_max_sync(0xffffffffu, top);
     if ((threadIdx.x & 31) == 0) s_top[threadIdx.x >> 5] = top;
@@ -61,24 +156,46 @@ __global__ void __launch_bounds__(256) k_quantize_rows(const T *__restrict__ x, 
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = max(top, s_top[i]);
     const RowCode c = row_code(top);
-    if (threadIdx.x == 0) scale[r] = c.scale;
-    for (int k = threadIdx.x; k < cols; k += 256) {
+    if (threadIdx.x == 0) a.scale[r] = c.scale;
+#pragma unroll 4
+    for (int k = threadIdx.x; k < a.cols; k += 256) {
         const int v = code_of(to_f32<T>(row[k]), c);
-        q[r * ld_q + k] = (int8_t)v;
-        if (values) values[r * ld_v + k] = (float)v * c.scale;
+        a.q[r * a.ld_q + k] = (int8_t)v;
+        if (a.values) a.values[r * a.ld_v + k] = (float)v * c.scale;
+    }
+}
+
+template <class T>
+void quantize(const T *x, const QuantArgs &a, cudaStream_t st) {
+    const uintptr_t x4 = 4 * sizeof(T) - 1;
+    const bool vec = ((reinterpret_cast<uintptr_t>(x) & x4) | (a.ld_x & 3)) == 0 &&
+                     ((reinterpret_cast<uintptr_t>(a.q) | a.ld_q) & 3) == 0 &&
+                     (!a.values || ((reinterpret_cast<uintptr_t>(a.values) & 15) | (a.ld_v & 3)) == 0);
+    const unsigned rows = (unsigned)a.rows, warps = (rows + 7) / 8;
+    if (a.cols <= 256) {
+        if (vec) k_quantize_rows<T, 4, 8, 32><<<warps, 256, 0, st>>>(x, a);
+        else k_quantize_rows<T, 1, 8, 32><<<warps, 256, 0, st>>>(x, a);
+    } else if (a.cols <= 1024) {
+        if (vec) k_quantize_rows<T, 4, 32, 32><<<warps, 256, 0, st>>>(x, a);
+        else k_quantize_rows<T, 1, 32, 32><<<warps, 256, 0, st>>>(x, a);
+    } else if (a.cols <= 4096) {
+        if (vec) k_quantize_rows<T, 4, 16, 256><<<rows, 256, 0, st>>>(x, a);
+        else k_quantize_rows<T, 1, 16, 256><<<rows, 256, 0, st>>>(x, a);
+    } else if (a.cols <= 16384) {
+        if (vec) k_quantize_rows<T, 4, 16, 1024><<<rows, 1024, 0, st>>>(x, a);
+        else k_quantize_rows<T, 1, 16, 1024><<<rows, 1024, 0, st>>>(x, a);
+    } else {
+        k_quantize_long<T><<<rows, 256, 0, st>>>(x, a);
     }
 }
 
 cudaError_t launch_quantize_rows(const void *x, dstd_type type, int rows, int cols, long long ld_x, int8_t *q,
                                  long long ld_q, float *scale, float *values, long long ld_v, cudaStream_t st) {
     if (rows == 0) return cudaSuccess;
-    if (type == DSTD_TYPE_F32)
-        k_quantize_rows<float><<<rows, 256, 0, st>>>((const float *)x, cols, ld_x, q, ld_q, scale, values, ld_v);
-    else if (type == DSTD_TYPE_BF16)
-        k_quantize_rows<__nv_bfloat16>
-            <<<rows, 256, 0, st>>>((const __nv_bfloat16 *)x, cols, ld_x, q, ld_q, scale, values, ld_v);
-    else
-        k_quantize_rows<__half><<<rows, 256, 0, st>>>((const __half *)x, cols, ld_x, q, ld_q, scale, values, ld_v);
+    const QuantArgs a{rows, cols, ld_x, ld_q, ld_v, q, scale, values};
+    if (type == DSTD_TYPE_F32) quantize((const float *)x, a, st);
+    else if (type == DSTD_TYPE_BF16) quantize((const __nv_bfloat16 *)x, a, st);
+    else quantize((const __half *)x, a, st);
     return cudaGetLastError();
 }
 
