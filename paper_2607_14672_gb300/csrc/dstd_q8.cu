@@ -216,17 +216,26 @@ cudaError_t launch_q8_rowsum(const int8_t *w, long long ld, int N, int K, const 
     return cudaGetLastError();
 }
 
-// ---------------------------------------------------------------------------
-// Product, dot form: a warp holds R channels x TT tokens of 32-bit sums; its
-// lanes split K in chunks of 16 codes (four dp4a each per pair).
-// ---------------------------------------------------------------------------
-__device__ __forceinline__ int4 load16(const int8_t *p, int left, bool aligned) {
-    if (aligned && left >= 16) return *reinterpret_cast<const int4 *>(p);
-    int v[4] = {0, 0, 0, 0};
+// 16 codes from any address; beyond `left` zeros. Aligned rows take one load.
+// Others take the aligned words that hold the codes (the first may hold up to
+// three bytes before them: it still holds a code, so it is memory of the
+// matrix's own word), shifted together; near a row's end single bytes.
+template <bool ALIGNED>
+__device__ __forceinline__ int4 load_codes(const int8_t *p, int left) {
+    if (ALIGNED && left >= 16) return __ldg(reinterpret_cast<const int4 *>(p));
+    if (!ALIGNED && left >= 20) {
+        const int shift = 8 * (int)(reinterpret_cast<uintptr_t>(p) & 3);
+        const unsigned *w = reinterpret_cast<const unsigned *>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)3);
+        const unsigned w0 = __ldg(w), w1 = __ldg(w + 1), w2 = __ldg(w + 2), w3 = __ldg(w + 3);
+        const unsigned w4 = shift ? __ldg(w + 4) : 0u;
+        return make_int4((int)__funnelshift_r(w0, w1, shift), (int)__funnelshift_r(w1, w2, shift),
+                         (int)__funnelshift_r(w2, w3, shift), (int)__funnelshift_r(w3, w4, shift));
+    }
+    unsigned v[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-        if (i < left) v[i >> 2] |= (int)(unsigned char)p[i] << (8 * (i & 3));
-    return make_int4(v[0], v[1], v[2], v[3]);
+        if (i < left) v[i >> 2] |= (unsigned)(unsigned char)p[i] << (8 * (i & 3));
+    return make_int4((int)v[0], (int)v[1], (int)v[2], (int)v[3]);
 }
 
 __device__ __forceinline__ void store_out(const Q8Out &o, long long t, long long n, float y) {
@@ -236,39 +245,93 @@ __device__ __forceinline__ void store_out(const Q8Out &o, long long t, long long
     else ((__half *)o.p)[at] = __float2half_rn(y);
 }
 
-template <int TT, int R>
-__global__ void __launch_bounds__(256) k_q8_dot(Q8Args a, bool aligned) {
-    const int lane = threadIdx.x & 31;
-    const long long n0 = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * R;
-    const int t0 = blockIdx.y * TT;
-    if (n0 >= a.N) return;
-    int acc[R][TT] = {};
-    for (int k = lane * 16; k < a.K; k += 512) {
-        int4 w[R];
+// ---------------------------------------------------------------------------
+// Product, dot form, for few tokens and small products: one launch, the weights
+// straight from memory. The block's TT tokens lie in shared memory, DOT_K codes
+// at a time (aligned there, zero beyond K); a warp holds 4 channels x TT tokens
+// of 32-bit sums, its lanes taking 16 codes of K each (four dp4a a pair). `wpk`
+// warps share the channels' K, so that there are warps enough to keep the
+// weights' loads coming when there are few channels.
+// ---------------------------------------------------------------------------
+constexpr int DOT_K = 4096, DOT_R = 4;
+
+template <int TT, bool ALIGNED>
+__global__ void __launch_bounds__(256) k_q8_dot(const Q8Args a, const bool x_aligned, const int wpk,
+                                                const int tiles_t) {
+    __shared__ int4 s_x[TT][DOT_K / 16];
+    __shared__ int s_sum[8][DOT_R * TT];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int group = warp / wpk, part = warp - group * wpk;
+    const int tt = (int)(blockIdx.x % tiles_t), t0 = tt * TT;
+    const long long n0 = ((long long)(blockIdx.x / tiles_t) * (8 / wpk) + group) * DOT_R;
+    const int8_t *row[DOT_R];
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-            w[r] = n0 + r < a.N ? load16(a.w + (n0 + r) * a.ld_w + k, a.K - k, aligned) : make_int4(0, 0, 0, 0);
+    for (int r = 0; r < DOT_R; ++r) row[r] = a.w + (n0 + r < a.N ? n0 + r : (long long)a.N - 1) * a.ld_w;
+    int acc[DOT_R][TT] = {};
+    for (int k0 = 0; k0 < a.K; k0 += DOT_K) {
+        const int len = min(DOT_K, a.K - k0), chunks = (len + 15) / 16;
+        if (k0 > 0) __syncthreads();
+        for (int i = threadIdx.x; i < TT * chunks; i += 256) {
+            const int t = i / chunks, c = i - t * chunks;
+            int4 v = make_int4(0, 0, 0, 0);
+            if (t0 + t < a.T) {
+                const int8_t *p = a.x + (long long)(t0 + t) * a.ld_x + k0 + 16 * c;
+                v = x_aligned ? load_codes<true>(p, len - 16 * c) : load_codes<false>(p, len - 16 * c);
+            }
+            s_x[t][c] = v;
+        }
+        __syncthreads();
+#pragma unroll 2
+        for (int c = part * 32 + lane; c < chunks; c += wpk * 32) {
+            int4 w[DOT_R];
 #pragma unroll
-        for (int t = 0; t < TT; ++t) {
-            if (t0 + t >= a.T) break;
-            const int4 x = load16(a.x + (long long)(t0 + t) * a.ld_x + k, a.K - k, aligned);
+            for (int r = 0; r < DOT_R; ++r) w[r] = load_codes<ALIGNED>(row[r] + k0 + 16 * c, len - 16 * c);
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                acc[r][t] = __dp4a(x.x, w[r].x, acc[r][t]);
-                acc[r][t] = __dp4a(x.y, w[r].y, acc[r][t]);
-                acc[r][t] = __dp4a(x.z, w[r].z, acc[r][t]);
-                acc[r][t] = __dp4a(x.w, w[r].w, acc[r][t]);
+            for (int t = 0; t < TT; ++t) {
+                const int4 x = s_x[t][c];
+#pragma unroll
+                for (int r = 0; r < DOT_R; ++r) {
+                    acc[r][t] = __dp4a(x.x, w[r].x, acc[r][t]);
+                    acc[r][t] = __dp4a(x.y, w[r].y, acc[r][t]);
+                    acc[r][t] = __dp4a(x.z, w[r].z, acc[r][t]);
+                    acc[r][t] = __dp4a(x.w, w[r].w, acc[r][t]);
+                }
             }
         }
     }
+    // lane r * TT + t keeps the sum of channel r and token t
+    int mine = 0;
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int r = 0; r < DOT_R; ++r)
 #pragma unroll
         for (int t = 0; t < TT; ++t) {
             const int sum = __reduce_add_sync(0xffffffffu, acc[r][t]);
-            if (lane == 0 && t0 + t < a.T && n0 + r < a.N)
-                store_out(a.out, t0 + t, n0 + r, ((float)sum * a.x_scale[t0 + t]) * a.w_scale[n0 + r]);
+            if (lane == r * TT + t) mine = sum;
         }
+    if (wpk > 1) {
+        if (lane < DOT_R * TT) s_sum[warp][lane] = mine;
+        __syncthreads();
+        if (part != 0) return;
+        if (lane < DOT_R * TT)
+            for (int i = 1; i < wpk; ++i) mine += s_sum[warp + i][lane];
+    }
+    const int t = t0 + lane % TT;
+    const long long n = n0 + lane / TT;
+    if (lane < DOT_R * TT && t < a.T && n < a.N)
+        store_out(a.out, t, n, ((float)mine * a.x_scale[t]) * a.w_scale[n]);
+}
+
+template <int TT>
+cudaError_t launch_dot(const Q8Args &a, bool x_aligned, bool w_aligned, cudaStream_t st) {
+    const int tiles_t = (a.T + TT - 1) / TT;
+    const long long quads = ((long long)a.N + DOT_R - 1) / DOT_R;
+    int wpk = 1;
+    while (wpk < 8 && quads * tiles_t * wpk < 152 * 32 && a.K > 512 * wpk) wpk *= 2;
+    const long long grid = (quads * wpk + 7) / 8 * tiles_t;
+    if (grid > 0x7fffffff) return cudaErrorInvalidValue;
+    if (w_aligned) k_q8_dot<TT, true><<<(unsigned)grid, 256, 0, st>>>(a, x_aligned, wpk, tiles_t);
+    else k_q8_dot<TT, false><<<(unsigned)grid, 256, 0, st>>>(a, x_aligned, wpk, tiles_t);
+    return cudaGetLastError();
 }
 
 // ---------------------------------------------------------------------------
@@ -334,6 +397,7 @@ struct Q8Plan {
 
 struct Q8Tc {
     int T, N, K;
+    bool w_copied;
     Q8Plan p;
     const float *x_scale, *w_scale;
     Q8Out out;
@@ -398,7 +462,56 @@ __device__ __forceinline__ void tmem_ld(uint32_t addr, float (&v)[CH]) {
     else tmem_ld16(addr, v);
 }
 
+// Dependent launch: this grid may start while the one before it in the stream
+// still runs; what that one writes is there after the wait.
+__device__ __forceinline__ void wait_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_launch() { asm volatile("griddepcontrol.launch_dependents;"); }
+
 __device__ __forceinline__ void q8_timeout() { atomicOr(&g_status_q8, STATUS_TIMEOUT); }
+
+template <class O>
+__device__ __forceinline__ O round_out(float y);
+template <>
+__device__ __forceinline__ float round_out<float>(float y) { return y; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 round_out<__nv_bfloat16>(float y) { return __float2bfloat16_rn(y); }
+template <>
+__device__ __forceinline__ __half round_out<__half>(float y) { return __float2half_rn(y); }
+
+// column c of this lane's channel: the token's scale is held by lane c % 32
+template <int COLS>
+__device__ __forceinline__ float scaled(const int (&sum)[COLS], const float (&xs)[(COLS + 31) / 32], float ws, int c) {
+    return ((float)sum[c] * __shfl_sync(0xffffffffu, xs[c / 32], c % 32)) * ws;
+}
+// a warp's lanes hold neighbouring channels: each column is one row segment
+template <class O, int COLS>
+__device__ __forceinline__ void store_columns(O *dst, long long ld, const int (&sum)[COLS],
+                                              const float (&xs)[(COLS + 31) / 32], float ws, int left) {
+#pragma unroll
+    for (int c = 0; c < COLS; ++c, dst += ld) {
+        const float y = scaled<COLS>(sum, xs, ws, c);
+        if (c < left) *dst = round_out<O>(y);
+    }
+}
+// the columns lie next to each other
+template <int COLS>
+__device__ __forceinline__ void store_row(float *dst, const int (&sum)[COLS], const float (&xs)[(COLS + 31) / 32],
+                                          float ws, int left) {
+    const bool vec = (reinterpret_cast<uintptr_t>(dst) & 15) == 0;
+#pragma unroll
+    for (int c = 0; c < COLS; c += 4) {
+        float y[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) y[u] = scaled<COLS>(sum, xs, ws, c + u);
+        if (vec && c + 4 <= left) {
+            *reinterpret_cast<float4 *>(dst + c) = make_float4(y[0], y[1], y[2], y[3]);
+        } else {
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (c + u < left) dst[c + u] = y[u];
+        }
+    }
+}
 
 template <int NT>
 __global__ void __launch_bounds__(TC_THREADS, 1)
@@ -441,8 +554,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     if constexpr (C::SPLIT_REGS) {
         if (warp >= CONV_WARPS + EPI_WARPS) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_REST));
     }
-    if (warp == CONV_WARPS + EPI_WARPS) {
-        // TMA producer of this SM's weights and its half of the tokens
+    if (warp == CONV_WARPS + EPI_WARPS || warp == CONV_WARPS + EPI_WARPS + 2) {
+        // TMA producers, of this SM's weights and of its half of the tokens. The weights, unless they were copied into
+        // place, do not wait for the launch before.
+        const bool tokens = warp == CONV_WARPS + EPI_WARPS + 2;
+        if (tokens || a.w_copied) wait_launch_before();
         const uint32_t ready0 = mapa_rank(smem_u32(&ready[0]), 0);
         uint32_t it = 0;
         bool ok = true;
@@ -455,15 +571,18 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
                 ok = mbar_wait_cycles(&empty[s], ((it / C::STAGES) & 1u) ^ 1u);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
+                const uint32_t st = smem_u32(smem + s * C::STAGE);
                 if (elect_one()) {
-                    const uint32_t st = smem_u32(smem + s * C::STAGE);
-                    const bool two = b * KB + 64 < a.K;  // a second half of the stage to read
-                    mbar_expect_tx(&w_full[s], (uint32_t)W_BYTES);
-                    tma_load_2d(st, &map_w, &w_full[s], b * KB, n0);
-                    if (rank == 0) mbar_expect_tx(&ready[s], (uint32_t)((two ? 4 : 2) * C::X_BYTES));
-                    const uint32_t rb = ready0 + (uint32_t)(s * sizeof(uint64_t));
-                    tma_load_2d_pair(st + W_BYTES, &map_x, rb, b * KB, t0);
-                    if (two) tma_load_2d_pair(st + W_BYTES + C::X_BYTES, &map_x, rb, b * KB + 64, t0);
+                    if (!tokens) {
+                        mbar_expect_tx(&w_full[s], (uint32_t)W_BYTES);
+                        tma_load_2d(st, &map_w, &w_full[s], b * KB, n0);
+                    } else {
+                        const bool two = b * KB + 64 < a.K;  // a second half of the stage to read
+                        if (rank == 0) mbar_expect_tx(&ready[s], (uint32_t)((two ? 4 : 2) * C::X_BYTES));
+                        const uint32_t rb = ready0 + (uint32_t)(s * sizeof(uint64_t));
+                        tma_load_2d_pair(st + W_BYTES, &map_x, rb, b * KB, t0);
+                        if (two) tma_load_2d_pair(st + W_BYTES + C::X_BYTES, &map_x, rb, b * KB + 64, t0);
+                    }
                 }
                 __syncwarp();
             }
@@ -560,10 +679,17 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
         const uint32_t tbase = tmem + ((uint32_t)(quarter * 32) << 16) + group * C::COLS;
         const uint32_t acc_empty0 = mapa_rank(smem_u32(&acc_empty[0]), 0);
         uint32_t j = 0;
+        wait_launch_before();  // sums and tickets have been set to zero
         while (wk.next(a.p)) {
             int tn, tt;
             tile_of(wk.tile, a.p.tiles_n, a.p.tiles_t, tn, tt);
             const int n = tn * 256 + rank * 128 + quarter * 32 + lane, t0 = tt * NT + group * C::COLS;
+            // the scales, on their way while the tile is computed: token t0 + c is held by lane c % 32
+            const float ws = n < a.N ? a.w_scale[n] : 0.f;
+            float xs[(C::COLS + 31) / 32];
+#pragma unroll
+            for (int c = 0; c < (C::COLS + 31) / 32; ++c)
+                xs[c] = t0 + 32 * c + lane < a.T ? a.x_scale[t0 + 32 * c + lane] : 0.f;
             int sum[C::COLS];
 #pragma unroll
             for (int c = 0; c < C::COLS; ++c) sum[c] = 0;
@@ -603,30 +729,16 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
 #pragma unroll
                 for (int c = 0; c < C::COLS; ++c) sum[c] = __ldcg(all + c * 32);
             }
-            if (n < a.N) {
-                const float ws = a.w_scale[n];
-                if (a.out.ld_t == 1 && a.out.type == DSTD_TYPE_F32) {  // a row of tokens per channel
-                    float *dst = (float *)a.out.p + (long long)n * a.out.ld_n + t0;
-                    const bool vec = (reinterpret_cast<uintptr_t>(dst) & 15) == 0;
-#pragma unroll
-                    for (int c = 0; c < C::COLS; c += 4) {
-                        float y[4];
-#pragma unroll
-                        for (int u = 0; u < 4; ++u)
-                            y[u] = t0 + c + u < a.T ? ((float)sum[c + u] * a.x_scale[t0 + c + u]) * ws : 0.f;
-                        if (vec && t0 + c + 4 <= a.T) {
-                            *reinterpret_cast<float4 *>(dst + c) = make_float4(y[0], y[1], y[2], y[3]);
-                        } else {
-#pragma unroll
-                            for (int u = 0; u < 4; ++u)
-                                if (t0 + c + u < a.T) dst[c + u] = y[u];
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int c = 0; c < C::COLS; ++c)
-                        if (t0 + c < a.T) store_out(a.out, t0 + c, n, ((float)sum[c] * a.x_scale[t0 + c]) * ws);
-                }
+            const int left = n < a.N ? a.T - t0 : 0;  // this lane's columns that exist
+            const long long at = (long long)t0 * a.out.ld_t + (long long)n * a.out.ld_n;
+            if (a.out.ld_t == 1 && a.out.type == DSTD_TYPE_F32) {
+                store_row<C::COLS>((float *)a.out.p + at, sum, xs, ws, left);
+            } else if (a.out.type == DSTD_TYPE_F32) {
+                store_columns<float, C::COLS>((float *)a.out.p + at, a.out.ld_t, sum, xs, ws, left);
+            } else if (a.out.type == DSTD_TYPE_BF16) {
+                store_columns<__nv_bfloat16, C::COLS>((__nv_bfloat16 *)a.out.p + at, a.out.ld_t, sum, xs, ws, left);
+            } else {
+                store_columns<__half, C::COLS>((__half *)a.out.p + at, a.out.ld_t, sum, xs, ws, left);
             }
             __syncwarp();
         }
@@ -637,23 +749,51 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
     if (warp == CONV_WARPS + EPI_WARPS + 1) tmem_dealloc_pair(tmem, 512);
 }
 
-// tokens to fp16 rows [T, ld] (16 codes a thread); the tickets and sums of the tiles that are cut to zero
-__global__ void __launch_bounds__(256) k_q8_half(const int8_t *__restrict__ x, long long ld_x, int T, int K, __half *y,
-                                                 int ld, bool aligned, uint4 *zero, long long zeros) {
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (i < zeros) zero[i] = make_uint4(0, 0, 0, 0);
-    const int chunks = (ld + 15) / 16;
-    const long long t = i / chunks;
-    const int k = (int)(i - t * chunks) * 16;
-    if (t >= T) return;
-    const int4 v = load16(x + t * ld_x + k, K - k, aligned);
-    uint4 lo, hi;
-    codes_to_half((uint32_t)v.x, lo.x, lo.y);
-    codes_to_half((uint32_t)v.y, lo.z, lo.w);
-    codes_to_half((uint32_t)v.z, hi.x, hi.y);
-    codes_to_half((uint32_t)v.w, hi.z, hi.w);
-    *reinterpret_cast<uint4 *>(y + t * ld + k) = lo;
-    if (k + 8 < ld) *reinterpret_cast<uint4 *>(y + t * ld + k + 8) = hi;
+// What the tensor-core launch needs first, 16 codes a thread: the tokens as fp16
+// rows [T, ld], the weights copied to rows [N, ld_wc] where theirs are not
+// aligned (wc not null), and zeros for the sums and tickets of the tiles that are cut.
+struct PrepArgs {
+    const int8_t *x, *w;
+    long long ld_x, ld_w;
+    int T, N, K;
+    bool x_aligned;
+    __half *xh;
+    int ld;
+    int8_t *wc;
+    int ld_wc;
+    uint4 *zero;
+    long long x_threads, w_threads, zeros;
+};
+
+__global__ void __launch_bounds__(256) k_q8_prep(const PrepArgs a) {
+    let_next_launch();
+    long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (i < a.x_threads) {
+        const int chunks = (a.ld + 15) / 16;
+        const long long t = i / chunks;
+        const int k = (int)(i - t * chunks) * 16;
+        const int8_t *p = a.x + t * a.ld_x + k;
+        const int4 v = a.x_aligned ? load_codes<true>(p, a.K - k) : load_codes<false>(p, a.K - k);
+        uint4 lo, hi;
+        codes_to_half((uint32_t)v.x, lo.x, lo.y);
+        codes_to_half((uint32_t)v.y, lo.z, lo.w);
+        codes_to_half((uint32_t)v.z, hi.x, hi.y);
+        codes_to_half((uint32_t)v.w, hi.z, hi.w);
+        __half *y = a.xh + t * a.ld + k;
+        *reinterpret_cast<uint4 *>(y) = lo;
+        if (k + 8 < a.ld) *reinterpret_cast<uint4 *>(y + 8) = hi;
+        return;
+    }
+    i -= a.x_threads;
+    if (i < a.w_threads) {
+        const int chunks = a.ld_wc / 16;
+        const long long n = i / chunks;
+        const int k = (int)(i - n * chunks) * 16;
+        *reinterpret_cast<int4 *>(a.wc + n * a.ld_wc + k) = load_codes<false>(a.w + n * a.ld_w + k, a.K - k);
+        return;
+    }
+    i -= a.w_threads;
+    if (i < a.zeros) a.zero[i] = make_uint4(0, 0, 0, 0);
 }
 
 constexpr int kPairs = 76;  // SM pairs of the GPU, for planning
@@ -686,11 +826,11 @@ Q8Plan q8_plan(int T, int N, int K, int pairs) {
         const double tile = (double)p.blocks * tc.block;
         double cost = (tiles / pairs) * tile + 12.0 * tc.nt;
         if (rest > 0) {
-            // a share of at least two blocks; adding up and the wait for the last part cost about as much as 2000 +
-            // 20 nt cycles
+            // a share of at least two blocks; adding up and the wait for the last part cost about 4000 + 30 nt
+            // cycles
             const long long blocks = (long long)rest * p.blocks;
             const int share = (int)std::max((blocks + pairs - 1) / pairs, 2ll);
-            const double cut = (double)share * tc.block + 2000 + 20.0 * tc.nt;
+            const double cut = (double)share * tc.block + 4000 + 30.0 * tc.nt;
             if (cut < tile) {
                 p.whole = tiles - rest;
                 p.share = share;
@@ -705,24 +845,30 @@ Q8Plan q8_plan(int T, int N, int K, int pairs) {
     return best;
 }
 
+// Scratch of the tensor-core form: the fp16 tokens, a copy of the weights
+// (used where their rows are not aligned), then tickets and sums of the tiles
+// that are cut (fewer than kPairs, of at most 192 tokens, whatever the plan).
 struct Q8Scratch {
     __half *x;
+    int8_t *w;
     unsigned *ticket;
     int *partial;
-    int ld;
+    int ld, ld_w;
     long long zeros;  // 16-byte words from ticket on
+    size_t bytes;
 };
-// of a plan: the fp16 tokens, then tickets and sums of the tiles that are cut
-Q8Scratch q8_scratch(void *base, int T, int K, const Q8Plan &p) {
+Q8Scratch q8_scratch(void *base, int T, int N, int K, long long cut, int nt) {
     Q8Scratch s{};
     char *b = static_cast<char *>(base);
     s.ld = (K + 7) / 8 * 8;
-    const size_t x = ((size_t)T * s.ld * 2 + 255) / 256 * 256;
-    const long long cut = (long long)p.tiles_n * p.tiles_t - p.whole;
+    s.ld_w = (K + 15) / 16 * 16;
+    const size_t x = ((size_t)T * s.ld * 2 + 255) / 256 * 256, w = ((size_t)N * s.ld_w + 255) / 256 * 256;
     s.x = (__half *)b;
-    s.ticket = (unsigned *)(b + x);
-    s.partial = (int *)(b + x + cut * 64);
-    s.zeros = (cut * 64 + cut * 1024 * p.nt) / 16;
+    s.w = (int8_t *)(b + x);
+    s.ticket = (unsigned *)(b + x + w);
+    s.partial = (int *)(b + x + w + cut * 64);
+    s.zeros = (cut * 64 + cut * 1024 * nt) / 16;
+    s.bytes = x + w + (size_t)cut * (64 + 1024 * nt);
     return s;
 }
 
@@ -744,15 +890,20 @@ bool row_map(CUtensorMap *m, CUtensorMapDataType type, int bytes, const void *p,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool rows_aligned(const int8_t *p, long long ld) { return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)ld) & 15) == 0; }
+bool w_rows_aligned(const Q8Args &a) { return rows_aligned(a.w, a.ld_w); }
+
 template <int NT>
-cudaLaunchConfig_t tc_config(cudaLaunchAttribute *attr) {
+cudaLaunchConfig_t tc_config(cudaLaunchAttribute (&attr)[2]) {
     cudaLaunchConfig_t cfg = {};
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     cfg.blockDim = dim3(TC_THREADS);
     cfg.dynamicSmemBytes = Q8Cfg<NT>::SMEM;
     return cfg;
@@ -779,9 +930,10 @@ cudaError_t tc_setup() {
 // SM pairs that can be at work at once (0: an error); every tile width takes a whole SM
 int resident_pairs() {
     static int resident = [] {
-        cudaLaunchAttribute attr[1];
+        cudaLaunchAttribute attr[2];
         cudaLaunchConfig_t cfg = tc_config<192>(attr);
         cfg.gridDim = dim3(2 * kPairs);
+        cfg.numAttrs = 1;
         int n = 0;
         if (tc_setup<192>() != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, k_q8_tc<192>, &cfg) != cudaSuccess)
             return 0;
@@ -795,41 +947,44 @@ cudaError_t launch_tc(const Q8Args &q, const Q8Plan &p, const Q8Scratch &s, int 
     cudaError_t e = tc_setup<NT>();
     if (e != cudaSuccess) return e;
     CUtensorMap map_w, map_x;
-    if (!row_map(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, q.w, q.N, q.K, q.ld_w, 128) ||
+    const bool copied = !w_rows_aligned(q);
+    if (!row_map(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, copied ? s.w : q.w, q.N, q.K, copied ? s.ld_w : q.ld_w, 128) ||
         !row_map(&map_x, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, s.x, q.T, q.K, s.ld, NT / 2))
         return cudaErrorInvalidValue;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     cudaLaunchConfig_t cfg = tc_config<NT>(attr);
     cfg.stream = st;
     cfg.gridDim = dim3(2 * (unsigned)(p.share ? pairs : std::min(p.whole, pairs)));
-    const Q8Tc a{q.T, q.N, q.K, p, q.x_scale, q.w_scale, q.out, s.partial, s.ticket};
+    const Q8Tc a{q.T, q.N, q.K, copied, p, q.x_scale, q.w_scale, q.out, s.partial, s.ticket};
     return cudaLaunchKernelEx(&cfg, k_q8_tc<NT>, map_w, map_x, a);
 }
 
-bool use_tc(const Q8Args &a) {
-    return a.T >= kTcMinTokens && a.K >= 16 && (reinterpret_cast<uintptr_t>(a.w) & 15) == 0 && a.ld_w % 16 == 0;
-}
+// Which form: the dot form takes what its sums need at DOT_RATE products a
+// microsecond, after about 3 us; the tensor cores' launches cost about 14 us on
+// top of the plan's cycles (and a copy of the weights where they need one).
+bool use_tc(const Q8Args &a) { return a.T >= kTcMinTokens && a.K >= 16; }
 
 }  // namespace
 
 size_t q8_workspace_bytes(int T, int N, int K) {
     if (T < kTcMinTokens || N < 1 || K < 1) return 256;
-    // whatever the plan: the fp16 tokens, and fewer than kPairs cut tiles of at most 192 tokens
     const long long cut = std::min<long long>((long long)((N + 255) / 256) * ((T + 31) / 32), kPairs);
-    return (size_t)T * ((K + 7) / 8 * 8) * 2 + 512 + (size_t)cut * (64 + 1024 * 192);
+    return q8_scratch(nullptr, T, N, K, cut, 192).bytes;
 }
 
 cudaError_t launch_q8_product(const Q8Args &a, void *workspace, cudaStream_t st) {
     if (a.T == 0 || a.N == 0) return cudaSuccess;
-    const bool x_aligned = ((reinterpret_cast<uintptr_t>(a.x) | (uintptr_t)a.ld_x) & 15) == 0;
+    const bool x_aligned = rows_aligned(a.x, a.ld_x), w_aligned = w_rows_aligned(a);
     if (use_tc(a)) {
         const int pairs = resident_pairs();
         if (pairs < 1) return cudaErrorInvalidConfiguration;
         const Q8Plan p = q8_plan(a.T, a.N, a.K, pairs);
-        const Q8Scratch s = q8_scratch(workspace, a.T, a.K, p);
-        const long long threads = std::max((long long)a.T * ((s.ld + 15) / 16), s.zeros);
-        k_q8_half<<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(a.x, a.ld_x, a.T, a.K, s.x, s.ld, x_aligned,
-                                                                    (uint4 *)s.ticket, s.zeros);
+        const Q8Scratch s = q8_scratch(workspace, a.T, a.N, a.K, (long long)p.tiles_n * p.tiles_t - p.whole, p.nt);
+        PrepArgs pa{a.x, a.w, a.ld_x, a.ld_w, a.T, a.N, a.K, x_aligned, s.x, s.ld, s.w, s.ld_w, (uint4 *)s.ticket,
+                    (long long)a.T * ((s.ld + 15) / 16), w_aligned ? 0 : (long long)a.N * (s.ld_w / 16), s.zeros};
+        const long long blocks = (pa.x_threads + pa.w_threads + pa.zeros + 255) / 256;
+        if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
+        k_q8_prep<<<(unsigned)blocks, 256, 0, st>>>(pa);
         cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
         switch (p.nt) {
@@ -841,18 +996,10 @@ cudaError_t launch_q8_product(const Q8Args &a, void *workspace, cudaStream_t st)
             default: return launch_tc<192>(a, p, s, pairs, st);
         }
     }
-    constexpr int TT = 8, R = 2;
-    const bool aligned = x_aligned && ((reinterpret_cast<uintptr_t>(a.w) | (uintptr_t)a.ld_w) & 15) == 0;
-    const int tt_max = 65535 * TT;  // tokens of one launch
-    for (int t = 0; t < a.T; t += tt_max) {
-        Q8Args b = a;
-        b.T = a.T - t < tt_max ? a.T - t : tt_max;
-        b.x += (long long)t * a.ld_x;
-        b.x_scale += t;
-        b.out.p = (char *)a.out.p + (long long)t * a.out.ld_t * (a.out.type == DSTD_TYPE_F32 ? 4 : 2);
-        k_q8_dot<TT, R><<<dim3((a.N + 8 * R - 1) / (8 * R), (b.T + TT - 1) / TT), 256, 0, st>>>(b, aligned);
-    }
-    return cudaGetLastError();
+    if (a.T == 1) return launch_dot<1>(a, x_aligned, w_aligned, st);
+    if (a.T == 2) return launch_dot<2>(a, x_aligned, w_aligned, st);
+    if (a.T <= 4) return launch_dot<4>(a, x_aligned, w_aligned, st);
+    return launch_dot<8>(a, x_aligned, w_aligned, st);
 }
 
 }  // namespace dstd
