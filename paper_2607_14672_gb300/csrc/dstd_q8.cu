@@ -216,26 +216,54 @@ cudaError_t launch_q8_rowsum(const int8_t *w, long long ld, int N, int K, const 
     return cudaGetLastError();
 }
 
-// 16 codes from any address; beyond `left` zeros. Aligned rows take one load.
-// Others take the aligned words that hold the codes (the first may hold up to
-// three bytes before them: it still holds a code, so it is memory of the
-// matrix's own word), shifted together; near a row's end single bytes.
+// 16 codes from any address. Aligned ones take one load; others the two aligned
+// 16-byte words that hold them, shifted together (the first may begin up to 15
+// bytes before the codes: in the same word as a code, so in the same allocation).
 template <bool ALIGNED>
-__device__ __forceinline__ int4 load_codes(const int8_t *p, int left) {
-    if (ALIGNED && left >= 16) return __ldg(reinterpret_cast<const int4 *>(p));
-    if (!ALIGNED && left >= 20) {
-        const int shift = 8 * (int)(reinterpret_cast<uintptr_t>(p) & 3);
-        const unsigned *w = reinterpret_cast<const unsigned *>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)3);
-        const unsigned w0 = __ldg(w), w1 = __ldg(w + 1), w2 = __ldg(w + 2), w3 = __ldg(w + 3);
-        const unsigned w4 = shift ? __ldg(w + 4) : 0u;
-        return make_int4((int)__funnelshift_r(w0, w1, shift), (int)__funnelshift_r(w1, w2, shift),
-                         (int)__funnelshift_r(w2, w3, shift), (int)__funnelshift_r(w3, w4, shift));
+__device__ __forceinline__ uint4 load_codes(const int8_t *p) {
+    if constexpr (ALIGNED) {
+        return __ldg(reinterpret_cast<const uint4 *>(p));
+    } else {
+        const int r = (int)(reinterpret_cast<uintptr_t>(p) & 15), shift = 8 * (r & 3);
+        const uint4 *word = reinterpret_cast<const uint4 *>(p - r);
+        const uint4 u = __ldg(word), n = __ldg(word + 1);
+        const bool two = r & 8, one = r & 4;
+        const uint32_t w0 = two ? u.z : u.x, w1 = two ? u.w : u.y, w2 = two ? n.x : u.z, w3 = two ? n.y : u.w,
+                       w4 = two ? n.z : n.x, w5 = two ? n.w : n.y;
+        const uint32_t x0 = one ? w1 : w0, x1 = one ? w2 : w1, x2 = one ? w3 : w2, x3 = one ? w4 : w3,
+                       x4 = one ? w5 : w4;
+        return make_uint4(__funnelshift_r(x0, x1, shift), __funnelshift_r(x1, x2, shift),
+                          __funnelshift_r(x2, x3, shift), __funnelshift_r(x3, x4, shift));
     }
-    unsigned v[4] = {0, 0, 0, 0};
+}
+// the same near a row's end: zeros beyond `left` (which may be negative); words
+// that would pass the matrix's end are read by bytes
+template <bool ALIGNED>
+__device__ __noinline__ uint4 load_codes(const int8_t *p, int left, const int8_t *end) {
+    uint32_t v[4] = {0, 0, 0, 0};
+    if (left > 0) {
+        if (p + (ALIGNED ? 16 : 32) <= end) {
+            const uint4 u = load_codes<ALIGNED>(p);
+            v[0] = u.x, v[1] = u.y, v[2] = u.z, v[3] = u.w;
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-        if (i < left) v[i >> 2] |= (unsigned)(unsigned char)p[i] << (8 * (i & 3));
-    return make_int4((int)v[0], (int)v[1], (int)v[2], (int)v[3]);
+            for (int i = 0; i < 4; ++i) {
+                const int keep = left - 4 * i;
+                v[i] = keep <= 0 ? 0u : (keep < 4 ? v[i] & ((1u << (8 * keep)) - 1u) : v[i]);
+            }
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < 16 && i < left; ++i) {
+                const uint32_t byte = (uint32_t)(unsigned char)p[i] << (8 * (i & 3));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] |= (i >> 2) == j ? byte : 0u;
+            }
+        }
+    }
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+// the end of a matrix of codes
+__host__ __device__ __forceinline__ const int8_t *matrix_end(const int8_t *p, int rows, int cols, long long ld) {
+    return p + (long long)(rows - 1) * ld + cols;
 }
 
 __device__ __forceinline__ void store_out(const Q8Out &o, long long t, long long n, float y) {
@@ -245,92 +273,159 @@ __device__ __forceinline__ void store_out(const Q8Out &o, long long t, long long
     else ((__half *)o.p)[at] = __float2half_rn(y);
 }
 
-// ---------------------------------------------------------------------------
-// Product, dot form, for few tokens and small products: one launch, the weights
-// straight from memory. The block's TT tokens lie in shared memory, DOT_K codes
-// at a time (aligned there, zero beyond K); a warp holds 4 channels x TT tokens
-// of 32-bit sums, its lanes taking 16 codes of K each (four dp4a a pair). `wpk`
-// warps share the channels' K, so that there are warps enough to keep the
-// weights' loads coming when there are few channels.
-// ---------------------------------------------------------------------------
-constexpr int DOT_K = 4096, DOT_R = 4;
-
-template <int TT, bool ALIGNED>
-__global__ void __launch_bounds__(256) k_q8_dot(const Q8Args a, const bool x_aligned, const int wpk,
-                                                const int tiles_t) {
-    __shared__ int4 s_x[TT][DOT_K / 16];
-    __shared__ int s_sum[8][DOT_R * TT];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int group = warp / wpk, part = warp - group * wpk;
-    const int tt = (int)(blockIdx.x % tiles_t), t0 = tt * TT;
-    const long long n0 = ((long long)(blockIdx.x / tiles_t) * (8 / wpk) + group) * DOT_R;
-    const int8_t *row[DOT_R];
-#pragma unroll
-    for (int r = 0; r < DOT_R; ++r) row[r] = a.w + (n0 + r < a.N ? n0 + r : (long long)a.N - 1) * a.ld_w;
-    int acc[DOT_R][TT] = {};
-    for (int k0 = 0; k0 < a.K; k0 += DOT_K) {
-        const int len = min(DOT_K, a.K - k0), chunks = (len + 15) / 16;
-        if (k0 > 0) __syncthreads();
-        for (int i = threadIdx.x; i < TT * chunks; i += 256) {
-            const int t = i / chunks, c = i - t * chunks;
-            int4 v = make_int4(0, 0, 0, 0);
-            if (t0 + t < a.T) {
-                const int8_t *p = a.x + (long long)(t0 + t) * a.ld_x + k0 + 16 * c;
-                v = x_aligned ? load_codes<true>(p, len - 16 * c) : load_codes<false>(p, len - 16 * c);
-            }
-            s_x[t][c] = v;
-        }
-        __syncthreads();
-#pragma unroll 2
-        for (int c = part * 32 + lane; c < chunks; c += wpk * 32) {
-            int4 w[DOT_R];
-#pragma unroll
-            for (int r = 0; r < DOT_R; ++r) w[r] = load_codes<ALIGNED>(row[r] + k0 + 16 * c, len - 16 * c);
-#pragma unroll
-            for (int t = 0; t < TT; ++t) {
-                const int4 x = s_x[t][c];
-#pragma unroll
-                for (int r = 0; r < DOT_R; ++r) {
-                    acc[r][t] = __dp4a(x.x, w[r].x, acc[r][t]);
-                    acc[r][t] = __dp4a(x.y, w[r].y, acc[r][t]);
-                    acc[r][t] = __dp4a(x.z, w[r].z, acc[r][t]);
-                    acc[r][t] = __dp4a(x.w, w[r].w, acc[r][t]);
-                }
-            }
-        }
-    }
-    // lane r * TT + t keeps the sum of channel r and token t
-    int mine = 0;
-#pragma unroll
-    for (int r = 0; r < DOT_R; ++r)
-#pragma unroll
-        for (int t = 0; t < TT; ++t) {
-            const int sum = __reduce_add_sync(0xffffffffu, acc[r][t]);
-            if (lane == r * TT + t) mine = sum;
-        }
-    if (wpk > 1) {
-        if (lane < DOT_R * TT) s_sum[warp][lane] = mine;
-        __syncthreads();
-        if (part != 0) return;
-        if (lane < DOT_R * TT)
-            for (int i = 1; i < wpk; ++i) mine += s_sum[warp + i][lane];
-    }
-    const int t = t0 + lane % TT;
-    const long long n = n0 + lane / TT;
-    if (lane < DOT_R * TT && t < a.T && n < a.N)
-        store_out(a.out, t, n, ((float)mine * a.x_scale[t]) * a.w_scale[n]);
+// four codes (one word) to two fp16 pairs: 1024 + (code + 128) as fp16 bits
+// (0x6400 | byte), minus 1152
+__device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t &lo, uint32_t &hi) {
+    const uint32_t u = w ^ 0x80808080u;
+    const __half2 off = __half2half2(__ushort_as_half(0x6480));
+    uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
+    const __half2 x = __hsub2(*reinterpret_cast<__half2 *>(&a), off), y = __hsub2(*reinterpret_cast<__half2 *>(&b), off);
+    lo = *reinterpret_cast<const uint32_t *>(&x);
+    hi = *reinterpret_cast<const uint32_t *>(&y);
 }
 
-template <int TT>
-cudaError_t launch_dot(const Q8Args &a, bool x_aligned, bool w_aligned, cudaStream_t st) {
-    const int tiles_t = (a.T + TT - 1) / TT;
-    const long long quads = ((long long)a.N + DOT_R - 1) / DOT_R;
-    int wpk = 1;
-    while (wpk < 8 && quads * tiles_t * wpk < 152 * 32 && a.K > 512 * wpk) wpk *= 2;
-    const long long grid = (quads * wpk + 7) / 8 * tiles_t;
-    if (grid > 0x7fffffff) return cudaErrorInvalidValue;
-    if (w_aligned) k_q8_dot<TT, true><<<(unsigned)grid, 256, 0, st>>>(a, x_aligned, wpk, tiles_t);
-    else k_q8_dot<TT, false><<<(unsigned)grid, 256, 0, st>>>(a, x_aligned, wpk, tiles_t);
+// ---------------------------------------------------------------------------
+// Product for few tokens or small sizes: one launch, the weights from memory
+// straight into registers. 8-bit dot instructions run at a fraction of their
+// usual rate on this part (dp4a: about 70 products a cycle and SM, which made 8
+// tokens take twice as long as reading the weights), so the codes become fp16
+// here too and go through mma.sync (16 channels x 8 tokens x 16 codes, fp32
+// sums, exact up to 1024 codes as on the big path): at these sizes the
+// products are few and the point is to spend nothing between memory and the
+// tensor core. Any order of K will do as long as both operands have the same, so a
+// lane takes 16 consecutive codes of its rows, one load each, as its share of
+// four instructions.
+// A warp has 16 channels and 8 NT tokens; `wpk` warps share their K in blocks of
+// 128 codes (whole 128-byte lines), so that there are loads enough under way.
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ void mma_16x8x16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                            uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t word_of(const uint4 &v, int i) {
+    return i == 0 ? v.x : (i == 1 ? v.y : (i == 2 ? v.z : v.w));
+}
+
+// blocks of 8 warps on an SM, as the registers allow
+template <int NT>
+constexpr int few_resident() { return NT == 1 ? 4 : (NT == 2 ? 3 : 2); }
+
+template <int NT, bool ALIGNED>
+__global__ void __launch_bounds__(256, few_resident<NT>()) k_q8_few(const Q8Args a, const int wpk, const int tiles_t) {
+    __shared__ int s_sum[8][4 * NT][32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+    const int group = warp / wpk, part = warp - group * wpk;
+    const int t0 = (int)(blockIdx.x % tiles_t) * (8 * NT);
+    const long long n0 = ((long long)(blockIdx.x / tiles_t) * (8 / wpk) + group) * 16;
+    // rows and tokens beyond the end repeat the last (their results are not stored)
+    const int8_t *row0 = a.w + min(n0 + g, (long long)a.N - 1) * a.ld_w + 16 * q;
+    const int8_t *row1 = a.w + min(n0 + g + 8, (long long)a.N - 1) * a.ld_w + 16 * q;
+    const int8_t *tok[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) tok[j] = a.x + (long long)min(t0 + 8 * j + g, a.T - 1) * a.ld_x + 16 * q;
+    const int8_t *w_end = matrix_end(a.w, a.N, a.K, a.ld_w), *x_end = matrix_end(a.x, a.T, a.K, a.ld_x);
+    float c[NT][4] = {};
+    int sum[NT][4] = {};
+    // blocks whose loads need no care, for any row
+    const int blocks = (a.K + 127) / 128, whole = ALIGNED ? a.K / 128 : (a.K < 16 ? 0 : (a.K - 16) / 128);
+    int run = 0;
+    for (int b = part; b < blocks; b += wpk) {
+        uint4 w0[2], w1[2], x[2][NT];
+        if (b < whole) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int k = b * 128 + h * 64;
+                w0[h] = load_codes<ALIGNED>(row0 + k);
+                w1[h] = load_codes<ALIGNED>(row1 + k);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) x[h][j] = load_codes<ALIGNED>(tok[j] + b * 128 + h * 64);
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int k = b * 128 + h * 64, left = a.K - k - 16 * q;
+                w0[h] = load_codes<ALIGNED>(row0 + k, left, w_end);
+                w1[h] = load_codes<ALIGNED>(row1 + k, left, w_end);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) x[h][j] = load_codes<ALIGNED>(tok[j] + k, left, x_end);
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t a0, a1, a2, a3;
+                codes_to_half(word_of(w0[h], i), a0, a2);
+                codes_to_half(word_of(w1[h], i), a1, a3);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    uint32_t b0, b1;
+                    codes_to_half(word_of(x[h][j], i), b0, b1);
+                    mma_16x8x16(c[j], a0, a1, a2, a3, b0, b1);
+                }
+            }
+        if (++run == 8) {  // 1024 codes
+            run = 0;
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    sum[j][i] += __float2int_rn(c[j][i]);
+                    c[j][i] = 0.f;
+                }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[j][i] += __float2int_rn(c[j][i]);
+    if (wpk > 1) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s_sum[warp][4 * j + i][lane] = sum[j][i];
+        __syncthreads();
+        if (part != 0) return;
+        for (int v = 1; v < wpk; ++v)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[j][i] += s_sum[warp + v][4 * j + i][lane];
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = t0 + 8 * j + 2 * q + (i & 1);
+            const long long n = n0 + g + (i >> 1) * 8;
+            if (t < a.T && n < a.N) store_out(a.out, t, n, ((float)sum[j][i] * a.x_scale[t]) * a.w_scale[n]);
+        }
+}
+
+struct FewPlan {
+    int tiles_t, wpk, blocks;  // blocks of 128 along K
+    long long grid;
+};
+FewPlan few_plan(int T, int N, int K, int nt) {
+    FewPlan p{(T + 8 * nt - 1) / (8 * nt), 1, (K + 127) / 128, 0};
+    const long long rows = ((long long)N + 15) / 16;
+    while (p.wpk < 8 && rows * p.tiles_t * p.wpk < 152 * 32 && p.blocks > p.wpk) p.wpk *= 2;
+    p.grid = (rows * p.wpk + 7) / 8 * p.tiles_t;
+    return p;
+}
+
+template <int NT>
+cudaError_t launch_few(const Q8Args &a, bool aligned, cudaStream_t st) {
+    const FewPlan p = few_plan(a.T, a.N, a.K, NT);
+    if (p.grid > 0x7fffffff) return cudaErrorInvalidValue;
+    if (aligned) k_q8_few<NT, true><<<(unsigned)p.grid, 256, 0, st>>>(a, p.wpk, p.tiles_t);
+    else k_q8_few<NT, false><<<(unsigned)p.grid, 256, 0, st>>>(a, p.wpk, p.tiles_t);
     return cudaGetLastError();
 }
 
@@ -393,6 +488,7 @@ struct Q8Plan {
     int nt, tiles_n, tiles_t, blocks;  // blocks of 128 along K
     int whole;                         // tiles computed in one piece
     int share;                         // blocks of one pair's share of the others (0: none are left)
+    double cycles;                     // estimate
 };
 
 struct Q8Tc {
@@ -443,17 +539,6 @@ __device__ __forceinline__ void tile_of(int i, int tiles_n, int tiles_t, int &tn
     const int left = tiles_t - group * 8, wide = left < 8 ? left : 8;
     tn = r / wide;
     tt = group * 8 + r - tn * wide;
-}
-
-// four codes (one word) to two fp16 pairs: 1024 + (code + 128) as fp16 bits
-// (0x6400 | byte), minus 1152
-__device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t &lo, uint32_t &hi) {
-    const uint32_t u = w ^ 0x80808080u;
-    const __half2 off = __half2half2(__ushort_as_half(0x6480));
-    uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
-    const __half2 x = __hsub2(*reinterpret_cast<__half2 *>(&a), off), y = __hsub2(*reinterpret_cast<__half2 *>(&b), off);
-    lo = *reinterpret_cast<const uint32_t *>(&x);
-    hi = *reinterpret_cast<const uint32_t *>(&y);
 }
 
 template <int CH>
@@ -773,12 +858,15 @@ __global__ void __launch_bounds__(256) k_q8_prep(const PrepArgs a) {
         const long long t = i / chunks;
         const int k = (int)(i - t * chunks) * 16;
         const int8_t *p = a.x + t * a.ld_x + k;
-        const int4 v = a.x_aligned ? load_codes<true>(p, a.K - k) : load_codes<false>(p, a.K - k);
+        const int8_t *end = matrix_end(a.x, a.T, a.K, a.ld_x);
+        const uint4 v = k + 32 <= a.K ? (a.x_aligned ? load_codes<true>(p) : load_codes<false>(p))
+                        : a.x_aligned ? load_codes<true>(p, a.K - k, end)
+                                      : load_codes<false>(p, a.K - k, end);
         uint4 lo, hi;
-        codes_to_half((uint32_t)v.x, lo.x, lo.y);
-        codes_to_half((uint32_t)v.y, lo.z, lo.w);
-        codes_to_half((uint32_t)v.z, hi.x, hi.y);
-        codes_to_half((uint32_t)v.w, hi.z, hi.w);
+        codes_to_half(v.x, lo.x, lo.y);
+        codes_to_half(v.y, lo.z, lo.w);
+        codes_to_half(v.z, hi.x, hi.y);
+        codes_to_half(v.w, hi.z, hi.w);
         __half *y = a.xh + t * a.ld + k;
         *reinterpret_cast<uint4 *>(y) = lo;
         if (k + 8 < a.ld) *reinterpret_cast<uint4 *>(y + 8) = hi;
@@ -789,7 +877,9 @@ __global__ void __launch_bounds__(256) k_q8_prep(const PrepArgs a) {
         const int chunks = a.ld_wc / 16;
         const long long n = i / chunks;
         const int k = (int)(i - n * chunks) * 16;
-        *reinterpret_cast<int4 *>(a.wc + n * a.ld_wc + k) = load_codes<false>(a.w + n * a.ld_w + k, a.K - k);
+        const int8_t *p = a.w + n * a.ld_w + k;
+        *reinterpret_cast<uint4 *>(a.wc + n * a.ld_wc + k) =
+            k + 32 <= a.K ? load_codes<false>(p) : load_codes<false>(p, a.K - k, matrix_end(a.w, a.N, a.K, a.ld_w));
         return;
     }
     i -= a.w_threads;
@@ -798,7 +888,7 @@ __global__ void __launch_bounds__(256) k_q8_prep(const PrepArgs a) {
 
 constexpr int kPairs = 76;  // SM pairs of the GPU, for planning
 
-// fewer tokens than this go to the dot form
+// fewer tokens than this never go to the big form
 constexpr int kTcMinTokens = 9;
 
 // Time of one block of 128 codes in a pair's pipeline, in cycles, measured with
@@ -826,11 +916,11 @@ Q8Plan q8_plan(int T, int N, int K, int pairs) {
         const double tile = (double)p.blocks * tc.block;
         double cost = (tiles / pairs) * tile + 12.0 * tc.nt;
         if (rest > 0) {
-            // a share of at least two blocks; adding up and the wait for the last part cost about 4000 + 30 nt
+            // a share of at least two blocks; adding up and the wait for the last part cost about 6000 + 30 nt
             // cycles
             const long long blocks = (long long)rest * p.blocks;
             const int share = (int)std::max((blocks + pairs - 1) / pairs, 2ll);
-            const double cut = (double)share * tc.block + 4000 + 30.0 * tc.nt;
+            const double cut = (double)share * tc.block + 6000 + 30.0 * tc.nt;
             if (cut < tile) {
                 p.whole = tiles - rest;
                 p.share = share;
@@ -840,6 +930,7 @@ Q8Plan q8_plan(int T, int N, int K, int pairs) {
         if (best.nt == 0 || cost < best_cost) {
             best_cost = cost;
             best = p;
+            best.cycles = cost;
         }
     }
     return best;
@@ -959,10 +1050,24 @@ cudaError_t launch_tc(const Q8Args &q, const Q8Plan &p, const Q8Scratch &s, int 
     return cudaLaunchKernelEx(&cfg, k_q8_tc<NT>, map_w, map_x, a);
 }
 
-// Which form: the dot form takes what its sums need at DOT_RATE products a
-// microsecond, after about 3 us; the tensor cores' launches cost about 14 us on
-// top of the plan's cycles (and a copy of the weights where they need one).
-bool use_tc(const Q8Args &a) { return a.T >= kTcMinTokens && a.K >= 16; }
+// Which form, by two estimates in microseconds (both without what any launch
+// costs), fitted to times with cold caches. mma.sync: rounds of resident blocks,
+// each warp passing `steps` blocks of 128 codes of K. The big form: its plan, 4 us
+// for the preparation and the pipeline's ends, and the copy of weights whose rows
+// are not aligned. Measured with the other form beside it (us): 32 x 784 x 800
+// 10.8 and 12.9, 16 x 4096 x 4096 12.9 and 18.0, 64 x 4096 x 4096 23.1 and 19.1,
+// 32 x 16384 x 16384 103 and 56, 256 x 3000 x 1000 (not aligned) 31 and 17.
+// Up to 8 tokens mma.sync reads the weights as fast as memory gives them.
+bool use_tc(const Q8Args &a, bool aligned, const Q8Plan &p) {
+    if (a.T < kTcMinTokens || a.K < 16) return false;
+    const int nt = a.T <= 16 ? 2 : 4;
+    const FewPlan f = few_plan(a.T, a.N, a.K, nt);
+    const long long resident = 152 * (nt == 2 ? few_resident<2>() : few_resident<4>());
+    const double rounds = (double)((f.grid + resident - 1) / resident), steps = (f.blocks + f.wpk - 1) / f.wpk;
+    const double few = 3.5 + rounds * steps * (nt == 2 ? 1.1 : 1.5) * (aligned ? 1.0 : 1.5) + (aligned ? 0.0 : 4.0);
+    const double tc = 4.0 + p.cycles / 1900.0 + (w_rows_aligned(a) ? 0.0 : 2.0 * a.N * (double)a.K / 6.5e6);
+    return tc < few;
+}
 
 }  // namespace
 
@@ -975,10 +1080,10 @@ size_t q8_workspace_bytes(int T, int N, int K) {
 cudaError_t launch_q8_product(const Q8Args &a, void *workspace, cudaStream_t st) {
     if (a.T == 0 || a.N == 0) return cudaSuccess;
     const bool x_aligned = rows_aligned(a.x, a.ld_x), w_aligned = w_rows_aligned(a);
-    if (use_tc(a)) {
-        const int pairs = resident_pairs();
-        if (pairs < 1) return cudaErrorInvalidConfiguration;
-        const Q8Plan p = q8_plan(a.T, a.N, a.K, pairs);
+    const int pairs = resident_pairs();
+    if (pairs < 1) return cudaErrorInvalidConfiguration;
+    const Q8Plan p = a.T < kTcMinTokens ? Q8Plan{} : q8_plan(a.T, a.N, a.K, pairs);
+    if (use_tc(a, x_aligned && w_aligned, p)) {
         const Q8Scratch s = q8_scratch(workspace, a.T, a.N, a.K, (long long)p.tiles_n * p.tiles_t - p.whole, p.nt);
         PrepArgs pa{a.x, a.w, a.ld_x, a.ld_w, a.T, a.N, a.K, x_aligned, s.x, s.ld, s.w, s.ld_w, (uint4 *)s.ticket,
                     (long long)a.T * ((s.ld + 15) / 16), w_aligned ? 0 : (long long)a.N * (s.ld_w / 16), s.zeros};
@@ -996,10 +1101,9 @@ cudaError_t launch_q8_product(const Q8Args &a, void *workspace, cudaStream_t st)
             default: return launch_tc<192>(a, p, s, pairs, st);
         }
     }
-    if (a.T == 1) return launch_dot<1>(a, x_aligned, w_aligned, st);
-    if (a.T == 2) return launch_dot<2>(a, x_aligned, w_aligned, st);
-    if (a.T <= 4) return launch_dot<4>(a, x_aligned, w_aligned, st);
-    return launch_dot<8>(a, x_aligned, w_aligned, st);
+    if (a.T <= 8) return launch_few<1>(a, x_aligned && w_aligned, st);
+    if (a.T <= 16) return launch_few<2>(a, x_aligned && w_aligned, st);
+    return launch_few<4>(a, x_aligned && w_aligned, st);
 }
 
 }  // namespace dstd
