@@ -383,35 +383,59 @@ def adamw_multi(ws, gs, ms, vs, lr, beta1, beta2, eps, weight_decay, step, lr_de
 
 
 # -- training and serving in 8 bits ------------------------------------------
+_TORCH = None       # torch, once one of these calls has needed it
+_CODES = {}         # torch dtype -> dstd_type
+_RAW_STREAM = None  # device index -> the current stream's handle
+
+
+def _torch():
+    global _TORCH, _RAW_STREAM
+    if _TORCH is None:
+        import torch
+        _CODES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+        _RAW_STREAM = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda index: torch.cuda.current_stream(index).cuda_stream)
+        _TORCH = torch
+    return _TORCH
+
+
+def _stream_of(stream, x):
+    """The stream to launch on: the given one, or the current one of x's device."""
+    if stream is None:
+        return _RAW_STREAM(x.get_device())
+    return stream if isinstance(stream, int) else stream.cuda_stream
+
+
 def _type_code(dtype, name):
     """dstd_type of a torch dtype (include/dstd.h)."""
-    import torch
-    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(dtype)
+    code = _CODES.get(dtype)
     if code is None:
         raise ValueError(f"{name} must be float32, bfloat16 or float16, not {dtype}")
     return code
 
 
-def _rows(x, name, dtype=None, shape=None):
-    """Row stride of a CUDA matrix whose rows are contiguous (rows may be padded, not overlap)."""
-    if not x.is_cuda or x.dim() != 2 or (dtype is not None and x.dtype != dtype):
-        raise ValueError(f"{name} must be a CUDA matrix" + (f" of {dtype}" if dtype is not None else ""))
-    if shape is not None and tuple(x.shape) != shape:
-        raise ValueError(f"{name} has shape {tuple(x.shape)}, expected {shape}")
-    R, K = x.shape
-    if K > 1 and x.stride(1) != 1:
-        raise ValueError(f"{name} must have contiguous rows")
-    if R <= 1 or K == 0:
-        return K
-    if x.stride(0) < K:
-        raise ValueError(f"{name} must not have overlapping rows")
-    return x.stride(0)
+def _rows(x, name, R, K, dtype=None):
+    """Row stride of a CUDA matrix [R, K] whose rows are contiguous (they may be padded, not overlap)."""
+    if x.shape == (R, K) and x.is_cuda and (dtype is None or x.dtype == dtype):
+        ld, one = x.stride()
+        if (one == 1 or K <= 1) and ld >= K:
+            return ld
+        if (one == 1 or K <= 1) and R <= 1:
+            return K
+        raise ValueError(f"{name} must have contiguous rows that do not overlap")
+    raise ValueError(f"{name} must be a CUDA matrix of shape {(R, K)}" +
+                     (f" and {dtype}" if dtype is not None else "") + f", not {tuple(x.shape)}, {x.dtype}, {x.device}")
+
+
+def _floats(x, name, n):
+    if x.shape != (n,) or x.dtype != _TORCH.float32 or not x.is_cuda or (n > 1 and x.stride(0) != 1):
+        raise ValueError(f"{name} must be a contiguous CUDA float32 tensor of {n}")
 
 
 def _scratch(ws, where):
     if not ws.is_cuda or not ws.is_contiguous():
         raise ValueError(f"{where}: workspace must be a contiguous CUDA tensor")
-    return ws.data_ptr(), ws.numel() * ws.element_size()
+    return ws.numel() * ws.element_size()
 
 
 def quantize_rows(x, q, scale, values=None, stream=None):
@@ -419,18 +443,24 @@ def quantize_rows(x, q, scale, values=None, stream=None):
     and scales [R]: scale = max |x| / 127, q = x / scale to the nearest.
     ``values`` [R, K] float32 receives what the codes stand for. A row that is
     not finite gets scale NaN. Rows may be padded."""
-    import torch
-    ld_x = _rows(x, "x")
-    shape = tuple(x.shape)
-    ld_q = _rows(q, "q", torch.int8, shape)
-    _f32(scale, "scale", (shape[0],))
-    ld_v = _rows(values, "values", torch.float32, shape) if values is not None else 0
-    _check(load().dstd_quantize_rows(x.data_ptr(), _type_code(x.dtype, "x"), shape[0], shape[1], ld_x, q.data_ptr(),
-                                     ld_q, scale.data_ptr(), _ptr(values), ld_v, _stream(stream)),
-           "dstd_quantize_rows")
+    torch = _torch()
+    R, K = x.shape
+    ld_x = _rows(x, "x", R, K)
+    ld_q = _rows(q, "q", R, K, torch.int8)
+    _floats(scale, "scale", R)
+    ld_v, v = 0, None
+    if values is not None:
+        ld_v, v = _rows(values, "values", R, K, torch.float32), values.data_ptr()
+    code = load().dstd_quantize_rows(x.data_ptr(), _type_code(x.dtype, "x"), R, K, ld_x, q.data_ptr(), ld_q,
+                                     scale.data_ptr(), v, ld_v, _stream_of(stream, x))
+    if code:
+        raise DstdError(code, "dstd_quantize_rows")
 
 
 def int8_matmul_workspace_bytes(T, N, K):
+    """Scratch of int8_matmul for T tokens, N channels, K inputs: from 9 tokens
+    on the tokens in 16 bits and room for a copy of the weights (touched only
+    where their rows are not 16-byte aligned)."""
     return load().dstd_int8_matmul_workspace_bytes(T, N, K)
 
 
@@ -438,18 +468,19 @@ def int8_matmul(x, x_scale, w, w_scale, out, workspace, stream=None):
     """out [T, N] = x_scale[:, None] * w_scale * (x @ w^T) of int8 rows x [T, K]
     and w [N, K]; the sum over K is exact. out is float32, bfloat16 or float16;
     rows may be padded."""
-    import torch
+    torch = _torch()
     T, K = x.shape
     N = w.shape[0]
-    ld_x = _rows(x, "x", torch.int8)
-    ld_w = _rows(w, "w", torch.int8, (N, K))
-    ld_out = _rows(out, "out", None, (T, N))
-    _f32(x_scale, "x_scale", (T,))
-    _f32(w_scale, "w_scale", (N,))
-    ws, ws_bytes = _scratch(workspace, "int8_matmul")
-    _check(load().dstd_int8_matmul(x.data_ptr(), ld_x, x_scale.data_ptr(), w.data_ptr(), ld_w, w_scale.data_ptr(), T,
-                                   N, K, out.data_ptr(), _type_code(out.dtype, "out"), ld_out, ws, ws_bytes,
-                                   _stream(stream)), "dstd_int8_matmul")
+    ld_x = _rows(x, "x", T, K, torch.int8)
+    ld_w = _rows(w, "w", N, K, torch.int8)
+    ld_out = _rows(out, "out", T, N)
+    _floats(x_scale, "x_scale", T)
+    _floats(w_scale, "w_scale", N)
+    code = load().dstd_int8_matmul(x.data_ptr(), ld_x, x_scale.data_ptr(), w.data_ptr(), ld_w, w_scale.data_ptr(), T,
+                                   N, K, out.data_ptr(), _type_code(out.dtype, "out"), ld_out, workspace.data_ptr(),
+                                   _scratch(workspace, "int8_matmul"), _stream_of(stream, x))
+    if code:
+        raise DstdError(code, "dstd_int8_matmul")
 
 
 def dense_q8_workspace_bytes(B, N_in, N_out, p):
@@ -460,7 +491,7 @@ def dense_fwd_q8(t_in, w_q, w_scale, p, t_out, saved, penalty, workspace, stream
     """dense_fwd with an 8-bit contraction: w_q [N_out, N_in] int8 codes and
     w_scale [N_out] from quantize_rows; the grid weights are quantised for each
     (sample, grid point). Backward: dense_bwd with the weights' values."""
-    import torch
+    torch = _torch()
     B, N_in = t_in.shape
     N_out = w_q.shape[0]
     _f32(t_in, "t_in")
@@ -468,10 +499,10 @@ def dense_fwd_q8(t_in, w_q, w_scale, p, t_out, saved, penalty, workspace, stream
     _f32(t_out, "t_out", (B, N_out))
     if w_q.dtype != torch.int8 or not w_q.is_cuda or not w_q.is_contiguous() or tuple(w_q.shape) != (N_out, N_in):
         raise ValueError("w_q must be a contiguous CUDA int8 tensor [N_out, N_in]")
-    ws, ws_bytes = _scratch(workspace, "dense_fwd_q8")
     _check(load().dstd_dense_fwd_q8(t_in.data_ptr(), w_q.data_ptr(), w_scale.data_ptr(), B, N_in, N_out,
-                                    ctypes.byref(p), t_out.data_ptr(), _ptr(saved), _ptr(penalty), ws, ws_bytes,
-                                    _stream(stream)), "dstd_dense_fwd_q8")
+                                    ctypes.byref(p), t_out.data_ptr(), _ptr(saved), _ptr(penalty),
+                                    workspace.data_ptr(), _scratch(workspace, "dense_fwd_q8"),
+                                    _stream_of(stream, t_in)), "dstd_dense_fwd_q8")
 
 
 class TensorList:
@@ -480,6 +511,7 @@ class TensorList:
     tensors alive; their storage must stay where it is."""
 
     def __init__(self, tensors):
+        _torch()
         self.tensors = list(tensors)
         for i, t in enumerate(self.tensors):
             if not t.is_cuda or not t.is_contiguous():
@@ -487,6 +519,7 @@ class TensorList:
         k = len(self.tensors)
         self.sizes = tuple(t.numel() for t in self.tensors)
         self.codes = tuple(_type_code(t.dtype, f"tensor {i} of the list") for i, t in enumerate(self.tensors))
+        self.f32 = not any(self.codes)
         self.ptr = (ctypes.c_void_p * k)(*[t.data_ptr() for t in self.tensors])
         self.n = (ctypes.c_int64 * k)(*self.sizes)
         self.type = (ctypes.c_int32 * k)(*self.codes)
@@ -499,13 +532,6 @@ def _list(x):
     return x if isinstance(x, TensorList) else TensorList(x)
 
 
-def _same_sizes(a, b, where, f32=False):
-    if a.sizes != b.sizes:
-        raise ValueError(f"{where}: tensor lists differ in length or sizes")
-    if f32 and any(b.codes):
-        raise ValueError(f"{where}: weights and moments must be float32")
-
-
 def grad_norm_workspace_bytes(gs):
     """Bytes of the workspace that grad_norm, clip_grads and adamw_clip share
     for these gradients: a tensor of zeros at first, left ready by each call."""
@@ -516,28 +542,31 @@ def grad_norm_workspace_bytes(gs):
 def grad_norm(gs, norm, workspace, tensor_norms=None, stream=None):
     """norm[0] = the 2-norm over all gradients of the list (float32, bfloat16 or
     float16 tensors, or a TensorList); tensor_norms [len(gs)]: of each."""
+    _torch()
     gs = _list(gs)
-    _f32(norm, "norm", (1,))
+    _floats(norm, "norm", 1)
     if tensor_norms is not None:
-        _f32(tensor_norms, "tensor_norms", (len(gs),))
-    ws, ws_bytes = _scratch(workspace, "grad_norm")
-    _check(load().dstd_grad_norm(len(gs), gs.ptr, gs.n, gs.type, norm.data_ptr(), _ptr(tensor_norms), ws, ws_bytes,
-                                 _stream(stream)), "dstd_grad_norm")
+        _floats(tensor_norms, "tensor_norms", len(gs.sizes))
+    code = load().dstd_grad_norm(len(gs.sizes), gs.ptr, gs.n, gs.type, norm.data_ptr(), _ptr(tensor_norms),
+                                 workspace.data_ptr(), _scratch(workspace, "grad_norm"), _stream_of(stream, norm))
+    if code:
+        raise DstdError(code, "dstd_grad_norm")
 
 
 def clip_grads(gs, max_norm, norm, workspace, outs=None, stream=None):
     """Gradients times min(1, max_norm / norm), in place or into ``outs``;
     norm[0] receives the norm before clipping. When it is not finite the
     gradients pass unchanged."""
+    _torch()
     gs = _list(gs)
     outs = gs if outs is None else _list(outs)
-    _same_sizes(gs, outs, "clip_grads")
-    if gs.codes != outs.codes:
-        raise ValueError("clip_grads: outs must have the gradients' types")
-    _f32(norm, "norm", (1,))
-    ws, ws_bytes = _scratch(workspace, "clip_grads")
-    _check(load().dstd_clip_grads(len(gs), gs.ptr, outs.ptr, gs.n, gs.type, float(max_norm), norm.data_ptr(), ws,
-                                  ws_bytes, _stream(stream)), "dstd_clip_grads")
+    if gs.sizes != outs.sizes or gs.codes != outs.codes:
+        raise ValueError("clip_grads: outs must have the gradients' sizes and types")
+    _floats(norm, "norm", 1)
+    code = load().dstd_clip_grads(len(gs.sizes), gs.ptr, outs.ptr, gs.n, gs.type, max_norm, norm.data_ptr(),
+                                  workspace.data_ptr(), _scratch(workspace, "clip_grads"), _stream_of(stream, norm))
+    if code:
+        raise DstdError(code, "dstd_clip_grads")
 
 
 def adamw_clip(ws, gs, ms, vs, lr, beta1, beta2, eps, weight_decay, step, max_norm, norm, workspace, lr_dev=None,
@@ -546,20 +575,22 @@ def adamw_clip(ws, gs, ms, vs, lr, beta1, beta2, eps, weight_decay, step, max_no
     clipped to the global norm max_norm; gs is only read. step: device int32
     tensor whose first element counts the updates done. A norm that is not
     finite changes nothing but norm[0]."""
-    import torch
+    torch = _torch()
     ws, gs, ms, vs = _list(ws), _list(gs), _list(ms), _list(vs)
-    for x in (ws, ms, vs):
-        _same_sizes(gs, x, "adamw_clip", f32=True)
+    if not (ws.sizes == gs.sizes == ms.sizes == vs.sizes):
+        raise ValueError("adamw_clip: tensor lists differ in length or sizes")
+    if not (ws.f32 and ms.f32 and vs.f32):
+        raise ValueError("adamw_clip: weights and moments must be float32")
     if step.dtype != torch.int32 or step.numel() < 1 or not step.is_cuda:
         raise ValueError("adamw_clip: step must be a device int32 tensor")
     if lr_dev is not None:
         _f32(lr_dev, "lr_dev")
-    _f32(norm, "norm", (1,))
-    scratch, ws_bytes = _scratch(workspace, "adamw_clip")
-    _check(load().dstd_adamw_clip(len(gs), ws.ptr, gs.ptr, ms.ptr, vs.ptr, gs.n, gs.type, float(lr), float(beta1),
-                                  float(beta2), float(eps), float(weight_decay), float(max_norm), step.data_ptr(),
-                                  _ptr(lr_dev), norm.data_ptr(), scratch, ws_bytes, _stream(stream)),
-           "dstd_adamw_clip")
+    _floats(norm, "norm", 1)
+    code = load().dstd_adamw_clip(len(gs.sizes), ws.ptr, gs.ptr, ms.ptr, vs.ptr, gs.n, gs.type, lr, beta1, beta2, eps,
+                                  weight_decay, max_norm, step.data_ptr(), _ptr(lr_dev), norm.data_ptr(),
+                                  workspace.data_ptr(), _scratch(workspace, "adamw_clip"), _stream_of(stream, norm))
+    if code:
+        raise DstdError(code, "dstd_adamw_clip")
 
 
 def device_status(clear=True):
