@@ -179,6 +179,8 @@ __global__ void __launch_bounds__(THREADS) k_sum_squares(const ClipArgs<CAP> a) 
     __shared__ double s_rare[THREADS / 32];
     __shared__ bool s_last;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    // the pass that applies the norm may be launched while this one runs
+    asm volatile("griddepcontrol.launch_dependents;");
     for (unsigned c = blockIdx.x; c < a.chunks; c += gridDim.x) {
         const ClipSeg &sg = a.seg[seg_of(a, c)];
         const long long lo = (long long)(c - sg.first) * a.chunk;
@@ -281,6 +283,7 @@ __device__ __forceinline__ void scale_chunk(const T *g, T *out, long long n, flo
 
 template <int CAP>
 __global__ void __launch_bounds__(THREADS) k_clip_scale(const ClipArgs<CAP> a) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // for the norm
     const float coef = a.result->coef;
     for (unsigned c = blockIdx.x; c < a.chunks; c += gridDim.x) {
         const ClipSeg &sg = a.seg[seg_of(a, c)];
@@ -354,6 +357,7 @@ __device__ __forceinline__ void adamw_chunk(const StepConst &c, const T *g, floa
 
 template <int CAP>
 __global__ void __launch_bounds__(THREADS) k_adamw_clip(const ClipArgs<CAP> a) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // for the norm
     if (a.result->skip) return;
     StepConst k;
     const float t = (float)a.step[0];
@@ -409,10 +413,20 @@ cudaError_t launch_group(const ClipTensors &t, ClipOp op, int begin, int count, 
     }
     a.chunks = chunks;
     const unsigned grid = chunks < 1 ? 1 : (chunks < kBlocks ? chunks : kBlocks);
-    if (op == ClipOp::Norm) k_sum_squares<CAP><<<grid, THREADS, 0, st>>>(a);
-    else if (op == ClipOp::Scale) k_clip_scale<CAP><<<grid, THREADS, 0, st>>>(a);
-    else k_adamw_clip<CAP><<<grid, THREADS, 0, st>>>(a);
-    return cudaGetLastError();
+    if (op == ClipOp::Norm) {
+        k_sum_squares<CAP><<<grid, THREADS, 0, st>>>(a);
+        return cudaGetLastError();
+    }
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = begin == 0 ? 1 : 0;  // the launch before this one is the norm's last
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(THREADS);
+    cfg.stream = st;
+    return cudaLaunchKernelEx(&cfg, op == ClipOp::Scale ? k_clip_scale<CAP> : k_adamw_clip<CAP>, a);
 }
 
 }  // namespace
