@@ -386,14 +386,15 @@ __global__ void __launch_bounds__(THREADS) k_adamw_clip(const ClipArgs<CAP> a) {
 
 constexpr int kBlocks = 152 * 6;
 
-// elements of a chunk: about one chunk per resident block, in multiples of 4096
-// (four 16-byte loads of fp32 a thread); small lists take fewer blocks, since
-// the last one has to collect what the others leave
-long long chunk_elements(int count, const int64_t *n) {
+// elements of a chunk: about one chunk per resident block. For the norm in
+// multiples of 4096 (four 16-byte loads of fp32 a thread): small lists take
+// fewer blocks, since the last one has to collect what the others leave. The
+// passes after it take 2048 at least (one step of the update).
+long long chunk_elements(int count, const int64_t *n, int least) {
     long long total = 0;
     for (int i = 0; i < count; ++i) total += n[i];
     const long long c = (total + kBlocks - 1) / kBlocks;
-    return c < 4096 ? 4096 : (c + 4095) / 4096 * 4096;
+    return c < least ? least : (c + least - 1) / least * least;
 }
 
 template <int CAP>
@@ -432,7 +433,7 @@ cudaError_t launch_group(const ClipTensors &t, ClipOp op, int begin, int count, 
 }  // namespace
 
 size_t clip_workspace_bytes(int count, const int64_t *n) {
-    const long long chunk = chunk_elements(count, n);
+    const long long chunk = chunk_elements(count, n, 4096);
     size_t chunks = 0;
     for (int i = 0; i < count; ++i) chunks += (size_t)((n[i] + chunk - 1) / chunk);
     return 256 + 8 * chunks;
@@ -457,7 +458,7 @@ cudaError_t launch_clip(const ClipTensors &t, ClipOp op, const ClipHyper &h, flo
         a.ln_b2 = (float)log(h.b2);
         a.eps = (float)h.eps;
         a.wd = (float)h.wd;
-        a.chunk = chunk_elements(t.count, t.n);
+        a.chunk = chunk_elements(t.count, t.n, op == ClipOp::Norm ? 4096 : 2048);
     };
     for (int begin = 0, launch = 0; begin < t.count; begin += kClipMaxTensors, ++launch) {
         const int count = t.count - begin < kClipMaxTensors ? t.count - begin : kClipMaxTensors;

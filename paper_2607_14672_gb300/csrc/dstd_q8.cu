@@ -7,6 +7,28 @@
 
 namespace dstd {
 
+// Dependent launch. A grid launched with launch_dependent may start while the
+// one before it in the stream still runs, from when all of that one's blocks
+// have called let_next_launch (or ended); what that one writes, and what was
+// there before it, is there after wait_launch_before. A grid that lets the next
+// one start has itself waited first, so nothing older is still running then.
+__device__ __forceinline__ void wait_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+template <class... P, class... A>
+cudaError_t launch_dependent(void (*kernel)(P...), unsigned grid, unsigned block, cudaStream_t st, const A &...args) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.stream = st;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 // ---------------------------------------------------------------------------
 // Row quantiser. With a = max_k |x_k|:
 //     scale = a / 127,  q_k = rint(x_k (127 (1 / a))),  value_k = q_k scale,
@@ -77,6 +99,7 @@ struct QuantArgs {
 template <class T, int VEC, int E, int THREADS, int BLOCK = THREADS == 32 ? 256 : THREADS>
 __global__ void __launch_bounds__(BLOCK) k_quantize_rows(const T *__restrict__ x, const QuantArgs a) {
     __shared__ unsigned s_top[32];
+    let_next_launch();
     const int t = threadIdx.x % THREADS;
     const long long r = (long long)blockIdx.x * (BLOCK / THREADS) + threadIdx.x / THREADS;
     if (r >= a.rows) return;  // a whole warp, or never
@@ -295,8 +318,9 @@ __device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t &lo, uint32_t
 // tensor core. Any order of K will do as long as both operands have the same, so a
 // lane takes 16 consecutive codes of its rows, one load each, as its share of
 // four instructions.
-// A warp has 16 channels and 8 NT tokens; `wpk` warps share their K in blocks of
-// 128 codes (whole 128-byte lines), so that there are loads enough under way.
+// A block has 16 channels and 8 NT tokens; its warps (1 to 8) share K in blocks
+// of 128 codes (whole 128-byte lines): as many as fit the GPU in one round of
+// blocks, so that there are loads enough under way and no second, half-empty round.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ void mma_16x8x16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                             uint32_t b0, uint32_t b1) {
@@ -310,17 +334,17 @@ __device__ __forceinline__ uint32_t word_of(const uint4 &v, int i) {
     return i == 0 ? v.x : (i == 1 ? v.y : (i == 2 ? v.z : v.w));
 }
 
-// blocks of 8 warps on an SM, as the registers allow
+// warps on an SM, as the registers allow
 template <int NT>
-constexpr int few_resident() { return NT == 1 ? 4 : (NT == 2 ? 3 : 2); }
+constexpr int few_resident() { return NT == 1 ? 32 : (NT == 2 ? 24 : 16); }
 
 template <int NT, bool ALIGNED>
-__global__ void __launch_bounds__(256, few_resident<NT>()) k_q8_few(const Q8Args a, const int wpk, const int tiles_t) {
+__global__ void __launch_bounds__(256, few_resident<NT>() / 8) k_q8_few(const Q8Args a, const int tiles_t) {
     __shared__ int s_sum[8][4 * NT][32];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-    const int group = warp / wpk, part = warp - group * wpk;
+    const int part = threadIdx.x >> 5, wpk = blockDim.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
     const int t0 = (int)(blockIdx.x % tiles_t) * (8 * NT);
-    const long long n0 = ((long long)(blockIdx.x / tiles_t) * (8 / wpk) + group) * 16;
+    const long long n0 = (long long)(blockIdx.x / tiles_t) * 16;
+    wait_launch_before();
     // rows and tokens beyond the end repeat the last (their results are not stored)
     const int8_t *row0 = a.w + min(n0 + g, (long long)a.N - 1) * a.ld_w + 16 * q;
     const int8_t *row1 = a.w + min(n0 + g + 8, (long long)a.N - 1) * a.ld_w + 16 * q;
@@ -389,14 +413,14 @@ __global__ void __launch_bounds__(256, few_resident<NT>()) k_q8_few(const Q8Args
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s_sum[warp][4 * j + i][lane] = sum[j][i];
+            for (int i = 0; i < 4; ++i) s_sum[part][4 * j + i][lane] = sum[j][i];
         __syncthreads();
         if (part != 0) return;
         for (int v = 1; v < wpk; ++v)
 #pragma unroll
             for (int j = 0; j < NT; ++j)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum[j][i] += s_sum[warp + v][4 * j + i][lane];
+                for (int i = 0; i < 4; ++i) sum[j][i] += s_sum[v][4 * j + i][lane];
     }
 #pragma unroll
     for (int j = 0; j < NT; ++j)
@@ -411,22 +435,24 @@ __global__ void __launch_bounds__(256, few_resident<NT>()) k_q8_few(const Q8Args
 struct FewPlan {
     int tiles_t, wpk, blocks;  // blocks of 128 along K
     long long grid;
+    int rounds;
 };
-FewPlan few_plan(int T, int N, int K, int nt) {
-    FewPlan p{(T + 8 * nt - 1) / (8 * nt), 1, (K + 127) / 128, 0};
-    const long long rows = ((long long)N + 15) / 16;
-    while (p.wpk < 8 && rows * p.tiles_t * p.wpk < 152 * 32 && p.blocks > p.wpk) p.wpk *= 2;
-    p.grid = (rows * p.wpk + 7) / 8 * p.tiles_t;
+template <int NT>
+FewPlan few_plan(int T, int N, int K) {
+    FewPlan p{(T + 8 * NT - 1) / (8 * NT), 1, (K + 127) / 128, 0, 0};
+    constexpr int warps = 152 * few_resident<NT>();
+    p.grid = ((long long)N + 15) / 16 * p.tiles_t;
+    while (p.wpk < 8 && p.grid * p.wpk * 2 <= warps && p.blocks > p.wpk) p.wpk *= 2;
+    p.rounds = (int)std::min<long long>((p.grid * p.wpk + warps - 1) / warps, 1 << 20);
     return p;
 }
 
 template <int NT>
 cudaError_t launch_few(const Q8Args &a, bool aligned, cudaStream_t st) {
-    const FewPlan p = few_plan(a.T, a.N, a.K, NT);
+    const FewPlan p = few_plan<NT>(a.T, a.N, a.K);
     if (p.grid > 0x7fffffff) return cudaErrorInvalidValue;
-    if (aligned) k_q8_few<NT, true><<<(unsigned)p.grid, 256, 0, st>>>(a, p.wpk, p.tiles_t);
-    else k_q8_few<NT, false><<<(unsigned)p.grid, 256, 0, st>>>(a, p.wpk, p.tiles_t);
-    return cudaGetLastError();
+    return launch_dependent(aligned ? k_q8_few<NT, true> : k_q8_few<NT, false>, (unsigned)p.grid, 32 * p.wpk, st, a,
+                            p.tiles_t);
 }
 
 // ---------------------------------------------------------------------------
@@ -546,11 +572,6 @@ __device__ __forceinline__ void tmem_ld(uint32_t addr, float (&v)[CH]) {
     if constexpr (CH == 32) tmem_ld32(addr, v);
     else tmem_ld16(addr, v);
 }
-
-// Dependent launch: this grid may start while the one before it in the stream
-// still runs; what that one writes is there after the wait.
-__device__ __forceinline__ void wait_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void let_next_launch() { asm volatile("griddepcontrol.launch_dependents;"); }
 
 __device__ __forceinline__ void q8_timeout() { atomicOr(&g_status_q8, STATUS_TIMEOUT); }
 
@@ -851,6 +872,7 @@ struct PrepArgs {
 };
 
 __global__ void __launch_bounds__(256) k_q8_prep(const PrepArgs a) {
+    wait_launch_before();
     let_next_launch();
     long long i = (long long)blockIdx.x * 256 + threadIdx.x;
     if (i < a.x_threads) {
@@ -1060,11 +1082,10 @@ cudaError_t launch_tc(const Q8Args &q, const Q8Plan &p, const Q8Scratch &s, int 
 // Up to 8 tokens mma.sync reads the weights as fast as memory gives them.
 bool use_tc(const Q8Args &a, bool aligned, const Q8Plan &p) {
     if (a.T < kTcMinTokens || a.K < 16) return false;
-    const int nt = a.T <= 16 ? 2 : 4;
-    const FewPlan f = few_plan(a.T, a.N, a.K, nt);
-    const long long resident = 152 * (nt == 2 ? few_resident<2>() : few_resident<4>());
-    const double rounds = (double)((f.grid + resident - 1) / resident), steps = (f.blocks + f.wpk - 1) / f.wpk;
-    const double few = 3.5 + rounds * steps * (nt == 2 ? 1.1 : 1.5) * (aligned ? 1.0 : 1.5) + (aligned ? 0.0 : 4.0);
+    const bool two = a.T <= 16;
+    const FewPlan f = two ? few_plan<2>(a.T, a.N, a.K) : few_plan<4>(a.T, a.N, a.K);
+    const double steps = (double)((f.blocks + f.wpk - 1) / f.wpk) * f.rounds;
+    const double few = 3.5 + steps * (two ? 1.1 : 1.5) * (aligned ? 1.0 : 1.5) + (aligned ? 0.0 : 4.0);
     const double tc = 4.0 + p.cycles / 1900.0 + (w_rows_aligned(a) ? 0.0 : 2.0 * a.N * (double)a.K / 6.5e6);
     return tc < few;
 }
@@ -1089,8 +1110,7 @@ cudaError_t launch_q8_product(const Q8Args &a, void *workspace, cudaStream_t st)
                     (long long)a.T * ((s.ld + 15) / 16), w_aligned ? 0 : (long long)a.N * (s.ld_w / 16), s.zeros};
         const long long blocks = (pa.x_threads + pa.w_threads + pa.zeros + 255) / 256;
         if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-        k_q8_prep<<<(unsigned)blocks, 256, 0, st>>>(pa);
-        cudaError_t e = cudaGetLastError();
+        cudaError_t e = launch_dependent(k_q8_prep, (unsigned)blocks, 256, st, pa);
         if (e != cudaSuccess) return e;
         switch (p.nt) {
             case 32: return launch_tc<32>(a, p, s, pairs, st);
