@@ -67,23 +67,20 @@ __device__ __forceinline__ RowCode row_code(unsigned top_bits) {
 // an infinity times pre = 0 is NaN, whose conversion to an integer is 0
 __device__ __forceinline__ int code_of(float x, const RowCode &c) { return __float2int_rn((x * c.pre) * c.inv); }
 
-// Four consecutive elements, the first at a multiple of four elements from an
-// address that the launch has checked; one at a time at the row's end.
-__device__ __forceinline__ void load4(const float *p, float (&x)[4]) {
-    const float4 v = *reinterpret_cast<const float4 *>(p);
-    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
-}
-__device__ __forceinline__ void load4(const __nv_bfloat16 *p, float (&x)[4]) {
-    const uint2 u = *reinterpret_cast<const uint2 *>(p);
-    x[0] = __uint_as_float(u.x << 16), x[1] = __uint_as_float(u.x & 0xffff0000u);
-    x[2] = __uint_as_float(u.y << 16), x[3] = __uint_as_float(u.y & 0xffff0000u);
-}
-__device__ __forceinline__ void load4(const __half *p, float (&x)[4]) {
-    const uint2 u = *reinterpret_cast<const uint2 *>(p);
-    const float2 lo = __half22float2(*reinterpret_cast<const __half2 *>(&u.x));
-    const float2 hi = __half22float2(*reinterpret_cast<const __half2 *>(&u.y));
-    x[0] = lo.x, x[1] = lo.y, x[2] = hi.x, x[3] = hi.y;
-}
+// 16 bytes of a type, kept as they are until used (a 16-bit row takes half the registers)
+template <class T>
+struct Pack {
+    static constexpr int P = 16 / sizeof(T);
+    static __device__ __forceinline__ float one(const uint4 &u, int i) {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        if constexpr (sizeof(T) == 4) {
+            return __uint_as_float(w[i]);
+        } else {
+            const unsigned short h = (unsigned short)(w[i / 2] >> (16 * (i & 1)));
+            return to_f32<T>(*reinterpret_cast<const T *>(&h));
+        }
+    }
+};
 
 struct QuantArgs {
     int rows, cols;
@@ -92,41 +89,44 @@ struct QuantArgs {
     float *scale, *values;
 };
 
-// One pass: THREADS threads (a warp, or a whole block) hold their row in E
-// registers each, find the largest |x|, and write. VEC elements at a time:
-// four where every row's start allows it, else one (loads and stores of
-// neighbouring threads are still neighbours).
-template <class T, int VEC, int E, int THREADS, int BLOCK = THREADS == 32 ? 256 : THREADS>
+// One pass: THREADS threads (a warp, or a whole block) hold their row in
+// registers, E elements each, find the largest |x|, and write. 16 bytes at a
+// time where every row's start allows it (VEC), else one element (loads and
+// stores of neighbouring threads are still neighbours).
+template <class T, bool VEC, int E, int THREADS, int BLOCK = THREADS == 32 ? 256 : THREADS>
 __global__ void __launch_bounds__(BLOCK) k_quantize_rows(const T *__restrict__ x, const QuantArgs a) {
+    constexpr int P = VEC ? Pack<T>::P : 1, L = E / P;
     __shared__ unsigned s_top[32];
     let_next_launch();
     const int t = threadIdx.x % THREADS;
     const long long r = (long long)blockIdx.x * (BLOCK / THREADS) + threadIdx.x / THREADS;
     if (r >= a.rows) return;  // a whole warp, or never
     const T *row = x + r * a.ld_x;
-    float v[E / VEC][VEC];
-    unsigned top = 0;
+    uint4 raw[VEC ? L : 1];
+    float one[VEC ? 1 : L];
+    auto value = [&](int j, int i) { return VEC ? Pack<T>::one(raw[VEC ? j : 0], i) : one[VEC ? 0 : j]; };
 #pragma unroll
-    for (int j = 0; j < E / VEC; ++j) {
-        const int k = (j * THREADS + t) * VEC;
+    for (int j = 0; j < L; ++j) {
+        const int k = (j * THREADS + t) * P;
+        if constexpr (VEC) {
+            raw[j] = make_uint4(0, 0, 0, 0);
+            if (k + P <= a.cols) {
+                raw[j] = *reinterpret_cast<const uint4 *>(row + k);
+            } else if (k < a.cols) {
+                T part[P];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) v[j][i] = 0.f;
-        if constexpr (VEC == 4) {
-            if (k + 4 <= a.cols) {
-                load4(row + k, v[j]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (k + i < a.cols) v[j][i] = to_f32<T>(row[k + i]);
+                for (int i = 0; i < P; ++i) part[i] = k + i < a.cols ? row[k + i] : T(0.f);
+                raw[j] = *reinterpret_cast<const uint4 *>(part);
             }
         } else {
-            if (k < a.cols) v[j][0] = to_f32<T>(row[k]);
+            one[j] = k < a.cols ? to_f32<T>(row[k]) : 0.f;
         }
     }
+    unsigned top = 0;
 #pragma unroll
-    for (int j = 0; j < E / VEC; ++j)
+    for (int j = 0; j < L; ++j)
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) top = max(top, __float_as_uint(v[j][i]) & 0x7fffffffu);
+        for (int i = 0; i < P; ++i) top = max(top, __float_as_uint(value(j, i)) & 0x7fffffffu);
     top = __reduce_max_sync(0xffffffffu, top);
     if constexpr (THREADS > 32) {
         if ((t & 31) == 0) s_top[t >> 5] = top;
@@ -139,23 +139,32 @@ __global__ void __launch_bounds__(BLOCK) k_quantize_rows(const T *__restrict__ x
     int8_t *q = a.q + r * a.ld_q;
     float *val = a.values ? a.values + r * a.ld_v : nullptr;
 #pragma unroll
-    for (int j = 0; j < E / VEC; ++j) {
-        const int k = (j * THREADS + t) * VEC;
+    for (int j = 0; j < L; ++j) {
+        const int k = (j * THREADS + t) * P;
         if (k >= a.cols) break;
-        int n[VEC];
+        int n[P];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) n[i] = code_of(v[j][i], c);
-        if constexpr (VEC == 4) {
-            if (k + 4 <= a.cols) {
-                *reinterpret_cast<char4 *>(q + k) = make_char4((char)n[0], (char)n[1], (char)n[2], (char)n[3]);
-                if (val)
-                    *reinterpret_cast<float4 *>(val + k) =
-                        make_float4(n[0] * c.scale, n[1] * c.scale, n[2] * c.scale, n[3] * c.scale);
+        for (int i = 0; i < P; ++i) n[i] = code_of(value(j, i), c);
+        if constexpr (VEC) {
+            if (k + P <= a.cols) {
+                uint32_t w[P / 4];
+#pragma unroll
+                for (int i = 0; i < P / 4; ++i)
+                    w[i] = (uint32_t)(n[4 * i] & 255) | (uint32_t)(n[4 * i + 1] & 255) << 8 |
+                           (uint32_t)(n[4 * i + 2] & 255) << 16 | (uint32_t)n[4 * i + 3] << 24;
+                if constexpr (P == 4) *reinterpret_cast<uint32_t *>(q + k) = w[0];
+                else *reinterpret_cast<uint2 *>(q + k) = make_uint2(w[0], w[1]);
+                if (val) {
+#pragma unroll
+                    for (int i = 0; i < P; i += 4)
+                        *reinterpret_cast<float4 *>(val + k + i) = make_float4(
+                            n[i] * c.scale, n[i + 1] * c.scale, n[i + 2] * c.scale, n[i + 3] * c.scale);
+                }
                 continue;
             }
         }
 #pragma unroll
-        for (int i = 0; i < VEC; ++i)
+        for (int i = 0; i < P; ++i)
             if (k + i < a.cols) {
                 q[k + i] = (int8_t)n[i];
                 if (val) val[k + i] = n[i] * c.scale;
@@ -190,23 +199,25 @@ __global__ void __launch_bounds__(256) k_quantize_long(const T *__restrict__ x, 
 
 template <class T>
 void quantize(const T *x, const QuantArgs &a, cudaStream_t st) {
-    const uintptr_t x4 = 4 * sizeof(T) - 1;
-    const bool vec = ((reinterpret_cast<uintptr_t>(x) & x4) | (a.ld_x & 3)) == 0 &&
-                     ((reinterpret_cast<uintptr_t>(a.q) | a.ld_q) & 3) == 0 &&
+    constexpr int P = Pack<T>::P;
+    const bool vec = ((reinterpret_cast<uintptr_t>(x) & 15) | (a.ld_x & (P - 1))) == 0 &&
+                     ((reinterpret_cast<uintptr_t>(a.q) | a.ld_q) & (P - 1)) == 0 &&
                      (!a.values || ((reinterpret_cast<uintptr_t>(a.values) & 15) | (a.ld_v & 3)) == 0);
     const unsigned rows = (unsigned)a.rows, warps = (rows + 7) / 8;
     if (a.cols <= 256) {
-        if (vec) k_quantize_rows<T, 4, 8, 32><<<warps, 256, 0, st>>>(x, a);
-        else k_quantize_rows<T, 1, 8, 32><<<warps, 256, 0, st>>>(x, a);
+        if (vec) k_quantize_rows<T, true, 8, 32><<<warps, 256, 0, st>>>(x, a);
+        else k_quantize_rows<T, false, 8, 32><<<warps, 256, 0, st>>>(x, a);
     } else if (a.cols <= 1024) {
-        if (vec) k_quantize_rows<T, 4, 32, 32><<<warps, 256, 0, st>>>(x, a);
-        else k_quantize_rows<T, 1, 32, 32><<<warps, 256, 0, st>>>(x, a);
+        if (vec) k_quantize_rows<T, true, 32, 32><<<warps, 256, 0, st>>>(x, a);
+        else k_quantize_rows<T, false, 32, 32><<<warps, 256, 0, st>>>(x, a);
     } else if (a.cols <= 4096) {
-        if (vec) k_quantize_rows<T, 4, 16, 256><<<rows, 256, 0, st>>>(x, a);
-        else k_quantize_rows<T, 1, 16, 256><<<rows, 256, 0, st>>>(x, a);
+        if (vec) k_quantize_rows<T, true, 16, 256><<<rows, 256, 0, st>>>(x, a);
+        else k_quantize_rows<T, false, 16, 256><<<rows, 256, 0, st>>>(x, a);
     } else if (a.cols <= 16384) {
-        if (vec) k_quantize_rows<T, 4, 16, 1024><<<rows, 1024, 0, st>>>(x, a);
-        else k_quantize_rows<T, 1, 16, 1024><<<rows, 1024, 0, st>>>(x, a);
+        // as many elements a thread as leave 2048 threads on an SM
+        constexpr int E = sizeof(T) == 4 ? 16 : 32;
+        if (vec) k_quantize_rows<T, true, E, 16384 / E><<<rows, 16384 / E, 0, st>>>(x, a);
+        else k_quantize_rows<T, false, 16, 1024><<<rows, 1024, 0, st>>>(x, a);
     } else {
         k_quantize_long<T><<<rows, 256, 0, st>>>(x, a);
     }
@@ -871,13 +882,17 @@ struct PrepArgs {
     long long x_threads, w_threads, zeros;
 };
 
+__device__ __forceinline__ long long quotient(long long i, int d) {
+    return i < (1ll << 31) ? (long long)((unsigned)i / (unsigned)d) : i / d;
+}
+
 __global__ void __launch_bounds__(256) k_q8_prep(const PrepArgs a) {
     wait_launch_before();
     let_next_launch();
     long long i = (long long)blockIdx.x * 256 + threadIdx.x;
     if (i < a.x_threads) {
         const int chunks = (a.ld + 15) / 16;
-        const long long t = i / chunks;
+        const long long t = quotient(i, chunks);
         const int k = (int)(i - t * chunks) * 16;
         const int8_t *p = a.x + t * a.ld_x + k;
         const int8_t *end = matrix_end(a.x, a.T, a.K, a.ld_x);
@@ -897,7 +912,7 @@ __global__ void __launch_bounds__(256) k_q8_prep(const PrepArgs a) {
     i -= a.x_threads;
     if (i < a.w_threads) {
         const int chunks = a.ld_wc / 16;
-        const long long n = i / chunks;
+        const long long n = quotient(i, chunks);
         const int k = (int)(i - n * chunks) * 16;
         const int8_t *p = a.w + n * a.ld_w + k;
         *reinterpret_cast<uint4 *>(a.wc + n * a.ld_wc + k) =
