@@ -1683,25 +1683,22 @@ int check_tensors(int count, const void *const *g, const int64_t *n, const int32
     return DSTD_OK;
 }
 
-// layout of the 8-bit layer forward: grid weights, their codes and scales, w^
+// layout of the 8-bit layer forward: the grid weights' codes and scales, w^
 // (D[i][(b, m)], as the scan reads it), the weights' row sums, the product's scratch
 struct Q8Ws {
-    float *s32 = nullptr, *scale = nullptr, *D = nullptr, *rowsum = nullptr;
+    float *scale = nullptr, *D = nullptr, *rowsum = nullptr;
     int8_t *q = nullptr;
     char *product = nullptr;
     size_t bytes = 0;
-    int ld = 0;
     long long ld_q = 0;
 };
 Q8Ws q8_layout(void *base, int B, int N_in, int N_out, int Mp) {
     Q8Ws w;
     Bump b(base);
     const long long T = (long long)B * Mp;
-    w.ld = pad8(N_in);
     w.ld_q = ((long long)N_in + 15) / 16 * 16;
     w.rowsum = b.take<float>(N_out);
     w.scale = b.take<float>((size_t)T);
-    w.s32 = b.take<float>((size_t)T * w.ld);
     w.q = b.take<int8_t>((size_t)T * w.ld_q);
     w.D = b.take<float>((size_t)T * N_out);
     w.product = b.take<char>(q8_workspace_bytes((int)T, N_out, N_in));
@@ -1779,11 +1776,12 @@ int dstd_dense_fwd_q8(const float *t_in, const int8_t *w_q, const float *w_scale
     if (penalty) TRY(cu(cudaMemsetAsync(penalty, 0, 4 * sizeof(float), st)));
     {
         Timed tm(KK_BIN, st);
-        TRY(cu(launch_binning(t_in, B, N_in, c, OpKind::F32, false, ws.s32, nullptr, ws.ld, st)));
+        TRY(cu(launch_bin_codes(t_in, B, N_in, c, ws.q, ws.ld_q, ws.scale, st)));
     }
-    {
-        Timed tm(KK_QUANTIZE, st);
-        TRY(cu(launch_quantize_rows(ws.s32, DSTD_TYPE_F32, T, N_in, ws.ld, ws.q, ws.ld_q, ws.scale, nullptr, 0, st)));
+    // only the value of the dead-neuron penalty needs the weights' row sums
+    const bool sums = penalty && p->gamma_q != 0.0f;
+    if (sums) {
+        Timed tm(KK_PREP, st);
         TRY(cu(launch_q8_rowsum(w_q, N_in, N_out, N_in, w_scale, ws.rowsum, st)));
     }
     {
@@ -1792,8 +1790,8 @@ int dstd_dense_fwd_q8(const float *t_in, const int8_t *w_q, const float *w_scale
         TRY(cu(launch_q8_product(a, ws.product, st)));
     }
     Timed tm(KK_SCAN, st);
-    return cu(launch_scan_solve(ws.D, Mp, T, 1, B, N_out, c, nullptr, ws.rowsum, t_out, sv.q, sv.s, sv.vdot, penalty,
-                                st));
+    return cu(launch_scan_solve(ws.D, Mp, T, 1, B, N_out, c, nullptr, sums ? ws.rowsum : nullptr, t_out, sv.q, sv.s,
+                                sv.vdot, penalty, st));
 }
 
 size_t dstd_grad_norm_workspace_bytes(int count, const int64_t *n) {

@@ -723,6 +723,9 @@ cudaError_t launch_clip(const ClipTensors &t, ClipOp op, const ClipHyper &h, flo
 // 8-bit rows and their products (dstd_q8.cu).
 cudaError_t launch_quantize_rows(const void *x, dstd_type type, int rows, int cols, long long ld_x, int8_t *q,
                                  long long ld_q, float *scale, float *values, long long ld_v, cudaStream_t st);
+// grid weights of t [B, N] as codes [B Mp, ld_q] (ld_q a multiple of 4, >= N) and row scales [B Mp]; Mp <= 128
+cudaError_t launch_bin_codes(const float *t, int B, int N, const LifConst &c, int8_t *q, long long ld_q, float *scale,
+                             cudaStream_t st);
 cudaError_t launch_q8_rowsum(const int8_t *w, long long ld, int N, int K, const float *scale, float *rowsum,
                              cudaStream_t st);
 // y at p[t * ld_t + n * ld_n]

@@ -233,15 +233,92 @@ cudaError_t launch_quantize_rows(const void *x, dstd_type type, int rows, int co
     return cudaGetLastError();
 }
 
-// row sums of the weights' values: rowsum_n = scale_n sum_k q_nk (one warp per row)
+// ---------------------------------------------------------------------------
+// Grid weights of a layer's inputs straight to tokens: t [B, N] -> codes of row
+// (b, m), zero for M <= m < Mp, and the rows' scales; the same codes as from
+// writing the grid weights out and quantising their rows. An input touches two
+// grid points, so the fp32 rows (M times the inputs) never exist: a block first
+// takes the largest weight of every grid point over all inputs of its sample
+// (in shared memory; the bits of positive floats order like the floats; a plain
+// look first keeps all but the early ones from the atomics), then writes the
+// codes of its 4 THREADS inputs, four to a word.
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ void raise_top(unsigned *top, float w) {
+    const unsigned bits = __float_as_uint(w) & 0x7fffffffu;
+    if (bits > *(volatile unsigned *)top) atomicMax(top, bits);
+}
+
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) k_bin_codes(const float *__restrict__ t, int N, const LifConst c, int8_t *q,
+                                                   long long ld_q, float *scale) {
+    __shared__ unsigned s_top[128];
+    const int b = blockIdx.y;
+    const float *row = t + (long long)b * N;
+    for (int m = threadIdx.x; m < c.Mp; m += THREADS) s_top[m] = 0;
+    __syncthreads();
+    for (int j = threadIdx.x; j < N; j += 4 * THREADS) {
+        float x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = j + i * THREADS < N ? __ldg(row + j + i * THREADS) : INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (!isfinite(x[i])) continue;
+            const BinW w = bin_weights(c, x[i], false);
+            if (w.k >= 0 && w.k < c.M) raise_top(&s_top[w.k], w.wR);
+            if (w.k >= -1 && w.k + 1 < c.M) raise_top(&s_top[w.k + 1], w.wL);
+        }
+    }
+    __syncthreads();
+    if (blockIdx.x == 0)
+        for (int m = threadIdx.x; m < c.Mp; m += THREADS) scale[(long long)b * c.Mp + m] = row_code(s_top[m]).scale;
+    const int j0 = (blockIdx.x * THREADS + threadIdx.x) * 4;
+    if (j0 >= ld_q) return;
+    int k[4], first[4], second[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        k[i] = -100;
+        first[i] = second[i] = 0;
+        const float x = j0 + i < N ? row[j0 + i] : INFINITY;
+        if (!isfinite(x)) continue;
+        const BinW w = bin_weights(c, x, false);
+        k[i] = w.k;
+        if (w.k >= 0 && w.k < c.M) first[i] = code_of(w.wR, row_code(s_top[w.k])) & 255;
+        if (w.k >= -1 && w.k + 1 < c.M) second[i] = code_of(w.wL, row_code(s_top[w.k + 1])) & 255;
+    }
+    int8_t *out = q + (long long)b * c.Mp * ld_q + j0;
+    for (int m = 0; m < c.Mp; ++m, out += ld_q) {
+        uint32_t word = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) word |= (uint32_t)(m == k[i] ? first[i] : (m == k[i] + 1 ? second[i] : 0)) << (8 * i);
+        *reinterpret_cast<uint32_t *>(out) = word;
+    }
+}
+
+cudaError_t launch_bin_codes(const float *t, int B, int N, const LifConst &c, int8_t *q, long long ld_q, float *scale,
+                             cudaStream_t st) {
+    // every block passes over all inputs of its sample: long rows take blocks of more threads
+    if (ld_q <= 1024) k_bin_codes<256><<<dim3(1, (unsigned)B), 256, 0, st>>>(t, N, c, q, ld_q, scale);
+    else k_bin_codes<1024><<<dim3((unsigned)((ld_q + 4095) / 4096), (unsigned)B), 1024, 0, st>>>(t, N, c, q, ld_q, scale);
+    return cudaGetLastError();
+}
+
+// row sums of the weights' values: rowsum_n = scale_n sum_k q_nk (one warp per
+// row, whose start is at any address: words of four codes from the first aligned one)
 __global__ void __launch_bounds__(256) k_q8_rowsum(const int8_t *__restrict__ w, long long ld, int N, int K,
                                                    const float *__restrict__ scale, float *rowsum) {
-    const int n = blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int n = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (n >= N) return;
+    const int8_t *row = w + (long long)n * ld;
+    const int head = min(K, (int)(-reinterpret_cast<uintptr_t>(row) & 3)), words = (K - head) / 4;
     int sum = 0;
-    for (int k = threadIdx.x & 31; k < K; k += 32) sum += w[(long long)n * ld + k];
+    const int *p = reinterpret_cast<const int *>(row + head);
+#pragma unroll 8
+    for (int i = lane; i < words; i += 32) sum = __dp4a(__ldg(p + i), 0x01010101, sum);
+    const int done = head + 4 * words;
+    if (lane < head) sum += row[lane];
+    if (done + lane < K) sum += row[done + lane];
     sum = __reduce_add_sync(0xffffffffu, sum);
-    if ((threadIdx.x & 31) == 0) rowsum[n] = scale[n] * (float)sum;
+    if (lane == 0) rowsum[n] = scale[n] * (float)sum;
 }
 
 cudaError_t launch_q8_rowsum(const int8_t *w, long long ld, int N, int K, const float *scale, float *rowsum,

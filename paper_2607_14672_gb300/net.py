@@ -121,6 +121,11 @@ class DenseNet(Clipped):
         for w, q, scale, v in zip(self.W, self.Wq, self.w_scale, self.Wv):
             dstd.quantize_rows(w, q, scale, v, stream)
 
+    def take_codes(self, other):
+        """The 8-bit weights of another q8 network of the same layers (e.g. of another batch size)."""
+        for mine, theirs in zip(self.Wq + self.w_scale, other.Wq + other.w_scale):
+            mine.copy_(theirs)
+
     def serve(self, stream=None):
         """The forward on the 8-bit codes as they are (no weight is read in fp32)."""
         for l in range(len(self.W)):

@@ -379,3 +379,17 @@ def test_network_trains_and_serves_in_8_bits():
     for x, b in zip(n.W + n.m + n.v, after[:-1]):
         assert rel_l2(x.cpu().numpy(), b.cpu().numpy()) <= 1e-3
     assert torch.equal(n.adam_state, after[-1])
+
+
+def test_example_trains_and_serves():
+    """The example: a captured training loop, then single samples from the codes
+    alone with the batch's spike times (whole-number sums do not depend on the
+    number of tokens, nor the scan on the batch)."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "q8_mlp.py")
+    spec = importlib.util.spec_from_file_location("q8_mlp", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    losses, same = m.main(["--steps", "6", "--batch", "16"])
+    assert all(math.isfinite(x) for x in losses) and same
