@@ -471,9 +471,9 @@ int dstd_dense_fwd_q8(const float *t_in, const int8_t *w_q, const float *w_scale
 /* Norm of many gradients, clipping by it, and the clipped update.
  *
  * The three calls below share a workspace of
- * dstd_grad_norm_workspace_bytes(count, n) bytes, whose first 256 bytes are
- * zero before its first use and are left so; calls that can overlap on the GPU
- * need one each. count >= 1 tensors of n[i] >= 0 elements (the arrays of
+ * dstd_grad_norm_workspace_bytes(count, n) bytes, whose first 64 bytes are
+ * zero before its first use and are left so by every call (zero them again
+ * after a DSTD_E_TIMEOUT); calls that can overlap on the GPU need one each. count >= 1 tensors of n[i] >= 0 elements (the arrays of
  * pointers and sizes are host memory, read during the call); type[i] is the
  * dstd_type of gradient i. Sums are formed in a fixed order: the same call on
  * the same tensors gives the same bits. */

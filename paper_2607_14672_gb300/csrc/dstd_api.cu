@@ -1634,11 +1634,12 @@ int dstd_dense_fwd_noalloc(const float *t_in, const float *W, int B, int N_in, i
 
 int dstd_device_status(int clear) {
     if (cudaDeviceSynchronize() != cudaSuccess) return DSTD_E_CUDA;
-    unsigned int s = 0, s2 = 0, s3 = 0;
+    unsigned int s = 0, s2 = 0, s3 = 0, s4 = 0;
     if (status_read(&s, clear) != cudaSuccess) return DSTD_E_CUDA;
     if (conv_status_read(&s2, clear) != cudaSuccess) return DSTD_E_CUDA;
     if (q8_status_read(&s3, clear) != cudaSuccess) return DSTD_E_CUDA;
-    return ((s | s2 | s3) & STATUS_TIMEOUT) ? DSTD_E_TIMEOUT : DSTD_OK;
+    if (clip_status_read(&s4, clear) != cudaSuccess) return DSTD_E_CUDA;
+    return ((s | s2 | s3 | s4) & STATUS_TIMEOUT) ? DSTD_E_TIMEOUT : DSTD_OK;
 }
 
 int dstd_conv_set_chunk_images(int max_images) {
@@ -1825,7 +1826,6 @@ int dstd_clip_grads(int count, const void *const *g, void *const *out, const int
     const ClipTensors t{count, g, out, nullptr, nullptr, n, type};
     ClipHyper h{};
     h.max_norm = max_norm;
-    TRY(cu(launch_clip(t, ClipOp::Norm, h, norm, nullptr, workspace, (cudaStream_t)stream)));
     return cu(launch_clip(t, ClipOp::Scale, h, norm, nullptr, workspace, (cudaStream_t)stream));
 }
 
@@ -1847,7 +1847,6 @@ int dstd_adamw_clip(int count, float *const *w, const void *const *g, float *con
     Timed tm(KK_CLIP, (cudaStream_t)stream);
     const ClipTensors t{count, g, reinterpret_cast<void *const *>(w), m, v, n, type};
     const ClipHyper h{max_norm, lr, beta1, beta2, eps, weight_decay, step, lr_dev};
-    TRY(cu(launch_clip(t, ClipOp::Norm, h, norm, nullptr, workspace, (cudaStream_t)stream)));
     return cu(launch_clip(t, ClipOp::Adamw, h, norm, nullptr, workspace, (cudaStream_t)stream));
 }
 

@@ -4,7 +4,12 @@
 
 #include <math.h>
 
+#include <algorithm>
+#include <type_traits>
+
 namespace dstd {
+
+__device__ unsigned int g_status_clip = 0;
 
 namespace {
 
@@ -169,18 +174,16 @@ __device__ __forceinline__ void chunk_squares(const T *g, long long n, Pair &s, 
     }
 }
 
-// Sum of squares of every chunk into its own slot (no atomics on the sums:
-// the result does not depend on the order in which blocks run). The block that
-// draws the last ticket then adds the slots in order, and derives from the
-// total what the clipping needs.
-template <int CAP>
-__global__ void __launch_bounds__(THREADS) k_sum_squares(const ClipArgs<CAP> a) {
-    __shared__ float s_hi[THREADS / 32], s_lo[THREADS / 32];
-    __shared__ double s_rare[THREADS / 32];
-    __shared__ bool s_last;
+struct SumShared {
+    float hi[THREADS / 32], lo[THREADS / 32];
+    double rare[THREADS / 32];
+};
+// Sums of squares of this block's chunks (blockIdx.x, + gridDim.x, ...), each
+// into its own slot: no atomics on the sums, so that the result does not depend
+// on the order in which blocks run.
+template <class A>
+__device__ __forceinline__ void sum_chunks(const A &a, SumShared &sh) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    // the pass that applies the norm may be launched while this one runs
-    asm volatile("griddepcontrol.launch_dependents;");
     for (unsigned c = blockIdx.x; c < a.chunks; c += gridDim.x) {
         const ClipSeg &sg = a.seg[seg_of(a, c)];
         const long long lo = (long long)(c - sg.first) * a.chunk;
@@ -199,19 +202,44 @@ __global__ void __launch_bounds__(THREADS) k_sum_squares(const ClipArgs<CAP> a) 
             for (int o = 16; o > 0; o >>= 1) rare += __shfl_down_sync(0xffffffffu, rare, o);
         }
         if (lane == 0) {
-            s_hi[warp] = s.hi;
-            s_lo[warp] = s.lo;
-            s_rare[warp] = rare;
+            sh.hi[warp] = s.hi;
+            sh.lo[warp] = s.lo;
+            sh.rare[warp] = rare;
         }
         __syncthreads();
         if (threadIdx.x == 0) {
-            for (int w = 1; w < THREADS / 32; ++w) s.add(s_hi[w], s_lo[w]);
+            for (int w = 1; w < THREADS / 32; ++w) s.add(sh.hi[w], sh.lo[w]);
             if (any)
-                for (int w = 1; w < THREADS / 32; ++w) rare += s_rare[w];
+                for (int w = 1; w < THREADS / 32; ++w) rare += sh.rare[w];
             a.partial[c] = (double)s.hi + (double)s.lo + rare;
         }
         __syncthreads();
     }
+}
+// the slots' sum, by one warp (lane 0 has it)
+template <class A>
+__device__ __forceinline__ double sum_slots(const A &a) {
+    double s = 0.0;
+#pragma unroll 8
+    for (unsigned c = threadIdx.x & 31; c < a.chunks; c += 32) s += __ldcg(a.partial + c);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_down_sync(0xffffffffu, s, o);
+    return s;
+}
+__device__ __forceinline__ float clip_factor(double norm, double max_norm) {
+    return isfinite(norm) && norm > max_norm ? (float)(max_norm / norm) : 1.f;
+}
+
+// The norm by itself: the block that draws the last ticket adds the slots in
+// order, and derives from the total what the clipping needs.
+template <int CAP>
+__global__ void __launch_bounds__(THREADS) k_sum_squares(const ClipArgs<CAP> a) {
+    __shared__ SumShared sh;
+    __shared__ bool s_last;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    // the pass that applies the norm may be launched while this one runs
+    asm volatile("griddepcontrol.launch_dependents;");
+    sum_chunks(a, sh);
     if (threadIdx.x == 0) {
         __threadfence();
         s_last = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
@@ -230,23 +258,17 @@ __global__ void __launch_bounds__(THREADS) k_sum_squares(const ClipArgs<CAP> a) 
         }
     }
     if (warp != 0) return;
-    double s = 0.0;
-#pragma unroll 8
-    for (unsigned c = lane; c < a.chunks; c += 32) s += a.partial[c];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_down_sync(0xffffffffu, s, o);
+    const double s = sum_slots(a);
     if (lane == 0) {
         *a.ticket = 0;
-        const double before = a.launch == 0 ? 0.0 : a.result->sum;
-        const double sum = before + s;
+        const double sum = (a.launch == 0 ? 0.0 : a.result->sum) + s;
         a.result->sum = sum;
         if (a.last_launch) {
             const double norm = sqrt(sum);
-            const bool finite = isfinite(sum);
             a.norm[0] = (float)norm;
-            a.result->coef = finite && norm > a.max_norm ? (float)(a.max_norm / norm) : 1.f;
-            a.result->skip = finite ? 0 : 1;
-            if (a.step && finite) a.step[0] += 1;
+            a.result->coef = clip_factor(norm, a.max_norm);
+            a.result->skip = isfinite(norm) ? 0 : 1;
+            if (a.step && isfinite(norm)) a.step[0] += 1;
         }
     }
 }
@@ -281,10 +303,8 @@ __device__ __forceinline__ void scale_chunk(const T *g, T *out, long long n, flo
     }
 }
 
-template <int CAP>
-__global__ void __launch_bounds__(THREADS) k_clip_scale(const ClipArgs<CAP> a) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");  // for the norm
-    const float coef = a.result->coef;
+template <class A>
+__device__ __forceinline__ void scale_chunks(const A &a, float coef) {
     for (unsigned c = blockIdx.x; c < a.chunks; c += gridDim.x) {
         const ClipSeg &sg = a.seg[seg_of(a, c)];
         if (coef == 1.f && sg.out == sg.g) continue;
@@ -355,13 +375,11 @@ __device__ __forceinline__ void adamw_chunk(const StepConst &c, const T *g, floa
     }
 }
 
-template <int CAP>
-__global__ void __launch_bounds__(THREADS) k_adamw_clip(const ClipArgs<CAP> a) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");  // for the norm
-    if (a.result->skip) return;
+// t: updates done with this one
+template <class A>
+__device__ __forceinline__ void adamw_chunks(const A &a, float coef, float t) {
     StepConst k;
-    const float t = (float)a.step[0];
-    k.coef = a.result->coef;
+    k.coef = coef;
     k.b1 = a.b1;
     k.one_b1 = a.one_b1;
     k.b2 = a.b2;
@@ -384,7 +402,76 @@ __global__ void __launch_bounds__(THREADS) k_adamw_clip(const ClipArgs<CAP> a) {
     }
 }
 
+// The passes after k_sum_squares.
+template <int CAP, bool STEP>
+__global__ void __launch_bounds__(THREADS) k_clip_apply(const ClipArgs<CAP> a) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // for the norm
+    if constexpr (STEP) {
+        if (!a.result->skip) adamw_chunks(a, a.result->coef, (float)a.step[0]);
+    } else {
+        scale_chunks(a, a.result->coef);
+    }
+}
+
+// Short lists: norm and pass in one cooperative launch. Every block leaves its
+// sums, waits for the others', and adds up all slots itself, in the same order:
+// no ticket, no last block that the rest waits for, and no second launch
+// (asking for the update's other operands in L2 before the wait made it slower).
+// The wait ends by itself after about 2 s; a block whose wait ran out changes
+// nothing and sets the status word.
+template <int CAP, bool STEP>
+__global__ void __launch_bounds__(THREADS, 2) k_clip_once(const ClipArgs<CAP> a) {
+    __shared__ SumShared sh;
+    __shared__ float s_coef;
+    __shared__ int s_go;
+    unsigned *arrived = a.ticket + 1, *left = a.ticket + 2;
+    const float t = STEP ? (float)(a.step[0] + 1) : 0.f;
+    sum_chunks(a, sh);
+    if (threadIdx.x == 0) {
+        __threadfence();
+        atomicAdd(arrived, 1u);
+        int go = 1;
+        const long long t0 = clock64();
+        for (;;) {
+            unsigned n;
+            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(n) : "l"(arrived) : "memory");
+            if (n >= gridDim.x) break;
+            if (clock64() - t0 > 4000000000ll) {
+                go = 0;
+                atomicOr(&g_status_clip, STATUS_TIMEOUT);
+                break;
+            }
+        }
+        s_go = go;
+    }
+    __syncthreads();
+    if (s_go && threadIdx.x < 32) {
+        const double sum = sum_slots(a);
+        if (threadIdx.x == 0) {
+            const double norm = sqrt(sum);
+            s_coef = clip_factor(norm, a.max_norm);
+            if (STEP && !isfinite(norm)) s_go = 0;
+            if (blockIdx.x == 0) a.norm[0] = (float)norm;
+        }
+    }
+    __syncthreads();
+    if (s_go) {
+        if constexpr (STEP) adamw_chunks(a, s_coef, t);
+        else scale_chunks(a, s_coef);
+    }
+    if (threadIdx.x == 0) {
+        // the last block to leave: every other one has read the count and the slots
+        if (atomicAdd(left, 1u) == gridDim.x - 1) {
+            *arrived = 0;
+            *left = 0;
+            if (STEP && s_go) a.step[0] += 1;
+        }
+    }
+}
+
 constexpr int kBlocks = 152 * 6;
+constexpr int kOnceBlocks = 152 * 4;                    // at most, of the one-launch form
+constexpr long long kOnceElements = 1ll << 24;          // longer lists take two launches
 
 // elements of a chunk: about one chunk per resident block. For the norm in
 // multiples of 4096 (four 16-byte loads of fp32 a thread): small lists take
@@ -398,7 +485,7 @@ long long chunk_elements(int count, const int64_t *n, int least) {
 }
 
 template <int CAP>
-cudaError_t launch_group(const ClipTensors &t, ClipOp op, int begin, int count, ClipArgs<CAP> &a, cudaStream_t st) {
+void fill_segments(const ClipTensors &t, int begin, int count, ClipArgs<CAP> &a) {
     unsigned chunks = 0;
     a.count = 0;
     for (int i = begin; i < begin + count; ++i) {
@@ -413,6 +500,12 @@ cudaError_t launch_group(const ClipTensors &t, ClipOp op, int begin, int count, 
         chunks += (unsigned)((t.n[i] + a.chunk - 1) / a.chunk);
     }
     a.chunks = chunks;
+}
+
+template <int CAP>
+cudaError_t launch_group(const ClipTensors &t, ClipOp op, int begin, int count, ClipArgs<CAP> &a, cudaStream_t st) {
+    fill_segments(t, begin, count, a);
+    const unsigned chunks = a.chunks;
     const unsigned grid = chunks < 1 ? 1 : (chunks < kBlocks ? chunks : kBlocks);
     if (op == ClipOp::Norm) {
         k_sum_squares<CAP><<<grid, THREADS, 0, st>>>(a);
@@ -427,7 +520,42 @@ cudaError_t launch_group(const ClipTensors &t, ClipOp op, int begin, int count, 
     cfg.gridDim = dim3(grid);
     cfg.blockDim = dim3(THREADS);
     cfg.stream = st;
-    return cudaLaunchKernelEx(&cfg, op == ClipOp::Scale ? k_clip_scale<CAP> : k_adamw_clip<CAP>, a);
+    return cudaLaunchKernelEx(&cfg, op == ClipOp::Scale ? k_clip_apply<CAP, false> : k_clip_apply<CAP, true>, a);
+}
+
+// blocks of the one-launch form that are resident at once (0: an error)
+template <int CAP, bool STEP>
+unsigned once_blocks() {
+    static const unsigned blocks = [] {
+        int dev = 0, sms = 0, each = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess ||
+            cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+            cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, k_clip_once<CAP, STEP>, THREADS, 0) != cudaSuccess)
+            return 0u;
+        return (unsigned)(sms * std::min(each, kOnceBlocks / 152));
+    }();
+    return blocks;
+}
+
+template <int CAP, bool STEP>
+cudaError_t launch_once(const ClipTensors &t, long long total, ClipArgs<CAP> &a, cudaStream_t st) {
+    const unsigned blocks = std::min(once_blocks<CAP, STEP>(), (unsigned)kOnceBlocks);
+    if (blocks == 0) return cudaErrorInvalidConfiguration;
+    // one chunk a block where the list allows it: every tensor's last chunk may be a short one
+    const long long share = blocks > 2u * t.count ? (total + blocks - t.count - 1) / (blocks - t.count)
+                                                  : 2 * ((total + blocks - 1) / blocks);
+    a.chunk = std::max(1024ll, (share + 63) / 64 * 64);
+    fill_segments(t, 0, t.count, a);
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeCooperative;
+    attr[0].val.cooperative = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cfg.gridDim = dim3(std::max(1u, std::min(a.chunks, blocks)));
+    cfg.blockDim = dim3(THREADS);
+    cfg.stream = st;
+    return cudaLaunchKernelEx(&cfg, k_clip_once<CAP, STEP>, a);
 }
 
 }  // namespace
@@ -436,18 +564,26 @@ size_t clip_workspace_bytes(int count, const int64_t *n) {
     const long long chunk = chunk_elements(count, n, 4096);
     size_t chunks = 0;
     for (int i = 0; i < count; ++i) chunks += (size_t)((n[i] + chunk - 1) / chunk);
-    return 256 + 8 * chunks;
+    // the one-launch form has at most a chunk a block and one more a tensor
+    return 256 + 8 * std::max(chunks, (size_t)kOnceBlocks + (size_t)std::min(count, kClipMaxTensors));
+}
+
+cudaError_t clip_status_read(unsigned int *out, int clear) {
+    cudaError_t e = cudaMemcpyFromSymbol(out, g_status_clip, sizeof(unsigned int));
+    if (e != cudaSuccess || !clear) return e;
+    unsigned int z = 0;
+    return cudaMemcpyToSymbol(g_status_clip, &z, sizeof(z));
 }
 
 cudaError_t launch_clip(const ClipTensors &t, ClipOp op, const ClipHyper &h, float *norm, float *norm_each,
                         void *workspace, cudaStream_t st) {
-    auto fill = [&](auto &a) {
+    auto fill = [&](auto &a, ClipOp pass) {
         a.ticket = (unsigned *)workspace;
         a.result = (ClipResult *)((char *)workspace + 64);
         a.partial = (double *)((char *)workspace + 256);
         a.norm = norm;
         a.max_norm = h.max_norm;
-        a.step = op == ClipOp::Norm || op == ClipOp::Adamw ? h.step : nullptr;
+        a.step = h.step;
         a.lr_dev = h.lr_dev;
         a.lr = (float)h.lr;
         a.b1 = (float)h.b1;
@@ -458,27 +594,47 @@ cudaError_t launch_clip(const ClipTensors &t, ClipOp op, const ClipHyper &h, flo
         a.ln_b2 = (float)log(h.b2);
         a.eps = (float)h.eps;
         a.wd = (float)h.wd;
-        a.chunk = chunk_elements(t.count, t.n, op == ClipOp::Norm ? 4096 : 2048);
+        a.chunk = chunk_elements(t.count, t.n, pass == ClipOp::Norm ? 4096 : 2048);
     };
-    for (int begin = 0, launch = 0; begin < t.count; begin += kClipMaxTensors, ++launch) {
-        const int count = t.count - begin < kClipMaxTensors ? t.count - begin : kClipMaxTensors;
-        cudaError_t e;
-        if (count <= kClipFewTensors) {
+    long long total = 0;
+    for (int i = 0; i < t.count; ++i) total += t.n[i];
+    // one launch against two, cold caches, without what any launch costs (us): a step of 100 thousand weights 6.5
+    // and 8.5, 1.3 M 12.6 and 14.6, 4.7 M 26.9 and 29.0, 16 M 82 and 83, 67 M 343 and 333
+    if (op != ClipOp::Norm && t.count <= kClipMaxTensors && total <= kOnceElements) {
+        auto once = [&](auto &a) {
+            fill(a, op);
+            return op == ClipOp::Scale ? launch_once<std::extent_v<decltype(a.seg)>, false>(t, total, a, st)
+                                       : launch_once<std::extent_v<decltype(a.seg)>, true>(t, total, a, st);
+        };
+        if (t.count <= kClipFewTensors) {
             ClipArgs<kClipFewTensors> a{};
-            fill(a);
-            a.launch = launch;
-            a.last_launch = begin + count == t.count;
-            a.norm_each = norm_each ? norm_each + begin : nullptr;
-            e = launch_group(t, op, begin, count, a, st);
-        } else {
-            ClipArgs<kClipMaxTensors> a{};
-            fill(a);
-            a.launch = launch;
-            a.last_launch = begin + count == t.count;
-            a.norm_each = norm_each ? norm_each + begin : nullptr;
-            e = launch_group(t, op, begin, count, a, st);
+            return once(a);
         }
-        if (e != cudaSuccess) return e;
+        ClipArgs<kClipMaxTensors> a{};
+        return once(a);
+    }
+    // the norm (whose last launch counts the update), then the pass
+    for (int pass = 0; pass < (op == ClipOp::Norm ? 1 : 2); ++pass) {
+        const ClipOp now = pass == 0 ? ClipOp::Norm : op;
+        for (int begin = 0, launch = 0; begin < t.count; begin += kClipMaxTensors, ++launch) {
+            const int count = std::min(t.count - begin, kClipMaxTensors);
+            auto group = [&](auto &a) {
+                fill(a, now);
+                a.launch = launch;
+                a.last_launch = begin + count == t.count;
+                a.norm_each = norm_each ? norm_each + begin : nullptr;
+                return launch_group(t, now, begin, count, a, st);
+            };
+            cudaError_t e;
+            if (count <= kClipFewTensors) {
+                ClipArgs<kClipFewTensors> a{};
+                e = group(a);
+            } else {
+                ClipArgs<kClipMaxTensors> a{};
+                e = group(a);
+            }
+            if (e != cudaSuccess) return e;
+        }
     }
     return cudaSuccess;
 }

@@ -706,7 +706,7 @@ struct ClipArgs {
     unsigned chunks;
     long long chunk;  // elements of a chunk
     int launch, last_launch;
-    unsigned *ticket;  // 0 between calls
+    unsigned *ticket;  // [3]: tickets drawn, blocks arrived, blocks left; 0 between calls
     ClipResult *result;
     double *partial;  // one sum of squares per chunk of the launch
     float *norm, *norm_each;
@@ -715,7 +715,8 @@ struct ClipArgs {
     int32_t *step;
     const float *lr_dev;
 };
-enum class ClipOp { Norm, Scale, Adamw };
+enum class ClipOp { Norm, Scale, Adamw };  // the last two with the norm before them
+cudaError_t clip_status_read(unsigned int *out, int clear);
 size_t clip_workspace_bytes(int count, const int64_t *n);
 cudaError_t launch_clip(const ClipTensors &t, ClipOp op, const ClipHyper &h, float *norm, float *norm_each,
                         void *workspace, cudaStream_t st);

@@ -62,7 +62,8 @@ F, H, P = torch.float32, torch.bfloat16, torch.float16
 LISTS = [((1,), (F,), 0), ((5,), (H,), 1), ((1000, 64, 4096), (F,), 0), ((1000, 63, 7), (F, H), 0),
          ((0, 17, 0, 1), (F, P), 0), ((0,), (F,), 0), ((1023, 1024, 1025, 2049), (F, H, P), 1),
          ((627200, 640000, 8000), (F,), 1), ((3000001, 5), (H,), 3), ((2500000, 1, 77), (F,), 0),
-         (tuple(range(1, 41)), (H, F), 0), (tuple([3, 1500] * 300), (F, P), 1)]
+         (tuple(range(1, 41)), (H, F), 0), (tuple([3, 1500] * 300), (F, P), 1),
+         ((17000001, 300), (H, F), 1), ((5,) * 200 + (900000,), (F,), 0)]
 
 
 @pytest.mark.parametrize("sizes,types,gap", LISTS)
@@ -227,6 +228,26 @@ def test_adamw_clip_matches_adamw_multi_without_clipping():
     # adamw_multi forms 1 - beta2 and the bias corrections in fp32: 1e-5 relative
     for x, y in zip(a[0] + a[1] + a[2], b[0] + b[1] + b[2]):
         np.testing.assert_allclose(host(x), host(y), rtol=1e-4, atol=1e-6)
+
+
+def test_workspace_serves_lists_of_any_size_in_turn():
+    """One workspace, large enough for the longest list, used by lists that take
+    different launches, in turn and twice over; its counters are left at zero."""
+    from paper_2607_14672_gb300 import dstd
+    lists = [tensors(s, (F,), 11 + i) for i, s in enumerate([(40,), (1000, 64), (20000000,), tuple([64] * 600)])]
+    ws = torch.zeros(max(dstd.grad_norm_workspace_bytes(l) for l in lists), dtype=torch.uint8, device="cuda")
+    norm = torch.empty(1, device="cuda")
+    for _ in range(2):
+        for l in lists:
+            outs = [torch.empty_like(x) for x in l]
+            dstd.clip_grads(l, 1.0, norm, ws, outs)
+            want, _ = norms(l)
+            assert norm.item() == pytest.approx(want, rel=NORM)
+            got, _ = norms(outs)
+            assert got == pytest.approx(1.0, rel=FACTOR + U)
+            dstd.grad_norm(l, norm, ws)
+            assert norm.item() == pytest.approx(want, rel=NORM)
+            assert not ws[:64].any()
 
 
 def test_lists_that_do_not_match_are_refused():

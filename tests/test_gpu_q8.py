@@ -251,6 +251,31 @@ def test_int8_matmul_streams_and_graph():
             assert torch.equal(out, expected(x, sx, w, sw, torch.float32))
 
 
+@pytest.mark.parametrize("T,N,K", [(3, 3000, 4096), (70, 3000, 4096), (300, 2000, 1500)])
+def test_codes_written_just_before_the_product(T, N, K):
+    """Weights and tokens quantised right before the product on the same stream,
+    again and again: what the quantiser writes is what the product reads."""
+    from paper_2607_14672_gb300 import dstd
+    g = torch.Generator(device="cuda").manual_seed(T)
+    w = [torch.randn(N, K, generator=g, device="cuda") for _ in range(2)]
+    x = [torch.randn(T, K, generator=g, device="cuda") for _ in range(2)]
+    wq, xq = torch.empty(N, K, dtype=torch.int8, device="cuda"), torch.empty(T, K, dtype=torch.int8, device="cuda")
+    ws, xs = torch.empty(N, device="cuda"), torch.empty(T, device="cuda")
+    scratch = torch.empty(dstd.int8_matmul_workspace_bytes(T, N, K), dtype=torch.uint8, device="cuda")
+    outs = [torch.empty(T, N, device="cuda") for _ in range(12)]
+    for i, o in enumerate(outs):
+        dstd.quantize_rows(x[i % 2], xq, xs)
+        dstd.quantize_rows(w[i % 2], wq, ws)
+        dstd.int8_matmul(xq, xs, wq, ws, o, scratch)
+    torch.cuda.synchronize()
+    for k in range(2):
+        dstd.quantize_rows(x[k], xq, xs)
+        dstd.quantize_rows(w[k], wq, ws)
+        torch.cuda.synchronize()
+        want = expected(xq, xs, wq, ws, torch.float32)
+        assert all(torch.equal(o, want) for o in outs[k::2])
+
+
 # ---------------------------------------------------------------------------
 # layer
 # ---------------------------------------------------------------------------
