@@ -1751,7 +1751,7 @@ int dstd_int8_matmul(const int8_t *x, int64_t ld_x, const float *x_scale, const 
     }
     TRY(device_ok());
     Timed tm(KK_INT8, (cudaStream_t)stream);
-    const Q8Args a{x, w, ld_x, ld_w, x_scale, w_scale, T, N, K, Q8Out{out, out_type, ld_out, 1}};
+    const Q8Args a{x, w, ld_x, ld_w, x_scale, w_scale, T, N, K, Q8Out{out, out_type, ld_out, 1}, false};
     return cu(launch_q8_product(a, workspace, (cudaStream_t)stream));
 }
 
@@ -1787,7 +1787,7 @@ int dstd_dense_fwd_q8(const float *t_in, const int8_t *w_q, const float *w_scale
     }
     {
         Timed tm(KK_INT8, st);
-        const Q8Args a{ws.q, w_q, ws.ld_q, N_in, ws.scale, w_scale, T, N_out, N_in, Q8Out{ws.D, DSTD_TYPE_F32, 1, T}};
+        const Q8Args a{ws.q, w_q, ws.ld_q, N_in, ws.scale, w_scale, T, N_out, N_in, Q8Out{ws.D, DSTD_TYPE_F32, 1, T}, false};
         TRY(cu(launch_q8_product(a, ws.product, st)));
     }
     Timed tm(KK_SCAN, st);

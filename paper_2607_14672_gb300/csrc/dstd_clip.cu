@@ -471,7 +471,8 @@ __global__ void __launch_bounds__(THREADS, 2) k_clip_once(const ClipArgs<CAP> a)
 
 constexpr int kBlocks = 152 * 6;
 constexpr int kOnceBlocks = 152 * 4;                    // at most, of the one-launch form
-constexpr long long kOnceElements = 1ll << 24;          // longer lists take two launches
+// longer lists take two launches: of a step, and of a clipping (whose second pass is too short to gain by it)
+constexpr long long kOnceStep = 1ll << 24, kOnceClip = 1ll << 19;
 
 // elements of a chunk: about one chunk per resident block. For the norm in
 // multiples of 4096 (four 16-byte loads of fp32 a thread): small lists take
@@ -599,8 +600,9 @@ cudaError_t launch_clip(const ClipTensors &t, ClipOp op, const ClipHyper &h, flo
     long long total = 0;
     for (int i = 0; i < t.count; ++i) total += t.n[i];
     // one launch against two, cold caches, without what any launch costs (us): a step of 100 thousand weights 6.5
-    // and 8.5, 1.3 M 12.6 and 14.6, 4.7 M 26.9 and 29.0, 16 M 82 and 83, 67 M 343 and 333
-    if (op != ClipOp::Norm && t.count <= kClipMaxTensors && total <= kOnceElements) {
+    // and 8.5, 1.3 M 12.6 and 14.6, 4.7 M 26.9 and 29.0, 16 M 82 and 83, 67 M 343 and 333; clipping 100 thousand
+    // gradients 4.4 and 5.4, 1.3 M 8.5 and 7.5
+    if (op != ClipOp::Norm && t.count <= kClipMaxTensors && total <= (op == ClipOp::Adamw ? kOnceStep : kOnceClip)) {
         auto once = [&](auto &a) {
             fill(a, op);
             return op == ClipOp::Scale ? launch_once<std::extent_v<decltype(a.seg)>, false>(t, total, a, st)

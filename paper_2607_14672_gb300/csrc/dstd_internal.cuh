@@ -741,6 +741,7 @@ struct Q8Args {
     const float *x_scale, *w_scale;
     int T, N, K;
     Q8Out out;
+    bool swapped;  // x holds the channels' rows and w the tokens': w_scale is multiplied first
 };
 constexpr int kQ8MaxK = 131071;  // (2^31 - 1) / 128^2: no 32-bit sum of products overflows
 size_t q8_workspace_bytes(int T, int N, int K);

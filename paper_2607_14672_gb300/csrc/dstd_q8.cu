@@ -90,39 +90,50 @@ struct QuantArgs {
 };
 
 // One pass: THREADS threads (a warp, or a whole block) hold their row in
-// registers, E elements each, find the largest |x|, and write. 16 bytes at a
-// time where every row's start allows it (VEC), else one element (loads and
-// stores of neighbouring threads are still neighbours).
-template <class T, bool VEC, int E, int THREADS, int BLOCK = THREADS == 32 ? 256 : THREADS>
-__global__ void __launch_bounds__(BLOCK) k_quantize_rows(const T *__restrict__ x, const QuantArgs a) {
-    constexpr int P = VEC ? Pack<T>::P : 1, L = E / P;
+// registers, find the largest |x|, and write. PACKED: 16 bytes of x at a time,
+// from the first aligned one of the row; up to P - 1 elements at each end are
+// taken singly. That needs the row's codes (and values) aligned at the same
+// element, as they are when x and q are both contiguous. Otherwise one element
+// at a time (loads and stores of neighbouring threads are still neighbours).
+// A thread has up to 4 or 8 of these loads under way, and a block's threads are
+// few enough for several rows to be on an SM (4153 rows of 4480 16-bit elements:
+// 13 us; with 512 threads a row and one load each 21 us). HBM bounds it: 16384 x
+// 16384 fp32 with values in 341 us, 7.1 TB/s.
+template <class T, bool PACKED, int L, int THREADS, int BLOCK = THREADS == 32 ? 256 : THREADS>
+__global__ void __launch_bounds__(BLOCK, THREADS == 32 ? 1 : (BLOCK == 1024 ? 2 : (L == 8 ? 1024 : 1536) / BLOCK)) k_quantize_rows(const T *__restrict__ x, const QuantArgs a) {
+    constexpr int P = PACKED ? Pack<T>::P : 1;
     __shared__ unsigned s_top[32];
     let_next_launch();
     const int t = threadIdx.x % THREADS;
     const long long r = (long long)blockIdx.x * (BLOCK / THREADS) + threadIdx.x / THREADS;
     if (r >= a.rows) return;  // a whole warp, or never
     const T *row = x + r * a.ld_x;
-    uint4 raw[VEC ? L : 1];
-    float one[VEC ? 1 : L];
-    auto value = [&](int j, int i) { return VEC ? Pack<T>::one(raw[VEC ? j : 0], i) : one[VEC ? 0 : j]; };
+    int8_t *q = a.q + r * a.ld_q;
+    float *val = a.values ? a.values + r * a.ld_v : nullptr;
+    // packs cover [head, head + packs P); `edge` are this thread's elements before and after them
+    const int head = PACKED ? min(a.cols, (int)((0 - reinterpret_cast<uintptr_t>(row) / sizeof(T)) & (P - 1))) : 0;
+    const int packs = (a.cols - head) / P, done = head + packs * P;
+    const int edge[2] = {t < head ? t : -1, PACKED && done + t < a.cols ? done + t : -1};
+    uint4 raw[PACKED ? L : 1];
+    float one[PACKED ? 2 : L];
+    auto value = [&](int j, int i) { return PACKED ? Pack<T>::one(raw[PACKED ? j : 0], i) : one[PACKED ? 0 : j]; };
 #pragma unroll
     for (int j = 0; j < L; ++j) {
-        const int k = (j * THREADS + t) * P;
-        if constexpr (VEC) {
-            raw[j] = make_uint4(0, 0, 0, 0);
-            if (k + P <= a.cols) {
-                raw[j] = *reinterpret_cast<const uint4 *>(row + k);
-            } else if (k < a.cols) {
-                T part[P];
-#pragma unroll
-                for (int i = 0; i < P; ++i) part[i] = k + i < a.cols ? row[k + i] : T(0.f);
-                raw[j] = *reinterpret_cast<const uint4 *>(part);
-            }
+        const int k = j * THREADS + t;
+        if constexpr (PACKED) {
+            raw[j] = k < packs ? *reinterpret_cast<const uint4 *>(row + head + k * P) : make_uint4(0, 0, 0, 0);
         } else {
             one[j] = k < a.cols ? to_f32<T>(row[k]) : 0.f;
         }
     }
     unsigned top = 0;
+    if constexpr (PACKED) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            one[e] = edge[e] >= 0 ? to_f32<T>(row[edge[e]]) : 0.f;
+            top = max(top, __float_as_uint(one[e]) & 0x7fffffffu);
+        }
+    }
 #pragma unroll
     for (int j = 0; j < L; ++j)
 #pragma unroll
@@ -136,39 +147,41 @@ __global__ void __launch_bounds__(BLOCK) k_quantize_rows(const T *__restrict__ x
     }
     const RowCode c = row_code(top);
     if (t == 0) a.scale[r] = c.scale;
-    int8_t *q = a.q + r * a.ld_q;
-    float *val = a.values ? a.values + r * a.ld_v : nullptr;
+    auto put = [&](int k, float v) {
+        const int n = code_of(v, c);
+        q[k] = (int8_t)n;
+        if (val) val[k] = n * c.scale;
+    };
+    if constexpr (PACKED) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (edge[e] >= 0) put(edge[e], one[e]);
+    }
 #pragma unroll
     for (int j = 0; j < L; ++j) {
-        const int k = (j * THREADS + t) * P;
-        if (k >= a.cols) break;
-        int n[P];
+        const int k = j * THREADS + t;
+        if constexpr (PACKED) {
+            if (k >= packs) break;
+            int n[P];
 #pragma unroll
-        for (int i = 0; i < P; ++i) n[i] = code_of(value(j, i), c);
-        if constexpr (VEC) {
-            if (k + P <= a.cols) {
-                uint32_t w[P / 4];
+            for (int i = 0; i < P; ++i) n[i] = code_of(value(j, i), c);
+            uint32_t w[P / 4];
 #pragma unroll
-                for (int i = 0; i < P / 4; ++i)
-                    w[i] = (uint32_t)(n[4 * i] & 255) | (uint32_t)(n[4 * i + 1] & 255) << 8 |
-                           (uint32_t)(n[4 * i + 2] & 255) << 16 | (uint32_t)n[4 * i + 3] << 24;
-                if constexpr (P == 4) *reinterpret_cast<uint32_t *>(q + k) = w[0];
-                else *reinterpret_cast<uint2 *>(q + k) = make_uint2(w[0], w[1]);
-                if (val) {
+            for (int i = 0; i < P / 4; ++i)
+                w[i] = (uint32_t)(n[4 * i] & 255) | (uint32_t)(n[4 * i + 1] & 255) << 8 |
+                       (uint32_t)(n[4 * i + 2] & 255) << 16 | (uint32_t)n[4 * i + 3] << 24;
+            if constexpr (P == 4) *reinterpret_cast<uint32_t *>(q + head + k * P) = w[0];
+            else *reinterpret_cast<uint2 *>(q + head + k * P) = make_uint2(w[0], w[1]);
+            if (val) {
 #pragma unroll
-                    for (int i = 0; i < P; i += 4)
-                        *reinterpret_cast<float4 *>(val + k + i) = make_float4(
-                            n[i] * c.scale, n[i + 1] * c.scale, n[i + 2] * c.scale, n[i + 3] * c.scale);
-                }
-                continue;
+                for (int i = 0; i < P; i += 4)
+                    *reinterpret_cast<float4 *>(val + head + k * P + i) =
+                        make_float4(n[i] * c.scale, n[i + 1] * c.scale, n[i + 2] * c.scale, n[i + 3] * c.scale);
             }
+        } else {
+            if (k >= a.cols) break;
+            put(k, one[j]);
         }
-#pragma unroll
-        for (int i = 0; i < P; ++i)
-            if (k + i < a.cols) {
-                q[k + i] = (int8_t)n[i];
-                if (val) val[k + i] = n[i] * c.scale;
-            }
     }
 }
 
@@ -200,26 +213,28 @@ __global__ void __launch_bounds__(256) k_quantize_long(const T *__restrict__ x, 
 template <class T>
 void quantize(const T *x, const QuantArgs &a, cudaStream_t st) {
     constexpr int P = Pack<T>::P;
-    const bool vec = ((reinterpret_cast<uintptr_t>(x) & 15) | (a.ld_x & (P - 1))) == 0 &&
-                     ((reinterpret_cast<uintptr_t>(a.q) | a.ld_q) & (P - 1)) == 0 &&
-                     (!a.values || ((reinterpret_cast<uintptr_t>(a.values) & 15) | (a.ld_v & 3)) == 0);
-    const unsigned rows = (unsigned)a.rows, warps = (rows + 7) / 8;
-    if (a.cols <= 256) {
-        if (vec) k_quantize_rows<T, true, 8, 32><<<warps, 256, 0, st>>>(x, a);
-        else k_quantize_rows<T, false, 8, 32><<<warps, 256, 0, st>>>(x, a);
-    } else if (a.cols <= 1024) {
-        if (vec) k_quantize_rows<T, true, 32, 32><<<warps, 256, 0, st>>>(x, a);
-        else k_quantize_rows<T, false, 32, 32><<<warps, 256, 0, st>>>(x, a);
-    } else if (a.cols <= 4096) {
-        if (vec) k_quantize_rows<T, true, 16, 256><<<rows, 256, 0, st>>>(x, a);
-        else k_quantize_rows<T, false, 16, 256><<<rows, 256, 0, st>>>(x, a);
-    } else if (a.cols <= 16384) {
-        // as many elements a thread as leave 2048 threads on an SM
-        constexpr int E = sizeof(T) == 4 ? 16 : 32;
-        if (vec) k_quantize_rows<T, true, E, 16384 / E><<<rows, 16384 / E, 0, st>>>(x, a);
-        else k_quantize_rows<T, false, 16, 1024><<<rows, 1024, 0, st>>>(x, a);
+    // element of the first aligned 16 bytes, codes and values, in every row the same for all three
+    const auto phase = [](const void *p, size_t bytes) { return (long long)(reinterpret_cast<uintptr_t>(p) / bytes); };
+    const bool packed = ((phase(x, sizeof(T)) - phase(a.q, 1)) & (P - 1)) == 0 && ((a.ld_x - a.ld_q) & (P - 1)) == 0 &&
+                        (!a.values || (((phase(x, sizeof(T)) - phase(a.values, 4)) & 3) == 0 &&
+                                       ((a.ld_x - a.ld_v) & 3) == 0));
+    const int cols = a.cols;
+    if (cols > 16384) {
+        k_quantize_long<T><<<(unsigned)a.rows, 256, 0, st>>>(x, a);
+    } else if (!packed) {
+        if (cols <= 256) k_quantize_rows<T, false, 8, 32><<<((unsigned)a.rows + 7) / 8, 256, 0, st>>>(x, a);
+        else if (cols <= 1024) k_quantize_rows<T, false, 32, 32><<<((unsigned)a.rows + 7) / 8, 256, 0, st>>>(x, a);
+        else if (cols <= 4096) k_quantize_rows<T, false, 16, 256><<<(unsigned)a.rows, 256, 0, st>>>(x, a);
+        else if (cols <= 8192) k_quantize_rows<T, false, 16, 512><<<(unsigned)a.rows, 512, 0, st>>>(x, a);
+        else k_quantize_rows<T, false, 16, 1024><<<(unsigned)a.rows, 1024, 0, st>>>(x, a);
     } else {
-        k_quantize_long<T><<<rows, 256, 0, st>>>(x, a);
+        const int bytes = cols * (int)sizeof(T);
+        if (bytes <= 1024) k_quantize_rows<T, true, 2, 32><<<((unsigned)a.rows + 7) / 8, 256, 0, st>>>(x, a);
+        else if (bytes <= 4096) k_quantize_rows<T, true, 8, 32><<<((unsigned)a.rows + 7) / 8, 256, 0, st>>>(x, a);
+        else if (bytes <= 8192) k_quantize_rows<T, true, 4, 128><<<(unsigned)a.rows, 128, 0, st>>>(x, a);
+        else if (bytes <= 16384) k_quantize_rows<T, true, 4, 256><<<(unsigned)a.rows, 256, 0, st>>>(x, a);
+        else if (bytes <= 32768) k_quantize_rows<T, true, 8, 256><<<(unsigned)a.rows, 256, 0, st>>>(x, a);
+        else k_quantize_rows<T, true, 8, 512><<<(unsigned)a.rows, 512, 0, st>>>(x, a);
     }
 }
 
@@ -516,7 +531,9 @@ __global__ void __launch_bounds__(256, few_resident<NT>() / 8) k_q8_few(const Q8
         for (int i = 0; i < 4; ++i) {
             const int t = t0 + 8 * j + 2 * q + (i & 1);
             const long long n = n0 + g + (i >> 1) * 8;
-            if (t < a.T && n < a.N) store_out(a.out, t, n, ((float)sum[j][i] * a.x_scale[t]) * a.w_scale[n]);
+            if (t >= a.T || n >= a.N) continue;
+            const float first = a.swapped ? a.w_scale[n] : a.x_scale[t], second = a.swapped ? a.x_scale[t] : a.w_scale[n];
+            store_out(a.out, t, n, ((float)sum[j][i] * first) * second);
         }
 }
 
@@ -607,7 +624,7 @@ struct Q8Plan {
 
 struct Q8Tc {
     int T, N, K;
-    bool w_copied;
+    bool w_copied, swapped;
     Q8Plan p;
     const float *x_scale, *w_scale;
     Q8Out out;
@@ -672,39 +689,49 @@ __device__ __forceinline__ __nv_bfloat16 round_out<__nv_bfloat16>(float y) { ret
 template <>
 __device__ __forceinline__ __half round_out<__half>(float y) { return __float2half_rn(y); }
 
-// column c of this lane's channel: the token's scale is held by lane c % 32
+// column c of this lane's channel: the token's scale is held by lane c % 32, and
+// multiplied first (the lane's own, where the lanes hold tokens)
 template <int COLS>
-__device__ __forceinline__ float scaled(const int (&sum)[COLS], const float (&xs)[(COLS + 31) / 32], float ws, int c) {
-    return ((float)sum[c] * __shfl_sync(0xffffffffu, xs[c / 32], c % 32)) * ws;
+__device__ __forceinline__ float scaled(const int (&sum)[COLS], const float (&xs)[(COLS + 31) / 32], float ws,
+                                        bool swapped, int c) {
+    const float x = __shfl_sync(0xffffffffu, xs[c / 32], c % 32);
+    return ((float)sum[c] * (swapped ? ws : x)) * (swapped ? x : ws);
 }
 // a warp's lanes hold neighbouring channels: each column is one row segment
 template <class O, int COLS>
 __device__ __forceinline__ void store_columns(O *dst, long long ld, const int (&sum)[COLS],
-                                              const float (&xs)[(COLS + 31) / 32], float ws, int left) {
+                                              const float (&xs)[(COLS + 31) / 32], float ws, bool swapped, int left) {
 #pragma unroll
     for (int c = 0; c < COLS; ++c, dst += ld) {
-        const float y = scaled<COLS>(sum, xs, ws, c);
+        const float y = scaled<COLS>(sum, xs, ws, swapped, c);
         if (c < left) *dst = round_out<O>(y);
     }
 }
-// the columns lie next to each other
-template <int COLS>
-__device__ __forceinline__ void store_row(float *dst, const int (&sum)[COLS], const float (&xs)[(COLS + 31) / 32],
-                                          float ws, int left) {
+// the columns lie next to each other: 16 bytes at a time where the row allows it
+template <class O, int COLS>
+__device__ __forceinline__ void store_row(O *dst, const int (&sum)[COLS], const float (&xs)[(COLS + 31) / 32],
+                                          float ws, bool swapped, int left) {
+    constexpr int P = 16 / sizeof(O);
     const bool vec = (reinterpret_cast<uintptr_t>(dst) & 15) == 0;
 #pragma unroll
-    for (int c = 0; c < COLS; c += 4) {
-        float y[4];
+    for (int c = 0; c < COLS; c += P) {
+        alignas(16) O y[P];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) y[u] = scaled<COLS>(sum, xs, ws, c + u);
-        if (vec && c + 4 <= left) {
-            *reinterpret_cast<float4 *>(dst + c) = make_float4(y[0], y[1], y[2], y[3]);
+        for (int u = 0; u < P; ++u) y[u] = round_out<O>(scaled<COLS>(sum, xs, ws, swapped, c + u));
+        if (vec && c + P <= left) {
+            *reinterpret_cast<uint4 *>(dst + c) = *reinterpret_cast<const uint4 *>(y);
         } else {
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+            for (int u = 0; u < P; ++u)
                 if (c + u < left) dst[c + u] = y[u];
         }
     }
+}
+template <class O, int COLS>
+__device__ __forceinline__ void store_tile(const Q8Out &o, long long at, const int (&sum)[COLS],
+                                           const float (&xs)[(COLS + 31) / 32], float ws, bool swapped, int left) {
+    if (o.ld_t == 1) store_row<O, COLS>((O *)o.p + at, sum, xs, ws, swapped, left);
+    else store_columns<O, COLS>((O *)o.p + at, o.ld_t, sum, xs, ws, swapped, left);
 }
 
 template <int NT>
@@ -925,15 +952,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1)
             }
             const int left = n < a.N ? a.T - t0 : 0;  // this lane's columns that exist
             const long long at = (long long)t0 * a.out.ld_t + (long long)n * a.out.ld_n;
-            if (a.out.ld_t == 1 && a.out.type == DSTD_TYPE_F32) {
-                store_row<C::COLS>((float *)a.out.p + at, sum, xs, ws, left);
-            } else if (a.out.type == DSTD_TYPE_F32) {
-                store_columns<float, C::COLS>((float *)a.out.p + at, a.out.ld_t, sum, xs, ws, left);
-            } else if (a.out.type == DSTD_TYPE_BF16) {
-                store_columns<__nv_bfloat16, C::COLS>((__nv_bfloat16 *)a.out.p + at, a.out.ld_t, sum, xs, ws, left);
-            } else {
-                store_columns<__half, C::COLS>((__half *)a.out.p + at, a.out.ld_t, sum, xs, ws, left);
-            }
+            if (a.out.type == DSTD_TYPE_F32) store_tile<float, C::COLS>(a.out, at, sum, xs, ws, a.swapped, left);
+            else if (a.out.type == DSTD_TYPE_BF16)
+                store_tile<__nv_bfloat16, C::COLS>(a.out, at, sum, xs, ws, a.swapped, left);
+            else store_tile<__half, C::COLS>(a.out, at, sum, xs, ws, a.swapped, left);
             __syncwarp();
         }
     }
@@ -1160,62 +1182,106 @@ cudaError_t launch_tc(const Q8Args &q, const Q8Plan &p, const Q8Scratch &s, int 
     cudaLaunchConfig_t cfg = tc_config<NT>(attr);
     cfg.stream = st;
     cfg.gridDim = dim3(2 * (unsigned)(p.share ? pairs : std::min(p.whole, pairs)));
-    const Q8Tc a{q.T, q.N, q.K, copied, p, q.x_scale, q.w_scale, q.out, s.partial, s.ticket};
+    const Q8Tc a{q.T, q.N, q.K, copied, q.swapped, p, q.x_scale, q.w_scale, q.out, s.partial, s.ticket};
     return cudaLaunchKernelEx(&cfg, k_q8_tc<NT>, map_w, map_x, a);
 }
 
-// Which form, by two estimates in microseconds (both without what any launch
-// costs), fitted to times with cold caches. mma.sync: rounds of resident blocks,
-// each warp passing `steps` blocks of 128 codes of K. The big form: its plan, 4 us
-// for the preparation and the pipeline's ends, and the copy of weights whose rows
-// are not aligned. Measured with the other form beside it (us): 32 x 784 x 800
-// 10.8 and 12.9, 16 x 4096 x 4096 12.9 and 18.0, 64 x 4096 x 4096 23.1 and 19.1,
-// 32 x 16384 x 16384 103 and 56, 256 x 3000 x 1000 (not aligned) 31 and 17.
-// Up to 8 tokens mma.sync reads the weights as fast as memory gives them.
-bool use_tc(const Q8Args &a, bool aligned, const Q8Plan &p) {
-    if (a.T < kTcMinTokens || a.K < 16) return false;
-    const bool two = a.T <= 16;
-    const FewPlan f = two ? few_plan<2>(a.T, a.N, a.K) : few_plan<4>(a.T, a.N, a.K);
+// Estimates in microseconds, without what any launch costs, fitted to times with
+// cold caches. mma.sync: rounds of resident blocks, each warp passing `steps`
+// blocks of 128 codes of K, or the weights' reading time. The big form: its plan,
+// 4 us for the pipeline's ends, the preparation's traffic (the tokens to 16 bits, a
+// copy of weights whose rows are not aligned) and, where a lane's row goes out
+// piece by piece, the stores. Measured with the other form beside it (us, with
+// 6.5 of launch and events): 32 x 784 x 800 10.8 and 12.9, 16 x 4096 x 4096 12.9
+// and 18.0, 64 x 4096 x 4096 23.1 and 19.1, 32 x 16384 x 16384 103 and 56,
+// 256 x 3000 x 1000 (not aligned) 31 and 17.
+double few_time(const Q8Args &a) {
+    const int nt = a.T <= 8 ? 1 : (a.T <= 16 ? 2 : 4);
+    const FewPlan f = nt == 1 ? few_plan<1>(a.T, a.N, a.K) : (nt == 2 ? few_plan<2>(a.T, a.N, a.K) : few_plan<4>(a.T, a.N, a.K));
+    const bool aligned = rows_aligned(a.x, a.ld_x) && rows_aligned(a.w, a.ld_w);
     const double steps = (double)((f.blocks + f.wpk - 1) / f.wpk) * f.rounds;
-    const double few = 3.5 + steps * (two ? 1.1 : 1.5) * (aligned ? 1.0 : 1.5) + (aligned ? 0.0 : 4.0);
-    const double tc = 4.0 + p.cycles / 1900.0 + (w_rows_aligned(a) ? 0.0 : 2.0 * a.N * (double)a.K / 6.5e6);
-    return tc < few;
+    const double each = (nt == 1 ? 1.0 : (nt == 2 ? 1.1 : 1.5)) * (aligned ? 1.0 : 1.5);
+    return 3.5 + std::max(steps * each, (double)a.N * a.K / 6.2e6) + (aligned ? 0.0 : 4.0);
+}
+double tc_time(const Q8Args &a, const Q8Plan &p) {
+    const double prep = (3.0 * a.T + (w_rows_aligned(a) ? 0.0 : 2.0 * a.N)) * a.K / 6.0e6;
+    const bool pieces = a.out.ld_t == 1, wide = pieces && a.out.ld_n % 8 == 0;
+    const double stores = pieces ? (double)a.T * a.N / (152.0 * (wide ? 4 : 1)) : 0.0;
+    return 4.0 + prep + (p.cycles + stores) / 1900.0;
+}
+// the same product with the sides exchanged
+Q8Args exchanged(const Q8Args &a) {
+    return Q8Args{a.w, a.x, a.ld_w, a.ld_x, a.w_scale, a.x_scale, a.N, a.T, a.K,
+                  Q8Out{a.out.p, a.out.type, a.out.ld_n, a.out.ld_t}, !a.swapped};
+}
+
+cudaError_t run_few(const Q8Args &a, cudaStream_t st) {
+    const bool aligned = rows_aligned(a.x, a.ld_x) && rows_aligned(a.w, a.ld_w);
+    if (a.T <= 8) return launch_few<1>(a, aligned, st);
+    if (a.T <= 16) return launch_few<2>(a, aligned, st);
+    return launch_few<4>(a, aligned, st);
+}
+
+cudaError_t run_tc(const Q8Args &a, const Q8Plan &p, int pairs, void *workspace, cudaStream_t st) {
+    const Q8Scratch s = q8_scratch(workspace, a.T, a.N, a.K, (long long)p.tiles_n * p.tiles_t - p.whole, p.nt);
+    PrepArgs pa{a.x, a.w, a.ld_x, a.ld_w, a.T, a.N, a.K, rows_aligned(a.x, a.ld_x), s.x, s.ld, s.w, s.ld_w,
+                (uint4 *)s.ticket, (long long)a.T * ((s.ld + 15) / 16),
+                w_rows_aligned(a) ? 0 : (long long)a.N * (s.ld_w / 16), s.zeros};
+    const long long blocks = (pa.x_threads + pa.w_threads + pa.zeros + 255) / 256;
+    if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
+    cudaError_t e = launch_dependent(k_q8_prep, (unsigned)blocks, 256, st, pa);
+    if (e != cudaSuccess) return e;
+    switch (p.nt) {
+        case 32: return launch_tc<32>(a, p, s, pairs, st);
+        case 64: return launch_tc<64>(a, p, s, pairs, st);
+        case 96: return launch_tc<96>(a, p, s, pairs, st);
+        case 128: return launch_tc<128>(a, p, s, pairs, st);
+        case 160: return launch_tc<160>(a, p, s, pairs, st);
+        default: return launch_tc<192>(a, p, s, pairs, st);
+    }
 }
 
 }  // namespace
 
+// Exchanging the sides takes no more scratch than this: it is done only where
+// there are more tokens than channels.
 size_t q8_workspace_bytes(int T, int N, int K) {
     if (T < kTcMinTokens || N < 1 || K < 1) return 256;
     const long long cut = std::min<long long>((long long)((N + 255) / 256) * ((T + 31) / 32), kPairs);
-    return q8_scratch(nullptr, T, N, K, cut, 192).bytes;
+    const long long cut_exchanged = std::min<long long>((long long)((T + 255) / 256) * ((N + 31) / 32), kPairs);
+    const size_t bytes = q8_scratch(nullptr, T, N, K, cut, 192).bytes;
+    return T > N ? std::max(bytes, q8_scratch(nullptr, N, T, K, cut_exchanged, 192).bytes) : bytes;
 }
 
+// The big form computes 256 rows of one side by up to 192 of the other at a
+// time, and reads the first in 8 bits; mma.sync streams one side past up to 32
+// rows of the other. So which side is which is chosen with the form: with more
+// tokens than channels they are exchanged where that is estimated to be faster
+// (7561 tokens, 4181 inputs, 21 channels: 25 us instead of 42).
 cudaError_t launch_q8_product(const Q8Args &a, void *workspace, cudaStream_t st) {
     if (a.T == 0 || a.N == 0) return cudaSuccess;
-    const bool x_aligned = rows_aligned(a.x, a.ld_x), w_aligned = w_rows_aligned(a);
     const int pairs = resident_pairs();
     if (pairs < 1) return cudaErrorInvalidConfiguration;
-    const Q8Plan p = a.T < kTcMinTokens ? Q8Plan{} : q8_plan(a.T, a.N, a.K, pairs);
-    if (use_tc(a, x_aligned && w_aligned, p)) {
-        const Q8Scratch s = q8_scratch(workspace, a.T, a.N, a.K, (long long)p.tiles_n * p.tiles_t - p.whole, p.nt);
-        PrepArgs pa{a.x, a.w, a.ld_x, a.ld_w, a.T, a.N, a.K, x_aligned, s.x, s.ld, s.w, s.ld_w, (uint4 *)s.ticket,
-                    (long long)a.T * ((s.ld + 15) / 16), w_aligned ? 0 : (long long)a.N * (s.ld_w / 16), s.zeros};
-        const long long blocks = (pa.x_threads + pa.w_threads + pa.zeros + 255) / 256;
-        if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-        cudaError_t e = launch_dependent(k_q8_prep, (unsigned)blocks, 256, st, pa);
-        if (e != cudaSuccess) return e;
-        switch (p.nt) {
-            case 32: return launch_tc<32>(a, p, s, pairs, st);
-            case 64: return launch_tc<64>(a, p, s, pairs, st);
-            case 96: return launch_tc<96>(a, p, s, pairs, st);
-            case 128: return launch_tc<128>(a, p, s, pairs, st);
-            case 160: return launch_tc<160>(a, p, s, pairs, st);
-            default: return launch_tc<192>(a, p, s, pairs, st);
+    const Q8Args b = exchanged(a);
+    const bool may_exchange = a.T > a.N, may_tc = a.T >= kTcMinTokens && a.K >= 16;
+    double best = few_time(a);
+    int form = 0;  // 1: exchanged, 2: big
+    Q8Plan plan{};
+    if (may_exchange && few_time(b) < best) {
+        best = few_time(b);
+        form = 1;
+    }
+    for (int i = 0; may_tc && i < (may_exchange ? 2 : 1); ++i) {
+        const Q8Args &c = i ? b : a;
+        const Q8Plan p = q8_plan(c.T, c.N, c.K, pairs);
+        if (tc_time(c, p) < best) {
+            best = tc_time(c, p);
+            form = 2 + i;
+            plan = p;
         }
     }
-    if (a.T <= 8) return launch_few<1>(a, x_aligned && w_aligned, st);
-    if (a.T <= 16) return launch_few<2>(a, x_aligned && w_aligned, st);
-    return launch_few<4>(a, x_aligned && w_aligned, st);
+    const Q8Args &c = form & 1 ? b : a;
+    return form & 2 ? run_tc(c, plan, pairs, workspace, st) : run_few(c, st);
 }
 
 }  // namespace dstd

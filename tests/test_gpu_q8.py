@@ -137,7 +137,8 @@ SHAPES = [(1, 1, 1, 0), (1, 5, 16, 0), (2, 3, 15, 0), (3, 130, 17, 0), (1, 4096,
           (17, 300, 1040, 0), (31, 801, 1023, 9), (32, 256, 2064, 0), (33, 512, 64, 0), (64, 1000, 1100, 4),
           (65, 10, 784, 0), (100, 300, 5000, 0), (128, 128, 128, 16), (129, 1025, 48, 0), (192, 256, 1200, 0),
           (200, 513, 2050, 0), (256, 800, 784, 0), (385, 700, 3000, 3), (1000, 1000, 1000, 0), (1500, 260, 16, 0),
-          (2500, 40, 333, 0), (3000, 3100, 96, 0)]
+          (2500, 40, 333, 0), (3000, 3100, 96, 0), (7000, 20, 1000, 0), (5000, 8, 300, 0), (9000, 1, 4100, 0),
+          (3000, 100, 2000, 0), (2000, 33, 64, 5), (9000, 150, 500, 7), (4000, 129, 1040, 0), (20000, 64, 2048, 0)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
