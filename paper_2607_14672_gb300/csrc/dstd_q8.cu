@@ -11,7 +11,8 @@ namespace dstd {
 // one before it in the stream still runs, from when all of that one's blocks
 // have called let_next_launch (or ended); what that one writes, and what was
 // there before it, is there after wait_launch_before. A grid that lets the next
-// one start has itself waited first, so nothing older is still running then.
+// one start was launched without this, or has itself waited first: nothing older
+// is still running then.
 __device__ __forceinline__ void wait_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void let_next_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
@@ -34,10 +35,11 @@ cudaError_t launch_dependent(void (*kernel)(P...), unsigned grid, unsigned block
 //     scale = a / 127,  q_k = rint(x_k (127 (1 / a))),  value_k = q_k scale,
 // each operation rounded to fp32 (three roundings move x 127 / a by less than
 // 127 * 3 * 2^-24 code steps). 1 / a overflows for a below 2^-128; rows of
-// very small a are multiplied by 2^64 first (exact), which gives the same codes. A row of zeros has scale 0; a row
-// that holds an infinity or a NaN has scale NaN and codes 0, so that whatever
-// is computed from it is NaN. The largest |x| is taken on the bit patterns:
-// without the sign they order like the values, with infinities and NaN on top.
+// very small a are multiplied by 2^64 first (exact), which gives the same codes.
+// A row of zeros has scale 0; a row that holds an infinity or a NaN has scale
+// NaN and codes 0, so that whatever is computed from it is NaN. The largest |x|
+// is taken on the bit patterns: without the sign they order like the values,
+// with infinities and NaN on top.
 // ---------------------------------------------------------------------------
 template <class T>
 __device__ __forceinline__ float to_f32(T x);
@@ -424,6 +426,9 @@ __device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t &lo, uint32_t
 // A block has 16 channels and 8 NT tokens; its warps (1 to 8) share K in blocks
 // of 128 codes (whole 128-byte lines): as many as fit the GPU in one round of
 // blocks, so that there are loads enough under way and no second, half-empty round.
+// Memory bounds it: 8 tokens x 16384 x 16384 in 48 us, 5.6 TB/s of weights (two
+// blocks' loads under way per warp took registers from other warps: 57 us). Small
+// layers are bound by the launch: 16 tokens x 784 x 800 in about 2.5 us.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ void mma_16x8x16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                             uint32_t b0, uint32_t b1) {
@@ -566,9 +571,13 @@ cudaError_t launch_few(const Q8Args &a, bool aligned, cudaStream_t st) {
 // cores give the whole-number sum as long as it stays within 2^24, which 1024
 // products of at most 2^14 do. Computed transposed, D[n, t]: the weights are
 // the M operand. They stay 8 bits wide until they are in the SM (TMA tiles of
-// 128 rows x 128 codes); four warps turn them into fp16 pairs in TMEM, from
-// where the tensor core reads them. The tokens, which every tile row shares,
-// are turned into fp16 once per call and read through TMA.
+// 128 rows x 128 codes): with both operands in 16 bits the widest tile would take
+// in 83 bytes a cycle and SM, where 16-bit tiles were measured to get about 57
+// from L2. Eight warps turn them into fp16 pairs in TMEM, from where the tensor
+// core reads them, two groups of four taking blocks in turn (one group's chain of
+// load, convert, store and signal was longer than the block's MMAs). The tokens,
+// which every tile row shares, are turned into fp16 once per call and read
+// through TMA.
 // A pair of SMs works on 256 channels x NT tokens: each holds 128 channels and
 // half of the tokens' operand. Two accumulators of NT columns alternate every
 // 1024 codes of K; eight epilogue warps take the full one into 32-bit integers
@@ -578,6 +587,11 @@ cudaError_t launch_few(const Q8Args &a, bool aligned, cudaStream_t st) {
 // is shorter than one more round: a pair adds its integer sums into the
 // workspace with atomics, and the last one of a part (a ticket counts them)
 // stores the result. Whole-number sums do not depend on the order.
+// The tensor pipe bounds large products: 4096 x 16384 x 16384 in 1.09 ms, 2.0
+// PFLOP/s (cuBLAS bf16 burst: 1.91); 4096^3 in 90 us (the pipe is active 82% of
+// the time at 4096 x 4096 x 8192; the rest are the pipeline's ends and the last
+// round). Small ones are bound by the pipeline's ends, about 8 us from launch to
+// the last store.
 // ---------------------------------------------------------------------------
 __device__ unsigned int g_status_q8 = 0;
 
@@ -598,7 +612,6 @@ constexpr int CONV_WARPS = 8, EPI_WARPS = 8, TC_THREADS = 32 * (CONV_WARPS + EPI
 // registers a thread of each role, where the kernel splits them (whole warpgroups)
 constexpr int REGS_CONV = 72, REGS_EPI = 136, REGS_REST = 48;
 constexpr int REGS_SUM = 32 * (CONV_WARPS * REGS_CONV + EPI_WARPS * REGS_EPI + 4 * REGS_REST);
-
 
 template <int NT>
 struct Q8Cfg {
@@ -1028,9 +1041,10 @@ constexpr int kPairs = 76;  // SM pairs of the GPU, for planning
 constexpr int kTcMinTokens = 9;
 
 // Time of one block of 128 codes in a pair's pipeline, in cycles, measured with
-// 4096 tokens, 16384 inputs and channels: the conversion and the issue of the
-// MMAs hold it at about 700 up to 128 tokens a tile, and with 192 only two
-// blocks fit beside the accumulators in TMEM.
+// 4096 tokens, 16384 inputs and channels (the MMAs alone: 4 nt). The conversion
+// and the issue of the MMAs hold it at about 700 up to 128 tokens a tile; 160
+// reach the tensor pipe's rate (1.22 ms); with 192 only two blocks fit beside the
+// accumulators in TMEM (1.30 ms).
 struct TileCost {
     int nt, block;
 };
