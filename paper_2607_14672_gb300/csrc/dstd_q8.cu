@@ -1203,9 +1203,9 @@ cudaError_t launch_tc(const Q8Args &q, const Q8Plan &p, const Q8Scratch &s, int 
 // Estimates in microseconds, without what any launch costs, fitted to times with
 // cold caches. mma.sync: rounds of resident blocks, each warp passing `steps`
 // blocks of 128 codes of K, or the weights' reading time. The big form: its plan,
-// 4 us for the pipeline's ends, the preparation's traffic (the tokens to 16 bits, a
-// copy of weights whose rows are not aligned) and, where a lane's row goes out
-// piece by piece, the stores. Measured with the other form beside it (us, with
+// 4 us for the pipeline's ends and 2 for its second launch, the preparation's
+// traffic (the tokens to 16 bits, a copy of weights whose rows are not aligned)
+// and, where a lane's row goes out piece by piece, the stores. Measured with the other form beside it (us, with
 // 6.5 of launch and events): 32 x 784 x 800 10.8 and 12.9, 16 x 4096 x 4096 12.9
 // and 18.0, 64 x 4096 x 4096 23.1 and 19.1, 32 x 16384 x 16384 103 and 56,
 // 256 x 3000 x 1000 (not aligned) 31 and 17.
@@ -1221,7 +1221,7 @@ double tc_time(const Q8Args &a, const Q8Plan &p) {
     const double prep = (3.0 * a.T + (w_rows_aligned(a) ? 0.0 : 2.0 * a.N)) * a.K / 6.0e6;
     const bool pieces = a.out.ld_t == 1, wide = pieces && a.out.ld_n % 8 == 0;
     const double stores = pieces ? (double)a.T * a.N / (152.0 * (wide ? 4 : 1)) : 0.0;
-    return 4.0 + prep + (p.cycles + stores) / 1900.0;
+    return 6.0 + prep + (p.cycles + stores) / 1900.0;
 }
 // the same product with the sides exchanged
 Q8Args exchanged(const Q8Args &a) {

@@ -335,6 +335,21 @@ def test_dense_fwd_q8(B, N_in, N_out, M):
     assert counts[1] == pytest.approx(-1e-3 / B * (silent * rowsum).sum(), rel=1e-4, abs=1e-9)
 
 
+def test_dense_fwd_q8_without_penalty():
+    """No penalty asked for, or one without the dead-neuron term: the same times, and that term is 0."""
+    from paper_2607_14672_gb300 import dstd
+    B, N_in, N_out, M = 3, 120, 90, 16
+    t_in, layer = dense_layer(B, N_in, N_out, M, 0.5, 0.25, seed=8, gammas=(0.05, 0.01, 0.0))
+    t_in, layer["W"] = f32(t_in), f32(layer["W"])
+    p, t, wq, w_scale, _, t_out, saved, pen = run_q8(t_in, layer, 1.0 / B)
+    assert pen[1].item() == 0 and pen[2].item() + pen[3].item() == B * N_out
+    again = torch.empty_like(t_out)
+    ws = torch.empty(dstd.dense_q8_workspace_bytes(B, N_in, N_out, p), dtype=torch.uint8, device="cuda")
+    dstd.dense_fwd_q8(t, wq, w_scale, p, again, saved, None, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(again, t_out)
+
+
 def test_dense_q8_gradient_passes_straight_through():
     """dense_bwd at the weights' values and the 8-bit forward's spike state,
     against the oracle's backward there."""
