@@ -252,6 +252,36 @@ def test_int8_matmul_streams_and_graph():
             assert torch.equal(out, expected(x, sx, w, sw, torch.float32))
 
 
+@pytest.mark.parametrize("T,N,K", [(3, 1000, 2048), (150, 1000, 2048)])
+def test_capture_after_copies_and_joins(T, N, K):
+    """Captured behind a copy, behind a fill on a forked stream and in a row of its own kind: replays see the new inputs."""
+    from paper_2607_14672_gb300 import dstd
+    src, sx, w, sw, out = random_case(T, N, K, 0, 21)
+    x, out2, half = torch.zeros_like(src), torch.empty_like(out), torch.empty(T, N, dtype=torch.bfloat16, device="cuda")
+    scratch = torch.empty(dstd.int8_matmul_workspace_bytes(T, N, K), dtype=torch.uint8, device="cuda")
+    dstd.int8_matmul(x, sx, w, sw, out, scratch)
+    torch.cuda.synchronize()
+    s, side = torch.cuda.Stream(), torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        x.copy_(src)
+        dstd.int8_matmul(x, sx, w, sw, out, scratch, stream=s)
+        side.wait_stream(s)
+        with torch.cuda.stream(side):
+            half.fill_(1.0)
+        s.wait_stream(side)
+        dstd.int8_matmul(x, sx, w, sw, half, scratch, stream=s)
+        dstd.int8_matmul(x, sx, w, sw, out2, scratch, stream=s)
+    for seed in (3, 4):
+        src.copy_(random_case(T, N, K, 0, seed)[0])
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = expected(src, sx, w, sw, torch.float32)
+        assert torch.equal(out, want) and torch.equal(out2, want) and torch.equal(half, want.bfloat16())
+
+
 @pytest.mark.parametrize("T,N,K", [(3, 3000, 4096), (70, 3000, 4096), (300, 2000, 1500)])
 def test_codes_written_just_before_the_product(T, N, K):
     """Weights and tokens quantised right before the product on the same stream,
