@@ -439,8 +439,11 @@ int dstd_quantize_rows(const void *x, dstd_type type, int rows, int cols, int64_
                        float *scale, float *values, int64_t ld_values, dstd_stream_t stream);
 
 /* Workspace bytes of dstd_int8_matmul for T tokens, N channels and K inputs;
- * 0 on invalid sizes. */
+ * 0 on invalid sizes. The first is enough for any operands; the second, without
+ * room for a copy of either, where the rows of both x and w start at multiples
+ * of 16 bytes (base addresses and ld_x, ld_w). */
 size_t dstd_int8_matmul_workspace_bytes(int T, int N, int K);
+size_t dstd_int8_matmul_aligned_workspace_bytes(int T, int N, int K);
 
 /* Product of 8-bit rows with a scale for each token and channel:
  *     out_tn = x_scale_t w_scale_n sum_k x_tk w_nk.
@@ -449,8 +452,8 @@ size_t dstd_int8_matmul_workspace_bytes(int T, int N, int K);
  *  x [T, K], w [N, K], row strides ld_x, ld_w >= K; T, N >= 0, 0 <= K <= 131071
  *  (K = 0 gives zeros); x_scale [T], w_scale [N].
  *  out [T, N] of out_type, row stride ld_out >= N; overlaps no input.
- *  workspace  dstd_int8_matmul_workspace_bytes(T, N, K) bytes, any contents;
- *             calls that can overlap on the GPU need one each. */
+ *  workspace  as the queries say, any contents; calls that can overlap on the
+ *             GPU need one each. */
 int dstd_int8_matmul(const int8_t *x, int64_t ld_x, const float *x_scale, const int8_t *w, int64_t ld_w,
                      const float *w_scale, int T, int N, int K, void *out, dstd_type out_type, int64_t ld_out,
                      void *workspace, size_t ws_bytes, dstd_stream_t stream);

@@ -1702,7 +1702,8 @@ Q8Ws q8_layout(void *base, int B, int N_in, int N_out, int Mp) {
     w.scale = b.take<float>((size_t)T);
     w.q = b.take<int8_t>((size_t)T * w.ld_q);
     w.D = b.take<float>((size_t)T * N_out);
-    w.product = b.take<char>(q8_workspace_bytes((int)T, N_out, N_in));
+    // the tokens' rows are aligned, the weights' where N_in is a multiple of 16
+    w.product = b.take<char>(q8_workspace_bytes((int)T, N_out, N_in, N_in % 16 == 0));
     w.bytes = b.off;
     return w;
 }
@@ -1733,7 +1734,12 @@ int dstd_quantize_rows(const void *x, dstd_type type, int rows, int cols, int64_
 
 size_t dstd_int8_matmul_workspace_bytes(int T, int N, int K) {
     if (T < 0 || N < 0 || K < 0 || K > kQ8MaxK) return 0;
-    return q8_workspace_bytes(T, N, K);
+    return q8_workspace_bytes(T, N, K, false);
+}
+
+size_t dstd_int8_matmul_aligned_workspace_bytes(int T, int N, int K) {
+    if (T < 0 || N < 0 || K < 0 || K > kQ8MaxK) return 0;
+    return q8_workspace_bytes(T, N, K, true);
 }
 
 int dstd_int8_matmul(const int8_t *x, int64_t ld_x, const float *x_scale, const int8_t *w, int64_t ld_w,
@@ -1747,11 +1753,11 @@ int dstd_int8_matmul(const int8_t *x, int64_t ld_x, const float *x_scale, const 
             return DSTD_E_INVALID;
         if (K > 0 && (!x || !w || ld_x < K || ld_w < K)) return DSTD_E_INVALID;
         if (!workspace || !aligned16(workspace)) return DSTD_E_INVALID;
-        if (ws_bytes < q8_workspace_bytes(T, N, K)) return DSTD_E_WORKSPACE;
     }
+    const Q8Args a{x, w, ld_x, ld_w, x_scale, w_scale, T, N, K, Q8Out{out, out_type, ld_out, 1}, false};
+    if (T > 0 && N > 0 && ws_bytes < q8_workspace_bytes(T, N, K, q8_rows_aligned(a))) return DSTD_E_WORKSPACE;
     TRY(device_ok());
     Timed tm(KK_INT8, (cudaStream_t)stream);
-    const Q8Args a{x, w, ld_x, ld_w, x_scale, w_scale, T, N, K, Q8Out{out, out_type, ld_out, 1}, false};
     return cu(launch_q8_product(a, workspace, (cudaStream_t)stream));
 }
 

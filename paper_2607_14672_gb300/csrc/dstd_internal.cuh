@@ -744,7 +744,8 @@ struct Q8Args {
     bool swapped;  // x holds the channels' rows and w the tokens': w_scale is multiplied first
 };
 constexpr int kQ8MaxK = 131071;  // (2^31 - 1) / 128^2: no 32-bit sum of products overflows
-size_t q8_workspace_bytes(int T, int N, int K);
+bool q8_rows_aligned(const Q8Args &a);  // both operands' rows start at multiples of 16 bytes
+size_t q8_workspace_bytes(int T, int N, int K, bool aligned);
 cudaError_t q8_status_read(unsigned int *out, int clear);
 cudaError_t launch_q8_product(const Q8Args &a, void *workspace, cudaStream_t st);
 

@@ -1098,12 +1098,12 @@ struct Q8Scratch {
     long long zeros;  // 16-byte words from ticket on
     size_t bytes;
 };
-Q8Scratch q8_scratch(void *base, int T, int N, int K, long long cut, int nt) {
+Q8Scratch q8_scratch(void *base, int T, int N, int K, bool copy, long long cut, int nt) {
     Q8Scratch s{};
     char *b = static_cast<char *>(base);
     s.ld = (K + 7) / 8 * 8;
     s.ld_w = (K + 15) / 16 * 16;
-    const size_t x = ((size_t)T * s.ld * 2 + 255) / 256 * 256, w = ((size_t)N * s.ld_w + 255) / 256 * 256;
+    const size_t x = ((size_t)T * s.ld * 2 + 255) / 256 * 256, w = copy ? ((size_t)N * s.ld_w + 255) / 256 * 256 : 0;
     s.x = (__half *)b;
     s.w = (int8_t *)(b + x);
     s.ticket = (unsigned *)(b + x + w);
@@ -1237,7 +1237,8 @@ cudaError_t run_few(const Q8Args &a, cudaStream_t st) {
 }
 
 cudaError_t run_tc(const Q8Args &a, const Q8Plan &p, int pairs, void *workspace, cudaStream_t st) {
-    const Q8Scratch s = q8_scratch(workspace, a.T, a.N, a.K, (long long)p.tiles_n * p.tiles_t - p.whole, p.nt);
+    const Q8Scratch s = q8_scratch(workspace, a.T, a.N, a.K, !w_rows_aligned(a),
+                                   (long long)p.tiles_n * p.tiles_t - p.whole, p.nt);
     PrepArgs pa{a.x, a.w, a.ld_x, a.ld_w, a.T, a.N, a.K, rows_aligned(a.x, a.ld_x), s.x, s.ld, s.w, s.ld_w,
                 (uint4 *)s.ticket, (long long)a.T * ((s.ld + 15) / 16),
                 w_rows_aligned(a) ? 0 : (long long)a.N * (s.ld_w / 16), s.zeros};
@@ -1257,14 +1258,16 @@ cudaError_t run_tc(const Q8Args &a, const Q8Plan &p, int pairs, void *workspace,
 
 }  // namespace
 
-// Exchanging the sides takes no more scratch than this: it is done only where
-// there are more tokens than channels.
-size_t q8_workspace_bytes(int T, int N, int K) {
+// Then no copy is made, whichever side is which.
+bool q8_rows_aligned(const Q8Args &a) { return rows_aligned(a.x, a.ld_x) && rows_aligned(a.w, a.ld_w); }
+
+// The sides are exchanged only where there are more tokens than channels.
+size_t q8_workspace_bytes(int T, int N, int K, bool aligned) {
     if (T < kTcMinTokens || N < 1 || K < 1) return 256;
     const long long cut = std::min<long long>((long long)((N + 255) / 256) * ((T + 31) / 32), kPairs);
     const long long cut_exchanged = std::min<long long>((long long)((T + 255) / 256) * ((N + 31) / 32), kPairs);
-    const size_t bytes = q8_scratch(nullptr, T, N, K, cut, 192).bytes;
-    return T > N ? std::max(bytes, q8_scratch(nullptr, N, T, K, cut_exchanged, 192).bytes) : bytes;
+    const size_t bytes = q8_scratch(nullptr, T, N, K, !aligned, cut, 192).bytes;
+    return T > N ? std::max(bytes, q8_scratch(nullptr, N, T, K, !aligned, cut_exchanged, 192).bytes) : bytes;
 }
 
 // The big form computes 256 rows of one side by up to 192 of the other at a

@@ -25,7 +25,8 @@ EXPORTS = ("dstd_dense_saved_bytes", "dstd_dense_workspace_bytes", "dstd_binning
            "dstd_dense_fwd_noalloc", "dstd_conv_workspace_bytes", "dstd_conv_fwd", "dstd_conv_bwd",
            "dstd_exact_workspace_bytes", "dstd_exact_fwd", "dstd_exact_bwd", "dstd_concat_channels", "dstd_split_channels",
            "dstd_ms_saved_bytes", "dstd_ms_workspace_bytes", "dstd_dense_fwd_ms", "dstd_dense_bwd_ms",
-           "dstd_quantize_rows", "dstd_int8_matmul_workspace_bytes", "dstd_int8_matmul", "dstd_dense_q8_workspace_bytes",
+           "dstd_quantize_rows", "dstd_int8_matmul_workspace_bytes", "dstd_int8_matmul_aligned_workspace_bytes",
+           "dstd_int8_matmul", "dstd_dense_q8_workspace_bytes",
            "dstd_dense_fwd_q8", "dstd_grad_norm_workspace_bytes", "dstd_grad_norm", "dstd_clip_grads", "dstd_adamw_clip")
 
 
@@ -111,6 +112,7 @@ def load(path=None):
         "dstd_dense_bwd_ms": (_I, [_P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _PP, _I, _P, _P, _P, _SZ, _P]),
         "dstd_quantize_rows": (_I, [_P, _I, _I, _I, _I64, _P, _I64, _P, _P, _I64, _P]),
         "dstd_int8_matmul_workspace_bytes": (_SZ, [_I, _I, _I]),
+        "dstd_int8_matmul_aligned_workspace_bytes": (_SZ, [_I, _I, _I]),
         "dstd_int8_matmul": (_I, [_P, _I64, _P, _P, _I64, _P, _I, _I, _I, _P, _I, _I64, _P, _SZ, _P]),
         "dstd_dense_q8_workspace_bytes": (_SZ, [_I, _I, _I, _PP]),
         "dstd_dense_fwd_q8": (_I, [_P, _P, _P, _I, _I, _I, _PP, _P, _P, _P, _P, _SZ, _P]),
@@ -457,11 +459,12 @@ def quantize_rows(x, q, scale, values=None, stream=None):
         raise DstdError(code, "dstd_quantize_rows")
 
 
-def int8_matmul_workspace_bytes(T, N, K):
+def int8_matmul_workspace_bytes(T, N, K, aligned=False):
     """Scratch of int8_matmul for T tokens, N channels, K inputs: from 9 tokens
-    on the tokens in 16 bits and room for a copy of the weights (touched only
-    where their rows are not 16-byte aligned)."""
-    return load().dstd_int8_matmul_workspace_bytes(T, N, K)
+    on the tokens in 16 bits and room for a copy of the weights; without the
+    latter where the rows of x and w start at multiples of 16 bytes (aligned)."""
+    f = load().dstd_int8_matmul_aligned_workspace_bytes if aligned else load().dstd_int8_matmul_workspace_bytes
+    return f(T, N, K)
 
 
 def int8_matmul(x, x_scale, w, w_scale, out, workspace, stream=None):

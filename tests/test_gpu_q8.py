@@ -185,6 +185,25 @@ def test_int8_matmul_misaligned(T):
         assert torch.equal(out, expected(x, sx, w, sw, torch.float32))
 
 
+@pytest.mark.parametrize("T,N,K", [(40, 3000, 4096), (9000, 64, 1024), (600, 600, 784), (5, 100, 64)])
+def test_aligned_workspace(T, N, K):
+    """The smaller workspace serves aligned operands, and is refused for others."""
+    from paper_2607_14672_gb300 import dstd
+    x, sx, w, sw, out = random_case(T, N, K, 0, 31)
+    small, full = (dstd.int8_matmul_workspace_bytes(T, N, K, aligned=a) for a in (True, False))
+    assert small <= full and (small < full or T < 9)
+    room = torch.full((small + 256,), 85, dtype=torch.uint8, device="cuda")
+    dstd.int8_matmul(x, sx, w, sw, out, room[:small])
+    torch.cuda.synchronize()
+    assert torch.equal(out, expected(x, sx, w, sw, torch.float32)) and (room[small:] == 85).all()
+    if T >= 9:
+        for which in range(2):  # either operand's rows at other addresses
+            y = padded((x if which else w).cpu(), 1, torch.int8)
+            with pytest.raises(dstd.DstdError) as e:
+                dstd.int8_matmul(y if which else x, sx, w if which else y, sw, out, room[:small])
+            assert e.value.code == -3
+
+
 def test_int8_matmul_empty():
     for T, N, K in ((0, 5, 16), (5, 0, 16), (5, 7, 0), (40, 70, 0)):
         x, w = torch.zeros(T, K, dtype=torch.int8, device="cuda"), torch.zeros(N, K, dtype=torch.int8, device="cuda")

@@ -62,6 +62,11 @@ def test_int8_matmul_refuses(lib):
     assert lib.dstd_int8_matmul_workspace_bytes(4, 8, 16) > 0
     for bad in ((-1, 8, 16), (4, -8, 16), (4, 8, -16), (4, 8, 131072)):
         assert lib.dstd_int8_matmul_workspace_bytes(*bad) == 0, bad
+        assert lib.dstd_int8_matmul_aligned_workspace_bytes(*bad) == 0, bad
+    # the weights' copy is what the aligned size leaves out
+    full, small = (f(64, 1000, 2048) for f in (lib.dstd_int8_matmul_workspace_bytes,
+                                               lib.dstd_int8_matmul_aligned_workspace_bytes))
+    assert abs((full - small) - 1000 * 2048) <= 256
 
 
 def test_dense_fwd_q8_refuses(lib):
