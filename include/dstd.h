@@ -476,10 +476,11 @@ int dstd_dense_fwd_q8(const float *t_in, const int8_t *w_q, const float *w_scale
  * The three calls below share a workspace of
  * dstd_grad_norm_workspace_bytes(count, n) bytes, whose first 64 bytes are
  * zero before its first use and are left so by every call (zero them again
- * after a DSTD_E_TIMEOUT); calls that can overlap on the GPU need one each. count >= 1 tensors of n[i] >= 0 elements (the arrays of
- * pointers and sizes are host memory, read during the call); type[i] is the
- * dstd_type of gradient i. Sums are formed in a fixed order: the same call on
- * the same tensors gives the same bits. */
+ * after a DSTD_E_TIMEOUT); calls that can overlap on the GPU need one each.
+ * count >= 1 tensors of n[i] >= 0 elements (the arrays of pointers and sizes
+ * are host memory, read during the call); type[i] is the dstd_type of gradient
+ * i. Sums are formed in a fixed order: the same call on the same tensors gives
+ * the same bits. */
 size_t dstd_grad_norm_workspace_bytes(int count, const int64_t *n);
 
 /* norm[0] = sqrt(sum over all tensors of g^2), fp32 (+inf where it passes fp32;

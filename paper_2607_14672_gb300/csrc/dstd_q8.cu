@@ -1205,10 +1205,10 @@ cudaError_t launch_tc(const Q8Args &q, const Q8Plan &p, const Q8Scratch &s, int 
 // blocks of 128 codes of K, or the weights' reading time. The big form: its plan,
 // 4 us for the pipeline's ends and 2 for its second launch, the preparation's
 // traffic (the tokens to 16 bits, a copy of weights whose rows are not aligned)
-// and, where a lane's row goes out piece by piece, the stores. Measured with the other form beside it (us, with
-// 6.5 of launch and events): 32 x 784 x 800 10.8 and 12.9, 16 x 4096 x 4096 12.9
-// and 18.0, 64 x 4096 x 4096 23.1 and 19.1, 32 x 16384 x 16384 103 and 56,
-// 256 x 3000 x 1000 (not aligned) 31 and 17.
+// and, where a lane's row goes out piece by piece, the stores. Measured with the
+// other form beside it (us, with 6.5 of launch and events): 32 x 784 x 800 10.8
+// and 12.9, 16 x 4096 x 4096 12.9 and 18.0, 64 x 4096 x 4096 23.1 and 19.1,
+// 32 x 16384 x 16384 103 and 56, 256 x 3000 x 1000 (not aligned) 31 and 17.
 double few_time(const Q8Args &a) {
     const int nt = a.T <= 8 ? 1 : (a.T <= 16 ? 2 : 4);
     const FewPlan f = nt == 1 ? few_plan<1>(a.T, a.N, a.K) : (nt == 2 ? few_plan<2>(a.T, a.N, a.K) : few_plan<4>(a.T, a.N, a.K));
