@@ -187,15 +187,18 @@ __global__ void __launch_bounds__(BLOCK, THREADS == 32 ? 1 : (BLOCK == 1024 ? 2 
     }
 }
 
-// rows too long for the registers: read twice (the second time mostly from L2)
+// rows too long for the registers: read twice (the second time mostly from L2).
+// Columns are counted without a sign: a row may have up to 2^31 - 1 of them, and
+// the count passes that by a step before the loop ends.
 template <class T>
 __global__ void __launch_bounds__(256) k_quantize_long(const T *__restrict__ x, const QuantArgs a) {
     __shared__ unsigned s_top[8];
     const long long r = blockIdx.x;
+    const unsigned cols = (unsigned)a.cols;
     const T *row = x + r * a.ld_x;
     unsigned top = 0;
 #pragma unroll 8
-    for (int k = threadIdx.x; k < a.cols; k += 256)
+    for (unsigned k = threadIdx.x; k < cols; k += 256)
         top = max(top, __float_as_uint(to_f32<T>(row[k])) & 0x7fffffffu);
     top = __reduce_max_sync(0xffffffffu, top);
     if ((threadIdx.x & 31) == 0) s_top[threadIdx.x >> 5] = top;
@@ -205,7 +208,7 @@ __global__ void __launch_bounds__(256) k_quantize_long(const T *__restrict__ x, 
     const RowCode c = row_code(top);
     if (threadIdx.x == 0) a.scale[r] = c.scale;
 #pragma unroll 4
-    for (int k = threadIdx.x; k < a.cols; k += 256) {
+    for (unsigned k = threadIdx.x; k < cols; k += 256) {
         const int v = code_of(to_f32<T>(row[k]), c);
         a.q[r * a.ld_q + k] = (int8_t)v;
         if (a.values) a.values[r * a.ld_v + k] = (float)v * c.scale;
