@@ -450,7 +450,8 @@ size_t dstd_int8_matmul_aligned_workspace_bytes(int T, int N, int K);
  * The sum is exact (any codes, -128 among them); it is rounded to fp32, times
  * x_scale_t, times w_scale_n, and rounded once more to a 16-bit out_type.
  *  x [T, K], w [N, K], row strides ld_x, ld_w >= K; T, N >= 0, 0 <= K <= 131071
- *  (K = 0 gives zeros); x_scale [T], w_scale [N].
+ *  (K = 0 gives zeros); from 9 tokens on T and N at most 2^31 - 256;
+ *  x_scale [T], w_scale [N].
  *  out [T, N] of out_type, row stride ld_out >= N; overlaps no input.
  *  workspace  as the queries say, any contents; calls that can overlap on the
  *             GPU need one each. */

@@ -1733,12 +1733,12 @@ int dstd_quantize_rows(const void *x, dstd_type type, int rows, int cols, int64_
 }
 
 size_t dstd_int8_matmul_workspace_bytes(int T, int N, int K) {
-    if (T < 0 || N < 0 || K < 0 || K > kQ8MaxK) return 0;
+    if (T < 0 || N < 0 || K < 0 || K > kQ8MaxK || !q8_sizes_ok(T, N)) return 0;
     return q8_workspace_bytes(T, N, K, false);
 }
 
 size_t dstd_int8_matmul_aligned_workspace_bytes(int T, int N, int K) {
-    if (T < 0 || N < 0 || K < 0 || K > kQ8MaxK) return 0;
+    if (T < 0 || N < 0 || K < 0 || K > kQ8MaxK || !q8_sizes_ok(T, N)) return 0;
     return q8_workspace_bytes(T, N, K, true);
 }
 
@@ -1746,7 +1746,7 @@ int dstd_int8_matmul(const int8_t *x, int64_t ld_x, const float *x_scale, const 
                      const float *w_scale, int T, int N, int K, void *out, dstd_type out_type, int64_t ld_out,
                      void *workspace, size_t ws_bytes, dstd_stream_t stream) {
     if (T < 0 || N < 0 || K < 0 || !type_ok(out_type)) return DSTD_E_INVALID;
-    if (K > kQ8MaxK) return DSTD_E_UNSUPPORTED;
+    if (K > kQ8MaxK || !q8_sizes_ok(T, N)) return DSTD_E_UNSUPPORTED;
     if (T > 0 && N > 0) {
         if (!x_scale || !w_scale || !out || !aligned_to(x_scale, 4) || !aligned_to(w_scale, 4) ||
             !aligned_to(out, type_bytes(out_type)) || ld_out < N)

@@ -744,6 +744,7 @@ struct Q8Args {
     bool swapped;  // x holds the channels' rows and w the tokens': w_scale is multiplied first
 };
 constexpr int kQ8MaxK = 131071;  // (2^31 - 1) / 128^2: no 32-bit sum of products overflows
+bool q8_sizes_ok(int T, int N);         // no row of a tile past the end has a number that passes 32 bits
 bool q8_rows_aligned(const Q8Args &a);  // both operands' rows start at multiples of 16 bytes
 size_t q8_workspace_bytes(int T, int N, int K, bool aligned);
 cudaError_t q8_status_read(unsigned int *out, int clear);

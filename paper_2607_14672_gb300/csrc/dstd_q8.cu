@@ -1261,6 +1261,12 @@ cudaError_t run_tc(const Q8Args &a, const Q8Plan &p, int pairs, void *workspace,
 
 }  // namespace
 
+// The big form counts whole tiles of up to 256 rows of either side.
+bool q8_sizes_ok(int T, int N) {
+    constexpr int most = 0x7fffffff - 255;
+    return T < kTcMinTokens || (T <= most && N <= most);
+}
+
 // Then no copy is made, whichever side is which.
 bool q8_rows_aligned(const Q8Args &a) { return rows_aligned(a.x, a.ld_x) && rows_aligned(a.w, a.ld_w); }
 
