@@ -531,15 +531,14 @@ cudaError_t launch_group(const ClipTensors &t, ClipOp op, int begin, int count, 
 // blocks of the one-launch form that are resident at once (0: an error)
 template <int CAP, bool STEP>
 unsigned once_blocks() {
-    static const unsigned blocks = [] {
-        int dev = 0, sms = 0, each = 0;
-        if (cudaGetDevice(&dev) != cudaSuccess ||
-            cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+    static PerDevice blocks;
+    return (unsigned)blocks.get([](int dev) {
+        int sms = 0, each = 0;
+        if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
             cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, k_clip_once<CAP, STEP>, THREADS, 0) != cudaSuccess)
-            return 0u;
-        return (unsigned)(sms * std::min(each, kOnceBlocks / 152));
-    }();
-    return blocks;
+            return 0;
+        return sms * std::min(each, kOnceBlocks / 152);
+    });
 }
 
 template <int CAP, bool STEP>

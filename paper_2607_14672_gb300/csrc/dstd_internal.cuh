@@ -7,6 +7,8 @@
 #include <cuda_fp16.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/dstd.h"
 
 namespace dstd {
@@ -413,6 +415,27 @@ __device__ __forceinline__ void finish_neuron(const LifConst &c, const ScanState
 constexpr unsigned int STATUS_TIMEOUT = 1u;
 cudaError_t status_read(unsigned int *out, int clear);
 void *tensor_map_encoder();  // the driver's cuTensorMapEncodeTiled, or null
+
+// A number of the present device (how many blocks fit at once), asked for once
+// per device. 0 is an error; it is not kept.
+class PerDevice {
+    static constexpr int kDevices = 64;
+    std::atomic<int> known_[kDevices] = {};
+
+  public:
+    template <class F>
+    int get(F ask) {
+        int dev = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+        if (dev < 0 || dev >= kDevices) return ask(dev);
+        int n = known_[dev].load(std::memory_order_relaxed);
+        if (n == 0) {
+            n = ask(dev);
+            known_[dev].store(n, std::memory_order_relaxed);
+        }
+        return n;
+    }
+};
 cudaError_t launch_wait_selftest(unsigned long long limit_ns, cudaStream_t st);
 
 // ---------------------------------------------------------------------------

@@ -1153,27 +1153,27 @@ cudaLaunchConfig_t tc_config(cudaLaunchAttribute (&attr)[2]) {
     return cfg;
 }
 
-// kernel attributes, set once per tile width; 0 or an error
+// Kernel attributes of a tile width. The grant of shared memory belongs to the
+// device that is current, so it is made at every launch.
 template <int NT>
 cudaError_t tc_setup() {
     using C = Q8Cfg<NT>;
-    static cudaError_t done = [] {
-        cudaError_t e = cudaFuncSetAttribute(k_q8_tc<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
-        if (e != cudaSuccess || !C::SPLIT_REGS) return e;
-        // a split of more registers than the block has would wait forever
+    const cudaError_t e = cudaFuncSetAttribute(k_q8_tc<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    if (e != cudaSuccess || !C::SPLIT_REGS) return e;
+    // a split of more registers than the block has would wait forever
+    static PerDevice registers;
+    const int regs = registers.get([](int) {
         cudaFuncAttributes at;
-        e = cudaFuncGetAttributes(&at, k_q8_tc<NT>);
-        if (e != cudaSuccess) return e;
-        if (at.numRegs * TC_THREADS < REGS_SUM || at.numRegs < REGS_CONV || at.numRegs > REGS_EPI)
-            return cudaErrorInvalidConfiguration;
-        return cudaSuccess;
-    }();
-    return done;
+        return cudaFuncGetAttributes(&at, k_q8_tc<NT>) == cudaSuccess ? at.numRegs : 0;
+    });
+    return regs * TC_THREADS < REGS_SUM || regs < REGS_CONV || regs > REGS_EPI ? cudaErrorInvalidConfiguration
+                                                                               : cudaSuccess;
 }
 
 // SM pairs that can be at work at once (0: an error); every tile width takes a whole SM
 int resident_pairs() {
-    static int resident = [] {
+    static PerDevice resident;
+    return resident.get([](int) {
         cudaLaunchAttribute attr[2];
         cudaLaunchConfig_t cfg = tc_config<192>(attr);
         cfg.gridDim = dim3(2 * kPairs);
@@ -1182,8 +1182,7 @@ int resident_pairs() {
         if (tc_setup<192>() != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, k_q8_tc<192>, &cfg) != cudaSuccess)
             return 0;
         return std::min(n, kPairs);
-    }();
-    return resident;
+    });
 }
 
 template <int NT>
