@@ -24,6 +24,9 @@ def narrow_layer(n_in, n_out, M, math_mode):
     return smem <= 200 * 1024
 
 
+OWN = object()  # the network's own setting
+
+
 class Clipped:
     """The optimiser's buffers of a network and its clipped AdamW step: one
     norm over the gradients of all layers, then every layer's update."""
@@ -34,9 +37,11 @@ class Clipped:
         # of the last clipped step, before clipping
         self.grad_norm = torch.zeros(1, dtype=torch.float32, device=self.device)
 
-    def optimizer(self, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, stream=None, max_norm=None):
-        """AdamW; with max_norm on gradients clipped to that global norm
-        (a step whose norm is not finite changes no weight)."""
+    def optimizer(self, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, stream=None, max_norm=OWN):
+        """AdamW on gradients clipped to the global norm max_norm: the network's
+        own unless one is given, None for no clipping (a clipped step whose norm
+        is not finite changes no weight)."""
+        max_norm = self.max_norm if max_norm is OWN else max_norm
         if max_norm is None:
             dstd.adamw_multi(self.W, self.gW, self.m, self.v, lr, betas[0], betas[1], eps, weight_decay,
                              self.adam_state, None, stream)
@@ -174,7 +179,7 @@ class DenseNet(Clipped):
         self.forward_loss(stream)
         self.backward(stream)
         if self.with_adamw:
-            self.optimizer(stream=stream, max_norm=self.max_norm)
+            self.optimizer(stream=stream)
 
     def objective(self):
         """Eq. cost_function on the last batch: loss + T + gamma_Q Q (device scalar)."""
@@ -357,7 +362,7 @@ class ConvNet(Clipped):
         self.loss_grad(stream)
         self.backward(stream)
         if self.with_adamw:
-            self.optimizer(stream=stream, max_norm=self.max_norm)
+            self.optimizer(stream=stream)
 
     def objective(self):
         return self.loss[0] + self.penalty[:, 0].sum() + self.penalty[:, 1].sum()

@@ -1,0 +1,31 @@
+"""What a network's optimiser asks of the library, without a GPU."""
+
+import pytest
+import torch
+
+from paper_2607_14672_gb300 import dstd, net
+
+
+class Stub(net.Clipped):
+    def __init__(self, max_norm):
+        self.W = self.gW = self.m = self.v = [torch.zeros(3)]
+        self.adam_state = torch.zeros(2, dtype=torch.int32)
+        self.grad_norm, self.clip_workspace, self.max_norm = torch.zeros(1), None, max_norm
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    seen = []
+    monkeypatch.setattr(dstd, "adamw_multi", lambda *a, **k: seen.append(None))
+    monkeypatch.setattr(dstd, "adamw_clip", lambda *a, **k: seen.append(a[10]))
+    return seen
+
+
+def test_optimizer_clips_to_the_networks_norm(calls):
+    Stub(0.5).optimizer()
+    Stub(0.5).optimizer(lr=1e-2)
+    Stub(0.5).optimizer(max_norm=2.0)
+    Stub(0.5).optimizer(max_norm=None)          # without clipping, asked for
+    Stub(None).optimizer()
+    Stub(None).optimizer(max_norm=3.0)
+    assert calls == [0.5, 0.5, 2.0, None, None, 3.0]
