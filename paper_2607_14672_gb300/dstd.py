@@ -537,9 +537,10 @@ def _list(x):
 
 def grad_norm_workspace_bytes(gs):
     """Bytes of the workspace that grad_norm, clip_grads and adamw_clip share
-    for these gradients: a tensor of zeros at first, left ready by each call."""
-    gs = _list(gs)
-    return load().dstd_grad_norm_workspace_bytes(len(gs), gs.n)
+    for these gradients: a tensor of zeros at first, left ready by each call.
+    Asks for nothing but the sizes: tensors of any device will do."""
+    sizes = gs.sizes if isinstance(gs, TensorList) else [t.numel() for t in gs]
+    return load().dstd_grad_norm_workspace_bytes(len(sizes), (ctypes.c_int64 * len(sizes))(*sizes))
 
 
 def grad_norm(gs, norm, workspace, tensor_norms=None, stream=None):

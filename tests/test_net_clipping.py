@@ -29,3 +29,19 @@ def test_optimizer_clips_to_the_networks_norm(calls):
     Stub(None).optimizer()
     Stub(None).optimizer(max_norm=3.0)
     assert calls == [0.5, 0.5, 2.0, None, None, 3.0]
+
+
+@pytest.mark.parametrize("kind", ["dense", "conv"])
+def test_networks_with_an_optimiser_are_built_on_any_device(kind):
+    """Their buffers need no GPU until a step runs."""
+    from paper_2607_14672_gb300 import build, configs
+    try:
+        build.build()
+    except RuntimeError:
+        pytest.skip("the library does not build here")
+    for max_norm in (None, 0.5):
+        if kind == "dense":
+            n = net.DenseNet(configs.config2(batch=4, M=8), "x3", device="cpu", with_adamw=True, max_norm=max_norm)
+        else:
+            n = net.ConvNet(configs.config4(batch=2, M=8), device="cpu", max_norm=max_norm)
+        assert len(n.m) == len(n.W) and n.clip_workspace.numel() > 64 and not n.clip_workspace.any()
