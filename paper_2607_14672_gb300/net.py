@@ -57,7 +57,8 @@ class DenseNet(Clipped):
     weights by rows and runs the layers' contractions on 8-bit codes; the
     backward (three-product mode) runs at the values the codes stand for, and
     the gradient passes straight through the rounding to the fp32 weights.
-    ``serve`` is the forward alone on the codes of the last ``quantize``.
+    ``serve`` is the forward alone on the codes of the last ``quantize`` or
+    ``take_codes`` (``has_codes``: there are some).
     max_norm: clip the AdamW step's gradients to this global norm.
     """
 
@@ -92,6 +93,7 @@ class DenseNet(Clipped):
             self.Wq = [torch.empty_like(w, dtype=torch.int8) for w in self.W]
             self.w_scale = [torch.empty(w.shape[0], dtype=torch.float32, device=dev) for w in self.W]
             self.Wv = [torch.empty_like(w) for w in self.W]
+            self.has_codes = False
         if ws == 0:
             raise ValueError("unsupported layer sizes or constants for the library")
         self.workspace = torch.empty(ws, dtype=torch.uint8, device=dev)
@@ -125,14 +127,22 @@ class DenseNet(Clipped):
         """8-bit codes, row scales and values of the present weights."""
         for w, q, scale, v in zip(self.W, self.Wq, self.w_scale, self.Wv):
             dstd.quantize_rows(w, q, scale, v, stream)
+        self.has_codes = True
 
     def take_codes(self, other):
         """The 8-bit weights of another q8 network of the same layers (e.g. of another batch size)."""
+        if not (self.q8 and other.q8 and other.has_codes):
+            raise ValueError("take_codes: both networks must be of mode q8, and the other one must have codes")
+        if self.sizes != other.sizes:
+            raise ValueError(f"take_codes: layers of {self.sizes} neurons cannot take those of {other.sizes}")
+        self.has_codes = True
         for mine, theirs in zip(self.Wq + self.w_scale, other.Wq + other.w_scale):
             mine.copy_(theirs)
 
     def serve(self, stream=None):
         """The forward on the 8-bit codes as they are (no weight is read in fp32)."""
+        if not (self.q8 and self.has_codes):
+            raise RuntimeError("serve: no 8-bit codes; a q8 network has them after quantize, forward or take_codes")
         for l in range(len(self.W)):
             dstd.dense_fwd_q8(self.layer_input(l), self.Wq[l], self.w_scale[l], self.p[l], self.t[l], self.saved[l],
                               self.penalty[l], self.workspace, stream)
