@@ -124,12 +124,15 @@ struct Pair {
 };
 
 // A thread's share of the chunk's sum of squares. Squares are added in plain
-// fp32 in runs of at most 64 elements, whose sums go into the pair. A run whose
-// sum leaves the range where fp32 squares are good (or is zero) is formed again
-// in 64 bits, into `rare`.
+// fp32 in runs of four packs (16 fp32 or 32 16-bit elements), whose sums go into
+// the pair. A run whose sum leaves the range where fp32 squares are good is formed
+// again in 64 bits, into `rare`, which is slow. Runs of zeros are not: silent
+// neurons leave whole rows of them in a network's gradients (268 M zeros took 985
+// us that way, as many other numbers 157).
 template <class T>
 __device__ __forceinline__ void chunk_squares(const T *g, long long n, Pair &s, double &rare) {
     constexpr int P = Pack<T>::P, RUN = 4;
+    constexpr uint32_t MAGNITUDE = sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu;
     const int tid = threadIdx.x;
     int head = 0;
     while ((reinterpret_cast<uintptr_t>(g + head) & 15) != 0) ++head;
@@ -138,26 +141,30 @@ __device__ __forceinline__ void chunk_squares(const T *g, long long n, Pair &s, 
     const long long packs = (n - head) / P;
     for (long long base = tid; base < packs; base += THREADS * RUN) {
         float f = 0.f;
+        uint32_t bits = 0;
         if (base + THREADS * (RUN - 1) < packs) {
             uint4 u[RUN];
 #pragma unroll
             for (int i = 0; i < RUN; ++i) u[i] = load16(p + P * (base + THREADS * i));
 #pragma unroll
-            for (int i = 0; i < RUN; ++i)
+            for (int i = 0; i < RUN; ++i) {
+                bits |= u[i].x | u[i].y | u[i].z | u[i].w;
 #pragma unroll
                 for (int e = 0; e < P; ++e) f = fmaf(Pack<T>::one(u[i], e), Pack<T>::one(u[i], e), f);
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < RUN; ++i)
                 if (base + THREADS * i < packs) {
                     const uint4 u = load16(p + P * (base + THREADS * i));
+                    bits |= u.x | u.y | u.z | u.w;
 #pragma unroll
                     for (int e = 0; e < P; ++e) f = fmaf(Pack<T>::one(u, e), Pack<T>::one(u, e), f);
                 }
         }
         if (f > 1e-30f && f < 1e30f) {
             s.add(f);
-        } else {
+        } else if ((bits & MAGNITUDE) != 0) {
 #pragma unroll 1
             for (int i = 0; i < RUN * P; ++i) {
                 const long long at = base + THREADS * (i / P);

@@ -52,3 +52,40 @@ def test_dense_network_optimizer_by_hand_is_clipped():
     torch.cuda.synchronize()
     m, _ = norms(n.m)
     assert m == pytest.approx(0.1 * 1e-3, rel=FACTOR + 8 * U)
+
+
+def microseconds(f, n=10):
+    for _ in range(3):
+        f()
+    times = []
+    for _ in range(7):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        for _ in range(n):
+            f()
+        b.record()
+        torch.cuda.synchronize()
+        times.append(a.elapsed_time(b) / n * 1e3)
+    return sorted(times)[3]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_norm_of_zeros_takes_no_longer(dtype):
+    """Gradients with rows of zeros, as silent neurons leave them, and of nothing
+    else: the same bytes are read, so about the same time is taken (a factor of
+    1.5 for the measurement), and the zeros count for nothing."""
+    from paper_2607_14672_gb300 import dstd
+    n = 1 << 26
+    dense = torch.randn(n, device="cuda").to(dtype)
+    rows = dense.clone()
+    rows.view(-1, 4096)[::2] = 0
+    rows.view(-1, 4096)[1::4] *= -0.0
+    zeros = torch.zeros_like(dense)
+    norm, ws = torch.empty(1, device="cuda"), workspace([dense])
+    lists = [dstd.TensorList([x]) for x in (dense, rows, zeros)]
+    took = [microseconds(lambda: dstd.grad_norm(l, norm, ws)) for l in lists]
+    assert max(took[1:]) <= 1.5 * took[0], took
+    assert norm.item() == 0.0
+    dstd.grad_norm(lists[1], norm, ws)
+    want = rows.double().square().sum().sqrt().item()
+    assert norm.item() == pytest.approx(want, rel=NORM, abs=0)
