@@ -237,9 +237,13 @@ __device__ __forceinline__ double sum_slots(const A &a) {
     for (int o = 16; o > 0; o >>= 1) s += __shfl_down_sync(0xffffffffu, s, o);
     return s;
 }
-__device__ __forceinline__ float clip_factor(double norm, double max_norm) {
-    return isfinite(norm) && norm > max_norm ? (float)(max_norm / norm) : 1.f;
+__device__ __forceinline__ ClipFactor clip_factor(double norm, double max_norm) {
+    if (!isfinite(norm) || !(norm > max_norm)) return ClipFactor{1.f, 1.f};
+    const double c = max_norm / norm;
+    return c >= 0x1p-126 ? ClipFactor{(float)c, 1.f} : ClipFactor{(float)(c * 0x1p126), 0x1p-126f};
 }
+// a < 1 where b is not 1: nothing overflows on the way
+__device__ __forceinline__ float clipped(float g, ClipFactor c) { return g * c.a * c.b; }
 
 // The norm by itself: the block that draws the last ticket adds the slots in
 // order, and derives from the total what the clipping needs.
@@ -287,18 +291,18 @@ __global__ void __launch_bounds__(THREADS) k_sum_squares(const ClipArgs<CAP> a) 
 // The passes after the norm take each chunk from its end: the norm read it from
 // its start, so what of the gradients is still in L2 is at the ends.
 template <class T>
-__device__ __forceinline__ void scale_chunk(const T *g, T *out, long long n, float coef) {
+__device__ __forceinline__ void scale_chunk(const T *g, T *out, long long n, ClipFactor coef) {
     const int tid = threadIdx.x;
     int head = 0;
     while (head < 4 && !(fits(g, head) && fits(out, head))) ++head;
     if (head == 4 || n < 4) {  // the two are placed differently (or hardly anything is there)
 #pragma unroll 4
-        for (long long i = tid; i < n; i += THREADS) out[i] = Four<T>::round(Four<T>::one(g[i]) * coef);
+        for (long long i = tid; i < n; i += THREADS) out[i] = Four<T>::round(clipped(Four<T>::one(g[i]), coef));
         return;
     }
     const long long fours = (n - head) / 4, done = head + 4 * fours;
-    if (tid < head) out[tid] = Four<T>::round(Four<T>::one(g[tid]) * coef);
-    if (done + tid < n) out[done + tid] = Four<T>::round(Four<T>::one(g[done + tid]) * coef);
+    if (tid < head) out[tid] = Four<T>::round(clipped(Four<T>::one(g[tid]), coef));
+    if (done + tid < n) out[done + tid] = Four<T>::round(clipped(Four<T>::one(g[done + tid]), coef));
     const T *p = g + head;
     T *q = out + head;
     for (long long base = fours - 1 - tid; base >= 0; base -= THREADS * 4) {
@@ -310,15 +314,16 @@ __device__ __forceinline__ void scale_chunk(const T *g, T *out, long long n, flo
         for (int i = 0; i < 4; ++i)
             if (base - THREADS * i >= 0)
                 Four<T>::store(q + 4 * (base - THREADS * i),
-                               make_float4(x[i].x * coef, x[i].y * coef, x[i].z * coef, x[i].w * coef));
+                               make_float4(clipped(x[i].x, coef), clipped(x[i].y, coef), clipped(x[i].z, coef),
+                                           clipped(x[i].w, coef)));
     }
 }
 
 template <class A>
-__device__ __forceinline__ void scale_chunks(const A &a, float coef) {
+__device__ __forceinline__ void scale_chunks(const A &a, ClipFactor coef) {
     for (unsigned c = blockIdx.x; c < a.chunks; c += gridDim.x) {
         const ClipSeg &sg = a.seg[seg_of(a, c)];
-        if (coef == 1.f && sg.out == sg.g) continue;
+        if (coef.a == 1.f && coef.b == 1.f && sg.out == sg.g) continue;
         const long long lo = (long long)(c - sg.first) * a.chunk;
         const long long n = lo + a.chunk < sg.n ? a.chunk : sg.n - lo;
         if (sg.type == DSTD_TYPE_F32) scale_chunk((const float *)sg.g + lo, (float *)sg.out + lo, n, coef);
@@ -329,10 +334,11 @@ __device__ __forceinline__ void scale_chunks(const A &a, float coef) {
 }
 
 struct StepConst {
-    float coef, b1, one_b1, b2, one_b2, bc1, bc2, lr, decay, eps;
+    ClipFactor coef;
+    float b1, one_b1, b2, one_b2, bc1, bc2, lr, decay, eps;
 };
 __device__ __forceinline__ void adamw_one(const StepConst &c, float g, float &w, float &m, float &v) {
-    g *= c.coef;
+    g = clipped(g, c.coef);
     m = c.b1 * m + c.one_b1 * g;
     v = c.b2 * v + c.one_b2 * (g * g);
     w = w * c.decay - c.lr * (m / c.bc1) / (sqrtf(v / c.bc2) + c.eps);
@@ -388,7 +394,7 @@ __device__ __forceinline__ void adamw_chunk(const StepConst &c, const T *g, floa
 
 // t: updates done with this one
 template <class A>
-__device__ __forceinline__ void adamw_chunks(const A &a, float coef, float t) {
+__device__ __forceinline__ void adamw_chunks(const A &a, ClipFactor coef, float t) {
     StepConst k;
     k.coef = coef;
     k.b1 = a.b1;
@@ -433,7 +439,7 @@ __global__ void __launch_bounds__(THREADS) k_clip_apply(const ClipArgs<CAP> a) {
 template <int CAP, bool STEP>
 __global__ void __launch_bounds__(THREADS, 2) k_clip_once(const ClipArgs<CAP> a) {
     __shared__ SumShared sh;
-    __shared__ float s_coef;
+    __shared__ ClipFactor s_coef;
     __shared__ int s_go;
     unsigned *arrived = a.ticket + 1, *left = a.ticket + 2;
     const float t = STEP ? (float)(a.step[0] + 1) : 0.f;

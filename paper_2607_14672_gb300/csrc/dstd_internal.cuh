@@ -715,10 +715,16 @@ struct ClipSeg {
     unsigned first;  // number of the tensor's first chunk
     int type;
 };
+// c = min(1, max_norm / norm) as a * b, b a power of two. A norm near or past the
+// end of fp32 makes a c below fp32's normal numbers, which alone would have lost
+// bits (or all of them): b is 2^-126 then, else 1.
+struct ClipFactor {
+    float a, b;
+};
 struct ClipResult {
     double sum;
-    float coef;  // min(1, max_norm / norm); 1 when the norm is not finite
-    int skip;    // 1 when the norm is not finite
+    ClipFactor coef;  // 1 when the norm is not finite in 64 bits (a gradient is not)
+    int skip;         // 1 then
 };
 // tensors of one launch (a kernel's arguments hold them); longer lists take several
 constexpr int kClipFewTensors = 32, kClipMaxTensors = 512;

@@ -89,3 +89,18 @@ def test_norm_of_zeros_takes_no_longer(dtype):
     dstd.grad_norm(lists[1], norm, ws)
     want = rows.double().square().sum().sqrt().item()
     assert norm.item() == pytest.approx(want, rel=NORM, abs=0)
+
+
+@pytest.mark.parametrize("max_norm", [0.5, 1e-7, 1e-30])
+@pytest.mark.parametrize("n", [1 << 18, (1 << 19) + 77])   # one launch, two launches
+def test_clip_factors_below_fp32(n, max_norm):
+    """max_norm / norm below fp32's normal numbers, or below its smallest one: the clipped gradients are as
+    near as with any other factor."""
+    from paper_2607_14672_gb300 import dstd
+    g = torch.full((n,), 3e38, device="cuda")
+    g[::2] = -1e38
+    total, _ = norms([g])
+    out, norm = torch.empty_like(g), torch.empty(1, device="cuda")
+    dstd.clip_grads([g], max_norm, norm, workspace([g]), [out])
+    want = host(g) * (max_norm / total)
+    assert (abs(host(out) - want) <= (FACTOR + U) * abs(want)).all()
