@@ -491,9 +491,10 @@ int dstd_grad_norm(int count, const void *const *g, const int64_t *n, const int3
                    float *tensor_norms, void *workspace, size_t ws_bytes, dstd_stream_t stream);
 
 /* out_i = c g_i with c = min(1, max_norm / norm), norm as above (norm[0] out).
- * When the norm is not finite the gradients pass unchanged (c = 1): the caller
- * sees it in norm. out_i has g_i's type and is g_i itself or does not overlap
- * any gradient. max_norm > 0 (+inf: no clipping). */
+ * Where a gradient is infinite or NaN all pass unchanged (c = 1), and norm[0] is
+ * infinite or NaN. Finite gradients whose norm passes fp32 are clipped (c is
+ * formed in 64 bits), although norm[0] is +inf. out_i has g_i's type and is g_i
+ * itself or does not overlap any gradient. max_norm > 0 (+inf: no clipping). */
 int dstd_clip_grads(int count, const void *const *g, void *const *out, const int64_t *n, const int32_t *type,
                     double max_norm, float *norm, void *workspace, size_t ws_bytes, dstd_stream_t stream);
 
@@ -501,8 +502,10 @@ int dstd_clip_grads(int count, const void *const *g, void *const *out, const int
  * gradients are only read. With t the count of updates after this one:
  *     m = beta1 m + (1 - beta1) c g,  v = beta2 v + (1 - beta2) (c g)^2,
  *     w = w (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps).
- * When the norm is not finite (a gradient is infinite or NaN), w, m, v and the
- * count stay as they were. w, m, v are fp32; g of type[i].
+ * Where a gradient is infinite or NaN, w, m, v and the count stay as they were.
+ * The count tells such a step from one whose finite gradients have a norm that
+ * passes fp32, which is done: norm[0] is +inf there too. w, m, v are fp32; g of
+ * type[i].
  *  step    device int32[1]: updates done so far, advanced by the call.
  *  lr_dev  device float replacing lr (may be NULL).
  *  norm    device float[1] out.

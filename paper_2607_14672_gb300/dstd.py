@@ -559,8 +559,9 @@ def grad_norm(gs, norm, workspace, tensor_norms=None, stream=None):
 
 def clip_grads(gs, max_norm, norm, workspace, outs=None, stream=None):
     """Gradients times min(1, max_norm / norm), in place or into ``outs``;
-    norm[0] receives the norm before clipping. When it is not finite the
-    gradients pass unchanged."""
+    norm[0] receives the norm before clipping. Where a gradient is infinite or
+    NaN all pass unchanged. Finite gradients whose norm passes float32 are
+    clipped, although norm[0] is inf."""
     _torch()
     gs = _list(gs)
     outs = gs if outs is None else _list(outs)
@@ -577,8 +578,10 @@ def adamw_clip(ws, gs, ms, vs, lr, beta1, beta2, eps, weight_decay, step, max_no
                stream=None):
     """One AdamW step of the tensors ws (in place, with ms, vs) on gradients
     clipped to the global norm max_norm; gs is only read. step: device int32
-    tensor whose first element counts the updates done. A norm that is not
-    finite changes nothing but norm[0]."""
+    tensor whose first element counts the updates done. Where a gradient is
+    infinite or NaN nothing changes but norm[0], and the count tells so:
+    norm[0] is also inf where the norm of finite gradients passes float32, and
+    those are clipped and the step is done."""
     torch = _torch()
     ws, gs, ms, vs = _list(ws), _list(gs), _list(ms), _list(vs)
     if not (ws.sizes == gs.sizes == ms.sizes == vs.sizes):

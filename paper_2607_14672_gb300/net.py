@@ -39,8 +39,8 @@ class Clipped:
 
     def optimizer(self, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, stream=None, max_norm=OWN):
         """AdamW on gradients clipped to the global norm max_norm: the network's
-        own unless one is given, None for no clipping (a clipped step whose norm
-        is not finite changes no weight)."""
+        own unless one is given, None for no clipping (a clipped step with an
+        infinite or NaN gradient changes no weight and is not counted)."""
         max_norm = self.max_norm if max_norm is OWN else max_norm
         if max_norm is None:
             dstd.adamw_multi(self.W, self.gW, self.m, self.v, lr, betas[0], betas[1], eps, weight_decay,

@@ -7,7 +7,7 @@ import math
 import pytest
 import torch
 
-from test_gpu_clip import FACTOR, NORM, U, host, lib, norms, workspace  # noqa: F401 (lib is a fixture)
+from test_gpu_clip import FACTOR, NORM, U, adamw_ref, host, lib, norms, workspace  # noqa: F401 (lib is a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -104,3 +104,28 @@ def test_clip_factors_below_fp32(n, max_norm):
     dstd.clip_grads([g], max_norm, norm, workspace([g]), [out])
     want = host(g) * (max_norm / total)
     assert (abs(host(out) - want) <= (FACTOR + U) * abs(want)).all()
+
+
+@pytest.mark.parametrize("n", [1 << 20, (1 << 24) + 5])   # one launch, two launches
+def test_step_of_gradients_whose_norm_passes_fp32(n):
+    """Finite gradients with a norm beyond fp32: norm[0] is inf, and the step is clipped, done and counted. One
+    infinite gradient among them: norm[0] is inf as well, and nothing is done or counted."""
+    from paper_2607_14672_gb300 import dstd
+    lr, b1, b2, eps, wd, max_norm = 1e-3, 0.9, 0.999, 1e-8, 1e-2, 0.5
+    g = torch.full((n,), 3e38, device="cuda")
+    g[::2] = -1e38
+    w, m, v = (torch.rand(n, device="cuda") * s for s in (0.1, 1e-2, 1e-6))
+    before = [host(x) for x in (w, m, v)]
+    step, norm, ws = torch.tensor([4], dtype=torch.int32, device="cuda"), torch.zeros(1, device="cuda"), workspace([g])
+    dstd.adamw_clip([w], [g], [m], [v], lr, b1, b2, eps, wd, step, max_norm, norm, ws)
+    total, _ = norms([g])
+    assert total > 3.5e38 and norm.item() == math.inf and step.item() == 5
+    w2, m2, v2, e_w, e_m, e_v = adamw_ref(before[0], host(g), before[1], before[2], 5, lr, b1, b2, eps, wd,
+                                          max_norm / total)
+    for got, want, off in ((w, w2, e_w), (m, m2, e_m), (v, v2, e_v)):
+        assert (abs(host(got) - want) <= off).all()
+    kept = [x.clone() for x in (w, m, v)]
+    g[n // 3] = math.inf
+    dstd.adamw_clip([w], [g], [m], [v], lr, b1, b2, eps, wd, step, max_norm, norm, ws)
+    assert norm.item() == math.inf and step.item() == 5
+    assert all(torch.equal(a, b) for a, b in zip((w, m, v), kept))
