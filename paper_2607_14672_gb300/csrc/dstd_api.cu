@@ -97,14 +97,18 @@ const char *const kKindNames[KK_COUNT] = {
     "gradt_gather", "gemm_dW", "dw_reduce", "loss", "adamw", "binning_public", "what_public", "selftest", "narrow_fwd",
     "narrow_bwd", "exact_fwd", "skip_channels", "exact_bwd", "quantize_rows", "int8_matmul", "clip"};
 
+struct Span {
+    cudaEvent_t first, second;
+    int launches;  // between the two
+};
 struct Timing {
     std::mutex mu;
     bool on = false;
     std::vector<cudaEvent_t> pool;
-    std::vector<std::pair<cudaEvent_t, cudaEvent_t>> pending[KK_COUNT];
+    std::vector<Span> pending[KK_COUNT];
     // pairs captured into a CUDA graph as event-record nodes: every replay
     // records them again; dstd_timing_collect adds one replay's worth
-    std::vector<std::pair<cudaEvent_t, cudaEvent_t>> graph[KK_COUNT];
+    std::vector<Span> graph[KK_COUNT];
     double ms[KK_COUNT] = {};
     long long n[KK_COUNT] = {};
 };
@@ -128,7 +132,7 @@ void drain_pending() {
             float ms = 0.f;
             if (cudaEventElapsedTime(&ms, pr.first, pr.second) == cudaSuccess) {
                 g_timing.ms[k] += ms;
-                g_timing.n[k] += 1;
+                g_timing.n[k] += pr.launches;
             }
             g_timing.pool.push_back(pr.first);
             g_timing.pool.push_back(pr.second);
@@ -142,6 +146,7 @@ void drain_pending() {
 // nodes of the graph (read back per replay by dstd_timing_collect).
 struct Timed {
     int kind;
+    int launches = 1;  // what a scope that makes none or several counts here
     cudaStream_t st;
     cudaEvent_t a = nullptr;
     bool captured = false;
@@ -165,7 +170,7 @@ struct Timed {
         cudaEvent_t b = take_event();
         const cudaError_t e =
             !b ? cudaErrorUnknown : (captured ? cudaEventRecordWithFlags(b, st, cudaEventRecordExternal) : cudaEventRecord(b, st));
-        if (e == cudaSuccess) (captured ? g_timing.graph : g_timing.pending)[kind].push_back({a, b});
+        if (e == cudaSuccess) (captured ? g_timing.graph : g_timing.pending)[kind].push_back({a, b, launches});
         else {
             g_timing.pool.push_back(a);
             if (b) g_timing.pool.push_back(b);
@@ -1545,7 +1550,7 @@ int dstd_timing_collect(void) {
             float ms = 0.f;
             if (cudaEventElapsedTime(&ms, pr.first, pr.second) == cudaSuccess) {
                 g_timing.ms[k] += ms;
-                g_timing.n[k] += 1;
+                g_timing.n[k] += pr.launches;
             }
         }
     }
@@ -1728,6 +1733,7 @@ int dstd_quantize_rows(const void *x, dstd_type type, int rows, int cols, int64_
     }
     TRY(device_ok());
     Timed tm(KK_QUANTIZE, (cudaStream_t)stream);
+    tm.launches = rows > 0 ? 1 : 0;
     return cu(launch_quantize_rows(x, type, rows, cols, ld_x, q, ld_q, scale, values, ld_values,
                                    (cudaStream_t)stream));
 }
@@ -1758,7 +1764,7 @@ int dstd_int8_matmul(const int8_t *x, int64_t ld_x, const float *x_scale, const 
     if (T > 0 && N > 0 && ws_bytes < q8_workspace_bytes(T, N, K, q8_rows_aligned(a))) return DSTD_E_WORKSPACE;
     TRY(device_ok());
     Timed tm(KK_INT8, (cudaStream_t)stream);
-    return cu(launch_q8_product(a, workspace, (cudaStream_t)stream));
+    return cu(launch_q8_product(a, workspace, tm.launches, (cudaStream_t)stream));
 }
 
 size_t dstd_dense_q8_workspace_bytes(int B, int N_in, int N_out, const dstd_params *p) {
@@ -1794,7 +1800,7 @@ int dstd_dense_fwd_q8(const float *t_in, const int8_t *w_q, const float *w_scale
     {
         Timed tm(KK_INT8, st);
         const Q8Args a{ws.q, w_q, ws.ld_q, N_in, ws.scale, w_scale, T, N_out, N_in, Q8Out{ws.D, DSTD_TYPE_F32, 1, T}, false};
-        TRY(cu(launch_q8_product(a, ws.product, st)));
+        TRY(cu(launch_q8_product(a, ws.product, tm.launches, st)));
     }
     Timed tm(KK_SCAN, st);
     return cu(launch_scan_solve(ws.D, Mp, T, 1, B, N_out, c, nullptr, sums ? ws.rowsum : nullptr, t_out, sv.q, sv.s,
@@ -1818,7 +1824,7 @@ int dstd_grad_norm(int count, const void *const *g, const int64_t *n, const int3
     const ClipTensors t{count, g, nullptr, nullptr, nullptr, n, type};
     ClipHyper h{};
     h.max_norm = INFINITY;
-    return cu(launch_clip(t, ClipOp::Norm, h, norm, tensor_norms, workspace, (cudaStream_t)stream));
+    return cu(launch_clip(t, ClipOp::Norm, h, norm, tensor_norms, workspace, tm.launches, (cudaStream_t)stream));
 }
 
 int dstd_clip_grads(int count, const void *const *g, void *const *out, const int64_t *n, const int32_t *type,
@@ -1832,7 +1838,7 @@ int dstd_clip_grads(int count, const void *const *g, void *const *out, const int
     const ClipTensors t{count, g, out, nullptr, nullptr, n, type};
     ClipHyper h{};
     h.max_norm = max_norm;
-    return cu(launch_clip(t, ClipOp::Scale, h, norm, nullptr, workspace, (cudaStream_t)stream));
+    return cu(launch_clip(t, ClipOp::Scale, h, norm, nullptr, workspace, tm.launches, (cudaStream_t)stream));
 }
 
 int dstd_adamw_clip(int count, float *const *w, const void *const *g, float *const *m, float *const *v,
@@ -1853,7 +1859,7 @@ int dstd_adamw_clip(int count, float *const *w, const void *const *g, float *con
     Timed tm(KK_CLIP, (cudaStream_t)stream);
     const ClipTensors t{count, g, reinterpret_cast<void *const *>(w), m, v, n, type};
     const ClipHyper h{max_norm, lr, beta1, beta2, eps, weight_decay, step, lr_dev};
-    return cu(launch_clip(t, ClipOp::Adamw, h, norm, nullptr, workspace, (cudaStream_t)stream));
+    return cu(launch_clip(t, ClipOp::Adamw, h, norm, nullptr, workspace, tm.launches, (cudaStream_t)stream));
 }
 
 }  // extern "C"

@@ -593,7 +593,7 @@ cudaError_t clip_status_read(unsigned int *out, int clear) {
 }
 
 cudaError_t launch_clip(const ClipTensors &t, ClipOp op, const ClipHyper &h, float *norm, float *norm_each,
-                        void *workspace, cudaStream_t st) {
+                        void *workspace, int &launches, cudaStream_t st) {
     auto fill = [&](auto &a, ClipOp pass) {
         a.ticket = (unsigned *)workspace;
         a.result = (ClipResult *)((char *)workspace + 64);
@@ -619,6 +619,7 @@ cudaError_t launch_clip(const ClipTensors &t, ClipOp op, const ClipHyper &h, flo
     // and 8.5, 1.3 M 12.6 and 14.6, 4.7 M 26.9 and 29.0, 16 M 82 and 83, 67 M 343 and 333; clipping 100 thousand
     // gradients 4.4 and 5.4, 1.3 M 8.5 and 7.5
     if (op != ClipOp::Norm && t.count <= kClipMaxTensors && total <= (op == ClipOp::Adamw ? kOnceStep : kOnceClip)) {
+        launches = 1;
         auto once = [&](auto &a) {
             fill(a, op);
             return op == ClipOp::Scale ? launch_once<std::extent_v<decltype(a.seg)>, false>(t, total, a, st)
@@ -632,6 +633,7 @@ cudaError_t launch_clip(const ClipTensors &t, ClipOp op, const ClipHyper &h, flo
         return once(a);
     }
     // the norm (whose last launch counts the update), then the pass
+    launches = 0;
     for (int pass = 0; pass < (op == ClipOp::Norm ? 1 : 2); ++pass) {
         const ClipOp now = pass == 0 ? ClipOp::Norm : op;
         for (int begin = 0, launch = 0; begin < t.count; begin += kClipMaxTensors, ++launch) {
@@ -643,6 +645,7 @@ cudaError_t launch_clip(const ClipTensors &t, ClipOp op, const ClipHyper &h, flo
                 a.norm_each = norm_each ? norm_each + begin : nullptr;
                 return launch_group(t, now, begin, count, a, st);
             };
+            ++launches;
             cudaError_t e;
             if (count <= kClipFewTensors) {
                 ClipArgs<kClipFewTensors> a{};

@@ -748,7 +748,7 @@ enum class ClipOp { Norm, Scale, Adamw };  // the last two with the norm before 
 cudaError_t clip_status_read(unsigned int *out, int clear);
 size_t clip_workspace_bytes(int count, const int64_t *n);
 cudaError_t launch_clip(const ClipTensors &t, ClipOp op, const ClipHyper &h, float *norm, float *norm_each,
-                        void *workspace, cudaStream_t st);
+                        void *workspace, int &launches, cudaStream_t st);  // launches out
 
 // 8-bit rows and their products (dstd_q8.cu).
 cudaError_t launch_quantize_rows(const void *x, dstd_type type, int rows, int cols, long long ld_x, int8_t *q,
@@ -777,6 +777,6 @@ bool q8_sizes_ok(int T, int N);         // no row of a tile past the end has a n
 bool q8_rows_aligned(const Q8Args &a);  // both operands' rows start at multiples of 16 bytes
 size_t q8_workspace_bytes(int T, int N, int K, bool aligned);
 cudaError_t q8_status_read(unsigned int *out, int clear);
-cudaError_t launch_q8_product(const Q8Args &a, void *workspace, cudaStream_t st);
+cudaError_t launch_q8_product(const Q8Args &a, void *workspace, int &launches, cudaStream_t st);  // launches out
 
 }  // namespace dstd

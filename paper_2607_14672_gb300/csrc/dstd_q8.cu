@@ -1283,7 +1283,8 @@ size_t q8_workspace_bytes(int T, int N, int K, bool aligned) {
 // rows of the other. So which side is which is chosen with the form: with more
 // tokens than channels they are exchanged where that is estimated to be faster
 // (7561 tokens, 4181 inputs, 21 channels: 25 us instead of 42).
-cudaError_t launch_q8_product(const Q8Args &a, void *workspace, cudaStream_t st) {
+cudaError_t launch_q8_product(const Q8Args &a, void *workspace, int &launches, cudaStream_t st) {
+    launches = 0;
     if (a.T == 0 || a.N == 0) return cudaSuccess;
     const int pairs = resident_pairs();
     if (pairs < 1) return cudaErrorInvalidConfiguration;
@@ -1306,6 +1307,7 @@ cudaError_t launch_q8_product(const Q8Args &a, void *workspace, cudaStream_t st)
         }
     }
     const Q8Args &c = form & 1 ? b : a;
+    launches = form & 2 ? 2 : 1;
     return form & 2 ? run_tc(c, plan, pairs, workspace, st) : run_few(c, st);
 }
 

@@ -176,10 +176,16 @@ cudaError_t cudaGetSymbolAddress(void **p, const void *) {
     *p = (void *)256;
     return cudaSuccess;
 }
-cudaError_t cudaEventCreate(cudaEvent_t *) { return cudaErrorUnknown; }
+cudaError_t cudaEventCreate(cudaEvent_t *e) {
+    *e = (cudaEvent_t)256;
+    return cudaSuccess;
+}
 cudaError_t cudaEventCreateWithFlags(cudaEvent_t *, unsigned) { return cudaErrorUnknown; }
-cudaError_t cudaEventElapsedTime(float *, cudaEvent_t, cudaEvent_t) { return cudaErrorUnknown; }
-cudaError_t cudaEventRecord(cudaEvent_t, cudaStream_t) { return cudaErrorUnknown; }
+cudaError_t cudaEventElapsedTime(float *ms, cudaEvent_t, cudaEvent_t) {
+    *ms = 1.0f;
+    return cudaSuccess;
+}
+cudaError_t cudaEventRecord(cudaEvent_t, cudaStream_t) { return cudaSuccess; }
 cudaError_t cudaEventRecordWithFlags(cudaEvent_t, cudaStream_t, unsigned) { return cudaErrorUnknown; }
 cudaError_t cudaStreamCreateWithFlags(cudaStream_t *, unsigned) { return cudaErrorUnknown; }
 cudaError_t cudaStreamIsCapturing(cudaStream_t, cudaStreamCaptureStatus *s) {

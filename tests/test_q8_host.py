@@ -121,3 +121,37 @@ def test_step_after_a_failure(loaded):
     lib.fake_refuse_occupancy(1)
     assert step(lib, [1000])[0] != OK
     assert step(lib, [1000])[0] == OK
+
+
+def test_timing_counts_every_launch(lib):
+    """The launches that the timing of a kind reports are those that were made."""
+    def counted(call):
+        lib.dstd_timing_enable(1)
+        before = lib.fake_launches()
+        assert call() == OK
+        ms, n, total = ctypes.c_float(), ctypes.c_int64(), 0
+        for k in range(lib.dstd_kernel_kind_count()):
+            assert lib.dstd_timing_read(k, ctypes.byref(ms), ctypes.byref(n)) == OK
+            total += n.value
+        lib.dstd_timing_enable(0)
+        return total, lib.fake_launches() - before
+
+    def clip(sizes):
+        g, n, ty = tensor_list(sizes)
+        return lib.dstd_clip_grads(len(sizes), g, g, n, ty, 1.0, P, P, lib.dstd_grad_norm_workspace_bytes(len(sizes), n), None)
+
+    def norm(sizes):
+        g, n, ty = tensor_list(sizes)
+        return lib.dstd_grad_norm(len(sizes), g, n, ty, P, None, P, lib.dstd_grad_norm_workspace_bytes(len(sizes), n), None)
+
+    made = []
+    for call in (lambda: product(lib, 0, 64, 64), lambda: product(lib, 2, 64, 64), lambda: product(lib, 4096, 4096, 4096),
+                 lambda: lib.dstd_quantize_rows(P, 0, 0, 16, 16, P, 16, P, None, 0, None),
+                 lambda: lib.dstd_quantize_rows(P, 0, 3, 16, 16, P, 16, P, None, 0, None),
+                 lambda: norm([100]), lambda: norm([100] * 600), lambda: clip([100]), lambda: clip([1 << 20]),
+                 lambda: clip([100] * 600), lambda: step(lib, [1 << 20])[0], lambda: step(lib, [1 << 25])[0],
+                 lambda: step(lib, [10] * 1100)[0]):
+        total, launched = counted(call)
+        assert total == launched
+        made.append(launched)
+    assert made == [0, 1, 2, 0, 1, 1, 2, 1, 2, 4, 1, 2, 6]
