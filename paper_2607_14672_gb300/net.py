@@ -50,6 +50,15 @@ class Clipped:
                             self.adam_state, max_norm, self.grad_norm, self.clip_workspace, stream=stream)
 
 
+    def optimizer_launches(self):
+        """Kernels of one ``optimizer`` call: one for all layers; of a clipped
+        step one up to 2^24 weights in up to 512 tensors, else the norm and the
+        update for every 512 tensors (as dstd_adamw_clip takes them)."""
+        if self.max_norm is None or (len(self.W) <= 512 and sum(w.numel() for w in self.W) <= 1 << 24):
+            return 1
+        return 2 * ((len(self.W) + 511) // 512)
+
+
 class DenseNet(Clipped):
     """A stack of dense DSTD layers (configs.py layer dicts) on one GPU.
 
@@ -214,7 +223,7 @@ class DenseNet(Clipped):
             if l > 0:                             # bwd input times: prep W^T + dS gemm [+ gather]
                 n += 2 if tc else 3
         if self.with_adamw:
-            n += 1                                # one AdamW launch for all layers
+            n += self.optimizer_launches()
         return n
 
 

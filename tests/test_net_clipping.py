@@ -45,3 +45,17 @@ def test_networks_with_an_optimiser_are_built_on_any_device(kind):
         else:
             n = net.ConvNet(configs.config4(batch=2, M=8), device="cpu", max_norm=max_norm)
         assert len(n.m) == len(n.W) and n.clip_workspace.numel() > 64 and not n.clip_workspace.any()
+
+
+def test_launches_of_a_step_with_a_long_clipped_update():
+    """A step of more than 2^24 weights forms its norm in a launch of its own."""
+    from paper_2607_14672_gb300 import build, configs
+    try:
+        build.build()
+    except RuntimeError:
+        pytest.skip("the library does not build here")
+    cfg = configs.config2(batch=4, M=8)
+    cfg["layers"] = [dict(cfg["layers"][0], W=torch.zeros(4160, 4096).numpy())]
+    plain, clipped = (net.DenseNet(cfg, "x3", device="cpu", with_adamw=True, max_norm=c).launches_per_step()
+                      for c in (None, 0.5))
+    assert clipped == plain + 1

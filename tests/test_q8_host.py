@@ -155,3 +155,21 @@ def test_timing_counts_every_launch(lib):
         assert total == launched
         made.append(launched)
     assert made == [0, 1, 2, 0, 1, 1, 2, 1, 2, 4, 1, 2, 6]
+
+
+@pytest.mark.parametrize("sizes", [(64,), (1 << 24,), ((1 << 24) - 7, 7), ((1 << 24) - 7, 8), (1 << 26, 5), (3,) * 512,
+                                   (3,) * 513, (3,) * 1025])
+def test_networks_count_the_launches_of_a_clipped_step(lib, sizes):
+    """DenseNet.launches_per_step counts the optimiser's launches as the library makes them."""
+    from paper_2607_14672_gb300 import net
+
+    class Sized:
+        def __init__(self, n):
+            self.numel = lambda: n
+
+    stub = net.Clipped()
+    stub.W, stub.max_norm = [Sized(n) for n in sizes], 0.5
+    code, made = step(lib, list(sizes))
+    assert code == OK and stub.optimizer_launches() == len(made)
+    stub.max_norm = None
+    assert stub.optimizer_launches() == 1
