@@ -1153,21 +1153,21 @@ cudaLaunchConfig_t tc_config(cudaLaunchAttribute (&attr)[2]) {
     return cfg;
 }
 
-// Kernel attributes of a tile width. The grant of shared memory belongs to the
-// device that is current, so it is made at every launch.
+// Kernel attributes of a tile width: the grant of shared memory belongs to the
+// device that is current. False on an error.
 template <int NT>
-cudaError_t tc_setup() {
+bool tc_setup() {
     using C = Q8Cfg<NT>;
-    const cudaError_t e = cudaFuncSetAttribute(k_q8_tc<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
-    if (e != cudaSuccess || !C::SPLIT_REGS) return e;
-    // a split of more registers than the block has would wait forever
-    static PerDevice registers;
-    const int regs = registers.get([](int) {
+    static PerDevice done;
+    return done.get([](int) {
+        if (cudaFuncSetAttribute(k_q8_tc<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess)
+            return 0;
+        if (!C::SPLIT_REGS) return 1;
+        // a split of more registers than the block has would wait forever
         cudaFuncAttributes at;
-        return cudaFuncGetAttributes(&at, k_q8_tc<NT>) == cudaSuccess ? at.numRegs : 0;
-    });
-    return regs * TC_THREADS < REGS_SUM || regs < REGS_CONV || regs > REGS_EPI ? cudaErrorInvalidConfiguration
-                                                                               : cudaSuccess;
+        if (cudaFuncGetAttributes(&at, k_q8_tc<NT>) != cudaSuccess) return 0;
+        return at.numRegs * TC_THREADS >= REGS_SUM && at.numRegs >= REGS_CONV && at.numRegs <= REGS_EPI ? 1 : 0;
+    }) != 0;
 }
 
 // SM pairs that can be at work at once (0: an error); every tile width takes a whole SM
@@ -1179,7 +1179,7 @@ int resident_pairs() {
         cfg.gridDim = dim3(2 * kPairs);
         cfg.numAttrs = 1;
         int n = 0;
-        if (tc_setup<192>() != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, k_q8_tc<192>, &cfg) != cudaSuccess)
+        if (!tc_setup<192>() || cudaOccupancyMaxActiveClusters(&n, k_q8_tc<192>, &cfg) != cudaSuccess)
             return 0;
         return std::min(n, kPairs);
     });
@@ -1187,8 +1187,7 @@ int resident_pairs() {
 
 template <int NT>
 cudaError_t launch_tc(const Q8Args &q, const Q8Plan &p, const Q8Scratch &s, int pairs, cudaStream_t st) {
-    cudaError_t e = tc_setup<NT>();
-    if (e != cudaSuccess) return e;
+    if (!tc_setup<NT>()) return cudaErrorInvalidConfiguration;
     CUtensorMap map_w, map_x;
     const bool copied = !w_rows_aligned(q);
     if (!row_map(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, copied ? s.w : q.w, q.N, q.K, copied ? s.ld_w : q.ld_w, 128) ||
