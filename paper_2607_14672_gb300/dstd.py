@@ -388,23 +388,35 @@ def adamw_multi(ws, gs, ms, vs, lr, beta1, beta2, eps, weight_decay, step, lr_de
 _TORCH = None       # torch, once one of these calls has needed it
 _CODES = {}         # torch dtype -> dstd_type
 _RAW_STREAM = None  # device index -> the current stream's handle
+_DEVICE = None      # index of the current device
+_ONLY = -2          # 0 where there is one device: it is the current one
 
 
 def _torch():
-    global _TORCH, _RAW_STREAM
+    global _TORCH, _RAW_STREAM, _DEVICE, _ONLY
     if _TORCH is None:
         import torch
         _CODES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
         _RAW_STREAM = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda index: torch.cuda.current_stream(index).cuda_stream)
+        _DEVICE = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+        _ONLY = 0 if torch.cuda.device_count() == 1 else -2
         _TORCH = torch
     return _TORCH
 
 
-def _stream_of(stream, x):
-    """The stream to launch on: the given one, or the current one of x's device."""
+def _here(x, dev, name):
+    """Refuses x of device dev unless that is the current one: kernels run there,
+    and another device's memory is out of their reach. The other tensors of a
+    call are checked against dev. (With one device there is nothing to ask.)"""
+    if dev < 0 or dev != _DEVICE():
+        raise ValueError(f"{name} must be a tensor on the current CUDA device, not on {x.device}")
+
+
+def _stream_of(stream, dev):
+    """The stream to launch on: the given one, or the device's current one."""
     if stream is None:
-        return _RAW_STREAM(x.get_device())
+        return _RAW_STREAM(dev)
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -416,27 +428,27 @@ def _type_code(dtype, name):
     return code
 
 
-def _rows(x, name, R, K, dtype=None):
-    """Row stride of a CUDA matrix [R, K] whose rows are contiguous (they may be padded, not overlap)."""
-    if x.shape == (R, K) and x.is_cuda and (dtype is None or x.dtype == dtype):
+def _rows(x, name, R, K, dev, dtype=None):
+    """Row stride of a matrix [R, K] on the device whose rows are contiguous (they may be padded, not overlap)."""
+    if x.shape == (R, K) and x.get_device() == dev and (dtype is None or x.dtype == dtype):
         ld, one = x.stride()
         if (one == 1 or K <= 1) and ld >= K:
             return ld
         if (one == 1 or K <= 1) and R <= 1:
             return K
         raise ValueError(f"{name} must have contiguous rows that do not overlap")
-    raise ValueError(f"{name} must be a CUDA matrix of shape {(R, K)}" +
+    raise ValueError(f"{name} must be a matrix of shape {(R, K)} on cuda:{dev}" +
                      (f" and {dtype}" if dtype is not None else "") + f", not {tuple(x.shape)}, {x.dtype}, {x.device}")
 
 
-def _floats(x, name, n):
-    if x.shape != (n,) or x.dtype != _TORCH.float32 or not x.is_cuda or (n > 1 and x.stride(0) != 1):
-        raise ValueError(f"{name} must be a contiguous CUDA float32 tensor of {n}")
+def _floats(x, name, n, dev):
+    if x.shape != (n,) or x.dtype != _TORCH.float32 or x.get_device() != dev or (n > 1 and x.stride(0) != 1):
+        raise ValueError(f"{name} must be a contiguous float32 tensor of {n} on cuda:{dev}")
 
 
-def _scratch(ws, where):
-    if not ws.is_cuda or not ws.is_contiguous():
-        raise ValueError(f"{where}: workspace must be a contiguous CUDA tensor")
+def _scratch(ws, where, dev):
+    if ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError(f"{where}: workspace must be a contiguous tensor on cuda:{dev}")
     return ws.numel() * ws.element_size()
 
 
@@ -447,14 +459,17 @@ def quantize_rows(x, q, scale, values=None, stream=None):
     not finite gets scale NaN. Rows may be padded."""
     torch = _torch()
     R, K = x.shape
-    ld_x = _rows(x, "x", R, K)
-    ld_q = _rows(q, "q", R, K, torch.int8)
-    _floats(scale, "scale", R)
+    dev = x.get_device()
+    if dev != _ONLY:
+        _here(x, dev, "x")
+    ld_x = _rows(x, "x", R, K, dev)
+    ld_q = _rows(q, "q", R, K, dev, torch.int8)
+    _floats(scale, "scale", R, dev)
     ld_v, v = 0, None
     if values is not None:
-        ld_v, v = _rows(values, "values", R, K, torch.float32), values.data_ptr()
+        ld_v, v = _rows(values, "values", R, K, dev, torch.float32), values.data_ptr()
     code = load().dstd_quantize_rows(x.data_ptr(), _type_code(x.dtype, "x"), R, K, ld_x, q.data_ptr(), ld_q,
-                                     scale.data_ptr(), v, ld_v, _stream_of(stream, x))
+                                     scale.data_ptr(), v, ld_v, _stream_of(stream, dev))
     if code:
         raise DstdError(code, "dstd_quantize_rows")
 
@@ -474,14 +489,17 @@ def int8_matmul(x, x_scale, w, w_scale, out, workspace, stream=None):
     torch = _torch()
     T, K = x.shape
     N = w.shape[0]
-    ld_x = _rows(x, "x", T, K, torch.int8)
-    ld_w = _rows(w, "w", N, K, torch.int8)
-    ld_out = _rows(out, "out", T, N)
-    _floats(x_scale, "x_scale", T)
-    _floats(w_scale, "w_scale", N)
+    dev = x.get_device()
+    if dev != _ONLY:
+        _here(x, dev, "x")
+    ld_x = _rows(x, "x", T, K, dev, torch.int8)
+    ld_w = _rows(w, "w", N, K, dev, torch.int8)
+    ld_out = _rows(out, "out", T, N, dev)
+    _floats(x_scale, "x_scale", T, dev)
+    _floats(w_scale, "w_scale", N, dev)
     code = load().dstd_int8_matmul(x.data_ptr(), ld_x, x_scale.data_ptr(), w.data_ptr(), ld_w, w_scale.data_ptr(), T,
                                    N, K, out.data_ptr(), _type_code(out.dtype, "out"), ld_out, workspace.data_ptr(),
-                                   _scratch(workspace, "int8_matmul"), _stream_of(stream, x))
+                                   _scratch(workspace, "int8_matmul", dev), _stream_of(stream, dev))
     if code:
         raise DstdError(code, "dstd_int8_matmul")
 
@@ -500,12 +518,17 @@ def dense_fwd_q8(t_in, w_q, w_scale, p, t_out, saved, penalty, workspace, stream
     _f32(t_in, "t_in")
     _f32(w_scale, "w_scale", (N_out,))
     _f32(t_out, "t_out", (B, N_out))
-    if w_q.dtype != torch.int8 or not w_q.is_cuda or not w_q.is_contiguous() or tuple(w_q.shape) != (N_out, N_in):
-        raise ValueError("w_q must be a contiguous CUDA int8 tensor [N_out, N_in]")
+    dev = t_in.get_device()
+    if dev != _ONLY:
+        _here(t_in, dev, "t_in")
+    if w_scale.get_device() != dev or t_out.get_device() != dev:
+        raise ValueError(f"w_scale and t_out must be on cuda:{dev}")
+    if w_q.dtype != torch.int8 or w_q.get_device() != dev or not w_q.is_contiguous() or tuple(w_q.shape) != (N_out, N_in):
+        raise ValueError(f"w_q must be a contiguous int8 tensor [N_out, N_in] on cuda:{dev}")
     _check(load().dstd_dense_fwd_q8(t_in.data_ptr(), w_q.data_ptr(), w_scale.data_ptr(), B, N_in, N_out,
                                     ctypes.byref(p), t_out.data_ptr(), _ptr(saved), _ptr(penalty),
-                                    workspace.data_ptr(), _scratch(workspace, "dense_fwd_q8"),
-                                    _stream_of(stream, t_in)), "dstd_dense_fwd_q8")
+                                    workspace.data_ptr(), _scratch(workspace, "dense_fwd_q8", dev),
+                                    _stream_of(stream, dev)), "dstd_dense_fwd_q8")
 
 
 class TensorList:
@@ -519,6 +542,10 @@ class TensorList:
         for i, t in enumerate(self.tensors):
             if not t.is_cuda or not t.is_contiguous():
                 raise ValueError(f"tensor {i} of the list must be a contiguous CUDA tensor")
+        devices = set(t.get_device() for t in self.tensors)
+        if len(devices) > 1:
+            raise ValueError("the tensors of a list must be on one device")
+        self.device = devices.pop() if devices else None
         k = len(self.tensors)
         self.sizes = tuple(t.numel() for t in self.tensors)
         self.codes = tuple(_type_code(t.dtype, f"tensor {i} of the list") for i, t in enumerate(self.tensors))
@@ -535,6 +562,10 @@ def _list(x):
     return x if isinstance(x, TensorList) else TensorList(x)
 
 
+def _elsewhere(dev, where):
+    raise ValueError(f"{where}: the lists' tensors must be on cuda:{dev}")
+
+
 def grad_norm_workspace_bytes(gs):
     """Bytes of the workspace that grad_norm, clip_grads and adamw_clip share
     for these gradients: a tensor of zeros at first, left ready by each call.
@@ -548,11 +579,16 @@ def grad_norm(gs, norm, workspace, tensor_norms=None, stream=None):
     float16 tensors, or a TensorList); tensor_norms [len(gs)]: of each."""
     _torch()
     gs = _list(gs)
-    _floats(norm, "norm", 1)
+    dev = norm.get_device()
+    if dev != _ONLY:
+        _here(norm, dev, "norm")
+    if gs.device not in (dev, None):
+        _elsewhere(dev, "grad_norm")
+    _floats(norm, "norm", 1, dev)
     if tensor_norms is not None:
-        _floats(tensor_norms, "tensor_norms", len(gs.sizes))
+        _floats(tensor_norms, "tensor_norms", len(gs.sizes), dev)
     code = load().dstd_grad_norm(len(gs.sizes), gs.ptr, gs.n, gs.type, norm.data_ptr(), _ptr(tensor_norms),
-                                 workspace.data_ptr(), _scratch(workspace, "grad_norm"), _stream_of(stream, norm))
+                                 workspace.data_ptr(), _scratch(workspace, "grad_norm", dev), _stream_of(stream, dev))
     if code:
         raise DstdError(code, "dstd_grad_norm")
 
@@ -567,9 +603,14 @@ def clip_grads(gs, max_norm, norm, workspace, outs=None, stream=None):
     outs = gs if outs is None else _list(outs)
     if gs.sizes != outs.sizes or gs.codes != outs.codes:
         raise ValueError("clip_grads: outs must have the gradients' sizes and types")
-    _floats(norm, "norm", 1)
+    dev = norm.get_device()
+    if dev != _ONLY:
+        _here(norm, dev, "norm")
+    if not (gs.device == outs.device and gs.device in (dev, None)):
+        _elsewhere(dev, "clip_grads")
+    _floats(norm, "norm", 1, dev)
     code = load().dstd_clip_grads(len(gs.sizes), gs.ptr, outs.ptr, gs.n, gs.type, max_norm, norm.data_ptr(),
-                                  workspace.data_ptr(), _scratch(workspace, "clip_grads"), _stream_of(stream, norm))
+                                  workspace.data_ptr(), _scratch(workspace, "clip_grads", dev), _stream_of(stream, dev))
     if code:
         raise DstdError(code, "dstd_clip_grads")
 
@@ -588,14 +629,21 @@ def adamw_clip(ws, gs, ms, vs, lr, beta1, beta2, eps, weight_decay, step, max_no
         raise ValueError("adamw_clip: tensor lists differ in length or sizes")
     if not (ws.f32 and ms.f32 and vs.f32):
         raise ValueError("adamw_clip: weights and moments must be float32")
-    if step.dtype != torch.int32 or step.numel() < 1 or not step.is_cuda:
-        raise ValueError("adamw_clip: step must be a device int32 tensor")
+    dev = norm.get_device()
+    if dev != _ONLY:
+        _here(norm, dev, "norm")
+    if not (ws.device == gs.device == ms.device == vs.device and gs.device in (dev, None)):
+        _elsewhere(dev, "adamw_clip")
+    if step.dtype != torch.int32 or step.numel() < 1 or step.get_device() != dev:
+        raise ValueError(f"adamw_clip: step must be an int32 tensor on cuda:{dev}")
     if lr_dev is not None:
         _f32(lr_dev, "lr_dev")
-    _floats(norm, "norm", 1)
+        if lr_dev.get_device() != dev:
+            raise ValueError(f"adamw_clip: lr_dev must be on cuda:{dev}")
+    _floats(norm, "norm", 1, dev)
     code = load().dstd_adamw_clip(len(gs.sizes), ws.ptr, gs.ptr, ms.ptr, vs.ptr, gs.n, gs.type, lr, beta1, beta2, eps,
                                   weight_decay, max_norm, step.data_ptr(), _ptr(lr_dev), norm.data_ptr(),
-                                  workspace.data_ptr(), _scratch(workspace, "adamw_clip"), _stream_of(stream, norm))
+                                  workspace.data_ptr(), _scratch(workspace, "adamw_clip", dev), _stream_of(stream, dev))
     if code:
         raise DstdError(code, "dstd_adamw_clip")
 
