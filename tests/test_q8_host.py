@@ -3,10 +3,12 @@ the ends of the ranges, and what is launched (through a runtime that runs
 nothing, see fake_cuda.cpp)."""
 
 import ctypes
+import struct
 
 import pytest
 
 import fake_cuda
+from q8_plans import PLANS, row_stride
 
 pytestmark = pytest.mark.skipif(fake_cuda.compiler() is None, reason="no C++ compiler")
 
@@ -173,3 +175,53 @@ def test_networks_count_the_launches_of_a_clipped_step(lib, sizes):
     assert code == OK and stub.optimizer_launches() == len(made)
     stub.max_norm = None
     assert stub.optimizer_launches() == 1
+
+
+def plan(lib, T, N, K):
+    """Width, form of the work and whether the sides are exchanged, from the tensor-core launch's own argument:
+    T, N, K, two truth values (weights copied, sides exchanged), then the plan's width, tiles along N and T,
+    blocks of K, whole tiles, and blocks of a share of the others."""
+    lib.fake_keep_arg2_of(b"k_q8_tc")
+    assert product(lib, T, N, K, ld=row_stride(K)) == OK
+    name, grid, _, _ = fake_cuda.launches(lib)[-1]
+    assert "k_q8_tc" in name
+    a = bytes(lib.fake_arg2(lib.fake_launches() - 1).contents)
+    t, n, k, copied, exchanged, nt, tiles_n, tiles_t, blocks, whole, share = struct.unpack("3i2?2x6i", a[:40])
+    assert (t, n, k) == ((N, T, K) if exchanged else (T, N, K)) and not copied
+    assert f"ILi{nt}E" in name
+    tiles = tiles_n * tiles_t
+    assert tiles == -(-n // 256) * -(-t // nt) and blocks == -(-k // 128) and 0 <= whole <= tiles
+    assert (share > 0) == (whole < tiles)
+    if share:
+        assert share * (grid // 2) >= (tiles - whole) * blocks     # the shares cover what is cut
+    return nt, "one piece" if not share else ("whole and cut" if whole else "cut"), exchanged
+
+
+@pytest.mark.parametrize("T,N,K,nt,form,exchanged", PLANS)
+def test_plans_of_the_tested_shapes(lib, T, N, K, nt, form, exchanged):
+    """The shapes whose results are compared on the GPU reach what they are there for."""
+    assert plan(lib, T, N, K) == (nt, form, exchanged)
+
+
+def test_every_width_is_tested_in_every_form():
+    assert {p[3:] for p in PLANS} == {(nt, form, exchanged) for nt in (32, 64, 96, 128, 160, 192)
+                                      for form in ("one piece", "cut", "whole and cut") for exchanged in (False, True)}
+
+
+@pytest.mark.parametrize("B,N_in,N_out,M,writers,tc,exchanged", [
+    (2, 5000, 60, 16, 2, True, False), (2, 9001, 40, 32, 3, True, True), (2, 16384, 50, 8, 4, True, False),
+    (64, 300, 21, 32, 1, True, True), (128, 2000, 40, 32, 1, False, None), (64, 1500, 130, 32, 1, True, True)])
+def test_launches_of_the_tested_layers(lib, B, N_in, N_out, M, writers, tc, exchanged):
+    """The layers whose spike times are compared on the GPU reach several blocks a sample of the token writer, both
+    forms of the product, and either side first."""
+    from paper_2607_14672_gb300 import dstd
+    p = dstd.params(dict(tau_v=0.5, tau_I=0.25, v_th=1.0, t_first=0.0, t_end=1.2, M=M, t_offset=0.0), 1.0 / B)
+    lib.fake_keep_arg2_of(b"k_q8_tc")
+    need = lib.dstd_dense_q8_workspace_bytes(B, N_in, N_out, ctypes.byref(p))
+    assert lib.dstd_dense_fwd_q8(P, P, P, B, N_in, N_out, ctypes.byref(p), P, P, None, P, need, None) == OK
+    names = fake_cuda.launches(lib)
+    assert "k_bin_codes" in names[0][0] and names[0][1] == writers
+    where = [i for i, n in enumerate(names) if "k_q8_tc" in n[0]]
+    assert bool(where) == tc
+    if tc:
+        assert struct.unpack("2?", bytes(lib.fake_arg2(where[0]).contents)[12:14])[1] == exchanged
