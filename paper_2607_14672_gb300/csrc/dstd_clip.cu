@@ -2,8 +2,9 @@
 // global norm, clipping by it, and the clipped AdamW update. All of it is bound
 // by memory: the norm has to be known before the first gradient is scaled, so
 // gradients are read twice, the second time from L2 as far as they fit. Long
-// lists (us): norm of 268 M bf16 gradients 78 (6.9 TB/s), clipped copies 255 (6.3
-// TB/s over three passes), their AdamW step 1205 (6.2 TB/s with both reads).
+// lists (us a call among others): norm of 268 M bf16 gradients 83 (6.5 TB/s),
+// clipped copies 274 (5.9 TB/s over three passes), their AdamW step 1229 (6.1 TB/s
+// with both reads).
 #include "dstd_internal.cuh"
 
 #include <math.h>

@@ -34,7 +34,8 @@ cudaError_t launch_dependent(void (*kernel)(P...), unsigned grid, unsigned block
 // Row quantiser. With a = max_k |x_k|:
 //     scale = a / 127,  q_k = rint(x_k (127 (1 / a))),  value_k = q_k scale,
 // each operation rounded to fp32 (three roundings move x 127 / a by less than
-// 127 * 3 * 2^-24 code steps). 1 / a overflows for a below 2^-128; rows of
+// 127 * 3 * 2^-24 code steps; above a = 2^126, where 1 / a is subnormal, by less
+// than twice that). 1 / a overflows for a below 2^-128; rows of
 // very small a are multiplied by 2^64 first (exact), which gives the same codes.
 // A row of zeros has scale 0; a row that holds an infinity or a NaN has scale
 // NaN and codes 0, so that whatever is computed from it is NaN. The largest |x|
@@ -100,7 +101,7 @@ struct QuantArgs {
 // A thread has up to 4 or 8 of these loads under way, and a block's threads are
 // few enough for several rows to be on an SM (4153 rows of 4480 16-bit elements:
 // 13 us; with 512 threads a row and one load each 21 us). HBM bounds it: 16384 x
-// 16384 fp32 with values in 341 us, 7.1 TB/s.
+// 16384 fp32 with values in 345 us, 7.0 TB/s.
 template <class T, bool PACKED, int L, int THREADS, int BLOCK = THREADS == 32 ? 256 : THREADS>
 __global__ void __launch_bounds__(BLOCK, THREADS == 32 ? 1 : (BLOCK == 1024 ? 2 : (L == 8 ? 1024 : 1536) / BLOCK)) k_quantize_rows(const T *__restrict__ x, const QuantArgs a) {
     constexpr int P = PACKED ? Pack<T>::P : 1;
@@ -189,7 +190,9 @@ __global__ void __launch_bounds__(BLOCK, THREADS == 32 ? 1 : (BLOCK == 1024 ? 2 
 
 // rows too long for the registers: read twice (the second time mostly from L2).
 // Columns are counted without a sign: a row may have up to 2^31 - 1 of them, and
-// the count passes that by a step before the loop ends.
+// the count passes that by a step before the loop ends. One element a load, so
+// neither the loads nor HBM are used fully: 1024 rows of 40000 fp32 with values in
+// 97 us (3.8 TB/s), 8192 rows of 32768 bf16 in 245 us (3.3 TB/s).
 template <class T>
 __global__ void __launch_bounds__(256) k_quantize_long(const T *__restrict__ x, const QuantArgs a) {
     __shared__ unsigned s_top[8];
@@ -429,7 +432,7 @@ __device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t &lo, uint32_t
 // A block has 16 channels and 8 NT tokens; its warps (1 to 8) share K in blocks
 // of 128 codes (whole 128-byte lines): as many as fit the GPU in one round of
 // blocks, so that there are loads enough under way and no second, half-empty round.
-// Memory bounds it: 8 tokens x 16384 x 16384 in 48 us, 5.6 TB/s of weights (two
+// Memory bounds it: 8 tokens x 16384 x 16384 in 47 us, 5.7 TB/s of weights (two
 // blocks' loads under way per warp took registers from other warps: 57 us). Small
 // layers are bound by the launch: 16 tokens x 784 x 800 in about 2.5 us.
 // ---------------------------------------------------------------------------
@@ -591,9 +594,9 @@ cudaError_t launch_few(const Q8Args &a, bool aligned, cudaStream_t st) {
 // workspace with atomics, and the last one of a part (a ticket counts them)
 // stores the result. Whole-number sums do not depend on the order.
 // The tensor pipe bounds large products: 4096 x 16384 x 16384 in 1.09 ms, 2.0
-// PFLOP/s (cuBLAS bf16 burst: 1.91); 4096^3 in 90 us (the pipe is active 82% of
-// the time at 4096 x 4096 x 8192; the rest are the pipeline's ends and the last
-// round). Small ones are bound by the pipeline's ends, about 8 us from launch to
+// PFLOP/s, with the preparation 1.17 (cuBLAS bf16 burst: 1.91 PFLOP/s); 4096^3 in
+// 97 us as a call with cold caches (the pipe is active 82% of the time at 4096 x
+// 4096 x 8192; the rest are the pipeline's ends and the last round). Small ones are bound by the pipeline's ends, about 8 us from launch to
 // the last store.
 // ---------------------------------------------------------------------------
 __device__ unsigned int g_status_q8 = 0;
@@ -1046,8 +1049,8 @@ constexpr int kTcMinTokens = 9;
 // Time of one block of 128 codes in a pair's pipeline, in cycles, measured with
 // 4096 tokens, 16384 inputs and channels (the MMAs alone: 4 nt). The conversion
 // and the issue of the MMAs hold it at about 700 up to 128 tokens a tile; 160
-// reach the tensor pipe's rate (1.22 ms); with 192 only two blocks fit beside the
-// accumulators in TMEM (1.30 ms).
+// reach the tensor pipe's rate (that product's call in 1.17 ms); with 192 only two
+// blocks fit beside the accumulators in TMEM (1.19 ms).
 struct TileCost {
     int nt, block;
 };
