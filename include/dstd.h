@@ -515,6 +515,108 @@ int dstd_adamw_clip(int count, float *const *w, const void *const *g, float *con
                     double weight_decay, double max_norm, int32_t *step, const float *lr_dev, float *norm,
                     void *workspace, size_t ws_bytes, dstd_stream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Training and serving in 4 bits
+ *
+ * A layer's contraction w^ = W s on the part's 4-bit tensor cores: rows of
+ * weights (channels) and of grid weights (tokens) as codes of
+ * {0, 0.5, 1, 1.5, 2, 3, 4, 6} with a sign (E2M1), with a power of two for each
+ * block of 32 columns of a row. Training passes the gradient straight through
+ * the rounding, as for 8 bits. (The paper trains in floating point.)
+ *
+ * Layout. blocks = ceil(cols / 32).
+ *  codes   a row is 16 blocks bytes: the even column in a byte's low half, zero
+ *          beyond the last column; rows start at multiples of 16 bytes (base
+ *          address and ld_*, which is in bytes).
+ *  scales  exponents plus 127 in bytes (255: NaN), in tiles of 128 rows by 4
+ *          blocks of 512 bytes: block b of row r is byte
+ *              ((r / 128) ceil(blocks / 4) + b / 4) 512 + (r % 32) 16 + (r % 128 / 32) 4 + b % 4
+ *          of dstd_mx4_scale_bytes(rows, cols) bytes, at a multiple of 16. Bytes
+ *          of blocks past the last are 0; those of rows past the last may be
+ *          anything.
+ * No columns, no rows or no tokens are valid.
+ * ------------------------------------------------------------------------- */
+size_t dstd_mx4_scale_bytes(int rows, int cols); /* 0 for negative sizes */
+
+/* Rows to 4 bits. Of each block, e = the least whole number >= -127 with
+ * max |x| <= 6 2^e; code = x 2^-e to the nearest, ties to the even code (0, 1, 2, 4);
+ * value = code 2^e, in fp32 (infinite where |x| >= 3.5 2^126 went up to 2^128). A block that holds an infinity or a NaN has scale
+ * NaN and codes 0, so that every result computed from it is NaN.
+ *  x       [rows, cols] of `type`, row stride ld_x >= cols (elements).
+ *  q       [rows] rows of codes out, row stride ld_q (bytes).
+ *  scale   out (all bytes of blocks past the last too).
+ *  values  [rows, cols] fp32 out, row stride ld_values >= cols (may be NULL).
+ * The outputs must not overlap x. */
+int dstd_quantize_mx4(const void *x, dstd_type type, int rows, int cols, int64_t ld_x, uint8_t *q, int64_t ld_q,
+                      uint8_t *scale, float *values, int64_t ld_values, dstd_stream_t stream);
+
+/* Product of 4-bit rows: out_tn = sum_k x_tk w_nk over the values of the codes.
+ * Products are exact, sums in fp32 (a sum below fp32's normal numbers may be
+ * lost), rounded once more to a 16-bit out_type. No order of work depends on
+ * anything but the sizes: the same call gives the same bits.
+ *  x, x_scale  T rows of K columns in the layout above; w, w_scale N rows.
+ *  K = 0 gives zeros. T, N, K at most 2^31 - 256.
+ *  out [T, N] of out_type, row stride ld_out >= N (elements); overlaps no input. */
+int dstd_mx4_matmul(const uint8_t *x, int64_t ld_x, const uint8_t *x_scale, const uint8_t *w, int64_t ld_w,
+                    const uint8_t *w_scale, int T, int N, int K, void *out, dstd_type out_type, int64_t ld_out,
+                    dstd_stream_t stream);
+
+/* Workspace bytes of dstd_dense_fwd_mx4; 0 on invalid arguments. */
+size_t dstd_dense_mx4_workspace_bytes(int B, int N_in, int N_out, const dstd_params *p);
+
+/* dstd_dense_fwd with the contraction in 4 bits: binning, the grid weights of
+ * each (sample, grid point) quantised, the 4-bit product with the weights' codes,
+ * scan/solve/select in fp32.
+ *  w_q  N_out rows of codes of N_in columns, 16 ceil(N_in / 32) bytes apart, and
+ *  w_scale, as from dstd_quantize_mx4; the other arguments as in dstd_dense_fwd.
+ *  M <= 128.
+ * The backward is dstd_dense_bwd with the weights' values. */
+int dstd_dense_fwd_mx4(const float *t_in, const uint8_t *w_q, const uint8_t *w_scale, int B, int N_in, int N_out,
+                       const dstd_params *p, float *t_out, void *saved, float *penalty, void *workspace,
+                       size_t ws_bytes, dstd_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Learning from a teacher
+ *
+ * The outputs y of a readout give logits factor y: spike times t give -t/tau_soft
+ * with factor = -1/tau_soft, as in dstd_ce_loss; y may as well hold logits. Where
+ * factor y is -infinity (a silent output, a masked class) the logit is
+ * factor silent, a constant that passes no gradient; with factor silent =
+ * -infinity such a class has no probability.
+ *  y [R, C] of `type`, row stride ld_y >= C (elements); any element alignment.
+ *  factor finite, not 0; factor silent not NaN or +infinity.
+ *  R, C >= 1; R at most 2^31 - 1, C at most 2^30.
+ * ------------------------------------------------------------------------- */
+
+/* The K largest logits of each row, descending, equal ones by ascending class: what
+ * is kept of a teacher. A NaN comes before all others.
+ *  top [R, K] fp32 out, index [R, K] int32 out; 1 <= K <= min(C, 256). */
+int dstd_top_logits(const void *y, dstd_type type, int R, int C, int64_t ld_y, float factor, float silent, int K,
+                    float *top, int32_t *index, dstd_stream_t stream);
+
+/* Distillation from a teacher's top logits, forward and backward. With
+ * q = softmax(factor y) over the C classes of a row and p = softmax(teacher_factor top)
+ * over its used entries (those whose class lies in [0, C) and whose logit is not
+ * -infinity; any number of them, the same class several times too):
+ *     row_loss_r = sum_k p_k (log p_k - log q_{index_k}),
+ *     loss[0] = weight sum_r w_r row_loss_r,   g = d loss[0] / dy.
+ * A row without used entries or logits, or with w_r = 0, has row_loss 0 and
+ * gradient 0. Infinite logits and NaN in a row (of the student or the teacher)
+ * make its loss NaN.
+ *  top [R, K] fp32, index [R, K] int32; 1 <= K <= 256.
+ *  row_weight [R] device floats w_r, or NULL for 1/R each.
+ *  loss  float[2], 8-byte aligned: loss[1] is scratch, zero before the first
+ *        call (each call leaves it zero); calls that can overlap need one each.
+ *  row_loss [R] out.
+ *  g     [R, C] of `type` out, row stride ld_g >= C, not overlapping y; NULL:
+ *        the losses alone. accumulate != 0 adds the gradient to what g holds.
+ * Sums are formed in fp32 (fp64 over rows) in a fixed order; each gradient is
+ * rounded once. */
+int dstd_distill_loss(const void *y, dstd_type type, int R, int C, int64_t ld_y, float factor, float silent,
+                      const float *top, const int32_t *index, int K, float teacher_factor, float weight,
+                      const float *row_weight, float *loss, float *row_loss, void *g, int64_t ld_g, int accumulate,
+                      dstd_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -90,12 +90,13 @@ inline int cu(cudaError_t e) { return e == cudaSuccess ? DSTD_OK : DSTD_E_CUDA; 
 enum Kind {
     KK_PREP = 0, KK_BIN, KK_BIN_T, KK_GEMM_FWD, KK_SCAN, KK_DWHAT, KK_GEMM_DS, KK_GT, KK_GEMM_DW, KK_REDUCE,
     KK_LOSS, KK_ADAMW, KK_BIN_PUB, KK_WHAT_PUB, KK_SELFTEST, KK_NARROW_FWD, KK_NARROW_BWD, KK_EXACT_FWD, KK_SKIP,
-    KK_EXACT_BWD, KK_QUANTIZE, KK_INT8, KK_CLIP, KK_COUNT
+    KK_EXACT_BWD, KK_QUANTIZE, KK_INT8, KK_CLIP, KK_QUANT4, KK_MX4, KK_TOP, KK_DISTILL, KK_COUNT
 };
 const char *const kKindNames[KK_COUNT] = {
     "prep_weights", "binning", "binning_T", "gemm_fwd_scan", "scan_solve", "dwhat", "gemm_dS_gradt",
     "gradt_gather", "gemm_dW", "dw_reduce", "loss", "adamw", "binning_public", "what_public", "selftest", "narrow_fwd",
-    "narrow_bwd", "exact_fwd", "skip_channels", "exact_bwd", "quantize_rows", "int8_matmul", "clip"};
+    "narrow_bwd", "exact_fwd", "skip_channels", "exact_bwd", "quantize_rows", "int8_matmul", "clip",
+    "quantize_mx4", "mx4_matmul", "top_logits", "distill"};
 
 struct Span {
     cudaEvent_t first, second;
@@ -1860,6 +1861,162 @@ int dstd_adamw_clip(int count, float *const *w, const void *const *g, float *con
     const ClipTensors t{count, g, reinterpret_cast<void *const *>(w), m, v, n, type};
     const ClipHyper h{max_norm, lr, beta1, beta2, eps, weight_decay, step, lr_dev};
     return cu(launch_clip(t, ClipOp::Adamw, h, norm, nullptr, workspace, tm.launches, (cudaStream_t)stream));
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// Training and serving in 4 bits, and learning from a teacher.
+// ---------------------------------------------------------------------------
+namespace {
+
+constexpr int kMx4Most = 0x7fffffff - 255;  // rows and columns of a product: whole tiles stay below 2^31
+
+int row_bytes(int cols) { return 16 * mx4_blocks(cols); }
+
+// layout of the 4-bit layer forward: the grid weights' codes and scales, w^ (D[i][(b, m)]), the weights' row sums
+struct Mx4Ws {
+    float *D = nullptr, *rowsum = nullptr;
+    uint8_t *q = nullptr, *scale = nullptr;
+    size_t bytes = 0;
+};
+Mx4Ws mx4_layout(void *base, int B, int N_in, int N_out, int Mp) {
+    Mx4Ws w;
+    Bump b(base);
+    const long long T = (long long)B * Mp;
+    w.rowsum = b.take<float>(N_out);
+    w.scale = b.take<uint8_t>(mx4_scale_bytes(T, N_in));
+    w.q = b.take<uint8_t>((size_t)T * row_bytes(N_in));
+    w.D = b.take<float>((size_t)T * N_out);
+    w.bytes = b.off;
+    return w;
+}
+int check_mx4_sizes(int B, int N_in, int N_out, const dstd_params *p) {
+    TRY(check_sizes(B, N_in, N_out));
+    TRY(check_params(p));
+    return padded_M(p->M) > 128 ? DSTD_E_UNSUPPORTED : DSTD_OK;
+}
+
+int check_logits(const void *y, dstd_type type, int R, int C, int64_t ld_y, float factor, float silent) {
+    if (!y || !type_ok(type) || R < 1 || C < 1 || ld_y < C || !aligned_to(y, type_bytes(type))) return DSTD_E_INVALID;
+    if (!isfinite(factor) || factor == 0.0f) return DSTD_E_INVALID;
+    const float none = factor * silent;
+    if (isnan(none) || none == INFINITY) return DSTD_E_INVALID;
+    return C > (1 << 30) ? DSTD_E_UNSUPPORTED : DSTD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t dstd_mx4_scale_bytes(int rows, int cols) {
+    return rows < 0 || cols < 0 ? 0 : mx4_scale_bytes(rows, cols);
+}
+
+int dstd_quantize_mx4(const void *x, dstd_type type, int rows, int cols, int64_t ld_x, uint8_t *q, int64_t ld_q,
+                      uint8_t *scale, float *values, int64_t ld_values, dstd_stream_t stream) {
+    if (rows < 0 || cols < 0 || !type_ok(type)) return DSTD_E_INVALID;
+    if (rows > 0 && cols > 0) {
+        if (!x || !q || !scale || !aligned_to(x, type_bytes(type)) || !aligned16(q) || !aligned16(scale) || ld_x < cols)
+            return DSTD_E_INVALID;
+        if (ld_q < row_bytes(cols) || ld_q % 16 != 0) return DSTD_E_INVALID;
+        if (values && (!aligned_to(values, 4) || ld_values < cols)) return DSTD_E_INVALID;
+        if (rows > kMx4Most || cols > kMx4Most) return DSTD_E_UNSUPPORTED;
+    }
+    TRY(device_ok());
+    Timed tm(KK_QUANT4, (cudaStream_t)stream);
+    tm.launches = rows > 0 && cols > 0 ? 1 : 0;
+    return cu(launch_quantize_mx4(x, type, rows, cols, ld_x, q, ld_q, scale, values, ld_values,
+                                  (cudaStream_t)stream));
+}
+
+int dstd_mx4_matmul(const uint8_t *x, int64_t ld_x, const uint8_t *x_scale, const uint8_t *w, int64_t ld_w,
+                    const uint8_t *w_scale, int T, int N, int K, void *out, dstd_type out_type, int64_t ld_out,
+                    dstd_stream_t stream) {
+    if (T < 0 || N < 0 || K < 0 || !type_ok(out_type)) return DSTD_E_INVALID;
+    if (T > 0 && N > 0) {
+        if (!out || !aligned_to(out, type_bytes(out_type)) || ld_out < N) return DSTD_E_INVALID;
+        if (K > 0 && (!x || !w || !x_scale || !w_scale || !aligned16(x) || !aligned16(w) || !aligned16(x_scale) ||
+                      !aligned16(w_scale) || ld_x < row_bytes(K) || ld_w < row_bytes(K) || (ld_x | ld_w) % 16 != 0))
+            return DSTD_E_INVALID;
+        if (T > kMx4Most || N > kMx4Most || K > kMx4Most) return DSTD_E_UNSUPPORTED;
+    }
+    TRY(device_ok());
+    Timed tm(KK_MX4, (cudaStream_t)stream);
+    tm.launches = T > 0 && N > 0 ? 1 : 0;
+    const Mx4Args a{x, w, ld_x, ld_w, x_scale, w_scale, T, N, mx4_blocks(K), Q8Out{out, out_type, ld_out, 1}};
+    return cu(launch_mx4_product(a, (cudaStream_t)stream));
+}
+
+size_t dstd_dense_mx4_workspace_bytes(int B, int N_in, int N_out, const dstd_params *p) {
+    if (check_mx4_sizes(B, N_in, N_out, p) != DSTD_OK) return 0;
+    return mx4_layout(nullptr, B, N_in, N_out, padded_M(p->M)).bytes;
+}
+
+int dstd_dense_fwd_mx4(const float *t_in, const uint8_t *w_q, const uint8_t *w_scale, int B, int N_in, int N_out,
+                       const dstd_params *p, float *t_out, void *saved, float *penalty, void *workspace,
+                       size_t ws_bytes, dstd_stream_t stream) {
+    if (!t_in || !w_q || !w_scale || !t_out || !saved || !workspace) return DSTD_E_INVALID;
+    TRY(check_mx4_sizes(B, N_in, N_out, p));
+    if (!aligned16(t_in) || !aligned16(w_q) || !aligned16(w_scale) || !aligned16(workspace) || !aligned16(saved))
+        return DSTD_E_INVALID;
+    const int Mp = padded_M(p->M), T = B * Mp;
+    Mx4Ws ws = mx4_layout(workspace, B, N_in, N_out, Mp);
+    if (ws_bytes < ws.bytes) return DSTD_E_WORKSPACE;
+    TRY(device_ok());
+    LifConst c = make_const(*p, Mp);
+    cudaStream_t st = (cudaStream_t)stream;
+    Saved sv = saved_view(saved, B, N_out);
+    if (penalty) TRY(cu(cudaMemsetAsync(penalty, 0, 4 * sizeof(float), st)));
+    {
+        Timed tm(KK_BIN, st);
+        TRY(cu(launch_bin_mx4(t_in, B, N_in, c, ws.q, row_bytes(N_in), ws.scale, st)));
+    }
+    // only the value of the dead-neuron penalty needs the weights' row sums
+    const bool sums = penalty && p->gamma_q != 0.0f;
+    if (sums) {
+        Timed tm(KK_PREP, st);
+        TRY(cu(launch_mx4_rowsum(w_q, row_bytes(N_in), w_scale, N_out, N_in, ws.rowsum, st)));
+    }
+    {
+        Timed tm(KK_MX4, st);
+        const Mx4Args a{ws.q, w_q, row_bytes(N_in), row_bytes(N_in), ws.scale, w_scale, T, N_out, mx4_blocks(N_in),
+                        Q8Out{ws.D, DSTD_TYPE_F32, 1, T}};
+        TRY(cu(launch_mx4_product(a, st)));
+    }
+    Timed tm(KK_SCAN, st);
+    return cu(launch_scan_solve(ws.D, Mp, T, 1, B, N_out, c, nullptr, sums ? ws.rowsum : nullptr, t_out, sv.q, sv.s,
+                                sv.vdot, penalty, st));
+}
+
+int dstd_top_logits(const void *y, dstd_type type, int R, int C, int64_t ld_y, float factor, float silent, int K,
+                    float *top, int32_t *index, dstd_stream_t stream) {
+    TRY(check_logits(y, type, R, C, ld_y, factor, silent));
+    if (K < 1 || K > C || !top || !index || !aligned_to(top, 4) || !aligned_to(index, 4)) return DSTD_E_INVALID;
+    if (K > kTopMax) return DSTD_E_UNSUPPORTED;
+    TRY(device_ok());
+    Timed tm(KK_TOP, (cudaStream_t)stream);
+    const LogitArgs a{y, type, R, C, ld_y, factor, silent};
+    return cu(launch_top_logits(a, K, top, index, (cudaStream_t)stream));
+}
+
+int dstd_distill_loss(const void *y, dstd_type type, int R, int C, int64_t ld_y, float factor, float silent,
+                      const float *top, const int32_t *index, int K, float teacher_factor, float weight,
+                      const float *row_weight, float *loss, float *row_loss, void *g, int64_t ld_g, int accumulate,
+                      dstd_stream_t stream) {
+    TRY(check_logits(y, type, R, C, ld_y, factor, silent));
+    if (K < 1 || !top || !index || !loss || !row_loss || !aligned_to(top, 4) || !aligned_to(index, 4) ||
+        !aligned_to(loss, 8) || !aligned_to(row_loss, 4) || (row_weight && !aligned_to(row_weight, 4)))
+        return DSTD_E_INVALID;
+    if (g && (ld_g < C || !aligned_to(g, type_bytes(type)))) return DSTD_E_INVALID;
+    if (!isfinite(teacher_factor) || teacher_factor == 0.0f || !isfinite(weight)) return DSTD_E_INVALID;
+    if (K > kTopMax) return DSTD_E_UNSUPPORTED;
+    TRY(device_ok());
+    Timed tm(KK_DISTILL, (cudaStream_t)stream);
+    const LogitArgs a{y, type, R, C, ld_y, factor, silent};
+    return cu(launch_distill(DistillArgs{a, top, index, K, teacher_factor, weight, row_weight, loss, row_loss, g, ld_g,
+                                         accumulate != 0},
+                             (cudaStream_t)stream));
 }
 
 }  // extern "C"

@@ -779,4 +779,49 @@ size_t q8_workspace_bytes(int T, int N, int K, bool aligned);
 cudaError_t q8_status_read(unsigned int *out, int clear);
 cudaError_t launch_q8_product(const Q8Args &a, void *workspace, int &launches, cudaStream_t st);  // launches out
 
+// 4-bit rows with a power of two for each block of 32 columns, and their products (dstd_mx4.cu).
+__host__ __device__ inline int mx4_blocks(int cols) { return (int)(((long long)cols + 31) / 32); }
+size_t mx4_scale_bytes(long long rows, int cols);
+cudaError_t launch_quantize_mx4(const void *x, dstd_type type, int rows, int cols, long long ld_x, uint8_t *q,
+                                long long ld_q, uint8_t *scale, float *values, long long ld_v, cudaStream_t st);
+// grid weights of t [B, N] as codes [B Mp, ld_q] (ld_q a multiple of 16) and exponents; Mp <= 128
+cudaError_t launch_bin_mx4(const float *t, int B, int N, const LifConst &c, uint8_t *q, long long ld_q, uint8_t *scale,
+                           cudaStream_t st);
+cudaError_t launch_mx4_rowsum(const uint8_t *w, long long ld, const uint8_t *scale, int N, int K, float *rowsum,
+                              cudaStream_t st);
+struct Mx4Args {
+    const uint8_t *x, *w;  // [T, 16 blocks] and [N, 16 blocks] bytes
+    long long ld_x, ld_w;
+    const uint8_t *x_scale, *w_scale;
+    int T, N, blocks;
+    Q8Out out;
+};
+cudaError_t launch_mx4_product(const Mx4Args &a, cudaStream_t st);
+
+// Largest logits of each row, and the distillation loss from them (dstd_distill.cu).
+// logit of an output y: factor y, and factor silent where that is -infinity
+struct LogitArgs {
+    const void *y;
+    dstd_type type;
+    int rows, cols;
+    long long ld;
+    float factor, silent;
+};
+constexpr int kTopMax = 256;
+cudaError_t launch_top_logits(const LogitArgs &a, int K, float *top, int32_t *index, cudaStream_t st);
+struct DistillArgs {
+    LogitArgs y;
+    const float *top;
+    const int32_t *index;
+    int K;
+    float teacher_factor, weight;
+    const float *row_weight;  // or null: 1 / rows each
+    float *loss;              // value, ticket
+    float *row_loss;
+    void *g;                  // or null
+    long long ld_g;
+    bool accumulate;
+};
+cudaError_t launch_distill(const DistillArgs &a, cudaStream_t st);
+
 }  // namespace dstd

@@ -8,6 +8,7 @@ fallback of any kind. A missing library raises at load time.
 """
 
 import ctypes
+import math
 import os
 
 from .build import LIB_PATH
@@ -27,7 +28,9 @@ EXPORTS = ("dstd_dense_saved_bytes", "dstd_dense_workspace_bytes", "dstd_binning
            "dstd_ms_saved_bytes", "dstd_ms_workspace_bytes", "dstd_dense_fwd_ms", "dstd_dense_bwd_ms",
            "dstd_quantize_rows", "dstd_int8_matmul_workspace_bytes", "dstd_int8_matmul_aligned_workspace_bytes",
            "dstd_int8_matmul", "dstd_dense_q8_workspace_bytes",
-           "dstd_dense_fwd_q8", "dstd_grad_norm_workspace_bytes", "dstd_grad_norm", "dstd_clip_grads", "dstd_adamw_clip")
+           "dstd_dense_fwd_q8", "dstd_grad_norm_workspace_bytes", "dstd_grad_norm", "dstd_clip_grads", "dstd_adamw_clip",
+           "dstd_mx4_scale_bytes", "dstd_quantize_mx4", "dstd_mx4_matmul", "dstd_dense_mx4_workspace_bytes",
+           "dstd_dense_fwd_mx4", "dstd_top_logits", "dstd_distill_loss")
 
 
 class DstdError(RuntimeError):
@@ -120,6 +123,13 @@ def load(path=None):
         "dstd_grad_norm": (_I, [_I, _P, _P, _P, _P, _P, _P, _SZ, _P]),
         "dstd_clip_grads": (_I, [_I, _P, _P, _P, _P, _D, _P, _P, _SZ, _P]),
         "dstd_adamw_clip": (_I, [_I, _P, _P, _P, _P, _P, _P, _D, _D, _D, _D, _D, _D, _P, _P, _P, _P, _SZ, _P]),
+        "dstd_mx4_scale_bytes": (_SZ, [_I, _I]),
+        "dstd_quantize_mx4": (_I, [_P, _I, _I, _I, _I64, _P, _I64, _P, _P, _I64, _P]),
+        "dstd_mx4_matmul": (_I, [_P, _I64, _P, _P, _I64, _P, _I, _I, _I, _P, _I, _I64, _P]),
+        "dstd_dense_mx4_workspace_bytes": (_SZ, [_I, _I, _I, _PP]),
+        "dstd_dense_fwd_mx4": (_I, [_P, _P, _P, _I, _I, _I, _PP, _P, _P, _P, _P, _SZ, _P]),
+        "dstd_top_logits": (_I, [_P, _I, _I, _I, _I64, _F, _F, _I, _P, _P, _P]),
+        "dstd_distill_loss": (_I, [_P, _I, _I, _I, _I64, _F, _F, _P, _P, _I, _F, _F, _P, _P, _P, _P, _I64, _I, _P]),
         "dstd_split_channels": (_I, [_P, _I, _I, _I64, _P, _I, _P, _I, _P]),
     }
     for name, (res, args) in sig.items():
@@ -529,6 +539,174 @@ def dense_fwd_q8(t_in, w_q, w_scale, p, t_out, saved, penalty, workspace, stream
                                     ctypes.byref(p), t_out.data_ptr(), _ptr(saved), _ptr(penalty),
                                     workspace.data_ptr(), _scratch(workspace, "dense_fwd_q8", dev),
                                     _stream_of(stream, dev)), "dstd_dense_fwd_q8")
+
+
+# -- training and serving in 4 bits ------------------------------------------
+def mx4_row_bytes(cols):
+    """Bytes of a row of 4-bit codes: 16 for each block of 32 columns."""
+    return 16 * ((cols + 31) // 32)
+
+
+def mx4_scale_bytes(rows, cols):
+    """Bytes of the scales of rows of 4-bit codes (their layout: include/dstd.h)."""
+    return load().dstd_mx4_scale_bytes(rows, cols)
+
+
+def _codes4(q, name, R, row, dev):
+    """Row stride in bytes of R rows of 4-bit codes, `row` bytes each, at multiples of 16 bytes."""
+    ld = _rows(q, name, R, row, dev, _TORCH.uint8)
+    if q.numel() and (q.data_ptr() % 16 or ld % 16):
+        raise ValueError(f"{name}: rows of codes must start at multiples of 16 bytes")
+    return ld
+
+
+def _scales4(s, name, R, cols, dev):
+    need = mx4_scale_bytes(R, cols)
+    if s.dtype != _TORCH.uint8 or s.get_device() != dev or not s.is_contiguous() or s.numel() < need:
+        raise ValueError(f"{name} must be a contiguous uint8 tensor of at least {need} on cuda:{dev}")
+
+
+def quantize_mx4(x, q, scale, values=None, stream=None):
+    """Rows of x [R, K] (float32, bfloat16 or float16) to 4-bit floating-point
+    codes q [R, mx4_row_bytes(K)] uint8, two to a byte, with a power of two for each
+    block of 32 columns in scale [mx4_scale_bytes(R, K)] uint8: the least with
+    no code beyond 6. ``values`` [R, K] float32 receives what the codes stand
+    for. A block that is not finite gets scale NaN. Rows may be padded."""
+    torch = _torch()
+    R, K = x.shape
+    dev = x.get_device()
+    if dev != _ONLY:
+        _here(x, dev, "x")
+    ld_x = _rows(x, "x", R, K, dev)
+    ld_q = _codes4(q, "q", R, mx4_row_bytes(K), dev)
+    _scales4(scale, "scale", R, K, dev)
+    ld_v, v = 0, None
+    if values is not None:
+        ld_v, v = _rows(values, "values", R, K, dev, torch.float32), values.data_ptr()
+    code = load().dstd_quantize_mx4(x.data_ptr(), _type_code(x.dtype, "x"), R, K, ld_x, q.data_ptr(), ld_q,
+                                    scale.data_ptr(), v, ld_v, _stream_of(stream, dev))
+    if code:
+        raise DstdError(code, "dstd_quantize_mx4")
+
+
+def mx4_matmul(x, x_scale, w, w_scale, out, stream=None):
+    """out [T, N] = x @ w^T of 4-bit rows x [T, bytes] and w [N, bytes] with their
+    scales, as from quantize_mx4; sums in float32. out is float32, bfloat16 or
+    float16; rows may be padded."""
+    _torch()
+    T, row = x.shape
+    N = w.shape[0]
+    dev = x.get_device()
+    if dev != _ONLY:
+        _here(x, dev, "x")
+    if row % 16 or row > 1 << 30:
+        raise ValueError("mx4_matmul: a row of codes is 16 bytes for each block of 32 columns")
+    K = 2 * row
+    ld_x = _codes4(x, "x", T, row, dev)
+    ld_w = _codes4(w, "w", N, row, dev)
+    _scales4(x_scale, "x_scale", T, K, dev)
+    _scales4(w_scale, "w_scale", N, K, dev)
+    ld_out = _rows(out, "out", T, N, dev)
+    code = load().dstd_mx4_matmul(x.data_ptr(), ld_x, x_scale.data_ptr(), w.data_ptr(), ld_w, w_scale.data_ptr(), T, N,
+                                  K, out.data_ptr(), _type_code(out.dtype, "out"), ld_out, _stream_of(stream, dev))
+    if code:
+        raise DstdError(code, "dstd_mx4_matmul")
+
+
+def dense_mx4_workspace_bytes(B, N_in, N_out, p):
+    return load().dstd_dense_mx4_workspace_bytes(B, N_in, N_out, ctypes.byref(p))
+
+
+def dense_fwd_mx4(t_in, w_q, w_scale, p, t_out, saved, penalty, workspace, stream=None):
+    """dense_fwd with a 4-bit contraction: w_q [N_out, mx4_row_bytes(N_in)] and
+    w_scale from quantize_mx4; the grid weights are quantised for each (sample,
+    grid point). Backward: dense_bwd with the weights' values."""
+    torch = _torch()
+    B, N_in = t_in.shape
+    N_out = w_q.shape[0]
+    _f32(t_in, "t_in")
+    _f32(t_out, "t_out", (B, N_out))
+    dev = t_in.get_device()
+    if dev != _ONLY:
+        _here(t_in, dev, "t_in")
+    if t_out.get_device() != dev:
+        raise ValueError(f"t_out must be on cuda:{dev}")
+    row = mx4_row_bytes(N_in)
+    if w_q.dtype != torch.uint8 or w_q.get_device() != dev or not w_q.is_contiguous() or tuple(w_q.shape) != (N_out, row):
+        raise ValueError(f"w_q must be a contiguous uint8 tensor {(N_out, row)} on cuda:{dev}")
+    _scales4(w_scale, "w_scale", N_out, N_in, dev)
+    _check(load().dstd_dense_fwd_mx4(t_in.data_ptr(), w_q.data_ptr(), w_scale.data_ptr(), B, N_in, N_out,
+                                     ctypes.byref(p), t_out.data_ptr(), _ptr(saved), _ptr(penalty),
+                                     workspace.data_ptr(), _scratch(workspace, "dense_fwd_mx4", dev),
+                                     _stream_of(stream, dev)), "dstd_dense_fwd_mx4")
+
+
+# -- learning from a teacher -------------------------------------------------
+def _record(top, index, R, K, dev):
+    """A teacher's record: contiguous float32 logits and int32 classes [R, K]."""
+    if top.shape != (R, K) or top.dtype != _TORCH.float32 or top.get_device() != dev or not top.is_contiguous():
+        raise ValueError(f"top must be a contiguous float32 tensor {(R, K)} on cuda:{dev}")
+    if index.shape != (R, K) or index.dtype != _TORCH.int32 or index.get_device() != dev or not index.is_contiguous():
+        raise ValueError(f"index must be a contiguous int32 tensor {(R, K)} on cuda:{dev}")
+
+
+def _no_logit(factor, silent):
+    """The output that stands in where a logit is -infinity: none, unless one is given."""
+    if silent is not None:
+        return silent
+    return -math.inf if factor > 0 else math.inf
+
+
+def top_logits(y, top, index, factor=1.0, silent=None, stream=None):
+    """The K largest logits factor * y of each row of y [R, C] (float32,
+    bfloat16 or float16), descending, equal ones by ascending class, into top
+    [R, K] float32 and index [R, K] int32: what is kept of a teacher. Spike times
+    have factor -1/tau_soft and, for silent outputs, ``silent`` = t_end; without
+    it those (and masked classes) come last, with -inf. Rows may be padded."""
+    _torch()
+    R, C = y.shape
+    dev = y.get_device()
+    if dev != _ONLY:
+        _here(y, dev, "y")
+    ld_y = _rows(y, "y", R, C, dev)
+    K = top.shape[-1]
+    _record(top, index, R, K, dev)
+    code = load().dstd_top_logits(y.data_ptr(), _type_code(y.dtype, "y"), R, C, ld_y, factor,
+                                  _no_logit(factor, silent), K, top.data_ptr(), index.data_ptr(),
+                                  _stream_of(stream, dev))
+    if code:
+        raise DstdError(code, "dstd_top_logits")
+
+
+def distill_loss(y, top, index, loss, row_loss, g=None, factor=1.0, silent=None, teacher_factor=1.0, weight=1.0,
+                 row_weight=None, accumulate=False, stream=None):
+    """Kullback-Leibler divergence of softmax(factor * y) from the teacher's
+    softmax(teacher_factor * top) over the classes ``index`` (entries outside
+    [0, C) are unused), and its gradient: row_loss [R], loss[0] = weight * their
+    mean (or their sum with row_weight [R]), g [R, C] of y's type (may be None;
+    accumulate: added to what it holds). loss: float32[2], zeros at first.
+    factor and silent as in top_logits; silent outputs pass no gradient."""
+    _torch()
+    R, C = y.shape
+    dev = y.get_device()
+    if dev != _ONLY:
+        _here(y, dev, "y")
+    ld_y = _rows(y, "y", R, C, dev)
+    K = top.shape[-1]
+    _record(top, index, R, K, dev)
+    _floats(loss, "loss", 2, dev)
+    _floats(row_loss, "row_loss", R, dev)
+    if row_weight is not None:
+        _floats(row_weight, "row_weight", R, dev)
+    ld_g, gp = 0, None
+    if g is not None:
+        ld_g, gp = _rows(g, "g", R, C, dev, y.dtype), g.data_ptr()
+    code = load().dstd_distill_loss(y.data_ptr(), _type_code(y.dtype, "y"), R, C, ld_y, factor,
+                                    _no_logit(factor, silent), top.data_ptr(), index.data_ptr(), K, teacher_factor,
+                                    weight, _ptr(row_weight), loss.data_ptr(), row_loss.data_ptr(), gp, ld_g,
+                                    bool(accumulate), _stream_of(stream, dev))
+    if code:
+        raise DstdError(code, "dstd_distill_loss")
 
 
 class TensorList:
