@@ -797,6 +797,7 @@ struct Mx4Args {
     Q8Out out;
 };
 cudaError_t launch_mx4_product(const Mx4Args &a, cudaStream_t st);
+cudaError_t mx4_status_read(unsigned int *out, int clear);
 
 // Largest logits of each row, and the distillation loss from them (dstd_distill.cu).
 // logit of an output y: factor y, and factor silent where that is -infinity

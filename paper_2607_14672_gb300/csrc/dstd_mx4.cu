@@ -243,57 +243,353 @@ cudaError_t launch_mx4_rowsum(const uint8_t *w, long long ld, const uint8_t *sca
 }
 
 // ---------------------------------------------------------------------------
-// Product, simplest form: a block of 256 threads computes 64 channels x 64 tokens,
-// one block of 32 columns at a time, values in shared memory.
+// Product on the 4-bit tensor cores, D[n, t]: a block computes 128 rows of one
+// side (the channels, as a rule) times NT of the other. TMA brings 256 columns of K a stage,
+// codes as they are, and the scales of both; one thread copies the scales to
+// TMEM and issues the MMAs, in that order; four warps take the sums out.
+// Where there are few tiles, `parts` blocks of a cluster share K: each leaves its sums in its own shared
+// memory, and each adds up its share of the columns over all, in order.
 // ---------------------------------------------------------------------------
-__global__ void __launch_bounds__(256) k_mx4_product(const Mx4Args a) {
-    __shared__ float s_w[32][65], s_x[32][65];
-    const int tiles = (a.N + 63) / 64;
-    const long long n0 = (long long)(blockIdx.x % tiles) * 64, t0 = (long long)(blockIdx.x / tiles) * 64;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    float acc[4][4] = {};
-    for (int b = 0; b < a.blocks; ++b) {
-        for (int i = threadIdx.x; i < 2 * 64 * 16; i += 256) {
-            const bool tok = i >= 1024;
-            const int r = (i >> 4) & 63, byte = i & 15;
-            const long long row = (tok ? t0 : n0) + r;
-            float2 v = make_float2(0.f, 0.f);
-            if (row < (tok ? a.T : a.N)) {
-                v = pair_values((tok ? a.x + row * a.ld_x : a.w + row * a.ld_w)[(long long)b * 16 + byte]);
-                const float s = block_scale((tok ? a.x_scale : a.w_scale)[scale_at(row, b, (a.blocks + 3) / 4)]);
-                v.x *= s;
-                v.y *= s;
-            }
-            (tok ? s_x : s_w)[2 * byte][r] = v.x;
-            (tok ? s_x : s_w)[2 * byte + 1][r] = v.y;
-        }
-        __syncthreads();
-        for (int k = 0; k < 32; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] += s_x[k][ty + 16 * i] * s_w[k][tx + 16 * j];
-        __syncthreads();
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const long long t = t0 + ty + 16 * i, n = n0 + tx + 16 * j;
-            if (t >= a.T || n >= a.N) continue;
-            const long long at = t * a.out.ld_t + n * a.out.ld_n;
-            if (a.out.type == DSTD_TYPE_F32) ((float *)a.out.p)[at] = acc[i][j];
-            else if (a.out.type == DSTD_TYPE_BF16) ((__nv_bfloat16 *)a.out.p)[at] = __float2bfloat16_rn(acc[i][j]);
-            else ((__half *)a.out.p)[at] = __float2half_rn(acc[i][j]);
-        }
+__device__ unsigned int g_status_mx4 = 0;
+
+cudaError_t mx4_status_read(unsigned int *out, int clear) {
+    cudaError_t e = cudaMemcpyFromSymbol(out, g_status_mx4, sizeof(unsigned int));
+    if (e != cudaSuccess || !clear) return e;
+    unsigned int z = 0;
+    return cudaMemcpyToSymbol(g_status_mx4, &z, sizeof(z));
 }
+
+namespace {
+using namespace tc;
+
+constexpr int kStageBlocks = 8;          // blocks of 32 along K a stage: rows of 128 bytes
+constexpr int kRowBytes = 16 * kStageBlocks;
+constexpr int kTileBytes = 128 * kRowBytes;
+constexpr int kScaleTile = 512;          // scales of 128 rows by 4 blocks
+
+template <int NT>
+struct Mx4Cfg {
+    static constexpr int B_BYTES = NT * kRowBytes;
+    static constexpr int B_TILES = (NT + 127) / 128;  // of 128 rows of scales
+    static constexpr int SF_BYTES = 2 * kScaleTile * (1 + B_TILES);
+    static constexpr int STAGE = (kTileBytes + B_BYTES + SF_BYTES + 1023) / 1024 * 1024;
+    static constexpr int BUDGET = NT >= 256 ? 216 * 1024 : 108 * 1024;  // two blocks to an SM up to 128 columns
+    static constexpr int STAGES = BUDGET / STAGE > 6 ? 6 : BUDGET / STAGE;
+    static constexpr int SMEM = STAGES * STAGE + 1024 + 256;
+    static constexpr int SF_COL = NT;                    // scales: two sets of (A, B) in turn
+    static constexpr int SF_SET = 2 * 4 * (1 + B_TILES);
+    static constexpr int USED = NT + 2 * SF_SET;
+    static constexpr int COLS = USED <= 64 ? 64 : (USED <= 128 ? 128 : (USED <= 256 ? 256 : 512));
+    static_assert(NT * 128 * 4 <= STAGES * STAGE, "the sums of a tile fit the stages");
+};
+
+// rows of one side of the product, a the side of 128-row tiles
+struct Mx4Side {
+    const uint8_t *scale;
+    int rows;
+};
+struct Mx4Tc {
+    Mx4Side a, b;
+    int blocks, ktiles, tiles_a, tiles_b, parts;
+    void *out;
+    long long ld_a, ld_b;  // of out; one of them is 1
+};
+
+// tiles are taken in groups of 8 of one side, so that blocks at work at one time share both operands in L2
+__device__ __forceinline__ void mx4_tile(int i, int tiles_a, int tiles_b, int &ta, int &tb) {
+    const int per = 8 * tiles_a, group = i / per, r = i - group * per;
+    const int left = tiles_b - group * 8, wide = left < 8 ? left : 8;
+    ta = r / wide;
+    tb = group * 8 + r - ta * wide;
+}
+
+__device__ __forceinline__ void mx4_timeout() { atomicOr(&g_status_mx4, STATUS_TIMEOUT); }
+
+// CH columns of a lane's row to out: neighbouring lanes next to each other (ld_a = 1), or the lane's own
+// columns (ld_b = 1)
+template <class O, int CH>
+__device__ __forceinline__ void mx4_store(O *dst, long long ld_a, long long ld_b, const float (&v)[CH], int left) {
+    if (ld_b != 1 || ld_a == 1) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            if (c < left) dst[c * ld_b] = round_out<O>(v[c]);
+        return;
+    }
+    constexpr int P = 16 / sizeof(O);
+    const bool vec = (reinterpret_cast<uintptr_t>(dst) & 15) == 0;
+#pragma unroll
+    for (int c = 0; c < CH; c += P) {
+        alignas(16) O y[P];
+#pragma unroll
+        for (int u = 0; u < P; ++u) y[u] = round_out<O>(v[c + u]);
+        if (vec && c + P <= left) {
+            *reinterpret_cast<uint4 *>(dst + c) = *reinterpret_cast<const uint4 *>(y);
+        } else {
+#pragma unroll
+            for (int u = 0; u < P; ++u)
+                if (c + u < left) dst[c + u] = y[u];
+        }
+    }
+}
+
+__device__ __forceinline__ float ld_cluster(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+template <int NT, class O>
+__global__ void __launch_bounds__(192) k_mx4_tc(const __grid_constant__ CUtensorMap map_a,
+                                                const __grid_constant__ CUtensorMap map_b, const Mx4Tc p) {
+    using C = Mx4Cfg<NT>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint64_t *full = reinterpret_cast<uint64_t *>(smem + C::STAGES * C::STAGE);
+    uint64_t *empty = full + C::STAGES, *done = empty + C::STAGES;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(done + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int part = p.parts > 1 ? (int)cluster_ctarank() : 0;
+    int ta, tb;
+    mx4_tile((int)(blockIdx.x / p.parts), p.tiles_a, p.tiles_b, ta, tb);
+    const int stages = (p.blocks + kStageBlocks - 1) / kStageBlocks;
+    const int s0 = (int)((long long)stages * part / p.parts), s1 = (int)((long long)stages * (part + 1) / p.parts);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::STAGES; ++s) {
+            mbar_init(&full[s], 1);
+            mbar_init(&empty[s], 1);
+        }
+        mbar_init(done, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 5) tmem_alloc(tmem_slot, C::COLS);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    wait_launch_before();
+
+    if (warp == 4) {
+        bool ok = true;
+        int it = 0;
+        for (int s = s0; s < s1; ++s, ++it) {
+            const int slot = it % C::STAGES;
+            ok = mbar_wait_cycles(&empty[slot], ((it / C::STAGES) & 1u) ^ 1u);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            if (elect_one()) {
+                const uint32_t st = smem_u32(smem + slot * C::STAGE), sf = st + kTileBytes + C::B_BYTES;
+                const int k0 = s * 2, kt = min(2, p.ktiles - k0);
+                const uint32_t sf_bytes = (uint32_t)kt * kScaleTile;
+                int b_tiles = 0;
+#pragma unroll
+                for (int i = 0; i < C::B_TILES; ++i) b_tiles += tb * NT + i * 128 < p.b.rows ? 1 : 0;
+                mbar_expect_tx(&full[slot], (uint32_t)(kTileBytes + C::B_BYTES) + sf_bytes * (1 + b_tiles));
+                tma_load_2d(st, &map_a, &full[slot], s * kRowBytes, ta * 128);
+                tma_load_2d(st + kTileBytes, &map_b, &full[slot], s * kRowBytes, tb * NT);
+                bulk_load(sf, p.a.scale + ((long long)ta * p.ktiles + k0) * kScaleTile, sf_bytes, &full[slot]);
+#pragma unroll
+                for (int i = 0; i < C::B_TILES; ++i)
+                    if (i < b_tiles)
+                        bulk_load(sf + (1 + i) * 2 * kScaleTile,
+                                  p.b.scale + (((long long)tb * NT / 128 + i) * p.ktiles + k0) * kScaleTile, sf_bytes,
+                                  &full[slot]);
+            }
+            __syncwarp();
+        }
+        // every stage released: no copy is in flight
+        for (int i = 0; i < C::STAGES && ok; ++i, ++it)
+            ok = mbar_wait_cycles(&empty[it % C::STAGES], ((it / C::STAGES) & 1u) ^ 1u);
+        if (!ok) mx4_timeout();
+        __syncwarp();
+    } else if (warp == 5) {
+        bool ok = true;
+        int it = 0;
+        for (int s = s0; s < s1; ++s, ++it) {
+            const int slot = it % C::STAGES;
+            ok = mbar_wait_cycles(&full[slot], (it / C::STAGES) & 1u);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint32_t st = smem_u32(smem + slot * C::STAGE), sf = st + kTileBytes + C::B_BYTES;
+                const uint32_t sfa = tmem + C::SF_COL + (it & 1) * C::SF_SET, sfb = sfa + 8;
+                const uint64_t ad = sdesc_sw128(st), bd = sdesc_sw128(st + kTileBytes);
+                const int left = p.blocks - s * kStageBlocks;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (h * 4 >= left) break;
+                    tmem_cp_scales(sfa + h * 4, sdesc_rows16(sf + h * kScaleTile));
+#pragma unroll
+                    for (int i = 0; i < C::B_TILES; ++i)
+                        tmem_cp_scales(sfb + (h * C::B_TILES + i) * 4,
+                                       sdesc_rows16(sf + (1 + i) * 2 * kScaleTile + h * kScaleTile));
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int kk = 2 * h + i;
+                        if (kk * 2 >= left) break;
+                        mma_mx4(tmem, ad + kk * 2, bd + kk * 2, idesc_mx4(128, NT, 2 * i), sfa + h * 4,
+                                sfb + h * C::B_TILES * 4, it > 0 || kk > 0 ? 1u : 0u);
+                    }
+                }
+                mma_commit(&empty[slot]);
+                if (s + 1 == s1) mma_commit(done);
+            }
+            __syncwarp();
+        }
+        if (!ok) mx4_timeout();
+        __syncwarp();
+    }
+    bool ok = true;
+    if (warp < 4) {
+        const int row = warp * 32 + lane;
+        const long long r = (long long)ta * 128 + row, c0 = (long long)tb * NT;
+        const bool any = s1 > s0;
+        ok = !any || mbar_wait_cycles(done, 0);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok && lane == 0) mx4_timeout();
+        tc_fence_after();
+        constexpr int CH = 16;
+        const uint32_t t0 = tmem + ((uint32_t)(warp * 32) << 16);
+#pragma unroll 1
+        for (int c = 0; c < NT && ok; c += CH) {
+            float v[CH];
+            if (any) tmem_ld16(t0 + c, v);
+            else
+#pragma unroll
+                for (int i = 0; i < CH; ++i) v[i] = 0.f;
+            if (p.parts > 1) {
+                float *sum = reinterpret_cast<float *>(smem) + c * 128 + row;
+#pragma unroll
+                for (int i = 0; i < CH; ++i) sum[i * 128] = v[i];
+            } else {
+                const long long left = r < p.a.rows ? p.b.rows - (c0 + c) : 0;
+                mx4_store<O, CH>(static_cast<O *>(p.out) + r * p.ld_a + (c0 + c) * p.ld_b, p.ld_a, p.ld_b, v,
+                                 (int)max(0ll, min((long long)CH, left)));
+            }
+        }
+    }
+    if (p.parts > 1) {
+        __syncwarp();
+        cluster_sync();
+        // this block's share of the columns
+        const int first = NT * part / p.parts, last = NT * (part + 1) / p.parts;
+        const uint32_t base = smem_u32(smem);
+        for (int i = threadIdx.x; i < (last - first) * 128; i += 192) {
+            const int c = first + (i >> 7), row = i & 127;
+            float sum = 0.f;
+            for (int q = 0; q < p.parts; ++q) sum += ld_cluster(mapa_rank(base + (c * 128 + row) * 4, q));
+            const long long r = (long long)ta * 128 + row, col = (long long)tb * NT + c;
+            if (r < p.a.rows && col < p.b.rows)
+                static_cast<O *>(p.out)[r * p.ld_a + col * p.ld_b] = round_out<O>(sum);
+        }
+        __syncwarp();
+        cluster_sync();
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 5) tmem_dealloc(tmem, C::COLS);
+}
+
+typedef CUresult (*EncodeFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                             const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                             CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// boxes of box_rows rows of 128 bytes, swizzled; beyond the matrix zeros are read
+bool code_map(CUtensorMap *m, const uint8_t *p, int rows, int blocks, long long ld, int box_rows) {
+    EncodeFn enc = reinterpret_cast<EncodeFn>(tensor_map_encoder());
+    if (!enc) return false;
+    const cuuint64_t dim[2] = {(cuuint64_t)blocks * 16, (cuuint64_t)rows};
+    const cuuint64_t stride[1] = {(cuuint64_t)ld};
+    const cuuint32_t box[2] = {(cuuint32_t)kRowBytes, (cuuint32_t)box_rows};
+    const cuuint32_t one[2] = {1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t *>(p), dim, stride, box, one,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Mx4Plan {
+    int nt, parts;
+    bool exchanged;  // the tokens are the side of 128-row tiles
+};
+
+template <int NT, class O>
+cudaError_t launch_mx4_tc(const Mx4Args &a, const Mx4Plan &plan, cudaStream_t st) {
+    using C = Mx4Cfg<NT>;
+    static PerDevice granted;
+    if (!granted.get([](int) {
+            return cudaFuncSetAttribute(k_mx4_tc<NT, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) ==
+                           cudaSuccess ? 1 : 0;
+        }))
+        return cudaErrorInvalidConfiguration;
+    const bool ex = plan.exchanged;
+    const int rows_a = ex ? a.T : a.N, rows_b = ex ? a.N : a.T;
+    CUtensorMap map_a, map_b;
+    if (!code_map(&map_a, ex ? a.x : a.w, rows_a, a.blocks, ex ? a.ld_x : a.ld_w, 128) ||
+        !code_map(&map_b, ex ? a.w : a.x, rows_b, a.blocks, ex ? a.ld_w : a.ld_x, NT))
+        return cudaErrorInvalidValue;
+    const Mx4Tc p{{ex ? a.x_scale : a.w_scale, rows_a}, {ex ? a.w_scale : a.x_scale, rows_b}, a.blocks, (a.blocks + 3) / 4,
+                  (rows_a - 1) / 128 + 1, (rows_b - 1) / NT + 1, plan.parts, a.out.p, ex ? a.out.ld_t : a.out.ld_n,
+                  ex ? a.out.ld_n : a.out.ld_t};
+    const long long grid = (long long)p.tiles_a * p.tiles_b * plan.parts;
+    if (grid > 0x7fffffff) return cudaErrorInvalidValue;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)plan.parts;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = plan.parts > 1 ? 2 : 1;
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(192);
+    cfg.dynamicSmemBytes = C::SMEM;
+    cfg.stream = st;
+    return cudaLaunchKernelEx(&cfg, k_mx4_tc<NT, O>, map_a, map_b, p);
+}
+
+Mx4Plan mx4_plan(int T, int N, int blocks) {
+    Mx4Plan p{};
+    p.exchanged = T > N;
+    const int b = p.exchanged ? N : T, a = p.exchanged ? T : N;
+    p.nt = b <= 16 ? 16 : (b <= 32 ? 32 : (b <= 64 ? 64 : 128));
+    const long long tiles = (((long long)a + 127) / 128) * (((long long)b + p.nt - 1) / p.nt);
+    const int stages = (blocks + kStageBlocks - 1) / kStageBlocks;
+    p.parts = 1;
+    while (p.parts < 8 && tiles * p.parts * 2 <= 304 && p.parts * 2 <= stages) p.parts *= 2;
+    return p;
+}
+
+template <class O>
+cudaError_t run_mx4(const Mx4Args &a, cudaStream_t st) {
+    const Mx4Plan p = mx4_plan(a.T, a.N, a.blocks);
+    if (p.nt == 16) return launch_mx4_tc<16, O>(a, p, st);
+    if (p.nt == 32) return launch_mx4_tc<32, O>(a, p, st);
+    if (p.nt == 64) return launch_mx4_tc<64, O>(a, p, st);
+    return launch_mx4_tc<128, O>(a, p, st);
+}
+
+// a product of no columns
+__global__ void __launch_bounds__(256) k_zero_rows(char *out, long long bytes, long long ld_bytes, int rows) {
+    for (long long r = blockIdx.x; r < rows; r += gridDim.x)
+        for (long long i = threadIdx.x; i < bytes; i += 256) out[r * ld_bytes + i] = 0;
+}
+
+}  // namespace
 
 cudaError_t launch_mx4_product(const Mx4Args &a, cudaStream_t st) {
     if (a.T == 0 || a.N == 0) return cudaSuccess;
-    const long long grid = (((long long)a.N + 63) / 64) * (((long long)a.T + 63) / 64);
-    if (grid > 0x7fffffff) return cudaErrorInvalidValue;
-    k_mx4_product<<<(unsigned)grid, 256, 0, st>>>(a);
-    return cudaGetLastError();
+    if (a.blocks == 0) {
+        const long long size = a.out.type == DSTD_TYPE_F32 ? 4 : 2;
+        k_zero_rows<<<(unsigned)std::min(a.T, 4096), 256, 0, st>>>((char *)a.out.p, a.N * size, a.out.ld_t * size, a.T);
+        return cudaGetLastError();
+    }
+    if (a.out.type == DSTD_TYPE_F32) return run_mx4<float>(a, st);
+    if (a.out.type == DSTD_TYPE_BF16) return run_mx4<__nv_bfloat16>(a, st);
+    return run_mx4<__half>(a, st);
 }
 
 }  // namespace dstd

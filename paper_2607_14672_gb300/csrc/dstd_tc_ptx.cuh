@@ -377,6 +377,47 @@ static __device__ __forceinline__ uint64_t sdesc_sw128_mn(uint32_t saddr, uint32
     return d;
 }
 
+// 4-bit operands (E2M1) with a power of two for each block of 32 along K: D += A B^T for 64 columns of
+// K, both operands K-major in shared memory, their scales in TMEM (one 32-bit column for 32 rows and
+// 128 columns of K: sf_id 0 and 2 select the halves)
+static __device__ __forceinline__ void mma_mx4(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+                                               uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%5], [%6], p;\n"
+        "}\n" ::"r"(d_tmem),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb)
+        : "memory");
+}
+// 32 rows of 16 bytes from shared memory to 4 columns of TMEM, in all four quarters of the lanes; in
+// order with the mma of the same thread
+static __device__ __forceinline__ void tmem_cp_scales(uint32_t taddr, uint64_t sdesc) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
+}
+static __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint64_t *bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+                 "l"(src), "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
+}
+
+// rows of 16 bytes without swizzle, 8 rows to a 128-byte group, groups next to each other
+static __device__ __forceinline__ uint64_t sdesc_rows16(uint32_t saddr) {
+    uint64_t d = 0;
+    d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);  // start address >> 4
+    d |= (uint64_t)1 << 16;                    // LBO (not used: one group along K)
+    d |= (uint64_t)(128u >> 4) << 32;          // SBO
+    d |= (uint64_t)1 << 46;                    // descriptor version
+    return d;
+}
+
+// Instruction descriptor, kind::mxf4: E2M1 operands, power-of-two scales, fp32 sums
+static __host__ __device__ constexpr uint32_t idesc_mx4(int M, int N, int sf_id) {
+    return ((uint32_t)sf_id << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | (1u << 23) |
+           ((uint32_t)(M >> 4) << 24) | ((uint32_t)sf_id << 29);
+}
+
 // Instruction descriptor, kind::f16: D fp32, A and B both bf16 (format 1)
 // or both fp16 (format 0); A K-major, B K-major or (b_mn) MN-major.
 static __host__ __device__ constexpr uint32_t idesc_16bit(int M, int N, bool f16, bool b_mn = false) {
