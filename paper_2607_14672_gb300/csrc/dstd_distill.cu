@@ -11,46 +11,97 @@
 namespace dstd {
 namespace {
 
-template <class T>
-__device__ __forceinline__ float logit_of(float y, float factor, float none, bool &silent) {
-    const float z = factor * y;
-    silent = z == -INFINITY;
-    return silent ? none : z;
-}
+using tc::cluster_ctarank;
+using tc::cluster_sync;
+using tc::mapa_rank;
+using tc::smem_u32;
 
-// A row in 16-byte pieces from its first aligned address: packs cover
-// [head, head + packs P), up to P - 1 columns before and after them are taken singly.
+// exp2 as the special-function unit gives it (off by 2^-22 or so)
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+constexpr float kLog2e = 1.44269504f;
+
+struct Logit {
+    float factor, none;
+    __device__ __forceinline__ explicit Logit(const LogitArgs &a) : factor(a.factor), none(a.factor * a.silent) {}
+    __device__ __forceinline__ float of(float y, bool &silent) const {
+        const float z = factor * y;
+        silent = z == -INFINITY;
+        return silent ? none : z;
+    }
+    __device__ __forceinline__ float of(float y) const {
+        bool silent;
+        return of(y, silent);
+    }
+};
+
+// A block's share of a row, in 16-byte pieces from the row's first aligned address: packs
+// [first, last) at column head + k P. Up to P - 1 columns before and after all packs are
+// taken singly, by the first and the last share; columns [low, high) are the share's.
 template <class T>
 struct RowView {
+    static constexpr int P = Pack<T>::P;
     const T *row;
-    int cols, head, packs;
-    __device__ __forceinline__ RowView(const LogitArgs &a, long long r) {
-        constexpr int P = Pack<T>::P;
+    int cols, head, packs, first, last, low, high;
+    __device__ __forceinline__ RowView(const LogitArgs &a, long long r, int part = 0, int parts = 1) {
         row = static_cast<const T *>(a.y) + r * a.ld;
         cols = a.cols;
         head = min(cols, (int)((0 - reinterpret_cast<uintptr_t>(row) / sizeof(T)) & (P - 1)));
         packs = (cols - head) / P;
+        first = (int)((long long)packs * part / parts);
+        last = (int)((long long)packs * (part + 1) / parts);
+        low = part == 0 ? 0 : head + first * P;
+        high = part == parts - 1 ? cols : head + last * P;
     }
     // column of a thread's single element (t below 2 P), -1: none
     __device__ __forceinline__ int single(int t) const {
-        constexpr int P = Pack<T>::P;
-        if (t < P) return t < head ? t : -1;
-        const int c = head + packs * P + t - P;
-        return t < 2 * P && c < cols ? c : -1;
+        const int c = t < P ? t : head + packs * P + t - P;
+        return (t < P ? t < head : t < 2 * P) && c >= low && c < high ? c : -1;
     }
     __device__ __forceinline__ uint4 pack(int k) const {
-        return __ldg(reinterpret_cast<const uint4 *>(row + head + (long long)k * Pack<T>::P));
+        return __ldg(reinterpret_cast<const uint4 *>(row + head + (long long)k * P));
+    }
+};
+
+constexpr int kHeld = 8;  // packs of a thread in registers; those of longer rows are read in every pass
+
+template <class T, int THREADS>
+struct HeldRow {
+    uint4 raw[kHeld];
+    float one;
+    int at;  // column of `one`, or -1
+    __device__ __forceinline__ HeldRow(const RowView<T> &v) {
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) {
+            const int k = v.first + j * THREADS + (int)threadIdx.x;
+            raw[j] = k < v.last ? v.pack(k) : make_uint4(0, 0, 0, 0);
+        }
+        at = v.single(threadIdx.x);
+        one = at >= 0 ? to_f32<T>(v.row[at]) : 0.f;
+    }
+    // f(pack, its number) for every pack of this thread
+    template <class F>
+    __device__ __forceinline__ void each(const RowView<T> &v, F f) const {
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) {
+            const int k = v.first + j * THREADS + (int)threadIdx.x;
+            if (k < v.last) f(raw[j], k);
+        }
+        for (int k = v.first + kHeld * THREADS + (int)threadIdx.x; k < v.last; k += THREADS) f(v.pack(k), k);
     }
 };
 
 // ---------------------------------------------------------------------------
 // The K largest logits of a row, descending, equal ones by ascending column. The
 // logits are ordered as 32-bit keys (-0 as 0, NaN above all). Each thread takes
-// the largest of its columns; the K-th largest of those is a bound that no
-// smaller logit of the row can be among the K largest below, and few are above
-// it: with 1024 threads about K. Those are gathered and put in order by counting,
-// for each, the larger ones. Rows with more than CAP logits at the bound (many equal
-// ones) go digit by digit.
+// the largest of its columns; the K-th largest of those is a bound that none of
+// the row's K largest is below, and few are above it: with 512 threads and K = 64
+// about 68. Those are gathered and put in order by counting, for each, the larger ones. Rows
+// with more than kCap logits at the bound (many equal ones) go digit by digit. Few long rows
+// are shared by the blocks of a cluster, which then count each other's.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t key_of(float z) {
     if (z != z) return 0xffffffffu;
@@ -63,48 +114,51 @@ __device__ __forceinline__ float logit_of_key(uint32_t k) {
 
 constexpr int kCap = 2048;
 
+__device__ __forceinline__ uint64_t ld_cluster64(uint32_t addr) {
+    uint64_t v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(addr) : "memory");
+    return v;
+}
+
 template <class T, int THREADS>
-__global__ void __launch_bounds__(THREADS) k_top_logits(const LogitArgs a, const int K, float *top, int32_t *index) {
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS)
+    k_top_logits(const LogitArgs a, const int parts, const int K, float *top, int32_t *index) {
     constexpr int P = Pack<T>::P;
-    __shared__ uint64_t s_cand[kCap];
+    __shared__ uint64_t s_cand[kCap], s_best[kTopMax];
     __shared__ unsigned s_n, s_hist[256], s_digit[2], s_warp[THREADS / 32];
-    const int t = threadIdx.x;
-    const long long r = blockIdx.x;
-    const RowView<T> v(a, r);
-    const float none = a.factor * a.silent;
-    const auto key = [&](float y) {
-        bool silent;
-        return key_of(logit_of<T>(y, a.factor, none, silent));
-    };
-    // every column once, in any order
-    const auto each = [&](auto f) {
-        const int c = v.single(t);
-        if (c >= 0) f(c, key(to_f32<T>(v.row[c])));
-        for (int k = t; k < v.packs; k += THREADS) {
-            const uint4 w = v.pack(k);
-#pragma unroll
-            for (int i = 0; i < P; ++i) f(v.head + k * P + i, key(Pack<T>::one(w, i)));
-        }
-    };
+    const int t = threadIdx.x, part = parts > 1 ? (int)cluster_ctarank() : 0;
+    const long long r = blockIdx.x / parts;
+    const RowView<T> v(a, r, part, parts);
+    const HeldRow<T, THREADS> h(v);
+    const Logit logit(a);
     if (t == 0) s_n = 0;
+    // every column of the share once, in any order
+    const auto each = [&](auto f) {
+        if (h.at >= 0) f(h.at, key_of(logit.of(h.one)));
+        h.each(v, [&](const uint4 &w, int k) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) f(v.head + k * P + i, key_of(logit.of(Pack<T>::one(w, i))));
+        });
+    };
+    const int want = min(K, v.high - v.low);
     uint32_t mine = 0, bound = 0;
     each([&](int, uint32_t k) { mine = max(mine, k); });
     for (int bit = 31; bit >= 0; --bit) {
         const uint32_t trial = bound | (1u << bit);
-        if (__syncthreads_count(mine >= trial) >= K) bound = trial;
+        if (__syncthreads_count(mine >= trial) >= want) bound = trial;
     }
-    __syncthreads();
-    each([&](int c, uint32_t k) {
-        if (k >= bound) {
-            const unsigned at = atomicAdd(&s_n, 1u);
-            if (at < kCap) s_cand[at] = (uint64_t)k << 32 | (uint32_t)~c;
-        }
-    });
+    if (mine >= bound)
+        each([&](int c, uint32_t k) {
+            if (k >= bound) {
+                const unsigned at = atomicAdd(&s_n, 1u);
+                if (at < kCap) s_cand[at] = (uint64_t)k << 32 | (uint32_t)~c;
+            }
+        });
     __syncthreads();
     unsigned n = s_n;
     if (n > kCap) {
         uint32_t prefix = 0, mask = 0;
-        unsigned need = K;
+        unsigned need = want;
         for (int shift = 24; shift >= 0; shift -= 8) {
             for (int i = t; i < 256; i += THREADS) s_hist[i] = 0;
             __syncthreads();
@@ -130,10 +184,10 @@ __global__ void __launch_bounds__(THREADS) k_top_logits(const LogitArgs a, const
         each([&](int c, uint32_t k) {
             if (k > prefix) s_cand[atomicAdd(&s_n, 1u)] = (uint64_t)k << 32 | (uint32_t)~c;
         });
-        // the first `need` columns of those equal to the K-th
+        // the first `need` columns of those equal to the last one wanted
         unsigned found = 0;
-        for (long long c0 = 0; c0 < v.cols && found < need; c0 += THREADS) {
-            const bool here = c0 + t < v.cols && key(to_f32<T>(v.row[c0 + t])) == prefix;
+        for (int c0 = v.low; c0 < v.high && found < need; c0 += THREADS) {
+            const bool here = c0 + t < v.high && key_of(logit.of(to_f32<T>(v.row[c0 + t]))) == prefix;
             const unsigned ballot = __ballot_sync(0xffffffffu, here);
             if ((t & 31) == 0) s_warp[t >> 5] = __popc(ballot);
             __syncthreads();
@@ -143,29 +197,82 @@ __global__ void __launch_bounds__(THREADS) k_top_logits(const LogitArgs a, const
                 all += s_warp[w];
             }
             before += __popc(ballot & ((1u << (t & 31)) - 1u));
-            if (here && before < need) s_cand[K - need + before] = (uint64_t)prefix << 32 | (uint32_t)~(uint32_t)(c0 + t);
+            if (here && before < need) s_cand[want - need + before] = (uint64_t)prefix << 32 | (uint32_t)~(uint32_t)(c0 + t);
             found = all;
             __syncthreads();
         }
-        n = K;
+        n = want;
         __syncthreads();
     }
+    const auto put = [&](uint64_t e, int rank) {
+        if (rank >= K) return;
+        top[r * K + rank] = logit_of_key((uint32_t)(e >> 32));
+        index[r * K + rank] = (int32_t)~(uint32_t)e;
+    };
     for (unsigned i = t; i < n; i += THREADS) {
         const uint64_t me = s_cand[i];
         int rank = 0;
         for (unsigned j = 0; j < n; ++j) rank += s_cand[j] > me;
-        if (rank < K) {
-            top[r * K + rank] = logit_of_key((uint32_t)(me >> 32));
-            index[r * K + rank] = (int32_t)~(uint32_t)me;
+        if (parts == 1) put(me, rank);
+        else if (rank < K) s_best[rank] = me;
+    }
+    if (parts > 1) {
+        if (t >= want && t < K) s_best[t] = 0;  // below every entry
+        __syncwarp();
+        cluster_sync();
+        // all shares' entries, in the blocks' order
+        for (int i = t; i < parts * K; i += THREADS)
+            s_cand[i] = ld_cluster64(mapa_rank(smem_u32(s_best + i % K), (uint32_t)(i / K)));
+        __syncwarp();
+        cluster_sync();
+        if (t < want) {
+            const uint64_t me = s_best[t];
+            int rank = t;
+            for (int q = 0; q < parts && rank < K; ++q) {
+                if (q == part) continue;
+                int lo = 0, hi = K;  // entries above me
+                while (lo < hi) {
+                    const int mid = (lo + hi) / 2;
+                    if (s_cand[q * K + mid] > me) lo = mid + 1;
+                    else hi = mid;
+                }
+                rank += lo;
+            }
+            put(me, rank);
         }
     }
 }
 
+// blocks that share a row: where the rows alone do not fill the GPU, up to 8 of at least `least` packs
+int shares(int rows, int packs, int least) {
+    int parts = 1;
+    while (parts < 8 && rows * 2ll * parts <= 304 && packs >= 2 * parts * least) parts *= 2;
+    return parts;
+}
+
+template <class... P, class... A>
+cudaError_t launch_shared(void (*kernel)(P...), int rows, int parts, int threads, cudaStream_t st, const A &...args) {
+    if ((long long)rows * parts > 0x7fffffff) return cudaErrorInvalidValue;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)parts;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = parts > 1 ? 1 : 0;
+    cfg.gridDim = dim3((unsigned)(rows * parts));
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.stream = st;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 template <class T>
 cudaError_t top_logits(const LogitArgs &a, int K, float *top, int32_t *index, cudaStream_t st) {
-    if (a.cols <= 8192) k_top_logits<T, 256><<<(unsigned)a.rows, 256, 0, st>>>(a, K, top, index);
-    else k_top_logits<T, 1024><<<(unsigned)a.rows, 1024, 0, st>>>(a, K, top, index);
-    return cudaGetLastError();
+    const int packs = (int)(((long long)a.cols * sizeof(T) + 15) / 16), parts = shares(a.rows, packs, 512);
+    if (packs / parts <= 256 * kHeld)
+        return launch_shared(k_top_logits<T, 256>, a.rows, parts, 256, st, a, parts, K, top, index);
+    return launch_shared(k_top_logits<T, 512>, a.rows, parts, 512, st, a, parts, K, top, index);
 }
 
 // ---------------------------------------------------------------------------
@@ -173,200 +280,101 @@ cudaError_t top_logits(const LogitArgs &a, int K, float *top, int32_t *index, cu
 // and q = softmax of its logits:
 //     L_r = sum_k p_k (log p_k - log q_{i_k}),
 //     dL_r / dy_c = factor (q_c - sum_{k: i_k = c} p_k)   (0 where silent).
-// The first pass takes the largest logit m and sum_c exp(z_c - m), rescaling when
-// m grows; the second writes exp(z - m) times a constant. The few columns that
-// the teacher names are written once more, from fp32, so that every gradient is
-// rounded once; entries of the same column are added up in their order.
+// A row is read once and stays in registers: the largest logit and the sum of
+// exp(z - largest), by warps, then over the block (or the cluster that shares the row), then exp(z - m)
+// times a constant. The few columns that the teacher names are written once
+// more, from fp32, so that every gradient is rounded once; entries of the
+// same column are added up in their order.
 // ---------------------------------------------------------------------------
+struct Teacher {
+    int at;       // column of this thread's entry, -1: none
+    float log_p, p, mass, z, old;
+    bool silent, first, any;
+};
+
+// one entry a lane: entries [32 w, 32 w + 32) of the row to warp w; every warp goes through all of them
 template <class T>
-__device__ __forceinline__ float exp_of(float x) {
-    if constexpr (sizeof(T) == 4) return expf(x);
-    else return __expf(x);  // off by 2^-21 or so near 0, far below a 16-bit rounding
+__device__ __forceinline__ Teacher teacher_of(const DistillArgs &a, const Logit &logit, const T *row, const T *g,
+                                              long long r, int w, int lane) {
+    const auto entry = [&](int k, int &at) {
+        at = k < a.K ? a.index[r * a.K + k] : -1;
+        const float z = k < a.K ? a.teacher_factor * a.top[r * a.K + k] : -INFINITY;
+        if (at < 0 || at >= a.y.cols || z == -INFINITY) at = -1;
+        return z;
+    };
+    Teacher t;
+    const float mine = entry(32 * w + lane, t.at);
+    t.silent = false;
+    t.z = t.old = 0.f;
+    if (t.at >= 0) {
+        t.z = logit.of(to_f32<T>(row[t.at]), t.silent);
+        if (a.accumulate && g) t.old = to_f32<T>(g[t.at]);
+    }
+    float m = -INFINITY;
+    for (int k = lane; k < a.K; k += 32) {
+        int at;
+        const float z = entry(k, at);
+        if (at >= 0) m = fmaxf(m, z);
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    float sum = 0.f, same = 0.f;
+    bool any = false;
+    t.first = t.at >= 0;
+    for (int k0 = 0; k0 < a.K; k0 += 32) {
+        int at;
+        const float z = entry(k0 + lane, at), e = at >= 0 ? expf(z - m) : 0.f;
+        sum += e;
+        any = any || at >= 0;
+        if (__any_sync(0xffffffffu, at >= 0 && t.at >= 0))
+            for (int j = 0; j < 32; ++j) {
+                const int other = __shfl_sync(0xffffffffu, at, j);
+                const float oe = __shfl_sync(0xffffffffu, e, j);
+                if (other >= 0 && other == t.at) {
+                    same += oe;
+                    if (k0 + j < 32 * w + lane) t.first = false;
+                }
+            }
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    t.any = __any_sync(0xffffffffu, any);
+    t.log_p = mine - m - logf(sum);
+    t.p = expf(t.log_p);
+    t.mass = same / sum;
+    return t;
+}
+// this entry's share of the row's loss, given the log of the softmax's denominator
+__device__ __forceinline__ float teacher_loss(const Teacher &t, float m, float log_sum) {
+    return t.at >= 0 && t.p != 0.f ? t.p * (t.log_p - (t.z - m - log_sum)) : 0.f;
 }
 
-template <int THREADS>
-__device__ __forceinline__ void group_sync() {
-    if constexpr (THREADS == 32) __syncwarp();
-    else __syncthreads();
-}
-template <int THREADS>
-__device__ __forceinline__ float group_sum(float v, float *s_part) {
+// largest and sum of (m, s) pairs of all lanes
+__device__ __forceinline__ void join_lanes(float &m, float &s) {
+    const float own = m;
 #pragma unroll
-    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-    if constexpr (THREADS > 32) {
-        const int t = threadIdx.x;
-        __syncthreads();
-        if ((t & 31) == 0) s_part[t >> 5] = v;
-        __syncthreads();
-        v = s_part[0];
-        for (int i = 1; i < THREADS / 32; ++i) v += s_part[i];
-    }
-    return v;
-}
-template <int THREADS>
-__device__ __forceinline__ float group_max(float v, float *s_part) {
+    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    // an infinite m has nothing to rescale: such a sum is 0 or already NaN
+    s = own == m ? s : s * expf(own - m);
 #pragma unroll
-    for (int d = 16; d; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
-    if constexpr (THREADS > 32) {
-        const int t = threadIdx.x;
-        __syncthreads();
-        if ((t & 31) == 0) s_part[t >> 5] = v;
-        __syncthreads();
-        v = s_part[0];
-        for (int i = 1; i < THREADS / 32; ++i) v = fmaxf(v, s_part[i]);
-    }
-    return v;
+    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
 }
 
-// THREADS to a row: a warp, 8 rows to a block, or a whole block. VEC: y's and g's
-// rows have their aligned 16 bytes at the same columns.
-template <class T, int THREADS, bool VEC>
-__global__ void __launch_bounds__(THREADS == 32 ? 256 : THREADS) k_distill(const DistillArgs a) {
-    constexpr int P = Pack<T>::P, ROWS = THREADS == 32 ? 8 : 1;
-    __shared__ float s_p[ROWS][kTopMax];
-    __shared__ int s_at[ROWS][kTopMax];
-    __shared__ float s_part[32];
+// the last block adds the rows' losses up, in a fixed order
+__device__ __forceinline__ void finish_loss(const DistillArgs &a, unsigned blocks) {
     __shared__ double s_total[32];
     __shared__ unsigned s_last;
-    const int t = threadIdx.x % THREADS, sub = threadIdx.x / THREADS;
-    const long long r = (long long)blockIdx.x * ROWS + sub;
-    const LogitArgs &y = a.y;
-    const float none = y.factor * y.silent;
-    if (r < y.rows) {
-        const RowView<T> v(y, r);
-        const float rw = a.row_weight ? a.row_weight[r] : 1.f / (float)y.rows;
-        float *p = s_p[sub];
-        int *at = s_at[sub];
-        // the teacher's softmax
-        float m = -INFINITY;
-        for (int k = t; k < a.K; k += THREADS) {
-            const int i = a.index[r * a.K + k];
-            const float z = a.teacher_factor * a.top[r * a.K + k];
-            const bool used = i >= 0 && i < y.cols && z != -INFINITY;
-            at[k] = used ? i : -1;
-            p[k] = z;
-            if (used) m = fmaxf(m, z);
-        }
-        m = group_max<THREADS>(m, s_part);
-        float s = 0.f;
-        for (int k = t; k < a.K; k += THREADS)
-            if (at[k] >= 0) s += expf(p[k] - m);
-        s = group_sum<THREADS>(s, s_part);
-        const bool any = group_max<THREADS>([&] {
-            float u = 0.f;
-            for (int k = t; k < a.K; k += THREADS) u = at[k] >= 0 ? 1.f : u;
-            return u;
-        }(), s_part) > 0.f;
-        const bool taught = any && rw != 0.f;
-        const float t_max = m, t_log = logf(s);
-        // the row's largest logit and its sum
-        float z_max = -INFINITY, z_sum = 0.f;
-        const auto take = [&](float yv) {
-            bool silent;
-            const float z = logit_of<T>(yv, y.factor, none, silent);
-            if (z > z_max) {
-                z_sum *= expf(z_max - z);
-                z_max = z;
-            }
-            z_sum += z == -INFINITY ? 0.f : exp_of<T>(z - z_max);
-        };
-        if (taught) {
-            for (int c = t; c < 2 * P; c += THREADS) {
-                const int i = v.single(c);
-                if (i >= 0) take(to_f32<T>(v.row[i]));
-            }
-            for (int k = t; k < v.packs; k += THREADS) {
-                const uint4 w = v.pack(k);
-#pragma unroll
-                for (int i = 0; i < P; ++i) take(Pack<T>::one(w, i));
-            }
-        }
-        const float row_max = group_max<THREADS>(z_max, s_part);
-        z_sum = group_sum<THREADS>(z_max == row_max ? z_sum : z_sum * expf(z_max - row_max), s_part);
-        // a row without logits has no softmax: it is left out (a NaN counts as a logit)
-        const bool empty = row_max == -INFINITY && !(z_sum != z_sum);
-        const float z_log = logf(z_sum);
-        const bool done = taught && !empty;
-        float part = 0.f;
-        if (done)
-            for (int k = t; k < a.K; k += THREADS) {
-                if (at[k] < 0) continue;
-                bool silent;
-                const float z = logit_of<T>(to_f32<T>(v.row[at[k]]), y.factor, none, silent);
-                const float log_p = p[k] - t_max - t_log, pk = expf(log_p);
-                if (pk != 0.f) part += pk * (log_p - (z - row_max - z_log));
-                p[k] = pk;
-            }
-        const float loss = group_sum<THREADS>(part, s_part);
-        if (t == 0) a.row_loss[r] = loss;
-        if (a.g && (done || !a.accumulate)) {
-            T *g = static_cast<T *>(a.g) + r * a.ld_g;
-            const float coef = a.weight * rw * y.factor, scale = done ? coef / z_sum : 0.f;
-            const auto grad = [&](float yv, float old) {
-                bool silent;
-                const float z = logit_of<T>(yv, y.factor, none, silent);
-                return old + (silent || !done ? 0.f : exp_of<T>(z - row_max) * scale);
-            };
-            // what the named columns hold before they are written
-            constexpr int EACH = kTopMax / THREADS > 0 ? kTopMax / THREADS : 1;
-            float old[EACH];
-#pragma unroll
-            for (int e = 0; e < EACH; ++e) {
-                const int k = e * THREADS + t;
-                old[e] = k < a.K && at[k] >= 0 && a.accumulate ? to_f32<T>(g[at[k]]) : 0.f;
-            }
-            group_sync<THREADS>();
-            if constexpr (VEC) {
-                for (int c = t; c < 2 * P; c += THREADS) {
-                    const int i = v.single(c);
-                    if (i >= 0) g[i] = round_out<T>(grad(to_f32<T>(v.row[i]), a.accumulate ? to_f32<T>(g[i]) : 0.f));
-                }
-                for (int k = t; k < v.packs; k += THREADS) {
-                    const uint4 w = v.pack(k);
-                    uint4 *dst = reinterpret_cast<uint4 *>(g + v.head + (long long)k * P);
-                    uint4 was = make_uint4(0, 0, 0, 0);
-                    if (a.accumulate) was = *dst;
-                    alignas(16) T out[P];
-#pragma unroll
-                    for (int i = 0; i < P; ++i) out[i] = round_out<T>(grad(Pack<T>::one(w, i), Pack<T>::one(was, i)));
-                    *dst = *reinterpret_cast<const uint4 *>(out);
-                }
-            } else {
-                for (long long c = t; c < v.cols; c += THREADS)
-                    g[c] = round_out<T>(grad(to_f32<T>(v.row[c]), a.accumulate ? to_f32<T>(g[c]) : 0.f));
-            }
-            group_sync<THREADS>();
-            if (done) {
-#pragma unroll
-                for (int e = 0; e < EACH; ++e) {
-                    const int k = e * THREADS + t;
-                    if (k >= a.K || at[k] < 0) continue;
-                    const int c = at[k];
-                    bool first = true;
-                    for (int j = 0; j < k; ++j) first = first && at[j] != c;
-                    if (!first) continue;
-                    float mass = p[k];
-                    for (int j = k + 1; j < a.K; ++j)
-                        if (at[j] == c) mass += p[j];
-                    bool silent;
-                    const float z = logit_of<T>(to_f32<T>(v.row[c]), y.factor, none, silent);
-                    if (!silent) g[c] = round_out<T>(old[e] + (expf(z - row_max) / z_sum - mass) * coef);
-                }
-            }
-        }
-    }
-    // the last block adds the rows' losses up, in a fixed order
     __syncthreads();
     if (threadIdx.x == 0) {
         __threadfence();
-        s_last = atomicAdd(reinterpret_cast<unsigned *>(a.loss + 1), 1u) == gridDim.x - 1;
+        s_last = atomicAdd(reinterpret_cast<unsigned *>(a.loss + 1), 1u) == blocks - 1;
     }
     __syncthreads();
     if (!s_last) return;
     __threadfence();
     double sum = 0.0;
-    for (long long i = threadIdx.x; i < y.rows; i += blockDim.x) {
-        const float w = a.row_weight ? a.row_weight[i] : 1.f / (float)y.rows;
+    for (long long i = threadIdx.x; i < a.y.rows; i += blockDim.x) {
+        const float w = a.row_weight ? a.row_weight[i] : 1.f / (float)a.y.rows;
         if (w != 0.f) sum += (double)w * __ldcg(a.row_loss + i);
     }
 #pragma unroll
@@ -381,23 +389,208 @@ __global__ void __launch_bounds__(THREADS == 32 ? 256 : THREADS) k_distill(const
     }
 }
 
+// Rows of up to 256 classes and 64 entries: a warp to a row, 8 columns a lane.
+template <class T>
+__global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
+    constexpr int E = 8;
+    const int lane = threadIdx.x & 31;
+    const long long r = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (r < a.y.rows) {
+        const Logit logit(a.y);
+        const T *row = static_cast<const T *>(a.y.y) + r * a.y.ld;
+        T *g = a.g ? static_cast<T *>(a.g) + r * a.ld_g : nullptr;
+        const float rw = a.row_weight ? a.row_weight[r] : 1.f / (float)a.y.rows;
+        float z[E], was[E];
+        bool silent[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const int c = lane + 32 * i;
+            silent[i] = true;
+            z[i] = c < a.y.cols ? logit.of(to_f32<T>(row[c]), silent[i]) : -INFINITY;
+            was[i] = a.accumulate && g && c < a.y.cols ? to_f32<T>(g[c]) : 0.f;
+        }
+        const Teacher t0 = teacher_of<T>(a, logit, row, g, r, 0, lane);
+        Teacher t1;
+        t1.at = -1;
+        if (a.K > 32) t1 = teacher_of<T>(a, logit, row, g, r, 1, lane);
+        float m = -INFINITY, s = 0.f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) m = fmaxf(m, z[i]);
+#pragma unroll
+        for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+#pragma unroll
+        for (int i = 0; i < E; ++i) s += z[i] == -INFINITY ? 0.f : expf(z[i] - m);
+#pragma unroll
+        for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+        // a row without logits has no softmax: it is left out (a NaN counts as a logit)
+        const bool done = t0.any && rw != 0.f && !(m == -INFINITY && !(s != s));
+        float loss = 0.f;
+        if (done) {
+            const float log_sum = logf(s);
+            loss = teacher_loss(t0, m, log_sum);
+            if (a.K > 32) loss += teacher_loss(t1, m, log_sum);
+        }
+#pragma unroll
+        for (int d = 16; d; d >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, d);
+        if (lane == 0) a.row_loss[r] = loss;
+        if (g && (done || !a.accumulate)) {
+            const float coef = a.weight * rw * logit.factor;
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const int c = lane + 32 * i;
+                if (c < a.y.cols)
+                    g[c] = round_out<T>(was[i] + (silent[i] || !done ? 0.f : expf(z[i] - m) * (coef / s)));
+            }
+            __syncwarp();
+            if (done) {
+                const auto named = [&](const Teacher &t) {
+                    if (t.at >= 0 && t.first && !t.silent)
+                        g[t.at] = round_out<T>(t.old + (expf(t.z - m) / s - t.mass) * coef);
+                };
+                named(t0);
+                if (a.K > 32) named(t1);
+            }
+        }
+    }
+    finish_loss(a, gridDim.x);
+}
+
+// FAST: 16-bit outputs without a stand-in for silent ones, whose exp is 0 by
+// itself: exp(z - m) = 2^(factor log2(e) y - m log2(e)), one multiply-add and the
+// special-function unit (the product's rounding moves it by 2^-24 |z|, far below a 16-bit rounding).
+template <class T, int THREADS, bool FAST>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill(const DistillArgs a, const int parts) {
+    constexpr int P = Pack<T>::P, WARPS = THREADS / 32;
+    __shared__ float2 s_stat[WARPS], s_share[8];
+    __shared__ float s_loss[kTopMax / 32];
+    __shared__ int s_any;
+    const int t = threadIdx.x, warp = t >> 5, lane = t & 31, part = parts > 1 ? (int)cluster_ctarank() : 0;
+    const long long r = blockIdx.x / parts;
+    const RowView<T> v(a.y, r, part, parts);
+    const HeldRow<T, THREADS> h(v);
+    const Logit logit(a.y);
+    T *g = a.g ? static_cast<T *>(a.g) + r * a.ld_g : nullptr;
+    const float rw = a.row_weight ? a.row_weight[r] : 1.f / (float)a.y.rows;
+    Teacher teach;
+    teach.at = -1;
+    if (warp * 32 < a.K) {
+        teach = teacher_of<T>(a, logit, v.row, g, r, warp, lane);
+        if (t == 0) s_any = teach.any;
+    }
+    // largest logit and sum, over the warp's columns
+    float m = -INFINITY, s = 0.f;
+    const float scale = logit.factor * kLog2e;
+    if (h.at >= 0) m = logit.of(h.one);
+    h.each(v, [&](const uint4 &w, int) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) m = fmaxf(m, FAST ? logit.factor * Pack<T>::one(w, i) : logit.of(Pack<T>::one(w, i)));
+    });
+#pragma unroll
+    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    // nothing but -infinity: every exp below is 0 with any finite m (NaN stays NaN)
+    float base = m == -INFINITY ? 0.f : m;
+    const auto exp_of = [&](float y) {
+        if constexpr (FAST) return exp2_fast(fmaf(y, scale, -base * kLog2e));
+        else return expf(logit.of(y) - base);
+    };
+    if (h.at >= 0) s = exp_of(h.one);
+    h.each(v, [&](const uint4 &w, int) {
+        float part_sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < P; ++i) part_sum += exp_of(Pack<T>::one(w, i));
+        s += part_sum;
+    });
+#pragma unroll
+    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+    if (lane == 0) s_stat[warp] = make_float2(m, s);
+    __syncthreads();
+    const bool any = s_any != 0;
+    {
+        const float2 w = lane < WARPS ? s_stat[lane] : make_float2(-INFINITY, 0.f);
+        m = w.x;
+        s = w.y;
+        join_lanes(m, s);
+    }
+    if (parts > 1) {
+        if (t < parts) {
+            const uint32_t to = mapa_rank(smem_u32(s_share + part), (uint32_t)t);
+            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(m), "f"(s) : "memory");
+        }
+        __syncwarp();
+        cluster_sync();
+        const float2 w = lane < parts ? s_share[lane] : make_float2(-INFINITY, 0.f);
+        m = w.x;
+        s = w.y;
+        join_lanes(m, s);
+    }
+    // a row without logits has no softmax: it is left out (a NaN counts as a logit)
+    const bool done = any && rw != 0.f && !(m == -INFINITY && !(s != s));
+    base = m == -INFINITY ? 0.f : m;
+    if (warp * 32 < a.K) {
+        float loss = done ? teacher_loss(teach, m, logf(s)) : 0.f;
+#pragma unroll
+        for (int d = 16; d; d >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, d);
+        if (lane == 0) s_loss[warp] = loss;
+    }
+    const float coef = a.weight * rw * logit.factor, over = done ? coef / s : 0.f;
+    const auto grad = [&](float y, float old) {
+        if (!done) return old;
+        if constexpr (FAST) return fmaf(exp_of(y), over, old);
+        bool silent;
+        const float z = logit.of(y, silent);
+        return silent ? old : old + expf(z - base) * over;
+    };
+    if (g && (done || !a.accumulate)) {
+        if (h.at >= 0) g[h.at] = round_out<T>(grad(h.one, a.accumulate ? to_f32<T>(g[h.at]) : 0.f));
+        T *dst = g + v.head;
+        if ((reinterpret_cast<uintptr_t>(dst) & 15) == 0) {
+            h.each(v, [&](const uint4 &w, int k) {
+                uint4 *to = reinterpret_cast<uint4 *>(dst + (long long)k * P);
+                uint4 was = make_uint4(0, 0, 0, 0);
+                if (a.accumulate) was = *to;
+                alignas(16) T out[P];
+#pragma unroll
+                for (int i = 0; i < P; ++i) out[i] = round_out<T>(grad(Pack<T>::one(w, i), Pack<T>::one(was, i)));
+                *to = *reinterpret_cast<const uint4 *>(out);
+            });
+        } else {
+            h.each(v, [&](const uint4 &w, int k) {
+                T *to = dst + (long long)k * P;
+#pragma unroll
+                for (int i = 0; i < P; ++i)
+                    to[i] = round_out<T>(grad(Pack<T>::one(w, i), a.accumulate ? to_f32<T>(to[i]) : 0.f));
+            });
+        }
+    }
+    __syncthreads();
+    if (g && done && teach.at >= 0 && teach.first && !teach.silent && teach.at >= v.low && teach.at < v.high)
+        g[teach.at] = round_out<T>(teach.old + (expf(teach.z - m) / s - teach.mass) * coef);
+    if (part == 0) {
+        if (t == 0) {
+            float loss = s_loss[0];
+            for (int w = 1; w * 32 < a.K; ++w) loss += s_loss[w];
+            a.row_loss[r] = loss;
+        }
+        finish_loss(a, gridDim.x / parts);
+    }
+}
+
+template <class T, bool FAST>
+cudaError_t distill_rows(const DistillArgs &a, cudaStream_t st) {
+    const int packs = (int)(((long long)a.y.cols * sizeof(T) + 15) / 16), parts = shares(a.y.rows, packs, 512);
+    if (packs / parts <= 256 * kHeld) return launch_shared(k_distill<T, 256, FAST>, a.y.rows, parts, 256, st, a, parts);
+    return launch_shared(k_distill<T, 512, FAST>, a.y.rows, parts, 512, st, a, parts);
+}
+
 template <class T>
 cudaError_t distill(const DistillArgs &a, cudaStream_t st) {
-    constexpr int P = Pack<T>::P;
-    const auto phase = [](const void *p) { return (long long)(reinterpret_cast<uintptr_t>(p) / sizeof(T)); };
-    const bool vec = !a.g || (((phase(a.y.y) - phase(a.g)) | (a.y.ld - a.ld_g)) & (P - 1)) == 0;
-    const unsigned rows = (unsigned)a.y.rows;
-    if (a.y.cols <= 1024 && a.K <= 64) {
-        if (vec) k_distill<T, 32, true><<<(rows + 7) / 8, 256, 0, st>>>(a);
-        else k_distill<T, 32, false><<<(rows + 7) / 8, 256, 0, st>>>(a);
-    } else if (a.y.cols <= 8192) {
-        if (vec) k_distill<T, 256, true><<<rows, 256, 0, st>>>(a);
-        else k_distill<T, 256, false><<<rows, 256, 0, st>>>(a);
-    } else {
-        if (vec) k_distill<T, 1024, true><<<rows, 1024, 0, st>>>(a);
-        else k_distill<T, 1024, false><<<rows, 1024, 0, st>>>(a);
+    if (a.y.cols <= 256 && a.K <= 64) {
+        k_distill_small<T><<<((unsigned)a.y.rows + 7) / 8, 256, 0, st>>>(a);
+        return cudaGetLastError();
     }
-    return cudaGetLastError();
+    if constexpr (sizeof(T) == 2)
+        if (a.y.factor * a.y.silent == -INFINITY && fabsf(a.y.factor) < 1e30f) return distill_rows<T, true>(a, st);
+    return distill_rows<T, false>(a, st);
 }
 
 }  // namespace
