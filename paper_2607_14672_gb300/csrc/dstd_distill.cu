@@ -112,6 +112,19 @@ __device__ __forceinline__ float logit_of_key(uint32_t k) {
     return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k);
 }
 
+// the larger of two, NaN if either is
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+template <class T>
+struct Two;  // two 16-bit values in a word
+template <>
+struct Two<__half> { using type = __half2; };
+template <>
+struct Two<__nv_bfloat16> { using type = __nv_bfloat162; };
+
 constexpr int kCap = 2048;
 
 __device__ __forceinline__ uint64_t ld_cluster64(uint32_t addr) {
@@ -120,18 +133,52 @@ __device__ __forceinline__ uint64_t ld_cluster64(uint32_t addr) {
     return v;
 }
 
-template <class T, int THREADS>
+// Largest logit of a pack. PAIRS (16-bit outputs, none of whose logits is a stand-in): the order of
+// the logits is that of the outputs, or of the negated ones (flip), and two are compared at once.
+// Without WITH_NAN a NaN is passed over, unless there is nothing else.
+template <class T, bool PAIRS, bool WITH_NAN>
+struct PackMax {
+    Logit logit;
+    uint32_t flip;
+    __device__ __forceinline__ explicit PackMax(const Logit &l) : logit(l), flip(l.factor < 0.f ? 0x80008000u : 0u) {}
+    __device__ __forceinline__ float operator()(const uint4 &w) const {
+        if constexpr (PAIRS) {
+            using V = typename Two<T>::type;
+            const uint32_t u[4] = {w.x ^ flip, w.y ^ flip, w.z ^ flip, w.w ^ flip};
+            const V *v = reinterpret_cast<const V *>(u);
+            if constexpr (WITH_NAN) {
+                const V m = __hmax2_nan(__hmax2_nan(v[0], v[1]), __hmax2_nan(v[2], v[3]));
+                return fabsf(logit.factor) * to_f32<T>(__hmax_nan(m.x, m.y));
+            } else {
+                const V m = __hmax2(__hmax2(v[0], v[1]), __hmax2(v[2], v[3]));
+                return fabsf(logit.factor) * to_f32<T>(__hmax(m.x, m.y));
+            }
+        } else {
+            float m = logit.of(Pack<T>::one(w, 0));
+#pragma unroll
+            for (int i = 1; i < Pack<T>::P; ++i) {
+                const float z = logit.of(Pack<T>::one(w, i));
+                m = WITH_NAN ? max_nan(m, z) : fmaxf(m, z);
+            }
+            return m;
+        }
+    }
+};
+
+template <class T, int THREADS, bool PAIRS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
     k_top_logits(const LogitArgs a, const int parts, const int K, float *top, int32_t *index) {
     constexpr int P = Pack<T>::P;
     __shared__ uint64_t s_cand[kCap], s_best[kTopMax];
-    __shared__ unsigned s_n, s_hist[256], s_digit[2], s_warp[THREADS / 32];
+    __shared__ unsigned s_n, s_hits, s_hist[256], s_digit[2], s_warp[THREADS / 32];
+    __shared__ int s_hit[kCap];
     const int t = threadIdx.x, part = parts > 1 ? (int)cluster_ctarank() : 0;
     const long long r = blockIdx.x / parts;
     const RowView<T> v(a, r, part, parts);
     const HeldRow<T, THREADS> h(v);
     const Logit logit(a);
-    if (t == 0) s_n = 0;
+    const PackMax<T, PAIRS, true> pack_max(logit);
+    if (t == 0) s_n = s_hits = 0;
     // every column of the share once, in any order
     const auto each = [&](auto f) {
         if (h.at >= 0) f(h.at, key_of(logit.of(h.one)));
@@ -141,19 +188,47 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
         });
     };
     const int want = min(K, v.high - v.low);
-    uint32_t mine = 0, bound = 0;
-    each([&](int, uint32_t k) { mine = max(mine, k); });
-    for (int bit = 31; bit >= 0; --bit) {
+    uint32_t mine = 0, bound = 0;  // 0: below every logit's key
+    {
+        float m = -INFINITY;
+        bool some = h.at >= 0;
+        if (some) m = logit.of(h.one);
+        h.each(v, [&](const uint4 &w, int) {
+            m = max_nan(m, pack_max(w));
+            some = true;
+        });
+        if (some) mine = key_of(m);
+    }
+    // the upper half of the key will do: a bound lower by 2^-7 at most lets few more pass
+    for (int bit = 31; bit >= 16; --bit) {
         const uint32_t trial = bound | (1u << bit);
         if (__syncthreads_count(mine >= trial) >= want) bound = trial;
     }
-    if (mine >= bound)
-        each([&](int c, uint32_t k) {
-            if (k >= bound) {
-                const unsigned at = atomicAdd(&s_n, 1u);
-                if (at < kCap) s_cand[at] = (uint64_t)k << 32 | (uint32_t)~c;
-            }
+    // packs with a logit at the bound (found by their largest one), then their columns, a thread to each
+    const auto gather = [&](int c, float z) {
+        const uint32_t k = key_of(z);
+        if (k < bound) return;
+        const unsigned at = atomicAdd(&s_n, 1u);
+        if (at < kCap) s_cand[at] = (uint64_t)k << 32 | (uint32_t)~c;
+    };
+    if (h.at >= 0) gather(h.at, logit.of(h.one));
+    if (mine >= bound) {
+        const float least = bound ? logit_of_key(bound) : -INFINITY;
+        h.each(v, [&](const uint4 &w, int k) {
+            if (pack_max(w) < least) return;
+            const unsigned at = atomicAdd(&s_hits, 1u);
+            if (at < kCap) s_hit[at] = k;
         });
+    }
+    __syncthreads();
+    if (s_hits > kCap) {
+        if (t == 0) s_n = kCap + 1;
+    } else {
+        for (unsigned i = t; i < s_hits * P; i += THREADS) {
+            const int c = v.head + s_hit[i / P] * P + (int)(i % P);
+            gather(c, logit.of(to_f32<T>(v.row[c])));
+        }
+    }
     __syncthreads();
     unsigned n = s_n;
     if (n > kCap) {
@@ -212,6 +287,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
     for (unsigned i = t; i < n; i += THREADS) {
         const uint64_t me = s_cand[i];
         int rank = 0;
+#pragma unroll 8
         for (unsigned j = 0; j < n; ++j) rank += s_cand[j] > me;
         if (parts == 1) put(me, rank);
         else if (rank < K) s_best[rank] = me;
@@ -267,12 +343,19 @@ cudaError_t launch_shared(void (*kernel)(P...), int rows, int parts, int threads
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-template <class T>
-cudaError_t top_logits(const LogitArgs &a, int K, float *top, int32_t *index, cudaStream_t st) {
+template <class T, bool PAIRS>
+cudaError_t top_rows(const LogitArgs &a, int K, float *top, int32_t *index, cudaStream_t st) {
     const int packs = (int)(((long long)a.cols * sizeof(T) + 15) / 16), parts = shares(a.rows, packs, 512);
     if (packs / parts <= 256 * kHeld)
-        return launch_shared(k_top_logits<T, 256>, a.rows, parts, 256, st, a, parts, K, top, index);
-    return launch_shared(k_top_logits<T, 512>, a.rows, parts, 512, st, a, parts, K, top, index);
+        return launch_shared(k_top_logits<T, 256, PAIRS>, a.rows, parts, 256, st, a, parts, K, top, index);
+    return launch_shared(k_top_logits<T, 512, PAIRS>, a.rows, parts, 512, st, a, parts, K, top, index);
+}
+
+template <class T>
+cudaError_t top_logits(const LogitArgs &a, int K, float *top, int32_t *index, cudaStream_t st) {
+    if constexpr (sizeof(T) == 2)
+        if (a.factor * a.silent == -INFINITY) return top_rows<T, true>(a, K, top, index, st);
+    return top_rows<T, false>(a, K, top, index, st);
 }
 
 // ---------------------------------------------------------------------------
@@ -288,8 +371,8 @@ cudaError_t top_logits(const LogitArgs &a, int K, float *top, int32_t *index, cu
 // ---------------------------------------------------------------------------
 struct Teacher {
     int at;       // column of this thread's entry, -1: none
-    float log_p, p, mass, z, old;
-    bool silent, first, any;
+    float log_p, p, z, old;
+    bool silent, any;
 };
 
 // one entry a lane: entries [32 w, 32 w + 32) of the row to warp w; every warp goes through all of them
@@ -311,38 +394,37 @@ __device__ __forceinline__ Teacher teacher_of(const DistillArgs &a, const Logit 
         if (a.accumulate && g) t.old = to_f32<T>(g[t.at]);
     }
     float m = -INFINITY;
+    bool any = false;
     for (int k = lane; k < a.K; k += 32) {
         int at;
         const float z = entry(k, at);
         if (at >= 0) m = fmaxf(m, z);
+        any = any || at >= 0;
     }
 #pragma unroll
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    float sum = 0.f, same = 0.f;
-    bool any = false;
-    t.first = t.at >= 0;
-    for (int k0 = 0; k0 < a.K; k0 += 32) {
+    float sum = 0.f;
+    for (int k = lane; k < a.K; k += 32) {
         int at;
-        const float z = entry(k0 + lane, at), e = at >= 0 ? expf(z - m) : 0.f;
-        sum += e;
-        any = any || at >= 0;
-        if (__any_sync(0xffffffffu, at >= 0 && t.at >= 0))
-            for (int j = 0; j < 32; ++j) {
-                const int other = __shfl_sync(0xffffffffu, at, j);
-                const float oe = __shfl_sync(0xffffffffu, e, j);
-                if (other >= 0 && other == t.at) {
-                    same += oe;
-                    if (k0 + j < 32 * w + lane) t.first = false;
-                }
-            }
+        const float z = entry(k, at);
+        if (at >= 0) sum += expf(z - m);
     }
 #pragma unroll
     for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     t.any = __any_sync(0xffffffffu, any);
     t.log_p = mine - m - logf(sum);
     t.p = expf(t.log_p);
-    t.mass = same / sum;
     return t;
+}
+// What entry k's column gets: its p and those of later entries of the same column; false where an
+// earlier entry has it.
+__device__ __forceinline__ bool column_mass(const int *at, const float *p, int k, int K, float &mass) {
+    for (int j = 0; j < k; ++j)
+        if (at[j] == at[k]) return false;
+    mass = p[k];
+    for (int j = k + 1; j < K; ++j)
+        if (at[j] == at[k]) mass += p[j];
+    return true;
 }
 // this entry's share of the row's loss, given the log of the softmax's denominator
 __device__ __forceinline__ float teacher_loss(const Teacher &t, float m, float log_sum) {
@@ -393,8 +475,10 @@ __device__ __forceinline__ void finish_loss(const DistillArgs &a, unsigned block
 template <class T>
 __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
     constexpr int E = 8;
-    const int lane = threadIdx.x & 31;
-    const long long r = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    __shared__ int s_at[8][64];
+    __shared__ float s_p[8][64];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long r = (long long)blockIdx.x * 8 + warp;
     if (r < a.y.rows) {
         const Logit logit(a.y);
         const T *row = static_cast<const T *>(a.y.y) + r * a.y.ld;
@@ -413,6 +497,12 @@ __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
         Teacher t1;
         t1.at = -1;
         if (a.K > 32) t1 = teacher_of<T>(a, logit, row, g, r, 1, lane);
+        s_at[warp][lane] = t0.at;
+        s_p[warp][lane] = t0.p;
+        if (a.K > 32) {
+            s_at[warp][32 + lane] = t1.at;
+            s_p[warp][32 + lane] = t1.p;
+        }
         float m = -INFINITY, s = 0.f;
 #pragma unroll
         for (int i = 0; i < E; ++i) m = fmaxf(m, z[i]);
@@ -443,12 +533,13 @@ __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
             }
             __syncwarp();
             if (done) {
-                const auto named = [&](const Teacher &t) {
-                    if (t.at >= 0 && t.first && !t.silent)
-                        g[t.at] = round_out<T>(t.old + (expf(t.z - m) / s - t.mass) * coef);
+                const auto named = [&](const Teacher &t, int k) {
+                    float mass;
+                    if (t.at >= 0 && !t.silent && column_mass(s_at[warp], s_p[warp], k, a.K, mass))
+                        g[t.at] = round_out<T>(t.old + (expf(t.z - m) / s - mass) * coef);
                 };
-                named(t0);
-                if (a.K > 32) named(t1);
+                named(t0, lane);
+                if (a.K > 32) named(t1, 32 + lane);
             }
         }
     }
@@ -462,8 +553,8 @@ template <class T, int THREADS, bool FAST>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill(const DistillArgs a, const int parts) {
     constexpr int P = Pack<T>::P, WARPS = THREADS / 32;
     __shared__ float2 s_stat[WARPS], s_share[8];
-    __shared__ float s_loss[kTopMax / 32];
-    __shared__ int s_any;
+    __shared__ float s_loss[kTopMax / 32], s_p[kTopMax];
+    __shared__ int s_any, s_twice, s_at[kTopMax];
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31, part = parts > 1 ? (int)cluster_ctarank() : 0;
     const long long r = blockIdx.x / parts;
     const RowView<T> v(a.y, r, part, parts);
@@ -475,16 +566,19 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill(const Disti
     teach.at = -1;
     if (warp * 32 < a.K) {
         teach = teacher_of<T>(a, logit, v.row, g, r, warp, lane);
-        if (t == 0) s_any = teach.any;
+        if (t == 0) {
+            s_any = teach.any;
+            s_twice = 0;
+        }
+        s_at[t] = teach.at;
+        s_p[t] = teach.p;
     }
     // largest logit and sum, over the warp's columns
     float m = -INFINITY, s = 0.f;
     const float scale = logit.factor * kLog2e;
     if (h.at >= 0) m = logit.of(h.one);
-    h.each(v, [&](const uint4 &w, int) {
-#pragma unroll
-        for (int i = 0; i < P; ++i) m = fmaxf(m, FAST ? logit.factor * Pack<T>::one(w, i) : logit.of(Pack<T>::one(w, i)));
-    });
+    const PackMax<T, FAST, false> pack_max(logit);
+    h.each(v, [&](const uint4 &w, int) { m = fmaxf(m, pack_max(w)); });
 #pragma unroll
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
     // nothing but -infinity: every exp below is 0 with any finite m (NaN stays NaN)
@@ -505,6 +599,14 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill(const Disti
     if (lane == 0) s_stat[warp] = make_float2(m, s);
     __syncthreads();
     const bool any = s_any != 0;
+    // does the teacher name a column twice? every pair of entries, by all threads
+    {
+        const int rows_of = THREADS / kTopMax, k = t & (kTopMax - 1);
+        bool twice = false;
+        if (k < a.K && s_at[k] >= 0)
+            for (int j = k + 1 + t / kTopMax; j < a.K; j += rows_of) twice = twice || s_at[j] == s_at[k];
+        if (twice) s_twice = 1;
+    }
     {
         const float2 w = lane < WARPS ? s_stat[lane] : make_float2(-INFINITY, 0.f);
         m = w.x;
@@ -533,64 +635,92 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill(const Disti
         if (lane == 0) s_loss[warp] = loss;
     }
     const float coef = a.weight * rw * logit.factor, over = done ? coef / s : 0.f;
-    const auto grad = [&](float y, float old) {
-        if (!done) return old;
-        if constexpr (FAST) return fmaf(exp_of(y), over, old);
+    const auto grad = [&](float y) {
+        if constexpr (FAST) return exp_of(y) * over;
         bool silent;
         const float z = logit.of(y, silent);
-        return silent ? old : old + expf(z - base) * over;
+        return silent ? 0.f : expf(z - base) * over;
     };
-    if (g && (done || !a.accumulate)) {
-        if (h.at >= 0) g[h.at] = round_out<T>(grad(h.one, a.accumulate ? to_f32<T>(g[h.at]) : 0.f));
+    // each pack of the share to g: made(pack, its place) gives the P gradients
+    const auto write = [&](auto made) {
         T *dst = g + v.head;
         if ((reinterpret_cast<uintptr_t>(dst) & 15) == 0) {
             h.each(v, [&](const uint4 &w, int k) {
-                uint4 *to = reinterpret_cast<uint4 *>(dst + (long long)k * P);
-                uint4 was = make_uint4(0, 0, 0, 0);
-                if (a.accumulate) was = *to;
+                T *to = dst + (long long)k * P;
                 alignas(16) T out[P];
-#pragma unroll
-                for (int i = 0; i < P; ++i) out[i] = round_out<T>(grad(Pack<T>::one(w, i), Pack<T>::one(was, i)));
-                *to = *reinterpret_cast<const uint4 *>(out);
+                made(w, to, out);
+                *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(out);
             });
         } else {
             h.each(v, [&](const uint4 &w, int k) {
                 T *to = dst + (long long)k * P;
+                T out[P];
+                made(w, to, out);
 #pragma unroll
-                for (int i = 0; i < P; ++i)
-                    to[i] = round_out<T>(grad(Pack<T>::one(w, i), a.accumulate ? to_f32<T>(to[i]) : 0.f));
+                for (int i = 0; i < P; ++i) to[i] = out[i];
             });
         }
+    };
+    if (g && done) {
+        if (h.at >= 0) g[h.at] = round_out<T>(grad(h.one) + (a.accumulate ? to_f32<T>(g[h.at]) : 0.f));
+        if (a.accumulate)
+            write([&](const uint4 &w, const T *was, T (&out)[P]) {
+#pragma unroll
+                for (int i = 0; i < P; ++i) out[i] = round_out<T>(to_f32<T>(was[i]) + grad(Pack<T>::one(w, i)));
+            });
+        else
+            write([&](const uint4 &w, const T *, T (&out)[P]) {
+#pragma unroll
+                for (int i = 0; i < P; ++i) out[i] = round_out<T>(grad(Pack<T>::one(w, i)));
+            });
+    } else if (g && !a.accumulate) {
+        if (h.at >= 0) g[h.at] = round_out<T>(0.f);
+        write([&](const uint4 &, const T *, T (&out)[P]) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) out[i] = round_out<T>(0.f);
+        });
     }
     __syncthreads();
-    if (g && done && teach.at >= 0 && teach.first && !teach.silent && teach.at >= v.low && teach.at < v.high)
-        g[teach.at] = round_out<T>(teach.old + (expf(teach.z - m) / s - teach.mass) * coef);
+    if (g && done && teach.at >= 0 && !teach.silent && teach.at >= v.low && teach.at < v.high) {
+        float mass = teach.p;
+        if (!s_twice || column_mass(s_at, s_p, t, a.K, mass))
+            g[teach.at] = round_out<T>(teach.old + (expf(teach.z - m) / s - mass) * coef);
+    }
     if (part == 0) {
         if (t == 0) {
             float loss = s_loss[0];
             for (int w = 1; w * 32 < a.K; ++w) loss += s_loss[w];
             a.row_loss[r] = loss;
         }
-        finish_loss(a, gridDim.x / parts);
+        if (a.ticket) finish_loss(a, gridDim.x / parts);
     }
 }
 
+// the rows' losses added up by a launch of its own, where a block should not wait for its stores to count itself
+__global__ void __launch_bounds__(1024) k_distill_sum(const DistillArgs a) { finish_loss(a, 1); }
+
 template <class T, bool FAST>
-cudaError_t distill_rows(const DistillArgs &a, cudaStream_t st) {
+cudaError_t distill_rows(DistillArgs a, int &launches, cudaStream_t st) {
     const int packs = (int)(((long long)a.y.cols * sizeof(T) + 15) / 16), parts = shares(a.y.rows, packs, 512);
-    if (packs / parts <= 256 * kHeld) return launch_shared(k_distill<T, 256, FAST>, a.y.rows, parts, 256, st, a, parts);
-    return launch_shared(k_distill<T, 512, FAST>, a.y.rows, parts, 512, st, a, parts);
+    a.ticket = a.y.rows <= 304;
+    const cudaError_t e = packs / parts <= 256 * kHeld
+                              ? launch_shared(k_distill<T, 256, FAST>, a.y.rows, parts, 256, st, a, parts)
+                              : launch_shared(k_distill<T, 512, FAST>, a.y.rows, parts, 512, st, a, parts);
+    if (e != cudaSuccess || a.ticket) return e;
+    launches = 2;
+    k_distill_sum<<<1, 1024, 0, st>>>(a);
+    return cudaGetLastError();
 }
 
 template <class T>
-cudaError_t distill(const DistillArgs &a, cudaStream_t st) {
+cudaError_t distill(const DistillArgs &a, int &launches, cudaStream_t st) {
     if (a.y.cols <= 256 && a.K <= 64) {
         k_distill_small<T><<<((unsigned)a.y.rows + 7) / 8, 256, 0, st>>>(a);
         return cudaGetLastError();
     }
     if constexpr (sizeof(T) == 2)
-        if (a.y.factor * a.y.silent == -INFINITY && fabsf(a.y.factor) < 1e30f) return distill_rows<T, true>(a, st);
-    return distill_rows<T, false>(a, st);
+        if (a.y.factor * a.y.silent == -INFINITY && fabsf(a.y.factor) < 1e30f) return distill_rows<T, true>(a, launches, st);
+    return distill_rows<T, false>(a, launches, st);
 }
 
 }  // namespace
@@ -601,10 +731,11 @@ cudaError_t launch_top_logits(const LogitArgs &a, int K, float *top, int32_t *in
     return top_logits<__half>(a, K, top, index, st);
 }
 
-cudaError_t launch_distill(const DistillArgs &a, cudaStream_t st) {
-    if (a.y.type == DSTD_TYPE_F32) return distill<float>(a, st);
-    if (a.y.type == DSTD_TYPE_BF16) return distill<__nv_bfloat16>(a, st);
-    return distill<__half>(a, st);
+cudaError_t launch_distill(const DistillArgs &a, int &launches, cudaStream_t st) {
+    launches = 1;
+    if (a.y.type == DSTD_TYPE_F32) return distill<float>(a, launches, st);
+    if (a.y.type == DSTD_TYPE_BF16) return distill<__nv_bfloat16>(a, launches, st);
+    return distill<__half>(a, launches, st);
 }
 
 }  // namespace dstd
