@@ -24,6 +24,59 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 constexpr float kLog2e = 1.44269504f;
 
+// two fp32 at a time
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
+    uint64_t p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi));
+    return p;
+}
+__device__ __forceinline__ float2 of_pair(uint64_t p) {
+    float2 v;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+// both 16-bit values of a word as fp32, and two fp32 rounded to a word
+template <class T>
+__device__ __forceinline__ uint64_t word_pair(uint32_t w);
+template <>
+__device__ __forceinline__ uint64_t word_pair<__nv_bfloat16>(uint32_t w) {
+    return pair_of(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+template <>
+__device__ __forceinline__ uint64_t word_pair<__half>(uint32_t w) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+    return pair_of(f.x, f.y);
+}
+template <class T>
+__device__ __forceinline__ uint32_t pair_word(uint64_t p);
+template <>
+__device__ __forceinline__ uint32_t pair_word<__nv_bfloat16>(uint64_t p) {
+    const float2 f = of_pair(p);
+    const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+template <>
+__device__ __forceinline__ uint32_t pair_word<__half>(uint64_t p) {
+    const float2 f = of_pair(p);
+    const __half2 h = __floats2half2_rn(f.x, f.y);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
 struct Logit {
     float factor, none;
     __device__ __forceinline__ explicit Logit(const LogitArgs &a) : factor(a.factor), none(a.factor * a.silent) {}
@@ -74,23 +127,21 @@ struct HeldRow {
     float one;
     int at;  // column of `one`, or -1
     __device__ __forceinline__ HeldRow(const RowView<T> &v) {
+        const int k0 = v.first + (int)threadIdx.x, left = v.last - k0;
+        const uint4 *p = reinterpret_cast<const uint4 *>(v.row + v.head) + k0;
 #pragma unroll
-        for (int j = 0; j < kHeld; ++j) {
-            const int k = v.first + j * THREADS + (int)threadIdx.x;
-            raw[j] = k < v.last ? v.pack(k) : make_uint4(0, 0, 0, 0);
-        }
+        for (int j = 0; j < kHeld; ++j) raw[j] = j * THREADS < left ? __ldg(p + j * THREADS) : make_uint4(0, 0, 0, 0);
         at = v.single(threadIdx.x);
         one = at >= 0 ? to_f32<T>(v.row[at]) : 0.f;
     }
     // f(pack, its number) for every pack of this thread
     template <class F>
     __device__ __forceinline__ void each(const RowView<T> &v, F f) const {
+        const int k0 = v.first + (int)threadIdx.x, left = v.last - k0;
 #pragma unroll
-        for (int j = 0; j < kHeld; ++j) {
-            const int k = v.first + j * THREADS + (int)threadIdx.x;
-            if (k < v.last) f(raw[j], k);
-        }
-        for (int k = v.first + kHeld * THREADS + (int)threadIdx.x; k < v.last; k += THREADS) f(v.pack(k), k);
+        for (int j = 0; j < kHeld; ++j)
+            if (j * THREADS < left) f(raw[j], k0 + j * THREADS);
+        for (int k = k0 + kHeld * THREADS; k < v.last; k += THREADS) f(v.pack(k), k);
     }
 };
 
@@ -372,50 +423,57 @@ cudaError_t top_logits(const LogitArgs &a, int K, float *top, int32_t *index, cu
 struct Teacher {
     int at;       // column of this thread's entry, -1: none
     float log_p, p, z, old;
-    bool silent, any;
+    bool silent;
 };
 
-// one entry a lane: entries [32 w, 32 w + 32) of the row to warp w; every warp goes through all of them
-template <class T>
-__device__ __forceinline__ Teacher teacher_of(const DistillArgs &a, const Logit &logit, const T *row, const T *g,
-                                              long long r, int w, int lane) {
-    const auto entry = [&](int k, int &at) {
-        at = k < a.K ? a.index[r * a.K + k] : -1;
-        const float z = k < a.K ? a.teacher_factor * a.top[r * a.K + k] : -INFINITY;
-        if (at < 0 || at >= a.y.cols || z == -INFINITY) at = -1;
-        return z;
-    };
-    Teacher t;
-    const float mine = entry(32 * w + lane, t.at);
-    t.silent = false;
-    t.z = t.old = 0.f;
-    if (t.at >= 0) {
-        t.z = logit.of(to_f32<T>(row[t.at]), t.silent);
-        if (a.accumulate && g) t.old = to_f32<T>(g[t.at]);
-    }
-    float m = -INFINITY;
-    bool any = false;
-    for (int k = lane; k < a.K; k += 32) {
-        int at;
-        const float z = entry(k, at);
-        if (at >= 0) m = fmaxf(m, z);
-        any = any || at >= 0;
-    }
+// A row's entries, 32 K' of them by a warp: lane l has entries l, 32 + l, ...; `own` is the warp's share, one a lane.
+template <int EACH>
+struct Record {
+    int at[EACH];
+    float z[EACH];
+    __device__ __forceinline__ Record(const DistillArgs &a, long long r, int lane) {
 #pragma unroll
-    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    float sum = 0.f;
-    for (int k = lane; k < a.K; k += 32) {
-        int at;
-        const float z = entry(k, at);
-        if (at >= 0) sum += expf(z - m);
+        for (int e = 0; e < EACH; ++e) {
+            const int k = e * 32 + lane;
+            at[e] = k < a.K ? a.index[r * a.K + k] : -1;
+            z[e] = k < a.K ? a.teacher_factor * a.top[r * a.K + k] : -INFINITY;
+            if (at[e] >= a.y.cols || z[e] == -INFINITY) at[e] = -1;
+        }
     }
+    __device__ __forceinline__ bool any() const {
+        bool some = false;
 #pragma unroll
-    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    t.any = __any_sync(0xffffffffu, any);
-    t.log_p = mine - m - logf(sum);
-    t.p = expf(t.log_p);
-    return t;
-}
+        for (int e = 0; e < EACH; ++e) some = some || at[e] >= 0;
+        return __any_sync(0xffffffffu, some);
+    }
+    // the softmax's largest logit and the log of its sum
+    __device__ __forceinline__ void softmax(float &m, float &log_sum) const {
+        m = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e)
+            if (at[e] >= 0) m = fmaxf(m, z[e]);
+#pragma unroll
+        for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e)
+            if (at[e] >= 0) sum += expf(z[e] - m);
+#pragma unroll
+        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        log_sum = logf(sum);
+    }
+    // entry e of this lane, given its output y and what its gradient holds
+    __device__ __forceinline__ Teacher entry(int e, float m, float log_sum, const Logit &logit, float y,
+                                             float old) const {
+        Teacher t;
+        t.at = at[e];
+        t.z = logit.of(y, t.silent);
+        t.old = old;
+        t.log_p = z[e] - m - log_sum;
+        t.p = t.at >= 0 ? expf(t.log_p) : 0.f;
+        return t;
+    }
+};
 // What entry k's column gets: its p and those of later entries of the same column; false where an
 // earlier entry has it.
 __device__ __forceinline__ bool column_mass(const int *at, const float *p, int k, int K, float &mass) {
@@ -493,15 +551,23 @@ __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
             z[i] = c < a.y.cols ? logit.of(to_f32<T>(row[c]), silent[i]) : -INFINITY;
             was[i] = a.accumulate && g && c < a.y.cols ? to_f32<T>(g[c]) : 0.f;
         }
-        const Teacher t0 = teacher_of<T>(a, logit, row, g, r, 0, lane);
-        Teacher t1;
-        t1.at = -1;
-        if (a.K > 32) t1 = teacher_of<T>(a, logit, row, g, r, 1, lane);
-        s_at[warp][lane] = t0.at;
-        s_p[warp][lane] = t0.p;
-        if (a.K > 32) {
-            s_at[warp][32 + lane] = t1.at;
-            s_p[warp][32 + lane] = t1.p;
+        const Record<2> record(a, r, lane);
+        const bool any = record.any();
+        Teacher entry[2];
+        {
+            float y[2], old[2], tm, tl;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                y[e] = record.at[e] >= 0 ? to_f32<T>(row[record.at[e]]) : 0.f;
+                old[e] = record.at[e] >= 0 && a.accumulate && g ? to_f32<T>(g[record.at[e]]) : 0.f;
+            }
+            record.softmax(tm, tl);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                entry[e] = record.entry(e, tm, tl, logit, y[e], old[e]);
+                s_at[warp][32 * e + lane] = entry[e].at;
+                s_p[warp][32 * e + lane] = entry[e].p;
+            }
         }
         float m = -INFINITY, s = 0.f;
 #pragma unroll
@@ -513,12 +579,11 @@ __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
 #pragma unroll
         for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
         // a row without logits has no softmax: it is left out (a NaN counts as a logit)
-        const bool done = t0.any && rw != 0.f && !(m == -INFINITY && !(s != s));
+        const bool done = any && rw != 0.f && !(m == -INFINITY && !(s != s));
         float loss = 0.f;
         if (done) {
             const float log_sum = logf(s);
-            loss = teacher_loss(t0, m, log_sum);
-            if (a.K > 32) loss += teacher_loss(t1, m, log_sum);
+            loss = teacher_loss(entry[0], m, log_sum) + teacher_loss(entry[1], m, log_sum);
         }
 #pragma unroll
         for (int d = 16; d; d >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, d);
@@ -533,13 +598,13 @@ __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
             }
             __syncwarp();
             if (done) {
-                const auto named = [&](const Teacher &t, int k) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const Teacher &t = entry[e];
                     float mass;
-                    if (t.at >= 0 && !t.silent && column_mass(s_at[warp], s_p[warp], k, a.K, mass))
+                    if (t.at >= 0 && !t.silent && column_mass(s_at[warp], s_p[warp], 32 * e + lane, a.K, mass))
                         g[t.at] = round_out<T>(t.old + (expf(t.z - m) / s - mass) * coef);
-                };
-                named(t0, lane);
-                if (a.K > 32) named(t1, 32 + lane);
+                }
             }
         }
     }
@@ -552,26 +617,38 @@ __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
 template <class T, int THREADS, bool FAST>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill(const DistillArgs a, const int parts) {
     constexpr int P = Pack<T>::P, WARPS = THREADS / 32;
+    constexpr int SLOTS = 2 * kTopMax;
     __shared__ float2 s_stat[WARPS], s_share[8];
     __shared__ float s_loss[kTopMax / 32], s_p[kTopMax];
-    __shared__ int s_any, s_twice, s_at[kTopMax];
+    __shared__ int s_any, s_twice, s_at[kTopMax], s_slot[SLOTS];
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31, part = parts > 1 ? (int)cluster_ctarank() : 0;
     const long long r = blockIdx.x / parts;
     const RowView<T> v(a.y, r, part, parts);
-    const HeldRow<T, THREADS> h(v);
     const Logit logit(a.y);
     T *g = a.g ? static_cast<T *>(a.g) + r * a.ld_g : nullptr;
+    // the teacher's entries on their way before the row: all to each warp that has entries of its own
+    const bool teaches = warp * 32 < a.K;
+    int own_at = -1;
+    if (teaches && warp * 32 + lane < a.K) own_at = a.index[r * a.K + warp * 32 + lane];
+    const HeldRow<T, THREADS> h(v);
     const float rw = a.row_weight ? a.row_weight[r] : 1.f / (float)a.y.rows;
-    Teacher teach;
-    teach.at = -1;
-    if (warp * 32 < a.K) {
-        teach = teacher_of<T>(a, logit, v.row, g, r, warp, lane);
-        if (t == 0) {
-            s_any = teach.any;
+    for (int i = t; i < SLOTS; i += THREADS) s_slot[i] = -1;
+    float own_y = 0.f, own_old = 0.f;
+    if (own_at >= 0 && own_at < a.y.cols) {
+        own_y = to_f32<T>(v.row[own_at]);
+        if (a.accumulate && g) own_old = to_f32<T>(g[own_at]);
+    }
+    if (warp == 0) {
+        bool some = false;
+        for (int k = lane; k < a.K; k += 32) {
+            const int at = a.index[r * a.K + k];
+            some = some || (at >= 0 && at < a.y.cols && a.teacher_factor * a.top[r * a.K + k] != -INFINITY);
+        }
+        some = __any_sync(0xffffffffu, some);
+        if (lane == 0) {
+            s_any = some;
             s_twice = 0;
         }
-        s_at[t] = teach.at;
-        s_p[t] = teach.p;
     }
     // largest logit and sum, over the warp's columns
     float m = -INFINITY, s = 0.f;
@@ -587,26 +664,35 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill(const Disti
         if constexpr (FAST) return exp2_fast(fmaf(y, scale, -base * kLog2e));
         else return expf(logit.of(y) - base);
     };
-    if (h.at >= 0) s = exp_of(h.one);
-    h.each(v, [&](const uint4 &w, int) {
-        float part_sum = 0.f;
+    const auto exp_pair = [&](uint32_t w) {
+        if constexpr (FAST) {
+            const float2 x = of_pair(fma_pair(word_pair<T>(w), pair_of(scale, scale), pair_of(-base * kLog2e, -base * kLog2e)));
+            return pair_of(exp2_fast(x.x), exp2_fast(x.y));
+        } else {
+            return (uint64_t)w;
+        }
+    };
+    if constexpr (FAST) {
+        uint64_t two = pair_of(0.f, 0.f);
+        h.each(v, [&](const uint4 &w, int) {
+            two = add_pair(two, add_pair(add_pair(exp_pair(w.x), exp_pair(w.y)), add_pair(exp_pair(w.z), exp_pair(w.w))));
+        });
+        const float2 f = of_pair(two);
+        s = f.x + f.y;
+    } else {
+        h.each(v, [&](const uint4 &w, int) {
+            float part_sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < P; ++i) part_sum += exp_of(Pack<T>::one(w, i));
-        s += part_sum;
-    });
+            for (int i = 0; i < P; ++i) part_sum += exp_of(Pack<T>::one(w, i));
+            s += part_sum;
+        });
+    }
+    if (h.at >= 0) s += exp_of(h.one);
 #pragma unroll
     for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
     if (lane == 0) s_stat[warp] = make_float2(m, s);
     __syncthreads();
     const bool any = s_any != 0;
-    // does the teacher name a column twice? every pair of entries, by all threads
-    {
-        const int rows_of = THREADS / kTopMax, k = t & (kTopMax - 1);
-        bool twice = false;
-        if (k < a.K && s_at[k] >= 0)
-            for (int j = k + 1 + t / kTopMax; j < a.K; j += rows_of) twice = twice || s_at[j] == s_at[k];
-        if (twice) s_twice = 1;
-    }
     {
         const float2 w = lane < WARPS ? s_stat[lane] : make_float2(-INFINITY, 0.f);
         m = w.x;
@@ -628,8 +714,28 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill(const Disti
     // a row without logits has no softmax: it is left out (a NaN counts as a logit)
     const bool done = any && rw != 0.f && !(m == -INFINITY && !(s != s));
     base = m == -INFINITY ? 0.f : m;
-    if (warp * 32 < a.K) {
-        float loss = done ? teacher_loss(teach, m, logf(s)) : 0.f;
+    Teacher teach;
+    teach.at = -1;
+    if (teaches && done) {
+        const Record<kTopMax / 32> record(a, r, lane);
+        float tm, tl;
+        record.softmax(tm, tl);
+        const float z = t < a.K ? a.teacher_factor * a.top[r * a.K + t] : -INFINITY;
+        teach.at = own_at >= 0 && own_at < a.y.cols && z != -INFINITY ? own_at : -1;
+        teach.z = logit.of(own_y, teach.silent);
+        teach.old = own_old;
+        teach.log_p = z - tm - tl;
+        teach.p = teach.at >= 0 ? expf(teach.log_p) : 0.f;
+        s_at[t] = teach.at;
+        s_p[t] = teach.p;
+        // a column named twice finds itself in the table
+        if (teach.at >= 0)
+            for (int i = teach.at & (SLOTS - 1);; i = (i + 1) & (SLOTS - 1)) {
+                const int was = atomicCAS(&s_slot[i], -1, teach.at);
+                if (was == teach.at) s_twice = 1;
+                if (was == -1 || was == teach.at) break;
+            }
+        float loss = teacher_loss(teach, m, logf(s));
 #pragma unroll
         for (int d = 16; d; d >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, d);
         if (lane == 0) s_loss[warp] = loss;
@@ -654,7 +760,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill(const Disti
         } else {
             h.each(v, [&](const uint4 &w, int k) {
                 T *to = dst + (long long)k * P;
-                T out[P];
+                alignas(16) T out[P];
                 made(w, to, out);
 #pragma unroll
                 for (int i = 0; i < P; ++i) to[i] = out[i];
@@ -667,6 +773,13 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill(const Disti
             write([&](const uint4 &w, const T *was, T (&out)[P]) {
 #pragma unroll
                 for (int i = 0; i < P; ++i) out[i] = round_out<T>(to_f32<T>(was[i]) + grad(Pack<T>::one(w, i)));
+            });
+        else if constexpr (FAST)
+            write([&](const uint4 &w, const T *, T (&out)[P]) {
+                const uint64_t c = pair_of(over, over);
+                const uint4 y = make_uint4(pair_word<T>(mul_pair(exp_pair(w.x), c)), pair_word<T>(mul_pair(exp_pair(w.y), c)),
+                                           pair_word<T>(mul_pair(exp_pair(w.z), c)), pair_word<T>(mul_pair(exp_pair(w.w), c)));
+                *reinterpret_cast<uint4 *>(out) = y;
             });
         else
             write([&](const uint4 &w, const T *, T (&out)[P]) {
@@ -688,8 +801,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill(const Disti
     }
     if (part == 0) {
         if (t == 0) {
-            float loss = s_loss[0];
-            for (int w = 1; w * 32 < a.K; ++w) loss += s_loss[w];
+            float loss = 0.f;
+            if (done)
+                for (int w = 0; w * 32 < a.K; ++w) loss += s_loss[w];
             a.row_loss[r] = loss;
         }
         if (a.ticket) finish_loss(a, gridDim.x / parts);
