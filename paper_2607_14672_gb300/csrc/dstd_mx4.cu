@@ -492,6 +492,159 @@ __global__ void __launch_bounds__(192) k_mx4_tc(const __grid_constant__ CUtensor
     if (warp == 5) tmem_dealloc(tmem, C::COLS);
 }
 
+// Large products: a pair of SMs computes 256 x 256, each SM its 128 rows of a and half of b's codes,
+// so that a stage brings 35 KB to an SM for 512 cycles of MMAs. The pairs stay and take tiles in turn; eight
+// warps take the sums out to registers, from where they are stored while the next tile is computed.
+struct PairCfg {
+    static constexpr int SF_BYTES = 2 * kScaleTile * 3;  // of this SM's rows of a, of all of b's
+    static constexpr int STAGE = (2 * kTileBytes + SF_BYTES + 1023) / 1024 * 1024;
+    static constexpr int STAGES = 6;
+    static constexpr int SMEM = STAGES * STAGE + 1024 + 256;
+    static constexpr int SF_COL = 256, SF_SET = 8 + 16;
+};
+
+template <class O>
+__global__ void __launch_bounds__(320, 1)
+    k_mx4_pair(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+               const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb, const Mx4Tc p) {
+    using C = PairCfg;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint64_t *full = reinterpret_cast<uint64_t *>(smem + C::STAGES * C::STAGE);  // (leader) both SMs' copies have landed
+    uint64_t *empty = full + C::STAGES;                                          // the pair's MMAs have read the stage
+    uint64_t *acc_full = empty + C::STAGES, *acc_empty = acc_full + 1;           // the latter at the leader
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(acc_empty + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)cluster_ctarank(), step = (int)cluster_count_x();
+    const int stages = (p.blocks + kStageBlocks - 1) / kStageBlocks, tiles = p.tiles_a * p.tiles_b;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::STAGES; ++s) {
+            mbar_init(&full[s], 1);
+            mbar_init(&empty[s], 1);
+        }
+        mbar_init(acc_full, 1);
+        mbar_init(acc_empty, 16);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 9) tmem_alloc_pair(tmem_slot, 512);
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();  // both SMs' barriers exist before any remote signal
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    wait_launch_before();
+
+    if (warp == 8) {
+        const uint32_t full0 = mapa_rank(smem_u32(&full[0]), 0);
+        uint32_t it = 0;
+        bool ok = true;
+        for (int i = (int)cluster_id_x(); ok && i < tiles; i += step) {
+            int ta, tb;
+            mx4_tile(i, p.tiles_a, p.tiles_b, ta, tb);
+            for (int s = 0; s < stages; ++s, ++it) {
+                const int slot = it % C::STAGES;
+                ok = mbar_wait_cycles(&empty[slot], ((it / C::STAGES) & 1u) ^ 1u);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                if (elect_one()) {
+                    const uint32_t st = smem_u32(smem + slot * C::STAGE);
+                    const uint32_t bar = full0 + (uint32_t)(slot * sizeof(uint64_t));
+                    if (rank == 0) mbar_expect_tx(&full[slot], (uint32_t)(2 * (2 * kTileBytes + C::SF_BYTES)));
+                    tma_load_2d_pair(st, &map_a, bar, s * kRowBytes, ta * 256 + rank * 128);
+                    tma_load_2d_pair(st + kTileBytes, &map_b, bar, s * kRowBytes, tb * 256 + rank * 128);
+                    tma_load_2d_pair(st + 2 * kTileBytes, &map_sa, bar, s * 256, ta * 2 + rank);
+                    tma_load_2d_pair(st + 2 * kTileBytes + 2 * kScaleTile, &map_sb, bar, s * 256, tb * 2);
+                }
+                __syncwarp();
+            }
+        }
+        // every stage released: no copy is in flight and no commit targets this SM's stages afterwards
+        for (int i = 0; i < C::STAGES && ok; ++i, ++it)
+            ok = mbar_wait_cycles(&empty[it % C::STAGES], ((it / C::STAGES) & 1u) ^ 1u);
+        if (!ok) mx4_timeout();
+        __syncwarp();
+    } else if (warp == 9) {
+        if (rank == 0) {
+            uint32_t it = 0, j = 0;
+            bool ok = true;
+            for (int i = (int)cluster_id_x(); ok && i < tiles; i += step, ++j) {
+                ok = mbar_wait_cycles(acc_empty, (j & 1u) ^ 1u);
+                for (int s = 0; s < stages; ++s, ++it) {
+                    const int slot = it % C::STAGES;
+                    ok = ok && mbar_wait_cycles(&full[slot], (it / C::STAGES) & 1u);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t st = smem_u32(smem + slot * C::STAGE), sf = st + 2 * kTileBytes;
+                        const uint32_t sfa = tmem + C::SF_COL + (it & 1u) * C::SF_SET, sfb = sfa + 8;
+                        const uint64_t ad = sdesc_sw128(st), bd = sdesc_sw128(st + kTileBytes);
+                        const int left = p.blocks - s * kStageBlocks;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            if (h * 4 >= left) break;
+                            tmem_cp_scales_pair(sfa + h * 4, sdesc_rows16(sf + h * kScaleTile));
+#pragma unroll
+                            for (int k = 0; k < 2; ++k)
+                                tmem_cp_scales_pair(sfb + (h * 2 + k) * 4,
+                                                    sdesc_rows16(sf + (1 + k) * 2 * kScaleTile + h * kScaleTile));
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                const int kk = 2 * h + k;
+                                if (kk * 2 >= left) break;
+                                mma_mx4_pair(tmem, ad + kk * 2, bd + kk * 2, idesc_mx4(256, 256, 2 * k), sfa + h * 4,
+                                             sfb + h * 8, s > 0 || kk > 0 ? 1u : 0u);
+                            }
+                        }
+                        mma_commit_pair(&empty[slot]);
+                        if (s + 1 == stages) mma_commit_pair(acc_full);
+                    }
+                    __syncwarp();
+                }
+            }
+            if (!ok) mx4_timeout();
+        }
+        __syncwarp();
+    } else {
+        // rows of quarter (warp & 3), half of the columns
+        const int quarter = warp & 3, half = warp >> 2;
+        const uint32_t t0 = tmem + ((uint32_t)(quarter * 32) << 16) + half * 128;
+        const uint32_t acc_empty0 = mapa_rank(smem_u32(acc_empty), 0);
+        uint32_t j = 0;
+        for (int i = (int)cluster_id_x(); i < tiles; i += step, ++j) {
+            int ta, tb;
+            mx4_tile(i, p.tiles_a, p.tiles_b, ta, tb);
+            if (!mbar_wait_cycles(acc_full, j & 1u)) {
+                mx4_timeout();
+                break;
+            }
+            __syncwarp();
+            tc_fence_after();
+            float v[4][32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld32(t0 + c * 32, v[c]);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_pair(acc_empty0);
+            const long long r = (long long)ta * 256 + rank * 128 + quarter * 32 + lane;
+            const long long c0 = (long long)tb * 256 + half * 128;
+            O *dst = static_cast<O *>(p.out) + r * p.ld_a + c0 * p.ld_b;
+            const long long left = r < p.a.rows ? p.b.rows - c0 : 0;
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                mx4_store<O, 32>(dst + c * 32 * p.ld_b, p.ld_a, p.ld_b, v[c],
+                                 (int)max(0ll, min(32ll, left - c * 32)));
+        }
+        __syncwarp();
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();  // both SMs are done with TMEM, every remote arrive has landed
+    if (warp == 9) tmem_dealloc_pair(tmem, 512);
+}
+
 typedef CUresult (*EncodeFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                              const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
                              CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -509,10 +662,86 @@ bool code_map(CUtensorMap *m, const uint8_t *p, int rows, int blocks, long long 
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// boxes of 2 tiles along K by `rows` tiles of the scales, as 32-bit words; beyond them zeros are read
+bool scale_map(CUtensorMap *m, const uint8_t *p, int rows, int ktiles, int box_rows) {
+    EncodeFn enc = reinterpret_cast<EncodeFn>(tensor_map_encoder());
+    if (!enc) return false;
+    const cuuint64_t dim[2] = {(cuuint64_t)ktiles * 128, ((cuuint64_t)rows + 127) / 128};
+    const cuuint64_t stride[1] = {(cuuint64_t)ktiles * kScaleTile};
+    const cuuint32_t box[2] = {256, (cuuint32_t)box_rows};
+    const cuuint32_t one[2] = {1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<uint8_t *>(p), dim, stride, box, one,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 struct Mx4Plan {
-    int nt, parts;
-    bool exchanged;  // the tokens are the side of 128-row tiles
+    int nt, parts;   // nt = 0: pairs of SMs
+    bool exchanged;  // the tokens are the side a
 };
+
+// the product with its sides named
+Mx4Tc mx4_sides(const Mx4Args &a, const Mx4Plan &plan, int tile_a, int tile_b) {
+    const bool ex = plan.exchanged;
+    const int rows_a = ex ? a.T : a.N, rows_b = ex ? a.N : a.T;
+    return Mx4Tc{{ex ? a.x_scale : a.w_scale, rows_a}, {ex ? a.w_scale : a.x_scale, rows_b}, a.blocks, (a.blocks + 3) / 4,
+                 (rows_a - 1) / tile_a + 1, (rows_b - 1) / tile_b + 1, plan.parts, a.out.p,
+                 ex ? a.out.ld_t : a.out.ld_n, ex ? a.out.ld_n : a.out.ld_t};
+}
+
+template <class O>
+cudaLaunchConfig_t pair_config(cudaLaunchAttribute (&attr)[2]) {
+    cudaLaunchConfig_t cfg = {};
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    cfg.blockDim = dim3(320);
+    cfg.dynamicSmemBytes = PairCfg::SMEM;
+    return cfg;
+}
+
+// SM pairs at work at a time (0: an error)
+template <class O>
+int mx4_pairs() {
+    static PerDevice resident;
+    return resident.get([](int) {
+        cudaLaunchAttribute attr[2];
+        cudaLaunchConfig_t cfg = pair_config<O>(attr);
+        cfg.gridDim = dim3(2 * 76);
+        cfg.numAttrs = 1;
+        int n = 0;
+        if (cudaFuncSetAttribute(k_mx4_pair<O>, cudaFuncAttributeMaxDynamicSharedMemorySize, PairCfg::SMEM) !=
+                cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&n, k_mx4_pair<O>, &cfg) != cudaSuccess)
+            return 0;
+        return n;
+    });
+}
+
+template <class O>
+cudaError_t launch_mx4_pair(const Mx4Args &a, const Mx4Plan &plan, cudaStream_t st) {
+    const int pairs = mx4_pairs<O>();
+    if (pairs < 1) return cudaErrorInvalidConfiguration;
+    const Mx4Tc p = mx4_sides(a, plan, 256, 256);
+    const bool ex = plan.exchanged;
+    CUtensorMap map_a, map_b, map_sa, map_sb;
+    if (!code_map(&map_a, ex ? a.x : a.w, p.a.rows, a.blocks, ex ? a.ld_x : a.ld_w, 128) ||
+        !code_map(&map_b, ex ? a.w : a.x, p.b.rows, a.blocks, ex ? a.ld_w : a.ld_x, 128) ||
+        !scale_map(&map_sa, p.a.scale, p.a.rows, p.ktiles, 1) || !scale_map(&map_sb, p.b.scale, p.b.rows, p.ktiles, 2))
+        return cudaErrorInvalidValue;
+    const long long tiles = (long long)p.tiles_a * p.tiles_b;
+    if (tiles > 0x7fffffff) return cudaErrorInvalidValue;
+    cudaLaunchAttribute attr[2];
+    cudaLaunchConfig_t cfg = pair_config<O>(attr);
+    cfg.gridDim = dim3(2 * (unsigned)std::min<long long>(tiles, pairs));
+    cfg.stream = st;
+    return cudaLaunchKernelEx(&cfg, k_mx4_pair<O>, map_a, map_b, map_sa, map_sb, p);
+}
 
 template <int NT, class O>
 cudaError_t launch_mx4_tc(const Mx4Args &a, const Mx4Plan &plan, cudaStream_t st) {
@@ -524,14 +753,11 @@ cudaError_t launch_mx4_tc(const Mx4Args &a, const Mx4Plan &plan, cudaStream_t st
         }))
         return cudaErrorInvalidConfiguration;
     const bool ex = plan.exchanged;
-    const int rows_a = ex ? a.T : a.N, rows_b = ex ? a.N : a.T;
+    const Mx4Tc p = mx4_sides(a, plan, 128, NT);
     CUtensorMap map_a, map_b;
-    if (!code_map(&map_a, ex ? a.x : a.w, rows_a, a.blocks, ex ? a.ld_x : a.ld_w, 128) ||
-        !code_map(&map_b, ex ? a.w : a.x, rows_b, a.blocks, ex ? a.ld_w : a.ld_x, NT))
+    if (!code_map(&map_a, ex ? a.x : a.w, p.a.rows, a.blocks, ex ? a.ld_x : a.ld_w, 128) ||
+        !code_map(&map_b, ex ? a.w : a.x, p.b.rows, a.blocks, ex ? a.ld_w : a.ld_x, NT))
         return cudaErrorInvalidValue;
-    const Mx4Tc p{{ex ? a.x_scale : a.w_scale, rows_a}, {ex ? a.w_scale : a.x_scale, rows_b}, a.blocks, (a.blocks + 3) / 4,
-                  (rows_a - 1) / 128 + 1, (rows_b - 1) / NT + 1, plan.parts, a.out.p, ex ? a.out.ld_t : a.out.ld_n,
-                  ex ? a.out.ld_n : a.out.ld_t};
     const long long grid = (long long)p.tiles_a * p.tiles_b * plan.parts;
     if (grid > 0x7fffffff) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
@@ -551,21 +777,34 @@ cudaError_t launch_mx4_tc(const Mx4Args &a, const Mx4Plan &plan, cudaStream_t st
     return cudaLaunchKernelEx(&cfg, k_mx4_tc<NT, O>, map_a, map_b, p);
 }
 
-Mx4Plan mx4_plan(int T, int N, int blocks) {
+// One orientation's plan: fewer padded rows, or neighbouring lanes that store neighbouring elements
+Mx4Plan mx4_plan(const Mx4Args &q) {
+    const auto width = [](int b) { return b <= 16 ? 16 : (b <= 32 ? 32 : (b <= 64 ? 64 : 128)); };
+    const auto area = [&](int a, int b) {
+        const long long nt = width(b);
+        return (((long long)a + 127) / 128 * 128) * (((long long)b + nt - 1) / nt * nt);
+    };
     Mx4Plan p{};
-    p.exchanged = T > N;
-    const int b = p.exchanged ? N : T, a = p.exchanged ? T : N;
-    p.nt = b <= 16 ? 16 : (b <= 32 ? 32 : (b <= 64 ? 64 : 128));
-    const long long tiles = (((long long)a + 127) / 128) * (((long long)b + p.nt - 1) / p.nt);
-    const int stages = (blocks + kStageBlocks - 1) / kStageBlocks;
+    const long long straight = area(q.N, q.T), exchanged = area(q.T, q.N);
+    p.exchanged = q.out.ld_n == 1 ? 2 * exchanged <= straight : 2 * straight > exchanged;
+    const int a = p.exchanged ? q.T : q.N, b = p.exchanged ? q.N : q.T;
+    const int stages = (q.blocks + kStageBlocks - 1) / kStageBlocks;
+    p.nt = width(b);
     p.parts = 1;
+    const long long pair_tiles = (((long long)a + 255) / 256) * (((long long)b + 255) / 256);
+    if (pair_tiles >= 76 && b > 128) {
+        p.nt = 0;
+        return p;
+    }
+    const long long tiles = (((long long)a + 127) / 128) * (((long long)b + p.nt - 1) / p.nt);
     while (p.parts < 8 && tiles * p.parts * 2 <= 304 && p.parts * 2 <= stages) p.parts *= 2;
     return p;
 }
 
 template <class O>
 cudaError_t run_mx4(const Mx4Args &a, cudaStream_t st) {
-    const Mx4Plan p = mx4_plan(a.T, a.N, a.blocks);
+    const Mx4Plan p = mx4_plan(a);
+    if (p.nt == 0) return launch_mx4_pair<O>(a, p, st);
     if (p.nt == 16) return launch_mx4_tc<16, O>(a, p, st);
     if (p.nt == 32) return launch_mx4_tc<32, O>(a, p, st);
     if (p.nt == 64) return launch_mx4_tc<64, O>(a, p, st);

@@ -549,21 +549,27 @@ def mx4_row_bytes(cols):
 
 def mx4_scale_bytes(rows, cols):
     """Bytes of the scales of rows of 4-bit codes (their layout: include/dstd.h)."""
-    return load().dstd_mx4_scale_bytes(rows, cols)
+    return (rows + 127) // 128 * ((cols + 127) // 128) * 512
 
 
 def _codes4(q, name, R, row, dev):
-    """Row stride in bytes of R rows of 4-bit codes, `row` bytes each, at multiples of 16 bytes."""
+    """Address of R rows of 4-bit codes, `row` bytes each, and their stride; rows start at multiples of 16 bytes."""
+    if q.shape == (R, row) and q.dtype == _TORCH.uint8 and q.get_device() == dev:
+        ld, one = q.stride()
+        at = q.data_ptr()
+        if one == 1 and ld >= row and not (at | ld) & 15:
+            return at, ld
     ld = _rows(q, name, R, row, dev, _TORCH.uint8)
     if q.numel() and (q.data_ptr() % 16 or ld % 16):
         raise ValueError(f"{name}: rows of codes must start at multiples of 16 bytes")
-    return ld
+    return q.data_ptr(), ld
 
 
 def _scales4(s, name, R, cols, dev):
-    need = mx4_scale_bytes(R, cols)
+    need = (R + 127) // 128 * ((cols + 127) // 128) * 512
     if s.dtype != _TORCH.uint8 or s.get_device() != dev or not s.is_contiguous() or s.numel() < need:
         raise ValueError(f"{name} must be a contiguous uint8 tensor of at least {need} on cuda:{dev}")
+    return s.data_ptr()
 
 
 def quantize_mx4(x, q, scale, values=None, stream=None):
@@ -572,19 +578,18 @@ def quantize_mx4(x, q, scale, values=None, stream=None):
     block of 32 columns in scale [mx4_scale_bytes(R, K)] uint8: the least with
     no code beyond 6. ``values`` [R, K] float32 receives what the codes stand
     for. A block that is not finite gets scale NaN. Rows may be padded."""
-    torch = _torch()
+    _torch()
     R, K = x.shape
     dev = x.get_device()
     if dev != _ONLY:
         _here(x, dev, "x")
     ld_x = _rows(x, "x", R, K, dev)
-    ld_q = _codes4(q, "q", R, mx4_row_bytes(K), dev)
-    _scales4(scale, "scale", R, K, dev)
+    q_at, ld_q = _codes4(q, "q", R, (K + 31) // 32 * 16, dev)
     ld_v, v = 0, None
     if values is not None:
-        ld_v, v = _rows(values, "values", R, K, dev, torch.float32), values.data_ptr()
-    code = load().dstd_quantize_mx4(x.data_ptr(), _type_code(x.dtype, "x"), R, K, ld_x, q.data_ptr(), ld_q,
-                                    scale.data_ptr(), v, ld_v, _stream_of(stream, dev))
+        ld_v, v = _rows(values, "values", R, K, dev, _TORCH.float32), values.data_ptr()
+    code = load().dstd_quantize_mx4(x.data_ptr(), _type_code(x.dtype, "x"), R, K, ld_x, q_at, ld_q,
+                                    _scales4(scale, "scale", R, K, dev), v, ld_v, _stream_of(stream, dev))
     if code:
         raise DstdError(code, "dstd_quantize_mx4")
 
@@ -602,13 +607,12 @@ def mx4_matmul(x, x_scale, w, w_scale, out, stream=None):
     if row % 16 or row > 1 << 30:
         raise ValueError("mx4_matmul: a row of codes is 16 bytes for each block of 32 columns")
     K = 2 * row
-    ld_x = _codes4(x, "x", T, row, dev)
-    ld_w = _codes4(w, "w", N, row, dev)
-    _scales4(x_scale, "x_scale", T, K, dev)
-    _scales4(w_scale, "w_scale", N, K, dev)
+    x_at, ld_x = _codes4(x, "x", T, row, dev)
+    w_at, ld_w = _codes4(w, "w", N, row, dev)
     ld_out = _rows(out, "out", T, N, dev)
-    code = load().dstd_mx4_matmul(x.data_ptr(), ld_x, x_scale.data_ptr(), w.data_ptr(), ld_w, w_scale.data_ptr(), T, N,
-                                  K, out.data_ptr(), _type_code(out.dtype, "out"), ld_out, _stream_of(stream, dev))
+    code = load().dstd_mx4_matmul(x_at, ld_x, _scales4(x_scale, "x_scale", T, K, dev), w_at, ld_w,
+                                  _scales4(w_scale, "w_scale", N, K, dev), T, N, K, out.data_ptr(),
+                                  _type_code(out.dtype, "out"), ld_out, _stream_of(stream, dev))
     if code:
         raise DstdError(code, "dstd_mx4_matmul")
 

@@ -149,6 +149,13 @@ def test_product_large(T, N, K):
     product(T, N, K)
 
 
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("T,N,K,pad", [(2100, 2400, 300, 0), (4100, 2500, 97, 1), (2305, 2561, 2049, 0), (20000, 300, 33, 3)])
+def test_product_on_pairs(T, N, K, pad, out):
+    """Tiles of SM pairs: several to a pair, ragged on both sides, K that ends within a stage."""
+    product(T, N, K, out, pad=pad)
+
+
 def test_product_of_ends():
     """Scales near both ends, zeros, and NaN blocks that reach their own row or channel alone."""
     x = torch.ones(4, 96)
@@ -238,7 +245,8 @@ def layer(M, **kw):
 
 @pytest.mark.parametrize("B,N_in,N_out,M,taus", [(1, 1, 1, 1, (0.5, 0.25)), (3, 50, 70, 10, (0.5, 0.25)),
                                                 (16, 256, 300, 32, (0.4, 0.4)), (5, 784, 800, 32, (0.5, 0.25)),
-                                                (2, 130, 40, 100, (float("inf"), 0.3)), (4, 33, 129, 128, (0.5, 0.25))])
+                                                (2, 130, 40, 100, (float("inf"), 0.3)), (4, 33, 129, 128, (0.5, 0.25)),
+                                                (64, 300, 2500, 32, (0.5, 0.25)), (1, 64, 5000, 16, (0.5, 0.25))])
 def test_layer_forward(B, N_in, N_out, M, taus):
     """The layer on codes gives what its parts give: binning, quantiser, product, scan."""
     gen = torch.Generator(device="cuda").manual_seed(N_in)

@@ -34,6 +34,8 @@ def test_sizes(lib):
     assert f(TOP, TOP) == 2 ** 24 * 2 ** 24 * 512
     from paper_2607_14672_gb300 import dstd
     assert [dstd.mx4_row_bytes(k) for k in (0, 1, 32, 33, 16384)] == [0, 16, 16, 32, 8192]
+    for r, c in ((0, 5), (5, 0), (1, 1), (128, 128), (129, 129), (800, 784), (16384, 16385)):
+        assert dstd.mx4_scale_bytes(r, c) == f(r, c)
 
 
 QUANT = dict(x=P, type=0, rows=4, cols=40, ld_x=40, q=P, ld_q=32, scale=P, values=P, ld_v=40)
@@ -142,25 +144,18 @@ def calls():
     }
 
 
-@pytest.fixture
-def binding(made, monkeypatch):  # noqa: F811
-    from paper_2607_14672_gb300 import dstd
-    monkeypatch.setattr(dstd, "mx4_scale_bytes", lambda r, c: -(-r // 128) * -(-c // 128) * 512)
-    return made
-
-
 @pytest.mark.parametrize("stream", [None, 7])
 @pytest.mark.parametrize("name", ["quantize_mx4", "mx4_matmul", "dense_fwd_mx4", "top_logits", "distill_loss"])
-def test_tensors_of_another_device_are_refused(binding, name, stream):
+def test_tensors_of_another_device_are_refused(made, name, stream):  # noqa: F811
     call, tensors = calls()[name]
     call([put(aligned(x), 0) for x in tensors], stream=stream)
-    assert binding == ["dstd_" + name]
+    assert made == ["dstd_" + name]
     with pytest.raises(ValueError):
         call([put(aligned(x), 1) for x in tensors], stream=stream)
     for other in range(len(tensors)):
         with pytest.raises(ValueError):
             call([put(aligned(x), int(i == other)) for i, x in enumerate(tensors)], stream=stream)
-    assert binding == ["dstd_" + name]
+    assert made == ["dstd_" + name]
 
 
 @pytest.mark.parametrize("name,at,bad", [
@@ -178,10 +173,10 @@ def test_tensors_of_another_device_are_refused(binding, name, stream):
     ("distill_loss", 1, floats(4, 6)[:, ::2]), ("distill_loss", 2, i32(4, 3).long()), ("distill_loss", 3, floats(1)),
     ("distill_loss", 4, floats(5)), ("distill_loss", 5, floats(4, 9).half()), ("distill_loss", 5, floats(4, 8)),
     ("distill_loss", 6, floats(3))])
-def test_shapes_and_types_are_refused(binding, name, at, bad):
+def test_shapes_and_types_are_refused(made, name, at, bad):  # noqa: F811
     call, tensors = calls()[name]
     tensors = [put(aligned(x), 0) for x in tensors]
     tensors[at] = put(bad, 0)
     with pytest.raises(ValueError):
         call(tensors)
-    assert binding == []
+    assert made == []
