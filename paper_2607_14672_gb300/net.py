@@ -59,13 +59,66 @@ class Clipped:
         return 2 * ((len(self.W) + 511) // 512)
 
 
-class DenseNet(Clipped):
+class Taught:
+    """Learning from a teacher's answers: a network's largest output logits
+    (``answers``), and the distillation loss from such a record."""
+
+    record = None  # (logits, classes) [B, K] of the teacher, once learn_from has been called
+
+    def logit_factor(self):
+        """The output times t give logits factor t; silent outputs count as the last layer's t_end."""
+        if not self.cfg.get("tau_soft"):
+            raise ValueError("output logits need a configuration with tau_soft")
+        return -1.0 / self.cfg["tau_soft"], self.layers[-1]["t_end"]
+
+    def answers(self, top, index, stream=None):
+        """The K largest logits of the last forward and their classes, into top and index [B, K]."""
+        factor, silent = self.logit_factor()
+        dstd.top_logits(self.t[-1], top, index, factor, silent, stream)
+
+    def learn_from(self, K, weight=1.0, teacher_factor=1.0, labels=True):
+        """From now on the loss has weight times the distillation loss from
+        records of K entries (``set_teacher``), whose softmax is taken with
+        teacher_factor; beside the cross-entropy of the labels, or instead."""
+        self.logit_factor()
+        self.record = (torch.zeros(self.B, K, dtype=torch.float32, device=self.device),
+                       torch.full((self.B, K), -1, dtype=torch.int32, device=self.device))
+        self.taught_loss = torch.zeros(2, dtype=torch.float32, device=self.device)  # value, the kernel's scratch
+        self.taught_rows = torch.zeros(self.B, dtype=torch.float32, device=self.device)
+        self.taught = dict(weight=float(weight), teacher_factor=float(teacher_factor))
+        self.from_labels = bool(labels)
+        self.loss.zero_()
+
+    def set_teacher(self, top, index):
+        """The teacher's record for the present batch (rows of classes -1: no teacher)."""
+        if self.record is None:
+            raise RuntimeError("set_teacher: call learn_from first")
+        self.record[0].copy_(torch.as_tensor(top), non_blocking=True)
+        self.record[1].copy_(torch.as_tensor(index), non_blocking=True)
+
+    def has_label_loss(self):
+        return self.record is None or self.from_labels
+
+    def teach(self, stream=None):
+        """The distillation loss and its gradient, added to that of the labels if there is one."""
+        if self.record is None:
+            return
+        factor, silent = self.logit_factor()
+        dstd.distill_loss(self.t[-1], *self.record, self.taught_loss, self.taught_rows, self.g[-1], factor, silent,
+                          accumulate=self.from_labels, stream=stream, **self.taught)
+
+    def taught_value(self):
+        return 0.0 if self.record is None else self.taught_loss[0]
+
+
+class DenseNet(Clipped, Taught):
     """A stack of dense DSTD layers (configs.py layer dicts) on one GPU.
 
     math_mode "q8" trains for 8-bit weights: every forward quantises the
     weights by rows and runs the layers' contractions on 8-bit codes; the
     backward (three-product mode) runs at the values the codes stand for, and
     the gradient passes straight through the rounding to the fp32 weights.
+    "mx4" does the same in 4 bits, with a power of two for each 32 weights of a row.
     ``serve`` is the forward alone on the codes of the last ``quantize`` or
     ``take_codes`` (``has_codes``: there are some).
     max_norm: clip the AdamW step's gradients to this global norm.
@@ -73,8 +126,9 @@ class DenseNet(Clipped):
 
     def __init__(self, cfg, math_mode="x3", batch=None, device="cuda", with_adamw=False, max_norm=None):
         self.cfg = cfg
-        self.q8 = math_mode == "q8"
-        self.math = "x3" if self.q8 else math_mode
+        self.q8, self.mx4 = math_mode == "q8", math_mode == "mx4"
+        self.coded = self.q8 or self.mx4
+        self.math = "x3" if self.coded else math_mode
         self.max_norm = max_norm
         math_mode = self.math
         self.B = int(batch or cfg["batch"])
@@ -95,12 +149,18 @@ class DenseNet(Clipped):
         self.gW = [torch.empty_like(w) for w in self.W]
         ws = max(dstd.dense_workspace_bytes(B, self.sizes[l], self.sizes[l + 1], self.p[l], math_mode)
                  for l in range(len(self.W)))
-        if self.q8:
-            need = [dstd.dense_q8_workspace_bytes(B, self.sizes[l], self.sizes[l + 1], self.p[l])
-                    for l in range(len(self.W))]
+        if self.coded:
+            query = dstd.dense_q8_workspace_bytes if self.q8 else dstd.dense_mx4_workspace_bytes
+            need = [query(B, self.sizes[l], self.sizes[l + 1], self.p[l]) for l in range(len(self.W))]
             ws = 0 if ws == 0 or 0 in need else max(ws, *need)
-            self.Wq = [torch.empty_like(w, dtype=torch.int8) for w in self.W]
-            self.w_scale = [torch.empty(w.shape[0], dtype=torch.float32, device=dev) for w in self.W]
+            if self.q8:
+                self.Wq = [torch.empty_like(w, dtype=torch.int8) for w in self.W]
+                self.w_scale = [torch.empty(w.shape[0], dtype=torch.float32, device=dev) for w in self.W]
+            else:
+                self.Wq = [torch.empty(w.shape[0], dstd.mx4_row_bytes(w.shape[1]), dtype=torch.uint8, device=dev)
+                           for w in self.W]
+                self.w_scale = [torch.empty(dstd.mx4_scale_bytes(*w.shape), dtype=torch.uint8, device=dev)
+                                for w in self.W]
             self.Wv = [torch.empty_like(w) for w in self.W]
             self.has_codes = False
         if ws == 0:
@@ -133,15 +193,16 @@ class DenseNet(Clipped):
         return self.t_in if l == 0 else self.t[l - 1]
 
     def quantize(self, stream=None):
-        """8-bit codes, row scales and values of the present weights."""
+        """Codes, scales and values of the present weights."""
+        quantize = dstd.quantize_rows if self.q8 else dstd.quantize_mx4
         for w, q, scale, v in zip(self.W, self.Wq, self.w_scale, self.Wv):
-            dstd.quantize_rows(w, q, scale, v, stream)
+            quantize(w, q, scale, v, stream)
         self.has_codes = True
 
     def take_codes(self, other):
-        """The 8-bit weights of another q8 network of the same layers (e.g. of another batch size)."""
-        if not (self.q8 and other.q8 and other.has_codes):
-            raise ValueError("take_codes: both networks must be of mode q8, and the other one must have codes")
+        """The codes of another network of the same mode and layers (e.g. of another batch size)."""
+        if not (self.coded and self.q8 == other.q8 and self.mx4 == other.mx4 and other.has_codes):
+            raise ValueError("take_codes: both networks must be of mode q8, or both of mx4, and the other one must have codes")
         if self.sizes != other.sizes:
             raise ValueError(f"take_codes: layers of {self.sizes} neurons cannot take those of {other.sizes}")
         self.has_codes = True
@@ -149,15 +210,16 @@ class DenseNet(Clipped):
             mine.copy_(theirs)
 
     def serve(self, stream=None):
-        """The forward on the 8-bit codes as they are (no weight is read in fp32)."""
-        if not (self.q8 and self.has_codes):
-            raise RuntimeError("serve: no 8-bit codes; a q8 network has them after quantize, forward or take_codes")
+        """The forward on the codes as they are (no weight is read in fp32)."""
+        if not (self.coded and self.has_codes):
+            raise RuntimeError("serve: no codes; a q8 or mx4 network has them after quantize, forward or take_codes")
+        layer = dstd.dense_fwd_q8 if self.q8 else dstd.dense_fwd_mx4
         for l in range(len(self.W)):
-            dstd.dense_fwd_q8(self.layer_input(l), self.Wq[l], self.w_scale[l], self.p[l], self.t[l], self.saved[l],
-                              self.penalty[l], self.workspace, stream)
+            layer(self.layer_input(l), self.Wq[l], self.w_scale[l], self.p[l], self.t[l], self.saved[l],
+                  self.penalty[l], self.workspace, stream)
 
     def forward(self, stream=None):
-        if self.q8:
+        if self.coded:
             self.quantize(stream)
             self.serve(stream)
             return
@@ -166,16 +228,18 @@ class DenseNet(Clipped):
                            self.penalty[l], self.workspace, stream)
 
     def loss_grad(self, stream=None):
-        if self.loss_kind == "ce":
-            dstd.ce_loss(self.t[-1], self.labels, self.cfg["tau_soft"], self.layers[-1]["t_end"], self.loss,
-                         self.g[-1], stream)
-        else:
-            dstd.sum_t_loss(self.t[-1], self.loss, self.g[-1], stream)
+        if self.has_label_loss():
+            if self.loss_kind == "ce":
+                dstd.ce_loss(self.t[-1], self.labels, self.cfg["tau_soft"], self.layers[-1]["t_end"], self.loss,
+                             self.g[-1], stream)
+            else:
+                dstd.sum_t_loss(self.t[-1], self.loss, self.g[-1], stream)
+        self.teach(stream)
 
     def forward_loss(self, stream=None):
         """forward, then the loss; with the CE loss the output layer and the
         loss are one library call (one kernel when the layer has few outputs)."""
-        if self.loss_kind != "ce" or self.q8:
+        if self.loss_kind != "ce" or self.coded or not self.has_label_loss():
             self.forward(stream)
             self.loss_grad(stream)
             return
@@ -186,12 +250,13 @@ class DenseNet(Clipped):
         dstd.dense_fwd_ce(self.layer_input(L - 1), self.W[L - 1], self.p[L - 1], self.math, self.t[L - 1],
                           self.saved[L - 1], self.penalty[L - 1], self.workspace, self.labels, self.cfg["tau_soft"],
                           self.layers[-1]["t_end"], self.loss, self.g[L - 1], stream)
+        self.teach(stream)
 
     def backward(self, stream=None):
         for l in range(len(self.W) - 1, -1, -1):
             g_in = self.g[l - 1] if l > 0 else None
-            dstd.dense_bwd(self.layer_input(l), self.Wv[l] if self.q8 else self.W[l], self.t[l], self.saved[l], self.g[l], self.p[l],
-                           self.math, g_in, self.gW[l], self.workspace, stream)
+            dstd.dense_bwd(self.layer_input(l), self.Wv[l] if self.coded else self.W[l], self.t[l], self.saved[l],
+                           self.g[l], self.p[l], self.math, g_in, self.gW[l], self.workspace, stream)
 
     def step(self, stream=None):
         """One training step: forward, loss, backward (and AdamW if enabled)."""
@@ -201,15 +266,16 @@ class DenseNet(Clipped):
             self.optimizer(stream=stream)
 
     def objective(self):
-        """Eq. cost_function on the last batch: loss + T + gamma_Q Q (device scalar)."""
-        return self.loss[0] + self.penalty[:, 0].sum() + self.penalty[:, 1].sum()
+        """Eq. cost_function on the last batch: loss + T + gamma_Q Q (device scalar); the loss with the
+        teacher's part where there is one."""
+        return self.loss[0] + self.taught_value() + self.penalty[:, 0].sum() + self.penalty[:, 1].sum()
 
     def launches_per_step(self):
         """Kernels the library launches per ``step`` (memsets not counted)."""
         tc = self.math != "f32"
         L = len(self.W)
-        if self.q8:
-            raise NotImplementedError("launches_per_step counts the f32, x3 and bf16 modes")
+        if self.coded or self.record is not None:
+            raise NotImplementedError("launches_per_step counts the f32, x3 and bf16 modes, without a teacher")
         fused_loss = self.loss_kind == "ce" and narrow_layer(self.sizes[-2], self.sizes[-1], self.layers[-1]["M"],
                                                              self.math)
         n = 0 if fused_loss else 1                # loss (inside the output layer's kernel when fused)
@@ -227,7 +293,7 @@ class DenseNet(Clipped):
         return n
 
 
-class ConvNet(Clipped):
+class ConvNet(Clipped, Taught):
     """A stack of conv DSTD layers and a dense readout (configs 4 and 5) on one GPU.
 
     Spike tensors are NHWC ([B, H, W, C]); filters are kept as [C_out, k, k,
@@ -343,8 +409,10 @@ class ConvNet(Clipped):
                                self.penalty[l], self.workspace, stream)
 
     def loss_grad(self, stream=None):
-        dstd.ce_loss(self.t[-1], self.labels, self.cfg["tau_soft"], self.layers[-1]["t_end"], self.loss,
-                     self.g[-1], stream)
+        if self.has_label_loss():
+            dstd.ce_loss(self.t[-1], self.labels, self.cfg["tau_soft"], self.layers[-1]["t_end"], self.loss,
+                         self.g[-1], stream)
+        self.teach(stream)
 
     def backward(self, stream=None):
         """Layers in reverse. A layer's input gradient overwrites the previous
@@ -384,7 +452,7 @@ class ConvNet(Clipped):
             self.optimizer(stream=stream)
 
     def objective(self):
-        return self.loss[0] + self.penalty[:, 0].sum() + self.penalty[:, 1].sum()
+        return self.loss[0] + self.taught_value() + self.penalty[:, 0].sum() + self.penalty[:, 1].sum()
 
     def dead_fraction(self):
         """Share of silent neurons per layer on the last batch (from the Q counters)."""
