@@ -51,105 +51,177 @@ __device__ __forceinline__ long long scale_at(long long r, int b, int ktiles) {
 
 struct Quant4Args {
     int rows, cols, blocks;
-    long long ld_x, ld_q, ld_v, items;
+    long long ld_x, ld_q, ld_v;
     uint8_t *q, *scale;
     float *values;
 };
 
-// A lane holds P = 16 / sizeof(T) columns of a block, 32 / P lanes make a block and a
-// warp takes U runs of 32 P columns of one row, all loads first.
-template <class T, bool PACKED, int U>
+// P = 16 / sizeof(T) columns as they are in memory: the bits of the largest |x| as fp32, and codes of x pre
+template <class T>
+struct Quant4 {
+    static constexpr int P = Pack<T>::P;
+    static __device__ __forceinline__ uint32_t top(const uint4 &w) {
+        if constexpr (P == 4) {
+            return max(max(w.x & 0x7fffffffu, w.y & 0x7fffffffu), max(w.z & 0x7fffffffu, w.w & 0x7fffffffu));
+        } else {  // two at a time: the bits without the sign order like the values, NaN on top
+            const uint32_t m = __vmaxu2(__vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu),
+                                        __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu));
+            return max(m >> 16, m & 0xffffu);
+        }
+    }
+    static __device__ __forceinline__ uint32_t fp32_bits(uint32_t top) {
+        if constexpr (P == 4) {
+            return top;
+        } else {
+            const unsigned short h = (unsigned short)top;
+            return __float_as_uint(to_f32<T>(*reinterpret_cast<const T *>(&h)));
+        }
+    }
+    // code of column i in bits 4 i
+    static __device__ __forceinline__ uint32_t codes(const uint4 &w, float pre) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < P ? Pack<T>::one(w, i < P ? i : 0) * pre : 0.f;
+        uint32_t word;
+        asm("{\n"
+            ".reg .b8 b0, b1, b2, b3;\n"
+            "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n"
+            "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n"
+            "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n"
+            "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n"
+            "mov.b32 %0, {b0, b1, b2, b3};\n"
+            "}"
+            : "=r"(word)
+            : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+        return word;
+    }
+};
+
+// 16 bytes from any address, zeros from element `left` on: the two aligned 16-byte words that hold them, shifted
+// together (a word that holds an element of the row lies in its allocation; others are not read).
+template <class T>
+__device__ __forceinline__ uint4 load_columns(const T *p, int left) {
+    constexpr int P = Pack<T>::P;
+    const int r = (int)(reinterpret_cast<uintptr_t>(p) & 15);
+    const uint4 *word = reinterpret_cast<const uint4 *>(reinterpret_cast<uintptr_t>(p) - r);
+    const int first = (16 - r) / (int)sizeof(T);  // elements in the first word
+    uint4 u = make_uint4(0, 0, 0, 0), n = u;
+    if (left > 0) u = __ldg(word);
+    if (left > first) n = __ldg(word + 1);
+    const bool two = r & 8, one = r & 4;
+    const uint32_t w0 = two ? u.z : u.x, w1 = two ? u.w : u.y, w2 = two ? n.x : u.z, w3 = two ? n.y : u.w,
+                   w4 = two ? n.z : n.x;
+    uint32_t v[5] = {one ? w1 : w0, one ? w2 : w1, one ? w3 : w2, one ? w4 : w3, one ? (two ? n.w : n.y) : w4};
+    if constexpr (P == 8) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __funnelshift_r(v[i], v[i + 1], 8 * (r & 2));
+    }
+    constexpr int E = P / 4;  // elements of a 32-bit word
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int keep = left - E * i;
+        v[i] = keep >= E ? v[i] : (keep <= 0 ? 0u : v[i] & 0xffffu);
+    }
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
+// A lane holds P columns of a block, 32 / P lanes make a block, and a warp takes U runs of 32 P columns of one
+// row, all loads first. HBM bounds large ones: 16384 x 16384 fp32 with values in 322 us (7.1 TB/s), without in 173
+// (U = 2: 223), 4096 x 16384 bf16 without in 29 (U = 1: 44). Small ones take fewer runs a warp, so that
+// there are warps for every SM (800 x 784 fp32 with values: 2.6 us, with U = 8 3.3).
+template <class T, bool PACKED, int U, bool VALUES>
 __global__ void __launch_bounds__(256) k_quantize_mx4(const T *__restrict__ x, const Quant4Args a) {
     constexpr int P = Pack<T>::P, LANES = 32 / P, RUN = 32 * P;
     let_next_launch();
     const long long item = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (item >= a.items) return;
-    const int lane = threadIdx.x & 31;
-    const int runs = (a.cols + U * RUN - 1) / (U * RUN);
+    const int lane = threadIdx.x & 31, runs = (int)(((long long)a.cols + U * RUN - 1) / (U * RUN));
     const long long r = item < (1ll << 31) ? (long long)((unsigned)item / (unsigned)runs) : item / runs;
-    const long long c0 = (item - r * runs) * (U * RUN) + lane * P;
-    const T *row = x + r * a.ld_x;
-    float v[U][P];
+    if (r >= a.rows) return;
+    const int c0 = (int)(item - r * runs) * (U * RUN), left = a.cols - c0 - lane * P;  // columns from this lane's first on
+    const bool whole = PACKED && a.cols - c0 >= U * RUN;
+    const T *row = x + r * a.ld_x + c0 + lane * P;
+    uint4 w[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const long long c = c0 + u * RUN;
-        if (PACKED && c + P <= a.cols) {
-            const uint4 w = __ldg(reinterpret_cast<const uint4 *>(row + c));
-#pragma unroll
-            for (int i = 0; i < P; ++i) v[u][i] = Pack<T>::one(w, i);
-        } else {
-#pragma unroll
-            for (int i = 0; i < P; ++i) v[u][i] = c + i < a.cols ? to_f32<T>(row[c + i]) : 0.f;
-        }
+        if (whole || (PACKED && left - u * RUN >= P)) w[u] = __ldg(reinterpret_cast<const uint4 *>(row + u * RUN));
+        else w[u] = load_columns<T>(row + u * RUN, left - u * RUN);
     }
-    const int ktiles = (a.blocks + 3) / 4;
+    const int b0 = (c0 + lane * P) >> 5;  // this lane's block
+    uint8_t *q = a.q + r * a.ld_q + ((c0 + lane * P) >> 1);
+    uint8_t *scale = a.scale + scale_at(r, b0, (a.blocks + 3) / 4);
+    const int tiles_left = (a.blocks + 3) / 4 * 4 - b0;
+    float *val = VALUES ? a.values + r * a.ld_v + c0 + lane * P : nullptr;
+    const bool wide = VALUES && (reinterpret_cast<uintptr_t>(val) & 15) == 0;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const long long c = c0 + u * RUN;
-        const int b = (int)(c >> 5);  // this lane's block
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < P; ++i) top = max(top, __float_as_uint(v[u][i]) & 0x7fffffffu);
+        if (!whole && c0 + u * RUN >= a.cols + 96) break;  // no tile of the row's left (a whole warp)
+        uint32_t top = Quant4<T>::top(w[u]);
 #pragma unroll
         for (int d = 1; d < LANES; d *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
-        const BlockCode k = block_code(top);
-        uint32_t word = 0;
+        const BlockCode k = block_code(Quant4<T>::fp32_bits(top));
+        const uint32_t word = k.byte == 255u ? 0u : Quant4<T>::codes(w[u], k.pre);
+        if (!whole && tiles_left <= u * P) continue;
+        // P blocks a run, four of them to a tile of 512 bytes
+        if ((lane & (LANES - 1)) == 0) scale[u * P / 4 * 512] = (uint8_t)k.byte;
+        if (!whole && b0 + u * P >= a.blocks) continue;
+        if constexpr (P == 4) *reinterpret_cast<uint16_t *>(q + u * (RUN / 2)) = (uint16_t)word;
+        else *reinterpret_cast<uint32_t *>(q + u * (RUN / 2)) = word;
+        if constexpr (VALUES) {
+            const float s = block_scale(k.byte);
+            float y[P];
 #pragma unroll
-        for (int i = 0; i < P; i += 2) word |= code_pair(v[u][i] * k.pre, v[u][i + 1] * k.pre) << (4 * i);
-        if (k.byte == 255u) word = 0;
-        // the exponents of a tile's four blocks are one word
-        uint32_t bytes = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            bytes |= __shfl_sync(0xffffffffu, k.byte, (lane & ~(4 * LANES - 1)) + i * LANES) << (8 * i);
-        if (b < a.blocks) {
-            uint8_t *q = a.q + r * a.ld_q + (c >> 1);
-            if constexpr (P == 4) *reinterpret_cast<uint16_t *>(q) = (uint16_t)word;
-            else *reinterpret_cast<uint32_t *>(q) = word;
-            if (a.values) {
-                const float s = block_scale(k.byte);
-                float *val = a.values + r * a.ld_v + c;
-                float y[P];
-#pragma unroll
-                for (int i = 0; i < P; i += 2) {
-                    const float2 f = pair_values((word >> (4 * i)) & 255u);
-                    y[i] = f.x * s;
-                    y[i + 1] = f.y * s;
-                }
-                if (PACKED && c + P <= a.cols) {
-#pragma unroll
-                    for (int i = 0; i < P; i += 4)
-                        *reinterpret_cast<float4 *>(val + i) = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < P; ++i)
-                        if (c + i < a.cols) val[i] = y[i];
-                }
+            for (int i = 0; i < P; i += 2) {
+                const float2 f = pair_values((word >> (4 * i)) & 255u);
+                y[i] = f.x * s;
+                y[i + 1] = f.y * s;
             }
-            if ((lane & (4 * LANES - 1)) == 0) *reinterpret_cast<uint32_t *>(a.scale + scale_at(r, b, ktiles)) = bytes;
+            if (wide && left - u * RUN >= P) {
+#pragma unroll
+                for (int i = 0; i < P; i += 4)
+                    *reinterpret_cast<float4 *>(val + u * RUN + i) = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < P; ++i)
+                    if (u * RUN + i < left) val[u * RUN + i] = y[i];
+            }
         }
     }
 }
 
-template <class T>
-cudaError_t quantize_mx4(const T *x, Quant4Args a, cudaStream_t st) {
-    constexpr int U = 2;
-    const auto at16 = [](const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
-    const bool packed = at16(x) && (a.ld_x * (long long)sizeof(T)) % 16 == 0 &&
-                        (!a.values || (at16(a.values) && a.ld_v % 4 == 0));
-    const int runs = (int)(((long long)a.cols + U * 32 * Pack<T>::P - 1) / (U * 32 * Pack<T>::P));
-    a.items = (long long)a.rows * runs;
-    if ((a.items + 7) / 8 > 0x7fffffff) return cudaErrorInvalidValue;
-    const unsigned grid = (unsigned)((a.items + 7) / 8);
-    if (packed) k_quantize_mx4<T, true, U><<<grid, 256, 0, st>>>(x, a);
-    else k_quantize_mx4<T, false, U><<<grid, 256, 0, st>>>(x, a);
+template <class T, bool PACKED, int U>
+cudaError_t quantize_runs(const T *x, const Quant4Args &a, cudaStream_t st) {
+    constexpr int RUN = 32 * Pack<T>::P;
+    const long long items = (long long)a.rows * (((long long)a.cols + U * RUN - 1) / (U * RUN)), blocks = (items + 7) / 8;
+    if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
+    if (a.values) k_quantize_mx4<T, PACKED, U, true><<<(unsigned)blocks, 256, 0, st>>>(x, a);
+    else k_quantize_mx4<T, PACKED, U, false><<<(unsigned)blocks, 256, 0, st>>>(x, a);
     return cudaGetLastError();
+}
+
+template <class T, bool PACKED>
+cudaError_t quantize_rows4(const T *x, const Quant4Args &a, cudaStream_t st) {
+    constexpr int RUN = 32 * Pack<T>::P;
+    const int runs = (a.cols - 1) / RUN + 1;
+    const long long all = (long long)a.rows * runs;
+    constexpr int most = sizeof(T) == 4 ? 8 : 4;
+    int u = 1;
+    while (u < (a.values ? 2 : most) && u < runs && all >= 2 * u * 4800ll) u *= 2;
+    if (u == 1) return quantize_runs<T, PACKED, 1>(x, a, st);
+    if (u == 2) return quantize_runs<T, PACKED, 2>(x, a, st);
+    if (u == 4) return quantize_runs<T, PACKED, 4>(x, a, st);
+    return quantize_runs<T, PACKED, most>(x, a, st);
+}
+
+template <class T>
+cudaError_t quantize_mx4(const T *x, const Quant4Args &a, cudaStream_t st) {
+    const bool packed = (reinterpret_cast<uintptr_t>(x) & 15) == 0 && (a.ld_x * (long long)sizeof(T)) % 16 == 0;
+    return packed ? quantize_rows4<T, true>(x, a, st) : quantize_rows4<T, false>(x, a, st);
 }
 
 cudaError_t launch_quantize_mx4(const void *x, dstd_type type, int rows, int cols, long long ld_x, uint8_t *q,
                                 long long ld_q, uint8_t *scale, float *values, long long ld_v, cudaStream_t st) {
     if (rows == 0 || cols == 0) return cudaSuccess;
-    const Quant4Args a{rows, cols, mx4_blocks(cols), ld_x, ld_q, ld_v, 0, q, scale, values};
+    const Quant4Args a{rows, cols, mx4_blocks(cols), ld_x, ld_q, ld_v, q, scale, values};
     if (type == DSTD_TYPE_F32) return quantize_mx4((const float *)x, a, st);
     if (type == DSTD_TYPE_BF16) return quantize_mx4((const __nv_bfloat16 *)x, a, st);
     return quantize_mx4((const __half *)x, a, st);
@@ -273,14 +345,15 @@ struct Mx4Cfg {
     static constexpr int B_TILES = (NT + 127) / 128;  // of 128 rows of scales
     static constexpr int SF_BYTES = 2 * kScaleTile * (1 + B_TILES);
     static constexpr int STAGE = (kTileBytes + B_BYTES + SF_BYTES + 1023) / 1024 * 1024;
-    static constexpr int BUDGET = NT >= 256 ? 216 * 1024 : 108 * 1024;  // two blocks to an SM up to 128 columns
-    static constexpr int STAGES = BUDGET / STAGE > 6 ? 6 : BUDGET / STAGE;
-    static constexpr int SMEM = STAGES * STAGE + 1024 + 256;
+    static constexpr int STAGES = 216 * 1024 / STAGE;                    // a block that has an SM to itself
+    static constexpr int HALF = 108 * 1024 / STAGE;                      // two to an SM
+    static constexpr int smem(int slots) { return slots * STAGE + 1024 + 256; }
     static constexpr int SF_COL = NT;                    // scales: two sets of (A, B) in turn
     static constexpr int SF_SET = 2 * 4 * (1 + B_TILES);
     static constexpr int USED = NT + 2 * SF_SET;
     static constexpr int COLS = USED <= 64 ? 64 : (USED <= 128 ? 128 : (USED <= 256 ? 256 : 512));
-    static_assert(NT * 128 * 4 <= STAGES * STAGE, "the sums of a tile fit the stages");
+    static_assert(NT * 128 * 4 <= HALF * STAGE, "the sums of a tile fit the stages");
+    static_assert(2 * STAGES * 8 + 16 <= 256, "the barriers fit");
 };
 
 // rows of one side of the product, a the side of 128-row tiles
@@ -290,7 +363,7 @@ struct Mx4Side {
 };
 struct Mx4Tc {
     Mx4Side a, b;
-    int blocks, ktiles, tiles_a, tiles_b, parts;
+    int blocks, ktiles, tiles_a, tiles_b, parts, slots;  // slots: stages of a block's ring
     void *out;
     long long ld_a, ld_b;  // of out; one of them is 1
 };
@@ -305,36 +378,47 @@ __device__ __forceinline__ void mx4_tile(int i, int tiles_a, int tiles_b, int &t
 
 __device__ __forceinline__ void mx4_timeout() { atomicOr(&g_status_mx4, STATUS_TIMEOUT); }
 
-// CH columns of a lane's row to out: neighbouring lanes next to each other (ld_a = 1), or the lane's own
-// columns (ld_b = 1)
+// The first `left` of CH columns of a lane's row to out: neighbouring lanes next to each other (ld_a = 1), or
+// the lane's own columns (ld_b = 1). Whole runs without a test for each element (with one, storing took 64
+// us of a product of 8192 x 32 into 8192).
 template <class O, int CH>
 __device__ __forceinline__ void mx4_store(O *dst, long long ld_a, long long ld_b, const float (&v)[CH], int left) {
     if (ld_b != 1 || ld_a == 1) {
+        if (left >= CH) {
 #pragma unroll
-        for (int c = 0; c < CH; ++c)
-            if (c < left) dst[c * ld_b] = round_out<O>(v[c]);
+            for (int c = 0; c < CH; ++c, dst += ld_b) *dst = round_out<O>(v[c]);
+        } else {
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+                if (c < left) dst[c * ld_b] = round_out<O>(v[c]);
+        }
         return;
     }
     constexpr int P = 16 / sizeof(O);
-    const bool vec = (reinterpret_cast<uintptr_t>(dst) & 15) == 0;
+    if (left >= CH && (reinterpret_cast<uintptr_t>(dst) & 15) == 0) {
 #pragma unroll
-    for (int c = 0; c < CH; c += P) {
-        alignas(16) O y[P];
+        for (int c = 0; c < CH; c += P) {
+            alignas(16) O y[P];
 #pragma unroll
-        for (int u = 0; u < P; ++u) y[u] = round_out<O>(v[c + u]);
-        if (vec && c + P <= left) {
+            for (int u = 0; u < P; ++u) y[u] = round_out<O>(v[c + u]);
             *reinterpret_cast<uint4 *>(dst + c) = *reinterpret_cast<const uint4 *>(y);
-        } else {
-#pragma unroll
-            for (int u = 0; u < P; ++u)
-                if (c + u < left) dst[c + u] = y[u];
         }
+    } else if (left >= CH) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) dst[c] = round_out<O>(v[c]);
+    } else {
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            if (c < left) dst[c] = round_out<O>(v[c]);
     }
 }
 
-__device__ __forceinline__ float ld_cluster(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(addr)
+                 : "memory");
     return v;
 }
 
@@ -344,8 +428,9 @@ __global__ void __launch_bounds__(192) k_mx4_tc(const __grid_constant__ CUtensor
     using C = Mx4Cfg<NT>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    uint64_t *full = reinterpret_cast<uint64_t *>(smem + C::STAGES * C::STAGE);
-    uint64_t *empty = full + C::STAGES, *done = empty + C::STAGES;
+    const int slots = p.slots;
+    uint64_t *full = reinterpret_cast<uint64_t *>(smem + slots * C::STAGE);
+    uint64_t *empty = full + slots, *done = empty + slots;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(done + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int part = p.parts > 1 ? (int)cluster_ctarank() : 0;
@@ -355,7 +440,7 @@ __global__ void __launch_bounds__(192) k_mx4_tc(const __grid_constant__ CUtensor
     const int s0 = (int)((long long)stages * part / p.parts), s1 = (int)((long long)stages * (part + 1) / p.parts);
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < C::STAGES; ++s) {
+        for (int s = 0; s < slots; ++s) {
             mbar_init(&full[s], 1);
             mbar_init(&empty[s], 1);
         }
@@ -372,10 +457,10 @@ __global__ void __launch_bounds__(192) k_mx4_tc(const __grid_constant__ CUtensor
 
     if (warp == 4) {
         bool ok = true;
-        int it = 0;
-        for (int s = s0; s < s1; ++s, ++it) {
-            const int slot = it % C::STAGES;
-            ok = mbar_wait_cycles(&empty[slot], ((it / C::STAGES) & 1u) ^ 1u);
+        int slot = 0;
+        uint32_t turn = 0;
+        for (int s = s0; s < s1; ++s) {
+            ok = mbar_wait_cycles(&empty[slot], turn ^ 1u);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             if (elect_one()) {
@@ -397,24 +482,27 @@ __global__ void __launch_bounds__(192) k_mx4_tc(const __grid_constant__ CUtensor
                                   &full[slot]);
             }
             __syncwarp();
+            if (++slot == slots) slot = 0, turn ^= 1u;
         }
         // every stage released: no copy is in flight
-        for (int i = 0; i < C::STAGES && ok; ++i, ++it)
-            ok = mbar_wait_cycles(&empty[it % C::STAGES], ((it / C::STAGES) & 1u) ^ 1u);
+        for (int i = 0; i < slots && ok; ++i) {
+            ok = mbar_wait_cycles(&empty[slot], turn ^ 1u);
+            if (++slot == slots) slot = 0, turn ^= 1u;
+        }
         if (!ok) mx4_timeout();
         __syncwarp();
     } else if (warp == 5) {
         bool ok = true;
-        int it = 0;
-        for (int s = s0; s < s1; ++s, ++it) {
-            const int slot = it % C::STAGES;
-            ok = mbar_wait_cycles(&full[slot], (it / C::STAGES) & 1u);
+        int slot = 0;
+        uint32_t turn = 0;
+        for (int s = s0; s < s1; ++s) {
+            ok = mbar_wait_cycles(&full[slot], turn);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
                 const uint32_t st = smem_u32(smem + slot * C::STAGE), sf = st + kTileBytes + C::B_BYTES;
-                const uint32_t sfa = tmem + C::SF_COL + (it & 1) * C::SF_SET, sfb = sfa + 8;
+                const uint32_t sfa = tmem + C::SF_COL + (s & 1) * C::SF_SET, sfb = sfa + 8;
                 const uint64_t ad = sdesc_sw128(st), bd = sdesc_sw128(st + kTileBytes);
                 const int left = p.blocks - s * kStageBlocks;
 #pragma unroll
@@ -430,13 +518,14 @@ __global__ void __launch_bounds__(192) k_mx4_tc(const __grid_constant__ CUtensor
                         const int kk = 2 * h + i;
                         if (kk * 2 >= left) break;
                         mma_mx4(tmem, ad + kk * 2, bd + kk * 2, idesc_mx4(128, NT, 2 * i), sfa + h * 4,
-                                sfb + h * C::B_TILES * 4, it > 0 || kk > 0 ? 1u : 0u);
+                                sfb + h * C::B_TILES * 4, s > s0 || kk > 0 ? 1u : 0u);
                     }
                 }
                 mma_commit(&empty[slot]);
                 if (s + 1 == s1) mma_commit(done);
             }
             __syncwarp();
+            if (++slot == slots) slot = 0, turn ^= 1u;
         }
         if (!ok) mx4_timeout();
         __syncwarp();
@@ -473,16 +562,44 @@ __global__ void __launch_bounds__(192) k_mx4_tc(const __grid_constant__ CUtensor
     if (p.parts > 1) {
         __syncwarp();
         cluster_sync();
-        // this block's share of the columns
+        // this block's share of the columns, 4 rows of one at a time: all blocks' sums on their way, then added in order
         const int first = NT * part / p.parts, last = NT * (part + 1) / p.parts;
         const uint32_t base = smem_u32(smem);
-        for (int i = threadIdx.x; i < (last - first) * 128; i += 192) {
-            const int c = first + (i >> 7), row = i & 127;
-            float sum = 0.f;
-            for (int q = 0; q < p.parts; ++q) sum += ld_cluster(mapa_rank(base + (c * 128 + row) * 4, q));
-            const long long r = (long long)ta * 128 + row, col = (long long)tb * NT + c;
-            if (r < p.a.rows && col < p.b.rows)
-                static_cast<O *>(p.out)[r * p.ld_a + col * p.ld_b] = round_out<O>(sum);
+        O *out = static_cast<O *>(p.out);
+        const int units = (last - first) * 32;
+        constexpr int U = NT >= 64 ? 4 : 1;  // a thread's units at a time
+        for (int i0 = threadIdx.x; i0 < units; i0 += U * 192) {
+            float4 sum[U], v[U][8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                if (q >= p.parts) break;
+                const uint32_t from = mapa_rank(base, q);
+#pragma unroll
+                for (int e = 0; e < U; ++e) {
+                    const int i = i0 + e * 192;
+                    if (i < units) v[e][q] = ld_cluster4(from + ((first + (i >> 5)) * 128 + (i & 31) * 4) * 4);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < U; ++e) {
+                sum[e] = v[e][0];
+#pragma unroll
+                for (int q = 1; q < 8; ++q) {
+                    if (q >= p.parts) break;
+                    sum[e].x += v[e][q].x;
+                    sum[e].y += v[e][q].y;
+                    sum[e].z += v[e][q].z;
+                    sum[e].w += v[e][q].w;
+                }
+                const int i = i0 + e * 192;
+                const long long r = (long long)ta * 128 + (i & 31) * 4, col = (long long)tb * NT + first + (i >> 5);
+                if (i >= units || col >= p.b.rows) continue;
+                O *dst = out + r * p.ld_a + col * p.ld_b;
+                const float y[4] = {sum[e].x, sum[e].y, sum[e].z, sum[e].w};
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (r + u < p.a.rows) dst[u * p.ld_a] = round_out<O>(y[u]);
+            }
         }
         __syncwarp();
         cluster_sync();
@@ -685,7 +802,7 @@ Mx4Tc mx4_sides(const Mx4Args &a, const Mx4Plan &plan, int tile_a, int tile_b) {
     const bool ex = plan.exchanged;
     const int rows_a = ex ? a.T : a.N, rows_b = ex ? a.N : a.T;
     return Mx4Tc{{ex ? a.x_scale : a.w_scale, rows_a}, {ex ? a.w_scale : a.x_scale, rows_b}, a.blocks, (a.blocks + 3) / 4,
-                 (rows_a - 1) / tile_a + 1, (rows_b - 1) / tile_b + 1, plan.parts, a.out.p,
+                 (rows_a - 1) / tile_a + 1, (rows_b - 1) / tile_b + 1, plan.parts, 0, a.out.p,
                  ex ? a.out.ld_t : a.out.ld_n, ex ? a.out.ld_n : a.out.ld_t};
 }
 
@@ -748,18 +865,19 @@ cudaError_t launch_mx4_tc(const Mx4Args &a, const Mx4Plan &plan, cudaStream_t st
     using C = Mx4Cfg<NT>;
     static PerDevice granted;
     if (!granted.get([](int) {
-            return cudaFuncSetAttribute(k_mx4_tc<NT, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) ==
-                           cudaSuccess ? 1 : 0;
+            return cudaFuncSetAttribute(k_mx4_tc<NT, O>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                        C::smem(C::STAGES)) == cudaSuccess ? 1 : 0;
         }))
         return cudaErrorInvalidConfiguration;
     const bool ex = plan.exchanged;
-    const Mx4Tc p = mx4_sides(a, plan, 128, NT);
+    Mx4Tc p = mx4_sides(a, plan, 128, NT);
     CUtensorMap map_a, map_b;
     if (!code_map(&map_a, ex ? a.x : a.w, p.a.rows, a.blocks, ex ? a.ld_x : a.ld_w, 128) ||
         !code_map(&map_b, ex ? a.w : a.x, p.b.rows, a.blocks, ex ? a.ld_w : a.ld_x, NT))
         return cudaErrorInvalidValue;
     const long long grid = (long long)p.tiles_a * p.tiles_b * plan.parts;
     if (grid > 0x7fffffff) return cudaErrorInvalidValue;
+    p.slots = grid <= 152 && plan.parts == 1 ? C::STAGES : C::HALF;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -772,7 +890,7 @@ cudaError_t launch_mx4_tc(const Mx4Args &a, const Mx4Plan &plan, cudaStream_t st
     cfg.numAttrs = plan.parts > 1 ? 2 : 1;
     cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3(192);
-    cfg.dynamicSmemBytes = C::SMEM;
+    cfg.dynamicSmemBytes = C::smem(p.slots);
     cfg.stream = st;
     return cudaLaunchKernelEx(&cfg, k_mx4_tc<NT, O>, map_a, map_b, p);
 }
@@ -792,12 +910,24 @@ Mx4Plan mx4_plan(const Mx4Args &q) {
     p.nt = width(b);
     p.parts = 1;
     const long long pair_tiles = (((long long)a + 255) / 256) * (((long long)b + 255) / 256);
-    if (pair_tiles >= 76 && b > 128) {
+    if (pair_tiles >= 48 && b > 128) {
         p.nt = 0;
         return p;
     }
+    // K is shared where that is faster, by times in us of a stage and of joining 2, 4 and 8 parts (measured at 1 x
+    // 4096 x 4096: 7.1 in one piece, 5.4 in four; 64 x 16384 into 2000: 22.3 and 11.0; 300 x 16384 into 130: 24.4
+    // and, in eight, 12.5), and where all blocks have an SM to themselves
+    const double stage = p.nt <= 32 ? 0.26 : (p.nt == 64 ? 0.29 : 0.33);
+    const double join[3][3] = {{1.6, 1.6, 1.8}, {2.7, 2.4, 2.7}, {4.2, 4.3, 4.5}};
     const long long tiles = (((long long)a + 127) / 128) * (((long long)b + p.nt - 1) / p.nt);
-    while (p.parts < 8 && tiles * p.parts * 2 <= 304 && p.parts * 2 <= stages) p.parts *= 2;
+    double best = stages * stage;
+    for (int i = 0; i < 3; ++i) {
+        const int parts = 2 << i;
+        const double cost = stages * stage / parts + join[p.nt <= 32 ? 0 : (p.nt == 64 ? 1 : 2)][i];
+        if (tiles * parts > 152 || parts > stages || cost >= best) continue;
+        best = cost;
+        p.parts = parts;
+    }
     return p;
 }
 
