@@ -610,8 +610,8 @@ int dstd_top_logits(const void *y, dstd_type type, int R, int C, int64_t ld_y, f
  *  row_loss [R] out.
  *  g     [R, C] of `type` out, row stride ld_g >= C, not overlapping y; NULL:
  *        the losses alone. accumulate != 0 adds the gradient to what g holds.
- * Sums are formed in fp32 (fp64 over rows) in a fixed order; each gradient is
- * rounded once. */
+ * Sums are formed in fp32 (over rows with what the additions lost) in a fixed
+ * order; each gradient is rounded once. */
 int dstd_distill_loss(const void *y, dstd_type type, int R, int C, int64_t ld_y, float factor, float silent,
                       const float *top, const int32_t *index, int K, float teacher_factor, float weight,
                       const float *row_weight, float *loss, float *row_loss, void *g, int64_t ld_g, int accumulate,

@@ -150,12 +150,13 @@ struct HeldRow {
 // logits are ordered as 32-bit keys (-0 as 0, NaN above all). Each thread takes
 // the largest of its columns; the K-th largest of those is a bound that none of
 // the row's K largest is below, and few are above it: with 512 threads and K = 64
-// about 68. Those are gathered and put in order by counting, for each, the larger ones. Rows
-// with more than kCap logits at the bound (many equal ones) go digit by digit. Few long rows
+// about 68. Those are gathered and put in order by counting, for each, the larger ones. Of rows
+// with more than kFew logits at the bound (many equal ones) those above it are gathered, and the first
+// columns of the equal ones. Few long rows
 // are shared by the blocks of a cluster, which then count each other's.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t key_of(float z) {
-    if (z != z) return 0xffffffffu;
+    if (z != z) return 0xfffffffeu;
     const uint32_t u = __float_as_uint(z + 0.f);  // -0 + 0 = 0
     return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
@@ -177,6 +178,7 @@ template <>
 struct Two<__nv_bfloat16> { using type = __nv_bfloat162; };
 
 constexpr int kCap = 2048;
+constexpr int kFew = 512;  // as many are put in order by counting: the square of them
 
 __device__ __forceinline__ uint64_t ld_cluster64(uint32_t addr) {
     uint64_t v;
@@ -282,38 +284,58 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
     }
     __syncthreads();
     unsigned n = s_n;
-    if (n > kCap) {
-        uint32_t prefix = 0, mask = 0;
-        unsigned need = want;
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int i = t; i < 256; i += THREADS) s_hist[i] = 0;
-            __syncthreads();
-            each([&](int, uint32_t k) {
-                if ((k & mask) == prefix) atomicAdd(&s_hist[(k >> shift) & 255u], 1u);
-            });
-            __syncthreads();
-            if (t == 0) {
-                unsigned above = 0;
-                int d = 255;
-                while (d > 0 && above + s_hist[d] < need) above += s_hist[d--];
-                s_digit[0] = (unsigned)d;
-                s_digit[1] = above;
-            }
-            __syncthreads();
-            prefix |= s_digit[0] << shift;
-            mask |= 255u << shift;
-            need -= s_digit[1];
-            __syncthreads();
+    if (n > kFew) {
+        // many equal logits at the bound. Those above the exact K-th largest of the threads' largest are few, as a rule:
+        uint32_t last = bound;
+        for (int bit = 15; bit >= 0; --bit) {
+            const uint32_t trial = last | (1u << bit);
+            if (__syncthreads_count(mine >= trial) >= want) last = trial;
         }
-        if (t == 0) s_n = 0;
-        __syncthreads();
-        each([&](int c, uint32_t k) {
-            if (k > prefix) s_cand[atomicAdd(&s_n, 1u)] = (uint64_t)k << 32 | (uint32_t)~c;
-        });
-        // the first `need` columns of those equal to the last one wanted
+        const auto above = [&](uint32_t least) {
+            if (t == 0) s_n = 0;
+            __syncthreads();
+            if (mine > least)
+                each([&](int c, uint32_t k) {
+                    if (k <= least) return;
+                    const unsigned at = atomicAdd(&s_n, 1u);
+                    if (at < kCap) s_cand[at] = (uint64_t)k << 32 | (uint32_t)~c;
+                });
+            __syncthreads();
+            return s_n;
+        };
+        n = above(last);
+        if (n > kFew) {
+            // the K-th largest digit by digit
+            uint32_t mask = 0;
+            unsigned need = want;
+            last = 0;
+            for (int shift = 24; shift >= 0; shift -= 8) {
+                for (int i = t; i < 256; i += THREADS) s_hist[i] = 0;
+                __syncthreads();
+                each([&](int, uint32_t k) {
+                    if ((k & mask) == last) atomicAdd(&s_hist[(k >> shift) & 255u], 1u);
+                });
+                __syncthreads();
+                if (t == 0) {
+                    unsigned over = 0;
+                    int d = 255;
+                    while (d > 0 && over + s_hist[d] < need) over += s_hist[d--];
+                    s_digit[0] = (unsigned)d;
+                    s_digit[1] = over;
+                }
+                __syncthreads();
+                last |= s_digit[0] << shift;
+                mask |= 255u << shift;
+                need -= s_digit[1];
+                __syncthreads();
+            }
+            n = above(last);
+        }
+        // then the first columns of those equal to it
+        const unsigned need = n < (unsigned)want ? want - n : 0;
         unsigned found = 0;
         for (int c0 = v.low; c0 < v.high && found < need; c0 += THREADS) {
-            const bool here = c0 + t < v.high && key_of(logit.of(to_f32<T>(v.row[c0 + t]))) == prefix;
+            const bool here = c0 + t < v.high && key_of(logit.of(to_f32<T>(v.row[c0 + t]))) == last;
             const unsigned ballot = __ballot_sync(0xffffffffu, here);
             if ((t & 31) == 0) s_warp[t >> 5] = __popc(ballot);
             __syncthreads();
@@ -323,11 +345,11 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
                 all += s_warp[w];
             }
             before += __popc(ballot & ((1u << (t & 31)) - 1u));
-            if (here && before < need) s_cand[want - need + before] = (uint64_t)prefix << 32 | (uint32_t)~(uint32_t)(c0 + t);
+            if (here && before < need) s_cand[n + before] = (uint64_t)last << 32 | (uint32_t)~(uint32_t)(c0 + t);
             found = all;
             __syncthreads();
         }
-        n = want;
+        n += need;
         __syncthreads();
     }
     const auto put = [&](uint64_t e, int rank) {
@@ -370,6 +392,40 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
     }
 }
 
+// Rows of up to 32 E classes: a warp to a row; a logit's place is the number of logits before it (larger, or equal
+// in an earlier column).
+template <class T, int E>
+__global__ void __launch_bounds__(256) k_top_small(const LogitArgs a, const int K, float *top, int32_t *index) {
+    __shared__ uint32_t s_key[8][32 * E];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long r = (long long)blockIdx.x * 8 + warp;
+    if (r >= a.rows) return;
+    const Logit logit(a);
+    const T *row = static_cast<const T *>(a.y) + r * a.ld;
+    uint32_t key[E];
+    int rank[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int c = lane + 32 * e;
+        key[e] = c < a.cols ? key_of(logit.of(to_f32<T>(row[c]))) : 0u;
+        s_key[warp][c] = key[e];
+        rank[e] = 0;
+    }
+    __syncwarp();
+#pragma unroll 4
+    for (int j = 0; j < a.cols; ++j) {
+        const uint32_t other = s_key[warp][j];
+#pragma unroll
+        for (int e = 0; e < E; ++e) rank[e] += other >= key[e] + (j < lane + 32 * e ? 0u : 1u);
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (lane + 32 * e < a.cols && rank[e] < K) {
+            top[r * K + rank[e]] = logit_of_key(key[e]);
+            index[r * K + rank[e]] = lane + 32 * e;
+        }
+}
+
 // blocks that share a row: where the rows alone do not fill the GPU, up to 8 of at least `least` packs
 int shares(int rows, int packs, int least) {
     int parts = 1;
@@ -404,6 +460,15 @@ cudaError_t top_rows(const LogitArgs &a, int K, float *top, int32_t *index, cuda
 
 template <class T>
 cudaError_t top_logits(const LogitArgs &a, int K, float *top, int32_t *index, cudaStream_t st) {
+    const unsigned blocks = ((unsigned)a.rows + 7) / 8;
+    if (a.cols <= 32) {
+        k_top_small<T, 1><<<blocks, 256, 0, st>>>(a, K, top, index);
+        return cudaGetLastError();
+    }
+    if (a.cols <= 128) {
+        k_top_small<T, 4><<<blocks, 256, 0, st>>>(a, K, top, index);
+        return cudaGetLastError();
+    }
     if constexpr (sizeof(T) == 2)
         if (a.factor * a.silent == -INFINITY) return top_rows<T, true>(a, K, top, index, st);
     return top_rows<T, false>(a, K, top, index, st);
@@ -502,7 +567,7 @@ __device__ __forceinline__ void join_lanes(float &m, float &s) {
 
 // the last block adds the rows' losses up, in a fixed order
 __device__ __forceinline__ void finish_loss(const DistillArgs &a, unsigned blocks) {
-    __shared__ double s_total[32];
+    __shared__ float s_total[32];
     __shared__ unsigned s_last;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -512,28 +577,63 @@ __device__ __forceinline__ void finish_loss(const DistillArgs &a, unsigned block
     __syncthreads();
     if (!s_last) return;
     __threadfence();
-    double sum = 0.0;
-    for (long long i = threadIdx.x; i < a.y.rows; i += blockDim.x) {
-        const float w = a.row_weight ? a.row_weight[i] : 1.f / (float)a.y.rows;
-        if (w != 0.f) sum += (double)w * __ldcg(a.row_loss + i);
+    // each thread's sum with what its additions lost (64-bit additions took most of a readout's time)
+    float sum = 0.f, lost = 0.f;
+    const float even = 1.f / (float)a.y.rows;
+    for (long long i0 = threadIdx.x; i0 < a.y.rows; i0 += 8 * blockDim.x) {
+        float w[8], loss[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const long long i = i0 + e * blockDim.x;
+            w[e] = i >= a.y.rows ? 0.f : (a.row_weight ? a.row_weight[i] : even);
+            loss[e] = i < a.y.rows ? __ldcg(a.row_loss + i) : 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float x = w[e] != 0.f ? __fmul_rn(w[e], loss[e]) : 0.f, all = __fadd_rn(sum, x);
+            const float part = __fsub_rn(all, sum);
+            lost = __fadd_rn(lost, __fadd_rn(__fsub_rn(sum, __fsub_rn(all, part)), __fsub_rn(x, part)));
+            sum = all;
+        }
     }
+    // an infinite sum has lost nothing that could be told
+    if (isfinite(sum)) sum += lost;
 #pragma unroll
     for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     if ((threadIdx.x & 31) == 0) s_total[threadIdx.x >> 5] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        sum = s_total[0];
-        for (unsigned i = 1; i < blockDim.x / 32; ++i) sum += s_total[i];
-        a.loss[0] = (float)(a.weight * sum);
-        *reinterpret_cast<unsigned *>(a.loss + 1) = 0u;
+    if (threadIdx.x < 32) {
+        sum = threadIdx.x < blockDim.x / 32 ? s_total[threadIdx.x] : 0.f;
+#pragma unroll
+        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (threadIdx.x == 0) {
+            a.loss[0] = a.weight * sum;
+            *reinterpret_cast<unsigned *>(a.loss + 1) = 0u;
+        }
     }
 }
 
-// Rows of up to 256 classes and 64 entries: a warp to a row, 8 columns a lane.
+// Columns that a teacher names, to find one named twice: open addressing, exact.
+template <int SLOTS>
+__device__ __forceinline__ bool named_before(int *slot, int at) {
+    for (int i = at & (SLOTS - 1);; i = (i + 1) & (SLOTS - 1)) {
+        const int was = atomicCAS(&slot[i], -1, at);
+        if (was == at) return true;
+        if (was == -1) return false;
+    }
+}
+
+// Rows of up to 32 E classes and 64 entries: a warp to a row, E columns a lane.
 template <class T>
+__device__ __forceinline__ float exp_for(float x) {
+    if constexpr (sizeof(T) == 4) return expf(x);
+    else return __expf(x);  // off by 2^-21 or so, far below a 16-bit rounding
+}
+
+template <class T, int E>
 __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
-    constexpr int E = 8;
-    __shared__ int s_at[8][64];
+    constexpr int SLOTS = 128;
+    __shared__ int s_at[8][64], s_slot[8][SLOTS];
     __shared__ float s_p[8][64];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long r = (long long)blockIdx.x * 8 + warp;
@@ -541,17 +641,19 @@ __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
         const Logit logit(a.y);
         const T *row = static_cast<const T *>(a.y.y) + r * a.y.ld;
         T *g = a.g ? static_cast<T *>(a.g) + r * a.ld_g : nullptr;
+        const Record<2> record(a, r, lane);
         const float rw = a.row_weight ? a.row_weight[r] : 1.f / (float)a.y.rows;
-        float z[E], was[E];
-        bool silent[E];
+        float z[E];
+        uint32_t silent = 0;
 #pragma unroll
         for (int i = 0; i < E; ++i) {
             const int c = lane + 32 * i;
-            silent[i] = true;
-            z[i] = c < a.y.cols ? logit.of(to_f32<T>(row[c]), silent[i]) : -INFINITY;
-            was[i] = a.accumulate && g && c < a.y.cols ? to_f32<T>(g[c]) : 0.f;
+            bool none = true;
+            z[i] = c < a.y.cols ? logit.of(to_f32<T>(row[c]), none) : -INFINITY;
+            silent |= (none ? 1u : 0u) << i;
         }
-        const Record<2> record(a, r, lane);
+#pragma unroll
+        for (int i = 0; i < SLOTS / 32; ++i) s_slot[warp][lane + 32 * i] = -1;
         const bool any = record.any();
         Teacher entry[2];
         {
@@ -569,13 +671,19 @@ __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
                 s_p[warp][32 * e + lane] = entry[e].p;
             }
         }
+        __syncwarp();
+        bool again = false;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (entry[e].at >= 0 && named_before<SLOTS>(s_slot[warp], entry[e].at)) again = true;
+        const bool twice = __any_sync(0xffffffffu, again);
         float m = -INFINITY, s = 0.f;
 #pragma unroll
         for (int i = 0; i < E; ++i) m = fmaxf(m, z[i]);
 #pragma unroll
         for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
 #pragma unroll
-        for (int i = 0; i < E; ++i) s += z[i] == -INFINITY ? 0.f : expf(z[i] - m);
+        for (int i = 0; i < E; ++i) s += z[i] == -INFINITY ? 0.f : exp_for<T>(z[i] - m);
 #pragma unroll
         for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
         // a row without logits has no softmax: it is left out (a NaN counts as a logit)
@@ -589,26 +697,28 @@ __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
         for (int d = 16; d; d >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, d);
         if (lane == 0) a.row_loss[r] = loss;
         if (g && (done || !a.accumulate)) {
-            const float coef = a.weight * rw * logit.factor;
+            const float coef = a.weight * rw * logit.factor, over = coef / s;
 #pragma unroll
             for (int i = 0; i < E; ++i) {
                 const int c = lane + 32 * i;
-                if (c < a.y.cols)
-                    g[c] = round_out<T>(was[i] + (silent[i] || !done ? 0.f : expf(z[i] - m) * (coef / s)));
+                if (c >= a.y.cols) continue;
+                const float d = ((silent >> i) & 1u) || !done ? 0.f : exp_for<T>(z[i] - m) * over;
+                g[c] = round_out<T>(a.accumulate ? to_f32<T>(g[c]) + d : d);
             }
             __syncwarp();
             if (done) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const Teacher &t = entry[e];
-                    float mass;
-                    if (t.at >= 0 && !t.silent && column_mass(s_at[warp], s_p[warp], 32 * e + lane, a.K, mass))
+                    float mass = t.p;
+                    if (t.at >= 0 && !t.silent &&
+                        (!twice || column_mass(s_at[warp], s_p[warp], 32 * e + lane, a.K, mass)))
                         g[t.at] = round_out<T>(t.old + (expf(t.z - m) / s - mass) * coef);
                 }
             }
         }
     }
-    finish_loss(a, gridDim.x);
+    if (a.ticket) finish_loss(a, gridDim.x);
 }
 
 // FAST: 16-bit outputs without a stand-in for silent ones, whose exp is 0 by
@@ -729,12 +839,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill(const Disti
         s_at[t] = teach.at;
         s_p[t] = teach.p;
         // a column named twice finds itself in the table
-        if (teach.at >= 0)
-            for (int i = teach.at & (SLOTS - 1);; i = (i + 1) & (SLOTS - 1)) {
-                const int was = atomicCAS(&s_slot[i], -1, teach.at);
-                if (was == teach.at) s_twice = 1;
-                if (was == -1 || was == teach.at) break;
-            }
+        if (teach.at >= 0 && named_before<SLOTS>(s_slot, teach.at)) s_twice = 1;
         float loss = teacher_loss(teach, m, logf(s));
 #pragma unroll
         for (int d = 16; d; d >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, d);
@@ -811,30 +916,41 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill(const Disti
 }
 
 // the rows' losses added up by a launch of its own, where a block should not wait for its stores to count itself
-__global__ void __launch_bounds__(1024) k_distill_sum(const DistillArgs a) { finish_loss(a, 1); }
+__global__ void __launch_bounds__(1024) k_distill_sum(const DistillArgs a) {
+    wait_launch_before();
+    finish_loss(a, 1);
+}
 
+// the rows' losses: by the last block where a block to each few rows fits the GPU at once, else by a launch of its own
 template <class T, bool FAST>
-cudaError_t distill_rows(DistillArgs a, int &launches, cudaStream_t st) {
+cudaError_t distill_rows(const DistillArgs &a, cudaStream_t st) {
     const int packs = (int)(((long long)a.y.cols * sizeof(T) + 15) / 16), parts = shares(a.y.rows, packs, 512);
-    a.ticket = a.y.rows <= 304;
-    const cudaError_t e = packs / parts <= 256 * kHeld
-                              ? launch_shared(k_distill<T, 256, FAST>, a.y.rows, parts, 256, st, a, parts)
-                              : launch_shared(k_distill<T, 512, FAST>, a.y.rows, parts, 512, st, a, parts);
-    if (e != cudaSuccess || a.ticket) return e;
-    launches = 2;
-    k_distill_sum<<<1, 1024, 0, st>>>(a);
-    return cudaGetLastError();
+    // few blocks have more threads each
+    return packs / parts <= 256 * kHeld && (a.y.rows * parts >= 152 || packs / parts <= 512)
+               ? launch_shared(k_distill<T, 256, FAST>, a.y.rows, parts, 256, st, a, parts)
+               : launch_shared(k_distill<T, 512, FAST>, a.y.rows, parts, 512, st, a, parts);
 }
 
 template <class T>
-cudaError_t distill(const DistillArgs &a, int &launches, cudaStream_t st) {
-    if (a.y.cols <= 256 && a.K <= 64) {
-        k_distill_small<T><<<((unsigned)a.y.rows + 7) / 8, 256, 0, st>>>(a);
-        return cudaGetLastError();
+cudaError_t distill(DistillArgs a, int &launches, cudaStream_t st) {
+    const bool small = a.y.cols <= 1024 && a.K <= 64;
+    const unsigned blocks = ((unsigned)a.y.rows + 7) / 8;
+    a.ticket = a.y.rows <= (small ? 8 * 304 : 304);
+    cudaError_t e;
+    if (small && a.y.cols <= 256) {
+        k_distill_small<T, 8><<<blocks, 256, 0, st>>>(a);
+        e = cudaGetLastError();
+    } else if (small) {
+        k_distill_small<T, 32><<<blocks, 256, 0, st>>>(a);
+        e = cudaGetLastError();
+    } else if (sizeof(T) == 2 && a.y.factor * a.y.silent == -INFINITY && fabsf(a.y.factor) < 1e30f) {
+        e = distill_rows<T, sizeof(T) == 2>(a, st);
+    } else {
+        e = distill_rows<T, false>(a, st);
     }
-    if constexpr (sizeof(T) == 2)
-        if (a.y.factor * a.y.silent == -INFINITY && fabsf(a.y.factor) < 1e30f) return distill_rows<T, true>(a, launches, st);
-    return distill_rows<T, false>(a, launches, st);
+    if (e != cudaSuccess || a.ticket) return e;
+    launches = 2;
+    return launch_dependent(k_distill_sum, 1, 1024, st, a);
 }
 
 }  // namespace
