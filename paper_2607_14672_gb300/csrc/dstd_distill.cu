@@ -119,28 +119,37 @@ struct RowView {
     }
 };
 
-constexpr int kHeld = 8;  // packs of a thread in registers; those of longer rows are read in every pass
+// A block's packs wait in shared memory, kHeld to a thread (64 KB for 512 threads, so that three rows are on an SM;
+// in registers there were two); those of longer rows are read in every pass. A thread reads back what it copied alone.
+constexpr int kHeld = 8;
 
 template <class T, int THREADS>
 struct HeldRow {
-    uint4 raw[kHeld];
+    const uint4 *slot;
     float one;
     int at;  // column of `one`, or -1
-    __device__ __forceinline__ HeldRow(const RowView<T> &v) {
+    // starts the copies; ready() before any use
+    __device__ __forceinline__ HeldRow(const RowView<T> &v, uint4 *held) {
         const int k0 = v.first + (int)threadIdx.x, left = v.last - k0;
         const uint4 *p = reinterpret_cast<const uint4 *>(v.row + v.head) + k0;
+        const uint32_t to = smem_u32(held + threadIdx.x);
 #pragma unroll
-        for (int j = 0; j < kHeld; ++j) raw[j] = j * THREADS < left ? __ldg(p + j * THREADS) : make_uint4(0, 0, 0, 0);
+        for (int j = 0; j < kHeld; ++j)
+            if (j * THREADS < left)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + j * THREADS * 16), "l"(p + j * THREADS)
+                             : "memory");
+        slot = held + threadIdx.x;
         at = v.single(threadIdx.x);
         one = at >= 0 ? to_f32<T>(v.row[at]) : 0.f;
     }
+    __device__ __forceinline__ void ready() const { asm volatile("cp.async.wait_all;" ::: "memory"); }
     // f(pack, its number) for every pack of this thread
     template <class F>
     __device__ __forceinline__ void each(const RowView<T> &v, F f) const {
         const int k0 = v.first + (int)threadIdx.x, left = v.last - k0;
 #pragma unroll
         for (int j = 0; j < kHeld; ++j)
-            if (j * THREADS < left) f(raw[j], k0 + j * THREADS);
+            if (j * THREADS < left) f(slot[j * THREADS], k0 + j * THREADS);
         for (int k = k0 + kHeld * THREADS; k < v.last; k += THREADS) f(v.pack(k), k);
     }
 };
@@ -177,7 +186,6 @@ struct Two<__half> { using type = __half2; };
 template <>
 struct Two<__nv_bfloat16> { using type = __nv_bfloat162; };
 
-constexpr int kCap = 2048;
 constexpr int kFew = 512;  // as many are put in order by counting: the square of them
 
 __device__ __forceinline__ uint64_t ld_cluster64(uint32_t addr) {
@@ -219,16 +227,17 @@ struct PackMax {
 };
 
 template <class T, int THREADS, bool PAIRS>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS)
+__global__ void __launch_bounds__(THREADS, 1536 / THREADS)
     k_top_logits(const LogitArgs a, const int parts, const int K, float *top, int32_t *index) {
     constexpr int P = Pack<T>::P;
-    __shared__ uint64_t s_cand[kCap], s_best[kTopMax];
+    __shared__ uint64_t s_cand[kFew], s_best[kTopMax];
     __shared__ unsigned s_n, s_hits, s_hist[256], s_digit[2], s_warp[THREADS / 32];
-    __shared__ int s_hit[kCap];
+    __shared__ int s_hit[kFew];
     const int t = threadIdx.x, part = parts > 1 ? (int)cluster_ctarank() : 0;
     const long long r = blockIdx.x / parts;
     const RowView<T> v(a, r, part, parts);
-    const HeldRow<T, THREADS> h(v);
+    extern __shared__ uint4 s_held[];
+    const HeldRow<T, THREADS> h(v, s_held);
     const Logit logit(a);
     const PackMax<T, PAIRS, true> pack_max(logit);
     if (t == 0) s_n = s_hits = 0;
@@ -241,6 +250,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
         });
     };
     const int want = min(K, v.high - v.low);
+    h.ready();
     uint32_t mine = 0, bound = 0;  // 0: below every logit's key
     {
         float m = -INFINITY;
@@ -262,7 +272,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
         const uint32_t k = key_of(z);
         if (k < bound) return;
         const unsigned at = atomicAdd(&s_n, 1u);
-        if (at < kCap) s_cand[at] = (uint64_t)k << 32 | (uint32_t)~c;
+        if (at < kFew) s_cand[at] = (uint64_t)k << 32 | (uint32_t)~c;
     };
     if (h.at >= 0) gather(h.at, logit.of(h.one));
     if (mine >= bound) {
@@ -270,12 +280,12 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
         h.each(v, [&](const uint4 &w, int k) {
             if (pack_max(w) < least) return;
             const unsigned at = atomicAdd(&s_hits, 1u);
-            if (at < kCap) s_hit[at] = k;
+            if (at < kFew) s_hit[at] = k;
         });
     }
     __syncthreads();
-    if (s_hits > kCap) {
-        if (t == 0) s_n = kCap + 1;
+    if (s_hits > kFew) {
+        if (t == 0) s_n = kFew + 1u;
     } else {
         for (unsigned i = t; i < s_hits * P; i += THREADS) {
             const int c = v.head + s_hit[i / P] * P + (int)(i % P);
@@ -298,7 +308,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
                 each([&](int c, uint32_t k) {
                     if (k <= least) return;
                     const unsigned at = atomicAdd(&s_n, 1u);
-                    if (at < kCap) s_cand[at] = (uint64_t)k << 32 | (uint32_t)~c;
+                    if (at < kFew) s_cand[at] = (uint64_t)k << 32 | (uint32_t)~c;
                 });
             __syncthreads();
             return s_n;
@@ -369,9 +379,10 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
         if (t >= want && t < K) s_best[t] = 0;  // below every entry
         __syncwarp();
         cluster_sync();
-        // all shares' entries, in the blocks' order
+        // all shares' entries, in the blocks' order, where the row was
+        uint64_t *s_all = reinterpret_cast<uint64_t *>(s_held);
         for (int i = t; i < parts * K; i += THREADS)
-            s_cand[i] = ld_cluster64(mapa_rank(smem_u32(s_best + i % K), (uint32_t)(i / K)));
+            s_all[i] = ld_cluster64(mapa_rank(smem_u32(s_best + i % K), (uint32_t)(i / K)));
         __syncwarp();
         cluster_sync();
         if (t < want) {
@@ -382,7 +393,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
                 int lo = 0, hi = K;  // entries above me
                 while (lo < hi) {
                     const int mid = (lo + hi) / 2;
-                    if (s_cand[q * K + mid] > me) lo = mid + 1;
+                    if (s_all[q * K + mid] > me) lo = mid + 1;
                     else hi = mid;
                 }
                 rank += lo;
@@ -433,8 +444,14 @@ int shares(int rows, int packs, int least) {
     return parts;
 }
 
-template <class... P, class... A>
-cudaError_t launch_shared(void (*kernel)(P...), int rows, int parts, int threads, cudaStream_t st, const A &...args) {
+template <auto KERNEL, int THREADS, class... A>
+cudaError_t launch_shared(int rows, int parts, cudaStream_t st, const A &...args) {
+    constexpr int held = kHeld * THREADS * 16;
+    static PerDevice granted;
+    if (!granted.get([](int) {
+            return cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, held) == cudaSuccess ? 1 : 0;
+        }))
+        return cudaErrorInvalidConfiguration;
     if ((long long)rows * parts > 0x7fffffff) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
@@ -445,17 +462,18 @@ cudaError_t launch_shared(void (*kernel)(P...), int rows, int parts, int threads
     cfg.attrs = attr;
     cfg.numAttrs = parts > 1 ? 1 : 0;
     cfg.gridDim = dim3((unsigned)(rows * parts));
-    cfg.blockDim = dim3((unsigned)threads);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = held;
     cfg.stream = st;
-    return cudaLaunchKernelEx(&cfg, kernel, args...);
+    return cudaLaunchKernelEx(&cfg, KERNEL, args...);
 }
 
 template <class T, bool PAIRS>
 cudaError_t top_rows(const LogitArgs &a, int K, float *top, int32_t *index, cudaStream_t st) {
     const int packs = (int)(((long long)a.cols * sizeof(T) + 15) / 16), parts = shares(a.rows, packs, 512);
     if (packs / parts <= 256 * kHeld)
-        return launch_shared(k_top_logits<T, 256, PAIRS>, a.rows, parts, 256, st, a, parts, K, top, index);
-    return launch_shared(k_top_logits<T, 512, PAIRS>, a.rows, parts, 512, st, a, parts, K, top, index);
+        return launch_shared<k_top_logits<T, 256, PAIRS>, 256>(a.rows, parts, st, a, parts, K, top, index);
+    return launch_shared<k_top_logits<T, 512, PAIRS>, 512>(a.rows, parts, st, a, parts, K, top, index);
 }
 
 template <class T>
@@ -632,7 +650,7 @@ __device__ __forceinline__ float exp_for(float x) {
 
 template <class T, int E>
 __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
-    constexpr int SLOTS = 128;
+    constexpr int SLOTS = 256;
     __shared__ int s_at[8][64], s_slot[8][SLOTS];
     __shared__ float s_p[8][64];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -725,7 +743,7 @@ __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
 // itself: exp(z - m) = 2^(factor log2(e) y - m log2(e)), one multiply-add and the
 // special-function unit (the product's rounding moves it by 2^-24 |z|, far below a 16-bit rounding).
 template <class T, int THREADS, bool FAST>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill(const DistillArgs a, const int parts) {
+__global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const DistillArgs a, const int parts) {
     constexpr int P = Pack<T>::P, WARPS = THREADS / 32;
     constexpr int SLOTS = 2 * kTopMax;
     __shared__ float2 s_stat[WARPS], s_share[8];
@@ -740,7 +758,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill(const Disti
     const bool teaches = warp * 32 < a.K;
     int own_at = -1;
     if (teaches && warp * 32 + lane < a.K) own_at = a.index[r * a.K + warp * 32 + lane];
-    const HeldRow<T, THREADS> h(v);
+    extern __shared__ uint4 s_held[];
+    const HeldRow<T, THREADS> h(v, s_held);
     const float rw = a.row_weight ? a.row_weight[r] : 1.f / (float)a.y.rows;
     for (int i = t; i < SLOTS; i += THREADS) s_slot[i] = -1;
     float own_y = 0.f, own_old = 0.f;
@@ -760,6 +779,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill(const Disti
             s_twice = 0;
         }
     }
+    h.ready();
     // largest logit and sum, over the warp's columns
     float m = -INFINITY, s = 0.f;
     const float scale = logit.factor * kLog2e;
@@ -927,8 +947,8 @@ cudaError_t distill_rows(const DistillArgs &a, cudaStream_t st) {
     const int packs = (int)(((long long)a.y.cols * sizeof(T) + 15) / 16), parts = shares(a.y.rows, packs, 512);
     // few blocks have more threads each
     return packs / parts <= 256 * kHeld && (a.y.rows * parts >= 152 || packs / parts <= 512)
-               ? launch_shared(k_distill<T, 256, FAST>, a.y.rows, parts, 256, st, a, parts)
-               : launch_shared(k_distill<T, 512, FAST>, a.y.rows, parts, 512, st, a, parts);
+               ? launch_shared<k_distill<T, 256, FAST>, 256>(a.y.rows, parts, st, a, parts)
+               : launch_shared<k_distill<T, 512, FAST>, 512>(a.y.rows, parts, st, a, parts);
 }
 
 template <class T>
@@ -937,7 +957,10 @@ cudaError_t distill(DistillArgs a, int &launches, cudaStream_t st) {
     const unsigned blocks = ((unsigned)a.y.rows + 7) / 8;
     a.ticket = a.y.rows <= (small ? 8 * 304 : 304);
     cudaError_t e;
-    if (small && a.y.cols <= 256) {
+    if (small && a.y.cols <= 64) {
+        k_distill_small<T, 2><<<blocks, 256, 0, st>>>(a);
+        e = cudaGetLastError();
+    } else if (small && a.y.cols <= 256) {
         k_distill_small<T, 8><<<blocks, 256, 0, st>>>(a);
         e = cudaGetLastError();
     } else if (small) {
