@@ -119,26 +119,28 @@ struct RowView {
     }
 };
 
-// A block's packs wait in shared memory, kHeld to a thread (64 KB for 512 threads, so that three rows are on an SM;
-// in registers there were two); those of longer rows are read in every pass. A thread reads back what it copied alone.
-constexpr int kHeld = 8;
-
-template <class T, int THREADS>
+// A block's packs wait in shared memory, HELD to a thread (about 64 KB for 512 threads, so that three rows are on an
+// SM; in registers there were two); those of longer rows are read in every pass. A thread reads back what it
+// copied alone.
+template <class T, int THREADS, int HELD>
 struct HeldRow {
     const uint4 *slot;
     float one;
     int at;  // column of `one`, or -1
     // starts the copies; ready() before any use
-    __device__ __forceinline__ HeldRow(const RowView<T> &v, uint4 *held) {
+    __device__ __forceinline__ HeldRow(const RowView<T> &v, uint4 *held, bool mine = true) {
+        slot = held + threadIdx.x;
+        at = -1;
+        one = 0.f;
+        if (!mine) return;
         const int k0 = v.first + (int)threadIdx.x, left = v.last - k0;
         const uint4 *p = reinterpret_cast<const uint4 *>(v.row + v.head) + k0;
         const uint32_t to = smem_u32(held + threadIdx.x);
 #pragma unroll
-        for (int j = 0; j < kHeld; ++j)
+        for (int j = 0; j < HELD; ++j)
             if (j * THREADS < left)
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + j * THREADS * 16), "l"(p + j * THREADS)
                              : "memory");
-        slot = held + threadIdx.x;
         at = v.single(threadIdx.x);
         one = at >= 0 ? to_f32<T>(v.row[at]) : 0.f;
     }
@@ -148,9 +150,9 @@ struct HeldRow {
     __device__ __forceinline__ void each(const RowView<T> &v, F f) const {
         const int k0 = v.first + (int)threadIdx.x, left = v.last - k0;
 #pragma unroll
-        for (int j = 0; j < kHeld; ++j)
+        for (int j = 0; j < HELD; ++j)
             if (j * THREADS < left) f(slot[j * THREADS], k0 + j * THREADS);
-        for (int k = k0 + kHeld * THREADS; k < v.last; k += THREADS) f(v.pack(k), k);
+        for (int k = k0 + HELD * THREADS; k < v.last; k += THREADS) f(v.pack(k), k);
     }
 };
 
@@ -160,7 +162,7 @@ struct HeldRow {
 // the largest of its columns; the K-th largest of those is a bound that none of
 // the row's K largest is below, and few are above it: with 512 threads and K = 64
 // about 68. Those are gathered and put in order by counting, for each, the larger ones. Of rows
-// with more than kFew logits at the bound (many equal ones) those above it are gathered, and the first
+// with many more logits at the bound (equal ones) those above it are gathered, and the first
 // columns of the equal ones. Few long rows
 // are shared by the blocks of a cluster, which then count each other's.
 // ---------------------------------------------------------------------------
@@ -186,7 +188,8 @@ struct Two<__half> { using type = __half2; };
 template <>
 struct Two<__nv_bfloat16> { using type = __nv_bfloat162; };
 
-constexpr int kFew = 512;  // as many are put in order by counting: the square of them
+constexpr int kTopHeld = 8;
+constexpr int kFew = 512;  // as many at most are put in order by counting, the square of them; kTopMax * 3 / 2 + 64 fit
 
 __device__ __forceinline__ uint64_t ld_cluster64(uint32_t addr) {
     uint64_t v;
@@ -237,7 +240,7 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS)
     const long long r = blockIdx.x / parts;
     const RowView<T> v(a, r, part, parts);
     extern __shared__ uint4 s_held[];
-    const HeldRow<T, THREADS> h(v, s_held);
+    const HeldRow<T, THREADS, kTopHeld> h(v, s_held);
     const Logit logit(a);
     const PackMax<T, PAIRS, true> pack_max(logit);
     if (t == 0) s_n = s_hits = 0;
@@ -288,13 +291,15 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS)
         if (t == 0) s_n = kFew + 1u;
     } else {
         for (unsigned i = t; i < s_hits * P; i += THREADS) {
-            const int c = v.head + s_hit[i / P] * P + (int)(i % P);
-            gather(c, logit.of(to_f32<T>(v.row[c])));
+            const int k = s_hit[i / P], c = v.head + k * P + (int)(i % P);
+            const T *from = k - v.first < kTopHeld * THREADS ? reinterpret_cast<const T *>(s_held + (k - v.first)) + i % P
+                                                             : v.row + c;
+            gather(c, logit.of(to_f32<T>(*from)));
         }
     }
     __syncthreads();
     unsigned n = s_n;
-    if (n > kFew) {
+    if (n > (unsigned)(K + K / 2 + 64)) {
         // many equal logits at the bound. Those above the exact K-th largest of the threads' largest are few, as a rule:
         uint32_t last = bound;
         for (int bit = 15; bit >= 0; --bit) {
@@ -444,9 +449,9 @@ int shares(int rows, int packs, int least) {
     return parts;
 }
 
-template <auto KERNEL, int THREADS, class... A>
+template <auto KERNEL, int THREADS, int PACKS, class... A>
 cudaError_t launch_shared(int rows, int parts, cudaStream_t st, const A &...args) {
-    constexpr int held = kHeld * THREADS * 16;
+    constexpr int held = PACKS * 16;  // bytes
     static PerDevice granted;
     if (!granted.get([](int) {
             return cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, held) == cudaSuccess ? 1 : 0;
@@ -471,9 +476,9 @@ cudaError_t launch_shared(int rows, int parts, cudaStream_t st, const A &...args
 template <class T, bool PAIRS>
 cudaError_t top_rows(const LogitArgs &a, int K, float *top, int32_t *index, cudaStream_t st) {
     const int packs = (int)(((long long)a.cols * sizeof(T) + 15) / 16), parts = shares(a.rows, packs, 512);
-    if (packs / parts <= 256 * kHeld)
-        return launch_shared<k_top_logits<T, 256, PAIRS>, 256>(a.rows, parts, st, a, parts, K, top, index);
-    return launch_shared<k_top_logits<T, 512, PAIRS>, 512>(a.rows, parts, st, a, parts, K, top, index);
+    if (packs / parts <= 256 * kTopHeld)
+        return launch_shared<k_top_logits<T, 256, PAIRS>, 256, 256 * kTopHeld>(a.rows, parts, st, a, parts, K, top, index);
+    return launch_shared<k_top_logits<T, 512, PAIRS>, 512, 512 * kTopHeld>(a.rows, parts, st, a, parts, K, top, index);
 }
 
 template <class T>
@@ -739,57 +744,30 @@ __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
     if (a.ticket) finish_loss(a, gridDim.x);
 }
 
-// FAST: 16-bit outputs without a stand-in for silent ones, whose exp is 0 by
+constexpr int kRowHeld = 9;
+
+// The last warp of a block has the teacher's entries, the others the row. FAST: 16-bit outputs without a stand-in for silent ones, whose exp is 0 by
 // itself: exp(z - m) = 2^(factor log2(e) y - m log2(e)), one multiply-add and the
 // special-function unit (the product's rounding moves it by 2^-24 |z|, far below a 16-bit rounding).
 template <class T, int THREADS, bool FAST>
 __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const DistillArgs a, const int parts) {
-    constexpr int P = Pack<T>::P, WARPS = THREADS / 32;
-    constexpr int SLOTS = 2 * kTopMax;
+    constexpr int P = Pack<T>::P, ROW = THREADS - 32, WARPS = ROW / 32, SLOTS = 2 * kTopMax;
     __shared__ float2 s_stat[WARPS], s_share[8];
-    __shared__ float s_loss[kTopMax / 32], s_p[kTopMax];
+    __shared__ float s_p[kTopMax], s_log[kTopMax], s_z[kTopMax], s_old[kTopMax];
     __shared__ int s_any, s_twice, s_at[kTopMax], s_slot[SLOTS];
+    extern __shared__ uint4 s_held[];
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31, part = parts > 1 ? (int)cluster_ctarank() : 0;
     const long long r = blockIdx.x / parts;
+    const bool teaches = warp == WARPS;
     const RowView<T> v(a.y, r, part, parts);
     const Logit logit(a.y);
     T *g = a.g ? static_cast<T *>(a.g) + r * a.ld_g : nullptr;
-    // the teacher's entries on their way before the row: all to each warp that has entries of its own
-    const bool teaches = warp * 32 < a.K;
-    int own_at = -1;
-    if (teaches && warp * 32 + lane < a.K) own_at = a.index[r * a.K + warp * 32 + lane];
-    extern __shared__ uint4 s_held[];
-    const HeldRow<T, THREADS> h(v, s_held);
     const float rw = a.row_weight ? a.row_weight[r] : 1.f / (float)a.y.rows;
-    for (int i = t; i < SLOTS; i += THREADS) s_slot[i] = -1;
-    float own_y = 0.f, own_old = 0.f;
-    if (own_at >= 0 && own_at < a.y.cols) {
-        own_y = to_f32<T>(v.row[own_at]);
-        if (a.accumulate && g) own_old = to_f32<T>(g[own_at]);
-    }
-    if (warp == 0) {
-        bool some = false;
-        for (int k = lane; k < a.K; k += 32) {
-            const int at = a.index[r * a.K + k];
-            some = some || (at >= 0 && at < a.y.cols && a.teacher_factor * a.top[r * a.K + k] != -INFINITY);
-        }
-        some = __any_sync(0xffffffffu, some);
-        if (lane == 0) {
-            s_any = some;
-            s_twice = 0;
-        }
-    }
-    h.ready();
-    // largest logit and sum, over the warp's columns
-    float m = -INFINITY, s = 0.f;
+    const HeldRow<T, ROW, kRowHeld> h(v, s_held, !teaches);
     const float scale = logit.factor * kLog2e;
-    if (h.at >= 0) m = logit.of(h.one);
-    const PackMax<T, FAST, false> pack_max(logit);
-    h.each(v, [&](const uint4 &w, int) { m = fmaxf(m, pack_max(w)); });
-#pragma unroll
-    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    // nothing but -infinity: every exp below is 0 with any finite m (NaN stays NaN)
-    float base = m == -INFINITY ? 0.f : m;
+    float m = -INFINITY, s = 0.f;
+    // nothing but -infinity: every exp below is 0 with any finite base (NaN stays NaN)
+    float base = 0.f;
     const auto exp_of = [&](float y) {
         if constexpr (FAST) return exp2_fast(fmaf(y, scale, -base * kLog2e));
         else return expf(logit.of(y) - base);
@@ -802,25 +780,80 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const Disti
             return (uint64_t)w;
         }
     };
-    if constexpr (FAST) {
-        uint64_t two = pair_of(0.f, 0.f);
-        h.each(v, [&](const uint4 &w, int) {
-            two = add_pair(two, add_pair(add_pair(exp_pair(w.x), exp_pair(w.y)), add_pair(exp_pair(w.z), exp_pair(w.w))));
-        });
-        const float2 f = of_pair(two);
-        s = f.x + f.y;
+    if (teaches) {
+        // the teacher's softmax, and which of its columns are named twice, beside the others' work on the row
+        for (int i = lane; i < SLOTS; i += 32) s_slot[i] = -1;
+        float tm = -INFINITY;
+        bool some = false;
+        for (int k = lane; k < a.K; k += 32) {
+            int at = a.index[r * a.K + k];
+            const float z = a.teacher_factor * a.top[r * a.K + k];
+            if (at >= a.y.cols || z == -INFINITY) at = -1;
+            s_at[k] = at;
+            s_log[k] = z;
+            if (at < 0) continue;
+            some = true;
+            tm = fmaxf(tm, z);
+        }
+#pragma unroll
+        for (int d = 16; d; d >>= 1) tm = fmaxf(tm, __shfl_xor_sync(0xffffffffu, tm, d));
+        __syncwarp();
+        float sum = 0.f;
+        bool again = false;
+        for (int k = lane; k < a.K; k += 32) {
+            const int at = s_at[k];
+            if (at < 0) continue;
+            bool silent;
+            const float z = logit.of(to_f32<T>(v.row[at]), silent);
+            s_z[k] = z;
+            s_old[k] = a.accumulate && g ? to_f32<T>(g[at]) : 0.f;
+            if (silent) s_at[k] = at | (1 << 30);  // its column gets no gradient
+            sum += expf(s_log[k] - tm);
+            if (named_before<SLOTS>(s_slot, at)) again = true;
+        }
+#pragma unroll
+        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        const float log_sum = logf(sum);
+        for (int k = lane; k < a.K; k += 32) {
+            const float log_p = s_log[k] - tm - log_sum;
+            s_log[k] = log_p;
+            s_p[k] = s_at[k] >= 0 ? expf(log_p) : 0.f;
+        }
+        some = __any_sync(0xffffffffu, some);
+        again = __any_sync(0xffffffffu, again);
+        if (lane == 0) {
+            s_any = some;
+            s_twice = again;
+        }
     } else {
-        h.each(v, [&](const uint4 &w, int) {
-            float part_sum = 0.f;
+        // largest logit and sum, over the warp's columns
+        h.ready();
+        if (h.at >= 0) m = logit.of(h.one);
+        const PackMax<T, FAST, false> pack_max(logit);
+        h.each(v, [&](const uint4 &w, int) { m = fmaxf(m, pack_max(w)); });
 #pragma unroll
-            for (int i = 0; i < P; ++i) part_sum += exp_of(Pack<T>::one(w, i));
-            s += part_sum;
-        });
+        for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+        base = m == -INFINITY ? 0.f : m;
+        if constexpr (FAST) {
+            uint64_t two = pair_of(0.f, 0.f);
+            h.each(v, [&](const uint4 &w, int) {
+                two = add_pair(two, add_pair(add_pair(exp_pair(w.x), exp_pair(w.y)), add_pair(exp_pair(w.z), exp_pair(w.w))));
+            });
+            const float2 f = of_pair(two);
+            s = f.x + f.y;
+        } else {
+            h.each(v, [&](const uint4 &w, int) {
+                float part_sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < P; ++i) part_sum += exp_of(Pack<T>::one(w, i));
+                s += part_sum;
+            });
+        }
+        if (h.at >= 0) s += exp_of(h.one);
+#pragma unroll
+        for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+        if (lane == 0) s_stat[warp] = make_float2(m, s);
     }
-    if (h.at >= 0) s += exp_of(h.one);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-    if (lane == 0) s_stat[warp] = make_float2(m, s);
     __syncthreads();
     const bool any = s_any != 0;
     {
@@ -844,27 +877,6 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const Disti
     // a row without logits has no softmax: it is left out (a NaN counts as a logit)
     const bool done = any && rw != 0.f && !(m == -INFINITY && !(s != s));
     base = m == -INFINITY ? 0.f : m;
-    Teacher teach;
-    teach.at = -1;
-    if (teaches && done) {
-        const Record<kTopMax / 32> record(a, r, lane);
-        float tm, tl;
-        record.softmax(tm, tl);
-        const float z = t < a.K ? a.teacher_factor * a.top[r * a.K + t] : -INFINITY;
-        teach.at = own_at >= 0 && own_at < a.y.cols && z != -INFINITY ? own_at : -1;
-        teach.z = logit.of(own_y, teach.silent);
-        teach.old = own_old;
-        teach.log_p = z - tm - tl;
-        teach.p = teach.at >= 0 ? expf(teach.log_p) : 0.f;
-        s_at[t] = teach.at;
-        s_p[t] = teach.p;
-        // a column named twice finds itself in the table
-        if (teach.at >= 0 && named_before<SLOTS>(s_slot, teach.at)) s_twice = 1;
-        float loss = teacher_loss(teach, m, logf(s));
-#pragma unroll
-        for (int d = 16; d; d >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, d);
-        if (lane == 0) s_loss[warp] = loss;
-    }
     const float coef = a.weight * rw * logit.factor, over = done ? coef / s : 0.f;
     const auto grad = [&](float y) {
         if constexpr (FAST) return exp_of(y) * over;
@@ -892,7 +904,9 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const Disti
             });
         }
     };
-    if (g && done) {
+    if (teaches) {
+        // (it has no columns)
+    } else if (g && done) {
         if (h.at >= 0) g[h.at] = round_out<T>(grad(h.one) + (a.accumulate ? to_f32<T>(g[h.at]) : 0.f));
         if (a.accumulate)
             write([&](const uint4 &w, const T *was, T (&out)[P]) {
@@ -918,21 +932,26 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const Disti
             for (int i = 0; i < P; ++i) out[i] = round_out<T>(0.f);
         });
     }
+    if (teaches && part == 0) {
+        float loss = 0.f;
+        const float log_sum = logf(s);
+        if (done)
+            for (int k = lane; k < a.K; k += 32)
+                if (s_p[k] != 0.f) loss += s_p[k] * (s_log[k] - (s_z[k] - m - log_sum));
+#pragma unroll
+        for (int d = 16; d; d >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, d);
+        if (lane == 0) a.row_loss[r] = loss;
+    }
     __syncthreads();
-    if (g && done && teach.at >= 0 && !teach.silent && teach.at >= v.low && teach.at < v.high) {
-        float mass = teach.p;
-        if (!s_twice || column_mass(s_at, s_p, t, a.K, mass))
-            g[teach.at] = round_out<T>(teach.old + (expf(teach.z - m) / s - mass) * coef);
-    }
-    if (part == 0) {
-        if (t == 0) {
-            float loss = 0.f;
-            if (done)
-                for (int w = 0; w * 32 < a.K; ++w) loss += s_loss[w];
-            a.row_loss[r] = loss;
+    if (teaches && g && done)
+        for (int k = lane; k < a.K; k += 32) {
+            const int at = s_at[k];
+            float mass = s_p[k];
+            if (at < 0 || (at >> 30) || at < v.low || at >= v.high) continue;
+            if (!s_twice || column_mass(s_at, s_p, k, a.K, mass))
+                g[at] = round_out<T>(s_old[k] + (expf(s_z[k] - m) / s - mass) * coef);
         }
-        if (a.ticket) finish_loss(a, gridDim.x / parts);
-    }
+    if (a.ticket && part == 0) finish_loss(a, gridDim.x / parts);
 }
 
 // the rows' losses added up by a launch of its own, where a block should not wait for its stores to count itself
@@ -946,9 +965,9 @@ template <class T, bool FAST>
 cudaError_t distill_rows(const DistillArgs &a, cudaStream_t st) {
     const int packs = (int)(((long long)a.y.cols * sizeof(T) + 15) / 16), parts = shares(a.y.rows, packs, 512);
     // few blocks have more threads each
-    return packs / parts <= 256 * kHeld && (a.y.rows * parts >= 152 || packs / parts <= 512)
-               ? launch_shared<k_distill<T, 256, FAST>, 256>(a.y.rows, parts, st, a, parts)
-               : launch_shared<k_distill<T, 512, FAST>, 512>(a.y.rows, parts, st, a, parts);
+    return packs / parts <= 224 * kRowHeld && (a.y.rows * parts >= 152 || packs / parts <= 512)
+               ? launch_shared<k_distill<T, 256, FAST>, 256, 224 * kRowHeld>(a.y.rows, parts, st, a, parts)
+               : launch_shared<k_distill<T, 512, FAST>, 512, 480 * kRowHeld>(a.y.rows, parts, st, a, parts);
 }
 
 template <class T>
