@@ -588,17 +588,15 @@ __device__ __forceinline__ void join_lanes(float &m, float &s) {
     for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
 }
 
+// Counts a row (or a block's rows) whose losses this thread has written; true for the last one.
+__device__ __forceinline__ bool last_counted(const DistillArgs &a, unsigned all) {
+    __threadfence();
+    return atomicAdd(reinterpret_cast<unsigned *>(a.loss + 1), 1u) == all - 1;
+}
+
 // the last block adds the rows' losses up, in a fixed order
-__device__ __forceinline__ void finish_loss(const DistillArgs &a, unsigned blocks) {
+__device__ __forceinline__ void add_losses(const DistillArgs &a) {
     __shared__ float s_total[32];
-    __shared__ unsigned s_last;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        __threadfence();
-        s_last = atomicAdd(reinterpret_cast<unsigned *>(a.loss + 1), 1u) == blocks - 1;
-    }
-    __syncthreads();
-    if (!s_last) return;
     __threadfence();
     // each thread's sum with what its additions lost (64-bit additions took most of a readout's time)
     float sum = 0.f, lost = 0.f;
@@ -741,7 +739,11 @@ __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
             }
         }
     }
-    if (a.ticket) finish_loss(a, gridDim.x);
+    __shared__ int s_last;
+    __syncthreads();
+    if (threadIdx.x == 0) s_last = last_counted(a, gridDim.x);
+    __syncthreads();
+    if (s_last) add_losses(a);
 }
 
 constexpr int kRowHeld = 9;
@@ -754,7 +756,7 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const Disti
     constexpr int P = Pack<T>::P, ROW = THREADS - 32, WARPS = ROW / 32, SLOTS = 2 * kTopMax;
     __shared__ float2 s_stat[WARPS], s_share[8];
     __shared__ float s_p[kTopMax], s_log[kTopMax], s_z[kTopMax], s_old[kTopMax];
-    __shared__ int s_any, s_twice, s_at[kTopMax], s_slot[SLOTS];
+    __shared__ int s_any, s_twice, s_last, s_at[kTopMax], s_slot[SLOTS];
     extern __shared__ uint4 s_held[];
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31, part = parts > 1 ? (int)cluster_ctarank() : 0;
     const long long r = blockIdx.x / parts;
@@ -940,7 +942,11 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const Disti
                 if (s_p[k] != 0.f) loss += s_p[k] * (s_log[k] - (s_z[k] - m - log_sum));
 #pragma unroll
         for (int d = 16; d; d >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, d);
-        if (lane == 0) a.row_loss[r] = loss;
+        // counted here, where this warp has written nothing else that the fence would wait for
+        if (lane == 0) {
+            a.row_loss[r] = loss;
+            s_last = last_counted(a, (unsigned)a.y.rows);
+        }
     }
     __syncthreads();
     if (teaches && g && done)
@@ -951,16 +957,9 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const Disti
             if (!s_twice || column_mass(s_at, s_p, k, a.K, mass))
                 g[at] = round_out<T>(s_old[k] + (expf(s_z[k] - m) / s - mass) * coef);
         }
-    if (a.ticket && part == 0) finish_loss(a, gridDim.x / parts);
+    if (part == 0 && s_last) add_losses(a);
 }
 
-// the rows' losses added up by a launch of its own, where a block should not wait for its stores to count itself
-__global__ void __launch_bounds__(1024) k_distill_sum(const DistillArgs a) {
-    wait_launch_before();
-    finish_loss(a, 1);
-}
-
-// the rows' losses: by the last block where a block to each few rows fits the GPU at once, else by a launch of its own
 template <class T, bool FAST>
 cudaError_t distill_rows(const DistillArgs &a, cudaStream_t st) {
     const int packs = (int)(((long long)a.y.cols * sizeof(T) + 15) / 16), parts = shares(a.y.rows, packs, 512);
@@ -971,28 +970,18 @@ cudaError_t distill_rows(const DistillArgs &a, cudaStream_t st) {
 }
 
 template <class T>
-cudaError_t distill(DistillArgs a, int &launches, cudaStream_t st) {
+cudaError_t distill(const DistillArgs &a, cudaStream_t st) {
     const bool small = a.y.cols <= 1024 && a.K <= 64;
     const unsigned blocks = ((unsigned)a.y.rows + 7) / 8;
-    a.ticket = a.y.rows <= (small ? 8 * 304 : 304);
-    cudaError_t e;
-    if (small && a.y.cols <= 64) {
-        k_distill_small<T, 2><<<blocks, 256, 0, st>>>(a);
-        e = cudaGetLastError();
-    } else if (small && a.y.cols <= 256) {
-        k_distill_small<T, 8><<<blocks, 256, 0, st>>>(a);
-        e = cudaGetLastError();
-    } else if (small) {
-        k_distill_small<T, 32><<<blocks, 256, 0, st>>>(a);
-        e = cudaGetLastError();
-    } else if (sizeof(T) == 2 && a.y.factor * a.y.silent == -INFINITY && fabsf(a.y.factor) < 1e30f) {
-        e = distill_rows<T, sizeof(T) == 2>(a, st);
-    } else {
-        e = distill_rows<T, false>(a, st);
+    if (small) {
+        if (a.y.cols <= 64) k_distill_small<T, 2><<<blocks, 256, 0, st>>>(a);
+        else if (a.y.cols <= 256) k_distill_small<T, 8><<<blocks, 256, 0, st>>>(a);
+        else k_distill_small<T, 32><<<blocks, 256, 0, st>>>(a);
+        return cudaGetLastError();
     }
-    if (e != cudaSuccess || a.ticket) return e;
-    launches = 2;
-    return launch_dependent(k_distill_sum, 1, 1024, st, a);
+    if (sizeof(T) == 2 && a.y.factor * a.y.silent == -INFINITY && fabsf(a.y.factor) < 1e30f)
+        return distill_rows<T, sizeof(T) == 2>(a, st);
+    return distill_rows<T, false>(a, st);
 }
 
 }  // namespace
@@ -1003,11 +992,10 @@ cudaError_t launch_top_logits(const LogitArgs &a, int K, float *top, int32_t *in
     return top_logits<__half>(a, K, top, index, st);
 }
 
-cudaError_t launch_distill(const DistillArgs &a, int &launches, cudaStream_t st) {
-    launches = 1;
-    if (a.y.type == DSTD_TYPE_F32) return distill<float>(a, launches, st);
-    if (a.y.type == DSTD_TYPE_BF16) return distill<__nv_bfloat16>(a, launches, st);
-    return distill<__half>(a, launches, st);
+cudaError_t launch_distill(const DistillArgs &a, cudaStream_t st) {
+    if (a.y.type == DSTD_TYPE_F32) return distill<float>(a, st);
+    if (a.y.type == DSTD_TYPE_BF16) return distill<__nv_bfloat16>(a, st);
+    return distill<__half>(a, st);
 }
 
 }  // namespace dstd

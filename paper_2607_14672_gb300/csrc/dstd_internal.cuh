@@ -822,8 +822,7 @@ struct DistillArgs {
     void *g;                  // or null
     long long ld_g;
     bool accumulate;
-    bool ticket;              // the last block of the rows' launch adds their losses up (set by the launch)
 };
-cudaError_t launch_distill(const DistillArgs &a, int &launches, cudaStream_t st);  // launches out
+cudaError_t launch_distill(const DistillArgs &a, cudaStream_t st);
 
 }  // namespace dstd
