@@ -552,22 +552,18 @@ def mx4_scale_bytes(rows, cols):
     return (rows + 127) // 128 * ((cols + 127) // 128) * 512
 
 
-def _codes4(q, name, R, row, dev):
-    """Address of R rows of 4-bit codes, `row` bytes each, and their stride; rows start at multiples of 16 bytes."""
-    if q.shape == (R, row) and q.dtype == _TORCH.uint8 and q.get_device() == dev:
-        ld, one = q.stride()
-        at = q.data_ptr()
-        if one == 1 and ld >= row and not (at | ld) & 15:
-            return at, ld
+def _not_codes4(q, name, R, row, dev):
+    """Says what is wrong with rows of codes, or gives the stride of ones without an address (no rows, or none to a row)."""
     ld = _rows(q, name, R, row, dev, _TORCH.uint8)
     if q.numel() and (q.data_ptr() % 16 or ld % 16):
         raise ValueError(f"{name}: rows of codes must start at multiples of 16 bytes")
-    return q.data_ptr(), ld
+    return ld
 
 
 def _scales4(s, name, R, cols, dev):
+    """Address of the scales of R rows of `cols` columns."""
     need = (R + 127) // 128 * ((cols + 127) // 128) * 512
-    if s.dtype != _TORCH.uint8 or s.get_device() != dev or not s.is_contiguous() or s.numel() < need:
+    if s.dtype is not _TORCH.uint8 or s.get_device() != dev or s.numel() < need or not s.is_contiguous():
         raise ValueError(f"{name} must be a contiguous uint8 tensor of at least {need} on cuda:{dev}")
     return s.data_ptr()
 
@@ -578,13 +574,19 @@ def quantize_mx4(x, q, scale, values=None, stream=None):
     block of 32 columns in scale [mx4_scale_bytes(R, K)] uint8: the least with
     no code beyond 6. ``values`` [R, K] float32 receives what the codes stand
     for. A block that is not finite gets scale NaN. Rows may be padded."""
-    _torch()
+    if _TORCH is None:
+        _torch()
     R, K = x.shape
     dev = x.get_device()
     if dev != _ONLY:
         _here(x, dev, "x")
-    ld_x = _rows(x, "x", R, K, dev)
-    q_at, ld_q = _codes4(q, "q", R, (K + 31) // 32 * 16, dev)
+    ld_x, one = x.stride()
+    if (one != 1 and K > 1) or ld_x < K:
+        ld_x = _rows(x, "x", R, K, dev)
+    ld_q, one = q.stride()
+    q_at, row = q.data_ptr(), (K + 31) // 32 * 16
+    if q.shape != (R, row) or q.dtype is not _TORCH.uint8 or q.get_device() != dev or one != 1 or ld_q < row or (q_at | ld_q) & 15:
+        ld_q = _not_codes4(q, "q", R, row, dev)
     ld_v, v = 0, None
     if values is not None:
         ld_v, v = _rows(values, "values", R, K, dev, _TORCH.float32), values.data_ptr()
@@ -598,17 +600,21 @@ def mx4_matmul(x, x_scale, w, w_scale, out, stream=None):
     """out [T, N] = x @ w^T of 4-bit rows x [T, bytes] and w [N, bytes] with their
     scales, as from quantize_mx4; sums in float32. out is float32, bfloat16 or
     float16; rows may be padded."""
-    _torch()
+    if _TORCH is None:
+        _torch()
     T, row = x.shape
-    N = w.shape[0]
+    N, row_w = w.shape
     dev = x.get_device()
     if dev != _ONLY:
         _here(x, dev, "x")
-    if row % 16 or row > 1 << 30:
+    if row & 15 or row > 1 << 30:
         raise ValueError("mx4_matmul: a row of codes is 16 bytes for each block of 32 columns")
-    K = 2 * row
-    x_at, ld_x = _codes4(x, "x", T, row, dev)
-    w_at, ld_w = _codes4(w, "w", N, row, dev)
+    K, u8 = 2 * row, _TORCH.uint8
+    x_at, (ld_x, one), w_at, (ld_w, one_w) = x.data_ptr(), x.stride(), w.data_ptr(), w.stride()
+    if x.dtype is not u8 or one != 1 or ld_x < row or (x_at | ld_x) & 15:
+        ld_x = _not_codes4(x, "x", T, row, dev)
+    if row_w != row or w.dtype is not u8 or w.get_device() != dev or one_w != 1 or ld_w < row or (w_at | ld_w) & 15:
+        ld_w = _not_codes4(w, "w", N, row, dev)
     ld_out = _rows(out, "out", T, N, dev)
     code = load().dstd_mx4_matmul(x_at, ld_x, _scales4(x_scale, "x_scale", T, K, dev), w_at, ld_w,
                                   _scales4(w_scale, "w_scale", N, K, dev), T, N, K, out.data_ptr(),
@@ -648,9 +654,9 @@ def dense_fwd_mx4(t_in, w_q, w_scale, p, t_out, saved, penalty, workspace, strea
 # -- learning from a teacher -------------------------------------------------
 def _record(top, index, R, K, dev):
     """A teacher's record: contiguous float32 logits and int32 classes [R, K]."""
-    if top.shape != (R, K) or top.dtype != _TORCH.float32 or top.get_device() != dev or not top.is_contiguous():
+    if top.shape != (R, K) or top.dtype is not _TORCH.float32 or top.get_device() != dev or not top.is_contiguous():
         raise ValueError(f"top must be a contiguous float32 tensor {(R, K)} on cuda:{dev}")
-    if index.shape != (R, K) or index.dtype != _TORCH.int32 or index.get_device() != dev or not index.is_contiguous():
+    if index.shape != (R, K) or index.dtype is not _TORCH.int32 or index.get_device() != dev or not index.is_contiguous():
         raise ValueError(f"index must be a contiguous int32 tensor {(R, K)} on cuda:{dev}")
 
 
@@ -667,7 +673,8 @@ def top_logits(y, top, index, factor=1.0, silent=None, stream=None):
     [R, K] float32 and index [R, K] int32: what is kept of a teacher. Spike times
     have factor -1/tau_soft and, for silent outputs, ``silent`` = t_end; without
     it those (and masked classes) come last, with -inf. Rows may be padded."""
-    _torch()
+    if _TORCH is None:
+        _torch()
     R, C = y.shape
     dev = y.get_device()
     if dev != _ONLY:
@@ -690,7 +697,8 @@ def distill_loss(y, top, index, loss, row_loss, g=None, factor=1.0, silent=None,
     mean (or their sum with row_weight [R]), g [R, C] of y's type (may be None;
     accumulate: added to what it holds). loss: float32[2], zeros at first.
     factor and silent as in top_logits; silent outputs pass no gradient."""
-    _torch()
+    if _TORCH is None:
+        _torch()
     R, C = y.shape
     dev = y.get_device()
     if dev != _ONLY:
