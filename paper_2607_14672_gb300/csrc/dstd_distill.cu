@@ -149,9 +149,14 @@ struct HeldRow {
     template <class F>
     __device__ __forceinline__ void each(const RowView<T> &v, F f) const {
         const int k0 = v.first + (int)threadIdx.x, left = v.last - k0;
+        if (left > (HELD - 2) * THREADS) {
 #pragma unroll
-        for (int j = 0; j < HELD; ++j)
-            if (j * THREADS < left) f(slot[j * THREADS], k0 + j * THREADS);
+            for (int j = 0; j < HELD - 1; ++j) f(slot[j * THREADS], k0 + j * THREADS);
+            if (left > (HELD - 1) * THREADS) f(slot[(HELD - 1) * THREADS], k0 + (HELD - 1) * THREADS);
+        } else {
+#pragma unroll 1
+            for (int j = 0; j * THREADS < left; ++j) f(slot[j * THREADS], k0 + j * THREADS);
+        }
         for (int k = k0 + HELD * THREADS; k < v.last; k += THREADS) f(v.pack(k), k);
     }
 };
@@ -197,26 +202,33 @@ __device__ __forceinline__ uint64_t ld_cluster64(uint32_t addr) {
     return v;
 }
 
-// Largest logit of a pack. PAIRS (16-bit outputs, none of whose logits is a stand-in): the order of
-// the logits is that of the outputs, or of the negated ones (flip), and two are compared at once.
-// Without WITH_NAN a NaN is passed over, unless there is nothing else.
+// Largest logits of packs. PAIRS (16-bit outputs, none of whose logits is a stand-in): the order of the logits is that
+// of the outputs, or of the negated ones (flip), and two are compared at once. Without WITH_NAN a NaN is passed
+// over, unless there is nothing else.
 template <class T, bool PAIRS, bool WITH_NAN>
 struct PackMax {
     Logit logit;
     uint32_t flip;
     __device__ __forceinline__ explicit PackMax(const Logit &l) : logit(l), flip(l.factor < 0.f ? 0x80008000u : 0u) {}
+    static __device__ __forceinline__ uint32_t two(uint32_t a, uint32_t b) {
+        using V = typename Two<T>::type;
+        const V x = *reinterpret_cast<const V *>(&a), y = *reinterpret_cast<const V *>(&b);
+        const V m = WITH_NAN ? __hmax2_nan(x, y) : __hmax2(x, y);
+        return *reinterpret_cast<const uint32_t *>(&m);
+    }
+    __device__ __forceinline__ uint32_t words(const uint4 &w) const {
+        if (flip) return two(two(w.x ^ flip, w.y ^ flip), two(w.z ^ flip, w.w ^ flip));
+        return two(two(w.x, w.y), two(w.z, w.w));
+    }
+    // of both halves of a word from words()
+    __device__ __forceinline__ float of_words(uint32_t u) const {
+        using V = typename Two<T>::type;
+        const V m = *reinterpret_cast<const V *>(&u);
+        return fabsf(logit.factor) * to_f32<T>(WITH_NAN ? __hmax_nan(m.x, m.y) : __hmax(m.x, m.y));
+    }
     __device__ __forceinline__ float operator()(const uint4 &w) const {
         if constexpr (PAIRS) {
-            using V = typename Two<T>::type;
-            const uint32_t u[4] = {w.x ^ flip, w.y ^ flip, w.z ^ flip, w.w ^ flip};
-            const V *v = reinterpret_cast<const V *>(u);
-            if constexpr (WITH_NAN) {
-                const V m = __hmax2_nan(__hmax2_nan(v[0], v[1]), __hmax2_nan(v[2], v[3]));
-                return fabsf(logit.factor) * to_f32<T>(__hmax_nan(m.x, m.y));
-            } else {
-                const V m = __hmax2(__hmax2(v[0], v[1]), __hmax2(v[2], v[3]));
-                return fabsf(logit.factor) * to_f32<T>(__hmax(m.x, m.y));
-            }
+            return of_words(words(w));
         } else {
             float m = logit.of(Pack<T>::one(w, 0));
 #pragma unroll
@@ -224,6 +236,20 @@ struct PackMax {
                 const float z = logit.of(Pack<T>::one(w, i));
                 m = WITH_NAN ? max_nan(m, z) : fmaxf(m, z);
             }
+            return m;
+        }
+    }
+    // the largest of a thread's packs, -infinity if there are none
+    template <class Row, class View>
+    __device__ __forceinline__ float of_row(const Row &h, const View &v) const {
+        if constexpr (PAIRS) {
+            const T least = round_out<T>(-INFINITY);
+            uint32_t m = (uint32_t)*reinterpret_cast<const unsigned short *>(&least) * 0x10001u;
+            h.each(v, [&](const uint4 &w, int) { m = two(m, words(w)); });
+            return of_words(m);
+        } else {
+            float m = -INFINITY;
+            h.each(v, [&](const uint4 &w, int) { m = WITH_NAN ? max_nan(m, (*this)(w)) : fmaxf(m, (*this)(w)); });
             return m;
         }
     }
@@ -255,15 +281,10 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS)
     const int want = min(K, v.high - v.low);
     h.ready();
     uint32_t mine = 0, bound = 0;  // 0: below every logit's key
-    {
-        float m = -INFINITY;
-        bool some = h.at >= 0;
-        if (some) m = logit.of(h.one);
-        h.each(v, [&](const uint4 &w, int) {
-            m = max_nan(m, pack_max(w));
-            some = true;
-        });
-        if (some) mine = key_of(m);
+    if (h.at >= 0 || v.first + t < v.last) {
+        float m = pack_max.of_row(h, v);
+        if (h.at >= 0) m = max_nan(m, logit.of(h.one));
+        mine = key_of(m);
     }
     // the upper half of the key will do: a bound lower by 2^-7 at most lets few more pass
     for (int bit = 31; bit >= 16; --bit) {
@@ -832,7 +853,7 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const Disti
         h.ready();
         if (h.at >= 0) m = logit.of(h.one);
         const PackMax<T, FAST, false> pack_max(logit);
-        h.each(v, [&](const uint4 &w, int) { m = fmaxf(m, pack_max(w)); });
+        m = fmaxf(m, pack_max.of_row(h, v));
 #pragma unroll
         for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
         base = m == -INFINITY ? 0.f : m;
