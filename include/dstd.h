@@ -534,7 +534,7 @@ int dstd_adamw_clip(int count, float *const *w, const void *const *g, float *con
  *          of dstd_mx4_scale_bytes(rows, cols) bytes, at a multiple of 16. Bytes
  *          of blocks past the last are 0; those of rows past the last may be
  *          anything.
- * No columns, no rows or no tokens are valid.
+ * No columns, no rows or no tokens are valid; at most 2^31 - 2048 of each.
  * ------------------------------------------------------------------------- */
 size_t dstd_mx4_scale_bytes(int rows, int cols); /* 0 for negative sizes */
 
@@ -555,7 +555,7 @@ int dstd_quantize_mx4(const void *x, dstd_type type, int rows, int cols, int64_t
  * lost), rounded once more to a 16-bit out_type. No order of work depends on
  * anything but the sizes: the same call gives the same bits.
  *  x, x_scale  T rows of K columns in the layout above; w, w_scale N rows.
- *  K = 0 gives zeros. T, N, K at most 2^31 - 256.
+ *  K = 0 gives zeros.
  *  out [T, N] of out_type, row stride ld_out >= N (elements); overlaps no input. */
 int dstd_mx4_matmul(const uint8_t *x, int64_t ld_x, const uint8_t *x_scale, const uint8_t *w, int64_t ld_w,
                     const uint8_t *w_scale, int T, int N, int K, void *out, dstd_type out_type, int64_t ld_out,

@@ -1871,7 +1871,7 @@ int dstd_adamw_clip(int count, float *const *w, const void *const *g, float *con
 // ---------------------------------------------------------------------------
 namespace {
 
-constexpr int kMx4Most = 0x7fffffff - 255;  // rows and columns of a product: whole tiles stay below 2^31
+constexpr int kMx4Most = 0x7fffffff - 2047;  // rows and columns: whole tiles and runs stay below 2^31
 
 int row_bytes(int cols) { return 16 * mx4_blocks(cols); }
 

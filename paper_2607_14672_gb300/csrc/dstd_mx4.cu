@@ -315,12 +315,15 @@ cudaError_t launch_mx4_rowsum(const uint8_t *w, long long ld, const uint8_t *sca
 }
 
 // ---------------------------------------------------------------------------
-// Product on the 4-bit tensor cores, D[n, t]: a block computes 128 rows of one
-// side (the channels, as a rule) times NT of the other. TMA brings 256 columns of K a stage,
-// codes as they are, and the scales of both; one thread copies the scales to
-// TMEM and issues the MMAs, in that order; four warps take the sums out.
-// Where there are few tiles, `parts` blocks of a cluster share K: each leaves its sums in its own shared
-// memory, and each adds up its share of the columns over all, in order.
+// Product on the 4-bit tensor cores (tcgen05, kind mxf4: a product of two codes times both powers of two, fp32
+// sums), D[n, t]: a block computes 128 rows of one side (the channels, as a rule: then neighbouring lanes store
+// neighbouring elements) times NT of the other. TMA brings 256 columns of K a stage, codes as they are, and the scales
+// of both sides in the tiles in which they are kept; one thread copies the scales to TMEM and issues the MMAs, in that
+// order; four warps take the sums out. No operand is converted on the way, so few tokens cost what reading the weights
+// costs: 8 x 16384 into 16384 in 26 us, 5.4 TB/s of codes and scales (about 3 us of it before the first byte). Wide
+// tiles take in 54 bytes a cycle and SM from L2, which bounds them. Where there are few tiles, `parts` blocks of a
+// cluster share K: each leaves its sums in its own shared memory, and each adds up its share of the columns over all, in
+// order (no atomics: the same call gives the same bits).
 // ---------------------------------------------------------------------------
 __device__ unsigned int g_status_mx4 = 0;
 
@@ -342,16 +345,15 @@ constexpr int kScaleTile = 512;          // scales of 128 rows by 4 blocks
 template <int NT>
 struct Mx4Cfg {
     static constexpr int B_BYTES = NT * kRowBytes;
-    static constexpr int B_TILES = (NT + 127) / 128;  // of 128 rows of scales
-    static constexpr int SF_BYTES = 2 * kScaleTile * (1 + B_TILES);
+    static constexpr int SF_BYTES = 4 * kScaleTile;  // 2 tiles along K of either side (NT divides 128 or b is one tile)
     static constexpr int STAGE = (kTileBytes + B_BYTES + SF_BYTES + 1023) / 1024 * 1024;
     static constexpr int STAGES = 216 * 1024 / STAGE;                    // a block that has an SM to itself
     static constexpr int HALF = 108 * 1024 / STAGE;                      // two to an SM
     static constexpr int smem(int slots) { return slots * STAGE + 1024 + 256; }
     static constexpr int SF_COL = NT;                    // scales: two sets of (A, B) in turn
-    static constexpr int SF_SET = 2 * 4 * (1 + B_TILES);
+    static constexpr int SF_SET = 16;
     static constexpr int USED = NT + 2 * SF_SET;
-    static constexpr int COLS = USED <= 64 ? 64 : (USED <= 128 ? 128 : (USED <= 256 ? 256 : 512));
+    static constexpr int COLS = USED <= 64 ? 64 : (USED <= 128 ? 128 : 256);
     static_assert(NT * 128 * 4 <= HALF * STAGE, "the sums of a tile fit the stages");
     static_assert(2 * STAGES * 8 + 16 <= 256, "the barriers fit");
 };
@@ -465,21 +467,14 @@ __global__ void __launch_bounds__(192) k_mx4_tc(const __grid_constant__ CUtensor
             if (!ok) break;
             if (elect_one()) {
                 const uint32_t st = smem_u32(smem + slot * C::STAGE), sf = st + kTileBytes + C::B_BYTES;
-                const int k0 = s * 2, kt = min(2, p.ktiles - k0);
-                const uint32_t sf_bytes = (uint32_t)kt * kScaleTile;
-                int b_tiles = 0;
-#pragma unroll
-                for (int i = 0; i < C::B_TILES; ++i) b_tiles += tb * NT + i * 128 < p.b.rows ? 1 : 0;
-                mbar_expect_tx(&full[slot], (uint32_t)(kTileBytes + C::B_BYTES) + sf_bytes * (1 + b_tiles));
+                const int k0 = s * 2;
+                const uint32_t sf_bytes = (uint32_t)min(2, p.ktiles - k0) * kScaleTile;
+                mbar_expect_tx(&full[slot], (uint32_t)(kTileBytes + C::B_BYTES) + 2 * sf_bytes);
                 tma_load_2d(st, &map_a, &full[slot], s * kRowBytes, ta * 128);
                 tma_load_2d(st + kTileBytes, &map_b, &full[slot], s * kRowBytes, tb * NT);
                 bulk_load(sf, p.a.scale + ((long long)ta * p.ktiles + k0) * kScaleTile, sf_bytes, &full[slot]);
-#pragma unroll
-                for (int i = 0; i < C::B_TILES; ++i)
-                    if (i < b_tiles)
-                        bulk_load(sf + (1 + i) * 2 * kScaleTile,
-                                  p.b.scale + (((long long)tb * NT / 128 + i) * p.ktiles + k0) * kScaleTile, sf_bytes,
-                                  &full[slot]);
+                bulk_load(sf + 2 * kScaleTile, p.b.scale + ((long long)tb * p.ktiles + k0) * kScaleTile, sf_bytes,
+                          &full[slot]);
             }
             __syncwarp();
             if (++slot == slots) slot = 0, turn ^= 1u;
@@ -509,16 +504,13 @@ __global__ void __launch_bounds__(192) k_mx4_tc(const __grid_constant__ CUtensor
                 for (int h = 0; h < 2; ++h) {
                     if (h * 4 >= left) break;
                     tmem_cp_scales(sfa + h * 4, sdesc_rows16(sf + h * kScaleTile));
-#pragma unroll
-                    for (int i = 0; i < C::B_TILES; ++i)
-                        tmem_cp_scales(sfb + (h * C::B_TILES + i) * 4,
-                                       sdesc_rows16(sf + (1 + i) * 2 * kScaleTile + h * kScaleTile));
+                    tmem_cp_scales(sfb + h * 4, sdesc_rows16(sf + (2 + h) * kScaleTile));
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const int kk = 2 * h + i;
                         if (kk * 2 >= left) break;
                         mma_mx4(tmem, ad + kk * 2, bd + kk * 2, idesc_mx4(128, NT, 2 * i), sfa + h * 4,
-                                sfb + h * C::B_TILES * 4, s > s0 || kk > 0 ? 1u : 0u);
+                                sfb + h * 4, s > s0 || kk > 0 ? 1u : 0u);
                     }
                 }
                 mma_commit(&empty[slot]);
@@ -534,8 +526,7 @@ __global__ void __launch_bounds__(192) k_mx4_tc(const __grid_constant__ CUtensor
     if (warp < 4) {
         const int row = warp * 32 + lane;
         const long long r = (long long)ta * 128 + row, c0 = (long long)tb * NT;
-        const bool any = s1 > s0;
-        ok = !any || mbar_wait_cycles(done, 0);
+        ok = mbar_wait_cycles(done, 0);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok && lane == 0) mx4_timeout();
         tc_fence_after();
@@ -544,10 +535,7 @@ __global__ void __launch_bounds__(192) k_mx4_tc(const __grid_constant__ CUtensor
 #pragma unroll 1
         for (int c = 0; c < NT && ok; c += CH) {
             float v[CH];
-            if (any) tmem_ld16(t0 + c, v);
-            else
-#pragma unroll
-                for (int i = 0; i < CH; ++i) v[i] = 0.f;
+            tmem_ld16(t0 + c, v);
             if (p.parts > 1) {
                 float *sum = reinterpret_cast<float *>(smem) + c * 128 + row;
 #pragma unroll
@@ -610,8 +598,11 @@ __global__ void __launch_bounds__(192) k_mx4_tc(const __grid_constant__ CUtensor
 }
 
 // Large products: a pair of SMs computes 256 x 256, each SM its 128 rows of a and half of b's codes,
-// so that a stage brings 35 KB to an SM for 512 cycles of MMAs. The pairs stay and take tiles in turn; eight
-// warps take the sums out to registers, from where they are stored while the next tile is computed.
+// so that a stage brings 35 KB to an SM for 512 cycles of MMAs (a block of its own, 128 x 128: 34 KB for 128). The
+// scales of b's 256 rows go to both. The pairs stay and take tiles in turn; eight warps take the sums out to
+// registers, from where they are stored while the next tile is computed: two accumulators of this width and the
+// scales do not fit TMEM. The tensor pipe bounds it: 4096 x 16384 into 16384 in 276 us, 8.0 PFLOP/s; 128 x 128
+// tiles took 440. With few columns the stores do: 8192 x 32 into 8192 fp32 in 49 us, 5.5 TB/s.
 struct PairCfg {
     static constexpr int SF_BYTES = 2 * kScaleTile * 3;  // of this SM's rows of a, of all of b's
     static constexpr int STAGE = (2 * kTileBytes + SF_BYTES + 1023) / 1024 * 1024;
@@ -895,7 +886,9 @@ cudaError_t launch_mx4_tc(const Mx4Args &a, const Mx4Plan &plan, cudaStream_t st
     return cudaLaunchKernelEx(&cfg, k_mx4_tc<NT, O>, map_a, map_b, p);
 }
 
-// One orientation's plan: fewer padded rows, or neighbouring lanes that store neighbouring elements
+// Which side is a: the one whose neighbouring rows are neighbours in out, unless the other way halves the padded
+// tiles (5325 x 285 into 123 fp32: 5.6 us, the other way 11). Pairs from 48 tiles of 256 x 256 on (2048 x 8192 into
+// 2048, 64 tiles: 17 us, in blocks of 128 x 128 21; 500 x 12000 into 3000, 24 tiles: 24 and 21).
 Mx4Plan mx4_plan(const Mx4Args &q) {
     const auto width = [](int b) { return b <= 16 ? 16 : (b <= 32 ? 32 : (b <= 64 ? 64 : 128)); };
     const auto area = [&](int a, int b) {

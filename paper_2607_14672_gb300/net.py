@@ -79,8 +79,11 @@ class Taught:
     def learn_from(self, K, weight=1.0, teacher_factor=1.0, labels=True):
         """From now on the loss has weight times the distillation loss from
         records of K entries (``set_teacher``), whose softmax is taken with
-        teacher_factor; beside the cross-entropy of the labels, or instead."""
+        teacher_factor; beside the cross-entropy of the labels, or instead.
+        Call it before a step is captured: it makes the record's buffers."""
         self.logit_factor()
+        if not 1 <= K <= 256:
+            raise ValueError(f"learn_from: records have 1 to 256 entries, not {K}")
         self.record = (torch.zeros(self.B, K, dtype=torch.float32, device=self.device),
                        torch.full((self.B, K), -1, dtype=torch.int32, device=self.device))
         self.taught_loss = torch.zeros(2, dtype=torch.float32, device=self.device)  # value, the kernel's scratch
@@ -93,8 +96,10 @@ class Taught:
         """The teacher's record for the present batch (rows of classes -1: no teacher)."""
         if self.record is None:
             raise RuntimeError("set_teacher: call learn_from first")
-        self.record[0].copy_(torch.as_tensor(top), non_blocking=True)
-        self.record[1].copy_(torch.as_tensor(index), non_blocking=True)
+        for mine, given in zip(self.record, (torch.as_tensor(top), torch.as_tensor(index))):
+            if given.shape != mine.shape:
+                raise ValueError(f"set_teacher: logits and classes {tuple(mine.shape)}, not {tuple(given.shape)}")
+            mine.copy_(given, non_blocking=True)
 
     def has_label_loss(self):
         return self.record is None or self.from_labels

@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+from mx4_plans import PLANS
 from oracle import mx4
 from paper_2607_14672_gb300 import dstd
 
@@ -67,6 +68,36 @@ def test_quantize(type, R, K, pad, offset):
     mine = torch.zeros_like(vflat, dtype=torch.bool)
     mine[offset:offset + R * (K + pad)].view(R, K + pad)[:, :K] = True
     assert (vflat[~mine] == 7).all()
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("R,K,pad,offset", [(20000, 130, 0, 0), (20000, 260, 4, 4), (40000, 500, 12, 0), (40000, 1000, 1, 3),
+                                            (12000, 1024, 0, 0), (9000, 5000, 0, 1), (80000, 250, 6, 2)])
+def test_many_rows(type, R, K, pad, offset):
+    """Many rows take several runs of a row to a warp: the same bytes as in slices of few, which take one."""
+    gen = torch.Generator(device="cuda").manual_seed(K)
+    _, x = padded(R, K, pad, TYPES[type], offset)
+    x.copy_(torch.randn(R, K, generator=gen, device="cuda") * torch.exp2(torch.randn(R, K, generator=gen, device="cuda") * 4))
+    x[5, K // 2], x[R - 1, K - 1] = float("inf"), float("nan")
+    q, scale, v = quantized(x, True)
+    plain, scale2, _ = quantized(x)
+    assert torch.equal(q, plain)
+    n = mx4.blocks_of(K)
+    for i in [0, 128 * 7, (R - 1) // 128 * 128]:
+        few = x[i:i + 128]
+        q1, s1, v1 = quantized(few, True)
+        assert torch.equal(q[i:i + 128], q1) and torch.equal(v[i:i + 128].nan_to_num(7.0), v1.nan_to_num(7.0))
+        r, b = np.arange(few.shape[0])[:, None], np.arange(-(-n // 4) * 4)[None, :]
+        mine, all = mx4.scale_place(r, b, K), mx4.scale_place(r + i, b, K)
+        for s in (scale, scale2):
+            assert (s.cpu().numpy()[all] == s1.cpu().numpy()[mine]).all()
+    # every row: the widest step, from 4 to 6, is off by at most 1, and 2^e is at most a third of the largest
+    fine = torch.isfinite(v)
+    wide = torch.nn.functional.pad(torch.isfinite(x), (0, -K % 32), value=True).view(R, n, 32)
+    assert torch.equal(fine, wide.all(2).repeat_interleave(32, 1)[:, :K]) and not fine.all()
+    d = (v.double() - x.double()).abs()[fine]
+    top = torch.nn.functional.pad(x.double(), (0, -K % 32)).view(R, n, 32).abs().amax(2).repeat_interleave(32, 1)[:, :K]
+    assert (d <= (top / 3)[fine]).all()
 
 
 def test_quantize_edges():
@@ -147,6 +178,13 @@ def test_product_types_and_padded_rows(T, N, K, out):
                                    (3000, 9, 700), (1024, 1024, 16384)])
 def test_product_large(T, N, K):
     product(T, N, K)
+
+
+@pytest.mark.parametrize("T,N,K,width,parts,exchanged", PLANS)
+def test_product_plans(T, N, K, width, parts, exchanged):
+    """Every form of the product (mx4_plans.py), fp32 and bf16."""
+    product(T, N, K)
+    product(T, N, K, "bf16", pad=1)
 
 
 @pytest.mark.parametrize("out", ["f32", "bf16"])

@@ -49,7 +49,7 @@ def test_quantize_refuses(lib, bad):
 
 
 def test_quantize_sizes(lib):
-    big = dict(rows=1, cols=TOP, ld_x=TOP, ld_q=2 ** 31, ld_v=TOP)
+    big = dict(rows=1, cols=TOP - 2047 + 1, ld_x=TOP, ld_q=2 ** 31, ld_v=TOP)
     assert lib.dstd_quantize_mx4(*dict(QUANT, **big).values(), None) == UNSUPPORTED
 
 
@@ -63,7 +63,7 @@ def test_matmul_refuses(lib, bad):
     assert lib.dstd_mx4_matmul(*dict(MATMUL, **bad).values(), None) == INVALID
 
 
-@pytest.mark.parametrize("big", [dict(T=TOP), dict(N=TOP, ld_out=TOP), dict(K=TOP, ld_x=2 ** 31, ld_w=2 ** 31)])
+@pytest.mark.parametrize("big", [dict(T=TOP - 2046), dict(N=TOP - 2046, ld_out=TOP), dict(K=TOP - 2046, ld_x=2 ** 31, ld_w=2 ** 31)])
 def test_matmul_sizes(lib, big):
     assert lib.dstd_mx4_matmul(*dict(MATMUL, **big).values(), None) == UNSUPPORTED
 

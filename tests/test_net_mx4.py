@@ -59,6 +59,14 @@ def test_teacher_is_refused_where_there_are_no_logits():
     with pytest.raises(ValueError):
         n.answers(torch.zeros(2, 3), torch.zeros(2, 3, dtype=torch.int32))
     assert n.record is None
+    n = network(mode="x3")
+    for K in (0, 257):
+        with pytest.raises(ValueError):
+            n.learn_from(K)
+    n.learn_from(3)
+    for top, index in ((torch.zeros(2, 2), torch.zeros(2, 3)), (torch.zeros(2, 3), torch.zeros(3)), (torch.zeros(3), torch.zeros(2, 3))):
+        with pytest.raises(ValueError):
+            n.set_teacher(top, index)
 
 
 @pytest.mark.parametrize("mode", ["mx4", "x3"])
