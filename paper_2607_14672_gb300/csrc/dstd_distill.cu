@@ -523,7 +523,7 @@ cudaError_t top_logits(const LogitArgs &a, int K, float *top, int32_t *index, cu
 // and q = softmax of its logits:
 //     L_r = sum_k p_k (log p_k - log q_{i_k}),
 //     dL_r / dy_c = factor (q_c - sum_{k: i_k = c} p_k)   (0 where silent).
-// A row is read once and stays in registers: the largest logit and the sum of
+// A row is read once and stays on chip: the largest logit and the sum of
 // exp(z - largest), by warps, then over the block (or the cluster that shares the row), then exp(z - m)
 // times a constant. The few columns that the teacher names are written once
 // more, from fp32, so that every gradient is rounded once; entries of the
@@ -665,101 +665,129 @@ __device__ __forceinline__ bool named_before(int *slot, int at) {
     }
 }
 
-// Rows of up to 32 E classes and 64 entries: a warp to a row, E columns a lane.
-template <class T>
-__device__ __forceinline__ float exp_for(float x) {
-    if constexpr (sizeof(T) == 4) return expf(x);
-    else return __expf(x);  // off by 2^-21 or so, far below a 16-bit rounding
-}
-
-template <class T, int E>
-__global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
-    constexpr int SLOTS = 256;
-    __shared__ int s_at[8][64], s_slot[8][SLOTS];
-    __shared__ float s_p[8][64];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long r = (long long)blockIdx.x * 8 + warp;
-    if (r < a.y.rows) {
-        const Logit logit(a.y);
-        const T *row = static_cast<const T *>(a.y.y) + r * a.y.ld;
-        T *g = a.g ? static_cast<T *>(a.g) + r * a.ld_g : nullptr;
-        const Record<2> record(a, r, lane);
-        const float rw = a.row_weight ? a.row_weight[r] : 1.f / (float)a.y.rows;
-        float z[E];
-        uint32_t silent = 0;
+// exp(z - m) of outputs, m the largest logit (nothing but -infinity: every exp is 0 with any finite m, and NaN stays
+// NaN). FAST: 16-bit outputs without a stand-in for silent ones, whose exp is 0 by itself:
+// exp(z - m) = 2^(factor log2(e) y - m log2(e)), one multiply-add and the special-function unit, two at a time
+// (the product's rounding moves it by 2^-24 |z|, far below a 16-bit rounding).
+template <class T, bool FAST>
+struct ExpOf {
+    static constexpr int P = Pack<T>::P;
+    Logit logit;
+    float base, scale;
+    __device__ __forceinline__ ExpOf(const Logit &l, float m)
+        : logit(l), base(m == -INFINITY ? 0.f : m), scale(l.factor * kLog2e) {}
+    __device__ __forceinline__ float one(float y) const {
+        if constexpr (FAST) return exp2_fast(fmaf(y, scale, -base * kLog2e));
+        else return expf(logit.of(y) - base);
+    }
+    __device__ __forceinline__ uint64_t two(uint32_t w) const {
+        const float2 x = of_pair(fma_pair(word_pair<T>(w), pair_of(scale, scale), pair_of(-base * kLog2e, -base * kLog2e)));
+        return pair_of(exp2_fast(x.x), exp2_fast(x.y));
+    }
+    __device__ __forceinline__ float sum(const uint4 &w) const {
+        if constexpr (FAST) {
+            const float2 f = of_pair(add_pair(add_pair(two(w.x), two(w.y)), add_pair(two(w.z), two(w.w))));
+            return f.x + f.y;
+        } else {
+            float s = 0.f;
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const int c = lane + 32 * i;
-            bool none = true;
-            z[i] = c < a.y.cols ? logit.of(to_f32<T>(row[c]), none) : -INFINITY;
-            silent |= (none ? 1u : 0u) << i;
+            for (int i = 0; i < P; ++i) s += one(Pack<T>::one(w, i));
+            return s;
         }
+    }
+    // over exp(z - m), 0 where silent
+    __device__ __forceinline__ float grad(float y, float over) const {
+        if constexpr (FAST) return one(y) * over;
+        bool silent;
+        const float z = logit.of(y, silent);
+        return silent ? 0.f : expf(z - base) * over;
+    }
+    __device__ __forceinline__ void grads(const uint4 &w, float over, T (&out)[P]) const {
+        if constexpr (FAST) {
+            const uint64_t c = pair_of(over, over);
+            *reinterpret_cast<uint4 *>(out) =
+                make_uint4(pair_word<T>(mul_pair(two(w.x), c)), pair_word<T>(mul_pair(two(w.y), c)),
+                           pair_word<T>(mul_pair(two(w.z), c)), pair_word<T>(mul_pair(two(w.w), c)));
+        } else {
 #pragma unroll
-        for (int i = 0; i < SLOTS / 32; ++i) s_slot[warp][lane + 32 * i] = -1;
-        const bool any = record.any();
-        Teacher entry[2];
-        {
-            float y[2], old[2], tm, tl;
+            for (int i = 0; i < P; ++i) out[i] = round_out<T>(grad(Pack<T>::one(w, i), over));
+        }
+    }
+};
+
+// What a warp that has a row to itself knows of the teacher: 64 entries, two a lane.
+constexpr int kWarpEntries = 64, kWarpSlots = 256;
+struct WarpShared {
+    int at[kWarpEntries], slot[kWarpSlots];
+    float p[kWarpEntries];
+};
+struct WarpTeacher {
+    Teacher entry[2];
+    bool any, twice;
+    template <class T>
+    __device__ __forceinline__ void read(const DistillArgs &a, const Logit &logit, const T *row, const T *g, long long r,
+                                         int lane, WarpShared &s) {
+        const Record<2> record(a, r, lane);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                y[e] = record.at[e] >= 0 ? to_f32<T>(row[record.at[e]]) : 0.f;
-                old[e] = record.at[e] >= 0 && a.accumulate && g ? to_f32<T>(g[record.at[e]]) : 0.f;
-            }
-            record.softmax(tm, tl);
+        for (int i = 0; i < kWarpSlots / 32; ++i) s.slot[lane + 32 * i] = -1;
+        any = record.any();
+        float y[2], old[2], m, log_sum;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                entry[e] = record.entry(e, tm, tl, logit, y[e], old[e]);
-                s_at[warp][32 * e + lane] = entry[e].at;
-                s_p[warp][32 * e + lane] = entry[e].p;
-            }
+        for (int e = 0; e < 2; ++e) {
+            y[e] = record.at[e] >= 0 ? to_f32<T>(row[record.at[e]]) : 0.f;
+            old[e] = record.at[e] >= 0 && a.accumulate && g ? to_f32<T>(g[record.at[e]]) : 0.f;
+        }
+        record.softmax(m, log_sum);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            entry[e] = record.entry(e, m, log_sum, logit, y[e], old[e]);
+            s.at[32 * e + lane] = entry[e].at;
+            s.p[32 * e + lane] = entry[e].p;
         }
         __syncwarp();
         bool again = false;
 #pragma unroll
         for (int e = 0; e < 2; ++e)
-            if (entry[e].at >= 0 && named_before<SLOTS>(s_slot[warp], entry[e].at)) again = true;
-        const bool twice = __any_sync(0xffffffffu, again);
-        float m = -INFINITY, s = 0.f;
+            if (entry[e].at >= 0 && named_before<kWarpSlots>(s.slot, entry[e].at)) again = true;
+        twice = __any_sync(0xffffffffu, again);
+    }
+    // the row's loss, in every lane
+    __device__ __forceinline__ float loss(float m, float sum, bool done) const {
+        const float log_sum = logf(sum);
+        float l = done ? teacher_loss(entry[0], m, log_sum) + teacher_loss(entry[1], m, log_sum) : 0.f;
 #pragma unroll
-        for (int i = 0; i < E; ++i) m = fmaxf(m, z[i]);
+        for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+        return l;
+    }
+    // the named columns' gradients, once all others have been written
+    template <class T>
+    __device__ __forceinline__ void write(const DistillArgs &a, T *g, float m, float sum, float coef, int lane,
+                                          const WarpShared &s) const {
 #pragma unroll
-        for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-#pragma unroll
-        for (int i = 0; i < E; ++i) s += z[i] == -INFINITY ? 0.f : exp_for<T>(z[i] - m);
-#pragma unroll
-        for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-        // a row without logits has no softmax: it is left out (a NaN counts as a logit)
-        const bool done = any && rw != 0.f && !(m == -INFINITY && !(s != s));
-        float loss = 0.f;
-        if (done) {
-            const float log_sum = logf(s);
-            loss = teacher_loss(entry[0], m, log_sum) + teacher_loss(entry[1], m, log_sum);
-        }
-#pragma unroll
-        for (int d = 16; d; d >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, d);
-        if (lane == 0) a.row_loss[r] = loss;
-        if (g && (done || !a.accumulate)) {
-            const float coef = a.weight * rw * logit.factor, over = coef / s;
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const int c = lane + 32 * i;
-                if (c >= a.y.cols) continue;
-                const float d = ((silent >> i) & 1u) || !done ? 0.f : exp_for<T>(z[i] - m) * over;
-                g[c] = round_out<T>(a.accumulate ? to_f32<T>(g[c]) + d : d);
-            }
-            __syncwarp();
-            if (done) {
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const Teacher &t = entry[e];
-                    float mass = t.p;
-                    if (t.at >= 0 && !t.silent &&
-                        (!twice || column_mass(s_at[warp], s_p[warp], 32 * e + lane, a.K, mass)))
-                        g[t.at] = round_out<T>(t.old + (expf(t.z - m) / s - mass) * coef);
-                }
-            }
+        for (int e = 0; e < 2; ++e) {
+            const Teacher &t = entry[e];
+            float mass = t.p;
+            if (t.at >= 0 && !t.silent && (!twice || column_mass(s.at, s.p, 32 * e + lane, a.K, mass)))
+                g[t.at] = round_out<T>(t.old + (expf(t.z - m) / sum - mass) * coef);
         }
     }
+};
+
+__device__ __forceinline__ float lanes_max(float v) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+    return v;
+}
+__device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+// a row without logits has no softmax: it is left out (a NaN counts as a logit)
+__device__ __forceinline__ bool has_logits(float m, float sum) { return !(m == -INFINITY && !(sum != sum)); }
+
+// a block's rows counted, and the losses added up by the last one
+__device__ __forceinline__ void finish_block(const DistillArgs &a) {
     __shared__ int s_last;
     __syncthreads();
     if (threadIdx.x == 0) s_last = last_counted(a, gridDim.x);
@@ -767,11 +795,128 @@ __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
     if (s_last) add_losses(a);
 }
 
+// Rows of up to 32 E classes: a warp to a row, E columns a lane.
+template <class T, int E>
+__global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
+    __shared__ WarpShared s_warp[8];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long r = (long long)blockIdx.x * 8 + warp;
+    if (r < a.y.rows) {
+        const Logit logit(a.y);
+        const T *row = static_cast<const T *>(a.y.y) + r * a.y.ld;
+        T *g = a.g ? static_cast<T *>(a.g) + r * a.ld_g : nullptr;
+        const float rw = a.row_weight ? a.row_weight[r] : 1.f / (float)a.y.rows;
+        float z[E];
+        bool silent[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const int c = lane + 32 * i;
+            silent[i] = true;
+            z[i] = c < a.y.cols ? logit.of(to_f32<T>(row[c]), silent[i]) : -INFINITY;
+        }
+        WarpTeacher teacher{};
+        teacher.read<T>(a, logit, row, g, r, lane, s_warp[warp]);
+        float m = -INFINITY, s = 0.f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) m = fmaxf(m, z[i]);
+        m = lanes_max(m);
+#pragma unroll
+        for (int i = 0; i < E; ++i) s += z[i] == -INFINITY ? 0.f : expf(z[i] - m);
+        s = lanes_sum(s);
+        const bool done = teacher.any && rw != 0.f && has_logits(m, s);
+        const float loss = teacher.loss(m, s, done);
+        if (lane == 0) a.row_loss[r] = loss;
+        if (g && (done || !a.accumulate)) {
+            const float coef = a.weight * rw * logit.factor, over = coef / s;
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const int c = lane + 32 * i;
+                if (c >= a.y.cols) continue;
+                const float d = silent[i] || !done ? 0.f : expf(z[i] - m) * over;
+                g[c] = round_out<T>(a.accumulate ? to_f32<T>(g[c]) + d : d);
+            }
+            __syncwarp();
+            if (done) teacher.write<T>(a, g, m, s, coef, lane, s_warp[warp]);
+        }
+    }
+    finish_block(a);
+}
+
+// Rows of up to 32 N packs: a warp to a row, N packs of 16 bytes a lane, in registers (13319 rows of 698 16-bit
+// classes, 64 entries: 71 us with single columns, in blocks 133).
+template <class T, int N, bool FAST>
+__global__ void __launch_bounds__(256) k_distill_packs(const DistillArgs a) {
+    constexpr int P = Pack<T>::P;
+    __shared__ WarpShared s_warp[8];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long r = (long long)blockIdx.x * 8 + warp;
+    if (r < a.y.rows) {
+        const Logit logit(a.y);
+        const RowView<T> v(a.y, r);
+        T *g = a.g ? static_cast<T *>(a.g) + r * a.ld_g : nullptr;
+        const float rw = a.row_weight ? a.row_weight[r] : 1.f / (float)a.y.rows;
+        uint4 raw[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) raw[j] = lane + 32 * j < v.packs ? v.pack(lane + 32 * j) : make_uint4(0, 0, 0, 0);
+        const int at = v.single(lane);
+        const float one = at >= 0 ? to_f32<T>(v.row[at]) : 0.f;
+        const auto each = [&](auto f) {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (lane + 32 * j < v.packs) f(raw[j], lane + 32 * j);
+        };
+        WarpTeacher teacher{};
+        teacher.read<T>(a, logit, v.row, g, r, lane, s_warp[warp]);
+        const PackMax<T, FAST, false> pack_max(logit);
+        float m = at >= 0 ? logit.of(one) : -INFINITY, s = 0.f;
+        each([&](const uint4 &w, int) { m = fmaxf(m, pack_max(w)); });
+        m = lanes_max(m);
+        const ExpOf<T, FAST> e(logit, m);
+        each([&](const uint4 &w, int) { s += e.sum(w); });
+        if (at >= 0) s += e.one(one);
+        s = lanes_sum(s);
+        const bool done = teacher.any && rw != 0.f && has_logits(m, s);
+        const float loss = teacher.loss(m, s, done);
+        if (lane == 0) a.row_loss[r] = loss;
+        if (g && (done || !a.accumulate)) {
+            const float coef = a.weight * rw * logit.factor, over = done ? coef / s : 0.f;
+            if (at >= 0) {
+                const float d = done ? e.grad(one, over) : 0.f;
+                g[at] = round_out<T>(a.accumulate ? to_f32<T>(g[at]) + d : d);
+            }
+            T *dst = g + v.head;
+            const bool wide = (reinterpret_cast<uintptr_t>(dst) & 15) == 0;
+            each([&](const uint4 &w, int k) {
+                T *to = dst + k * P;
+                alignas(16) T out[P];
+                if (a.accumulate) {
+#pragma unroll
+                    for (int i = 0; i < P; ++i) out[i] = round_out<T>(to_f32<T>(to[i]) + e.grad(Pack<T>::one(w, i), over));
+                } else if (done) {
+                    e.grads(w, over, out);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < P; ++i) out[i] = round_out<T>(0.f);
+                }
+                if (wide) {
+                    *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(out);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < P; ++i) to[i] = out[i];
+                }
+            });
+            __syncwarp();
+            if (done) teacher.write<T>(a, g, m, s, coef, lane, s_warp[warp]);
+        }
+    }
+    finish_block(a);
+}
+
 constexpr int kRowHeld = 9;
 
-// The last warp of a block has the teacher's entries, the others the row. FAST: 16-bit outputs without a stand-in for silent ones, whose exp is 0 by
-// itself: exp(z - m) = 2^(factor log2(e) y - m log2(e)), one multiply-add and the
-// special-function unit (the product's rounding moves it by 2^-24 |z|, far below a 16-bit rounding).
+// Longer rows, or longer records: the last warp of a block has the teacher's entries, the others the row. What
+// bounds it is the chain of passes between a row's barriers, with three rows to an SM: 4096 rows of 32768 bf16 in 122
+// us, 4.4 TB/s (two rows to an SM, in registers, every entry by the row's own threads: 157).
 template <class T, int THREADS, bool FAST>
 __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const DistillArgs a, const int parts) {
     constexpr int P = Pack<T>::P, ROW = THREADS - 32, WARPS = ROW / 32, SLOTS = 2 * kTopMax;
@@ -787,22 +932,7 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const Disti
     T *g = a.g ? static_cast<T *>(a.g) + r * a.ld_g : nullptr;
     const float rw = a.row_weight ? a.row_weight[r] : 1.f / (float)a.y.rows;
     const HeldRow<T, ROW, kRowHeld> h(v, s_held, !teaches);
-    const float scale = logit.factor * kLog2e;
     float m = -INFINITY, s = 0.f;
-    // nothing but -infinity: every exp below is 0 with any finite base (NaN stays NaN)
-    float base = 0.f;
-    const auto exp_of = [&](float y) {
-        if constexpr (FAST) return exp2_fast(fmaf(y, scale, -base * kLog2e));
-        else return expf(logit.of(y) - base);
-    };
-    const auto exp_pair = [&](uint32_t w) {
-        if constexpr (FAST) {
-            const float2 x = of_pair(fma_pair(word_pair<T>(w), pair_of(scale, scale), pair_of(-base * kLog2e, -base * kLog2e)));
-            return pair_of(exp2_fast(x.x), exp2_fast(x.y));
-        } else {
-            return (uint64_t)w;
-        }
-    };
     if (teaches) {
         // the teacher's softmax, and which of its columns are named twice, beside the others' work on the row
         for (int i = lane; i < SLOTS; i += 32) s_slot[i] = -1;
@@ -853,28 +983,11 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const Disti
         h.ready();
         if (h.at >= 0) m = logit.of(h.one);
         const PackMax<T, FAST, false> pack_max(logit);
-        m = fmaxf(m, pack_max.of_row(h, v));
-#pragma unroll
-        for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-        base = m == -INFINITY ? 0.f : m;
-        if constexpr (FAST) {
-            uint64_t two = pair_of(0.f, 0.f);
-            h.each(v, [&](const uint4 &w, int) {
-                two = add_pair(two, add_pair(add_pair(exp_pair(w.x), exp_pair(w.y)), add_pair(exp_pair(w.z), exp_pair(w.w))));
-            });
-            const float2 f = of_pair(two);
-            s = f.x + f.y;
-        } else {
-            h.each(v, [&](const uint4 &w, int) {
-                float part_sum = 0.f;
-#pragma unroll
-                for (int i = 0; i < P; ++i) part_sum += exp_of(Pack<T>::one(w, i));
-                s += part_sum;
-            });
-        }
-        if (h.at >= 0) s += exp_of(h.one);
-#pragma unroll
-        for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+        m = lanes_max(fmaxf(m, pack_max.of_row(h, v)));
+        const ExpOf<T, FAST> e(logit, m);
+        h.each(v, [&](const uint4 &w, int) { s += e.sum(w); });
+        if (h.at >= 0) s += e.one(h.one);
+        s = lanes_sum(s);
         if (lane == 0) s_stat[warp] = make_float2(m, s);
     }
     __syncthreads();
@@ -897,16 +1010,9 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const Disti
         s = w.y;
         join_lanes(m, s);
     }
-    // a row without logits has no softmax: it is left out (a NaN counts as a logit)
-    const bool done = any && rw != 0.f && !(m == -INFINITY && !(s != s));
-    base = m == -INFINITY ? 0.f : m;
+    const bool done = any && rw != 0.f && has_logits(m, s);
     const float coef = a.weight * rw * logit.factor, over = done ? coef / s : 0.f;
-    const auto grad = [&](float y) {
-        if constexpr (FAST) return exp_of(y) * over;
-        bool silent;
-        const float z = logit.of(y, silent);
-        return silent ? 0.f : expf(z - base) * over;
-    };
+    const ExpOf<T, FAST> e(logit, m);
     // each pack of the share to g: made(pack, its place) gives the P gradients
     const auto write = [&](auto made) {
         T *dst = g + v.head;
@@ -930,24 +1036,14 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const Disti
     if (teaches) {
         // (it has no columns)
     } else if (g && done) {
-        if (h.at >= 0) g[h.at] = round_out<T>(grad(h.one) + (a.accumulate ? to_f32<T>(g[h.at]) : 0.f));
+        if (h.at >= 0) g[h.at] = round_out<T>(e.grad(h.one, over) + (a.accumulate ? to_f32<T>(g[h.at]) : 0.f));
         if (a.accumulate)
             write([&](const uint4 &w, const T *was, T (&out)[P]) {
 #pragma unroll
-                for (int i = 0; i < P; ++i) out[i] = round_out<T>(to_f32<T>(was[i]) + grad(Pack<T>::one(w, i)));
-            });
-        else if constexpr (FAST)
-            write([&](const uint4 &w, const T *, T (&out)[P]) {
-                const uint64_t c = pair_of(over, over);
-                const uint4 y = make_uint4(pair_word<T>(mul_pair(exp_pair(w.x), c)), pair_word<T>(mul_pair(exp_pair(w.y), c)),
-                                           pair_word<T>(mul_pair(exp_pair(w.z), c)), pair_word<T>(mul_pair(exp_pair(w.w), c)));
-                *reinterpret_cast<uint4 *>(out) = y;
+                for (int i = 0; i < P; ++i) out[i] = round_out<T>(to_f32<T>(was[i]) + e.grad(Pack<T>::one(w, i), over));
             });
         else
-            write([&](const uint4 &w, const T *, T (&out)[P]) {
-#pragma unroll
-                for (int i = 0; i < P; ++i) out[i] = round_out<T>(grad(Pack<T>::one(w, i)));
-            });
+            write([&](const uint4 &w, const T *, T (&out)[P]) { e.grads(w, over, out); });
     } else if (g && !a.accumulate) {
         if (h.at >= 0) g[h.at] = round_out<T>(0.f);
         write([&](const uint4 &, const T *, T (&out)[P]) {
@@ -990,19 +1086,25 @@ cudaError_t distill_rows(const DistillArgs &a, cudaStream_t st) {
                : launch_shared<k_distill<T, 512, FAST>, 512, 480 * kRowHeld>(a.y.rows, parts, st, a, parts);
 }
 
+template <class T, bool FAST>
+cudaError_t distill_by_size(const DistillArgs &a, cudaStream_t st) {
+    const int packs = (int)(((long long)a.y.cols * sizeof(T) + 15) / 16);
+    if (a.K > kWarpEntries || packs > 32 * 8) return distill_rows<T, FAST>(a, st);
+    const unsigned blocks = ((unsigned)a.y.rows + 7) / 8;
+    if (packs <= 32 * 2) k_distill_packs<T, 2, FAST><<<blocks, 256, 0, st>>>(a);
+    else k_distill_packs<T, 8, FAST><<<blocks, 256, 0, st>>>(a);
+    return cudaGetLastError();
+}
+
 template <class T>
 cudaError_t distill(const DistillArgs &a, cudaStream_t st) {
-    const bool small = a.y.cols <= 1024 && a.K <= 64;
-    const unsigned blocks = ((unsigned)a.y.rows + 7) / 8;
-    if (small) {
-        if (a.y.cols <= 64) k_distill_small<T, 2><<<blocks, 256, 0, st>>>(a);
-        else if (a.y.cols <= 256) k_distill_small<T, 8><<<blocks, 256, 0, st>>>(a);
-        else k_distill_small<T, 32><<<blocks, 256, 0, st>>>(a);
+    if (a.y.cols <= 64 && a.K <= kWarpEntries) {
+        k_distill_small<T, 2><<<((unsigned)a.y.rows + 7) / 8, 256, 0, st>>>(a);
         return cudaGetLastError();
     }
     if (sizeof(T) == 2 && a.y.factor * a.y.silent == -INFINITY && fabsf(a.y.factor) < 1e30f)
-        return distill_rows<T, sizeof(T) == 2>(a, st);
-    return distill_rows<T, false>(a, st);
+        return distill_by_size<T, sizeof(T) == 2>(a, st);
+    return distill_by_size<T, false>(a, st);
 }
 
 }  // namespace

@@ -150,6 +150,33 @@ def test_distill(type, R, C, K):
     check(y, v, i, g, type)
 
 
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("C", [64, 65, 256, 257, 511, 512, 513, 1024, 2047, 2048, 2049, 9000])
+def test_sizes_where_the_form_changes(type, C):
+    y, v, i, g = make(11, C, 33, type, C, pad=1, gpad=1)
+    check(y, v, i, g, type)
+    check(y, v, i, g, type, factor=-0.5)
+    y, v, i, g = make(4, C, 64, type, C, times=True)
+    check(y, v, i, g, type, factor=-50.0, silent=1.2, weight=2.0)
+
+
+def test_many_rows():
+    """More rows than blocks at a time, each form; the sum over them."""
+    for C, K in ((12, 4), (200, 6), (900, 20), (3000, 70)):
+        y, v, i, g = make(5000, C, K, "bf16", C)
+        loss, rows = torch.zeros(2, device="cuda"), torch.empty(5000, device="cuda")
+        w = torch.rand(5000, device="cuda")
+        dstd.distill_loss(y, v, i, loss, rows, g[1], row_weight=w, weight=0.5)
+        want = 0.5 * (w.double() * rows.double()).sum().item()
+        # a rounding of each product and of the compensated sums, and a tree of 8 or 9 levels
+        assert abs(loss[0].item() - want) <= 12 * 2.0 ** -24 * 0.5 * (w.double() * rows.double().abs()).sum().item()
+        few = slice(4990, 5000)
+        loss2, rows2 = torch.zeros(2, device="cuda"), torch.empty(10, device="cuda")
+        g2 = torch.empty_like(g[1][few])
+        dstd.distill_loss(y[few], v[few], i[few], loss2, rows2, g2, row_weight=w[few], weight=0.5)
+        assert torch.equal(rows[few], rows2) and torch.equal(g[1][few], g2)
+
+
 @pytest.mark.parametrize("type", ["f32", "bf16"])
 @pytest.mark.parametrize("pad,offset,gpad,goffset", [(1, 0, 0, 0), (0, 1, 0, 1), (3, 5, 8, 2), (4, 4, 4, 4), (8, 3, 8, 3)])
 @pytest.mark.parametrize("C", [10, 77, 1500, 9001])

@@ -129,11 +129,15 @@ def test_rows_are_shared_only_where_they_are_few(lib):
 
 
 def test_short_rows_take_a_warp(lib):
-    for R, C, K, name in [(256, 10, 4, "k_distill_small"), (17, 1024, 64, "k_distill_small"), (17, 1025, 64, "k_distillI"), (17, 10, 65, "k_distillI")]:
+    for R, C, K, type, name in [(256, 10, 4, 0, "k_distill_small"), (9, 64, 64, 1, "k_distill_small"), (9, 65, 64, 0, "k_distill_packsIfLi2E"),
+                                (17, 256, 64, 0, "k_distill_packsIfLi2E"), (17, 257, 64, 0, "k_distill_packsIfLi8E"),
+                                (17, 512, 64, 2, "k_distill_packsI6__halfLi2E"), (17, 2048, 64, 2, "k_distill_packsI6__halfLi8E"),
+                                (17, 1024, 64, 0, "k_distill_packsIfLi8E"), (17, 1025, 64, 0, "k_distillI"), (17, 2049, 64, 1, "k_distillI"),
+                                (17, 10, 65, 0, "k_distillI")]:
         before = lib.fake_launches()
-        assert distill(lib, R, C, K) == OK
+        assert distill(lib, R, C, K, type) == OK
         (got, grid, _, _), = fake_cuda.launches(lib)[before:]
-        assert name in got and grid == (-(-R // 8) if "small" in name else R)
+        assert name in got and grid == (R if name == "k_distillI" else -(-R // 8))
     for R, C, name in [(256, 10, "k_top_small"), (9, 128, "k_top_small"), (9, 129, "k_top_logits")]:
         before = lib.fake_launches()
         assert top(lib, R, C, 5) == OK
