@@ -2016,8 +2016,8 @@ int dstd_distill_loss(const void *y, dstd_type type, int R, int C, int64_t ld_y,
     Timed tm(KK_DISTILL, (cudaStream_t)stream);
     const LogitArgs a{y, type, R, C, ld_y, factor, silent};
     return cu(launch_distill(DistillArgs{a, top, index, K, teacher_factor, weight, row_weight, loss, row_loss, g, ld_g,
-                                         accumulate != 0},
-                             (cudaStream_t)stream));
+                                         accumulate != 0, true},
+                             tm.launches, (cudaStream_t)stream));
 }
 
 }  // extern "C"

@@ -624,11 +624,20 @@ __device__ __forceinline__ void add_losses(const DistillArgs &a) {
     const float even = 1.f / (float)a.y.rows;
     for (long long i0 = threadIdx.x; i0 < a.y.rows; i0 += 8 * blockDim.x) {
         float w[8], loss[8];
+        // the last row again behind it, with no weight: eight loads under way at once
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const long long i = i0 + e * blockDim.x;
-            w[e] = i >= a.y.rows ? 0.f : (a.row_weight ? a.row_weight[i] : even);
-            loss[e] = i < a.y.rows ? __ldcg(a.row_loss + i) : 0.f;
+            const long long i = i0 + e * blockDim.x, at = min(i, (long long)a.y.rows - 1);
+            loss[e] = __ldcg(a.row_loss + at);
+            w[e] = i < a.y.rows ? even : 0.f;
+        }
+        if (a.row_weight) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const long long i = i0 + e * blockDim.x;
+                const float given = a.row_weight[min(i, (long long)a.y.rows - 1)];
+                w[e] = i < a.y.rows ? given : 0.f;
+            }
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -789,6 +798,7 @@ __device__ __forceinline__ bool has_logits(float m, float sum) { return !(m == -
 // a block's rows counted, and the losses added up by the last one
 __device__ __forceinline__ void finish_block(const DistillArgs &a) {
     __shared__ int s_last;
+    if (!a.ticket) return;
     __syncthreads();
     if (threadIdx.x == 0) s_last = last_counted(a, gridDim.x);
     __syncthreads();
@@ -799,6 +809,7 @@ __device__ __forceinline__ void finish_block(const DistillArgs &a) {
 template <class T, int E>
 __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
     __shared__ WarpShared s_warp[8];
+    let_next_launch();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long r = (long long)blockIdx.x * 8 + warp;
     if (r < a.y.rows) {
@@ -843,11 +854,12 @@ __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
 }
 
 // Rows of up to 32 N packs: a warp to a row, N packs of 16 bytes a lane, in registers (13319 rows of 698 16-bit
-// classes, 64 entries: 71 us with single columns, in blocks 133).
+// classes, 64 entries: 38 us; with single columns 71, in blocks 133).
 template <class T, int N, bool FAST>
 __global__ void __launch_bounds__(256) k_distill_packs(const DistillArgs a) {
     constexpr int P = Pack<T>::P;
     __shared__ WarpShared s_warp[8];
+    let_next_launch();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long r = (long long)blockIdx.x * 8 + warp;
     if (r < a.y.rows) {
@@ -924,6 +936,7 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const Disti
     __shared__ float s_p[kTopMax], s_log[kTopMax], s_z[kTopMax], s_old[kTopMax];
     __shared__ int s_any, s_twice, s_last, s_at[kTopMax], s_slot[SLOTS];
     extern __shared__ uint4 s_held[];
+    let_next_launch();
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31, part = parts > 1 ? (int)cluster_ctarank() : 0;
     const long long r = blockIdx.x / parts;
     const bool teaches = warp == WARPS;
@@ -1062,7 +1075,7 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const Disti
         // counted here, where this warp has written nothing else that the fence would wait for
         if (lane == 0) {
             a.row_loss[r] = loss;
-            s_last = last_counted(a, (unsigned)a.y.rows);
+            if (a.ticket) s_last = last_counted(a, (unsigned)a.y.rows);
         }
     }
     __syncthreads();
@@ -1074,7 +1087,13 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const Disti
             if (!s_twice || column_mass(s_at, s_p, k, a.K, mass))
                 g[at] = round_out<T>(s_old[k] + (expf(s_z[k] - m) / s - mass) * coef);
         }
-    if (part == 0 && s_last) add_losses(a);
+    if (a.ticket && part == 0 && s_last) add_losses(a);
+}
+
+// the losses of many rows, where a block should not wait for its stores to be counted
+__global__ void __launch_bounds__(512) k_distill_sum(const DistillArgs a) {
+    wait_launch_before();
+    add_losses(a);
 }
 
 template <class T, bool FAST>
@@ -1086,25 +1105,33 @@ cudaError_t distill_rows(const DistillArgs &a, cudaStream_t st) {
                : launch_shared<k_distill<T, 512, FAST>, 512, 480 * kRowHeld>(a.y.rows, parts, st, a, parts);
 }
 
+// blocks that count their rows: as many as two to an SM (4096 rows of 32768 bf16: 122 us when each counted its own)
+constexpr int kCounting = 304;
+
 template <class T, bool FAST>
-cudaError_t distill_by_size(const DistillArgs &a, cudaStream_t st) {
+cudaError_t distill_by_size(DistillArgs &a, cudaStream_t st) {
     const int packs = (int)(((long long)a.y.cols * sizeof(T) + 15) / 16);
-    if (a.K > kWarpEntries || packs > 32 * 8) return distill_rows<T, FAST>(a, st);
     const unsigned blocks = ((unsigned)a.y.rows + 7) / 8;
-    if (packs <= 32 * 2) k_distill_packs<T, 2, FAST><<<blocks, 256, 0, st>>>(a);
-    else k_distill_packs<T, 8, FAST><<<blocks, 256, 0, st>>>(a);
+    a.ticket = blocks <= kCounting;
+    if (a.y.cols <= 64 && a.K <= kWarpEntries) {
+        k_distill_small<T, 2><<<blocks, 256, 0, st>>>(a);
+    } else if (a.K <= kWarpEntries && packs <= 32 * 2) {
+        k_distill_packs<T, 2, FAST><<<blocks, 256, 0, st>>>(a);
+    } else if (a.K <= kWarpEntries && packs <= 32 * 8) {
+        k_distill_packs<T, 8, FAST><<<blocks, 256, 0, st>>>(a);
+    } else {
+        a.ticket = a.y.rows <= kCounting;
+        return distill_rows<T, FAST>(a, st);
+    }
     return cudaGetLastError();
 }
 
 template <class T>
-cudaError_t distill(const DistillArgs &a, cudaStream_t st) {
-    if (a.y.cols <= 64 && a.K <= kWarpEntries) {
-        k_distill_small<T, 2><<<((unsigned)a.y.rows + 7) / 8, 256, 0, st>>>(a);
-        return cudaGetLastError();
-    }
-    if (sizeof(T) == 2 && a.y.factor * a.y.silent == -INFINITY && fabsf(a.y.factor) < 1e30f)
-        return distill_by_size<T, sizeof(T) == 2>(a, st);
-    return distill_by_size<T, false>(a, st);
+cudaError_t distill(DistillArgs a, int &launches, cudaStream_t st) {
+    const bool fast = sizeof(T) == 2 && a.y.factor * a.y.silent == -INFINITY && fabsf(a.y.factor) < 1e30f;
+    const cudaError_t e = fast ? distill_by_size<T, sizeof(T) == 2>(a, st) : distill_by_size<T, false>(a, st);
+    launches = a.ticket ? 1 : 2;
+    return e != cudaSuccess || a.ticket ? e : launch_dependent(k_distill_sum, 1, 512, st, a);
 }
 
 }  // namespace
@@ -1115,10 +1142,10 @@ cudaError_t launch_top_logits(const LogitArgs &a, int K, float *top, int32_t *in
     return top_logits<__half>(a, K, top, index, st);
 }
 
-cudaError_t launch_distill(const DistillArgs &a, cudaStream_t st) {
-    if (a.y.type == DSTD_TYPE_F32) return distill<float>(a, st);
-    if (a.y.type == DSTD_TYPE_BF16) return distill<__nv_bfloat16>(a, st);
-    return distill<__half>(a, st);
+cudaError_t launch_distill(const DistillArgs &a, int &launches, cudaStream_t st) {
+    if (a.y.type == DSTD_TYPE_F32) return distill<float>(a, launches, st);
+    if (a.y.type == DSTD_TYPE_BF16) return distill<__nv_bfloat16>(a, launches, st);
+    return distill<__half>(a, launches, st);
 }
 
 }  // namespace dstd

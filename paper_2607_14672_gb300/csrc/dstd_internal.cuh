@@ -822,7 +822,8 @@ struct DistillArgs {
     void *g;                  // or null
     long long ld_g;
     bool accumulate;
+    bool ticket;              // the last block adds the rows' losses up (set by the launch)
 };
-cudaError_t launch_distill(const DistillArgs &a, cudaStream_t st);
+cudaError_t launch_distill(const DistillArgs &a, int &launches, cudaStream_t st);  // launches out
 
 }  // namespace dstd
