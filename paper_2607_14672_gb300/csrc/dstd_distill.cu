@@ -586,12 +586,16 @@ struct Record {
 // What entry k's column gets: its p and those of later entries of the same column; false where an
 // earlier entry has it.
 __device__ __forceinline__ bool column_mass(const int *at, const float *p, int k, int K, float &mass) {
-    for (int j = 0; j < k; ++j)
-        if (at[j] == at[k]) return false;
-    mass = p[k];
-    for (int j = k + 1; j < K; ++j)
-        if (at[j] == at[k]) mass += p[j];
-    return true;
+    const int own = at[k];
+    bool first = true;
+    mass = 0.f;
+#pragma unroll 8
+    for (int j = 0; j < K; ++j) {
+        const bool same = at[j] == own;
+        first = first && !(same && j < k);
+        mass += same && j >= k ? p[j] : 0.f;
+    }
+    return first;
 }
 // this entry's share of the row's loss, given the log of the softmax's denominator
 __device__ __forceinline__ float teacher_loss(const Teacher &t, float m, float log_sum) {
@@ -664,14 +668,36 @@ __device__ __forceinline__ void add_losses(const DistillArgs &a) {
     }
 }
 
-// Columns that a teacher names, to find one named twice: open addressing, exact.
-template <int SLOTS>
-__device__ __forceinline__ bool named_before(int *slot, int at) {
-    for (int i = at & (SLOTS - 1);; i = (i + 1) & (SLOTS - 1)) {
-        const int was = atomicCAS(&slot[i], -1, at);
-        if (was == at) return true;
-        if (was == -1) return false;
+// Whether one of a warp's K columns (negative: none) is named twice. Entries of one place in the table meet in rounds;
+// each leaves one of them there for the others to look at, so that every round ends some of them (single steps of
+// compare-and-swap took 5 us of 13, as lanes went their own ways).
+template <int EACH, int SLOTS>
+__device__ __forceinline__ bool named_twice(const int *at, int *slot, int K, int lane) {
+    int column[EACH];  // -1: none, or through
+    bool open = false, again = false;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        column[e] = 32 * e + lane < K ? at[32 * e + lane] : -1;
+        open = open || column[e] >= 0;
     }
+    while (__any_sync(0xffffffffu, open)) {
+#pragma unroll
+        for (int e = 0; e < EACH; ++e)
+            if (32 * e < K && column[e] >= 0) slot[column[e] & (SLOTS - 1)] = 32 * e + lane;
+        __syncwarp();
+        open = false;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e)
+            if (32 * e < K && column[e] >= 0) {
+                const int there = slot[column[e] & (SLOTS - 1)];
+                const bool own = there == 32 * e + lane, met = !own && at[there] == column[e];
+                again = again || met;
+                if (own || met) column[e] = -1;
+                else open = true;
+            }
+        __syncwarp();
+    }
+    return __any_sync(0xffffffffu, again);
 }
 
 // exp(z - m) of outputs, m the largest logit (nothing but -infinity: every exp is 0 with any finite m, and NaN stays
@@ -737,8 +763,6 @@ struct WarpTeacher {
     __device__ __forceinline__ void read(const DistillArgs &a, const Logit &logit, const T *row, const T *g, long long r,
                                          int lane, WarpShared &s) {
         const Record<2> record(a, r, lane);
-#pragma unroll
-        for (int i = 0; i < kWarpSlots / 32; ++i) s.slot[lane + 32 * i] = -1;
         any = record.any();
         float y[2], old[2], m, log_sum;
 #pragma unroll
@@ -754,11 +778,7 @@ struct WarpTeacher {
             s.p[32 * e + lane] = entry[e].p;
         }
         __syncwarp();
-        bool again = false;
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-            if (entry[e].at >= 0 && named_before<kWarpSlots>(s.slot, entry[e].at)) again = true;
-        twice = __any_sync(0xffffffffu, again);
+        twice = named_twice<2, kWarpSlots>(s.at, s.slot, a.K, lane);
     }
     // the row's loss, in every lane
     __device__ __forceinline__ float loss(float m, float sum, bool done) const {
@@ -854,7 +874,8 @@ __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
 }
 
 // Rows of up to 32 N packs: a warp to a row, N packs of 16 bytes a lane, in registers (13319 rows of 698 16-bit
-// classes, 64 entries: 38 us; with single columns 71, in blocks 133).
+// classes, 64 entries: 22 us, 1.7 TB/s; when in blocks 133 and with single columns 71, both before the losses had a
+// launch of their own). Instructions bound it: exponentials, the teacher's entries, and sums across lanes.
 template <class T, int N, bool FAST>
 __global__ void __launch_bounds__(256) k_distill_packs(const DistillArgs a) {
     constexpr int P = Pack<T>::P;
@@ -948,7 +969,6 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const Disti
     float m = -INFINITY, s = 0.f;
     if (teaches) {
         // the teacher's softmax, and which of its columns are named twice, beside the others' work on the row
-        for (int i = lane; i < SLOTS; i += 32) s_slot[i] = -1;
         float tm = -INFINITY;
         bool some = false;
         for (int k = lane; k < a.K; k += 32) {
@@ -965,7 +985,6 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const Disti
         for (int d = 16; d; d >>= 1) tm = fmaxf(tm, __shfl_xor_sync(0xffffffffu, tm, d));
         __syncwarp();
         float sum = 0.f;
-        bool again = false;
         for (int k = lane; k < a.K; k += 32) {
             const int at = s_at[k];
             if (at < 0) continue;
@@ -975,7 +994,6 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const Disti
             s_old[k] = a.accumulate && g ? to_f32<T>(g[at]) : 0.f;
             if (silent) s_at[k] = at | (1 << 30);  // its column gets no gradient
             sum += expf(s_log[k] - tm);
-            if (named_before<SLOTS>(s_slot, at)) again = true;
         }
 #pragma unroll
         for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
@@ -986,7 +1004,8 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const Disti
             s_p[k] = s_at[k] >= 0 ? expf(log_p) : 0.f;
         }
         some = __any_sync(0xffffffffu, some);
-        again = __any_sync(0xffffffffu, again);
+        __syncwarp();
+        const bool again = named_twice<kTopMax / 32, SLOTS>(s_at, s_slot, a.K, lane);
         if (lane == 0) {
             s_any = some;
             s_twice = again;
@@ -1105,7 +1124,8 @@ cudaError_t distill_rows(const DistillArgs &a, cudaStream_t st) {
                : launch_shared<k_distill<T, 512, FAST>, 512, 480 * kRowHeld>(a.y.rows, parts, st, a, parts);
 }
 
-// blocks that count their rows: as many as two to an SM (4096 rows of 32768 bf16: 122 us when each counted its own)
+// blocks that count their rows: as many as two to an SM. More have the losses added up by a launch of their own, since
+// a block that counts waits for its stores (13319 rows of 698 fp16: 38 us counted, 32 with the launch).
 constexpr int kCounting = 304;
 
 template <class T, bool FAST>
