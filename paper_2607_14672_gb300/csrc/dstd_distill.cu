@@ -169,7 +169,8 @@ struct HeldRow {
 // about 68. Those are gathered and put in order by counting, for each, the larger ones. Of rows
 // with many more logits at the bound (equal ones) those above it are gathered, and the first
 // columns of the equal ones. Few long rows
-// are shared by the blocks of a cluster, which then count each other's.
+// are shared by the blocks of a cluster, which then count each other's. What bounds it is the chain of passes between a
+// row's barriers, with three rows to an SM: 4096 rows of 32768 bf16, K = 64, in 71 us, 3.8 TB/s.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t key_of(float z) {
     if (z != z) return 0xfffffffeu;
@@ -463,6 +464,112 @@ __global__ void __launch_bounds__(256) k_top_small(const LogitArgs a, const int 
         }
 }
 
+// Rows of up to 32 E columns and K <= 64: a warp to a row, whose keys stay in registers. The least of the lanes' largest
+// (of their two largest, in two groups, for K > 32) is a bound with K logits or more at or above it; halving the
+// interval from there to the row's largest narrows them to a list that is put in order by counting. Where equal logits
+// keep the list long, their first columns are taken. Instructions bound it: 10000 rows of 1000 fp32, K = 10, 18 us, 2.2
+// TB/s (in blocks 46).
+constexpr int kTopWarp = 64;
+template <class T, int E>
+__global__ void __launch_bounds__(256) k_top_packs(const LogitArgs a, const int K, float *top, int32_t *index) {
+    constexpr int P = Pack<T>::P, N = E / P;
+    constexpr uint32_t ALL = 0xffffffffu;
+    __shared__ unsigned long long s_list[8][kTopWarp + 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long r = (long long)blockIdx.x * 8 + warp;
+    if (r >= a.rows) return;
+    const Logit logit(a);
+    const RowView<T> v(a, r);
+    uint32_t key[E + 1];  // 0: none
+    uint4 raw[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) raw[j] = lane + 32 * j < v.packs ? v.pack(lane + 32 * j) : make_uint4(0, 0, 0, 0);
+    const int at = v.single(lane);
+    const float one = at >= 0 ? to_f32<T>(v.row[at]) : 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        key[e] = lane + 32 * (e / P) < v.packs ? key_of(logit.of(Pack<T>::one(raw[e / P], e % P))) : 0u;
+    key[E] = at >= 0 ? key_of(logit.of(one)) : 0u;
+
+    uint32_t even = key[E], odd = 0u;
+#pragma unroll
+    for (int e = 0; e < E; e += 2) even = max(even, key[e]), odd = max(odd, key[e + 1]);
+    const auto count = [&](uint32_t least) {
+        unsigned c = 0;
+#pragma unroll
+        for (int e = 0; e <= E; ++e) c += key[e] >= least;
+        return c;
+    };
+    const unsigned wanted = (unsigned)K, most = (wanted + 39) & ~31u;
+    uint32_t low = max(1u, __reduce_min_sync(ALL, K <= 32 ? max(even, odd) : min(even, odd)));
+    uint32_t high = __reduce_max_sync(ALL, max(even, odd)) + 1;  // fewer than K from here on
+    unsigned n = __reduce_add_sync(ALL, count(low));
+    while (n > most && high - low > 1) {
+        const uint32_t middle = low + (high - low) / 2;
+        const unsigned c = __reduce_add_sync(ALL, count(middle));
+        if (c >= wanted) low = middle, n = c;
+        else high = middle;
+    }
+    if (n > most) {
+        // equal ones: as many as are wanted, by columns (single ones before the packs, packs, single ones behind)
+        unsigned left = wanted - __reduce_add_sync(ALL, count(high));
+        const auto keep = [&](unsigned equal) {  // how many of a lane's equal ones, and of all lanes'
+            unsigned before = equal;
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) {
+                const unsigned other = __shfl_up_sync(ALL, before, d);
+                if (lane >= d) before += other;
+            }
+            const unsigned all = __shfl_sync(ALL, before, 31);
+            before -= equal;
+            const unsigned kept = before < left ? left - before : 0u;
+            left -= min(left, all);
+            return kept;
+        };
+        if (keep(key[E] == low && at < v.head) == 0 && key[E] == low && at < v.head) key[E] = 0u;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            unsigned equal = 0;
+#pragma unroll
+            for (int i = 0; i < P; ++i) equal += key[j * P + i] == low;
+            unsigned kept = keep(equal);
+#pragma unroll
+            for (int i = 0; i < P; ++i)
+                if (key[j * P + i] == low) {
+                    if (kept) --kept;
+                    else key[j * P + i] = 0u;
+                }
+        }
+        if (keep(key[E] == low && at >= v.head) == 0 && key[E] == low && at >= v.head) key[E] = 0u;
+        n = wanted;
+    }
+    const unsigned own = count(low);
+    unsigned place = own;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const unsigned other = __shfl_up_sync(ALL, place, d);
+        if (lane >= d) place += other;
+    }
+    place -= own;
+    const auto list = [&](uint32_t k, int column) {
+        if (k >= low) s_list[warp][place++] = (unsigned long long)k << 32 | (uint32_t)~column;
+    };
+#pragma unroll
+    for (int e = 0; e < E; ++e) list(key[e], v.head + (lane + 32 * (e / P)) * P + e % P);
+    list(key[E], at);
+    __syncwarp();
+    for (unsigned i = lane; i < n; i += 32) {
+        const unsigned long long mine = s_list[warp][i];
+        unsigned rank = 0;
+#pragma unroll 8
+        for (unsigned j = 0; j < n; ++j) rank += s_list[warp][j] > mine;
+        if (rank < wanted) {
+            top[r * K + rank] = logit_of_key((uint32_t)(mine >> 32));
+            index[r * K + rank] = (int32_t)~(uint32_t)mine;
+        }
+    }
+}
+
 // blocks that share a row: where the rows alone do not fill the GPU, up to 8 of at least `least` packs
 int shares(int rows, int packs, int least) {
     int parts = 1;
@@ -507,6 +614,15 @@ cudaError_t top_logits(const LogitArgs &a, int K, float *top, int32_t *index, cu
     const unsigned blocks = ((unsigned)a.rows + 7) / 8;
     if (a.cols <= 32) {
         k_top_small<T, 1><<<blocks, 256, 0, st>>>(a, K, top, index);
+        return cudaGetLastError();
+    }
+    const int packs = (int)(((long long)a.cols * sizeof(T) + 15) / 16);
+    // few rows of more than 256 columns are faster in blocks (300 fp32, K = 20: 608 rows 4.3 us both ways, 152 rows 4.2
+    // and 3.3, 912 rows 4.7 and 6.8, 10000 rows 12 and 42); of up to 256 they are not
+    if (K <= kTopWarp && packs * Pack<T>::P <= (a.rows > 5 * 152 ? 32 * 32 : 32 * 8)) {
+        if (packs * Pack<T>::P <= 32 * 8) k_top_packs<T, 8><<<blocks, 256, 0, st>>>(a, K, top, index);
+        else if (packs * Pack<T>::P <= 32 * 16) k_top_packs<T, 16><<<blocks, 256, 0, st>>>(a, K, top, index);
+        else k_top_packs<T, 32><<<blocks, 256, 0, st>>>(a, K, top, index);
         return cudaGetLastError();
     }
     if (a.cols <= 128) {

@@ -77,6 +77,33 @@ def test_top_of_equal_rows(C):
         check_top(y.bfloat16().cuda(), K)
 
 
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("C", [32, 33, 64, 129, 255, 256, 257, 511, 1000, 1023, 1024, 1025])
+def test_top_where_the_form_changes(type, C):
+    """Random rows, rows of few different logits and rows with one that differs, at every alignment."""
+    gen = torch.Generator().manual_seed(C)
+    for offset in range(3):
+        _, y = padded(10, C, 1 + offset, TYPES[type], offset)
+        y.copy_(torch.randn(10, C, generator=gen) * 2.5)
+        y[2] = y[2].sign()
+        y[3] = (y[3] * 2).round()
+        y[4], y[5], y[6] = 1.0, float("-inf"), -float("inf")
+        y[4, C // 2], y[5, C - 1], y[5, 0] = 2.0, 0.5, float("nan")
+        y[7, :: 2] = -0.0
+        y[7, 1:: 2] = 0.0
+        y[8].copy_(torch.arange(C) * -1e-3)
+        y[9].copy_(torch.randn(C, generator=gen).clamp(max=0.0))
+        for K in sorted({1, min(C, 24), min(C, 25), 32, min(C, 33), min(C, 57), min(C, 64), min(C, 65)}):
+            check_top(y, K)
+        check_top(y, 20, factor=-3.0)
+        check_top(y, min(C, 50), -50.0, 1.2)
+        _, many = padded(800, C, 1 + offset, TYPES[type], offset)
+        many.copy_(y.repeat(80, 1))
+        for K, kw in [(1, {}), (24, {}), (min(C, 33), {}), (min(C, 64), {}), (20, dict(factor=-3.0)), (min(C, 50), dict(factor=-50.0, silent=1.2))]:
+            for few, all in zip(top(y, K, **kw), top(many, K, **kw)):
+                assert torch.equal(few.repeat(80, 1).view(torch.int32), all.view(torch.int32))
+
+
 def make(R, C, K, type, seed=0, pad=0, offset=0, times=False, gpad=0, goffset=0):
     gen = torch.Generator().manual_seed(seed)
     _, y = padded(R, C, pad, TYPES[type], offset)

@@ -139,7 +139,11 @@ def test_short_rows_take_a_warp(lib):
         assert distill(lib, R, C, K, type) == OK
         (got, grid, _, _), = fake_cuda.launches(lib)[before:]
         assert name in got and grid == (R if name == "k_distillI" else -(-R // 8))
-    for R, C, name in [(256, 10, "k_top_small"), (9, 128, "k_top_small"), (9, 129, "k_top_logits")]:
+    for R, C, K, type, name in [(256, 10, 4, 0, "k_top_small"), (9, 33, 5, 0, "k_top_packsIfLi8E"), (9, 256, 64, 1, "k_top_packsI13__nv_bfloat16Li8E"),
+                                (9, 257, 64, 0, "k_top_logits"), (760, 257, 64, 0, "k_top_logits"), (761, 257, 64, 0, "k_top_packsIfLi16E"),
+                                (761, 513, 64, 0, "k_top_packsIfLi32E"), (761, 1024, 64, 2, "k_top_packsI6__halfLi32E"), (761, 1025, 5, 0, "k_top_logits"),
+                                (9, 128, 65, 0, "k_top_small"), (9, 129, 65, 0, "k_top_logits")]:
         before = lib.fake_launches()
-        assert top(lib, R, C, 5) == OK
-        assert name in fake_cuda.launches(lib)[before][0]
+        assert top(lib, R, C, K, type) == OK
+        (got, grid, _, _), = fake_cuda.launches(lib)[before:]
+        assert name in got and grid == (R if name == "k_top_logits" else -(-R // 8))
