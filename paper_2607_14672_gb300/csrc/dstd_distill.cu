@@ -169,8 +169,9 @@ struct HeldRow {
 // about 68. Those are gathered and put in order by counting, for each, the larger ones. Of rows
 // with many more logits at the bound (equal ones) those above it are gathered, and the first
 // columns of the equal ones. Few long rows
-// are shared by the blocks of a cluster, which then count each other's. What bounds it is the chain of passes between a
-// row's barriers, with three rows to an SM: 4096 rows of 32768 bf16, K = 64, in 71 us, 3.8 TB/s.
+// are shared by the blocks of a cluster, which then count each other's. A row is not held: the few packs with logits at the
+// bound come from L2 once more (held in shared memory, three rows to an SM: 71 us). What bounds it is the latency of
+// those steps, with six rows to an SM: 4096 rows of 32768 bf16, K = 64, in 62 us, 4.3 TB/s.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t key_of(float z) {
     if (z != z) return 0xfffffffeu;
@@ -194,7 +195,9 @@ struct Two<__half> { using type = __half2; };
 template <>
 struct Two<__nv_bfloat16> { using type = __nv_bfloat162; };
 
-constexpr int kTopHeld = 8;
+constexpr int kTopBatch = 4;      // packs that a thread loads at once (4 groups: 67 us in place of 62)
+constexpr int kTopGroups = 2;     // of a thread's packs; one with a logit at the bound is read again
+constexpr int kTopThreads = 1536; // on an SM, 40 registers each
 constexpr int kFew = 512;  // as many at most are put in order by counting, the square of them; kTopMax * 3 / 2 + 64 fit
 
 __device__ __forceinline__ uint64_t ld_cluster64(uint32_t addr) {
@@ -240,6 +243,24 @@ struct PackMax {
             return m;
         }
     }
+    // the largest of packs k0, k0 + STEP and so on, COUNT of them or fewer, all loads first; there is one at least
+    template <int COUNT, int STEP, class View>
+    __device__ __forceinline__ float of_packs(const View &v, int k0) const {
+        uint4 w[COUNT];
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) w[i] = v.pack(k0 + i * STEP < v.last ? k0 + i * STEP : k0);
+        if constexpr (PAIRS) {
+            uint32_t m = words(w[0]);
+#pragma unroll
+            for (int i = 1; i < COUNT; ++i) m = two(m, words(w[i]));
+            return of_words(m);
+        } else {
+            float m = (*this)(w[0]);
+#pragma unroll
+            for (int i = 1; i < COUNT; ++i) m = WITH_NAN ? max_nan(m, (*this)(w[i])) : fmaxf(m, (*this)(w[i]));
+            return m;
+        }
+    }
     // the largest of a thread's packs, -infinity if there are none
     template <class Row, class View>
     __device__ __forceinline__ float of_row(const Row &h, const View &v) const {
@@ -257,34 +278,48 @@ struct PackMax {
 };
 
 template <class T, int THREADS, bool PAIRS>
-__global__ void __launch_bounds__(THREADS, 1536 / THREADS)
+__global__ void __launch_bounds__(THREADS, kTopThreads / THREADS)
     k_top_logits(const LogitArgs a, const int parts, const int K, float *top, int32_t *index) {
     constexpr int P = Pack<T>::P;
     __shared__ uint64_t s_cand[kFew], s_best[kTopMax];
     __shared__ unsigned s_n, s_hits, s_hist[256], s_digit[2], s_warp[THREADS / 32];
     __shared__ int s_hit[kFew];
+    __shared__ uint4 s_pack[kFew];
+    extern __shared__ uint64_t s_all[];
     const int t = threadIdx.x, part = parts > 1 ? (int)cluster_ctarank() : 0;
     const long long r = blockIdx.x / parts;
     const RowView<T> v(a, r, part, parts);
-    extern __shared__ uint4 s_held[];
-    const HeldRow<T, THREADS, kTopHeld> h(v, s_held);
     const Logit logit(a);
     const PackMax<T, PAIRS, true> pack_max(logit);
     if (t == 0) s_n = s_hits = 0;
+    const int single = v.single(t);
+    const float one = single >= 0 ? logit.of(to_f32<T>(v.row[single])) : 0.f;
     // every column of the share once, in any order
     const auto each = [&](auto f) {
-        if (h.at >= 0) f(h.at, key_of(logit.of(h.one)));
-        h.each(v, [&](const uint4 &w, int k) {
+        if (single >= 0) f(single, key_of(one));
+        for (int k = v.first + t; k < v.last; k += THREADS) {
+            const uint4 w = v.pack(k);
 #pragma unroll
             for (int i = 0; i < P; ++i) f(v.head + k * P + i, key_of(logit.of(Pack<T>::one(w, i))));
-        });
+        }
     };
     const int want = min(K, v.high - v.low);
-    h.ready();
+    // the largest of each group of this thread's packs
+    float largest[kTopGroups];
     uint32_t mine = 0, bound = 0;  // 0: below every logit's key
-    if (h.at >= 0 || v.first + t < v.last) {
-        float m = pack_max.of_row(h, v);
-        if (h.at >= 0) m = max_nan(m, logit.of(h.one));
+    constexpr int step = kTopBatch * THREADS;
+    const int group = step * max(1, (v.last - v.first + kTopGroups * step - 1) / (kTopGroups * step));
+#pragma unroll
+    for (int q = 0; q < kTopGroups; ++q) {
+        const int from = v.first + t + q * group, to = min(v.last, from - t + group);
+        largest[q] = -INFINITY;
+        for (int k0 = from; k0 < to; k0 += step)
+            largest[q] = max_nan(largest[q], pack_max.template of_packs<kTopBatch, THREADS>(v, k0));
+    }
+    if (single >= 0 || v.first + t < v.last) {
+        float m = single >= 0 ? one : -INFINITY;
+#pragma unroll
+        for (int q = 0; q < kTopGroups; ++q) m = max_nan(m, largest[q]);
         mine = key_of(m);
     }
     // the upper half of the key will do: a bound lower by 2^-7 at most lets few more pass
@@ -299,25 +334,38 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS)
         const unsigned at = atomicAdd(&s_n, 1u);
         if (at < kFew) s_cand[at] = (uint64_t)k << 32 | (uint32_t)~c;
     };
-    if (h.at >= 0) gather(h.at, logit.of(h.one));
+    if (single >= 0) gather(single, one);
     if (mine >= bound) {
         const float least = bound ? logit_of_key(bound) : -INFINITY;
-        h.each(v, [&](const uint4 &w, int k) {
-            if (pack_max(w) < least) return;
-            const unsigned at = atomicAdd(&s_hits, 1u);
-            if (at < kFew) s_hit[at] = k;
-        });
+        // a group's packs once more, from L2
+        const auto look = [&](int k0) {
+            uint4 w[kTopBatch];
+#pragma unroll
+            for (int i = 0; i < kTopBatch; ++i) w[i] = v.pack(k0 + i * THREADS < v.last ? k0 + i * THREADS : k0);
+#pragma unroll
+            for (int i = 0; i < kTopBatch; ++i) {
+                if (k0 + i * THREADS >= v.last || pack_max(w[i]) < least) continue;
+                const unsigned at = atomicAdd(&s_hits, 1u);
+                if (at < kFew) {
+                    s_hit[at] = k0 + i * THREADS;
+                    s_pack[at] = w[i];
+                }
+            }
+        };
+#pragma unroll
+        for (int q = 0; q < kTopGroups; ++q) {
+            if (largest[q] < least) continue;
+            const int from = v.first + t + q * group, to = min(v.last, from - t + group);
+            for (int k0 = from; k0 < to; k0 += step) look(k0);
+        }
     }
     __syncthreads();
     if (s_hits > kFew) {
         if (t == 0) s_n = kFew + 1u;
     } else {
-        for (unsigned i = t; i < s_hits * P; i += THREADS) {
-            const int k = s_hit[i / P], c = v.head + k * P + (int)(i % P);
-            const T *from = k - v.first < kTopHeld * THREADS ? reinterpret_cast<const T *>(s_held + (k - v.first)) + i % P
-                                                             : v.row + c;
-            gather(c, logit.of(to_f32<T>(*from)));
-        }
+        for (unsigned i = t; i < s_hits * P; i += THREADS)
+            gather(v.head + s_hit[i / P] * P + (int)(i % P),
+                   logit.of(to_f32<T>(reinterpret_cast<const T *>(s_pack + i / P)[i % P])));
     }
     __syncthreads();
     unsigned n = s_n;
@@ -406,8 +454,7 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS)
         if (t >= want && t < K) s_best[t] = 0;  // below every entry
         __syncwarp();
         cluster_sync();
-        // all shares' entries, in the blocks' order, where the row was
-        uint64_t *s_all = reinterpret_cast<uint64_t *>(s_held);
+        // all shares' entries, in the blocks' order
         for (int i = t; i < parts * K; i += THREADS)
             s_all[i] = ld_cluster64(mapa_rank(smem_u32(s_best + i % K), (uint32_t)(i / K)));
         __syncwarp();
@@ -577,14 +624,17 @@ int shares(int rows, int packs, int least) {
     return parts;
 }
 
-template <auto KERNEL, int THREADS, int PACKS, class... A>
+// `held`: bytes of shared memory, granted once for each device where they pass what a block has by itself
+template <auto KERNEL, int THREADS, int HELD, class... A>
 cudaError_t launch_shared(int rows, int parts, cudaStream_t st, const A &...args) {
-    constexpr int held = PACKS * 16;  // bytes
-    static PerDevice granted;
-    if (!granted.get([](int) {
-            return cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, held) == cudaSuccess ? 1 : 0;
-        }))
-        return cudaErrorInvalidConfiguration;
+    constexpr int held = HELD;
+    if constexpr (held > 48 * 1024) {
+        static PerDevice granted;
+        if (!granted.get([](int) {
+                return cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, held) == cudaSuccess ? 1 : 0;
+            }))
+            return cudaErrorInvalidConfiguration;
+    }
     if ((long long)rows * parts > 0x7fffffff) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
@@ -604,9 +654,11 @@ cudaError_t launch_shared(int rows, int parts, cudaStream_t st, const A &...args
 template <class T, bool PAIRS>
 cudaError_t top_rows(const LogitArgs &a, int K, float *top, int32_t *index, cudaStream_t st) {
     const int packs = (int)(((long long)a.cols * sizeof(T) + 15) / 16), parts = shares(a.rows, packs, 512);
-    if (packs / parts <= 256 * kTopHeld)
-        return launch_shared<k_top_logits<T, 256, PAIRS>, 256, 256 * kTopHeld>(a.rows, parts, st, a, parts, K, top, index);
-    return launch_shared<k_top_logits<T, 512, PAIRS>, 512, 512 * kTopHeld>(a.rows, parts, st, a, parts, K, top, index);
+    constexpr int all = 8 * kTopMax * 8;
+    // 256 threads have enough largest ones to bound 128 logits closely (32768 fp32: 99 us with them, 95 with 512)
+    if (parts == 1 && K <= 128 && packs <= 4096)
+        return launch_shared<k_top_logits<T, 256, PAIRS>, 256, 0>(a.rows, parts, st, a, parts, K, top, index);
+    return launch_shared<k_top_logits<T, 512, PAIRS>, 512, all>(a.rows, parts, st, a, parts, K, top, index);
 }
 
 template <class T>
@@ -1236,8 +1288,8 @@ cudaError_t distill_rows(const DistillArgs &a, cudaStream_t st) {
     const int packs = (int)(((long long)a.y.cols * sizeof(T) + 15) / 16), parts = shares(a.y.rows, packs, 512);
     // few blocks have more threads each
     return packs / parts <= 224 * kRowHeld && (a.y.rows * parts >= 152 || packs / parts <= 512)
-               ? launch_shared<k_distill<T, 256, FAST>, 256, 224 * kRowHeld>(a.y.rows, parts, st, a, parts)
-               : launch_shared<k_distill<T, 512, FAST>, 512, 480 * kRowHeld>(a.y.rows, parts, st, a, parts);
+               ? launch_shared<k_distill<T, 256, FAST>, 256, 224 * kRowHeld * 16>(a.y.rows, parts, st, a, parts)
+               : launch_shared<k_distill<T, 512, FAST>, 512, 480 * kRowHeld * 16>(a.y.rows, parts, st, a, parts);
 }
 
 // blocks that count their rows: as many as two to an SM. More have the losses added up by a launch of their own, since
