@@ -119,45 +119,34 @@ struct RowView {
     }
 };
 
-// A block's packs wait in shared memory, HELD to a thread (about 64 KB for 512 threads, so that three rows are on an
-// SM; in registers there were two); those of longer rows are read in every pass. A thread reads back what it
-// copied alone.
-template <class T, int THREADS, int HELD>
-struct HeldRow {
-    const uint4 *slot;
+// A thread's packs of a block's share, read in every pass (from L2 after the first), BATCH at a time.
+template <class T, int THREADS, int BATCH>
+struct OwnPacks {
     float one;
     int at;  // column of `one`, or -1
-    // starts the copies; ready() before any use
-    __device__ __forceinline__ HeldRow(const RowView<T> &v, uint4 *held, bool mine = true) {
-        slot = held + threadIdx.x;
-        at = -1;
-        one = 0.f;
-        if (!mine) return;
-        const int k0 = v.first + (int)threadIdx.x, left = v.last - k0;
-        const uint4 *p = reinterpret_cast<const uint4 *>(v.row + v.head) + k0;
-        const uint32_t to = smem_u32(held + threadIdx.x);
-#pragma unroll
-        for (int j = 0; j < HELD; ++j)
-            if (j * THREADS < left)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + j * THREADS * 16), "l"(p + j * THREADS)
-                             : "memory");
-        at = v.single(threadIdx.x);
+    __device__ __forceinline__ OwnPacks(const RowView<T> &v, bool mine) {
+        at = mine ? v.single(threadIdx.x) : -1;
         one = at >= 0 ? to_f32<T>(v.row[at]) : 0.f;
     }
-    __device__ __forceinline__ void ready() const { asm volatile("cp.async.wait_all;" ::: "memory"); }
+    // f(packs, the first one's number); those from v.last on are not set
+    template <class F>
+    __device__ __forceinline__ void batches(const RowView<T> &v, F f) const {
+        for (int k = v.first + (int)threadIdx.x; k < v.last; k += BATCH * THREADS) {
+            uint4 w[BATCH];
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i)
+                if (i == 0 || k + i * THREADS < v.last) w[i] = v.pack(k + i * THREADS);
+            f(w, k);
+        }
+    }
     // f(pack, its number) for every pack of this thread
     template <class F>
     __device__ __forceinline__ void each(const RowView<T> &v, F f) const {
-        const int k0 = v.first + (int)threadIdx.x, left = v.last - k0;
-        if (left > (HELD - 2) * THREADS) {
+        batches(v, [&](const uint4 (&w)[BATCH], int k) {
 #pragma unroll
-            for (int j = 0; j < HELD - 1; ++j) f(slot[j * THREADS], k0 + j * THREADS);
-            if (left > (HELD - 1) * THREADS) f(slot[(HELD - 1) * THREADS], k0 + (HELD - 1) * THREADS);
-        } else {
-#pragma unroll 1
-            for (int j = 0; j * THREADS < left; ++j) f(slot[j * THREADS], k0 + j * THREADS);
-        }
-        for (int k = k0 + HELD * THREADS; k < v.last; k += THREADS) f(v.pack(k), k);
+            for (int i = 0; i < BATCH; ++i)
+                if (i == 0 || k + i * THREADS < v.last) f(w[i], k + i * THREADS);
+        });
     }
 };
 
@@ -258,20 +247,6 @@ struct PackMax {
             float m = (*this)(w[0]);
 #pragma unroll
             for (int i = 1; i < COUNT; ++i) m = WITH_NAN ? max_nan(m, (*this)(w[i])) : fmaxf(m, (*this)(w[i]));
-            return m;
-        }
-    }
-    // the largest of a thread's packs, -infinity if there are none
-    template <class Row, class View>
-    __device__ __forceinline__ float of_row(const Row &h, const View &v) const {
-        if constexpr (PAIRS) {
-            const T least = round_out<T>(-INFINITY);
-            uint32_t m = (uint32_t)*reinterpret_cast<const unsigned short *>(&least) * 0x10001u;
-            h.each(v, [&](const uint4 &w, int) { m = two(m, words(w)); });
-            return of_words(m);
-        } else {
-            float m = -INFINITY;
-            h.each(v, [&](const uint4 &w, int) { m = WITH_NAN ? max_nan(m, (*this)(w)) : fmaxf(m, (*this)(w)); });
             return m;
         }
     }
@@ -624,17 +599,8 @@ int shares(int rows, int packs, int least) {
     return parts;
 }
 
-// `held`: bytes of shared memory, granted once for each device where they pass what a block has by itself
-template <auto KERNEL, int THREADS, int HELD, class... A>
+template <auto KERNEL, int THREADS, int SHARED, class... A>  // SHARED: bytes of dynamic shared memory
 cudaError_t launch_shared(int rows, int parts, cudaStream_t st, const A &...args) {
-    constexpr int held = HELD;
-    if constexpr (held > 48 * 1024) {
-        static PerDevice granted;
-        if (!granted.get([](int) {
-                return cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, held) == cudaSuccess ? 1 : 0;
-            }))
-            return cudaErrorInvalidConfiguration;
-    }
     if ((long long)rows * parts > 0x7fffffff) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
@@ -646,7 +612,7 @@ cudaError_t launch_shared(int rows, int parts, cudaStream_t st, const A &...args
     cfg.numAttrs = parts > 1 ? 1 : 0;
     cfg.gridDim = dim3((unsigned)(rows * parts));
     cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = held;
+    cfg.dynamicSmemBytes = SHARED;
     cfg.stream = st;
     return cudaLaunchKernelEx(&cfg, KERNEL, args...);
 }
@@ -1113,18 +1079,19 @@ __global__ void __launch_bounds__(256) k_distill_packs(const DistillArgs a) {
     finish_block(a);
 }
 
-constexpr int kRowHeld = 9;
+template <int BATCH>
+constexpr int kRowThreads = BATCH == 2 ? 2048 : 1280;  // threads on an SM
 
-// Longer rows, or longer records: the last warp of a block has the teacher's entries, the others the row. What
-// bounds it is the chain of passes between a row's barriers, with three rows to an SM: 4096 rows of 32768 bf16 in 122
-// us, 4.4 TB/s (two rows to an SM, in registers, every entry by the row's own threads: 157).
-template <class T, int THREADS, bool FAST>
-__global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const DistillArgs a, const int parts) {
+// Longer rows, or longer records: the last warp of a block has the teacher's entries, the others the row, with the sum
+// of exp(z - m) brought up to each new largest logit m as it comes. HBM bounds it, with the latency of a row's steps
+// between barriers, five rows of 32768 to an SM: 4096 of them in bf16 in 99 us, 5.4 TB/s (held in shared memory, three
+// rows to an SM: 121; in registers, two: 157).
+template <class T, int THREADS, int BATCH, bool FAST>
+__global__ void __launch_bounds__(THREADS, kRowThreads<BATCH> / THREADS) k_distill(const DistillArgs a, const int parts) {
     constexpr int P = Pack<T>::P, ROW = THREADS - 32, WARPS = ROW / 32, SLOTS = 2 * kTopMax;
     __shared__ float2 s_stat[WARPS], s_share[8];
     __shared__ float s_p[kTopMax], s_log[kTopMax], s_z[kTopMax], s_old[kTopMax];
     __shared__ int s_any, s_twice, s_last, s_at[kTopMax], s_slot[SLOTS];
-    extern __shared__ uint4 s_held[];
     let_next_launch();
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31, part = parts > 1 ? (int)cluster_ctarank() : 0;
     const long long r = blockIdx.x / parts;
@@ -1133,7 +1100,7 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const Disti
     const Logit logit(a.y);
     T *g = a.g ? static_cast<T *>(a.g) + r * a.ld_g : nullptr;
     const float rw = a.row_weight ? a.row_weight[r] : 1.f / (float)a.y.rows;
-    const HeldRow<T, ROW, kRowHeld> h(v, s_held, !teaches);
+    const OwnPacks<T, ROW, BATCH> h(v, !teaches);
     float m = -INFINITY, s = 0.f;
     if (teaches) {
         // the teacher's softmax, and which of its columns are named twice, beside the others' work on the row
@@ -1180,14 +1147,29 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill(const Disti
         }
     } else {
         // largest logit and sum, over the warp's columns
-        h.ready();
-        if (h.at >= 0) m = logit.of(h.one);
         const PackMax<T, FAST, false> pack_max(logit);
-        m = lanes_max(fmaxf(m, pack_max.of_row(h, v)));
-        const ExpOf<T, FAST> e(logit, m);
-        h.each(v, [&](const uint4 &w, int) { s += e.sum(w); });
-        if (h.at >= 0) s += e.one(h.one);
-        s = lanes_sum(s);
+        const auto raise = [&](float to) {
+            if (to > m) {
+                s *= expf(m - to);
+                m = to;
+            }
+        };
+        h.batches(v, [&](const uint4 (&w)[BATCH], int k) {
+            float most = pack_max(w[0]);
+#pragma unroll
+            for (int i = 1; i < BATCH; ++i)
+                if (k + i * ROW < v.last) most = fmaxf(most, pack_max(w[i]));
+            raise(most);
+            const ExpOf<T, FAST> e(logit, m);
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i)
+                if (i == 0 || k + i * ROW < v.last) s += e.sum(w[i]);
+        });
+        if (h.at >= 0) {
+            raise(logit.of(h.one));
+            s += ExpOf<T, FAST>(logit, m).one(h.one);
+        }
+        join_lanes(m, s);
         if (lane == 0) s_stat[warp] = make_float2(m, s);
     }
     __syncthreads();
@@ -1286,10 +1268,14 @@ __global__ void __launch_bounds__(512) k_distill_sum(const DistillArgs a) {
 template <class T, bool FAST>
 cudaError_t distill_rows(const DistillArgs &a, cudaStream_t st) {
     const int packs = (int)(((long long)a.y.cols * sizeof(T) + 15) / 16), parts = shares(a.y.rows, packs, 512);
+    const int blocks = a.y.rows * parts, each = packs / parts;
+    // short rows have less to load than to wait for, and want more blocks on an SM (4000 rows of 5000 fp32: 44 us, in
+    // fives 52); long ones are read with more loads under way (4096 of 32768 bf16: 99, with the short ones' form 129)
+    if (each <= 1280 && blocks > 5 * 152) return launch_shared<k_distill<T, 256, 2, FAST>, 256, 0>(a.y.rows, parts, st, a, parts);
     // few blocks have more threads each
-    return packs / parts <= 224 * kRowHeld && (a.y.rows * parts >= 152 || packs / parts <= 512)
-               ? launch_shared<k_distill<T, 256, FAST>, 256, 224 * kRowHeld * 16>(a.y.rows, parts, st, a, parts)
-               : launch_shared<k_distill<T, 512, FAST>, 512, 480 * kRowHeld * 16>(a.y.rows, parts, st, a, parts);
+    if (each <= 4096 && (blocks >= 152 || each <= 512))
+        return launch_shared<k_distill<T, 256, 4, FAST>, 256, 0>(a.y.rows, parts, st, a, parts);
+    return launch_shared<k_distill<T, 512, 4, FAST>, 512, 0>(a.y.rows, parts, st, a, parts);
 }
 
 // blocks that count their rows: as many as two to an SM. More have the losses added up by a launch of their own, since
