@@ -486,12 +486,12 @@ __global__ void __launch_bounds__(256) k_top_small(const LogitArgs a, const int 
         }
 }
 
-// Rows of up to 32 E columns and K <= 64: a warp to a row, whose keys stay in registers. The least of the lanes' largest
-// (of their two largest, in two groups, for K > 32) is a bound with K logits or more at or above it; halving the
+// Rows of up to 32 E columns and K <= 128: a warp to a row, whose keys stay in registers. The least of the lanes' largest
+// (in two groups of a lane's columns for K > 32, in four for K > 64) is a bound with K logits or more at or above it; halving the
 // interval from there to the row's largest narrows them to a list that is put in order by counting. Where equal logits
 // keep the list long, their first columns are taken. Instructions bound it: 10000 rows of 1000 fp32, K = 10, 18 us, 2.2
 // TB/s (in blocks 46).
-constexpr int kTopWarp = 64;
+constexpr int kTopWarp = 128;
 template <class T, int E>
 __global__ void __launch_bounds__(256) k_top_packs(const LogitArgs a, const int K, float *top, int32_t *index) {
     constexpr int P = Pack<T>::P, N = E / P;
@@ -513,17 +513,20 @@ __global__ void __launch_bounds__(256) k_top_packs(const LogitArgs a, const int 
         key[e] = lane + 32 * (e / P) < v.packs ? key_of(logit.of(Pack<T>::one(raw[e / P], e % P))) : 0u;
     key[E] = at >= 0 ? key_of(logit.of(one)) : 0u;
 
-    uint32_t even = key[E], odd = 0u;
+    uint32_t most_of[4] = {key[E], 0u, 0u, 0u};
 #pragma unroll
-    for (int e = 0; e < E; e += 2) even = max(even, key[e]), odd = max(odd, key[e + 1]);
-    const auto count = [&](uint32_t least) {
+    for (int e = 0; e < E; ++e) most_of[e % 4] = max(most_of[e % 4], key[e]);
+    const uint32_t even = max(most_of[0], most_of[2]), odd = max(most_of[1], most_of[3]);
+    const uint32_t least = K <= 32 ? max(even, odd)
+                                   : K <= 64 ? min(even, odd) : min(min(most_of[0], most_of[1]), min(most_of[2], most_of[3]));
+    const auto count = [&](uint32_t bound) {
         unsigned c = 0;
 #pragma unroll
-        for (int e = 0; e <= E; ++e) c += key[e] >= least;
+        for (int e = 0; e <= E; ++e) c += key[e] >= bound;
         return c;
     };
     const unsigned wanted = (unsigned)K, most = (wanted + 39) & ~31u;
-    uint32_t low = max(1u, __reduce_min_sync(ALL, K <= 32 ? max(even, odd) : min(even, odd)));
+    uint32_t low = max(1u, __reduce_min_sync(ALL, least));
     uint32_t high = __reduce_max_sync(ALL, max(even, odd)) + 1;  // fewer than K from here on
     unsigned n = __reduce_add_sync(ALL, count(low));
     while (n > most && high - low > 1) {
@@ -635,9 +638,10 @@ cudaError_t top_logits(const LogitArgs &a, int K, float *top, int32_t *index, cu
         return cudaGetLastError();
     }
     const int packs = (int)(((long long)a.cols * sizeof(T) + 15) / 16);
-    // few rows of more than 256 columns are faster in blocks (300 fp32, K = 20: 608 rows 4.3 us both ways, 152 rows 4.2
-    // and 3.3, 912 rows 4.7 and 6.8, 10000 rows 12 and 42); of up to 256 they are not
-    if (K <= kTopWarp && packs * Pack<T>::P <= (a.rows > 5 * 152 ? 32 * 32 : 32 * 8)) {
+    // few rows of more than 256 columns, or with more than 64 logits to find, are faster in blocks (300 fp32, K = 20: 608 rows 4.3 us both ways, 152 rows 4.2
+    // and 3.3, 912 rows 4.7 and 6.8, 10000 rows 12 and 42; 200 bf16, K = 100: 152 rows 7.4 and 4.9, 1216 rows 7.5 and 14)
+    const int warp_columns = a.rows > 5 * 152 ? 32 * 32 : K <= 64 ? 32 * 8 : 0;
+    if (K <= kTopWarp && packs * Pack<T>::P <= warp_columns) {
         if (packs * Pack<T>::P <= 32 * 8) k_top_packs<T, 8><<<blocks, 256, 0, st>>>(a, K, top, index);
         else if (packs * Pack<T>::P <= 32 * 16) k_top_packs<T, 16><<<blocks, 256, 0, st>>>(a, K, top, index);
         else k_top_packs<T, 32><<<blocks, 256, 0, st>>>(a, K, top, index);
@@ -884,40 +888,46 @@ struct ExpOf {
     }
 };
 
-// What a warp that has a row to itself knows of the teacher: 64 entries, two a lane.
-constexpr int kWarpEntries = 64, kWarpSlots = 256;
+// What a warp that has a row to itself knows of the teacher: EACH entries a lane.
+template <int EACH>
 struct WarpShared {
-    int at[kWarpEntries], slot[kWarpSlots];
-    float p[kWarpEntries];
+    static constexpr int SLOTS = 128 * EACH;
+    int at[32 * EACH], slot[SLOTS];
+    float p[32 * EACH];
 };
+template <int EACH>
 struct WarpTeacher {
-    Teacher entry[2];
+    Teacher entry[EACH];
     bool any, twice;
     template <class T>
     __device__ __forceinline__ void read(const DistillArgs &a, const Logit &logit, const T *row, const T *g, long long r,
-                                         int lane, WarpShared &s) {
-        const Record<2> record(a, r, lane);
+                                         int lane, WarpShared<EACH> &s) {
+        const Record<EACH> record(a, r, lane);
         any = record.any();
-        float y[2], old[2], m, log_sum;
+        float y[EACH], old[EACH], m, log_sum;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+        for (int e = 0; e < EACH; ++e) {
             y[e] = record.at[e] >= 0 ? to_f32<T>(row[record.at[e]]) : 0.f;
             old[e] = record.at[e] >= 0 && a.accumulate && g ? to_f32<T>(g[record.at[e]]) : 0.f;
         }
         record.softmax(m, log_sum);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+        for (int e = 0; e < EACH; ++e) {
             entry[e] = record.entry(e, m, log_sum, logit, y[e], old[e]);
             s.at[32 * e + lane] = entry[e].at;
             s.p[32 * e + lane] = entry[e].p;
         }
         __syncwarp();
-        twice = named_twice<2, kWarpSlots>(s.at, s.slot, a.K, lane);
+        twice = named_twice<EACH, WarpShared<EACH>::SLOTS>(s.at, s.slot, a.K, lane);
     }
     // the row's loss, in every lane
     __device__ __forceinline__ float loss(float m, float sum, bool done) const {
         const float log_sum = logf(sum);
-        float l = done ? teacher_loss(entry[0], m, log_sum) + teacher_loss(entry[1], m, log_sum) : 0.f;
+        float l = 0.f;
+        if (done) {
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) l += teacher_loss(entry[e], m, log_sum);
+        }
 #pragma unroll
         for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
         return l;
@@ -925,9 +935,9 @@ struct WarpTeacher {
     // the named columns' gradients, once all others have been written
     template <class T>
     __device__ __forceinline__ void write(const DistillArgs &a, T *g, float m, float sum, float coef, int lane,
-                                          const WarpShared &s) const {
+                                          const WarpShared<EACH> &s) const {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+        for (int e = 0; e < EACH; ++e) {
             const Teacher &t = entry[e];
             float mass = t.p;
             if (t.at >= 0 && !t.silent && (!twice || column_mass(s.at, s.p, 32 * e + lane, a.K, mass)))
@@ -962,7 +972,7 @@ __device__ __forceinline__ void finish_block(const DistillArgs &a) {
 // Rows of up to 32 E classes: a warp to a row, E columns a lane.
 template <class T, int E>
 __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
-    __shared__ WarpShared s_warp[8];
+    __shared__ WarpShared<2> s_warp[8];
     let_next_launch();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long r = (long long)blockIdx.x * 8 + warp;
@@ -979,7 +989,7 @@ __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
             silent[i] = true;
             z[i] = c < a.y.cols ? logit.of(to_f32<T>(row[c]), silent[i]) : -INFINITY;
         }
-        WarpTeacher teacher{};
+        WarpTeacher<2> teacher{};
         teacher.read<T>(a, logit, row, g, r, lane, s_warp[warp]);
         float m = -INFINITY, s = 0.f;
 #pragma unroll
@@ -1010,10 +1020,10 @@ __global__ void __launch_bounds__(256) k_distill_small(const DistillArgs a) {
 // Rows of up to 32 N packs: a warp to a row, N packs of 16 bytes a lane, in registers (13319 rows of 698 16-bit
 // classes, 64 entries: 22 us, 1.7 TB/s; when in blocks 133 and with single columns 71, both before the losses had a
 // launch of their own). Instructions bound it: exponentials, the teacher's entries, and sums across lanes.
-template <class T, int N, bool FAST>
+template <class T, int N, int EACH, bool FAST>
 __global__ void __launch_bounds__(256) k_distill_packs(const DistillArgs a) {
     constexpr int P = Pack<T>::P;
-    __shared__ WarpShared s_warp[8];
+    __shared__ WarpShared<EACH> s_warp[8];
     let_next_launch();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long r = (long long)blockIdx.x * 8 + warp;
@@ -1032,8 +1042,8 @@ __global__ void __launch_bounds__(256) k_distill_packs(const DistillArgs a) {
             for (int j = 0; j < N; ++j)
                 if (lane + 32 * j < v.packs) f(raw[j], lane + 32 * j);
         };
-        WarpTeacher teacher{};
-        teacher.read<T>(a, logit, v.row, g, r, lane, s_warp[warp]);
+        WarpTeacher<EACH> teacher{};
+        teacher.template read<T>(a, logit, v.row, g, r, lane, s_warp[warp]);
         const PackMax<T, FAST, false> pack_max(logit);
         float m = at >= 0 ? logit.of(one) : -INFINITY, s = 0.f;
         each([&](const uint4 &w, int) { m = fmaxf(m, pack_max(w)); });
@@ -1073,7 +1083,7 @@ __global__ void __launch_bounds__(256) k_distill_packs(const DistillArgs a) {
                 }
             });
             __syncwarp();
-            if (done) teacher.write<T>(a, g, m, s, coef, lane, s_warp[warp]);
+            if (done) teacher.template write<T>(a, g, m, s, coef, lane, s_warp[warp]);
         }
     }
     finish_block(a);
@@ -1281,18 +1291,23 @@ cudaError_t distill_rows(const DistillArgs &a, cudaStream_t st) {
 // blocks that count their rows: as many as two to an SM. More have the losses added up by a launch of their own, since
 // a block that counts waits for its stores (13319 rows of 698 fp16: 38 us counted, 32 with the launch).
 constexpr int kCounting = 304;
+// up to here, rows with records of more than 64 entries are as fast in blocks or faster (1000 fp32, K = 128: 304 rows 9.5
+// us by warps and 8.5 in blocks, 1216 rows 9.7 and 11.3, 16384 rows 64 and 103)
+constexpr int kFewRows = 608;
 
 template <class T, bool FAST>
 cudaError_t distill_by_size(DistillArgs &a, cudaStream_t st) {
     const int packs = (int)(((long long)a.y.cols * sizeof(T) + 15) / 16);
     const unsigned blocks = ((unsigned)a.y.rows + 7) / 8;
     a.ticket = blocks <= kCounting;
-    if (a.y.cols <= 64 && a.K <= kWarpEntries) {
+    if (a.y.cols <= 64 && a.K <= 64) {
         k_distill_small<T, 2><<<blocks, 256, 0, st>>>(a);
-    } else if (a.K <= kWarpEntries && packs <= 32 * 2) {
-        k_distill_packs<T, 2, FAST><<<blocks, 256, 0, st>>>(a);
-    } else if (a.K <= kWarpEntries && packs <= 32 * 8) {
-        k_distill_packs<T, 8, FAST><<<blocks, 256, 0, st>>>(a);
+    } else if (a.K <= 64 && packs <= 32 * 2) {
+        k_distill_packs<T, 2, 2, FAST><<<blocks, 256, 0, st>>>(a);
+    } else if (a.K <= 64 && packs <= 32 * 8) {
+        k_distill_packs<T, 8, 2, FAST><<<blocks, 256, 0, st>>>(a);
+    } else if (a.K <= 128 && packs <= 32 * 8 && a.y.rows > kFewRows) {
+        k_distill_packs<T, 8, 4, FAST><<<blocks, 256, 0, st>>>(a);
     } else {
         a.ticket = a.y.rows <= kCounting;
         return distill_rows<T, FAST>(a, st);

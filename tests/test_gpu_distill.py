@@ -99,7 +99,7 @@ def test_top_where_the_form_changes(type, C):
         check_top(y, min(C, 50), -50.0, 1.2)
         _, many = padded(800, C, 1 + offset, TYPES[type], offset)
         many.copy_(y.repeat(80, 1))
-        for K, kw in [(1, {}), (24, {}), (min(C, 33), {}), (min(C, 64), {}), (20, dict(factor=-3.0)), (min(C, 50), dict(factor=-50.0, silent=1.2))]:
+        for K, kw in [(1, {}), (24, {}), (min(C, 33), {}), (min(C, 64), {}), (min(C, 65), {}), (min(C, 100), {}), (min(C, 128), {}), (20, dict(factor=-3.0)), (min(C, 50), dict(factor=-50.0, silent=1.2))]:
             for few, all in zip(top(y, K, **kw), top(many, K, **kw)):
                 assert torch.equal(few.repeat(80, 1).view(torch.int32), all.view(torch.int32))
 
@@ -185,6 +185,14 @@ def test_sizes_where_the_form_changes(type, C):
     check(y, v, i, g, type, factor=-0.5)
     y, v, i, g = make(4, C, 64, type, C, times=True)
     check(y, v, i, g, type, factor=-50.0, silent=1.2, weight=2.0)
+
+
+@pytest.mark.parametrize("type,C,K", [("f32", 65, 65), ("bf16", 300, 128), ("f16", 1000, 97), ("f32", 1024, 128)])
+def test_many_rows_of_long_records(type, C, K):
+    y, v, i, g = make(700, C, K, type, seed=C, pad=1, offset=1)
+    check(y, v, i, g, type)
+    i[:, K // 2:] = i[:, :K - K // 2].clone()          # and classes named twice
+    check(y, v, i, g, type)
 
 
 def test_many_rows():

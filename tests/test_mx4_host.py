@@ -134,15 +134,17 @@ def test_short_rows_take_a_warp(lib):
                                 (17, 256, 64, 0, "k_distill_packsIfLi2E"), (17, 257, 64, 0, "k_distill_packsIfLi8E"),
                                 (17, 512, 64, 2, "k_distill_packsI6__halfLi2E"), (17, 2048, 64, 2, "k_distill_packsI6__halfLi8E"),
                                 (17, 1024, 64, 0, "k_distill_packsIfLi8E"), (17, 1025, 64, 0, "k_distillI"), (17, 2049, 64, 1, "k_distillI"),
-                                (17, 10, 65, 0, "k_distillI")]:
+                                (17, 10, 65, 0, "k_distillI"), (608, 1000, 65, 0, "k_distillI"), (609, 1000, 65, 0, "k_distill_packsIfLi8ELi4E"),
+                                (609, 2048, 128, 2, "k_distill_packsI6__halfLi8ELi4E"), (609, 1000, 129, 0, "k_distillI"), (609, 1025, 65, 0, "k_distillI")]:
         before = lib.fake_launches()
         assert distill(lib, R, C, K, type) == OK
-        (got, grid, _, _), = fake_cuda.launches(lib)[before:]
+        got, grid, _, _ = fake_cuda.launches(lib)[before]
         assert name in got and grid == (R if name == "k_distillI" else -(-R // 8))
     for R, C, K, type, name in [(256, 10, 4, 0, "k_top_small"), (9, 33, 5, 0, "k_top_packsIfLi8E"), (9, 256, 64, 1, "k_top_packsI13__nv_bfloat16Li8E"),
                                 (9, 257, 64, 0, "k_top_logits"), (760, 257, 64, 0, "k_top_logits"), (761, 257, 64, 0, "k_top_packsIfLi16E"),
                                 (761, 513, 64, 0, "k_top_packsIfLi32E"), (761, 1024, 64, 2, "k_top_packsI6__halfLi32E"), (761, 1025, 5, 0, "k_top_logits"),
-                                (9, 128, 65, 0, "k_top_small"), (9, 129, 65, 0, "k_top_logits")]:
+                                (9, 128, 65, 0, "k_top_small"), (9, 129, 65, 0, "k_top_logits"),
+                                (761, 129, 65, 0, "k_top_packsIfLi8E"), (761, 1024, 128, 0, "k_top_packsIfLi32E"), (761, 1024, 129, 0, "k_top_logits")]:
         before = lib.fake_launches()
         assert top(lib, R, C, K, type) == OK
         (got, grid, _, _), = fake_cuda.launches(lib)[before:]
