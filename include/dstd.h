@@ -608,7 +608,7 @@ int dstd_top_logits(const void *y, dstd_type type, int R, int C, int64_t ld_y, f
  *  loss  float[2], 8-byte aligned: loss[1] is scratch, zero before the first
  *        call (each call leaves it zero); calls that can overlap need one each.
  *  row_loss [R] out.
- *  g     [R, C] of `type` out, row stride ld_g >= C, not overlapping y; NULL:
+ *  g     [R, C] of `type` out, row stride ld_g >= C, not overlapping y (which is read twice); NULL:
  *        the losses alone. accumulate != 0 adds the gradient to what g holds.
  * Sums are formed in fp32 (over rows with what the additions lost) in a fixed
  * order; each gradient is rounded once. */

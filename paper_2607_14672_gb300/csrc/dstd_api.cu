@@ -2009,7 +2009,7 @@ int dstd_distill_loss(const void *y, dstd_type type, int R, int C, int64_t ld_y,
     if (K < 1 || !top || !index || !loss || !row_loss || !aligned_to(top, 4) || !aligned_to(index, 4) ||
         !aligned_to(loss, 8) || !aligned_to(row_loss, 4) || (row_weight && !aligned_to(row_weight, 4)))
         return DSTD_E_INVALID;
-    if (g && (ld_g < C || !aligned_to(g, type_bytes(type)))) return DSTD_E_INVALID;
+    if (g && (g == y || ld_g < C || !aligned_to(g, type_bytes(type)))) return DSTD_E_INVALID;
     if (!isfinite(teacher_factor) || teacher_factor == 0.0f || !isfinite(weight)) return DSTD_E_INVALID;
     if (K > kTopMax) return DSTD_E_UNSUPPORTED;
     TRY(device_ok());

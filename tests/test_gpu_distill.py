@@ -255,7 +255,7 @@ def test_rows_left_out(C):
     assert (g[:5] == 2).all() and (g[5:] != 2).any(1).all()
 
 
-@pytest.mark.parametrize("C", [10, 1200])
+@pytest.mark.parametrize("C", [10, 1200, 9000, 40000])
 def test_values_that_are_not_finite(C):
     y, v, i, (flat, g) = make(5, C, 3, "f32", 3)
     i[:] = torch.tensor([0, 1, 2])

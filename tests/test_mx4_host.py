@@ -79,7 +79,7 @@ def test_nothing_to_do(lib):
 
 
 def distill(lib, R, C, K, type=0, silent=float("-inf")):
-    return lib.dstd_distill_loss(P, type, R, C, C, F(1.0), F(silent), P, P, K, F(1.0), F(1.0), None, P, P, P, C, 0, None)
+    return lib.dstd_distill_loss(P, type, R, C, C, F(1.0), F(silent), P, P, K, F(1.0), F(1.0), None, P, P, ctypes.c_void_p(1 << 20), C, 0, None)
 
 
 def top(lib, R, C, K, type=0):

@@ -89,7 +89,7 @@ def test_layer_refuses(lib):
 F = ctypes.c_float
 TOPK = dict(y=P, type=0, R=4, C=10, ld=10, factor=F(1.0), silent=F(-math.inf), K=3, top=P, index=P)
 LOSS = dict(y=P, type=0, R=4, C=10, ld=10, factor=F(1.0), silent=F(-math.inf), top=P, index=P, K=3, tf=F(1.0),
-            weight=F(1.0), rw=P, loss=P, rows=P, g=P, ld_g=10, acc=0)
+            weight=F(1.0), rw=P, loss=P, rows=P, g=ctypes.c_void_p(1 << 20), ld_g=10, acc=0)
 COMMON = [dict(y=None), dict(type=3), dict(R=0), dict(C=0), dict(ld=9), dict(y=ODD), dict(factor=F(0.0)),
           dict(factor=F(math.inf)), dict(factor=F(math.nan)), dict(silent=F(math.inf)), dict(silent=F(math.nan)),
           dict(factor=F(-1.0)), dict(K=0), dict(top=None), dict(index=None), dict(top=ODD), dict(index=ODD)]
@@ -101,7 +101,7 @@ def test_top_refuses(lib, bad):
 
 
 @pytest.mark.parametrize("bad", COMMON + [dict(rw=ODD), dict(loss=None), dict(loss=ctypes.c_void_p(260)), dict(rows=None),
-                                          dict(rows=ODD), dict(g=ODD), dict(ld_g=9), dict(tf=F(0.0)), dict(tf=F(math.nan)),
+                                          dict(rows=ODD), dict(g=ODD), dict(g=P), dict(ld_g=9), dict(tf=F(0.0)), dict(tf=F(math.nan)),
                                           dict(weight=F(math.inf))])
 def test_loss_refuses(lib, bad):
     assert lib.dstd_distill_loss(*dict(LOSS, **bad).values(), None) == INVALID
