@@ -610,6 +610,7 @@ int dstd_top_logits(const void *y, dstd_type type, int R, int C, int64_t ld_y, f
  *  row_loss [R] out.
  *  g     [R, C] of `type` out, row stride ld_g >= C, not overlapping y (which is read twice); NULL:
  *        the losses alone. accumulate != 0 adds the gradient to what g holds.
+ * In 16-bit types exponentials below 2^-126 may count as 0.
  * Sums are formed in fp32 (over rows with what the additions lost) in a fixed
  * order; each gradient is rounded once. */
 int dstd_distill_loss(const void *y, dstd_type type, int R, int C, int64_t ld_y, float factor, float silent,
