@@ -160,7 +160,8 @@ struct OwnPacks {
 // columns of the equal ones. Few long rows
 // are shared by the blocks of a cluster, which then count each other's. A row is not held: the few packs with logits at the
 // bound come from L2 once more (held in shared memory, three rows to an SM: 71 us). What bounds it is the latency of
-// those steps, with six rows to an SM: 4096 rows of 32768 bf16, K = 64, in 62 us, 4.3 TB/s.
+// those steps, with six rows to an SM: 4096 rows of 32768 bf16, K = 64, in 58 us, 4.7 TB/s (62 when the threads at the
+// bound read their own packs again).
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t key_of(float z) {
     if (z != z) return 0xfffffffeu;
@@ -184,9 +185,9 @@ struct Two<__half> { using type = __half2; };
 template <>
 struct Two<__nv_bfloat16> { using type = __nv_bfloat162; };
 
-constexpr int kTopBatch = 4;      // packs that a thread loads at once (4 groups: 67 us in place of 62)
-constexpr int kTopGroups = 2;     // of a thread's packs; one with a logit at the bound is read again
-constexpr int kTopThreads = 1536; // on an SM, 40 registers each
+constexpr int kTopGroups = 4;  // of a thread's packs; those of one with a logit at the bound are read again
+template <int BATCH>
+constexpr int kTopThreads = BATCH == 2 ? 2048 : 1536;  // threads on an SM
 constexpr int kFew = 512;  // as many at most are put in order by counting, the square of them; kTopMax * 3 / 2 + 64 fit
 
 __device__ __forceinline__ uint64_t ld_cluster64(uint32_t addr) {
@@ -252,13 +253,13 @@ struct PackMax {
     }
 };
 
-template <class T, int THREADS, bool PAIRS>
-__global__ void __launch_bounds__(THREADS, kTopThreads / THREADS)
+template <class T, int THREADS, int BATCH, bool PAIRS>  // BATCH: packs that a thread loads at once
+__global__ void __launch_bounds__(THREADS, kTopThreads<BATCH> / THREADS)
     k_top_logits(const LogitArgs a, const int parts, const int K, float *top, int32_t *index) {
     constexpr int P = Pack<T>::P;
     __shared__ uint64_t s_cand[kFew], s_best[kTopMax];
-    __shared__ unsigned s_n, s_hits, s_hist[256], s_digit[2], s_warp[THREADS / 32];
-    __shared__ int s_hit[kFew];
+    __shared__ unsigned s_n, s_groups, s_hits, s_hist[256], s_digit[2], s_warp[THREADS / 32];
+    __shared__ int s_group[kFew], s_hit[kFew];
     __shared__ uint4 s_pack[kFew];
     extern __shared__ uint64_t s_all[];
     const int t = threadIdx.x, part = parts > 1 ? (int)cluster_ctarank() : 0;
@@ -266,7 +267,7 @@ __global__ void __launch_bounds__(THREADS, kTopThreads / THREADS)
     const RowView<T> v(a, r, part, parts);
     const Logit logit(a);
     const PackMax<T, PAIRS, true> pack_max(logit);
-    if (t == 0) s_n = s_hits = 0;
+    if (t == 0) s_n = s_groups = s_hits = 0;
     const int single = v.single(t);
     const float one = single >= 0 ? logit.of(to_f32<T>(v.row[single])) : 0.f;
     // every column of the share once, in any order
@@ -282,14 +283,14 @@ __global__ void __launch_bounds__(THREADS, kTopThreads / THREADS)
     // the largest of each group of this thread's packs
     float largest[kTopGroups];
     uint32_t mine = 0, bound = 0;  // 0: below every logit's key
-    constexpr int step = kTopBatch * THREADS;
+    constexpr int step = BATCH * THREADS;
     const int group = step * max(1, (v.last - v.first + kTopGroups * step - 1) / (kTopGroups * step));
 #pragma unroll
     for (int q = 0; q < kTopGroups; ++q) {
         const int from = v.first + t + q * group, to = min(v.last, from - t + group);
         largest[q] = -INFINITY;
         for (int k0 = from; k0 < to; k0 += step)
-            largest[q] = max_nan(largest[q], pack_max.template of_packs<kTopBatch, THREADS>(v, k0));
+            largest[q] = max_nan(largest[q], pack_max.template of_packs<BATCH, THREADS>(v, k0));
     }
     if (single >= 0 || v.first + t < v.last) {
         float m = single >= 0 ? one : -INFINITY;
@@ -302,7 +303,8 @@ __global__ void __launch_bounds__(THREADS, kTopThreads / THREADS)
         const uint32_t trial = bound | (1u << bit);
         if (__syncthreads_count(mine >= trial) >= want) bound = trial;
     }
-    // packs with a logit at the bound (found by their largest one), then their columns, a thread to each
+    // groups with a logit at the bound; then their packs once more, from L2, a thread to each; then the columns of those
+    // with such a logit, a thread to each
     const auto gather = [&](int c, float z) {
         const uint32_t k = key_of(z);
         if (k < bound) return;
@@ -310,28 +312,32 @@ __global__ void __launch_bounds__(THREADS, kTopThreads / THREADS)
         if (at < kFew) s_cand[at] = (uint64_t)k << 32 | (uint32_t)~c;
     };
     if (single >= 0) gather(single, one);
+    const float least = bound ? logit_of_key(bound) : -INFINITY;
     if (mine >= bound) {
-        const float least = bound ? logit_of_key(bound) : -INFINITY;
-        // a group's packs once more, from L2
-        const auto look = [&](int k0) {
-            uint4 w[kTopBatch];
-#pragma unroll
-            for (int i = 0; i < kTopBatch; ++i) w[i] = v.pack(k0 + i * THREADS < v.last ? k0 + i * THREADS : k0);
-#pragma unroll
-            for (int i = 0; i < kTopBatch; ++i) {
-                if (k0 + i * THREADS >= v.last || pack_max(w[i]) < least) continue;
-                const unsigned at = atomicAdd(&s_hits, 1u);
-                if (at < kFew) {
-                    s_hit[at] = k0 + i * THREADS;
-                    s_pack[at] = w[i];
-                }
-            }
-        };
 #pragma unroll
         for (int q = 0; q < kTopGroups; ++q) {
-            if (largest[q] < least) continue;
-            const int from = v.first + t + q * group, to = min(v.last, from - t + group);
-            for (int k0 = from; k0 < to; k0 += step) look(k0);
+            const int from = v.first + t + q * group;
+            if (from >= v.last || largest[q] < least) continue;
+            const unsigned at = atomicAdd(&s_groups, 1u);
+            if (at < kFew) s_group[at] = from;
+        }
+    }
+    __syncthreads();
+    if (s_groups > kFew) {
+        if (t == 0) s_hits = kFew + 1u;
+    } else {
+        const unsigned each_group = group / THREADS, all = s_groups * each_group;
+        for (unsigned i = t; i < all; i += THREADS) {
+            const unsigned q = i / each_group;
+            const int k = s_group[q] + (int)(i - q * each_group) * THREADS;
+            if (k >= v.last) continue;
+            const uint4 w = v.pack(k);
+            if (pack_max(w) < least) continue;
+            const unsigned at = atomicAdd(&s_hits, 1u);
+            if (at < kFew) {
+                s_hit[at] = k;
+                s_pack[at] = w;
+            }
         }
     }
     __syncthreads();
@@ -624,10 +630,13 @@ template <class T, bool PAIRS>
 cudaError_t top_rows(const LogitArgs &a, int K, float *top, int32_t *index, cudaStream_t st) {
     const int packs = (int)(((long long)a.cols * sizeof(T) + 15) / 16), parts = shares(a.rows, packs, 512);
     constexpr int all = 8 * kTopMax * 8;
-    // 256 threads have enough largest ones to bound 128 logits closely (32768 fp32: 99 us with them, 95 with 512)
+    // 256 threads have enough largest ones to bound 128 logits closely (32768 fp32: 95 us with 512 threads, 99 with them);
+    // short rows want more blocks on an SM (16384 rows of 1500 bf16: 71 us, with the long ones' form 87)
+    if (parts == 1 && K <= 128 && packs <= 1280)
+        return launch_shared<k_top_logits<T, 256, 2, PAIRS>, 256, 0>(a.rows, parts, st, a, parts, K, top, index);
     if (parts == 1 && K <= 128 && packs <= 4096)
-        return launch_shared<k_top_logits<T, 256, PAIRS>, 256, 0>(a.rows, parts, st, a, parts, K, top, index);
-    return launch_shared<k_top_logits<T, 512, PAIRS>, 512, all>(a.rows, parts, st, a, parts, K, top, index);
+        return launch_shared<k_top_logits<T, 256, 4, PAIRS>, 256, 0>(a.rows, parts, st, a, parts, K, top, index);
+    return launch_shared<k_top_logits<T, 512, 4, PAIRS>, 512, all>(a.rows, parts, st, a, parts, K, top, index);
 }
 
 template <class T>
