@@ -56,6 +56,21 @@ def test_plans(lib, T, N, K, width, parts, exchanged, out_type):
     assert parts <= -(-blocks // 8) and slots >= 3
 
 
+@pytest.mark.parametrize("T", [1, 16, 17, 40, 100, 1000])
+@pytest.mark.parametrize("N", [1, 128, 500, 2500, 20000])
+def test_no_part_without_columns(lib, T, N):
+    """A block whose share of K is empty would wait for sums that nobody forms; blocks that share K have an SM each."""
+    for K in (1, 32, 33, 256, 257, 512, 513, 1000, 1025, 2000, 2049, 5000, 40000):
+        lib.fake_reset()
+        lib.fake_keep_arg2_of(b"k_mx4_tc")
+        assert product(lib, T, N, K) == OK
+        (name, grid, _, _), = fake_cuda.launches(lib)
+        if "k_mx4_pair" in name:
+            continue
+        parts = struct.unpack("<QiiQiiiiiiii", bytes(lib.fake_arg2(0).contents)[:56])[10]
+        assert 1 <= parts <= -(-K // 256) and (parts == 1 or grid <= 152), (K, parts, grid)
+
+
 def test_the_plans_reach_every_form():
     assert {(w, p) for _, _, _, w, p, _ in PLANS} >= {(16, 1), (16, 2), (16, 4), (16, 8), (32, 1), (64, 1), (64, 2), (64, 4),
                                                       (64, 8), (128, 1), (128, 2), (128, 4), (128, 8), (0, 1)}
