@@ -11,8 +11,10 @@
 namespace dstd {
 namespace {
 
+using tc::cluster_arrive;
 using tc::cluster_ctarank;
 using tc::cluster_sync;
+using tc::cluster_wait;
 using tc::mapa_rank;
 using tc::smem_u32;
 
@@ -1112,6 +1114,7 @@ __global__ void __launch_bounds__(THREADS, kRowThreads<BATCH> / THREADS) k_disti
     __shared__ float s_p[kTopMax], s_log[kTopMax], s_z[kTopMax], s_old[kTopMax];
     __shared__ int s_any, s_twice, s_last, s_at[kTopMax], s_slot[SLOTS];
     let_next_launch();
+    if (parts > 1) cluster_arrive();  // waited for before the first store to another block
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31, part = parts > 1 ? (int)cluster_ctarank() : 0;
     const long long r = blockIdx.x / parts;
     const bool teaches = warp == WARPS;
@@ -1200,6 +1203,8 @@ __global__ void __launch_bounds__(THREADS, kRowThreads<BATCH> / THREADS) k_disti
         join_lanes(m, s);
     }
     if (parts > 1) {
+        __syncwarp();
+        cluster_wait();  // every block of the cluster has started (behind the row's first pass: nothing is left to wait for)
         if (t < parts) {
             const uint32_t to = mapa_rank(smem_u32(s_share + part), (uint32_t)t);
             asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(m), "f"(s) : "memory");
