@@ -7,6 +7,7 @@
 #include "dstd_tc_ptx.cuh"
 
 #include <algorithm>
+#include <cfloat>
 
 namespace dstd {
 namespace {
@@ -36,11 +37,6 @@ __device__ __forceinline__ float2 of_pair(uint64_t p) {
     float2 v;
     asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(p));
     return v;
-}
-__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
 }
 __device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
     uint64_t d;
@@ -217,10 +213,22 @@ struct PackMax {
         return two(two(w.x, w.y), two(w.z, w.w));
     }
     // of both halves of a word from words()
-    __device__ __forceinline__ float of_words(uint32_t u) const {
+    __device__ __forceinline__ float of_words(uint32_t u) const { return unit() * output(u); }
+    static __device__ __forceinline__ float output(uint32_t u) {
         using V = typename Two<T>::type;
         const V m = *reinterpret_cast<const V *>(&u);
-        return fabsf(logit.factor) * to_f32<T>(WITH_NAN ? __hmax_nan(m.x, m.y) : __hmax(m.x, m.y));
+        return to_f32<T>(WITH_NAN ? __hmax_nan(m.x, m.y) : __hmax(m.x, m.y));
+    }
+    // The largest as it is before the factor (PAIRS: outputs, negated for a negative factor; else logits), of a pack and
+    // of one output; unit() times that is the logit.
+    __device__ __forceinline__ float unit() const { return PAIRS ? fabsf(logit.factor) : 1.f; }
+    __device__ __forceinline__ float level(const uint4 &w) const {
+        if constexpr (PAIRS) return output(words(w));
+        else return (*this)(w);
+    }
+    __device__ __forceinline__ float level(float y) const {
+        if constexpr (PAIRS) return flip ? -y : y;
+        else return logit.of(y);
     }
     __device__ __forceinline__ float operator()(const uint4 &w) const {
         if constexpr (PAIRS) {
@@ -751,13 +759,13 @@ __device__ __forceinline__ float teacher_loss(const Teacher &t, float m, float l
     return t.at >= 0 && t.p != 0.f ? t.p * (t.log_p - (t.z - m - log_sum)) : 0.f;
 }
 
-// largest and sum of (m, s) pairs of all lanes
-__device__ __forceinline__ void join_lanes(float &m, float &s) {
+// largest and sum of (m, s) pairs of all lanes; `unit` times m is a logit
+__device__ __forceinline__ void join_lanes(float &m, float &s, float unit) {
     const float own = m;
 #pragma unroll
     for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
     // an infinite m has nothing to rescale: such a sum is 0 or already NaN
-    s = own == m ? s : s * expf(own - m);
+    s = own == m ? s : s * expf((own - m) * unit);
 #pragma unroll
     for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
 }
@@ -849,23 +857,25 @@ __device__ __forceinline__ bool named_twice(const int *at, int *slot, int K, int
     return __any_sync(0xffffffffu, again);
 }
 
-// exp(z - m) of outputs, m the largest logit (nothing but -infinity: every exp is 0 with any finite m, and NaN stays
-// NaN). FAST: 16-bit outputs without a stand-in for silent ones, whose exp is 0 by itself:
-// exp(z - m) = 2^(factor log2(e) y - m log2(e)), one multiply-add and the special-function unit, two at a time
-// (the product's rounding moves it by 2^-24 |z|, far below a 16-bit rounding).
+// exp(z - m) of outputs, m the largest logit, given as PackMax's level (nothing but -infinity: every exp is 0 with any
+// finite m, and NaN stays NaN). FAST: 16-bit outputs without a stand-in for silent ones, whose exp is 0 by itself:
+// with m = factor y*, exp(z - m) = 2^((y - y*) factor log2(e)), on the special-function unit, two at a time. The difference
+// comes first, so that the roundings are of the size of z - m, not of z (y - y* is exact for near ones): the argument
+// is off by 2^-22 |z - m|, and where the difference of finite outputs is infinite the exp is 0 anyway (least_factor).
+constexpr float least_factor = 0x1p-120f, most_factor = 1e30f;
 template <class T, bool FAST>
 struct ExpOf {
     static constexpr int P = Pack<T>::P;
     Logit logit;
-    float base, scale;
-    __device__ __forceinline__ ExpOf(const Logit &l, float m)
-        : logit(l), base(m == -INFINITY ? 0.f : m), scale(l.factor * kLog2e) {}
+    float minus, scale;  // what is added to a logit (FAST: to an output) before the factor
+    __device__ __forceinline__ ExpOf(const Logit &l, float level)
+        : logit(l), minus(fmaxf(level, -FLT_MAX) * (FAST && l.factor < 0.f ? 1.f : -1.f)), scale(l.factor * kLog2e) {}
     __device__ __forceinline__ float one(float y) const {
-        if constexpr (FAST) return exp2_fast(fmaf(y, scale, -base * kLog2e));
-        else return expf(logit.of(y) - base);
+        if constexpr (FAST) return exp2_fast((y + minus) * scale);
+        else return expf(logit.of(y) + minus);
     }
     __device__ __forceinline__ uint64_t two(uint32_t w) const {
-        const float2 x = of_pair(fma_pair(word_pair<T>(w), pair_of(scale, scale), pair_of(-base * kLog2e, -base * kLog2e)));
+        const float2 x = of_pair(mul_pair(add_pair(word_pair<T>(w), pair_of(minus, minus)), pair_of(scale, scale)));
         return pair_of(exp2_fast(x.x), exp2_fast(x.y));
     }
     __device__ __forceinline__ float sum(const uint4 &w) const {
@@ -884,7 +894,7 @@ struct ExpOf {
         if constexpr (FAST) return one(y) * over;
         bool silent;
         const float z = logit.of(y, silent);
-        return silent ? 0.f : expf(z - base) * over;
+        return silent ? 0.f : expf(z + minus) * over;
     }
     __device__ __forceinline__ void grads(const uint4 &w, float over, T (&out)[P]) const {
         if constexpr (FAST) {
@@ -966,6 +976,13 @@ __device__ __forceinline__ float lanes_sum(float v) {
 #pragma unroll
     for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
     return v;
+}
+// From the level of a row's largest to its logit. An infinite one has no softmax: its sum is NaN, also where the output
+// is finite and only factor y is infinite.
+__device__ __forceinline__ float largest_logit(float level, float unit, float &sum) {
+    const float m = level * unit;
+    if (m == INFINITY) sum = __uint_as_float(0x7fffffffu);
+    return m;
 }
 // a row without logits has no softmax: it is left out (a NaN counts as a logit)
 __device__ __forceinline__ bool has_logits(float m, float sum) { return !(m == -INFINITY && !(sum != sum)); }
@@ -1056,13 +1073,14 @@ __global__ void __launch_bounds__(256) k_distill_packs(const DistillArgs a) {
         WarpTeacher<EACH> teacher{};
         teacher.template read<T>(a, logit, v.row, g, r, lane, s_warp[warp]);
         const PackMax<T, FAST, false> pack_max(logit);
-        float m = at >= 0 ? logit.of(one) : -INFINITY, s = 0.f;
-        each([&](const uint4 &w, int) { m = fmaxf(m, pack_max(w)); });
-        m = lanes_max(m);
-        const ExpOf<T, FAST> e(logit, m);
+        float level = at >= 0 ? pack_max.level(one) : -INFINITY, s = 0.f;
+        each([&](const uint4 &w, int) { level = fmaxf(level, pack_max.level(w)); });
+        level = lanes_max(level);
+        const ExpOf<T, FAST> e(logit, level);
         each([&](const uint4 &w, int) { s += e.sum(w); });
         if (at >= 0) s += e.one(one);
         s = lanes_sum(s);
+        const float m = largest_logit(level, pack_max.unit(), s);
         const bool done = teacher.any && rw != 0.f && has_logits(m, s);
         const float loss = teacher.loss(m, s, done);
         if (lane == 0) a.row_loss[r] = loss;
@@ -1105,14 +1123,17 @@ constexpr int kRowThreads = BATCH == 2 ? 2048 : 1280;  // threads on an SM
 
 // Longer rows, or longer records: the last warp of a block has the teacher's entries, the others the row, with the sum
 // of exp(z - m) brought up to each new largest logit m as it comes. HBM bounds it, with the latency of a row's steps
-// between barriers, five rows of 32768 to an SM: 4096 of them in bf16 in 99 us, 5.4 TB/s (held in shared memory, three
-// rows to an SM: 121; in registers, two: 157).
-template <class T, int THREADS, int BATCH, bool FAST>
-__global__ void __launch_bounds__(THREADS, kRowThreads<BATCH> / THREADS) k_distill(const DistillArgs a, const int parts) {
+// between barriers, five rows of 32768 to an SM: 4096 of them in bf16 in 97 us, 5.5 TB/s (held in shared memory, three
+// rows to an SM: 121; in registers, two: 157). Without CLUSTER a block has a row to itself and knows it: fewer registers
+// to keep (16384 rows of 3000 bf16: 73 us, with the general form 89).
+template <class T, int THREADS, int BATCH, bool FAST, bool CLUSTER>
+__global__ void __launch_bounds__(THREADS, kRowThreads<BATCH> / THREADS)
+    k_distill(const DistillArgs a, const int shared_by) {
     constexpr int P = Pack<T>::P, ROW = THREADS - 32, WARPS = ROW / 32, SLOTS = 2 * kTopMax;
     __shared__ float2 s_stat[WARPS], s_share[8];
     __shared__ float s_p[kTopMax], s_log[kTopMax], s_z[kTopMax], s_old[kTopMax];
     __shared__ int s_any, s_twice, s_last, s_at[kTopMax], s_slot[SLOTS];
+    const int parts = CLUSTER ? shared_by : 1;
     let_next_launch();
     if (parts > 1) cluster_arrive();  // waited for before the first store to another block
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31, part = parts > 1 ? (int)cluster_ctarank() : 0;
@@ -1123,7 +1144,8 @@ __global__ void __launch_bounds__(THREADS, kRowThreads<BATCH> / THREADS) k_disti
     T *g = a.g ? static_cast<T *>(a.g) + r * a.ld_g : nullptr;
     const float rw = a.row_weight ? a.row_weight[r] : 1.f / (float)a.y.rows;
     const OwnPacks<T, ROW, BATCH> h(v, !teaches);
-    float m = -INFINITY, s = 0.f;
+    const PackMax<T, FAST, false> pack_max(logit);
+    float level = -INFINITY, s = 0.f;
     if (teaches) {
         // the teacher's softmax, and which of its columns are named twice, beside the others' work on the row
         float tm = -INFINITY;
@@ -1168,57 +1190,57 @@ __global__ void __launch_bounds__(THREADS, kRowThreads<BATCH> / THREADS) k_disti
             s_twice = again;
         }
     } else {
-        // largest logit and sum, over the warp's columns
-        const PackMax<T, FAST, false> pack_max(logit);
+        // largest and sum, over the warp's columns
         const auto raise = [&](float to) {
-            if (to > m) {
-                s *= expf(m - to);
-                m = to;
+            if (to > level) {
+                s *= expf((level - to) * pack_max.unit());
+                level = to;
             }
         };
         h.batches(v, [&](const uint4 (&w)[BATCH], int k) {
-            float most = pack_max(w[0]);
+            float most = pack_max.level(w[0]);
 #pragma unroll
             for (int i = 1; i < BATCH; ++i)
-                if (k + i * ROW < v.last) most = fmaxf(most, pack_max(w[i]));
+                if (k + i * ROW < v.last) most = fmaxf(most, pack_max.level(w[i]));
             raise(most);
-            const ExpOf<T, FAST> e(logit, m);
+            const ExpOf<T, FAST> e(logit, level);
 #pragma unroll
             for (int i = 0; i < BATCH; ++i)
                 if (i == 0 || k + i * ROW < v.last) s += e.sum(w[i]);
         });
         if (h.at >= 0) {
-            raise(logit.of(h.one));
-            s += ExpOf<T, FAST>(logit, m).one(h.one);
+            raise(pack_max.level(h.one));
+            s += ExpOf<T, FAST>(logit, level).one(h.one);
         }
-        join_lanes(m, s);
-        if (lane == 0) s_stat[warp] = make_float2(m, s);
+        join_lanes(level, s, pack_max.unit());
+        if (lane == 0) s_stat[warp] = make_float2(level, s);
     }
     __syncthreads();
     const bool any = s_any != 0;
     {
         const float2 w = lane < WARPS ? s_stat[lane] : make_float2(-INFINITY, 0.f);
-        m = w.x;
+        level = w.x;
         s = w.y;
-        join_lanes(m, s);
+        join_lanes(level, s, pack_max.unit());
     }
     if (parts > 1) {
         __syncwarp();
         cluster_wait();  // every block of the cluster has started (behind the row's first pass: nothing is left to wait for)
         if (t < parts) {
             const uint32_t to = mapa_rank(smem_u32(s_share + part), (uint32_t)t);
-            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(m), "f"(s) : "memory");
+            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(level), "f"(s) : "memory");
         }
         __syncwarp();
         cluster_sync();
         const float2 w = lane < parts ? s_share[lane] : make_float2(-INFINITY, 0.f);
-        m = w.x;
+        level = w.x;
         s = w.y;
-        join_lanes(m, s);
+        join_lanes(level, s, pack_max.unit());
     }
+    const float m = largest_logit(level, pack_max.unit(), s);
     const bool done = any && rw != 0.f && has_logits(m, s);
     const float coef = a.weight * rw * logit.factor, over = done ? coef / s : 0.f;
-    const ExpOf<T, FAST> e(logit, m);
+    const ExpOf<T, FAST> e(logit, level);
     // each pack of the share to g: made(pack, its place) gives the P gradients
     const auto write = [&](auto made) {
         T *dst = g + v.head;
@@ -1293,13 +1315,17 @@ template <class T, bool FAST>
 cudaError_t distill_rows(const DistillArgs &a, cudaStream_t st) {
     const int packs = (int)(((long long)a.y.cols * sizeof(T) + 15) / 16), parts = shares(a.y.rows, packs, 512);
     const int blocks = a.y.rows * parts, each = packs / parts;
-    // short rows have less to load than to wait for, and want more blocks on an SM (4000 rows of 5000 fp32: 44 us, in
-    // fives 52); long ones are read with more loads under way (4096 of 32768 bf16: 99, with the short ones' form 129)
-    if (each <= 1280 && blocks > 5 * 152) return launch_shared<k_distill<T, 256, 2, FAST>, 256, 0>(a.y.rows, parts, st, a, parts);
+    // short rows have less to load than to wait for, and want more blocks on an SM (4000 rows of 5000 fp32: 40 us; by a
+    // form that could share rows 42, with six of its blocks to an SM 44, with five 52); long ones are read with more loads
+    // under way (4096 of 32768 bf16: 97, with the short ones' form 129)
+    if (each <= 1280 && blocks > 5 * 152)  // (rows are not shared there)
+        return launch_shared<k_distill<T, 256, 2, FAST, false>, 256, 0>(a.y.rows, 1, st, a, 1);
     // few blocks have more threads each
-    if (each <= 4096 && (blocks >= 152 || each <= 512))
-        return launch_shared<k_distill<T, 256, 4, FAST>, 256, 0>(a.y.rows, parts, st, a, parts);
-    return launch_shared<k_distill<T, 512, 4, FAST>, 512, 0>(a.y.rows, parts, st, a, parts);
+    if (each <= 4096 && (blocks >= 152 || each <= 512)) {
+        if (parts == 1) return launch_shared<k_distill<T, 256, 4, FAST, false>, 256, 0>(a.y.rows, 1, st, a, 1);
+        return launch_shared<k_distill<T, 256, 4, FAST, true>, 256, 0>(a.y.rows, parts, st, a, parts);
+    }
+    return launch_shared<k_distill<T, 512, 4, FAST, true>, 512, 0>(a.y.rows, parts, st, a, parts);
 }
 
 // blocks that count their rows: as many as two to an SM. More have the losses added up by a launch of their own, since
@@ -1331,7 +1357,8 @@ cudaError_t distill_by_size(DistillArgs &a, cudaStream_t st) {
 
 template <class T>
 cudaError_t distill(DistillArgs a, int &launches, cudaStream_t st) {
-    const bool fast = sizeof(T) == 2 && a.y.factor * a.y.silent == -INFINITY && fabsf(a.y.factor) < 1e30f;
+    const bool fast = sizeof(T) == 2 && a.y.factor * a.y.silent == -INFINITY && fabsf(a.y.factor) < most_factor &&
+                      fabsf(a.y.factor) >= least_factor;
     const cudaError_t e = fast ? distill_by_size<T, sizeof(T) == 2>(a, st) : distill_by_size<T, false>(a, st);
     launches = a.ticket ? 1 : 2;
     return e != cudaSuccess || a.ticket ? e : launch_dependent(k_distill_sum, 1, 512, st, a);

@@ -321,3 +321,96 @@ def test_same_bits_and_a_graph():
     eager = torch.zeros(2, device="cuda")
     dstd.distill_loss(y, v, i, eager, rows, g)
     assert torch.equal(eager, seen[0][0])
+
+
+# -- logits far from 0 ---------------------------------------------------------
+def check_near(y, v, i, g, type, factor, w):
+    """Factors of a power of two, so that logits and near differences are exact in fp32: nothing may grow with |z|, only
+    with the distance from the row's largest. In units of 2^-24: an exponential's argument has up to four roundings of its
+    size (the difference, log2(e), two products), the exponential itself 4 (2^-22); a sum adds its terms' own, a rescaling
+    (one exponential and a product) and an addition for each batch of a thread's columns, and 16 for the trees and
+    the division; a log and the sums of the loss 8. exp below 2^-126 may count as 0."""
+    R, C = y.shape
+    K = v.shape[1]
+    loss, rows = torch.zeros(2, device="cuda"), torch.full((R,), 9.0, device="cuda")
+    dstd.distill_loss(y, v, i, loss, rows, g, factor, row_weight=w)
+    index, zt, wh = i.cpu().numpy(), host(v), host(w)
+    want, want_rows, want_g = oracle.distill(host(y), zt, index, factor, row_weight=wh)
+    z = factor * host(y)
+    gap = z.max(1, keepdims=True) - z
+    e = np.exp(-gap)
+    q = e / e.sum(1, keepdims=True)
+    far = np.where(q > 0, gap, 0.0)
+    sums = (q * 4 * far).sum(1) + 24 + 3 * C / 256
+    gt = zt.max(1, keepdims=True) - zt
+    p = np.exp(-gt) / np.exp(-gt).sum(1, keepdims=True)
+    of_p = 4 * gt + (p * 4 * gt).sum(1, keepdims=True) + 24 + K / 16
+    mass, of_mass = np.zeros((R, C)), np.zeros((R, C))
+    at = np.arange(R)[:, None].repeat(K, 1)
+    np.add.at(mass, (at, index), p)
+    np.add.at(of_mass, (at, index), p * (of_p + K / 16))
+    u = 2.0 ** -24
+    allow = HALF[type] * np.abs(want_g) + u * np.abs(wh * factor)[:, None] * (q * (4 * far + sums[:, None] + 8) + of_mass + 4 * mass)
+    off = np.abs(host(g) - want_g)
+    assert (off <= allow + TINY[type]).all(), (off / (allow + TINY[type])).max()
+    gap_k = np.take_along_axis(gap, index, 1)
+    log_s = np.log(e.sum(1))
+    apart = np.abs(np.log(p) + gap_k + log_s[:, None])
+    allow = u * ((p * ((of_p + 8) * (apart + 1) + 4 * (gt + gap_k))).sum(1) + sums + 8 * (log_s + 1) + 8 * np.abs(want_rows))
+    off = np.abs(host(rows) - want_rows)
+    assert (off <= allow).all(), (off / allow).max()
+    whole = (wh * (allow + 4 * u * np.abs(want_rows))).sum()
+    assert abs(loss[0].item() - want) <= whole and loss[1].item() == 0
+
+
+# sizes of every form: a warp to a row (single columns, packs), a block, blocks of a cluster, many rows of a block each
+FORMS = [(6, 10, 4), (6, 300, 9), (6, 1000, 64), (6, 3000, 7), (6, 9000, 100), (6, 40000, 30), (650, 1000, 100), (800, 3000, 5)]
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("R,C,K", FORMS)
+@pytest.mark.parametrize("factor", [1.0, -0.5])
+def test_logits_far_from_zero(type, R, C, K, factor):
+    """A common offset changes nothing but the inputs' own rounding."""
+    for offset in (50.0, -1000.0, 30000.0):
+        y, v, i, (_, g) = make(R, C, K, type, seed=C, pad=1)
+        y.copy_(y.float() + offset)
+        check_near(y, v, i.clamp_(min=0), g, type, factor, torch.full((R,), 1.0 / R, device="cuda"))
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("R,C,K", FORMS)
+@pytest.mark.parametrize("factor", [1.0, -1.0])
+def test_logits_at_the_types_ends(type, R, C, K, factor):
+    """Classes masked with the type's lowest value: all of a row's, all but one; rows at the largest value and near it."""
+    y, v, i, (_, g) = make(R, C, K, type, seed=C + 1, pad=1)
+    i.clamp_(min=0)
+    end = torch.finfo(TYPES[type]).max
+    z = y.float() * factor
+    z[0] = -end
+    z[1] = -end
+    z[1, C // 2] = 1.0
+    i[1] = C // 2
+    z[2] = end
+    z[3] = end * 0.75
+    z[3, C - 1] = end * 0.5
+    i[3] = 0
+    z[4, 1::2] = -end
+    i[4] = torch.arange(K) % ((C + 1) // 2) * 2
+    z[5, :] = end
+    z[5, ::3] = end * (1 - 2.0 ** -6)
+    i[5] = torch.arange(K) % (C // 3) * 3 + 1
+    y.copy_(z * factor)
+    check_near(y, v, i, g, type, factor, torch.full((R,), 1.0 / R, device="cuda"))
+
+
+@pytest.mark.parametrize("type,factor", [("bf16", 2.0 ** -126), ("bf16", 2.0 ** -119), ("f16", 2.0 ** -15)])
+@pytest.mark.parametrize("C", [300, 9000])
+def test_smallest_factors(type, factor, C):
+    """Outputs at both ends of the type whose logits lie near each other, for their factor is small."""
+    y, v, i, (_, g) = make(5, C, 6, type, seed=C)
+    i.clamp_(min=0)
+    end = torch.finfo(TYPES[type]).max
+    y.copy_((y.float() * 0.2).clamp(-1, 1) * end)
+    y[0, 0], y[0, 1] = end, -end
+    check_near(y, v, i, g, type, factor, torch.ones(5, device="cuda"))
