@@ -891,21 +891,23 @@ struct ExpOf {
     }
     // over exp(z - m), 0 where silent
     __device__ __forceinline__ float grad(float y, float over) const {
-        if constexpr (FAST) return one(y) * over;
         bool silent;
         const float z = logit.of(y, silent);
-        return silent ? 0.f : expf(z + minus) * over;
+        return silent ? 0.f : (FAST ? one(y) : expf(z + minus)) * over;
     }
     __device__ __forceinline__ void grads(const uint4 &w, float over, T (&out)[P]) const {
+        // a silent one's exp is 0, and so is its product, unless `over` is infinite or NaN
         if constexpr (FAST) {
-            const uint64_t c = pair_of(over, over);
-            *reinterpret_cast<uint4 *>(out) =
-                make_uint4(pair_word<T>(mul_pair(two(w.x), c)), pair_word<T>(mul_pair(two(w.y), c)),
-                           pair_word<T>(mul_pair(two(w.z), c)), pair_word<T>(mul_pair(two(w.w), c)));
-        } else {
-#pragma unroll
-            for (int i = 0; i < P; ++i) out[i] = round_out<T>(grad(Pack<T>::one(w, i), over));
+            if (isfinite(over)) {
+                const uint64_t c = pair_of(over, over);
+                *reinterpret_cast<uint4 *>(out) =
+                    make_uint4(pair_word<T>(mul_pair(two(w.x), c)), pair_word<T>(mul_pair(two(w.y), c)),
+                               pair_word<T>(mul_pair(two(w.z), c)), pair_word<T>(mul_pair(two(w.w), c)));
+                return;
+            }
         }
+#pragma unroll
+        for (int i = 0; i < P; ++i) out[i] = round_out<T>(grad(Pack<T>::one(w, i), over));
     }
 };
 
@@ -1125,7 +1127,7 @@ constexpr int kRowThreads = BATCH == 2 ? 2048 : 1280;  // threads on an SM
 // of exp(z - m) brought up to each new largest logit m as it comes. HBM bounds it, with the latency of a row's steps
 // between barriers, five rows of 32768 to an SM: 4096 of them in bf16 in 97 us, 5.5 TB/s (held in shared memory, three
 // rows to an SM: 121; in registers, two: 157). Without CLUSTER a block has a row to itself and knows it: fewer registers
-// to keep (16384 rows of 3000 bf16: 73 us, with the general form 89).
+// to keep (16384 rows of 3000 bf16: 77 us, with the form for clusters 89).
 template <class T, int THREADS, int BATCH, bool FAST, bool CLUSTER>
 __global__ void __launch_bounds__(THREADS, kRowThreads<BATCH> / THREADS)
     k_distill(const DistillArgs a, const int shared_by) {

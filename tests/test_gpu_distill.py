@@ -414,3 +414,62 @@ def test_smallest_factors(type, factor, C):
     y.copy_((y.float() * 0.2).clamp(-1, 1) * end)
     y[0, 0], y[0, 1] = end, -end
     check_near(y, v, i, g, type, factor, torch.ones(5, device="cuda"))
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("C", [10, 300, 1200, 9000, 40000])
+@pytest.mark.parametrize("factor", [1.0, -1.0])
+def test_masked_classes_of_rows_that_are_not_finite(type, C, factor):
+    """A masked class passes no gradient, whatever else its row holds: 0 written, nothing added."""
+    y, v, i, (_, g) = make(6, C, 3, type, 3, pad=1)
+    i[:] = torch.tensor([0, 1, 2])
+    masked = torch.zeros(6, C, dtype=torch.bool, device="cuda")
+    masked[:, 5::3] = True
+    masked[5] = True
+    y[masked] = -float("inf") * factor
+    y[0, 3], y[1, 3], v[2, 1] = float("nan"), float("inf") * factor, float("nan")
+    y[5, 4] = float("nan")                   # nothing but masked classes and a NaN
+    w = torch.full((6,), 0.25, device="cuda")
+    w[3] = float("nan")
+    loss, rows = torch.zeros(2, device="cuda"), torch.zeros(6, device="cuda")
+    for accumulate in (False, True):
+        g.fill_(3.0)
+        dstd.distill_loss(y, v, i, loss, rows, g, factor, row_weight=w, accumulate=accumulate)
+        assert (g[masked] == (3.0 if accumulate else 0.0))[~torch.isnan(y[masked])].all()
+        for r in (0, 1, 3):
+            assert torch.isnan(g[r][~masked[r]]).all()
+        assert torch.isnan(g[5, 4]) and torch.isnan(g[2, :3]).all() and torch.isfinite(g[2, 3:]).all()
+        assert torch.isfinite(g[4]).all()
+        assert torch.isnan(rows[[0, 1, 2, 5]]).all() and torch.isfinite(rows[[3, 4]]).all() and torch.isnan(loss[0])
+
+
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+@pytest.mark.parametrize("C", [10, 300, 1200, 9000, 40000])
+def test_rows_left_out_in_16_bits(type, C):
+    """As in fp32: no teacher, classes out of range, no logits, no weight, masked classes named."""
+    y, v, i, (flat, g) = make(8, C, 4, type, 3)
+    i[0] = -1
+    i[1] = torch.tensor([C, C + 5, -7, 2 ** 31 - 1])
+    v[2] = -float("inf")
+    y[3] = -float("inf")
+    w = torch.linspace(0.5, 1, 8, device="cuda")
+    w[4] = 0
+    y[5, 1::2] = -float("inf")
+    i[5] = torch.tensor([0, 2, 2, -1])
+    check(y, v, i, (flat, g), type, row_weight=w)
+    assert (g[:5] == 0).all()
+    g.fill_(2.0)
+    dstd.distill_loss(y, v, i, torch.zeros(2, device="cuda"), torch.empty(8, device="cuda"), g, row_weight=w, accumulate=True)
+    assert (g[:5] == 2).all() and (g[5:] != 2).any(1).all()
+
+
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+@pytest.mark.parametrize("C,K", [(10, 40), (300, 64), (600, 200), (9000, 256), (40000, 100)])
+def test_the_same_class_several_times_in_16_bits(type, C, K):
+    y, v, i, g = make(5, C, K, type, 7)
+    i[:, :] = i % 7
+    i[2] = 4
+    y[3, 1::3] = -float("inf")
+    i[3] = i[3] // 3 * 3
+    check(y, v, i, g, type)
+    check(y, v, i, g, type, accumulate=True)
