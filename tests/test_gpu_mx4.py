@@ -322,3 +322,50 @@ def test_layer_forward(B, N_in, N_out, M, taus):
         dstd.dense_fwd_mx4(t[i:i + 1].clone(), wq, ws, p, t1, s1, pen3, one)
         fine = torch.isfinite(t1[0]) & torch.isfinite(t_out[i])
         assert ((t1[0] - t_out[i])[fine].abs() <= 1e-4 * 1.2).all()
+
+
+@pytest.mark.parametrize("B,N_in,N_out,M", [(1, 1, 1, 1), (3, 33, 5, 1), (2, 50, 70, 10), (5, 127, 33, 100), (4, 160, 129, 128),
+                                            (16, 784, 300, 32), (3, 515, 40, 128), (129, 130, 600, 8)])
+def test_layer_forward_step_by_step(B, N_in, N_out, M):
+    """What the layer leaves in its workspace: the grid weights' codes and scales are those of quantising the rows that
+    the binning gives (zero rows from M up to the padded M), w^ is their product with the weights, and the spikes are
+    the scan's of that w^."""
+    gen = torch.Generator(device="cuda").manual_seed(M + N_in)
+    # weights of 12 in all, nine tenths of them spread over 1.6 s, raise v to 12 0.9 / 1.6 tau_v tau_I = 0.84 at most:
+    # with v_th = 0.3 most neurons fire
+    p = layer(M, v_th=0.3)
+    t = torch.rand(B, N_in, generator=gen, device="cuda") * 1.6 - 0.3        # before the first and behind the last grid point too
+    t[torch.rand(B, N_in, generator=gen, device="cuda") < 0.1] = float("inf")
+    t[0, :: 7] = -0.3 / M + 1.2 / M * (M // 2)                              # on a grid point, or next to it
+    W = torch.randn(N_out, N_in, generator=gen, device="cuda") / N_in ** 0.5 + 12.0 / N_in
+    wq, ws, _ = quantized(W)
+    t_out = torch.empty(B, N_out, device="cuda")
+    saved = torch.empty(dstd.dense_saved_bytes(B, N_out), dtype=torch.uint8, device="cuda")
+    work = torch.full((dstd.dense_mx4_workspace_bytes(B, N_in, N_out, p),), 0xFF, dtype=torch.uint8, device="cuda")
+    dstd.dense_fwd_mx4(t, wq, ws, p, t_out, saved, None, work)
+    assert dstd.device_status() == 0
+    Mp = 8
+    while Mp < M:
+        Mp *= 2
+    T, row, up = B * Mp, dstd.mx4_row_bytes(N_in), lambda n: -(-n // 256) * 256
+    scale_at = up(4 * N_out)                     # row sums, scales, codes, w^, each from a multiple of 256
+    code_at = up(scale_at + dstd.mx4_scale_bytes(T, N_in))
+    what_at = up(code_at + T * row)
+    assert what_at + 4 * T * N_out == work.numel()
+    s = torch.empty(B, M, N_in, device="cuda")
+    dstd.binning(t, p, s)
+    rows = torch.zeros(B, Mp, N_in, device="cuda")
+    rows[:, :M] = s
+    want_q, want_s, _ = quantized(rows.view(T, N_in))
+    assert torch.equal(work[code_at:code_at + T * row].view(T, row), want_q)
+    n = mx4.blocks_of(N_in)
+    at = torch.from_numpy(mx4.scale_place(np.arange(T)[:, None], np.arange(-(-n // 4) * 4)[None, :], N_in)).cuda()
+    assert torch.equal(work[scale_at:code_at][at], want_s[at])
+    what = work[what_at:].view(torch.float32).view(N_out, B, Mp)
+    a, b = decoded(want_q, want_s, N_in), decoded(wq, ws, N_in)
+    assert (np.abs(host(what.reshape(N_out, T).t()) - a @ b.T) <= bound(a, b, "f32")).all()
+    want = torch.empty(B, N_out, device="cuda")
+    dstd.scan_solve(what[:, :, :M].permute(1, 0, 2).contiguous(), p, None, want, None, None)
+    if M % 4 == 0:                               # the scan's same form
+        assert torch.equal(t_out, want)
+    assert N_in == 1 or torch.isfinite(t_out).any()
