@@ -96,10 +96,12 @@ class Taught:
         """The teacher's record for the present batch (rows of classes -1: no teacher)."""
         if self.record is None:
             raise RuntimeError("set_teacher: call learn_from first")
-        for mine, given in zip(self.record, (torch.as_tensor(top), torch.as_tensor(index))):
-            if given.shape != mine.shape:
-                raise ValueError(f"set_teacher: logits and classes {tuple(mine.shape)}, not {tuple(given.shape)}")
-            mine.copy_(given, non_blocking=True)
+        given = torch.as_tensor(top), torch.as_tensor(index)
+        for mine, x in zip(self.record, given):
+            if x.shape != mine.shape:
+                raise ValueError(f"set_teacher: logits and classes {tuple(mine.shape)}, not {tuple(x.shape)}")
+        for mine, x in zip(self.record, given):
+            mine.copy_(x, non_blocking=True)
 
     def has_label_loss(self):
         return self.record is None or self.from_labels

@@ -87,3 +87,14 @@ def test_what_a_step_calls(monkeypatch, mode, labels):
     assert names.index("distill_loss") < first
     if labels:
         assert max(i for i, x in enumerate(names) if x in ("ce_loss", "dense_fwd_ce")) < names.index("distill_loss")
+
+
+def test_a_record_is_taken_whole_or_not_at_all():
+    n = network(mode="x3")
+    n.learn_from(3)
+    logits, classes = torch.ones(2, 3), torch.ones(2, 3, dtype=torch.int32)
+    n.set_teacher(logits, classes)
+    for bad in ((logits + 1, classes[:, :2]), (logits[:1] + 1, classes)):
+        with pytest.raises(ValueError):
+            n.set_teacher(*bad)
+        assert torch.equal(n.record[0], logits) and torch.equal(n.record[1], classes)
