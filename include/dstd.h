@@ -538,10 +538,13 @@ int dstd_adamw_clip(int count, float *const *w, const void *const *g, float *con
  * ------------------------------------------------------------------------- */
 size_t dstd_mx4_scale_bytes(int rows, int cols); /* 0 for negative sizes */
 
-/* Rows to 4 bits. Of each block, e = the least whole number >= -127 with
+/* Rows to 4 bits (the OCP microscaling format's codes and scales; its example
+ * rule for the exponent, floor(log2 max |x|) - 2, rounds down and saturates, this one
+ * rounds up). Of each block, e = the least whole number >= -127 with
  * max |x| <= 6 2^e; code = x 2^-e to the nearest, ties to the even code (0, 1, 2, 4);
- * value = code 2^e, in fp32 (infinite where |x| >= 3.5 2^126 went up to 2^128). A block that holds an infinity or a NaN has scale
- * NaN and codes 0, so that every result computed from it is NaN.
+ * value = code 2^e, in fp32 (infinite where |x| >= 3.5 2^126 went up to 2^128). A
+ * block that holds an infinity or a NaN has scale NaN and codes 0, so that every
+ * result computed from it is NaN.
  *  x       [rows, cols] of `type`, row stride ld_x >= cols (elements).
  *  q       [rows] rows of codes out, row stride ld_q (bytes).
  *  scale   out (all bytes of blocks past the last too).

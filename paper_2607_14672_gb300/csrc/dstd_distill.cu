@@ -680,11 +680,14 @@ cudaError_t top_logits(const LogitArgs &a, int K, float *top, int32_t *index, cu
 // and q = softmax of its logits:
 //     L_r = sum_k p_k (log p_k - log q_{i_k}),
 //     dL_r / dy_c = factor (q_c - sum_{k: i_k = c} p_k)   (0 where silent).
-// A row is read once and stays on chip: the largest logit and the sum of
-// exp(z - largest), by warps, then over the block (or the cluster that shares the row), then exp(z - m)
-// times a constant. The few columns that the teacher names are written once
-// more, from fp32, so that every gradient is rounded once; entries of the
-// same column are added up in their order.
+// First the largest logit and the sum of exp(z - largest), by warps, then over
+// the block (or the cluster that shares the row), then exp(z - m) times a
+// constant. A row that a warp has stays in its registers in between; a block's is
+// read a second time, from L2 while the rows under way fit there (4096 rows of
+// 32768 bf16: 292 MB read from HBM for 268; 1000 rows of 100000 fp32: 752 for
+// 400). The few columns that the teacher names are written once more, from
+// fp32, so that every gradient is rounded once; entries of the same column are
+// added up in their order.
 // ---------------------------------------------------------------------------
 struct Teacher {
     int at;       // column of this thread's entry, -1: none
@@ -692,7 +695,7 @@ struct Teacher {
     bool silent;
 };
 
-// A row's entries, 32 K' of them by a warp: lane l has entries l, 32 + l, ...; `own` is the warp's share, one a lane.
+// A row's entries, EACH to a lane of a warp: lane l has entries l, 32 + l, ...; at: the column, -1 where it is not used.
 template <int EACH>
 struct Record {
     int at[EACH];
@@ -1125,7 +1128,7 @@ constexpr int kRowThreads = BATCH == 2 ? 2048 : 1280;  // threads on an SM
 
 // Longer rows, or longer records: the last warp of a block has the teacher's entries, the others the row, with the sum
 // of exp(z - m) brought up to each new largest logit m as it comes. HBM bounds it, with the latency of a row's steps
-// between barriers, five rows of 32768 to an SM: 4096 of them in bf16 in 97 us, 5.5 TB/s (held in shared memory, three
+// between barriers, five rows of 32768 to an SM: 4096 of them in bf16 in 98 us, 5.5 TB/s (held in shared memory, three
 // rows to an SM: 121; in registers, two: 157). Without CLUSTER a block has a row to itself and knows it: fewer registers
 // to keep (16384 rows of 3000 bf16: 77 us, with the form for clusters 89).
 template <class T, int THREADS, int BATCH, bool FAST, bool CLUSTER>
@@ -1319,7 +1322,7 @@ cudaError_t distill_rows(const DistillArgs &a, cudaStream_t st) {
     const int blocks = a.y.rows * parts, each = packs / parts;
     // short rows have less to load than to wait for, and want more blocks on an SM (4000 rows of 5000 fp32: 40 us; by a
     // form that could share rows 42, with six of its blocks to an SM 44, with five 52); long ones are read with more loads
-    // under way (4096 of 32768 bf16: 97, with the short ones' form 129)
+    // under way (4096 of 32768 bf16: 98, with the short ones' form 129)
     if (each <= 1280 && blocks > 5 * 152)  // (rows are not shared there)
         return launch_shared<k_distill<T, 256, 2, FAST, false>, 256, 0>(a.y.rows, 1, st, a, 1);
     // few blocks have more threads each

@@ -284,8 +284,8 @@ cudaError_t launch_bin_mx4(const float *t, int B, int N, const LifConst &c, uint
     return cudaGetLastError();
 }
 
-// row sums of the weights' values, one warp per row: a lane adds the whole
-// numbers of its blocks (twice the codes' values, exact) times their powers of two
+// row sums of the weights' values, one warp per row: a lane adds the codes'
+// values of each of its blocks (multiples of 1/2 up to 192: exact) times its power of two
 __global__ void __launch_bounds__(256) k_mx4_rowsum(const uint8_t *__restrict__ w, long long ld,
                                                     const uint8_t *__restrict__ scale, int N, int blocks,
                                                     float *rowsum) {
@@ -321,9 +321,9 @@ cudaError_t launch_mx4_rowsum(const uint8_t *w, long long ld, const uint8_t *sca
 // of both sides in the tiles in which they are kept; one thread copies the scales to TMEM and issues the MMAs, in that
 // order; four warps take the sums out. No operand is converted on the way, so few tokens cost what reading the weights
 // costs: 8 x 16384 into 16384 in 26 us, 5.4 TB/s of codes and scales (about 3 us of it before the first byte). Wide
-// tiles take in 54 bytes a cycle and SM from L2, which bounds them. Where there are few tiles, `parts` blocks of a
-// cluster share K: each leaves its sums in its own shared memory, and each adds up its share of the columns over all, in
-// order (no atomics: the same call gives the same bits).
+// tiles bring 34 KB a stage from L2, which bounds them: 4096 x 16384 into 16384 took 440 us in them, 9.1 GB, 21 TB/s.
+// Where there are few tiles, `parts` blocks of a cluster share K: each leaves its sums in its own shared memory, and each
+// adds up its share of the columns over all, in order (no atomics: the same call gives the same bits).
 // ---------------------------------------------------------------------------
 __device__ unsigned int g_status_mx4 = 0;
 
@@ -598,10 +598,10 @@ __global__ void __launch_bounds__(192) k_mx4_tc(const __grid_constant__ CUtensor
 }
 
 // Large products: a pair of SMs computes 256 x 256, each SM its 128 rows of a and half of b's codes,
-// so that a stage brings 35 KB to an SM for 512 cycles of MMAs (a block of its own, 128 x 128: 34 KB for 128). The
-// scales of b's 256 rows go to both. The pairs stay and take tiles in turn; eight warps take the sums out to
-// registers, from where they are stored while the next tile is computed: two accumulators of this width and the
-// scales do not fit TMEM. The tensor pipe bounds it: 4096 x 16384 into 16384 in 276 us, 8.0 PFLOP/s; 128 x 128
+// so that a stage brings 35 KB to an SM for 391 cycles of MMAs at the 4-bit nominal rate (a block of its own, 128 x 128:
+// 34 KB for half as many). The scales of b's 256 rows go to both. The pairs stay and take tiles in turn; eight warps
+// take the sums out to registers, from where they are stored while the next tile is computed: two accumulators of this
+// width and the scales do not fit TMEM. The tensor pipe bounds it: 4096 x 16384 into 16384 in 276 us, 8.0 PFLOP/s; 128 x 128
 // tiles took 440. With few columns the stores do: 8192 x 32 into 8192 fp32 in 49 us, 5.5 TB/s.
 struct PairCfg {
     static constexpr int SF_BYTES = 2 * kScaleTile * 3;  // of this SM's rows of a, of all of b's
